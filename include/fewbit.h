@@ -248,6 +248,151 @@ FEWBIT_API fewbit_status fewbit_bwd(const fewbit_table *table, const uint32_t *p
                                     fewbit_dtype dtype, void *stream);
 
 /* ------------------------------------------------------------------------- */
+/* Operators next to the activation in a transformer's training step          */
+/*                                                                            */
+/* The activations keep 1-4 bits per element; what else a training step keeps */
+/* is attention's probabilities, the copies around the head norm and the      */
+/* rotation, and the optimizer's moments.  The entry points below recompute   */
+/* the first, fuse the second and hold the third in 8 bits.  (The paper has   */
+/* no counterpart for any of them.)  Same conventions as above: asynchronous  */
+/* on `stream`, no allocation, no synchronisation, a status for every error   */
+/* that the host can see.                                                     */
+/* ------------------------------------------------------------------------- */
+
+/*
+ * A DEVICE tensor of heads: element (b, i, h, e) of a (batch, length, heads,
+ * head_dim) tensor lies at data[b * batch_stride + i * row_stride +
+ * h * head_stride + e].  Strides count elements and may be anything that
+ * keeps every head inside the caller's buffer (a view of a fused projection,
+ * a transposed layout); the elements of one head are contiguous.
+ */
+typedef struct fewbit_heads {
+    void *data;
+    int64_t batch_stride, row_stride, head_stride;
+} fewbit_heads;
+
+/*
+ * RMS norm of every query and key head, then the position rotation, in one
+ * pass.  For a head x of head_dim = D elements at position p:
+ *     u[e] = x[e] * rsqrt(mean(x^2) + eps) * weight[e]           in binary32
+ *     (y[a], y[b]) = (u[a] c - u[b] s, u[a] s + u[b] c)          for each rotated pair j,
+ * with c = cos[p * rotary_dim/2 + j], s = sin[...], and pair j being
+ * (j, j + rotary_dim/2), or (2j, 2j+1) when `interleaved`; elements from
+ * rotary_dim on are not rotated.  y is rounded once to `dtype`.
+ *
+ *   batch, length   tokens (batch * length < 2^31)
+ *   heads, kv_heads query and key heads (0 allowed: that tensor is not touched)
+ *   head_dim        even, 2 .. 256;   rotary_dim  even, 0 .. head_dim
+ *   positions       DEVICE, batch * length int32 (positions_are_64bit: int64),
+ *                   or NULL: token i of a sequence has position i
+ *   table_rows      rows of cos and sin (DEVICE, binary32, contiguous).  A
+ *                   position outside [0, table_rows) makes its token's heads
+ *                   NaN; nothing outside the tables is read.  Without
+ *                   `positions`, table_rows >= length is required.
+ *   q_weight, k_weight  DEVICE, head_dim binary32 values, or NULL for ones.
+ * The struct is HOST memory, read during the call only.
+ * Buffers need the alignment of their element type; 16-byte aligned heads (and
+ * pairs that keep whole 16-byte pieces together) move in wider pieces.
+ */
+typedef struct fewbit_qk_shape {
+    int64_t batch, length;
+    int heads, kv_heads, head_dim, rotary_dim, interleaved;
+    const void *positions;
+    int positions_are_64bit;
+    int64_t table_rows;
+    const float *cos, *sin;
+    const float *q_weight, *k_weight;
+    float eps;
+    fewbit_dtype dtype;
+} fewbit_qk_shape;
+
+/*
+ * q, k -> q_out, k_out; one launch.  An output may alias its input exactly.
+ * Errors: INVALID_ARG (NULL, sizes, eps < 0 or NaN), UNSUPPORTED (head_dim > 256),
+ * TOO_LARGE, ALIGNMENT, CUDA.
+ */
+FEWBIT_API fewbit_status fewbit_qk_norm_rope_fwd(const fewbit_qk_shape *shape, const fewbit_heads *q, const fewbit_heads *k,
+                                                 const fewbit_heads *q_out, const fewbit_heads *k_out, void *stream);
+
+/* Bytes of `workspace` for the backward pass with weight gradients; 0 without a device or for a bad shape. */
+FEWBIT_API size_t fewbit_qk_norm_rope_workspace_bytes(const fewbit_qk_shape *shape);
+
+/*
+ * Gradients of fewbit_qk_norm_rope_fwd: (grad_q_out, grad_k_out) and the
+ * forward pass's inputs q, k -> grad_q, grad_k (may alias grad_*_out exactly),
+ * and the weights' gradients, head_dim binary32 values each (NULL: not wanted).
+ * The norm's factor is recomputed.  With weight gradients: `workspace` (DEVICE,
+ * 16-byte aligned, fewbit_qk_norm_rope_workspace_bytes long), and a second
+ * launch that adds up the partial sums in a fixed order (the same inputs give
+ * the same bits).  Errors as above, ALLOC (workspace too small).
+ */
+FEWBIT_API fewbit_status fewbit_qk_norm_rope_bwd(const fewbit_qk_shape *shape, const fewbit_heads *grad_q_out,
+                                                 const fewbit_heads *grad_k_out, const fewbit_heads *q, const fewbit_heads *k,
+                                                 const fewbit_heads *grad_q, const fewbit_heads *grad_k,
+                                                 float *grad_q_weight, float *grad_k_weight,
+                                                 void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * One AdamW step over many tensors.  For every element, in binary32:
+ *     g  = grad * grad_scale
+ *     m  = beta1 m + (1 - beta1) g
+ *     v  = beta2 v + (1 - beta2) g^2
+ *     p  = p (1 - lr weight_decay) - lr (m / (1 - beta1^step)) / (sqrt(v / (1 - beta2^step)) + eps)
+ * With a master copy, p is read from and written to `master` (binary32) and
+ * `param` receives it rounded to `dtype`; without one, `param` is read.
+ *
+ * Moments of 8 bits (state_bits = 8): a tensor is cut into blocks of 256
+ * consecutive elements.  exp_avg holds m and exp_avg_sq holds sqrt(v), both as
+ * float8 codes (e4m3: sign, 4 bits of exponent, 3 of mantissa; 448 is the
+ * largest), one byte an element, with one binary32 scale a block: value =
+ * code * scale, scale = (largest magnitude of the block) / 448.  The new values
+ * are rounded stochastically: up with the probability of what is cut off, so
+ * that a moment that changes by less than a step still changes on average.
+ * Each product and sum of the moments is rounded to binary32 by itself, so the
+ * codes follow from the inputs and the seed alone.
+ * The 16 + 16 random bits of an element are a hash of `seed` and of its place
+ * in the call (tensors in order, each taking a whole number of blocks); give
+ * every step its own seed.  A positive second moment never becomes zero.  A
+ * block with a non-finite value gets a NaN scale: it reads back as NaN.  A
+ * block whose largest magnitude is below 2^-126 reads back as zero.
+ * Moments of 32 bits: exp_avg = m, exp_avg_sq = v, binary32; no scales.
+ *
+ * tensors: HOST array of `count` descriptions of DEVICE buffers; grads: HOST
+ * array of `count` DEVICE pointers (n elements of `dtype` each).  Both are read
+ * during the call only.  Any n, zero included.  Buffers need the alignment of
+ * their element type; tensors whose binary32 buffers are 32-byte aligned, 16-bit
+ * ones 16-byte and codes 8-byte move in wider pieces.  The tensors of
+ * a call must not overlap.  One launch for up to 400 tensors.
+ * grad_scale_device: DEVICE binary32 value that multiplies every gradient (1 /
+ * the loss scale, a clipping factor), or NULL.
+ */
+#define FEWBIT_ADAMW_BLOCK 256
+typedef struct fewbit_adamw_tensor {
+    void *param;
+    void *exp_avg, *exp_avg_sq;
+    float *exp_avg_scale, *exp_avg_sq_scale;   /* state_bits 8: ceil(n / 256) values each; else NULL */
+    float *master;                             /* NULL: none */
+    uint64_t n;
+} fewbit_adamw_tensor;
+
+typedef struct fewbit_adamw_options {
+    double lr, beta1, beta2, eps, weight_decay;
+    int64_t step;                              /* 1 for the first step */
+    const float *grad_scale_device;
+    uint32_t seed;
+    int state_bits;                            /* 8 or 32 */
+    fewbit_dtype dtype;                        /* of param and grad */
+} fewbit_adamw_options;
+
+/*
+ * Errors: INVALID_ARG (NULL, step < 1, a beta outside [0, 1), eps < 0, lr or weight_decay
+ * negative or not finite, some tensors with a master copy and some without,
+ * a master copy with FEWBIT_F32), TOO_LARGE (a tensor of more than 2^38 elements), ALIGNMENT, CUDA.
+ */
+FEWBIT_API fewbit_status fewbit_adamw_step(const fewbit_adamw_tensor *tensors, const void *const *grads, int count,
+                                           const fewbit_adamw_options *options, void *stream);
+
+/* ------------------------------------------------------------------------- */
 /* Hot path on HOST buffers                                                   */
 /* ------------------------------------------------------------------------- */
 
