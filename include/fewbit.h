@@ -333,6 +333,72 @@ FEWBIT_API fewbit_status fewbit_qk_norm_rope_bwd(const fewbit_qk_shape *shape, c
                                                  void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Attention, out = softmax(scale * q k^T + mask) v for each head, and its
+ * gradients.  The probabilities are never stored: the forward pass keeps the
+ * logarithm of each row's sum (lse, binary32, natural logarithm), from which
+ * the backward pass recomputes them.
+ *
+ *   dtype           FEWBIT_BF16 or FEWBIT_F16 (products with binary32 sums on
+ *                   the tensor cores; the probabilities and their gradients
+ *                   are rounded to `dtype` as operands of the second products)
+ *   heads, kv_heads query head h reads key head h / (heads / kv_heads)
+ *   head_dim        a multiple of 8, 8 .. 128
+ *   causal          row i of a sequence sees keys j <= i + k_len - q_len (the
+ *                   last row sees every key)
+ *   q_offsets, k_offsets   NULL: `batch` sequences of q_len rows and k_len keys.
+ *                   Otherwise DEVICE int32 arrays of batch + 1 non-decreasing
+ *                   values: sequence b is rows [q_offsets[b], q_offsets[b+1])
+ *                   of q and keys [k_offsets[b], k_offsets[b+1]) of k and v,
+ *                   in tensors of q_rows and k_rows rows (batch_stride is not
+ *                   used); q_len and k_len are then upper bounds of the
+ *                   sequences' lengths.  Rows of no sequence are not written.
+ *                   Offsets are clamped to [0, q_rows] / [0, k_rows], lengths to
+ *                   [0, q_len] / [0, k_len].
+ *   scale           finite, > 0
+ * lse: (batch, heads, q_len), or (heads, q_rows) for packed sequences.
+ * A row that sees no key has out = 0, lse = -inf and zero gradients.
+ * Pointers must be 16-byte aligned, strides multiples of 8 elements (of
+ * dimensions longer than 1).  Keys past the end of a sequence are not part of
+ * any sum, whatever the memory there holds.  A non-finite value inside a
+ * sequence's k or v can spread to rows that the causal mask hides it from.
+ */
+typedef struct fewbit_attention_shape {
+    int batch, heads, kv_heads, head_dim;
+    int64_t q_len, k_len;
+    int64_t q_rows, k_rows;
+    const int32_t *q_offsets, *k_offsets;
+    int causal;
+    float scale;
+    fewbit_dtype dtype;
+} fewbit_attention_shape;
+
+/* Errors: INVALID_ARG, UNSUPPORTED (head_dim, dtype), TOO_LARGE, ALIGNMENT, CUDA. */
+FEWBIT_API fewbit_status fewbit_attention_fwd(const fewbit_attention_shape *shape, const fewbit_heads *q, const fewbit_heads *k,
+                                              const fewbit_heads *v, const fewbit_heads *out, float *lse, void *stream);
+
+/* Bytes of `workspace` for the backward pass (one binary32 value for each row and head); 0 for a bad shape. */
+FEWBIT_API size_t fewbit_attention_workspace_bytes(const fewbit_attention_shape *shape);
+
+/*
+ * (grad_out; q, k, v, out, lse of the forward pass) -> grad_q, grad_k, grad_v,
+ * every element of every sequence written.  The gradients of a key head that
+ * several query heads share are summed in binary32, in a fixed order: the same
+ * inputs give the same bits.  Two launches.  workspace: DEVICE, 16-byte aligned.
+ */
+FEWBIT_API fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *shape, const fewbit_heads *grad_out,
+                                              const fewbit_heads *q, const fewbit_heads *k, const fewbit_heads *v,
+                                              const fewbit_heads *out, const float *lse,
+                                              const fewbit_heads *grad_q, const fewbit_heads *grad_k, const fewbit_heads *grad_v,
+                                              void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Diagnostic: *count (HOST) receives how often a wait inside the attention kernels gave up on the current
+ * device since the library was loaded (each wait is limited to two seconds; the results of such a launch are
+ * not valid).  Always 0 unless the device or the program is broken.  Synchronises the device.
+ */
+FEWBIT_API fewbit_status fewbit_attention_timeout_count(uint64_t *count);
+
+/*
  * One AdamW step over many tensors.  For every element, in binary32:
  *     g  = grad * grad_scale
  *     m  = beta1 m + (1 - beta1) g

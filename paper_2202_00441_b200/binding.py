@@ -90,12 +90,18 @@ def load_library():
     lib.fewbit_get_option.argtypes = [ci]
     lib.fewbit_tail_warp_count.restype = ci
     lib.fewbit_tail_warp_count.argtypes = [ctypes.POINTER(ctypes.c_uint64), ci]
-    for name in ("fewbit_qk_norm_rope_fwd", "fewbit_qk_norm_rope_bwd", "fewbit_adamw_step"):
+    for name in ("fewbit_qk_norm_rope_fwd", "fewbit_qk_norm_rope_bwd", "fewbit_attention_fwd", "fewbit_attention_bwd",
+                 "fewbit_attention_timeout_count", "fewbit_adamw_step"):
         getattr(lib, name).restype = ci
     lib.fewbit_qk_norm_rope_fwd.argtypes = [vp] * 6
     lib.fewbit_qk_norm_rope_bwd.argtypes = [vp] * 10 + [sz, vp]
     lib.fewbit_qk_norm_rope_workspace_bytes.restype = sz
     lib.fewbit_qk_norm_rope_workspace_bytes.argtypes = [vp]
+    lib.fewbit_attention_fwd.argtypes = [vp] * 7
+    lib.fewbit_attention_bwd.argtypes = [vp] * 11 + [sz, vp]
+    lib.fewbit_attention_workspace_bytes.restype = sz
+    lib.fewbit_attention_workspace_bytes.argtypes = [vp]
+    lib.fewbit_attention_timeout_count.argtypes = [ctypes.POINTER(ctypes.c_uint64)]
     lib.fewbit_adamw_step.argtypes = [vp, vp, ci, vp, vp]
     lib.fewbit_f32_activation_scan.restype = ci
     lib.fewbit_f32_activation_scan.argtypes = [ci, ctypes.c_uint64, ctypes.c_uint64, vp, vp]

@@ -16,7 +16,9 @@ OBJ_DIR = os.path.join(PKG, "build")
 SOURCES = [("fewbit_kernels.cu", "fewbit_kernels", []), ("fewbit_host.cu", "fewbit_host", []),
            ("fewbit_static.cu", "fewbit_static", []), ("fewbit_scan.cu", "fewbit_scan", []), ("fewbit_queue.cu", "fewbit_queue", []),
            ("fewbit_table.cpp", "fewbit_table", []), ("fewbit_adamw.cu", "fewbit_adamw", []),
-           ("fewbit_qknorm.cu", "fewbit_qknorm", [])]
+           ("fewbit_qknorm.cu", "fewbit_qknorm", []), ("fewbit_attention.cu", "fewbit_attention", []),
+           ("fewbit_attention_inst.cu", "fewbit_attention_bf16", ["-DFEWBIT_ATTN_F16=0"]),
+           ("fewbit_attention_inst.cu", "fewbit_attention_f16", ["-DFEWBIT_ATTN_F16=1"])]
 SOURCES += [("fewbit_fwd_inst.cu", f"fewbit_fwd_act{a}", [f"-DFEWBIT_ACT_ID={a}"]) for a in range(9)]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

@@ -1,0 +1,215 @@
+// Entry points of attention: argument checks, tensor maps, launches.
+#include "fewbit_attention.cuh"
+#include "fewbit_attention_launch.h"
+
+#include <cudaTypedefs.h>
+
+#include <atomic>
+
+namespace fewbit {
+namespace {
+
+using attn::Params;
+
+__device__ unsigned int g_attention_timeouts;
+
+fewbit_status cuda_status(cudaError_t err) {
+    if (err == cudaSuccess) return FEWBIT_OK;
+    t_last_cuda_error = static_cast<int>(err);
+    return FEWBIT_ERR_CUDA;
+}
+
+PFN_cuTensorMapEncodeTiled_v12000 encode_function(cudaError_t *err) {
+    static std::atomic<void *> cached{nullptr};
+    void *fn = cached.load(std::memory_order_acquire);
+    *err = cudaSuccess;
+    if (fn == nullptr) {
+        cudaDriverEntryPointQueryResult found;
+        *err = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found);
+        if (*err == cudaSuccess && (found != cudaDriverEntryPointSuccess || fn == nullptr)) *err = cudaErrorNotSupported;
+        if (*err != cudaSuccess) return nullptr;
+        cached.store(fn, std::memory_order_release);
+    }
+    return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
+}
+
+// Map of a (batch, rows, heads, dim) tensor as (dim, rows, heads, batch), read in boxes of 64 elements x 128 rows of one
+// head; places past the tensor's rows or dim read as zero.
+fewbit_status encode(CUtensorMap *map, const fewbit_heads *t, const fewbit_attention_shape *s, int64_t rows, int heads, int64_t batch) {
+    cudaError_t err;
+    const auto fn = encode_function(&err);
+    if (fn == nullptr) return cuda_status(err);
+    const cuuint64_t dense = static_cast<cuuint64_t>(s->head_dim) * 2;
+    cuuint64_t dims[4] = {static_cast<cuuint64_t>(s->head_dim), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(batch)};
+    // the stride of a dimension of length 1 is never used
+    cuuint64_t strides[3] = {rows > 1 ? static_cast<cuuint64_t>(t->row_stride) * 2 : dense, heads > 1 ? static_cast<cuuint64_t>(t->head_stride) * 2 : dense,
+                             batch > 1 ? static_cast<cuuint64_t>(t->batch_stride) * 2 : dense};
+    cuuint32_t box[4] = {64, static_cast<cuuint32_t>(attn::kTile), 1, 1}, steps[4] = {1, 1, 1, 1};
+    const CUresult r = fn(map, s->dtype == FEWBIT_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, t->data, dims, strides, box,
+                          steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        t_last_cuda_error = static_cast<int>(r);
+        return FEWBIT_ERR_CUDA;
+    }
+    return FEWBIT_OK;
+}
+
+struct Sizes {
+    int64_t q_rows, k_rows;           // rows of the tensors
+    int64_t batch;                    // of the tensors
+    bool packed;
+};
+
+fewbit_status check_shape(const fewbit_attention_shape *s, Sizes *z) {
+    if (s == nullptr || !valid_dtype(s->dtype) || s->batch < 0 || s->heads < 0 || s->kv_heads < 0 || s->head_dim < 1 || s->q_len < 0 || s->k_len < 0 ||
+        !(s->scale > 0) || !std::isfinite(s->scale) || (s->q_offsets == nullptr) != (s->k_offsets == nullptr))
+        return FEWBIT_ERR_INVALID_ARG;
+    if (s->heads > 0 && (s->kv_heads == 0 || s->heads % s->kv_heads != 0)) return FEWBIT_ERR_INVALID_ARG;
+    z->packed = s->q_offsets != nullptr;
+    if (z->packed && (s->q_rows < 0 || s->k_rows < 0 || s->q_len > s->q_rows || s->k_len > s->k_rows)) return FEWBIT_ERR_INVALID_ARG;
+    if (s->dtype == FEWBIT_F32 || s->head_dim % 8 != 0 || s->head_dim > 128) return FEWBIT_ERR_UNSUPPORTED;
+    if ((reinterpret_cast<uintptr_t>(s->q_offsets) | reinterpret_cast<uintptr_t>(s->k_offsets)) & 3) return FEWBIT_ERR_ALIGNMENT;
+    z->q_rows = z->packed ? s->q_rows : s->q_len;
+    z->k_rows = z->packed ? s->k_rows : s->k_len;
+    z->batch = z->packed ? 1 : s->batch;
+    // tiles, heads and sequences are counted in 31 bits, rows too
+    const int64_t most = INT32_MAX;
+    const int64_t longest = s->q_len > s->k_len ? s->q_len : s->k_len;
+    if (z->q_rows > most - 1024 || z->k_rows > most - 1024 ||
+        (longest / attn::kTile + 1) > most / (static_cast<int64_t>(s->heads) + 1) / (static_cast<int64_t>(s->batch) + 1))
+        return FEWBIT_ERR_TOO_LARGE;
+    return FEWBIT_OK;
+}
+
+fewbit_status check_tensor(const fewbit_heads *t, int64_t rows, int heads, int64_t batch) {
+    if (rows == 0 || heads == 0 || batch == 0) return FEWBIT_OK;
+    if (t == nullptr || t->data == nullptr) return FEWBIT_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(t->data) & 15) return FEWBIT_ERR_ALIGNMENT;
+    const int64_t strides[3] = {batch > 1 ? t->batch_stride : 8, rows > 1 ? t->row_stride : 8, heads > 1 ? t->head_stride : 8};
+    for (int64_t x : strides) {
+        if (x % 8 != 0) return FEWBIT_ERR_ALIGNMENT;
+        if (x <= 0 || x >= (int64_t{1} << 39)) return FEWBIT_ERR_UNSUPPORTED;   // the tensor maps hold 40 bits of bytes, no sign
+    }
+    return FEWBIT_OK;
+}
+
+attn::Rows rows_of(const fewbit_heads *t) { return t == nullptr ? attn::Rows{} : attn::Rows{t->data, t->batch_stride, t->row_stride, t->head_stride}; }
+
+fewbit_status fill(const fewbit_attention_shape *s, const Sizes &z, Params *p) {
+    p->q_offsets = s->q_offsets;
+    p->k_offsets = s->k_offsets;
+    p->q_rows = z.q_rows;
+    p->k_rows = z.k_rows;
+    p->batch = s->batch;
+    p->heads = s->heads;
+    p->kv_heads = s->kv_heads;
+    p->group = s->heads / s->kv_heads;
+    p->dim = s->head_dim;
+    p->q_len = static_cast<int>(s->q_len);
+    p->k_len = static_cast<int>(s->k_len);
+    p->causal = s->causal != 0;
+    p->scale = s->scale;
+    p->scale_log2 = s->scale * 1.4426950408889634f;
+    static std::atomic<unsigned int *> cached[64];                    // per device
+    int dev = 0;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err != cudaSuccess) return cuda_status(err);
+    unsigned int *at = dev < 64 ? cached[dev].load(std::memory_order_acquire) : nullptr;
+    if (at == nullptr) {
+        err = cudaGetSymbolAddress(reinterpret_cast<void **>(&at), g_attention_timeouts);
+        if (err != cudaSuccess) return cuda_status(err);
+        if (dev < 64) cached[dev].store(at, std::memory_order_release);
+    }
+    p->timeouts = at;
+    return FEWBIT_OK;
+}
+
+fewbit_status run(attn::Kernel which, const fewbit_attention_shape *s, Params &p, int64_t tiles, int heads, void *stream) {
+    p.tiles = static_cast<int>(tiles);
+    const unsigned grid = static_cast<unsigned>(tiles * heads * s->batch);
+    if (grid == 0) return FEWBIT_OK;
+    const cudaError_t err = (s->dtype == FEWBIT_F16 ? attn::launch_f16 : attn::launch_bf16)(which, s->head_dim > 64, p, grid, static_cast<cudaStream_t>(stream));
+    if (err == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
+    return cuda_status(err);
+}
+
+}  // namespace
+}  // namespace fewbit
+
+extern "C" {
+
+fewbit_status fewbit_attention_fwd(const fewbit_attention_shape *s, const fewbit_heads *q, const fewbit_heads *k, const fewbit_heads *v,
+                                   const fewbit_heads *out, float *lse, void *stream) {
+    using namespace fewbit;
+    Sizes z;
+    if (const fewbit_status st = check_shape(s, &z); st != FEWBIT_OK) return st;
+    if (s->batch == 0 || s->heads == 0 || z.q_rows == 0 || s->q_len == 0) return FEWBIT_OK;
+    for (const fewbit_heads *t : {q, out})
+        if (const fewbit_status st = check_tensor(t, z.q_rows, s->heads, z.batch); st != FEWBIT_OK) return st;
+    for (const fewbit_heads *t : {k, v})
+        if (const fewbit_status st = check_tensor(t, z.k_rows, s->kv_heads, z.batch); st != FEWBIT_OK) return st;
+    if (lse == nullptr) return FEWBIT_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(lse) & 3) return FEWBIT_ERR_ALIGNMENT;
+    Params p = {};
+    fewbit_status st = fill(s, z, &p);
+    if (st == FEWBIT_OK) st = encode(&p.q, q, s, z.q_rows, s->heads, z.batch);
+    if (st == FEWBIT_OK && z.k_rows > 0) st = encode(&p.k, k, s, z.k_rows, s->kv_heads, z.batch);
+    if (st == FEWBIT_OK && z.k_rows > 0) st = encode(&p.v, v, s, z.k_rows, s->kv_heads, z.batch);
+    if (st != FEWBIT_OK) return st;
+    p.out = rows_of(out);
+    p.lse = lse;
+    return run(attn::Kernel::forward, s, p, (s->q_len + 2 * attn::kTile - 1) / (2 * attn::kTile), s->heads, stream);
+}
+
+size_t fewbit_attention_workspace_bytes(const fewbit_attention_shape *s) {
+    using namespace fewbit;
+    Sizes z;
+    if (check_shape(s, &z) != FEWBIT_OK) return 0;
+    return static_cast<size_t>(z.batch) * s->heads * z.q_rows * sizeof(float);
+}
+
+fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *s, const fewbit_heads *grad_out, const fewbit_heads *q, const fewbit_heads *k,
+                                   const fewbit_heads *v, const fewbit_heads *out, const float *lse, const fewbit_heads *grad_q,
+                                   const fewbit_heads *grad_k, const fewbit_heads *grad_v, void *workspace, size_t workspace_bytes, void *stream) {
+    using namespace fewbit;
+    Sizes z;
+    if (const fewbit_status st = check_shape(s, &z); st != FEWBIT_OK) return st;
+    if (s->batch == 0 || s->heads == 0 || (z.q_rows == 0 && z.k_rows == 0)) return FEWBIT_OK;
+    for (const fewbit_heads *t : {grad_out, q, out, grad_q})
+        if (const fewbit_status st = check_tensor(t, z.q_rows, s->heads, z.batch); st != FEWBIT_OK) return st;
+    for (const fewbit_heads *t : {k, v, grad_k, grad_v})
+        if (const fewbit_status st = check_tensor(t, z.k_rows, s->kv_heads, z.batch); st != FEWBIT_OK) return st;
+    const bool some = z.q_rows > 0;
+    if (some && (lse == nullptr || workspace == nullptr)) return FEWBIT_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(lse) & 3) || (reinterpret_cast<uintptr_t>(workspace) & 15)) return FEWBIT_ERR_ALIGNMENT;
+    if (workspace_bytes < fewbit_attention_workspace_bytes(s)) return FEWBIT_ERR_ALLOC;
+    Params p = {};
+    fewbit_status st = fill(s, z, &p);
+    if (st == FEWBIT_OK && some) st = encode(&p.q, q, s, z.q_rows, s->heads, z.batch);
+    if (st == FEWBIT_OK && some) st = encode(&p.g, grad_out, s, z.q_rows, s->heads, z.batch);
+    if (st == FEWBIT_OK && z.k_rows > 0) st = encode(&p.k, k, s, z.k_rows, s->kv_heads, z.batch);
+    if (st == FEWBIT_OK && z.k_rows > 0) st = encode(&p.v, v, s, z.k_rows, s->kv_heads, z.batch);
+    if (st != FEWBIT_OK) return st;
+    p.o = rows_of(out);
+    p.go = rows_of(grad_out);
+    p.dq = rows_of(grad_q);
+    p.dk = rows_of(grad_k);
+    p.dv = rows_of(grad_v);
+    p.lse = const_cast<float *>(lse);
+    p.delta = static_cast<float *>(workspace);
+    st = run(attn::Kernel::dq, s, p, (s->q_len + attn::kTile - 1) / attn::kTile, s->heads, stream);
+    if (st != FEWBIT_OK) return st;
+    return run(attn::Kernel::dkv, s, p, (s->k_len + attn::kTile - 1) / attn::kTile, s->kv_heads, stream);
+}
+
+fewbit_status fewbit_attention_timeout_count(uint64_t *count) {
+    using namespace fewbit;
+    if (count == nullptr) return FEWBIT_ERR_INVALID_ARG;
+    unsigned int n = 0;
+    const cudaError_t err = cudaMemcpyFromSymbol(&n, g_attention_timeouts, sizeof(n));
+    *count = n;
+    return cuda_status(err);
+}
+
+}  // extern "C"

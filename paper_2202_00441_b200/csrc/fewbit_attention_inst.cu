@@ -1,0 +1,44 @@
+// The attention kernels for one 16-bit type (FEWBIT_ATTN_F16: binary16, else bfloat16).
+#include "fewbit_attention.cuh"
+#include "fewbit_attention_launch.h"
+
+namespace fewbit {
+bool pdl_enabled();
+
+namespace attn {
+namespace {
+
+#if FEWBIT_ATTN_F16
+using T = __half;
+#else
+using T = __nv_bfloat16;
+#endif
+
+template <typename K>
+cudaError_t launch(K kernel, int smem, const Params &p, unsigned grid, cudaStream_t st) {
+    // per device, so set on every call: a host-side table write, no synchronisation
+    const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (err != cudaSuccess) return err;
+    return launch_pdl(kernel, grid, kThreadsAttn, smem, st, pdl_enabled(), p);
+}
+
+}  // namespace
+
+#if FEWBIT_ATTN_F16
+cudaError_t launch_f16(
+#else
+cudaError_t launch_bf16(
+#endif
+    Kernel which, bool wide, const Params &p, unsigned grid, cudaStream_t st) {
+    switch (which) {
+    case Kernel::forward:
+        return wide ? launch(attention_fwd_kernel<T, 128>, fwd_smem<128>(), p, grid, st) : launch(attention_fwd_kernel<T, 64>, fwd_smem<64>(), p, grid, st);
+    case Kernel::dq:
+        return wide ? launch(attention_dq_kernel<T, 128>, dq_smem<128>(), p, grid, st) : launch(attention_dq_kernel<T, 64>, dq_smem<64>(), p, grid, st);
+    default:
+        return wide ? launch(attention_dkv_kernel<T, 128>, dkv_smem<128>(), p, grid, st) : launch(attention_dkv_kernel<T, 64>, dkv_smem<64>(), p, grid, st);
+    }
+}
+
+}  // namespace attn
+}  // namespace fewbit

@@ -1,0 +1,180 @@
+// The sm_100a instructions behind the attention kernels: mbarriers, TMA tile loads, tensor memory and
+// tcgen05.mma with one issuing thread.  16-bit operands, binary32 accumulators.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <cstdint>
+
+namespace fewbit {
+namespace tc {
+
+__device__ __forceinline__ uint32_t smem_address(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+
+// ---- mbarriers ------------------------------------------------------------------------------------
+__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" :: "r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void barrier_arrive(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(bar) : "memory");
+}
+__device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    return done != 0;
+}
+__device__ __forceinline__ uint64_t now_ns() {
+    uint64_t t;
+    asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+    return t;
+}
+
+// No wait is endless: after this long a wait gives up, the CTA's other waits follow, and the kernel winds up.
+constexpr uint64_t kWaitLimitNs = 2000000000ull;
+
+// Waits of a whole warp (every lane gets the same answer).  false: given up; `stop` (shared memory) is set.
+static __device__ __noinline__ bool barrier_wait_slow(uint32_t bar, uint32_t parity, volatile int *stop, unsigned int *timeouts) {
+    const uint64_t t0 = now_ns();
+    for (;;) {
+        for (int i = 0; i < 64; ++i)
+            if (barrier_try(bar, parity)) return true;
+        if (stop != nullptr && *stop != 0) return false;
+        if (now_ns() - t0 > kWaitLimitNs) {
+            if (stop != nullptr) *stop = 1;
+            atomicAdd(timeouts, 1u);
+            return false;
+        }
+    }
+}
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, volatile int *stop, unsigned int *timeouts) {
+    const bool ok = barrier_try(bar, parity) || barrier_wait_slow(bar, parity, stop, timeouts);
+    return __all_sync(0xffffffffu, ok);
+}
+
+// ---- TMA ------------------------------------------------------------------------------------------
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) {
+    asm volatile("prefetch.tensormap [%0];" :: "l"(map) : "memory");
+}
+// (x, row, head, batch) box of the map's size to shared memory; x is a multiple of 64 elements (128 bytes).
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, int x, int row, int head, int batch, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2,%3,%4,%5}], [%6];"
+                 :: "r"(dst), "l"(map), "r"(x), "r"(row), "r"(head), "r"(batch), "r"(bar) : "memory");
+}
+
+// ---- tensor memory --------------------------------------------------------------------------------
+__device__ __forceinline__ void tmem_alloc(uint32_t slot, uint32_t columns) {        // one whole warp
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" :: "r"(slot), "r"(columns) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+}
+__device__ __forceinline__ void tmem_free(uint32_t base, uint32_t columns) {
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" :: "r"(base), "r"(columns) : "memory");
+}
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// 32 columns of this thread's lane
+__device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t *r) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+                   "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+                   "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+                 : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t *r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+                 "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+                 :: "r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+                    "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]),
+                    "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]),
+                    "r"(r[30]), "r"(r[31])
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t *r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+                 :: "r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+                    "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+                 : "memory");
+}
+
+// ---- tcgen05.mma ----------------------------------------------------------------------------------
+// Shared-memory tiles hold rows of 64 elements (128 bytes) in the 128-byte swizzle, 128 rows = 16 KB; a tile of
+// 128 columns is two of them.  The same bytes serve as an operand whose contraction runs along the row (K-major)
+// and as one whose contraction runs down the rows (MN-major).
+constexpr uint32_t kHalfTile = 128 * 128;       // bytes of 128 rows x 64 elements
+__device__ __forceinline__ uint64_t descriptor(uint32_t address, uint32_t leading, uint32_t stride) {
+    return static_cast<uint64_t>((address >> 4) & 0x3fffu) | static_cast<uint64_t>(leading >> 4) << 16 |
+           static_cast<uint64_t>(stride >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+__device__ __forceinline__ uint64_t k_major(uint32_t address) { return descriptor(address, 16, 1024); }       // groups of 8 rows: 1 KB apart
+__device__ __forceinline__ uint64_t mn_major(uint32_t address) { return descriptor(address, kHalfTile, 1024); } // 64-element blocks: one half tile apart
+
+template <typename T> struct Format;
+template <> struct Format<__half> { static constexpr uint32_t value = 0; };
+template <> struct Format<__nv_bfloat16> { static constexpr uint32_t value = 1; };
+// M = 128, N, binary32 accumulator; b_mn: B is MN-major
+template <typename T>
+__host__ __device__ constexpr uint32_t instruction(uint32_t n, bool b_mn) {
+    return 1u << 4 | Format<T>::value << 7 | Format<T>::value << 10 | (b_mn ? 1u << 16 : 0u) | (n >> 3) << 17 | (128u >> 4) << 24;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(accumulate)) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(accumulate)) : "memory");
+}
+// the barrier's phase ends when every MMA issued so far by this thread has finished
+__device__ __forceinline__ void commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+}
+
+// D (128 x 128) = A B^T over DIM: both tiles K-major
+template <typename T, int DIM>
+__device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b) {
+    constexpr uint32_t idesc = instruction<T>(128, false);
+#pragma unroll
+    for (int k = 0; k < DIM / 16; ++k) {
+        const uint32_t off = (k / 4) * kHalfTile + (k % 4) * 32;
+        mma_ss(d, k_major(a + off), k_major(b + off), idesc, k > 0);
+    }
+}
+// D (128 x DIM) (+)= A B: A (128 x 128, 16 bits) in tensor memory, 16 columns of its contraction in 8 TMEM columns,
+// the second 64 of them at `a2`; B's rows are the contraction
+template <typename T, int DIM>
+__device__ __forceinline__ void product_columns(uint32_t d, uint32_t a, uint32_t a2, uint32_t b, bool accumulate) {
+    constexpr uint32_t idesc = instruction<T>(DIM, true);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        mma_ts(d, k < 4 ? a + 8 * k : a2 + 8 * (k - 4), mn_major(b + k * 2048), idesc, accumulate || k > 0);
+}
+
+template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float lo, float hi) {
+    uint32_t d;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi) {
+    uint32_t d;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+    return d;
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+}  // namespace tc
+}  // namespace fewbit

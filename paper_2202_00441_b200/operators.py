@@ -1,6 +1,6 @@
 """ctypes binding of the operators next to the activation in a transformer's training step: the norm of
-query and key heads with the position rotation, and AdamW over many tensors.  Argument marshalling only; the
-arithmetic is in include/fewbit.h."""
+query and key heads with the position rotation, attention, and AdamW over many tensors.  Argument marshalling
+only; the arithmetic is in include/fewbit.h."""
 from __future__ import annotations
 
 import contextlib
@@ -23,6 +23,13 @@ class _QkShape(ctypes.Structure):
                 ("positions", ctypes.c_void_p), ("positions_are_64bit", ctypes.c_int), ("table_rows", ctypes.c_int64),
                 ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
                 ("eps", ctypes.c_float), ("dtype", ctypes.c_int)]
+
+
+class _AttentionShape(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int), ("heads", ctypes.c_int), ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("q_len", ctypes.c_int64), ("k_len", ctypes.c_int64), ("q_rows", ctypes.c_int64), ("k_rows", ctypes.c_int64),
+                ("q_offsets", ctypes.c_void_p), ("k_offsets", ctypes.c_void_p), ("causal", ctypes.c_int),
+                ("scale", ctypes.c_float), ("dtype", ctypes.c_int)]
 
 
 class _AdamWTensor(ctypes.Structure):
@@ -152,6 +159,95 @@ def fewbit_qk_norm_rope_bwd(grad_q_out: torch.Tensor, grad_k_out: torch.Tensor, 
         _check(lib.fewbit_qk_norm_rope_bwd(ctypes.byref(s), *map(ctypes.byref, hs), *dw_ptr, None if ws is None else ws.data_ptr(),
                                            ws_bytes, _stream_ptr(stream, dev)), "fewbit_qk_norm_rope_bwd")
     return grad_q, grad_k, dw[0], dw[1]
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# attention
+# ---------------------------------------------------------------------------------------------------------------
+
+def _attention_shape(q, k, v, causal, scale, q_offsets, k_offsets, max_q_len, max_k_len) -> _AttentionShape:
+    packed = q_offsets is not None
+    if packed != (k_offsets is not None) or packed != (max_q_len is not None) or packed != (max_k_len is not None):
+        raise ValueError("packed sequences need q_offsets, k_offsets, max_q_len and max_k_len, others none of them")
+    dims = 3 if packed else 4
+    if q.dim() != dims or k.dim() != dims or k.shape != v.shape or q.shape[-1] != k.shape[-1] or (not packed and q.shape[0] != k.shape[0]):
+        raise ValueError("q, k and v must be (batch, length, heads, head_dim) tensors, or (rows, heads, head_dim) for packed "
+                         "sequences; k and v of one shape, head_dim the same for all")
+    dev = q.device
+    if q.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("attention takes bfloat16 or float16 tensors")
+    _need(q, "q", dev), _need(k, "k", dev, q.dtype), _need(v, "v", dev, q.dtype)
+    h, hk, d = q.shape[-2], k.shape[-2], q.shape[-1]
+    scale = d ** -0.5 if scale is None else scale
+    if not packed:
+        return _AttentionShape(q.shape[0], h, hk, d, q.shape[1], k.shape[1], 0, 0, None, None, int(bool(causal)), scale, _DTYPES[q.dtype])
+    for o, name in ((q_offsets, "q_offsets"), (k_offsets, "k_offsets")):
+        if _need(o, name, dev, torch.int32).dim() != 1 or o.numel() < 1 or o.numel() != q_offsets.numel() or not o.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous vector of batch + 1 int32 values")
+    return _AttentionShape(q_offsets.numel() - 1, h, hk, d, min(max_q_len, q.shape[0]), min(max_k_len, k.shape[0]), q.shape[0], k.shape[0],
+                           q_offsets.data_ptr(), k_offsets.data_ptr(), int(bool(causal)), scale, _DTYPES[q.dtype])
+
+
+def fewbit_attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool = False, scale: Optional[float] = None,
+                         q_offsets: Optional[torch.Tensor] = None, k_offsets: Optional[torch.Tensor] = None,
+                         max_q_len: Optional[int] = None, max_k_len: Optional[int] = None,
+                         stream: Optional[torch.cuda.Stream] = None):
+    """softmax(scale q k^T) v for every head; returns (out, lse).
+
+    q: (batch, q_len, heads, head_dim), k and v: (batch, k_len, kv_heads, head_dim), bfloat16 or float16, head_dim a multiple
+    of 8 up to 128, any strides that are multiples of 8 with contiguous heads; query head h reads key head
+    h // (heads // kv_heads).  ``causal``: row i sees keys up to i + k_len - q_len.  ``scale``: head_dim ** -0.5.
+    Packed sequences: q (rows, heads, head_dim), k and v (key rows, ...), with int32 ``q_offsets`` and ``k_offsets`` on the
+    device (batch + 1 values each) and the longest sequence's lengths ``max_q_len`` and ``max_k_len``.
+    lse: float32 (batch, heads, q_len), or (heads, rows) when packed: the logarithm of each row's sum of exponentials,
+    -inf for a row that sees no key (whose out is 0)."""
+    s = _attention_shape(q, k, v, causal, scale, q_offsets, k_offsets, max_q_len, max_k_len)
+    packed = q_offsets is not None
+    with _current(q.device), _on(stream, q, k, v, q_offsets, k_offsets):
+        # rows of no sequence are not written by the library: they are zero here
+        out = (torch.zeros if packed else torch.empty)(q.shape, dtype=q.dtype, device=q.device)
+        lse = torch.full((q.shape[1], q.shape[0]), -float("inf"), dtype=torch.float32, device=q.device) if packed else \
+            torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
+        hs = [_heads(t, name) for t, name in ((q, "q"), (k, "k"), (v, "v"), (out, "out"))]
+        _check(load_library().fewbit_attention_fwd(ctypes.byref(s), *map(ctypes.byref, hs), lse.data_ptr(), _stream_ptr(stream, q.device)),
+               "fewbit_attention_fwd")
+    return out, lse
+
+
+def fewbit_attention_bwd(grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                         lse: torch.Tensor, *, causal: bool = False, scale: Optional[float] = None,
+                         q_offsets: Optional[torch.Tensor] = None, k_offsets: Optional[torch.Tensor] = None,
+                         max_q_len: Optional[int] = None, max_k_len: Optional[int] = None,
+                         stream: Optional[torch.cuda.Stream] = None):
+    """Gradients (grad_q, grad_k, grad_v) of ``fewbit_attention_fwd`` from its inputs and outputs and ``grad_out``; the
+    probabilities are recomputed.  The same inputs give the same bits."""
+    s = _attention_shape(q, k, v, causal, scale, q_offsets, k_offsets, max_q_len, max_k_len)
+    packed = q_offsets is not None
+    dev = q.device
+    stats = (q.shape[1], q.shape[0]) if packed else (q.shape[0], q.shape[2], q.shape[1])
+    if grad_out.shape != q.shape or out.shape != q.shape or lse.shape != stats or not lse.is_contiguous():
+        raise ValueError("grad_out, out and lse must have the shapes that the forward pass gives")
+    _need(grad_out, "grad_out", dev, q.dtype), _need(out, "out", dev, q.dtype), _need(lse, "lse", dev, torch.float32)
+    lib = load_library()
+    with _current(dev), _on(stream, grad_out, q, k, v, out, lse, q_offsets, k_offsets):
+        new = torch.zeros if packed else torch.empty
+        grads = [new(t.shape, dtype=q.dtype, device=dev) for t in (q, k, v)]
+        ws_bytes = 4 * lse.numel()
+        ws = torch.empty(lse.numel(), dtype=torch.float32, device=dev)
+        hs = [_heads(t, name) for t, name in ((grad_out, "grad_out"), (q, "q"), (k, "k"), (v, "v"), (out, "out"))]
+        gs = [_heads(t, name) for t, name in zip(grads, ("grad_q", "grad_k", "grad_v"))]
+        _check(lib.fewbit_attention_bwd(ctypes.byref(s), *map(ctypes.byref, hs), lse.data_ptr(), *map(ctypes.byref, gs), ws.data_ptr(),
+                                        ws_bytes, _stream_ptr(stream, dev)), "fewbit_attention_bwd")
+    return tuple(grads)
+
+
+def fewbit_attention_timeout_count(device=None) -> int:
+    """How often a wait inside the attention kernels gave up on ``device``; 0 unless something is broken.  Synchronises."""
+    device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
+    out = ctypes.c_uint64()
+    with torch.cuda.device(device):
+        _check(load_library().fewbit_attention_timeout_count(ctypes.byref(out)), "fewbit_attention_timeout_count")
+    return int(out.value)
 
 
 # ---------------------------------------------------------------------------------------------------------------
