@@ -281,7 +281,7 @@ typedef struct fewbit_heads {
  * rotary_dim on are not rotated.  y is rounded once to `dtype`.
  *
  *   batch, length   tokens (batch * length < 2^31)
- *   heads, kv_heads query and key heads (0 allowed: that tensor is not touched)
+ *   heads, kv_heads query and key heads, up to 2^15 (0 allowed: that tensor is not touched)
  *   head_dim        even, 2 .. 256;   rotary_dim  even, 0 .. head_dim
  *   positions       DEVICE, batch * length int32 (positions_are_64bit: int64),
  *                   or NULL: token i of a sequence has position i

@@ -9,8 +9,8 @@
 // Decomposition: a head belongs to G lanes (a power of two).  A lane holds a "unit": two pieces of V
 // elements that the rotation pairs with one another ((j, j + rotary_dim/2) pairs: pieces rotary_dim/2
 // apart; neighbouring pairs: pieces side by side), so no value ever changes lanes and the sums are a
-// few shuffles.  A group works on kHeads heads of ONE token at a time: the token's cosines and sines are
-// read once for all of them, and their loads are in flight together.
+// few shuffles.  A CTA works on one chunk of heads (blockIdx.y) for a stride of tokens: a group reads a
+// token's cosines and sines once for the chunk, and kHeads heads are in flight at a time.
 #include <cmath>
 
 #include "fewbit_device.cuh"
@@ -23,8 +23,12 @@ namespace {
 
 constexpr int kQkThreads = 256;
 constexpr int kQkMaxDim = 256;
+// Heads in flight and CTAs on an SM, chosen together: bytes in flight against registers.  Measured on 4 x 8192 tokens,
+// 32 + 8 heads of 128, bfloat16, forward / backward in us: (4, 2 CTAs) 116 / -, (4, 3) 129 / -, (2, 3) 137 / -, (2, 4) 143 / -;
+// (2, 2) - / 210, (1, 2) - / 213, (1, 3) - / 306, (2, 3) - / 361 (spilled registers).
 constexpr int kFwdHeads = 4, kBwdHeads = 2;
-constexpr int kBwdCtasPerSm = 2;
+constexpr int kChunkHeads = 8;
+constexpr int kFwdCtasPerSm = 2, kBwdCtasPerSm = 2;
 
 struct QkTensor {
     void *p;
@@ -35,15 +39,15 @@ struct QkParams {
     const float *weight[2];
     const float *cos, *sin;
     const void *positions;
-    float *partial;                     // backward: (CTAs, 2, head_dim) sums of the weights' gradients, or nullptr
+    float *partial;                     // backward: a row of head_dim sums of the weight's gradient for each CTA, or nullptr
     long long table_rows;
     uint32_t tokens, length;
     int heads[2];
-    int jobs[2];                        // head groups of one token: queries, keys
+    int chunks[2], chunk;               // chunks of `chunk` heads: queries, keys
     int dim, rot, half;                 // half = rot / 2
     int units, rot_units;               // units of a head; those that are rotated half against half
     int group;                          // G
-    bool interleaved, positions64;
+    bool positions64;
     float eps, inv_dim;
 };
 
@@ -77,19 +81,72 @@ __device__ __forceinline__ void store_chunk(T *p, const float (&v)[V]) {
     *reinterpret_cast<Raw *>(p) = raw;
 }
 
+// Packed binary32 arithmetic: two lanes of one instruction, each rounded as the scalar operation is.
+__device__ __forceinline__ void fma2(float &d0, float &d1, float a0, float a1, float b0, float b1, float c0, float c1) {
+    asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\n"
+        "fma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
+        : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1), "f"(c0), "f"(c1));
+}
+__device__ __forceinline__ void mul2(float &d0, float &d1, float a0, float a1, float b0, float b1) {
+    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
+        : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
+}
+// d = a b, d = a b + c, over V elements; `scale` forms: b the same for all
+template <int V> __device__ __forceinline__ void vmul(float (&d)[V], const float (&a)[V], const float (&b)[V]) {
+    if constexpr (V == 1) d[0] = a[0] * b[0];
+    else {
+#pragma unroll
+        for (int e = 0; e < V; e += 2) mul2(d[e], d[e + 1], a[e], a[e + 1], b[e], b[e + 1]);
+    }
+}
+template <int V> __device__ __forceinline__ void vfma(float (&d)[V], const float (&a)[V], const float (&b)[V], const float (&c)[V]) {
+    if constexpr (V == 1) d[0] = fmaf(a[0], b[0], c[0]);
+    else {
+#pragma unroll
+        for (int e = 0; e < V; e += 2) fma2(d[e], d[e + 1], a[e], a[e + 1], b[e], b[e + 1], c[e], c[e + 1]);
+    }
+}
+template <int V> __device__ __forceinline__ void vscale(float (&d)[V], const float (&a)[V], float b) {
+    if constexpr (V == 1) d[0] = a[0] * b;
+    else {
+#pragma unroll
+        for (int e = 0; e < V; e += 2) mul2(d[e], d[e + 1], a[e], a[e + 1], b, b);
+    }
+}
+template <int V> __device__ __forceinline__ void vaxpy(float (&d)[V], const float (&a)[V], float b, const float (&c)[V]) {
+    if constexpr (V == 1) d[0] = fmaf(a[0], b, c[0]);
+    else {
+#pragma unroll
+        for (int e = 0; e < V; e += 2) fma2(d[e], d[e + 1], a[e], a[e + 1], b, b, c[e], c[e + 1]);
+    }
+}
+// s += a b, in two running sums
+template <int V> __device__ __forceinline__ void vdot(float (&s)[2], const float (&a)[V], const float (&b)[V]) {
+    if constexpr (V == 1) s[0] = fmaf(a[0], b[0], s[0]);
+    else {
+#pragma unroll
+        for (int e = 0; e < V; e += 2) fma2(s[0], s[1], a[e], a[e + 1], b[e], b[e + 1], s[0], s[1]);
+    }
+}
+
 __device__ __forceinline__ float group_sum(float x, int group) {
     for (int o = group >> 1; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
 }
 
-// Where a lane's units lie, and the rotation of their pairs for one position.
-template <int V, int CU>
+// Where a lane's units lie.  FULL: every lane has both pieces of each unit, and all of them are rotated.
+template <int V, int CU, bool FULL>
 struct Units {
     int a[CU], b[CU];                   // first element of each piece; b < 0: no second piece, a < 0: no unit
-    __device__ __forceinline__ void place(const QkParams &q, int sub) {
+    __device__ __forceinline__ void place(const QkParams &q, int sub, bool interleaved) {
 #pragma unroll
         for (int c = 0; c < CU; ++c) {
             const int u = sub + c * q.group;
+            if (FULL) {
+                a[c] = interleaved ? 2 * u * V : u * V;
+                b[c] = interleaved ? a[c] + V : q.half + a[c];
+                continue;
+            }
             a[c] = b[c] = -1;
             if (u >= q.units) continue;
             if (u < q.rot_units) {
@@ -101,24 +158,42 @@ struct Units {
             }
         }
     }
+    __device__ __forceinline__ bool has_a(int c) const { return FULL || a[c] >= 0; }
+    __device__ __forceinline__ bool has_b(int c) const { return FULL || b[c] >= 0; }
 };
 
 // cos and sin of a lane's pairs at one position: for units rotated half against half, V pairs; for neighbouring
 // pairs, V/2 pairs of each piece (with V = 1 the unit's two pieces are the pair).  Pairs that are not rotated get (1, 0).
-template <int V, int CU>
+template <int V, int CU, bool INTER, bool FULL>
 struct Turn {
     float c[CU][V], s[CU][V];
-    __device__ __forceinline__ void load(const QkParams &q, const Units<V, CU> &u, long long pos) {
+    __device__ __forceinline__ void load(const QkParams &q, const Units<V, CU, FULL> &u, long long pos) {
         const bool known = pos >= 0 && pos < q.table_rows;
         const float bad = __uint_as_float(0x7fc00000u);
         const long long row = known ? pos * q.half : 0;
+        if constexpr (FULL) {                                 // whole vectors (16-byte aligned by the host's check)
+            static_assert(V % 4 == 0, "");
+#pragma unroll
+            for (int k = 0; k < CU; ++k)
+#pragma unroll
+                for (int e = 0; e < V; e += 4) {
+                    const int j = (INTER ? u.a[k] / 2 : u.a[k]) + e;
+                    float4 x = make_float4(bad, bad, bad, bad), y = x;
+                    if (known) {
+                        x = __ldg(reinterpret_cast<const float4 *>(q.cos + row + j));
+                        y = __ldg(reinterpret_cast<const float4 *>(q.sin + row + j));
+                    }
+                    c[k][e] = x.x; c[k][e + 1] = x.y; c[k][e + 2] = x.z; c[k][e + 3] = x.w;
+                    s[k][e] = y.x; s[k][e + 1] = y.y; s[k][e + 2] = y.z; s[k][e + 3] = y.w;
+                }
+        } else {
 #pragma unroll
         for (int k = 0; k < CU; ++k)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 int j = -1;                                   // the pair's column of the tables
                 if (u.a[k] >= 0) {
-                    if (!q.interleaved) j = u.a[k] + V <= q.half ? u.a[k] + e : -1;
+                    if (!INTER) j = u.a[k] + V <= q.half ? u.a[k] + e : -1;
                     else if (V == 1) j = u.a[k] < q.rot ? u.a[k] / 2 : -1;
                     else {
                         const int first = e < V / 2 ? u.a[k] + 2 * e : u.b[k] + 2 * (e - V / 2);
@@ -128,23 +203,28 @@ struct Turn {
                 c[k][e] = !known ? bad : (j >= 0 ? __ldg(q.cos + row + j) : 1.0f);
                 s[k][e] = known && j >= 0 ? __ldg(q.sin + row + j) : 0.0f;
             }
+        }
     }
-    // (va, vb) <- R (va, vb), or R^T when `back`
-    __device__ __forceinline__ void apply(const QkParams &q, float (&va)[CU][V], float (&vb)[CU][V], bool back) const {
+    // (va, vb) <- R (va, vb), or R^T when BACK
+    template <bool BACK>
+    __device__ __forceinline__ void apply(float (&va)[CU][V], float (&vb)[CU][V]) const {
 #pragma unroll
         for (int k = 0; k < CU; ++k) {
-            if (!q.interleaved || V == 1) {
+            if constexpr (!INTER || V == 1) {                 // a pair's elements lie in different pieces
+                float to_a[V], to_b[V], x[V], y[V];
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float sn = back ? -s[k][e] : s[k][e];
-                    const float x = va[k][e], y = vb[k][e];
-                    va[k][e] = x * c[k][e] - y * sn;
-                    vb[k][e] = x * sn + y * c[k][e];
+                    to_a[e] = BACK ? s[k][e] : -s[k][e];
+                    to_b[e] = -to_a[e];
                 }
+                vmul<V>(x, vb[k], to_a);
+                vmul<V>(y, va[k], to_b);
+                vfma<V>(va[k], va[k], c[k], x);
+                vfma<V>(vb[k], vb[k], c[k], y);
             } else {
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
-                    const float sn = back ? -s[k][e] : s[k][e];
+                    const float sn = BACK ? -s[k][e] : s[k][e];
                     float &x = e < V / 2 ? va[k][2 * e % V] : vb[k][2 * e % V];
                     float &y = e < V / 2 ? va[k][(2 * e + 1) % V] : vb[k][(2 * e + 1) % V];
                     const float x0 = x, y0 = y;
@@ -161,228 +241,257 @@ __device__ __forceinline__ long long position_of(const QkParams &q, uint32_t tok
     return q.positions64 ? static_cast<const long long *>(q.positions)[token] : static_cast<const int *>(q.positions)[token];
 }
 
-template <typename T, int V, int CU, int NH>
-__device__ __forceinline__ void load_heads(const T *base, long long step, int n, const Units<V, CU> &u, Chunk<T, V> (&x)[NH][CU][2]) {
-#pragma unroll
-    for (int j = 0; j < NH; ++j)
-#pragma unroll
-        for (int c = 0; c < CU; ++c) {
-            x[j][c][0].zero();
-            x[j][c][1].zero();
-            if (j < n) {
-                if (u.a[c] >= 0) x[j][c][0].load(base + j * step + u.a[c]);
-                if (u.b[c] >= 0) x[j][c][1].load(base + j * step + u.b[c]);
-            }
-        }
-}
-
-template <typename T, int V, int CU>
-__device__ __forceinline__ void store_head(T *base, const Units<V, CU> &u, const float (&va)[CU][V], const float (&vb)[CU][V]) {
+template <typename T, int V, int CU, bool FULL>
+__device__ __forceinline__ void load_head(const T *base, bool live, const Units<V, CU, FULL> &u, Chunk<T, V> (&x)[CU][2]) {
 #pragma unroll
     for (int c = 0; c < CU; ++c) {
-        if (u.a[c] >= 0) store_chunk<T, V>(base + u.a[c], va[c]);
-        if (u.b[c] >= 0) store_chunk<T, V>(base + u.b[c], vb[c]);
+        x[c][0].zero();
+        x[c][1].zero();
+        if (live && u.has_a(c)) x[c][0].load(base + u.a[c]);
+        if (live && u.has_b(c)) x[c][1].load(base + u.b[c]);
     }
 }
 
-template <int V, int CU>
-__device__ __forceinline__ void load_weight(const float *w, const Units<V, CU> &u, float (&wa)[CU][V], float (&wb)[CU][V]) {
+template <typename T, int V, int CU, bool FULL>
+__device__ __forceinline__ void store_head(T *base, const Units<V, CU, FULL> &u, const float (&va)[CU][V], const float (&vb)[CU][V]) {
+#pragma unroll
+    for (int c = 0; c < CU; ++c) {
+        if (u.has_a(c)) store_chunk<T, V>(base + u.a[c], va[c]);
+        if (u.has_b(c)) store_chunk<T, V>(base + u.b[c], vb[c]);
+    }
+}
+
+template <int V, int CU, bool FULL>
+__device__ __forceinline__ void load_weight(const float *w, const Units<V, CU, FULL> &u, float (&wa)[CU][V], float (&wb)[CU][V]) {
 #pragma unroll
     for (int c = 0; c < CU; ++c)
 #pragma unroll
         for (int e = 0; e < V; ++e) {
-            wa[c][e] = w == nullptr ? 1.0f : (u.a[c] >= 0 ? __ldg(w + u.a[c] + e) : 0.0f);
-            wb[c][e] = w == nullptr ? 1.0f : (u.b[c] >= 0 ? __ldg(w + u.b[c] + e) : 0.0f);
+            wa[c][e] = w == nullptr ? 1.0f : (u.has_a(c) ? __ldg(w + u.a[c] + e) : 0.0f);
+            wb[c][e] = w == nullptr ? 1.0f : (u.has_b(c) ? __ldg(w + u.b[c] + e) : 0.0f);
         }
 }
 
-template <typename T, int V, int CU>
-__global__ void __launch_bounds__(kQkThreads)
+// The chunk of heads [first, end) of queries (which = 0) or keys that a CTA works on.
+struct HeadChunk {
+    int which, first, end;
+    __device__ __forceinline__ explicit HeadChunk(const QkParams &q) {
+        which = static_cast<int>(blockIdx.y) >= q.chunks[0];
+        first = (static_cast<int>(blockIdx.y) - (which ? q.chunks[0] : 0)) * q.chunk;
+        end = min(first + q.chunk, q.heads[which]);
+    }
+};
+
+template <typename T, int V, int CU, bool INTER, bool FULL>
+__global__ void __launch_bounds__(kQkThreads, kFwdCtasPerSm)
 qk_fwd_kernel(const __grid_constant__ QkParams q) {
     pdl_launch_dependents();
-    const int sub = threadIdx.x & (q.group - 1);
     const uint32_t per = kQkThreads / q.group;                      // groups of a CTA
-    const uint32_t jobs = q.jobs[0] + q.jobs[1];
-    const uint32_t total = q.tokens * jobs;                         // < 2^31 by the host's check
-    Units<V, CU> u;
-    u.place(q, sub);
+    const HeadChunk hc(q);
+    const QkTensor &in = q.in[hc.which], &out = q.out[hc.which];
+    Units<V, CU, FULL> u;
+    u.place(q, threadIdx.x & (q.group - 1), INTER);
     pdl_wait();
+    float wa[CU][V], wb[CU][V];
+    load_weight<V, CU, FULL>(q.weight[hc.which], u, wa, wb);
     // every lane of a warp runs the same number of rounds (the sums' shuffles need them all)
-    for (uint32_t base = blockIdx.x * per; base < total; base += gridDim.x * per) {
-        const uint32_t job = base + threadIdx.x / q.group;
-        const bool live = job < total;
-        const uint32_t token = live ? job / jobs : 0, part = live ? job % jobs : 0;
-        const int which = part >= static_cast<uint32_t>(q.jobs[0]);
-        const int head = (part - (which ? q.jobs[0] : 0)) * kFwdHeads;
-        const int n = live ? min(kFwdHeads, q.heads[which] - head) : 0;
-        const uint32_t bi = token / q.length, i = token % q.length;
-        const QkTensor &in = q.in[which], &out = q.out[which];
-        const T *src = static_cast<const T *>(in.p) + bi * in.b + i * in.i + head * in.h;
-        Chunk<T, V> x[kFwdHeads][CU][2];
-        load_heads<T, V, CU, kFwdHeads>(src, in.h, n, u, x);
-        Turn<V, CU> turn;
-        turn.load(q, u, position_of(q, token, i));
-        float wa[CU][V], wb[CU][V];
-        load_weight<V, CU>(q.weight[which], u, wa, wb);
-        T *dst = static_cast<T *>(out.p) + bi * out.b + i * out.i + head * out.h;
+    for (uint32_t base = blockIdx.x * per; base < q.tokens; base += gridDim.x * per) {
+        const uint32_t token = base + threadIdx.x / q.group;
+        const bool live = token < q.tokens;
+        const uint32_t bi = live ? token / q.length : 0, i = live ? token % q.length : 0;
+        Turn<V, CU, INTER, FULL> turn;
+        turn.load(q, u, position_of(q, live ? token : 0, i));
+        const T *src = static_cast<const T *>(in.p) + bi * in.b + i * in.i + hc.first * in.h;
+        T *dst = static_cast<T *>(out.p) + bi * out.b + i * out.i + hc.first * out.h;
+        for (int head = hc.first; head < hc.end; head += kFwdHeads, src += kFwdHeads * in.h, dst += kFwdHeads * out.h) {
+            Chunk<T, V> x[kFwdHeads][CU][2];
 #pragma unroll
-        for (int j = 0; j < kFwdHeads; ++j) {
-            float va[CU][V], vb[CU][V], sum = 0.0f;
+            for (int j = 0; j < kFwdHeads; ++j) load_head<T, V, CU, FULL>(src + j * in.h, live && head + j < hc.end, u, x[j]);
 #pragma unroll
-            for (int c = 0; c < CU; ++c) {
-                x[j][c][0].widen(va[c]);
-                x[j][c][1].widen(vb[c]);
+            for (int j = 0; j < kFwdHeads; ++j) {
+                float va[CU][V], vb[CU][V], sum[2] = {0.0f, 0.0f};
 #pragma unroll
-                for (int e = 0; e < V; ++e) sum += va[c][e] * va[c][e] + vb[c][e] * vb[c][e];
+                for (int c = 0; c < CU; ++c) {
+                    x[j][c][0].widen(va[c]);
+                    x[j][c][1].widen(vb[c]);
+                    vdot<V>(sum, va[c], va[c]);
+                    vdot<V>(sum, vb[c], vb[c]);
+                }
+                const float r = rsqrtf(group_sum(sum[0] + sum[1], q.group) * q.inv_dim + q.eps);
+                if (!live || head + j >= hc.end) continue;
+#pragma unroll
+                for (int c = 0; c < CU; ++c) {
+                    vscale<V>(va[c], va[c], r);
+                    vscale<V>(vb[c], vb[c], r);
+                    vmul<V>(va[c], va[c], wa[c]);
+                    vmul<V>(vb[c], vb[c], wb[c]);
+                }
+                turn.template apply<false>(va, vb);
+                store_head<T, V, CU, FULL>(dst + j * out.h, u, va, vb);
             }
-            const float r = rsqrtf(group_sum(sum, q.group) * q.inv_dim + q.eps);
-            if (j >= n) continue;
-#pragma unroll
-            for (int c = 0; c < CU; ++c)
-#pragma unroll
-                for (int e = 0; e < V; ++e) { va[c][e] *= r * wa[c][e]; vb[c][e] *= r * wb[c][e]; }
-            turn.apply(q, va, vb, false);
-            store_head<T, V, CU>(dst + j * out.h, u, va, vb);
         }
     }
 }
 
-template <typename T, int V, int CU>
-__global__ void __launch_bounds__(kQkThreads)
+template <typename T, int V, int CU, bool INTER, bool FULL>
+__global__ void __launch_bounds__(kQkThreads, kBwdCtasPerSm)
 qk_bwd_kernel(const __grid_constant__ QkParams q) {
     pdl_launch_dependents();
-    const int sub = threadIdx.x & (q.group - 1);
     const uint32_t per = kQkThreads / q.group;
-    Units<V, CU> u;
-    u.place(q, sub);
-    __shared__ float sums[kQkThreads / 32][2 * V * CU][33];
+    const HeadChunk hc(q);
+    const QkTensor &in = q.in[hc.which], &gin = q.g[hc.which], &out = q.out[hc.which];
+    Units<V, CU, FULL> u;
+    u.place(q, threadIdx.x & (q.group - 1), INTER);
+    __shared__ float sums[kQkThreads / 32][kQkMaxDim];
     pdl_wait();
-#pragma unroll 1
-    for (int which = 0; which < 2; ++which) {                       // queries, then keys: one set of weight sums at a time
-        const uint32_t jobs = q.jobs[which];
-        const uint32_t total = q.tokens * jobs;
-        float wa[CU][V], wb[CU][V], da[CU][V], db[CU][V];
-        load_weight<V, CU>(q.weight[which], u, wa, wb);
+    float wa[CU][V], wb[CU][V], da[CU][V], db[CU][V];
+    load_weight<V, CU, FULL>(q.weight[hc.which], u, wa, wb);
 #pragma unroll
-        for (int c = 0; c < CU; ++c)
+    for (int c = 0; c < CU; ++c)
 #pragma unroll
-            for (int e = 0; e < V; ++e) da[c][e] = db[c][e] = 0.0f;
-        const QkTensor &in = q.in[which], &gin = q.g[which], &out = q.out[which];
-        for (uint32_t base = blockIdx.x * per; base < total; base += gridDim.x * per) {
-            const uint32_t job = base + threadIdx.x / q.group;
-            const bool live = job < total;
-            const uint32_t token = live ? job / jobs : 0;
-            const int head = live ? (job % jobs) * kBwdHeads : 0;
-            const int n = live ? min(kBwdHeads, q.heads[which] - head) : 0;
-            const uint32_t bi = token / q.length, i = token % q.length;
+        for (int e = 0; e < V; ++e) da[c][e] = db[c][e] = 0.0f;
+    for (uint32_t base = blockIdx.x * per; base < q.tokens; base += gridDim.x * per) {
+        const uint32_t token = base + threadIdx.x / q.group;
+        const bool live = token < q.tokens;
+        const uint32_t bi = live ? token / q.length : 0, i = live ? token % q.length : 0;
+        Turn<V, CU, INTER, FULL> turn;
+        turn.load(q, u, position_of(q, live ? token : 0, i));
+        const T *src = static_cast<const T *>(in.p) + bi * in.b + i * in.i + hc.first * in.h;
+        const T *grd = static_cast<const T *>(gin.p) + bi * gin.b + i * gin.i + hc.first * gin.h;
+        T *dst = static_cast<T *>(out.p) + bi * out.b + i * out.i + hc.first * out.h;
+        for (int head = hc.first; head < hc.end; head += kBwdHeads, src += kBwdHeads * in.h, grd += kBwdHeads * gin.h, dst += kBwdHeads * out.h) {
             Chunk<T, V> x[kBwdHeads][CU][2], g[kBwdHeads][CU][2];
-            load_heads<T, V, CU, kBwdHeads>(static_cast<const T *>(in.p) + bi * in.b + i * in.i + head * in.h, in.h, n, u, x);
-            load_heads<T, V, CU, kBwdHeads>(static_cast<const T *>(gin.p) + bi * gin.b + i * gin.i + head * gin.h, gin.h, n, u, g);
-            Turn<V, CU> turn;
-            turn.load(q, u, position_of(q, token, i));
-            T *dst = static_cast<T *>(out.p) + bi * out.b + i * out.i + head * out.h;
 #pragma unroll
             for (int j = 0; j < kBwdHeads; ++j) {
-                float va[CU][V], vb[CU][V], ga[CU][V], gb[CU][V], sum = 0.0f, dot = 0.0f;
+                load_head<T, V, CU, FULL>(src + j * in.h, live && head + j < hc.end, u, x[j]);
+                load_head<T, V, CU, FULL>(grd + j * gin.h, live && head + j < hc.end, u, g[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < kBwdHeads; ++j) {
+                float va[CU][V], vb[CU][V], ga[CU][V], gb[CU][V], squares[2] = {0.0f, 0.0f}, dots[2] = {0.0f, 0.0f};
 #pragma unroll
                 for (int c = 0; c < CU; ++c) {
                     x[j][c][0].widen(va[c]);
                     x[j][c][1].widen(vb[c]);
                     g[j][c][0].widen(ga[c]);
                     g[j][c][1].widen(gb[c]);
+                    vdot<V>(squares, va[c], va[c]);
+                    vdot<V>(squares, vb[c], vb[c]);
                 }
-                turn.apply(q, ga, gb, true);
+                turn.template apply<true>(ga, gb);
+                // t = g' x: the weight's gradient without r, and, times the weight, the terms of the dot product
+                float ta[CU][V], tb[CU][V];
 #pragma unroll
-                for (int c = 0; c < CU; ++c)
+                for (int c = 0; c < CU; ++c) {
+                    vmul<V>(ta[c], ga[c], va[c]);
+                    vmul<V>(tb[c], gb[c], vb[c]);
+                    vdot<V>(dots, ta[c], wa[c]);
+                    vdot<V>(dots, tb[c], wb[c]);
+                }
+                float sum = squares[0] + squares[1], dot = dots[0] + dots[1];
+                for (int o = q.group >> 1; o > 0; o >>= 1) {          // both sums in one go
+                    sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                    dot += __shfl_xor_sync(0xffffffffu, dot, o);
+                }
+                const float r = rsqrtf(sum * q.inv_dim + q.eps);
+                const float shift = -dot * q.inv_dim * r * r * r;
+                if (!live || head + j >= hc.end) continue;
 #pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        sum += va[c][e] * va[c][e] + vb[c][e] * vb[c][e];
-                        dot += ga[c][e] * wa[c][e] * va[c][e] + gb[c][e] * wb[c][e] * vb[c][e];
-                    }
-                const float r = rsqrtf(group_sum(sum, q.group) * q.inv_dim + q.eps);
-                const float shift = group_sum(dot, q.group) * q.inv_dim * r * r;
-                if (j >= n) continue;
-#pragma unroll
-                for (int c = 0; c < CU; ++c)
-#pragma unroll
-                    for (int e = 0; e < V; ++e) {
-                        da[c][e] += ga[c][e] * (va[c][e] * r);
-                        db[c][e] += gb[c][e] * (vb[c][e] * r);
-                        va[c][e] = r * (ga[c][e] * wa[c][e] - va[c][e] * shift);
-                        vb[c][e] = r * (gb[c][e] * wb[c][e] - vb[c][e] * shift);
-                    }
-                store_head<T, V, CU>(dst + j * out.h, u, va, vb);
+                for (int c = 0; c < CU; ++c) {
+                    vaxpy<V>(da[c], ta[c], r, da[c]);
+                    vaxpy<V>(db[c], tb[c], r, db[c]);
+                    vscale<V>(ga[c], ga[c], r);                       // dx = (r g') w - (r^3 mean) x
+                    vscale<V>(gb[c], gb[c], r);
+                    vscale<V>(va[c], va[c], shift);
+                    vscale<V>(vb[c], vb[c], shift);
+                    vfma<V>(va[c], ga[c], wa[c], va[c]);
+                    vfma<V>(vb[c], gb[c], wb[c], vb[c]);
+                }
+                store_head<T, V, CU, FULL>(dst + j * out.h, u, va, vb);
             }
         }
-        if (q.partial == nullptr) continue;
-        // the CTA's sum of every element of the weight, in a fixed order: lane by lane through shared memory
-        __syncthreads();
+    }
+    if (q.partial == nullptr) return;
+    // the CTA's sum of every element of the weight, in a fixed order: over a warp's groups, then over its warps
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
-        for (int c = 0; c < CU; ++c)
+    for (int c = 0; c < CU; ++c)
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                sums[threadIdx.x >> 5][(2 * c) * V + e][threadIdx.x & 31] = da[c][e];
-                sums[threadIdx.x >> 5][(2 * c + 1) * V + e][threadIdx.x & 31] = db[c][e];
+        for (int e = 0; e < V; ++e) {
+            for (int o = q.group; o < 32; o <<= 1) {
+                da[c][e] += __shfl_xor_sync(0xffffffffu, da[c][e], o);
+                db[c][e] += __shfl_xor_sync(0xffffffffu, db[c][e], o);
             }
-        __syncthreads();
-        if (threadIdx.x < static_cast<unsigned>(q.group)) {
-            float *row = q.partial + (static_cast<size_t>(blockIdx.x) * 2 + which) * q.dim;
-#pragma unroll
-            for (int c = 0; c < CU; ++c)
-#pragma unroll
-                for (int e = 0; e < 2 * V; ++e) {
-                    const int first = e < V ? u.a[c] : u.b[c];
-                    if (first < 0) continue;
-                    float total_sum = 0.0f;
-                    for (int w = 0; w < kQkThreads / 32; ++w)
-                        for (int l = sub; l < 32; l += q.group) total_sum += sums[w][2 * c * V + e][l];
-                    row[first + e % V] = total_sum;
-                }
+            if (lane < q.group) {
+                if (u.has_a(c)) sums[warp][u.a[c] + e] = da[c][e];
+                if (u.has_b(c)) sums[warp][u.b[c] + e] = db[c][e];
+            }
         }
+    __syncthreads();
+    if (static_cast<int>(threadIdx.x) < q.dim) {
+        float total = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kQkThreads / 32; ++w) total += sums[w][threadIdx.x];
+        q.partial[(static_cast<size_t>(blockIdx.y) * gridDim.x + blockIdx.x) * q.dim + threadIdx.x] = total;
     }
 }
 
-// Adds up the CTAs' partial sums: 32 columns and 32 rows of threads for each CTA.
+// Adds up the CTAs' partial sums, `q_ctas` rows of the queries' weight and then `k_ctas` of the keys': 32 columns and
+// 32 rows of threads for each CTA (blockIdx.y: query or key).
 __global__ void __launch_bounds__(1024)
-qk_weight_kernel(const float *partial, int ctas, int dim, float *dq, float *dk) {
+qk_weight_kernel(const float *partial, int q_ctas, int k_ctas, int dim, float *dq, float *dk) {
     pdl_launch_dependents();
     __shared__ float part[32][33];
     const int lane = threadIdx.x & 31, row = threadIdx.x >> 5;
-    const int col = blockIdx.x * 32 + lane;                          // of 2 * dim
+    const int col = blockIdx.x * 32 + lane;
+    const int first = blockIdx.y ? q_ctas : 0, end = blockIdx.y ? q_ctas + k_ctas : q_ctas;
     pdl_wait();
     float sum = 0.0f;
-    if (col < 2 * dim)
-        for (int c = row; c < ctas; c += 32) sum += partial[static_cast<size_t>(c) * 2 * dim + col];
+    if (col < dim) {
+#pragma unroll 8
+        for (int c = first + row; c < end; c += 32) sum += partial[static_cast<size_t>(c) * dim + col];
+    }
     part[row][lane] = sum;
     __syncthreads();
-    if (row == 0 && col < 2 * dim) {
-        sum = 0.0f;
-        for (int r = 0; r < 32; ++r) sum += part[r][lane];
-        float *to = col < dim ? dq : dk;
-        if (to != nullptr) to[col < dim ? col : col - dim] = sum;
-    }
+    sum = part[lane][row];                                           // transposed: a warp adds one column
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    float *to = blockIdx.y ? dk : dq;
+    if (lane == 0 && blockIdx.x * 32 + row < dim && to != nullptr) to[blockIdx.x * 32 + row] = sum;
 }
 
-using QkLaunch = cudaError_t (*)(const QkParams &, unsigned, cudaStream_t);
-template <typename T, int V, int CU>
-cudaError_t launch_fwd(const QkParams &q, unsigned grid, cudaStream_t st) {
-    return launch_pdl(qk_fwd_kernel<T, V, CU>, grid, kQkThreads, 0, st, pdl_enabled(), q);
+using QkLaunch = cudaError_t (*)(const QkParams &, unsigned, unsigned, cudaStream_t);
+template <typename K>
+cudaError_t launch_qk(K kernel, const QkParams &q, unsigned x, unsigned y, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(x, y);
+    cfg.blockDim = dim3(kQkThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = pdl_enabled() ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, q);
 }
-template <typename T, int V, int CU>
-cudaError_t launch_bwd_qk(const QkParams &q, unsigned grid, cudaStream_t st) {
-    return launch_pdl(qk_bwd_kernel<T, V, CU>, grid, kQkThreads, 0, st, pdl_enabled(), q);
+template <typename T, int V, int CU, bool INTER, bool FULL>
+cudaError_t launch_fwd(const QkParams &q, unsigned x, unsigned y, cudaStream_t st) {
+    return launch_qk(qk_fwd_kernel<T, V, CU, INTER, FULL>, q, x, y, st);
 }
-// [dtype][log2 V]; a lane holds CU units so that 32 lanes cover the largest head
-const QkLaunch kQkFwd[3][4] = {
-    {launch_fwd<float, 1, 4>, launch_fwd<float, 2, 2>, launch_fwd<float, 4, 1>, nullptr},
-    {launch_fwd<__nv_bfloat16, 1, 4>, launch_fwd<__nv_bfloat16, 2, 2>, launch_fwd<__nv_bfloat16, 4, 1>, launch_fwd<__nv_bfloat16, 8, 1>},
-    {launch_fwd<__half, 1, 4>, launch_fwd<__half, 2, 2>, launch_fwd<__half, 4, 1>, launch_fwd<__half, 8, 1>},
-};
-const QkLaunch kQkBwd[3][4] = {
-    {launch_bwd_qk<float, 1, 4>, launch_bwd_qk<float, 2, 2>, launch_bwd_qk<float, 4, 1>, nullptr},
-    {launch_bwd_qk<__nv_bfloat16, 1, 4>, launch_bwd_qk<__nv_bfloat16, 2, 2>, launch_bwd_qk<__nv_bfloat16, 4, 1>, launch_bwd_qk<__nv_bfloat16, 8, 1>},
-    {launch_bwd_qk<__half, 1, 4>, launch_bwd_qk<__half, 2, 2>, launch_bwd_qk<__half, 4, 1>, launch_bwd_qk<__half, 8, 1>},
-};
+template <typename T, int V, int CU, bool INTER, bool FULL>
+cudaError_t launch_bwd_qk(const QkParams &q, unsigned x, unsigned y, cudaStream_t st) {
+    return launch_qk(qk_bwd_kernel<T, V, CU, INTER, FULL>, q, x, y, st);
+}
+// [dtype][interleaved][variant]: 16-byte pieces with full lanes, 16-byte pieces, 8-byte pieces of the 16-bit types, single
+// elements; a lane holds CU units so that 32 lanes cover the largest head
+enum { kFull, kWide, kHalfWide, kSingle, kVariants };
+#define FEWBIT_QK_ROW(launch, T, V, INTER) \
+    {launch<T, V, 1, INTER, true>, launch<T, V, 1, INTER, false>, launch<T, 4, 1, INTER, false>, launch<T, 1, 4, INTER, false>}
+#define FEWBIT_QK_TABLE(launch) \
+    {{FEWBIT_QK_ROW(launch, float, 4, false), FEWBIT_QK_ROW(launch, float, 4, true)}, \
+     {FEWBIT_QK_ROW(launch, __nv_bfloat16, 8, false), FEWBIT_QK_ROW(launch, __nv_bfloat16, 8, true)}, \
+     {FEWBIT_QK_ROW(launch, __half, 8, false), FEWBIT_QK_ROW(launch, __half, 8, true)}}
+const QkLaunch kQkFwd[3][2][kVariants] = FEWBIT_QK_TABLE(launch_fwd);
+const QkLaunch kQkBwd[3][2][kVariants] = FEWBIT_QK_TABLE(launch_bwd_qk);
 
 fewbit_status check_shape(const fewbit_qk_shape *s) {
     if (s == nullptr || !valid_dtype(s->dtype) || s->batch < 0 || s->length < 0 || s->heads < 0 || s->kv_heads < 0 ||
@@ -394,7 +503,7 @@ fewbit_status check_shape(const fewbit_qk_shape *s) {
     if (s->rotary_dim > 0 && s->positions == nullptr && s->table_rows < s->length) return FEWBIT_ERR_INVALID_ARG;
     if (s->batch > 0 && s->length > 0) {
         const int64_t most = INT32_MAX;
-        if (s->heads > 1 << 20 || s->kv_heads > 1 << 20 || s->batch > most / s->length ||
+        if (s->heads > 1 << 15 || s->kv_heads > 1 << 15 || s->batch > most / s->length ||
             s->batch * s->length > most / (static_cast<int64_t>(s->heads) + s->kv_heads + 1))
             return FEWBIT_ERR_TOO_LARGE;
     }
@@ -404,8 +513,18 @@ fewbit_status check_shape(const fewbit_qk_shape *s) {
     return FEWBIT_OK;
 }
 
-// Fills what both directions share; `all` are the tensors of the call (n of them, query and key in turn).
-fewbit_status fill(const fewbit_qk_shape *s, const fewbit_heads *const *all, int n, int heads_per_job, QkParams *q, int *log_v) {
+fewbit_status check_tensors(const fewbit_qk_shape *s, const fewbit_heads *const *all, int n) {
+    for (int k = 0; k < n; ++k) {
+        if ((k % 2 ? s->kv_heads : s->heads) == 0) continue;
+        if (all[k] == nullptr || all[k]->data == nullptr) return FEWBIT_ERR_INVALID_ARG;
+        if (reinterpret_cast<uintptr_t>(all[k]->data) % (s->dtype == FEWBIT_F32 ? 4 : 2)) return FEWBIT_ERR_ALIGNMENT;
+    }
+    return FEWBIT_OK;
+}
+
+// Fills what both directions share, and returns the kernels' variant; `all` are the tensors of the call (n of them, query
+// and key in turn).
+int fill(const fewbit_qk_shape *s, const fewbit_heads *const *all, int n, int heads_in_flight, unsigned sms, QkParams *q) {
     const int elem = s->dtype == FEWBIT_F32 ? 4 : 2;
     int v = 16 / elem;
     auto halve = [&](uint64_t bits) { while (v > 1 && bits % v != 0) v >>= 1; };
@@ -414,15 +533,13 @@ fewbit_status fill(const fewbit_qk_shape *s, const fewbit_heads *const *all, int
     for (int k = 0; k < n; ++k) {
         if ((k % 2 ? s->kv_heads : s->heads) == 0) continue;
         const fewbit_heads *t = all[k];
-        if (t == nullptr || t->data == nullptr) return FEWBIT_ERR_INVALID_ARG;
-        const uintptr_t at = reinterpret_cast<uintptr_t>(t->data);
-        if (at % elem) return FEWBIT_ERR_ALIGNMENT;
-        halve(at / elem);
+        halve(reinterpret_cast<uintptr_t>(t->data) / elem);
         if (s->batch > 1) halve(static_cast<uint64_t>(t->batch_stride));
         if (s->length > 1) halve(static_cast<uint64_t>(t->row_stride));
         if ((k % 2 ? s->kv_heads : s->heads) > 1) halve(static_cast<uint64_t>(t->head_stride));
     }
-    *log_v = v == 8 ? 3 : v == 4 ? 2 : v == 2 ? 1 : 0;
+    int variant = v == 16 / elem ? kWide : v >= 4 ? kHalfWide : kSingle;
+    if (variant == kSingle) v = 1;
     q->weight[0] = s->q_weight;
     q->weight[1] = s->k_weight;
     q->cos = s->cos;
@@ -431,22 +548,36 @@ fewbit_status fill(const fewbit_qk_shape *s, const fewbit_heads *const *all, int
     q->table_rows = s->rotary_dim > 0 ? s->table_rows : INT64_MAX;
     q->partial = nullptr;
     q->tokens = static_cast<uint32_t>(s->batch * s->length);
-    q->length = static_cast<uint32_t>(s->length > 0 ? s->length : 1);
+    q->length = static_cast<uint32_t>(s->length);
     q->heads[0] = s->heads;
     q->heads[1] = s->kv_heads;
-    for (int k = 0; k < 2; ++k) q->jobs[k] = (q->heads[k] + heads_per_job - 1) / heads_per_job;
     q->dim = s->head_dim;
     q->rot = s->rotary_dim;
     q->half = s->rotary_dim / 2;
-    q->interleaved = s->interleaved != 0;
     q->rot_units = s->interleaved ? 0 : q->half / v;
     q->units = q->rot_units + (s->head_dim - 2 * q->rot_units * v + 2 * v - 1) / (2 * v);
     q->group = 1;
     while (q->group < q->units && q->group < 32) q->group *= 2;
+    const uintptr_t table = reinterpret_cast<uintptr_t>(s->cos) | reinterpret_cast<uintptr_t>(s->sin);
+    if (variant == kWide && q->units == q->group && s->rotary_dim == s->head_dim && s->head_dim % (2 * v) == 0 && table % 16 == 0) variant = kFull;
+    // whole chunks of heads amortise a token's cosines; a call too small to fill the SMs takes fewer heads at a time
+    const uint32_t per = kQkThreads / q->group;
+    for (q->chunk = kChunkHeads;; q->chunk /= 2) {
+        for (int k = 0; k < 2; ++k) q->chunks[k] = (q->heads[k] + q->chunk - 1) / q->chunk;
+        const uint64_t ctas = static_cast<uint64_t>((q->tokens + per - 1) / per) * (q->chunks[0] + q->chunks[1]);
+        if (ctas >= sms || q->chunk <= heads_in_flight) break;
+    }
     q->positions64 = s->positions_are_64bit != 0;
     q->eps = s->eps;
     q->inv_dim = 1.0f / static_cast<float>(s->head_dim);
-    return FEWBIT_OK;
+    return variant;
+}
+
+// CTAs along the tokens: all of them, or as many as keep `per_sm` CTAs on every SM busy
+unsigned token_ctas(const QkParams &q, unsigned sms, int per_sm) {
+    const unsigned per = kQkThreads / q.group, want = (q.tokens + per - 1) / per, rows = static_cast<unsigned>(q.chunks[0] + q.chunks[1]);
+    const unsigned most = sms * per_sm / rows > 0 ? sms * per_sm / rows : 1;   // never a few CTAs more than fit at once
+    return want < most ? want : most;
 }
 
 QkTensor tensor(const fewbit_heads *t) { return t == nullptr ? QkTensor{} : QkTensor{t->data, t->batch_stride, t->row_stride, t->head_stride}; }
@@ -467,18 +598,16 @@ fewbit_status fewbit_qk_norm_rope_fwd(const fewbit_qk_shape *s, const fewbit_hea
     using namespace fewbit;
     if (const fewbit_status st = check_shape(s); st != FEWBIT_OK) return st;
     if (s->batch == 0 || s->length == 0 || s->heads + s->kv_heads == 0) return FEWBIT_OK;
-    QkParams q;
-    int log_v = 0;
-    const fewbit_heads *all[4] = {qi, ki, qo, ko};
-    if (const fewbit_status st = fill(s, all, 4, kFwdHeads, &q, &log_v); st != FEWBIT_OK) return st;
-    q.in[0] = tensor(qi); q.in[1] = tensor(ki);
-    q.out[0] = tensor(qo); q.out[1] = tensor(ko);
     cudaError_t err = cudaSuccess;
+    const fewbit_heads *all[4] = {qi, ki, qo, ko};
+    if (const fewbit_status st = check_tensors(s, all, 4); st != FEWBIT_OK) return st;
     const unsigned sms = device_sm_count(&err);
     if (err != cudaSuccess) return cuda_status(err);
-    const uint64_t groups = static_cast<uint64_t>(q.tokens) * (q.jobs[0] + q.jobs[1]);
-    const uint64_t per = kQkThreads / q.group, want = (groups + per - 1) / per, most = static_cast<uint64_t>(sms) * 16;
-    err = kQkFwd[s->dtype][log_v](q, static_cast<unsigned>(want < most ? want : most), static_cast<cudaStream_t>(stream));
+    QkParams q;
+    const int variant = fill(s, all, 4, kFwdHeads, sms, &q);
+    q.in[0] = tensor(qi); q.in[1] = tensor(ki);
+    q.out[0] = tensor(qo); q.out[1] = tensor(ko);
+    err = kQkFwd[s->dtype][s->interleaved != 0][variant](q, token_ctas(q, sms, kFwdCtasPerSm), q.chunks[0] + q.chunks[1], static_cast<cudaStream_t>(stream));
     if (err == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
     return cuda_status(err);
 }
@@ -488,7 +617,9 @@ size_t fewbit_qk_norm_rope_workspace_bytes(const fewbit_qk_shape *s) {
     if (check_shape(s) != FEWBIT_OK) return 0;
     cudaError_t err = cudaSuccess;
     const unsigned sms = device_sm_count(&err);
-    return err != cudaSuccess ? 0 : static_cast<size_t>(sms) * kBwdCtasPerSm * 2 * s->head_dim * sizeof(float);
+    // token_ctas rounds up once for each chunk of heads, of which there are at most this many
+    const size_t chunks = static_cast<size_t>(s->heads + kBwdHeads - 1) / kBwdHeads + (s->kv_heads + kBwdHeads - 1) / kBwdHeads;
+    return err != cudaSuccess ? 0 : (sms * kBwdCtasPerSm + chunks) * s->head_dim * sizeof(float);
 }
 
 fewbit_status fewbit_qk_norm_rope_bwd(const fewbit_qk_shape *s, const fewbit_heads *gqo, const fewbit_heads *gko, const fewbit_heads *qi,
@@ -507,28 +638,36 @@ fewbit_status fewbit_qk_norm_rope_bwd(const fewbit_qk_shape *s, const fewbit_hea
         if (err == cudaSuccess && dkw) err = cudaMemsetAsync(dkw, 0, s->head_dim * sizeof(float), stm);
         return cuda_status(err);
     }
-    QkParams q;
-    int log_v = 0;
     const fewbit_heads *all[6] = {gqo, gko, qi, ki, gq, gk};
-    if (const fewbit_status st = fill(s, all, 6, kBwdHeads, &q, &log_v); st != FEWBIT_OK) return st;
+    if (const fewbit_status st = check_tensors(s, all, 6); st != FEWBIT_OK) return st;
     if (weights && workspace == nullptr) return FEWBIT_ERR_INVALID_ARG;
     if (weights && (at & 15)) return FEWBIT_ERR_ALIGNMENT;
-    q.g[0] = tensor(gqo); q.g[1] = tensor(gko);
-    q.in[0] = tensor(qi); q.in[1] = tensor(ki);
-    q.out[0] = tensor(gq); q.out[1] = tensor(gk);
     cudaError_t err = cudaSuccess;
     const unsigned sms = device_sm_count(&err);
     if (err != cudaSuccess) return cuda_status(err);
-    const uint64_t per = kQkThreads / q.group, groups = static_cast<uint64_t>(q.tokens) * (q.jobs[0] > q.jobs[1] ? q.jobs[0] : q.jobs[1]);
-    const uint64_t want = (groups + per - 1) / per, most = static_cast<uint64_t>(sms) * kBwdCtasPerSm;
-    const unsigned grid = static_cast<unsigned>(want < most ? want : most);
-    if (weights && workspace_bytes < static_cast<size_t>(grid) * 2 * s->head_dim * sizeof(float)) return FEWBIT_ERR_ALLOC;
+    QkParams q;
+    const int variant = fill(s, all, 6, kBwdHeads, sms, &q);
+    q.g[0] = tensor(gqo); q.g[1] = tensor(gko);
+    q.in[0] = tensor(qi); q.in[1] = tensor(ki);
+    q.out[0] = tensor(gq); q.out[1] = tensor(gk);
+    const unsigned x = token_ctas(q, sms, kBwdCtasPerSm), y = q.chunks[0] + q.chunks[1];
+    if (weights && workspace_bytes < static_cast<size_t>(x) * y * s->head_dim * sizeof(float)) return FEWBIT_ERR_ALLOC;
     if (weights) q.partial = static_cast<float *>(workspace);
-    err = kQkBwd[s->dtype][log_v](q, grid, stm);
+    err = kQkBwd[s->dtype][s->interleaved != 0][variant](q, x, y, stm);
     if (err != cudaSuccess) return cuda_status(err);
     g_launches.fetch_add(1, std::memory_order_relaxed);
     if (!weights) return FEWBIT_OK;
-    err = launch_pdl(qk_weight_kernel, (2 * s->head_dim + 31) / 32, 1024, 0, stm, pdl_enabled(), q.partial, static_cast<int>(grid), s->head_dim, dqw, dkw);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((s->head_dim + 31) / 32, 2);
+    cfg.blockDim = dim3(1024);
+    cfg.stream = stm;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = pdl_enabled() ? 1 : 0;
+    err = cudaLaunchKernelEx(&cfg, qk_weight_kernel, static_cast<const float *>(q.partial), static_cast<int>(x) * q.chunks[0],
+                             static_cast<int>(x) * q.chunks[1], s->head_dim, dqw, dkw);
     if (err == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
     return cuda_status(err);
 }
