@@ -1,4 +1,6 @@
 // The attention kernels for one 16-bit type (FEWBIT_ATTN_F16: binary16, else bfloat16).
+#include <atomic>
+
 #include "fewbit_attention.cuh"
 #include "fewbit_attention_launch.h"
 
@@ -14,11 +16,18 @@ using T = __half;
 using T = __nv_bfloat16;
 #endif
 
-template <typename K>
-cudaError_t launch(K kernel, int smem, const Params &p, unsigned grid, cudaStream_t st) {
-    // per device, so set on every call: a host-side table write, no synchronisation
-    const cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+template <auto kernel, int smem>
+cudaError_t launch(const Params &p, unsigned grid, cudaStream_t st) {
+    static std::atomic<unsigned long long> ready{0};                  // devices (up to 64) whose limit has been raised
+    int dev = 0;
+    cudaError_t err = cudaGetDevice(&dev);
     if (err != cudaSuccess) return err;
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+    if ((ready.load(std::memory_order_relaxed) & bit) == 0) {
+        err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (err != cudaSuccess) return err;
+        ready.fetch_or(bit, std::memory_order_relaxed);
+    }
     return launch_pdl(kernel, grid, kThreadsAttn, smem, st, pdl_enabled(), p);
 }
 
@@ -32,11 +41,11 @@ cudaError_t launch_bf16(
     Kernel which, bool wide, const Params &p, unsigned grid, cudaStream_t st) {
     switch (which) {
     case Kernel::forward:
-        return wide ? launch(attention_fwd_kernel<T, 128>, fwd_smem<128>(), p, grid, st) : launch(attention_fwd_kernel<T, 64>, fwd_smem<64>(), p, grid, st);
+        return wide ? launch<attention_fwd_kernel<T, 128>, fwd_smem<128>()>(p, grid, st) : launch<attention_fwd_kernel<T, 64>, fwd_smem<64>()>(p, grid, st);
     case Kernel::dq:
-        return wide ? launch(attention_dq_kernel<T, 128>, dq_smem<128>(), p, grid, st) : launch(attention_dq_kernel<T, 64>, dq_smem<64>(), p, grid, st);
+        return wide ? launch<attention_dq_kernel<T, 128>, dq_smem<128>()>(p, grid, st) : launch<attention_dq_kernel<T, 64>, dq_smem<64>()>(p, grid, st);
     default:
-        return wide ? launch(attention_dkv_kernel<T, 128>, dkv_smem<128>(), p, grid, st) : launch(attention_dkv_kernel<T, 64>, dkv_smem<64>(), p, grid, st);
+        return wide ? launch<attention_dkv_kernel<T, 128>, dkv_smem<128>()>(p, grid, st) : launch<attention_dkv_kernel<T, 64>, dkv_smem<64>()>(p, grid, st);
     }
 }
 

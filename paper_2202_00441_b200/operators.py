@@ -5,11 +5,12 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import struct
 from typing import Optional, Sequence
 
 import torch
 
-from .binding import _DTYPES, _check, _current, _stream_ptr, load_library
+from .binding import _DTYPES, _check, _stream_ptr, load_library
 
 
 class _Heads(ctypes.Structure):
@@ -44,64 +45,121 @@ class _AdamWOptions(ctypes.Structure):
                 ("seed", ctypes.c_uint32), ("state_bits", ctypes.c_int), ("dtype", ctypes.c_int)]
 
 
-_NO_STREAM = contextlib.nullcontext()
+# The structs of a call are packed into one buffer: a small tensor's kernel takes less time than ctypes needs to fill
+# structs field by field.  Same fields in the same order, native alignment.
+_HEADS = struct.Struct("@Pqqq")
+_QK_SHAPE = struct.Struct("@qqiiiiiPiqPPPPfi")
+_ATTENTION_SHAPE = struct.Struct("@iiiiqqqqPPifi")
+for _packed, _fields in ((_HEADS, _Heads), (_QK_SHAPE, _QkShape), (_ATTENTION_SHAPE, _AttentionShape)):
+    assert ctypes.sizeof(_fields) - 7 <= _packed.size <= ctypes.sizeof(_fields)   # less padding at the end
+_SHAPE_ROOM = 128                                   # a shape, then the heads
+_Buffer = ctypes.c_char * (_SHAPE_ROOM + 9 * _HEADS.size)
 
 
-def _on(stream: Optional[torch.cuda.Stream], *tensors):
-    """Context in which outputs of a call on `stream` are allocated: they belong to that stream, and the memory of
-    the call's inputs is not handed out again before the call has read it."""
-    if stream is None:
-        return _NO_STREAM
+def _put_heads(buf, first: int, tensors) -> list:
+    """Packs the descriptions of `tensors` ((.., length, heads, head_dim), contiguous heads) into places first, first + 1, ...
+    of the buffer; returns their addresses."""
+    at = _SHAPE_ROOM + first * _HEADS.size
+    base, out = ctypes.addressof(buf), []
     for t in tensors:
-        if t is not None:
-            t.record_stream(stream)
-    return torch.cuda.stream(stream)
+        st = t.stride()
+        if st[-1] != 1 and t.shape[-1] > 1:
+            raise ValueError("the elements of one head must be contiguous")
+        if len(st) == 4:
+            _HEADS.pack_into(buf, at, t.data_ptr(), st[0], st[1], st[2])
+        else:
+            _HEADS.pack_into(buf, at, t.data_ptr(), 0, st[0], st[1])
+        out.append(base + at)
+        at += _HEADS.size
+    return out
+
+
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+class _On:
+    """Context of a call on `device` and, when given, on `stream`: outputs are allocated for that stream, and the memory
+    of the call's inputs is not handed out again before the call has read it."""
+
+    def __init__(self, device, stream, tensors):
+        self.inner = []
+        if device.index != _get_device():
+            self.inner.append(torch.cuda.device(device))
+        if stream is not None:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(stream)
+            self.inner.append(torch.cuda.stream(stream))
+
+    def __enter__(self):
+        for c in self.inner:
+            c.__enter__()
+
+    def __exit__(self, *exc):
+        for c in reversed(self.inner):
+            c.__exit__(*exc)
+        return False
+
+
+_PLAIN = contextlib.nullcontext()
+
+
+def _on(device, stream, *tensors):
+    if stream is None and device.index == _get_device():
+        return _PLAIN
+    return _On(device, stream, tensors)
 
 
 def _need(t: torch.Tensor, name: str, device, dtype=None) -> torch.Tensor:
-    if not t.is_cuda or t.device != device or (dtype is not None and t.dtype != dtype):
-        raise ValueError(f"{name} must be a {dtype or ''} CUDA tensor on {device}")
+    if t.device != device or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name} must be a {dtype or ''} tensor on {device}")
     return t
 
 
-def _heads(t: torch.Tensor, name: str) -> _Heads:
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError(f"the elements of one head of {name} must be contiguous")
-    if t.dim() == 4:
-        return _Heads(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
-    return _Heads(t.data_ptr(), 0, t.stride(0), t.stride(1))
+def _pointer(t: Optional[torch.Tensor]) -> int:
+    return 0 if t is None else t.data_ptr()
 
 
 # ---------------------------------------------------------------------------------------------------------------
 # norm of queries and keys with the position rotation
 # ---------------------------------------------------------------------------------------------------------------
 
-def _qk_shape(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved) -> _QkShape:
-    if q.dim() != 4 or k.dim() != 4 or q.shape[:2] != k.shape[:2] or q.shape[3] != k.shape[3] or q.dtype not in _DTYPES:
-        raise ValueError("q and k must be (batch, length, heads, head_dim) tensors of one float32, bfloat16 or float16 type, "
-                         "with the same batch, length and head_dim")
-    dev = q.device
-    _need(q, "q", dev), _need(k, "k", dev, q.dtype)
+def _qk_shape(buf, q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved):
+    """Checks the inputs and packs their shape; returns their device."""
+    dtype, dev = q.dtype, q.device
+    if q.dim() != 4 or k.dim() != 4 or dtype not in _DTYPES or not q.is_cuda:
+        raise ValueError("q and k must be (batch, length, heads, head_dim) CUDA tensors of float32, bfloat16 or float16")
     b, n, h, d = q.shape
-    for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if w is not None and (_need(w, name, dev, torch.float32).shape != (d,) or not w.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous vector of head_dim values")
-    s = _QkShape(b, n, h, k.shape[2], d, 0, int(bool(interleaved)), None, 0, 0, None, None,
-                 None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(),
-                 float(eps), _DTYPES[q.dtype])
-    if (cos is None) != (sin is None):
+    kb, kn, hk, kd = k.shape
+    if b != kb or n != kn or d != kd or k.dtype != dtype or k.device != dev:
+        raise ValueError("q and k must have one type and device, and the same batch, length and head_dim")
+    for w in (q_weight, k_weight):
+        if w is not None and (w.dtype != torch.float32 or w.device != dev or w.dim() != 1 or w.numel() != d or not w.is_contiguous()):
+            raise ValueError("q_weight and k_weight must be contiguous float32 vectors of head_dim values on the device of q")
+    rows = rot = wide = 0
+    if cos is not None and sin is not None:
+        if cos.dim() != 2 or cos.shape != sin.shape or not (cos.is_contiguous() and sin.is_contiguous()) or \
+                cos.dtype != torch.float32 or sin.dtype != torch.float32 or cos.device != dev or sin.device != dev:
+            raise ValueError("cos and sin must be contiguous float32 (rows, rotary_dim / 2) tables on the device of q")
+        rows, rot = cos.shape
+    elif cos is not None or sin is not None:
         raise ValueError("cos and sin come together")
-    if cos is not None:
-        if cos.dim() != 2 or cos.shape != sin.shape or not (cos.is_contiguous() and sin.is_contiguous()):
-            raise ValueError("cos and sin must be contiguous (rows, rotary_dim / 2) tables")
-        _need(cos, "cos", dev, torch.float32), _need(sin, "sin", dev, torch.float32)
-        s.table_rows, s.rotary_dim, s.cos, s.sin = cos.shape[0], 2 * cos.shape[1], cos.data_ptr(), sin.data_ptr()
     if positions is not None:
-        if positions.shape != (b, n) or positions.dtype not in (torch.int32, torch.int64) or not positions.is_contiguous():
-            raise ValueError("positions must be a contiguous (batch, length) tensor of int32 or int64")
-        _need(positions, "positions", dev)
-        s.positions, s.positions_are_64bit = positions.data_ptr(), int(positions.dtype == torch.int64)
-    return s
+        wide = positions.dtype == torch.int64
+        if positions.shape != (b, n) or not (wide or positions.dtype == torch.int32) or not positions.is_contiguous() or positions.device != dev:
+            raise ValueError("positions must be a contiguous (batch, length) tensor of int32 or int64 on the device of q")
+    _QK_SHAPE.pack_into(buf, 0, b, n, h, hk, d, 2 * rot, bool(interleaved), _pointer(positions), wide, rows, _pointer(cos), _pointer(sin),
+                        _pointer(q_weight), _pointer(k_weight), eps, _DTYPES[dtype])
+    return dev
+
+
+def _two_outputs(q, k, out, dev, dtype):
+    if out is None:
+        return q.new_empty(q.shape), k.new_empty(k.shape)
+    a, b = out
+    if a.shape != q.shape or b.shape != k.shape:
+        raise ValueError("out does not match q and k")
+    return _need(a, "out[0]", dev, dtype), _need(b, "out[1]", dev, dtype)
 
 
 def fewbit_qk_norm_rope_fwd(q: torch.Tensor, k: torch.Tensor, q_weight: Optional[torch.Tensor], k_weight: Optional[torch.Tensor],
@@ -115,16 +173,12 @@ def fewbit_qk_norm_rope_fwd(q: torch.Tensor, k: torch.Tensor, q_weight: Optional
     rotation; ``positions`` (batch, length) picks their rows (a position past the tables makes its heads NaN), without it
     token i has position i.  ``interleaved``: neighbouring elements are rotated with each other instead of the two
     halves.  ``out``: a pair of tensors to write to (q and k themselves are allowed)."""
-    s = _qk_shape(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
-    with _current(q.device), _on(stream, q, k, q_weight, k_weight, cos, sin, positions):
-        q_out, k_out = out if out is not None else (torch.empty(q.shape, dtype=q.dtype, device=q.device),
-                                                    torch.empty(k.shape, dtype=k.dtype, device=k.device))
-        if q_out.shape != q.shape or k_out.shape != k.shape:
-            raise ValueError("out does not match q and k")
-        _need(q_out, "q_out", q.device, q.dtype), _need(k_out, "k_out", q.device, q.dtype)
-        hs = [_heads(t, name) for t, name in ((q, "q"), (k, "k"), (q_out, "q_out"), (k_out, "k_out"))]
-        _check(load_library().fewbit_qk_norm_rope_fwd(ctypes.byref(s), *map(ctypes.byref, hs), _stream_ptr(stream, q.device)),
-               "fewbit_qk_norm_rope_fwd")
+    buf = _Buffer()
+    dev = _qk_shape(buf, q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
+    with _on(dev, stream, q, k, q_weight, k_weight, cos, sin, positions):
+        q_out, k_out = _two_outputs(q, k, out, dev, q.dtype)
+        hs = _put_heads(buf, 0, (q, k, q_out, k_out))
+        _check(load_library().fewbit_qk_norm_rope_fwd(ctypes.addressof(buf), *hs, _stream_ptr(stream, dev)), "fewbit_qk_norm_rope_fwd")
     return q_out, k_out
 
 
@@ -135,57 +189,61 @@ def fewbit_qk_norm_rope_bwd(grad_q_out: torch.Tensor, grad_k_out: torch.Tensor, 
                             stream: Optional[torch.cuda.Stream] = None):
     """Gradients of ``fewbit_qk_norm_rope_fwd`` from its inputs and the gradients of its outputs; returns
     (grad_q, grad_k, grad_q_weight, grad_k_weight), the last two float32 (None without ``weight_grads``)."""
-    s = _qk_shape(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
+    buf = _Buffer()
+    dev = _qk_shape(buf, q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
     if grad_q_out.shape != q.shape or grad_k_out.shape != k.shape:
         raise ValueError("the gradients do not match q and k")
-    dev = q.device
     _need(grad_q_out, "grad_q_out", dev, q.dtype), _need(grad_k_out, "grad_k_out", dev, q.dtype)
-    lib = load_library()
-    with _current(dev), _on(stream, grad_q_out, grad_k_out, q, k, q_weight, k_weight, cos, sin, positions):
-        grad_q, grad_k = out if out is not None else (torch.empty(q.shape, dtype=q.dtype, device=dev),
-                                                      torch.empty(k.shape, dtype=k.dtype, device=dev))
-        if grad_q.shape != q.shape or grad_k.shape != k.shape:
-            raise ValueError("out does not match q and k")
-        _need(grad_q, "grad_q", dev, q.dtype), _need(grad_k, "grad_k", dev, q.dtype)
-        dw, dw_ptr, ws, ws_bytes = (None, None), (None, None), None, 0
+    lib, base = load_library(), ctypes.addressof(buf)
+    with _on(dev, stream, grad_q_out, grad_k_out, q, k, q_weight, k_weight, cos, sin, positions):
+        grad_q, grad_k = _two_outputs(q, k, out, dev, q.dtype)
+        grad_qw = grad_kw = ws = None
+        ws_bytes = 0
         if weight_grads:
-            both = torch.empty(2, q.shape[-1], dtype=torch.float32, device=dev)
-            dw = (both[0], both[1])
-            dw_ptr = (both.data_ptr(), both.data_ptr() + 4 * q.shape[-1])
-            ws_bytes = lib.fewbit_qk_norm_rope_workspace_bytes(ctypes.byref(s))
+            grad_qw = torch.empty(q.shape[3], dtype=torch.float32, device=dev)
+            grad_kw = torch.empty(q.shape[3], dtype=torch.float32, device=dev)
+            ws_bytes = lib.fewbit_qk_norm_rope_workspace_bytes(base)
             ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
-        hs = [_heads(t, name) for t, name in ((grad_q_out, "grad_q_out"), (grad_k_out, "grad_k_out"), (q, "q"), (k, "k"),
-                                              (grad_q, "grad_q"), (grad_k, "grad_k"))]
-        _check(lib.fewbit_qk_norm_rope_bwd(ctypes.byref(s), *map(ctypes.byref, hs), *dw_ptr, None if ws is None else ws.data_ptr(),
-                                           ws_bytes, _stream_ptr(stream, dev)), "fewbit_qk_norm_rope_bwd")
-    return grad_q, grad_k, dw[0], dw[1]
+        hs = _put_heads(buf, 0, (grad_q_out, grad_k_out, q, k, grad_q, grad_k))
+        _check(lib.fewbit_qk_norm_rope_bwd(base, *hs, _pointer(grad_qw), _pointer(grad_kw), _pointer(ws), ws_bytes, _stream_ptr(stream, dev)),
+               "fewbit_qk_norm_rope_bwd")
+    return grad_q, grad_k, grad_qw, grad_kw
 
 
 # ---------------------------------------------------------------------------------------------------------------
 # attention
 # ---------------------------------------------------------------------------------------------------------------
 
-def _attention_shape(q, k, v, causal, scale, q_offsets, k_offsets, max_q_len, max_k_len) -> _AttentionShape:
-    packed = q_offsets is not None
-    if packed != (k_offsets is not None) or packed != (max_q_len is not None) or packed != (max_k_len is not None):
+def _attention_shape(buf, q, k, v, causal, scale, q_offsets, k_offsets, max_q_len, max_k_len):
+    """Checks the inputs and packs their shape; returns their device and the shape of lse."""
+    dtype, dev = q.dtype, q.device
+    if (dtype != torch.bfloat16 and dtype != torch.float16) or not q.is_cuda:
+        raise ValueError("attention takes bfloat16 or float16 CUDA tensors")
+    if k.dtype != dtype or v.dtype != dtype or k.device != dev or v.device != dev or k.shape != v.shape:
+        raise ValueError("q, k and v must have one type and device, k and v one shape")
+    if q_offsets is None:
+        if k_offsets is not None or max_q_len is not None or max_k_len is not None:
+            raise ValueError("packed sequences need q_offsets, k_offsets, max_q_len and max_k_len, others none of them")
+        if q.dim() != 4 or k.dim() != 4:
+            raise ValueError("q, k and v must be (batch, length, heads, head_dim) tensors")
+        b, n, h, d = q.shape
+        kb, m, hk, kd = k.shape
+        if kb != b or kd != d:
+            raise ValueError("q, k and v must have the same batch and head_dim")
+        _ATTENTION_SHAPE.pack_into(buf, 0, b, h, hk, d, n, m, 0, 0, 0, 0, bool(causal), d ** -0.5 if scale is None else scale, _DTYPES[dtype])
+        return dev, (b, h, n)
+    if k_offsets is None or max_q_len is None or max_k_len is None:
         raise ValueError("packed sequences need q_offsets, k_offsets, max_q_len and max_k_len, others none of them")
-    dims = 3 if packed else 4
-    if q.dim() != dims or k.dim() != dims or k.shape != v.shape or q.shape[-1] != k.shape[-1] or (not packed and q.shape[0] != k.shape[0]):
-        raise ValueError("q, k and v must be (batch, length, heads, head_dim) tensors, or (rows, heads, head_dim) for packed "
-                         "sequences; k and v of one shape, head_dim the same for all")
-    dev = q.device
-    if q.dtype not in (torch.bfloat16, torch.float16):
-        raise ValueError("attention takes bfloat16 or float16 tensors")
-    _need(q, "q", dev), _need(k, "k", dev, q.dtype), _need(v, "v", dev, q.dtype)
-    h, hk, d = q.shape[-2], k.shape[-2], q.shape[-1]
-    scale = d ** -0.5 if scale is None else scale
-    if not packed:
-        return _AttentionShape(q.shape[0], h, hk, d, q.shape[1], k.shape[1], 0, 0, None, None, int(bool(causal)), scale, _DTYPES[q.dtype])
-    for o, name in ((q_offsets, "q_offsets"), (k_offsets, "k_offsets")):
-        if _need(o, name, dev, torch.int32).dim() != 1 or o.numel() < 1 or o.numel() != q_offsets.numel() or not o.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous vector of batch + 1 int32 values")
-    return _AttentionShape(q_offsets.numel() - 1, h, hk, d, min(max_q_len, q.shape[0]), min(max_k_len, k.shape[0]), q.shape[0], k.shape[0],
-                           q_offsets.data_ptr(), k_offsets.data_ptr(), int(bool(causal)), scale, _DTYPES[q.dtype])
+    if q.dim() != 3 or k.dim() != 3 or k.shape[2] != q.shape[2]:
+        raise ValueError("packed sequences are (rows, heads, head_dim) tensors")
+    for o in (q_offsets, k_offsets):
+        if o.dtype != torch.int32 or o.device != dev or o.dim() != 1 or o.numel() < 1 or o.numel() != q_offsets.numel() or not o.is_contiguous():
+            raise ValueError("q_offsets and k_offsets must be contiguous vectors of batch + 1 int32 values on the device of q")
+    n, h, d = q.shape
+    m, hk, _ = k.shape
+    _ATTENTION_SHAPE.pack_into(buf, 0, q_offsets.numel() - 1, h, hk, d, min(max_q_len, n), min(max_k_len, m), n, m, q_offsets.data_ptr(),
+                               k_offsets.data_ptr(), bool(causal), d ** -0.5 if scale is None else scale, _DTYPES[dtype])
+    return dev, (h, n)
 
 
 def fewbit_attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool = False, scale: Optional[float] = None,
@@ -201,16 +259,15 @@ def fewbit_attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, c
     device (batch + 1 values each) and the longest sequence's lengths ``max_q_len`` and ``max_k_len``.
     lse: float32 (batch, heads, q_len), or (heads, rows) when packed: the logarithm of each row's sum of exponentials,
     -inf for a row that sees no key (whose out is 0)."""
-    s = _attention_shape(q, k, v, causal, scale, q_offsets, k_offsets, max_q_len, max_k_len)
-    packed = q_offsets is not None
-    with _current(q.device), _on(stream, q, k, v, q_offsets, k_offsets):
-        # rows of no sequence are not written by the library: they are zero here
-        out = (torch.zeros if packed else torch.empty)(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.full((q.shape[1], q.shape[0]), -float("inf"), dtype=torch.float32, device=q.device) if packed else \
-            torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
-        hs = [_heads(t, name) for t, name in ((q, "q"), (k, "k"), (v, "v"), (out, "out"))]
-        _check(load_library().fewbit_attention_fwd(ctypes.byref(s), *map(ctypes.byref, hs), lse.data_ptr(), _stream_ptr(stream, q.device)),
-               "fewbit_attention_fwd")
+    buf = _Buffer()
+    dev, stats = _attention_shape(buf, q, k, v, causal, scale, q_offsets, k_offsets, max_q_len, max_k_len)
+    with _on(dev, stream, q, k, v, q_offsets, k_offsets):
+        if q_offsets is None:
+            out, lse = q.new_empty(q.shape), torch.empty(stats, dtype=torch.float32, device=dev)
+        else:                                                # rows of no sequence are not written by the library
+            out, lse = q.new_zeros(q.shape), torch.full(stats, -float("inf"), dtype=torch.float32, device=dev)
+        hs = _put_heads(buf, 0, (q, k, v, out))
+        _check(load_library().fewbit_attention_fwd(ctypes.addressof(buf), *hs, lse.data_ptr(), _stream_ptr(stream, dev)), "fewbit_attention_fwd")
     return out, lse
 
 
@@ -221,24 +278,21 @@ def fewbit_attention_bwd(grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tenso
                          stream: Optional[torch.cuda.Stream] = None):
     """Gradients (grad_q, grad_k, grad_v) of ``fewbit_attention_fwd`` from its inputs and outputs and ``grad_out``; the
     probabilities are recomputed.  The same inputs give the same bits."""
-    s = _attention_shape(q, k, v, causal, scale, q_offsets, k_offsets, max_q_len, max_k_len)
-    packed = q_offsets is not None
-    dev = q.device
-    stats = (q.shape[1], q.shape[0]) if packed else (q.shape[0], q.shape[2], q.shape[1])
+    buf = _Buffer()
+    dev, stats = _attention_shape(buf, q, k, v, causal, scale, q_offsets, k_offsets, max_q_len, max_k_len)
     if grad_out.shape != q.shape or out.shape != q.shape or lse.shape != stats or not lse.is_contiguous():
         raise ValueError("grad_out, out and lse must have the shapes that the forward pass gives")
     _need(grad_out, "grad_out", dev, q.dtype), _need(out, "out", dev, q.dtype), _need(lse, "lse", dev, torch.float32)
-    lib = load_library()
-    with _current(dev), _on(stream, grad_out, q, k, v, out, lse, q_offsets, k_offsets):
-        new = torch.zeros if packed else torch.empty
-        grads = [new(t.shape, dtype=q.dtype, device=dev) for t in (q, k, v)]
-        ws_bytes = 4 * lse.numel()
-        ws = torch.empty(lse.numel(), dtype=torch.float32, device=dev)
-        hs = [_heads(t, name) for t, name in ((grad_out, "grad_out"), (q, "q"), (k, "k"), (v, "v"), (out, "out"))]
-        gs = [_heads(t, name) for t, name in zip(grads, ("grad_q", "grad_k", "grad_v"))]
-        _check(lib.fewbit_attention_bwd(ctypes.byref(s), *map(ctypes.byref, hs), lse.data_ptr(), *map(ctypes.byref, gs), ws.data_ptr(),
-                                        ws_bytes, _stream_ptr(stream, dev)), "fewbit_attention_bwd")
-    return tuple(grads)
+    with _on(dev, stream, grad_out, q, k, v, out, lse, q_offsets, k_offsets):
+        if q_offsets is None:
+            grads = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
+        else:
+            grads = q.new_zeros(q.shape), k.new_zeros(k.shape), v.new_zeros(v.shape)
+        ws = torch.empty(stats, dtype=torch.float32, device=dev)
+        hs = _put_heads(buf, 0, (grad_out, q, k, v, out, *grads))
+        _check(load_library().fewbit_attention_bwd(ctypes.addressof(buf), *hs[:5], lse.data_ptr(), *hs[5:], ws.data_ptr(), 4 * ws.numel(),
+                                                   _stream_ptr(stream, dev)), "fewbit_attention_bwd")
+    return grads
 
 
 def fewbit_attention_timeout_count(device=None) -> int:
@@ -334,8 +388,6 @@ def fewbit_adamw_step(tensors: AdamWTensors, grads: Sequence[torch.Tensor], *, s
         raise ValueError("grad_scale must be one value")
     o = _AdamWOptions(lr, betas[0], betas[1], eps, weight_decay, step, None if grad_scale is None else grad_scale.data_ptr(),
                       seed & 0xFFFFFFFF, tensors.bits, _DTYPES[dtype])
-    if stream is not None:
-        _on(stream, grad_scale, *grads, *tensors.tensors())
-    with _current(device):
+    with _on(device, stream, grad_scale, *grads, *(tensors.tensors() if stream is not None else ())):
         _check(load_library().fewbit_adamw_step(tensors._descs, into, n, ctypes.byref(o), _stream_ptr(stream, device)),
                "fewbit_adamw_step")
