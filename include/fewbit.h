@@ -351,7 +351,8 @@ FEWBIT_API fewbit_status fewbit_qk_norm_rope_bwd(const fewbit_qk_shape *shape, c
  *                   of q and keys [k_offsets[b], k_offsets[b+1]) of k and v,
  *                   in tensors of q_rows and k_rows rows (batch_stride is not
  *                   used); q_len and k_len are then upper bounds of the
- *                   sequences' lengths.  Rows of no sequence are not written.
+ *                   sequences' lengths.  Rows in front of the first and behind
+ *                   the last sequence get zeros (lse: -inf).
  *                   Offsets are clamped to [0, q_rows] / [0, k_rows], lengths to
  *                   [0, q_len] / [0, k_len].
  *   scale           finite, > 0
@@ -376,7 +377,7 @@ typedef struct fewbit_attention_shape {
 FEWBIT_API fewbit_status fewbit_attention_fwd(const fewbit_attention_shape *shape, const fewbit_heads *q, const fewbit_heads *k,
                                               const fewbit_heads *v, const fewbit_heads *out, float *lse, void *stream);
 
-/* Bytes of `workspace` for the backward pass (one binary32 value for each row and head); 0 for a bad shape. */
+/* Bytes of `workspace` for the backward pass (1 KB for each 128 rows of each head); 0 for a bad shape. */
 FEWBIT_API size_t fewbit_attention_workspace_bytes(const fewbit_attention_shape *shape);
 
 /*

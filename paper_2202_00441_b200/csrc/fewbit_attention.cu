@@ -7,6 +7,8 @@
 #include <atomic>
 
 namespace fewbit {
+int device_sm_count(cudaError_t *err);
+
 namespace {
 
 using attn::Params;
@@ -127,7 +129,7 @@ fewbit_status fill(const fewbit_attention_shape *s, const Sizes &z, Params *p) {
 
 fewbit_status run(attn::Kernel which, const fewbit_attention_shape *s, Params &p, int64_t tiles, int heads, void *stream) {
     p.tiles = static_cast<int>(tiles);
-    const unsigned grid = static_cast<unsigned>(tiles * heads * s->batch);
+    const unsigned grid = static_cast<unsigned>(tiles * heads * (s->batch + (p.q_offsets != nullptr)));   // one more for rows of no sequence
     if (grid == 0) return FEWBIT_OK;
     const cudaError_t err = (s->dtype == FEWBIT_F16 ? attn::launch_f16 : attn::launch_bf16)(which, s->head_dim > 64, p, grid, static_cast<cudaStream_t>(stream));
     if (err == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
@@ -166,7 +168,8 @@ size_t fewbit_attention_workspace_bytes(const fewbit_attention_shape *s) {
     using namespace fewbit;
     Sizes z;
     if (check_shape(s, &z) != FEWBIT_OK) return 0;
-    return static_cast<size_t>(z.batch) * s->heads * z.q_rows * sizeof(float);
+    const size_t tiles = z.packed ? static_cast<size_t>(z.q_rows / attn::kTile + s->batch + 1) : static_cast<size_t>((s->q_len + attn::kTile - 1) / attn::kTile) * s->batch;
+    return tiles * s->heads * attn::kStatBytes;
 }
 
 fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *s, const fewbit_heads *grad_out, const fewbit_heads *q, const fewbit_heads *k,
@@ -197,10 +200,18 @@ fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *s, const fewbit
     p.dk = rows_of(grad_k);
     p.dv = rows_of(grad_v);
     p.lse = const_cast<float *>(lse);
-    p.delta = static_cast<float *>(workspace);
+    p.stat = static_cast<float *>(workspace);
     st = run(attn::Kernel::dq, s, p, (s->q_len + attn::kTile - 1) / attn::kTile, s->heads, stream);
     if (st != FEWBIT_OK) return st;
-    return run(attn::Kernel::dkv, s, p, (s->k_len + attn::kTile - 1) / attn::kTile, s->kv_heads, stream);
+    // A key tile's row tiles are dealt out to a cluster of up to 4 CTAs while the grid is under two CTAs for each SM: fewer
+    // leave SMs idle, or one long (causal) CTA alone at the end.
+    cudaError_t err = cudaSuccess;
+    const int64_t sms = device_sm_count(&err), key_tiles = (s->k_len + attn::kTile - 1) / attn::kTile;
+    if (err != cudaSuccess) return cuda_status(err);
+    const int64_t iterations = (s->q_len + attn::kTile - 1) / attn::kTile * p.group;   // of one key tile, at most
+    p.split = 1;
+    while (p.split < 4 && key_tiles * s->kv_heads * s->batch * p.split < 2 * sms && iterations >= 4 * p.split) p.split *= 2;
+    return run(attn::Kernel::dkv, s, p, key_tiles, s->kv_heads, stream);
 }
 
 fewbit_status fewbit_attention_timeout_count(uint64_t *count) {

@@ -11,10 +11,14 @@
 // tensor memory, so nothing element-wise ever touches shared memory.
 //
 //   forward   two row tiles a CTA: one tile's softmax runs while the other's products do
-//   dQ        one row tile against all keys: S, dP, dQ (3 products); writes delta for the next kernel
-//   dK, dV    one key tile against all rows of all query heads that share it: S^T, dP^T, dV, dK (4 products)
+//   dQ        one row tile against all keys: S, dP, dQ (3 products); writes the rows' -lse and -delta for the next kernel
+//   dK, dV    one key tile against all rows of all query heads that share it: S^T, dP^T, dV, dK (4 products); a
+//             cluster of 1, 2 or 4 CTAs takes the row tiles in turn and adds up through distributed shared memory
 // S and dP are computed in both backward kernels (7 products where 5 would do): in exchange nothing is added
 // with atomics, so no binary32 copy of dQ is zeroed, summed and converted, and results are the same every time.
+//
+// A 128 x 128 x 128 product takes 512 clocks of the tensor cores, 16384 exponentials 1024 of the exponential unit; a
+// quarter of the latter are computed on the FMA pipe instead.
 #pragma once
 
 #include <climits>
@@ -29,8 +33,12 @@ namespace attn {
 using namespace tc;
 
 constexpr int kTile = 128;
-constexpr int kThreadsAttn = 320;
+constexpr int kThreadsAttn = 384;      // three warpgroups: two element-wise ones, and the MMA and load warps (two idle ones fill it up)
 constexpr int kMmaWarp = 8, kLoadWarp = 9;
+// 168 registers a thread at launch: 2 x 128 x 208 + 128 x 80 = 63488 of 64512
+constexpr int kWorkRegisters = 208, kIssueRegisters = 80;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kStatBytes = 2 * kTile * 4;   // a row tile's -lse * log2(e) and -delta
 
 struct Rows {                         // an output tensor
     void *p;
@@ -39,13 +47,14 @@ struct Rows {                         // an output tensor
 struct Params {
     CUtensorMap q, k, v, g;           // g: the gradient of the output
     Rows out, o, go, dq, dk, dv;      // o, go: outputs and their gradients, read row by row for delta
-    float *lse, *delta;
+    float *lse, *stat;                // stat: a block of kStatBytes for each row tile
     const int *q_offsets, *k_offsets;
     unsigned int *timeouts;
     long long q_rows, k_rows;
     int batch, heads, kv_heads, group, dim;
     int q_len, k_len;                 // of every sequence, or the most of any
     int tiles;                        // row or key tiles (of the kernel's size) in q_len or k_len
+    int split;                        // CTAs of a cluster that share a key tile (dK, dV)
     bool causal;
     float scale, scale_log2;          // scale * log2(e)
 };
@@ -58,18 +67,21 @@ struct Work {
     bool packed;
 };
 
-__device__ __forceinline__ Work find_work(const Params &p, int heads, bool last_first) {
+// `block`: the CTA's (or its cluster's) place in the grid.  Packed sequences have one more "sequence", number
+// `batch`: the rows that belong to none.
+__device__ __forceinline__ Work find_work(const Params &p, int block, int heads, bool last_first) {
     Work w;
-    const int pairs = heads * p.batch;
-    const int t = blockIdx.x / pairs, rest = blockIdx.x % pairs;
+    w.packed = p.q_offsets != nullptr;
+    const int pairs = heads * (p.batch + (w.packed ? 1 : 0));
+    const int t = block / pairs, rest = block % pairs;
     w.tile = last_first ? p.tiles - 1 - t : t;
     w.head = rest % heads;
     w.batch = rest / heads;
-    w.packed = p.q_offsets != nullptr;
     w.q_len = p.q_len;
     w.k_len = p.k_len;
     w.q_first = w.k_first = 0;
     w.q_batch = w.batch;
+    if (w.packed && w.batch == p.batch) return w;
     if (w.packed) {                   // offsets outside the tensors are cut to them: no access depends on their being right
         const long long q0 = min(max(static_cast<long long>(p.q_offsets[w.batch]), 0ll), p.q_rows);
         const long long q1 = min(max(static_cast<long long>(p.q_offsets[w.batch + 1]), q0), p.q_rows);
@@ -139,19 +151,42 @@ __device__ __forceinline__ void zero_columns(T *row, int dim) {
 __device__ __forceinline__ long long row_of(const Work &w, const Rows &t, int head, int i, int first) {
     return (w.packed ? 0 : w.batch * t.b) + (static_cast<long long>(first) + i) * t.i + head * t.h;
 }
-// Place of a row's lse and delta: (batch, heads, q_len), or (heads, rows) for packed sequences.
+// Block of a row tile in `stat`: (batch, heads, tiles), or (heads, rows / 128 + sequences + 1) for packed sequences, whose
+// tile t starts at block first / 128 + sequence (a sequence has at most one tile more than whole tiles of rows).
+__device__ __forceinline__ float *stat_block(const Params &p, const Work &w, int head, int tile) {
+    const long long at = w.packed ? static_cast<long long>(head) * (p.q_rows / kTile + p.batch + 1) + w.q_first / kTile + w.batch + tile
+                                  : (static_cast<long long>(w.batch) * p.heads + head) * ((p.q_len + kTile - 1) / kTile) + tile;
+    return p.stat + at * (kStatBytes / 4);
+}
+// Packed sequences: rows in front of the first and behind the last one are zero in every output, their lse -inf.
+// The CTAs of the extra sequence share them.
+template <typename T>
+__device__ __forceinline__ void fill_outside(const Params &p, const Work &w, const int *offsets, long long rows, const Rows &t, float *lse) {
+    const long long first = min(max(static_cast<long long>(offsets[0]), 0ll), rows);
+    const long long last = min(max(static_cast<long long>(offsets[p.batch]), first), rows);
+    for (long long i = static_cast<long long>(w.tile) * kThreadsAttn + threadIdx.x; i < first + rows - last;
+         i += static_cast<long long>(p.tiles) * kThreadsAttn) {
+        const long long row = i < first ? i : last + (i - first);
+        zero_columns<T>(static_cast<T *>(t.p) + row * t.i + w.head * t.h, p.dim);
+        if (lse != nullptr) lse[static_cast<long long>(w.head) * rows + row] = -INFINITY;
+    }
+}
+
+// Place of a row's lse: (batch, heads, q_len), or (heads, rows) for packed sequences.
 __device__ __forceinline__ long long stat_of(const Params &p, const Work &w, int head, int i) {
     return w.packed ? static_cast<long long>(head) * p.q_rows + w.q_first + i
                     : (static_cast<long long>(w.batch) * p.heads + head) * p.q_len + i;
 }
 
-__device__ __forceinline__ uint32_t start_cta(Sync *sync, int barriers, const uint32_t *counts, bool alloc) {
+__device__ __forceinline__ bool stopped(const Sync *sync) { return *reinterpret_cast<const volatile int *>(&sync->stop) != 0; }
+
+__device__ __forceinline__ uint32_t start_cta(Sync *sync, int barriers, const uint32_t *counts) {
     if (threadIdx.x == 0) {
         sync->stop = 0;
         for (int i = 0; i < barriers; ++i) barrier_init(smem_address(&sync->bar[i]), counts[i]);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (alloc && threadIdx.x / 32 == kMmaWarp) tmem_alloc(smem_address(&sync->tmem), 512);
+    if (threadIdx.x / 32 == kMmaWarp) tmem_alloc(smem_address(&sync->tmem), 512);
     fence_before();
     __syncthreads();
     fence_after();
@@ -168,10 +203,26 @@ __device__ __forceinline__ void end_cta(uint32_t tmem) {
 // ---------------------------------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------------------------------
-// Barriers: q (2 row tiles), k full/empty (2 stages), v full/empty, S full (2), P ready (2), O done (2), drained.
-enum { fQ = 0, fKFull = 2, fKEmpty = 4, fVFull = 6, fVEmpty = 8, fS = 10, fP = 12, fO = 14, fDrain = 16, fBars = 17 };
+// Barriers: q (2 row tiles), k full/empty (2 stages), v full/empty, S full (2), first three quarters of P ready (2), all of
+// it (2), O done (2), drained.
+enum { fQ = 0, fKFull = 2, fKEmpty = 4, fVFull = 6, fVEmpty = 8, fS = 10, fP = 12, fPEnd = 14, fO = 16, fDrain = 18, fBars = 19 };
 
 template <int DIM> constexpr int fwd_smem() { return 6 * (DIM / 64) * static_cast<int>(kHalfTile) + 1024 + static_cast<int>(sizeof(Sync)); }
+
+// 32 columns of a row: probabilities, rounded to `s_at`, and their sum.  MIXED: a quarter of them on the FMA pipe.
+template <typename T, bool MIXED>
+__device__ __forceinline__ void fwd_probabilities(const uint32_t *s, float scale, float shift, float (&part)[4], uint32_t at) {
+    uint32_t r[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        float a, b;
+        if (MIXED && e % 4 == 3) exp2_scaled<true>(a, b, __uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]), scale, shift, shift);
+        else exp2_scaled<false>(a, b, __uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]), scale, shift, shift);
+        add2(part[2 * (e & 1)], part[2 * (e & 1) + 1], part[2 * (e & 1)], part[2 * (e & 1) + 1], a, b);
+        r[e] = pack2<T>(a, b);
+    }
+    tmem_st16(at, r);
+}
 
 template <typename T, int DIM>
 __global__ void __launch_bounds__(kThreadsAttn, 1)
@@ -183,7 +234,11 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
     Sync *sync = reinterpret_cast<Sync *>(raw + (base - smem_address(raw)) + 6 * kBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
-    const Work w = find_work(p, p.heads, true);
+    const Work w = find_work(p, blockIdx.x, p.heads, true);
+    if (w.packed && w.batch == p.batch) {
+        fill_outside<T>(p, w, p.q_offsets, p.q_rows, p.out, p.lse);
+        return;
+    }
     const int q0 = w.tile * 2 * kTile;
     if (q0 >= w.q_len) return;                                        // packed: a shorter sequence
     const int kv_head = w.head / p.group;
@@ -192,94 +247,104 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
     const int n1 = q0 + kTile < w.q_len ? key_tiles(p, w, min(q0 + 2 * kTile, w.q_len) - 1) : 0;
     const int n = max(n0, n1);
 
-    constexpr uint32_t counts[fBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 4, 4, 1, 1, 1};
-    const uint32_t tmem = start_cta(sync, fBars, counts, true);
+    constexpr uint32_t counts[fBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 4, 4, 4, 4, 1, 1, 1};
+    const uint32_t tmem = start_cta(sync, fBars, counts);
     auto bar = [&](int i) { return smem_address(&sync->bar[i]); };
     auto wait = [&](int i, uint32_t parity) { return barrier_wait(bar(i), parity, &sync->stop, p.timeouts); };
     const uint32_t sm_q = base, sm_k = base + 2 * kBytes, sm_v = base + 4 * kBytes;
     // tensor memory: S (and P in its first half) of both row tiles, then O of both
     const uint32_t tm_s = tmem, tm_o = tmem + 2 * kTile;
 
-    if (warp == kLoadWarp) {
-        int issued_k = 0, issued_v = 0;
-        if (n > 0 && lane == 0) {
-            prefetch_map(&p.q);
-            prefetch_map(&p.k);
-            prefetch_map(&p.v);
-            barrier_expect(bar(fQ), kBytes);
-            load_halves<HALVES>(sm_q, &p.q, w.q_first + q0, w.head, w.q_batch, bar(fQ));
-            if (n1 > 0) {
-                barrier_expect(bar(fQ + 1), kBytes);
-                load_halves<HALVES>(sm_q + kBytes, &p.q, w.q_first + q0 + kTile, w.head, w.q_batch, bar(fQ + 1));
+    if (warp >= kMmaWarp) {
+        give_registers<kIssueRegisters>();
+        if (warp == kLoadWarp) {
+            int issued_k = 0, issued_v = 0;
+            if (n > 0 && lane == 0) {
+                prefetch_map(&p.q);
+                prefetch_map(&p.k);
+                prefetch_map(&p.v);
+                barrier_expect(bar(fQ), kBytes);
+                load_halves<HALVES>(sm_q, &p.q, w.q_first + q0, w.head, w.q_batch, bar(fQ));
+                if (n1 > 0) {
+                    barrier_expect(bar(fQ + 1), kBytes);
+                    load_halves<HALVES>(sm_q + kBytes, &p.q, w.q_first + q0 + kTile, w.head, w.q_batch, bar(fQ + 1));
+                }
             }
-        }
-        for (int j = 0; j < n; ++j) {
-            const int s = j & 1;
-            const uint32_t again = ((j >> 1) & 1) ^ 1;                // the stage's previous tile has been used
-            if (!wait(fKEmpty + s, again)) break;
-            if (lane == 0) {
-                barrier_expect(bar(fKFull + s), kBytes);
-                load_halves<HALVES>(sm_k + s * kBytes, &p.k, w.k_first + j * kTile, kv_head, w.q_batch, bar(fKFull + s));
-            }
-            issued_k = j + 1;
-            if (!wait(fVEmpty + s, again)) break;
-            if (lane == 0) {
-                barrier_expect(bar(fVFull + s), kBytes);
-                load_halves<HALVES>(sm_v + s * kBytes, &p.v, w.k_first + j * kTile, kv_head, w.q_batch, bar(fVFull + s));
-            }
-            issued_v = j + 1;
-        }
-        if (sync->stop) {                                             // given up somewhere: let the copies land before the CTA ends
-            if (n > 0) barrier_wait(bar(fQ), 0, nullptr, p.timeouts);
-            if (n1 > 0) barrier_wait(bar(fQ + 1), 0, nullptr, p.timeouts);
-            for (int s = 0; s < 2; ++s) {
-                if (issued_k > s) barrier_wait(bar(fKFull + s), ((issued_k - 1 - s) >> 1) & 1, nullptr, p.timeouts);
-                if (issued_v > s) barrier_wait(bar(fVFull + s), ((issued_v - 1 - s) >> 1) & 1, nullptr, p.timeouts);
-            }
-        }
-    } else if (warp == kMmaWarp) {
-        auto scores = [&](int t, int j) {                             // S of row tile t against key tile j
-            if (lane == 0) {
-                product_rows<T, DIM>(tm_s + t * kTile, sm_q + t * kBytes, sm_k + (j & 1) * kBytes);
-                commit(bar(fS + t));
-            }
-            __syncwarp();
-        };
-        bool ok = n == 0 || (wait(fQ, 0) && (n1 == 0 || wait(fQ + 1, 0)) && wait(fKFull, 0));
-        if (ok && n > 0) {
-            fence_after();
-            if (n0 > 0) scores(0, 0);
-            if (n1 > 0) scores(1, 0);
-            if (lane == 0) commit(bar(fKEmpty));
-        }
-        for (int j = 0; ok && j < n; ++j) {
-            ok = wait(fVFull + (j & 1), (j >> 1) & 1) && (j + 1 >= n || wait(fKFull + ((j + 1) & 1), ((j + 1) >> 1) & 1));
-            if (!ok) break;
-            if (w.packed && (j + 1) * kTile > w.k_len) clear_rows<HALVES>(sm_v + (j & 1) * kBytes, w.k_len - j * kTile);
-            for (int t = 0; t < 2 && ok; ++t) {
-                const int nt = t ? n1 : n0;
-                if (j >= nt) continue;
-                ok = wait(fP + t, j & 1);
-                if (!ok) break;
-                fence_after();
+            for (int j = 0; j < n; ++j) {
+                const int s = j & 1;
+                const uint32_t again = ((j >> 1) & 1) ^ 1;            // the stage's previous tile has been used
+                if (!wait(fKEmpty + s, again)) break;
                 if (lane == 0) {
-                    const uint32_t at = tm_s + t * kTile;
-                    product_columns<T, DIM>(tm_o + t * kTile, at, at + 32, sm_v + (j & 1) * kBytes, j > 0);
-                    commit(bar(fO + t));
+                    barrier_expect(bar(fKFull + s), kBytes);
+                    load_halves<HALVES>(sm_k + s * kBytes, &p.k, w.k_first + j * kTile, kv_head, w.q_batch, bar(fKFull + s));
+                }
+                issued_k = j + 1;
+                if (!wait(fVEmpty + s, again)) break;
+                if (lane == 0) {
+                    barrier_expect(bar(fVFull + s), kBytes);
+                    load_halves<HALVES>(sm_v + s * kBytes, &p.v, w.k_first + j * kTile, kv_head, w.q_batch, bar(fVFull + s));
+                }
+                issued_v = j + 1;
+            }
+            if (stopped(sync)) {                                      // given up somewhere: let the copies land before the CTA ends
+                if (n > 0) barrier_wait(bar(fQ), 0, nullptr, p.timeouts);
+                if (n1 > 0) barrier_wait(bar(fQ + 1), 0, nullptr, p.timeouts);
+                for (int s = 0; s < 2; ++s) {
+                    if (issued_k > s) barrier_wait(bar(fKFull + s), ((issued_k - 1 - s) >> 1) & 1, nullptr, p.timeouts);
+                    if (issued_v > s) barrier_wait(bar(fVFull + s), ((issued_v - 1 - s) >> 1) & 1, nullptr, p.timeouts);
+                }
+            }
+        } else if (warp == kMmaWarp) {
+            auto scores = [&](int t, int j) {                         // S of row tile t against key tile j
+                if (lane == 0) {
+                    product_rows<T, DIM>(tm_s + t * kTile, sm_q + t * kBytes, sm_k + (j & 1) * kBytes);
+                    commit(bar(fS + t));
                 }
                 __syncwarp();
-                if (j + 1 < nt) scores(t, j + 1);
+            };
+            bool ok = n == 0 || (wait(fQ, 0) && (n1 == 0 || wait(fQ + 1, 0)) && wait(fKFull, 0));
+            if (ok && n > 0) {
+                fence_after();
+                if (n0 > 0) scores(0, 0);
+                if (n1 > 0) scores(1, 0);
+                if (lane == 0) commit(bar(fKEmpty));
             }
-            if (lane == 0) {
-                commit(bar(fVEmpty + (j & 1)));
-                if (j + 1 < n) commit(bar(fKEmpty + ((j + 1) & 1)));
+            for (int j = 0; ok && j < n; ++j) {
+                ok = wait(fVFull + (j & 1), (j >> 1) & 1) && (j + 1 >= n || wait(fKFull + ((j + 1) & 1), ((j + 1) >> 1) & 1));
+                if (!ok) break;
+                if (w.packed && (j + 1) * kTile > w.k_len) clear_rows<HALVES>(sm_v + (j & 1) * kBytes, w.k_len - j * kTile);
+                for (int t = 0; t < 2 && ok; ++t) {
+                    const int nt = t ? n1 : n0;
+                    if (j >= nt) continue;
+                    const uint32_t at = tm_s + t * kTile;
+                    // the product starts on three quarters of P while the last one is computed
+                    ok = wait(fP + t, j & 1);
+                    if (!ok) break;
+                    fence_after();
+                    if (lane == 0) product_columns<T, DIM, 0, 6>(tm_o + t * kTile, at, at + 32, sm_v + (j & 1) * kBytes, j > 0);
+                    __syncwarp();
+                    ok = wait(fPEnd + t, j & 1);
+                    if (!ok) break;
+                    fence_after();
+                    if (lane == 0) {
+                        product_columns<T, DIM, 6, 8>(tm_o + t * kTile, at, at + 32, sm_v + (j & 1) * kBytes, true);
+                        commit(bar(fO + t));
+                    }
+                    __syncwarp();
+                    if (j + 1 < nt) scores(t, j + 1);
+                }
+                if (lane == 0) {
+                    commit(bar(fVEmpty + (j & 1)));
+                    if (j + 1 < n) commit(bar(fKEmpty + ((j + 1) & 1)));
+                }
+                __syncwarp();
             }
+            if (lane == 0) commit(bar(fDrain));
             __syncwarp();
+            barrier_wait(bar(fDrain), 0, nullptr, p.timeouts);
         }
-        if (lane == 0) commit(bar(fDrain));
-        __syncwarp();
-        barrier_wait(bar(fDrain), 0, nullptr, p.timeouts);
     } else {
+        take_registers<kWorkRegisters>();
         const int t = warp >> 2;                                      // row tile
         const int nt = t ? n1 : n0;
         const int i = q0 + t * kTile + (threadIdx.x & 127);           // this thread's row
@@ -298,14 +363,16 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
 #pragma unroll
             for (int c = 0; c < 4; ++c) tmem_ld32(s_at + 32 * c, s + 32 * c);
             wait_ld();
-            if ((j + 1) * kTile > tile_seen) {
+            const bool edge = (j + 1) * kTile > tile_seen;
+            if (edge) {
                 const int limit = seen - j * kTile;
 #pragma unroll
                 for (int c = 0; c < 128; ++c) s[c] = c < limit ? s[c] : 0xff800000u;
             }
             float best[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int c = 0; c < 128; ++c) best[c & 3] = fmaxf(best[c & 3], __uint_as_float(s[c]));
+            for (int c = 0; c < 128; c += 2)                          // two at a time: a three-operand maximum
+                best[(c >> 1) & 3] = fmaxf(best[(c >> 1) & 3], fmaxf(__uint_as_float(s[c]), __uint_as_float(s[c + 1])));
             const float high = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3]));
             // The sums' reference moves only when a product passes it by 2^8: until then probabilities up to 2^8
             // are held, which cost no precision, and O needs no rescaling.
@@ -328,29 +395,22 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
                         for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
                         tmem_st32(o_at + 32 * c, o);
                     }
-                    wait_st();
                 }
             }
-            const float shift = top == -INFINITY ? 0.0f : top * p.scale_log2;
+            const float shift = top == -INFINITY ? 0.0f : -top * p.scale_log2;
             float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int c = 0; c < 128; c += 64) {
-                uint32_t r[32];
-#pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    const float a = exp2_fast(fmaf(__uint_as_float(s[c + 2 * e]), p.scale_log2, -shift));
-                    const float b = exp2_fast(fmaf(__uint_as_float(s[c + 2 * e + 1]), p.scale_log2, -shift));
-                    part[2 * (e & 1)] += a;
-                    part[2 * (e & 1) + 1] += b;
-                    r[e] = pack2<T>(a, b);
+            for (int c = 0; c < 4; ++c) {
+                if (edge) fwd_probabilities<T, false>(s + 32 * c, p.scale_log2, shift, part, s_at + 16 * c);
+                else fwd_probabilities<T, true>(s + 32 * c, p.scale_log2, shift, part, s_at + 16 * c);
+                if (c >= 2) {
+                    wait_st();
+                    fence_before();
+                    __syncwarp();
+                    if (lane == 0) barrier_arrive(bar((c == 2 ? fP : fPEnd) + t));
                 }
-                tmem_st32(s_at + c / 2, r);
             }
             sum += (part[0] + part[1]) + (part[2] + part[3]);
-            wait_st();
-            fence_before();
-            __syncwarp();
-            if (lane == 0) barrier_arrive(bar(fP + t));
         }
         if (nt > 0 && ok) ok = wait(fO + t, (nt - 1) & 1);
         fence_after();
@@ -376,127 +436,125 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
 }
 
 // ---------------------------------------------------------------------------------------------------
-// backward, dQ (and delta)
+// backward, dQ (and the rows' statistics)
 // ---------------------------------------------------------------------------------------------------
-// Barriers: q and g, k full/empty (2 stages), v full/empty, S full (2), dP full, dS ready, dQ done.
-enum { qQ = 0, qKFull = 1, qKEmpty = 3, qVFull = 5, qVEmpty = 7, qS = 9, qDp = 11, qDs = 12, qDone = 13, qBars = 14 };
+// Barriers: q and g, k full/empty (3 stages: a tile is used twice, one iteration apart), v full/empty (2 stages), S full (2),
+// dP full, dS ready, dQ done.
+enum { qQ = 0, qKFull = 1, qKEmpty = 4, qVFull = 7, qVEmpty = 9, qS = 11, qDp = 13, qDs = 14, qDone = 15, qBars = 16 };
 
-template <int DIM> constexpr int dq_smem() { return 6 * (DIM / 64) * static_cast<int>(kHalfTile) + 1024 + static_cast<int>(sizeof(Sync)) + 2 * kTile * 4; }
+template <int DIM> constexpr int dq_smem() { return 7 * (DIM / 64) * static_cast<int>(kHalfTile) + static_cast<int>(sizeof(Sync)) + 2 * kTile * 4; }
 
 template <typename T, int DIM>
 __global__ void __launch_bounds__(kThreadsAttn, 1)
 attention_dq_kernel(const __grid_constant__ Params p) {
     constexpr int HALVES = DIM / 64;
     constexpr uint32_t kBytes = HALVES * kHalfTile;
-    extern __shared__ uint8_t raw[];
-    const uint32_t base = (smem_address(raw) + 1023u) & ~1023u;
-    Sync *sync = reinterpret_cast<Sync *>(raw + (base - smem_address(raw)) + 6 * kBytes);
+    extern __shared__ __align__(1024) uint8_t raw[];
+    const uint32_t base = smem_address(raw);                          // no room to align it here: the host checks
+    Sync *sync = reinterpret_cast<Sync *>(raw + 7 * kBytes);
     float *half_delta = reinterpret_cast<float *>(sync + 1);          // [2][128]
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
-    const Work w = find_work(p, p.heads, true);
+    const Work w = find_work(p, blockIdx.x, p.heads, true);
+    if (w.packed && w.batch == p.batch) {
+        fill_outside<T>(p, w, p.q_offsets, p.q_rows, p.dq, nullptr);
+        return;
+    }
     const int q0 = w.tile * kTile;
     if (q0 >= w.q_len) return;
     const int kv_head = w.head / p.group;
     const int n = key_tiles(p, w, min(q0 + kTile, w.q_len) - 1);
 
-    constexpr uint32_t counts[qBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 8, 1};
-    const uint32_t tmem = start_cta(sync, qBars, counts, true);
+    constexpr uint32_t counts[qBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 8, 1};
+    const uint32_t tmem = start_cta(sync, qBars, counts);
     auto bar = [&](int i) { return smem_address(&sync->bar[i]); };
     auto wait = [&](int i, uint32_t parity) { return barrier_wait(bar(i), parity, &sync->stop, p.timeouts); };
-    const uint32_t sm_q = base, sm_g = base + kBytes, sm_k = base + 2 * kBytes, sm_v = base + 4 * kBytes;
+    const uint32_t sm_q = base, sm_g = base + kBytes, sm_k = base + 2 * kBytes, sm_v = base + 5 * kBytes;
     // tensor memory: S twice (dS takes its place), dP, dQ
     const uint32_t tm_s = tmem, tm_dp = tmem + 2 * kTile, tm_dq = tmem + 3 * kTile;
 
-    if (warp == kLoadWarp) {
-        int issued_k = 0, issued_v = 0;
-        if (n > 0 && lane == 0) {
-            prefetch_map(&p.q);
-            prefetch_map(&p.k);
-            prefetch_map(&p.v);
-            prefetch_map(&p.g);
-            barrier_expect(bar(qQ), 2 * kBytes);
-            load_halves<HALVES>(sm_q, &p.q, w.q_first + q0, w.head, w.q_batch, bar(qQ));
-            load_halves<HALVES>(sm_g, &p.g, w.q_first + q0, w.head, w.q_batch, bar(qQ));
-        }
-        for (int j = 0; j < n; ++j) {
-            const int s = j & 1;
-            const uint32_t again = ((j >> 1) & 1) ^ 1;
-            if (!wait(qKEmpty + s, again)) break;
-            if (lane == 0) {
-                barrier_expect(bar(qKFull + s), kBytes);
-                load_halves<HALVES>(sm_k + s * kBytes, &p.k, w.k_first + j * kTile, kv_head, w.q_batch, bar(qKFull + s));
+    if (warp >= kMmaWarp) {
+        give_registers<kIssueRegisters>();
+        if (warp == kLoadWarp) {
+            int issued_k = 0, issued_v = 0;
+            if (n > 0 && lane == 0) {
+                prefetch_map(&p.q);
+                prefetch_map(&p.k);
+                prefetch_map(&p.v);
+                prefetch_map(&p.g);
+                barrier_expect(bar(qQ), 2 * kBytes);
+                load_halves<HALVES>(sm_q, &p.q, w.q_first + q0, w.head, w.q_batch, bar(qQ));
+                load_halves<HALVES>(sm_g, &p.g, w.q_first + q0, w.head, w.q_batch, bar(qQ));
             }
-            issued_k = j + 1;
-            if (!wait(qVEmpty + s, again)) break;
-            if (lane == 0) {
-                barrier_expect(bar(qVFull + s), kBytes);
-                load_halves<HALVES>(sm_v + s * kBytes, &p.v, w.k_first + j * kTile, kv_head, w.q_batch, bar(qVFull + s));
+            for (int j = 0; j < n; ++j) {
+                const int s = j & 1, s3 = j % 3;
+                if (!wait(qKEmpty + s3, ((j / 3) & 1) ^ 1)) break;
+                if (lane == 0) {
+                    barrier_expect(bar(qKFull + s3), kBytes);
+                    load_halves<HALVES>(sm_k + s3 * kBytes, &p.k, w.k_first + j * kTile, kv_head, w.q_batch, bar(qKFull + s3));
+                }
+                issued_k = j + 1;
+                if (!wait(qVEmpty + s, ((j >> 1) & 1) ^ 1)) break;
+                if (lane == 0) {
+                    barrier_expect(bar(qVFull + s), kBytes);
+                    load_halves<HALVES>(sm_v + s * kBytes, &p.v, w.k_first + j * kTile, kv_head, w.q_batch, bar(qVFull + s));
+                }
+                issued_v = j + 1;
             }
-            issued_v = j + 1;
-        }
-        if (sync->stop) {
-            if (n > 0) barrier_wait(bar(qQ), 0, nullptr, p.timeouts);
-            for (int s = 0; s < 2; ++s) {
-                if (issued_k > s) barrier_wait(bar(qKFull + s), ((issued_k - 1 - s) >> 1) & 1, nullptr, p.timeouts);
-                if (issued_v > s) barrier_wait(bar(qVFull + s), ((issued_v - 1 - s) >> 1) & 1, nullptr, p.timeouts);
+            if (stopped(sync)) {
+                if (n > 0) barrier_wait(bar(qQ), 0, nullptr, p.timeouts);
+                for (int s = 0; s < 3; ++s)
+                    if (issued_k > s) barrier_wait(bar(qKFull + s), ((issued_k - 1 - s) / 3) & 1, nullptr, p.timeouts);
+                for (int s = 0; s < 2; ++s)
+                    if (issued_v > s) barrier_wait(bar(qVFull + s), ((issued_v - 1 - s) >> 1) & 1, nullptr, p.timeouts);
             }
-        }
-    } else if (warp == kMmaWarp) {
-        // K tile j is used by S_j and, transposed, by dQ_j; V tile j by dP_j
-        auto scores = [&](int j) {
-            if (lane == 0) {
-                product_rows<T, DIM>(tm_s + (j & 1) * kTile, sm_q, sm_k + (j & 1) * kBytes);
-                commit(bar(qS + (j & 1)));
+        } else if (warp == kMmaWarp) {
+            // K tile j is used by S_j and, transposed, by dQ_j; V tile j by dP_j
+            auto scores = [&](int j) {
+                if (!wait(qKFull + j % 3, (j / 3) & 1)) return false;
+                if (w.packed && (j + 1) * kTile > w.k_len) clear_rows<HALVES>(sm_k + (j % 3) * kBytes, w.k_len - j * kTile);
+                if (lane == 0) {
+                    product_rows<T, DIM>(tm_s + (j & 1) * kTile, sm_q, sm_k + (j % 3) * kBytes);
+                    commit(bar(qS + (j & 1)));
+                }
+                __syncwarp();
+                return true;
+            };
+            auto dprobs = [&](int j) {
+                if (!wait(qVFull + (j & 1), (j >> 1) & 1)) return false;
+                if (lane == 0) {
+                    product_rows<T, DIM>(tm_dp, sm_g, sm_v + (j & 1) * kBytes);
+                    commit(bar(qDp));
+                    commit(bar(qVEmpty + (j & 1)));
+                }
+                __syncwarp();
+                return true;
+            };
+            bool ok = n == 0 || (wait(qQ, 0) && scores(0) && dprobs(0) && (n < 2 || scores(1)));
+            for (int j = 0; ok && j < n; ++j) {
+                ok = wait(qDs, j & 1);                                // dS_j written, dP_j read
+                if (!ok) break;
+                fence_after();
+                if (j + 1 < n && !(ok = dprobs(j + 1))) break;
+                if (lane == 0) {
+                    const uint32_t at = tm_s + (j & 1) * kTile;
+                    product_columns<T, DIM>(tm_dq, at, at + 64, sm_k + (j % 3) * kBytes, j > 0);
+                    commit(bar(qKEmpty + j % 3));
+                }
+                __syncwarp();
+                if (j + 2 < n) ok = scores(j + 2);                    // over dS_j, after its product
             }
+            if (lane == 0) commit(bar(qDone));
             __syncwarp();
-        };
-        auto arrived_k = [&](int j) {
-            if (!wait(qKFull + (j & 1), (j >> 1) & 1)) return false;
-            if (w.packed && (j + 1) * kTile > w.k_len) clear_rows<HALVES>(sm_k + (j & 1) * kBytes, w.k_len - j * kTile);
-            return true;
-        };
-        auto dprobs = [&](int j) {
-            if (!wait(qVFull + (j & 1), (j >> 1) & 1)) return false;
-            if (lane == 0) {
-                product_rows<T, DIM>(tm_dp, sm_g, sm_v + (j & 1) * kBytes);
-                commit(bar(qDp));
-                commit(bar(qVEmpty + (j & 1)));
-            }
-            __syncwarp();
-            return true;
-        };
-        bool ok = n == 0 || (wait(qQ, 0) && arrived_k(0));
-        if (ok && n > 0) {
-            scores(0);
-            ok = dprobs(0) && (n < 2 || arrived_k(1));
-            if (ok && n > 1) scores(1);
+            barrier_wait(bar(qDone), 0, nullptr, p.timeouts);
         }
-        for (int j = 0; ok && j < n; ++j) {
-            ok = wait(qDs, j & 1);                                    // dS_j written, dP_j read
-            if (!ok) break;
-            fence_after();
-            if (j + 1 < n && !(ok = dprobs(j + 1))) break;
-            if (lane == 0) {
-                const uint32_t at = tm_s + (j & 1) * kTile;
-                product_columns<T, DIM>(tm_dq, at, at + 64, sm_k + (j & 1) * kBytes, j > 0);
-                commit(bar(qKEmpty + (j & 1)));
-            }
-            __syncwarp();
-            if (j + 2 < n) {                                          // over dS_j, after its product
-                ok = arrived_k(j + 2);
-                if (ok) scores(j + 2);
-            }
-        }
-        if (lane == 0) commit(bar(qDone));
-        __syncwarp();
-        barrier_wait(bar(qDone), 0, nullptr, p.timeouts);
     } else {
+        take_registers<kWorkRegisters>();
         const int part = warp >> 2;                                   // columns [64 part, 64 part + 64) of every tile
         const int r = threadIdx.x & 127, i = q0 + r;
         const bool live = i < w.q_len;
         const uint32_t my_lane = static_cast<uint32_t>(warp & 3) << 21;
-        float delta = 0.0f, lse2 = INFINITY;                          // a row that sees nothing: every probability is 0
+        float delta = 0.0f, minus_lse = -INFINITY;                    // a row that sees nothing: every probability is 0
         if (live) {
             const T *o = static_cast<const T *>(p.o.p) + row_of(w, p.o, w.head, i, w.q_first);
             const T *g = static_cast<const T *>(p.go.p) + row_of(w, p.go, w.head, i, w.q_first);
@@ -508,12 +566,12 @@ attention_dq_kernel(const __grid_constant__ Params p) {
                 for (int e = 0; e < 8; ++e) delta = fmaf(a[e], b[e], delta);
             }
             const float l = p.lse[stat_of(p, w, w.head, i)];
-            if (l != -INFINITY) lse2 = l * 1.4426950408889634f;
+            if (l != -INFINITY) minus_lse = -l * kLog2e;
         }
         half_delta[part * kTile + r] = delta;
         asm volatile("bar.sync 1, 256;" ::: "memory");                // the element-wise warps only
-        delta = half_delta[r] + half_delta[kTile + r];
-        if (live && part == 0) p.delta[stat_of(p, w, w.head, i)] = delta;
+        const float minus_delta = -(half_delta[r] + half_delta[kTile + r]);
+        stat_block(p, w, w.head, w.tile)[part * kTile + r] = part == 0 ? minus_lse : minus_delta;
         const int seen = p.causal ? min(w.k_len, i + 1 + w.k_len - w.q_len) : w.k_len;
         const int tile_seen = p.causal ? min(w.k_len, q0 + 1 + w.k_len - w.q_len) : w.k_len;
         bool ok = true;
@@ -522,32 +580,42 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             ok = wait(qS + (j & 1), (j >> 1) & 1);
             if (!ok) break;
             fence_after();
-            uint32_t s[64];
+            uint32_t s[64], d[64], out[32];
+            float prob[64];
             tmem_ld32(s_at, s);
             tmem_ld32(s_at + 32, s + 32);
             wait_ld();
-#pragma unroll
-            for (int c = 0; c < 64; ++c) s[c] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[c]), p.scale_log2, -lse2)));
             const bool edge = (j + 1) * kTile > tile_seen;
-            const int limit = seen - j * kTile - 64 * part;
+            if (edge) {
+#pragma unroll
+                for (int c = 0; c < 64; c += 2)
+                    exp2_scaled<false>(prob[c], prob[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), p.scale_log2, minus_lse, minus_lse);
+            } else {
+#pragma unroll
+                for (int c = 0; c < 64; c += 2) {
+                    if (c % 8 == 6) exp2_scaled<true>(prob[c], prob[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), p.scale_log2, minus_lse, minus_lse);
+                    else exp2_scaled<false>(prob[c], prob[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), p.scale_log2, minus_lse, minus_lse);
+                }
+            }
             ok = wait(qDp, j & 1);
             if (!ok) break;
             fence_after();
-            uint32_t d[64];
             tmem_ld32(dp_at, d);
             tmem_ld32(dp_at + 32, d + 32);
             wait_ld();
-            uint32_t out[32];
+            float ds[64];
 #pragma unroll
-            for (int c = 0; c < 32; ++c) {
-                float a = __uint_as_float(s[2 * c]) * (__uint_as_float(d[2 * c]) - delta);
-                float b = __uint_as_float(s[2 * c + 1]) * (__uint_as_float(d[2 * c + 1]) - delta);
-                if (edge) {
-                    a = 2 * c < limit ? a : 0.0f;
-                    b = 2 * c + 1 < limit ? b : 0.0f;
-                }
-                out[c] = pack2<T>(a, b);
+            for (int c = 0; c < 64; c += 2) {
+                add2(ds[c], ds[c + 1], __uint_as_float(d[c]), __uint_as_float(d[c + 1]), minus_delta, minus_delta);
+                mul2(ds[c], ds[c + 1], ds[c], ds[c + 1], prob[c], prob[c + 1]);
             }
+            if (edge) {                                               // places that the row does not see, whatever they hold
+                const int limit = seen - j * kTile - 64 * part;
+#pragma unroll
+                for (int c = 0; c < 64; ++c) ds[c] = c < limit ? ds[c] : 0.0f;
+            }
+#pragma unroll
+            for (int c = 0; c < 32; ++c) out[c] = pack2<T>(ds[2 * c], ds[2 * c + 1]);
             tmem_st32(s_at, out);                                     // over the first half of what this thread read
             wait_st();
             fence_before();
@@ -578,181 +646,185 @@ attention_dq_kernel(const __grid_constant__ Params p) {
 // ---------------------------------------------------------------------------------------------------
 // backward, dK and dV
 // ---------------------------------------------------------------------------------------------------
-// Barriers: k and v, q full/empty (2 stages), g full/empty, S full, P ready, dP full, dS ready, done; the q stage
-// also carries the rows' lse and delta.
-enum { kKv = 0, kQFull = 1, kQEmpty = 3, kGFull = 5, kGEmpty = 7, kS = 9, kP = 10, kDp = 11, kDs = 12, kDone = 13, kBars = 14 };
+// Barriers: k and v, q full/empty (3 stages: a tile is used twice, one iteration apart), statistics full/empty (2 stages),
+// g full/empty (2 stages), S full, P ready, dP full, dS ready, done.
+enum { kKv = 0, kQFull = 1, kQEmpty = 4, kTFull = 7, kTEmpty = 9, kGFull = 11, kGEmpty = 13, kS = 15, kP = 16, kDp = 17, kDs = 18, kDone = 19, kBars = 20 };
 
-template <int DIM> constexpr int dkv_smem() { return 6 * (DIM / 64) * static_cast<int>(kHalfTile) + 1024 + static_cast<int>(sizeof(Sync)) + 16 + 4 * kTile * 4; }
+template <int DIM> constexpr int dkv_smem() { return 7 * (DIM / 64) * static_cast<int>(kHalfTile) + 2 * kStatBytes + static_cast<int>(sizeof(Sync)); }
 
 template <typename T, int DIM>
 __global__ void __launch_bounds__(kThreadsAttn, 1)
 attention_dkv_kernel(const __grid_constant__ Params p) {
     constexpr int HALVES = DIM / 64;
     constexpr uint32_t kBytes = HALVES * kHalfTile;
-    extern __shared__ uint8_t raw[];
-    const uint32_t base = (smem_address(raw) + 1023u) & ~1023u;
-    uint8_t *after = raw + (base - smem_address(raw)) + 6 * kBytes;
-    float *stat = reinterpret_cast<float *>(after);                   // [stage][lse * log2 e, delta][128]
-    Sync *sync = reinterpret_cast<Sync *>(after + 4 * kTile * 4);
+    extern __shared__ __align__(1024) uint8_t raw[];
+    const uint32_t base = smem_address(raw);
+    float *stat = reinterpret_cast<float *>(raw + 7 * kBytes);        // [stage][-lse * log2 e, -delta][128]
+    Sync *sync = reinterpret_cast<Sync *>(raw + 7 * kBytes + 2 * kStatBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
-    const Work w = find_work(p, p.kv_heads, false);
+    const int rank = p.split > 1 ? static_cast<int>(cluster_rank()) : 0;
+    const Work w = find_work(p, blockIdx.x / p.split, p.kv_heads, false);
+    if (w.packed && w.batch == p.batch) {                             // (the whole cluster)
+        if (rank == 0) {
+            fill_outside<T>(p, w, p.k_offsets, p.k_rows, p.dk, nullptr);
+            fill_outside<T>(p, w, p.k_offsets, p.k_rows, p.dv, nullptr);
+        }
+        return;
+    }
     const int k0 = w.tile * kTile;
     if (k0 >= w.k_len) return;
-    // row tiles [first, last) see a key of this tile; all query heads of the group, one after the other
+    // row tiles [first, last) see a key of this tile; all query heads of the group, one after the other, dealt out to the
+    // cluster's CTAs in turn
     const int reach = w.k_len - w.q_len;                              // row i sees keys up to i + reach
     const int first = p.causal ? max(0, k0 - reach) / kTile : 0;
     const int each = max(0, (w.q_len + kTile - 1) / kTile - first);
-    const int n = each * p.group;
+    const int n = (each * p.group - rank + p.split - 1) / p.split;
 
-    constexpr uint32_t counts[kBars] = {1, 33, 33, 1, 1, 1, 1, 1, 1, 1, 8, 1, 8, 1};
-    const uint32_t tmem = start_cta(sync, kBars, counts, true);
+    constexpr uint32_t counts[kBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 8, 8, 1, 1, 1, 1, 1, 8, 1, 8, 1};
+    const uint32_t tmem = start_cta(sync, kBars, counts);
     auto bar = [&](int i) { return smem_address(&sync->bar[i]); };
     auto wait = [&](int i, uint32_t parity) { return barrier_wait(bar(i), parity, &sync->stop, p.timeouts); };
-    const uint32_t sm_k = base, sm_v = base + kBytes, sm_q = base + 2 * kBytes, sm_g = base + 4 * kBytes;
+    const uint32_t sm_k = base, sm_v = base + kBytes, sm_q = base + 2 * kBytes, sm_g = base + 5 * kBytes;
     // tensor memory: S (P in its place), dP (dS in its place), dV, dK
     const uint32_t tm_s = tmem, tm_dp = tmem + kTile, tm_dv = tmem + 2 * kTile, tm_dk = tmem + 3 * kTile;
 
-    if (warp == kLoadWarp) {
-        int issued_q = 0, issued_g = 0;
-        if (n > 0 && lane == 0) {
-            prefetch_map(&p.q);
-            prefetch_map(&p.k);
-            prefetch_map(&p.v);
-            prefetch_map(&p.g);
-            barrier_expect(bar(kKv), 2 * kBytes);
-            load_halves<HALVES>(sm_k, &p.k, w.k_first + k0, w.head, w.q_batch, bar(kKv));
-            load_halves<HALVES>(sm_v, &p.v, w.k_first + k0, w.head, w.q_batch, bar(kKv));
-        }
-        for (int j = 0; j < n; ++j) {
-            const int s = j & 1, head = w.head * p.group + j / each, q0 = (first + j % each) * kTile;
-            const uint32_t again = ((j >> 1) & 1) ^ 1;
-            if (!wait(kQEmpty + s, again)) break;
-            if (lane == 0) {
-                barrier_expect(bar(kQFull + s), kBytes);
-                load_halves<HALVES>(sm_q + s * kBytes, &p.q, w.q_first + q0, head, w.q_batch, bar(kQFull + s));
+    bool ok = true;
+    if (warp >= kMmaWarp) {
+        give_registers<kIssueRegisters>();
+        if (warp == kLoadWarp) {
+            int issued_q = 0, issued_t = 0, issued_g = 0;
+            if (n > 0 && lane == 0) {
+                prefetch_map(&p.q);
+                prefetch_map(&p.k);
+                prefetch_map(&p.v);
+                prefetch_map(&p.g);
+                barrier_expect(bar(kKv), 2 * kBytes);
+                load_halves<HALVES>(sm_k, &p.k, w.k_first + k0, w.head, w.q_batch, bar(kKv));
+                load_halves<HALVES>(sm_v, &p.v, w.k_first + k0, w.head, w.q_batch, bar(kKv));
             }
-            // rows past the end, and rows that see nothing, get lse = inf: their probabilities are 0
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int r = lane + 32 * e;
-                float l = INFINITY, d = 0.0f;
-                if (q0 + r < w.q_len) {
-                    const long long at = stat_of(p, w, head, q0 + r);
-                    l = p.lse[at];
-                    d = p.delta[at];
-                    l = l == -INFINITY ? INFINITY : l * 1.4426950408889634f;
+            for (int j = 0; j < n; ++j) {
+                const int s = j & 1, s3 = j % 3, at = rank + j * p.split;
+                const int head = w.head * p.group + at / each, tile = first + at % each, q0 = tile * kTile;
+                const uint32_t again = ((j >> 1) & 1) ^ 1;
+                if (!wait(kQEmpty + s3, ((j / 3) & 1) ^ 1)) break;
+                if (lane == 0) {
+                    barrier_expect(bar(kQFull + s3), kBytes);
+                    load_halves<HALVES>(sm_q + s3 * kBytes, &p.q, w.q_first + q0, head, w.q_batch, bar(kQFull + s3));
                 }
-                stat[s * 2 * kTile + r] = l;
-                stat[s * 2 * kTile + kTile + r] = d;
+                issued_q = j + 1;
+                if (!wait(kTEmpty + s, again)) break;
+                if (lane == 0) {
+                    barrier_expect(bar(kTFull + s), kStatBytes);
+                    load_bytes(smem_address(stat + s * 2 * kTile), stat_block(p, w, head, tile), kStatBytes, bar(kTFull + s));
+                }
+                issued_t = j + 1;
+                if (!wait(kGEmpty + s, again)) break;
+                if (lane == 0) {
+                    barrier_expect(bar(kGFull + s), kBytes);
+                    load_halves<HALVES>(sm_g + s * kBytes, &p.g, w.q_first + q0, head, w.q_batch, bar(kGFull + s));
+                }
+                issued_g = j + 1;
             }
-            barrier_arrive(bar(kQFull + s));
-            issued_q = j + 1;
-            if (!wait(kGEmpty + s, again)) break;
-            if (lane == 0) {
-                barrier_expect(bar(kGFull + s), kBytes);
-                load_halves<HALVES>(sm_g + s * kBytes, &p.g, w.q_first + q0, head, w.q_batch, bar(kGFull + s));
+            if (stopped(sync)) {
+                if (n > 0) barrier_wait(bar(kKv), 0, nullptr, p.timeouts);
+                for (int s = 0; s < 3; ++s)
+                    if (issued_q > s) barrier_wait(bar(kQFull + s), ((issued_q - 1 - s) / 3) & 1, nullptr, p.timeouts);
+                for (int s = 0; s < 2; ++s) {
+                    if (issued_t > s) barrier_wait(bar(kTFull + s), ((issued_t - 1 - s) >> 1) & 1, nullptr, p.timeouts);
+                    if (issued_g > s) barrier_wait(bar(kGFull + s), ((issued_g - 1 - s) >> 1) & 1, nullptr, p.timeouts);
+                }
             }
-            issued_g = j + 1;
-        }
-        if (sync->stop) {
-            if (n > 0) barrier_wait(bar(kKv), 0, nullptr, p.timeouts);
-            for (int s = 0; s < 2; ++s) {
-                if (issued_q > s) barrier_wait(bar(kQFull + s), ((issued_q - 1 - s) >> 1) & 1, nullptr, p.timeouts);
-                if (issued_g > s) barrier_wait(bar(kGFull + s), ((issued_g - 1 - s) >> 1) & 1, nullptr, p.timeouts);
-            }
-        }
-    } else if (warp == kMmaWarp) {
-        // Q tile j is used by S_j and, transposed, by dK_j; G tile j by dP_j and, transposed, by dV_j
-        auto arrived = [&](int full, uint32_t tile, int j) {
-            if (!wait(full + (j & 1), (j >> 1) & 1)) return false;
-            const int rows = w.q_len - (first + j % each) * kTile;
-            if (w.packed && rows < kTile) clear_rows<HALVES>(tile + (j & 1) * kBytes, rows);
-            return true;
-        };
-        auto scores = [&](int j) {
-            if (lane == 0) {
-                product_rows<T, DIM>(tm_s, sm_k, sm_q + (j & 1) * kBytes);
-                commit(bar(kS));
-            }
-            __syncwarp();
-        };
-        auto dprobs = [&](int j) {
-            if (lane == 0) {
-                product_rows<T, DIM>(tm_dp, sm_v, sm_g + (j & 1) * kBytes);
-                commit(bar(kDp));
-            }
-            __syncwarp();
-        };
-        bool ok = n == 0 || (wait(kKv, 0) && arrived(kQFull, sm_q, 0));
-        if (ok && n > 0) {
-            scores(0);
-            ok = arrived(kGFull, sm_g, 0);
-            if (ok) dprobs(0);
-        }
-        for (int j = 0; ok && j < n; ++j) {
-            ok = wait(kP, j & 1);                                     // P_j written over S_j
-            if (!ok) break;
-            fence_after();
-            if (lane == 0) {
-                product_columns<T, DIM>(tm_dv, tm_s, tm_s + 64, sm_g + (j & 1) * kBytes, j > 0);
-                commit(bar(kGEmpty + (j & 1)));
-            }
-            __syncwarp();
-            if (j + 1 < n) {
-                ok = arrived(kQFull, sm_q, j + 1);
+        } else if (warp == kMmaWarp) {
+            // Q tile j is used by S_j and, transposed, by dK_j; G tile j by dP_j and, transposed, by dV_j
+            auto rows_left = [&](int j) { return w.q_len - (first + (rank + j * p.split) % each) * kTile; };
+            auto scores = [&](int j) {
+                const uint32_t tile = sm_q + (j % 3) * kBytes;
+                if (!wait(kQFull + j % 3, (j / 3) & 1)) return false;
+                if (w.packed && rows_left(j) < kTile) clear_rows<HALVES>(tile, rows_left(j));
+                if (lane == 0) {
+                    product_rows<T, DIM>(tm_s, sm_k, tile);
+                    commit(bar(kS));
+                }
+                __syncwarp();
+                return true;
+            };
+            auto dprobs = [&](int j) {
+                const uint32_t tile = sm_g + (j & 1) * kBytes;
+                if (!wait(kGFull + (j & 1), (j >> 1) & 1)) return false;
+                if (w.packed && rows_left(j) < kTile) clear_rows<HALVES>(tile, rows_left(j));
+                if (lane == 0) {
+                    product_rows<T, DIM>(tm_dp, sm_v, tile);
+                    commit(bar(kDp));
+                }
+                __syncwarp();
+                return true;
+            };
+            ok = n == 0 || (wait(kKv, 0) && scores(0) && dprobs(0));
+            for (int j = 0; ok && j < n; ++j) {
+                ok = wait(kP, j & 1);                                 // P_j written over S_j
                 if (!ok) break;
-                scores(j + 1);
+                fence_after();
+                if (lane == 0) {
+                    product_columns<T, DIM>(tm_dv, tm_s, tm_s + 64, sm_g + (j & 1) * kBytes, j > 0);
+                    commit(bar(kGEmpty + (j & 1)));
+                }
+                __syncwarp();
+                if (j + 1 < n && !(ok = scores(j + 1))) break;
+                ok = wait(kDs, j & 1);                                // dS_j written over dP_j
+                if (!ok) break;
+                fence_after();
+                if (lane == 0) {
+                    product_columns<T, DIM>(tm_dk, tm_dp, tm_dp + 64, sm_q + (j % 3) * kBytes, j > 0);
+                    commit(bar(kQEmpty + j % 3));
+                }
+                __syncwarp();
+                if (j + 1 < n) ok = dprobs(j + 1);
             }
-            ok = wait(kDs, j & 1);                                    // dS_j written over dP_j
-            if (!ok) break;
-            fence_after();
-            if (j + 1 < n && !arrived(kGFull, sm_g, j + 1)) break;
-            if (lane == 0) {
-                product_columns<T, DIM>(tm_dk, tm_dp, tm_dp + 64, sm_q + (j & 1) * kBytes, j > 0);
-                commit(bar(kQEmpty + (j & 1)));
-            }
+            if (lane == 0) commit(bar(kDone));
             __syncwarp();
-            if (j + 1 < n) dprobs(j + 1);
+            barrier_wait(bar(kDone), 0, nullptr, p.timeouts);
         }
-        if (lane == 0) commit(bar(kDone));
-        __syncwarp();
-        barrier_wait(bar(kDone), 0, nullptr, p.timeouts);
     } else {
+        take_registers<kWorkRegisters>();
         const int part = warp >> 2;                                   // rows [64 part, 64 part + 64) of every row tile
         const int key = k0 + (threadIdx.x & 127);
-        const bool live = key < w.k_len;
         const uint32_t my_lane = static_cast<uint32_t>(warp & 3) << 21;
         const uint32_t s_at = tm_s + 64 * part + my_lane, dp_at = tm_dp + 64 * part + my_lane;
-        bool ok = true;
         for (int j = 0; j < n; ++j) {
-            const int q0 = (first + j % each) * kTile;
-            ok = wait(kQFull + (j & 1), (j >> 1) & 1) && wait(kS, j & 1);
+            const int q0 = (first + (rank + j * p.split) % each) * kTile;
+            ok = wait(kTFull + (j & 1), (j >> 1) & 1) && wait(kS, j & 1);
             if (!ok) break;
             fence_after();
             const float4 *l4 = reinterpret_cast<const float4 *>(stat + (j & 1) * 2 * kTile + 64 * part);
             const float4 *d4 = l4 + kTile / 4;
-            uint32_t s[64], out[32];
+            uint32_t s[64], d[64], out[32];
+            float prob[64];
             tmem_ld32(s_at, s);
             tmem_ld32(s_at + 32, s + 32);
             wait_ld();
+            // rows past the end and rows that see nothing have -lse = -inf: their probabilities are 0
+            if (p.causal && k0 + kTile - 1 > q0 + reach) {            // some rows do not see this thread's key
+                const int from = key - reach - q0 - 64 * part;
 #pragma unroll
-            for (int c = 0; c < 16; ++c) {
-                const float4 l = l4[c];
-                s[4 * c] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[4 * c]), p.scale_log2, -l.x)));
-                s[4 * c + 1] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[4 * c + 1]), p.scale_log2, -l.y)));
-                s[4 * c + 2] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[4 * c + 2]), p.scale_log2, -l.z)));
-                s[4 * c + 3] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(s[4 * c + 3]), p.scale_log2, -l.w)));
+                for (int c = 0; c < 16; ++c) {
+                    const float4 l = l4[c];
+                    exp2_scaled<false>(prob[4 * c], prob[4 * c + 1], __uint_as_float(s[4 * c]), __uint_as_float(s[4 * c + 1]), p.scale_log2, l.x, l.y);
+                    exp2_scaled<false>(prob[4 * c + 2], prob[4 * c + 3], __uint_as_float(s[4 * c + 2]), __uint_as_float(s[4 * c + 3]), p.scale_log2, l.z, l.w);
+                }
+#pragma unroll
+                for (int c = 0; c < 64; ++c) prob[c] = c >= from ? prob[c] : 0.0f;
+            } else {
+#pragma unroll
+                for (int c = 0; c < 16; ++c) {
+                    const float4 l = l4[c];
+                    exp2_scaled<false>(prob[4 * c], prob[4 * c + 1], __uint_as_float(s[4 * c]), __uint_as_float(s[4 * c + 1]), p.scale_log2, l.x, l.y);
+                    if (c & 1) exp2_scaled<true>(prob[4 * c + 2], prob[4 * c + 3], __uint_as_float(s[4 * c + 2]), __uint_as_float(s[4 * c + 3]), p.scale_log2, l.z, l.w);
+                    else exp2_scaled<false>(prob[4 * c + 2], prob[4 * c + 3], __uint_as_float(s[4 * c + 2]), __uint_as_float(s[4 * c + 3]), p.scale_log2, l.z, l.w);
+                }
             }
-            // edges: rows that do not see this thread's key, and rows past the sequence's end (whose memory may hold anything)
-            const bool edge = q0 + kTile > w.q_len || (p.causal && k0 + kTile - 1 > q0 + reach);
-            const int from = p.causal ? key - reach - q0 - 64 * part : -1, to = w.q_len - q0 - 64 * part;
-            if (edge) {
 #pragma unroll
-                for (int c = 0; c < 64; ++c) s[c] = c >= from && c < to ? s[c] : 0u;
-            }
-#pragma unroll
-            for (int c = 0; c < 32; ++c) out[c] = pack2<T>(__uint_as_float(s[2 * c]), __uint_as_float(s[2 * c + 1]));
+            for (int c = 0; c < 32; ++c) out[c] = pack2<T>(prob[2 * c], prob[2 * c + 1]);
             tmem_st32(s_at, out);
             wait_st();
             fence_before();
@@ -761,47 +833,89 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             ok = wait(kDp, j & 1);
             if (!ok) break;
             fence_after();
-            uint32_t d[64];
             tmem_ld32(dp_at, d);
             tmem_ld32(dp_at + 32, d + 32);
             wait_ld();
 #pragma unroll
             for (int c = 0; c < 16; ++c) {
                 const float4 e = d4[c];
-                float v[4] = {__uint_as_float(d[4 * c]) - e.x, __uint_as_float(d[4 * c + 1]) - e.y, __uint_as_float(d[4 * c + 2]) - e.z,
-                              __uint_as_float(d[4 * c + 3]) - e.w};
-#pragma unroll
-                for (int x = 0; x < 4; ++x) v[x] *= __uint_as_float(s[4 * c + x]);
-                if (edge) {
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) v[x] = 4 * c + x >= from && 4 * c + x < to ? v[x] : 0.0f;
-                }
-                out[2 * c] = pack2<T>(v[0], v[1]);
-                out[2 * c + 1] = pack2<T>(v[2], v[3]);
+                float v0, v1, v2, v3;
+                add2(v0, v1, __uint_as_float(d[4 * c]), __uint_as_float(d[4 * c + 1]), e.x, e.y);
+                add2(v2, v3, __uint_as_float(d[4 * c + 2]), __uint_as_float(d[4 * c + 3]), e.z, e.w);
+                mul2(v0, v1, v0, v1, prob[4 * c], prob[4 * c + 1]);
+                mul2(v2, v3, v2, v3, prob[4 * c + 2], prob[4 * c + 3]);
+                out[2 * c] = pack2<T>(v0, v1);
+                out[2 * c + 1] = pack2<T>(v2, v3);
             }
             tmem_st32(dp_at, out);
             wait_st();
             fence_before();
             __syncwarp();
-            if (lane == 0) barrier_arrive(bar(kDs));
+            if (lane == 0) {
+                barrier_arrive(bar(kDs));
+                barrier_arrive(bar(kTEmpty + (j & 1)));
+            }
         }
         if (ok) ok = wait(kDone, 0);
         fence_after();
-        if (ok) {                                                     // the first four warps write dV, the others dK
-            const Rows &to = part == 0 ? p.dv : p.dk;
-            T *row = static_cast<T *>(to.p) + (live ? row_of(w, to, w.head, key, w.k_first) : 0);
+    }
+    // dV by the first four warps, dK by the next
+    const int part = (warp >> 2) & 1, r = threadIdx.x & 127, key = k0 + r;
+    const bool works = warp < kMmaWarp, live = works && key < w.k_len;
+    const Rows &to = part == 0 ? p.dv : p.dk;
+    const float factor = part == 0 ? 1.0f : p.scale;
+    const uint32_t from = (part == 0 ? tm_dv : tm_dk) + (static_cast<uint32_t>(warp & 3) << 21);
+    T *row = static_cast<T *>(to.p) + (live ? row_of(w, to, w.head, key, w.k_first) : 0);
+    if (p.split == 1) {
+        if (works && ok) {
             if (n > 0) {
 #pragma unroll
                 for (int c = 0; c < DIM / 32; ++c) {
                     uint32_t o[32];
-                    tmem_ld32((part == 0 ? tm_dv : tm_dk) + my_lane + 32 * c, o);
+                    tmem_ld32(from + 32 * c, o);
                     wait_ld();
-                    if (live) store_columns<T>(row, 32 * c, p.dim, o, part == 0 ? 1.0f : p.scale);
+                    if (live) store_columns<T>(row, 32 * c, p.dim, o, factor);
                 }
             } else if (live) {
                 zero_columns<T>(row, p.dim);
             }
         }
+    } else {
+        // Each CTA lays its sums out in its own shared memory, [dV or dK][column][key] (the tiles are no longer needed), and
+        // adds up a share of the columns over the cluster, in the order of the ranks.
+        const uint32_t mine = base + static_cast<uint32_t>(part * DIM) * (kTile * 4) + r * 4;
+        if (works) {
+#pragma unroll
+            for (int c = 0; c < DIM / 32; ++c) {
+                uint32_t o[32];
+                if (n > 0) {
+                    tmem_ld32(from + 32 * c, o);
+                    wait_ld();
+                }
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    asm volatile("st.shared.u32 [%0], %1;" :: "r"(mine + (32 * c + e) * (kTile * 4)), "r"(n > 0 ? o[e] : 0u) : "memory");
+            }
+        }
+        cluster_sync();
+        if (live) {
+            const int share = DIM / p.split;                          // a multiple of 16
+            for (int c = rank * share; c < (rank + 1) * share && c < p.dim; c += 8) {
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = load_peer(mine + (c + e) * (kTile * 4), 0);
+                for (int k = 1; k < p.split; ++k)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] += load_peer(mine + (c + e) * (kTile * 4), k);
+                uint4 x;
+                x.x = pack2<T>(v[0] * factor, v[1] * factor);
+                x.y = pack2<T>(v[2] * factor, v[3] * factor);
+                x.z = pack2<T>(v[4] * factor, v[5] * factor);
+                x.w = pack2<T>(v[6] * factor, v[7] * factor);
+                *reinterpret_cast<uint4 *>(row + c) = x;
+            }
+        }
+        cluster_sync();                                               // nobody's shared memory goes before it has been read
     }
     end_cta(tmem);
 }

@@ -14,6 +14,7 @@
 #include <cmath>
 
 #include "fewbit_device.cuh"
+#include "fewbit_packed.cuh"
 
 namespace fewbit {
 bool pdl_enabled();
@@ -81,16 +82,6 @@ __device__ __forceinline__ void store_chunk(T *p, const float (&v)[V]) {
     *reinterpret_cast<Raw *>(p) = raw;
 }
 
-// Packed binary32 arithmetic: two lanes of one instruction, each rounded as the scalar operation is.
-__device__ __forceinline__ void fma2(float &d0, float &d1, float a0, float a1, float b0, float b1, float c0, float c1) {
-    asm("{\n.reg .b64 a, b, c, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\n"
-        "fma.rn.f32x2 d, a, b, c;\nmov.b64 {%0, %1}, d;\n}"
-        : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1), "f"(c0), "f"(c1));
-}
-__device__ __forceinline__ void mul2(float &d0, float &d1, float a0, float a1, float b0, float b1) {
-    asm("{\n.reg .b64 a, b, d;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 d, a, b;\nmov.b64 {%0, %1}, d;\n}"
-        : "=f"(d0), "=f"(d1) : "f"(a0), "f"(a1), "f"(b0), "f"(b1));
-}
 // d = a b, d = a b + c, over V elements; `scale` forms: b the same for all
 template <int V> __device__ __forceinline__ void vmul(float (&d)[V], const float (&a)[V], const float (&b)[V]) {
     if constexpr (V == 1) d[0] = a[0] * b[0];

@@ -8,6 +8,8 @@
 
 #include <cstdint>
 
+#include "fewbit_packed.cuh"
+
 namespace fewbit {
 namespace tc {
 
@@ -39,7 +41,7 @@ __device__ __forceinline__ uint64_t now_ns() {
 constexpr uint64_t kWaitLimitNs = 2000000000ull;
 
 // Waits of a whole warp (every lane gets the same answer).  false: given up; `stop` (shared memory) is set.
-static __device__ __noinline__ bool barrier_wait_slow(uint32_t bar, uint32_t parity, volatile int *stop, unsigned int *timeouts) {
+__device__ __forceinline__ bool barrier_wait_slow(uint32_t bar, uint32_t parity, volatile int *stop, unsigned int *timeouts) {
     const uint64_t t0 = now_ns();
     for (;;) {
         for (int i = 0; i < 64; ++i)
@@ -66,6 +68,31 @@ __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, 
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2,%3,%4,%5}], [%6];"
                  :: "r"(dst), "l"(map), "r"(x), "r"(row), "r"(head), "r"(batch), "r"(bar) : "memory");
 }
+
+// Contiguous bytes (a multiple of 16, both ends 16-byte aligned) to shared memory.
+__device__ __forceinline__ void load_bytes(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 :: "r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
+// ---- clusters -------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync() {                      // every thread of every CTA of the cluster
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float load_peer(uint32_t address, uint32_t rank) {
+    float v;
+    asm volatile("{\n.reg .b32 a;\nmapa.shared::cluster.u32 a, %1, %2;\nld.shared::cluster.f32 %0, [a];\n}" : "=f"(v) : "r"(address), "r"(rank) : "memory");
+    return v;
+}
+
+// ---- registers: a warpgroup hands some to the others (the sums stay within what the CTA was launched with)
+template <int N> __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(N)); }
+template <int N> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(N)); }
 
 // ---- tensor memory --------------------------------------------------------------------------------
 __device__ __forceinline__ void tmem_alloc(uint32_t slot, uint32_t columns) {        // one whole warp
@@ -149,14 +176,14 @@ __device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b)
         mma_ss(d, k_major(a + off), k_major(b + off), idesc, k > 0);
     }
 }
-// D (128 x DIM) (+)= A B: A (128 x 128, 16 bits) in tensor memory, 16 columns of its contraction in 8 TMEM columns,
-// the second 64 of them at `a2`; B's rows are the contraction
-template <typename T, int DIM>
+// D (128 x DIM) (+)= A B over steps [FIRST, LAST) of 16: A (128 x 128, 16 bits) in tensor memory, 16 columns of its
+// contraction in 8 TMEM columns, the second 64 of them at `a2`; B's rows are the contraction
+template <typename T, int DIM, int FIRST = 0, int LAST = 8>
 __device__ __forceinline__ void product_columns(uint32_t d, uint32_t a, uint32_t a2, uint32_t b, bool accumulate) {
     constexpr uint32_t idesc = instruction<T>(DIM, true);
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-        mma_ts(d, k < 4 ? a + 8 * k : a2 + 8 * (k - 4), mn_major(b + k * 2048), idesc, accumulate || k > 0);
+    for (int k = FIRST; k < LAST; ++k)
+        mma_ts(d, k < 4 ? a + 8 * k : a2 + 8 * (k - 4), mn_major(b + k * 2048), idesc, accumulate || k > FIRST);
 }
 
 template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
@@ -174,6 +201,38 @@ __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+
+// 2^x for two values on the FMA pipe, which has room where the exponential unit (16 results a clock) is the limit:
+// x = n + f with n the nearest integer, f in [-1/2, 1/2]; 2^f by the degree-4 polynomial of least relative error (2.6e-6,
+// found by iteratively reweighted least squares), n added to the exponent.  Values below 2^-126 come out as 2^-126; a NaN or
+// an infinity comes out as a value that is not finite in 16 bits.
+__device__ __forceinline__ void exp2_polynomial(float &d0, float &d1, float x0, float x1) {
+    constexpr float kMagic = 12582912.0f;                             // 1.5 * 2^23: the sum's low bits are the integer
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(x0) : "f"(x0), "f"(-126.0f));
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(x1) : "f"(x1), "f"(-126.0f));
+    float t0, t1, n0, n1, f0, f1, p0, p1;
+    add2(t0, t1, x0, x1, kMagic, kMagic);
+    add2(n0, n1, t0, t1, -kMagic, -kMagic);
+    fma2(f0, f1, n0, n1, -1.0f, -1.0f, x0, x1);
+    fma2(p0, p1, f0, f1, 0.009570102207362652f, 0.009570102207362652f, 0.05591785907745361f, 0.05591785907745361f);
+    fma2(p0, p1, p0, p1, f0, f1, 0.240247443318367f, 0.240247443318367f);
+    fma2(p0, p1, p0, p1, f0, f1, 0.6931217908859253f, 0.6931217908859253f);
+    fma2(p0, p1, p0, p1, f0, f1, 0.9999992847442627f, 0.9999992847442627f);
+    d0 = __int_as_float(__float_as_int(p0) + (__float_as_int(t0) << 23));
+    d1 = __int_as_float(__float_as_int(p1) + (__float_as_int(t1) << 23));
+}
+// (d0, d1) = 2^(x c + m); POLY: on the FMA pipe
+template <bool POLY>
+__device__ __forceinline__ void exp2_scaled(float &d0, float &d1, float x0, float x1, float c, float m0, float m1) {
+    float y0, y1;
+    fma2(y0, y1, x0, x1, c, c, m0, m1);
+    if constexpr (POLY) {
+        exp2_polynomial(d0, d1, y0, y1);
+    } else {
+        d0 = exp2_fast(y0);
+        d1 = exp2_fast(y1);
+    }
 }
 
 }  // namespace tc

@@ -262,10 +262,7 @@ def fewbit_attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, c
     buf = _Buffer()
     dev, stats = _attention_shape(buf, q, k, v, causal, scale, q_offsets, k_offsets, max_q_len, max_k_len)
     with _on(dev, stream, q, k, v, q_offsets, k_offsets):
-        if q_offsets is None:
-            out, lse = q.new_empty(q.shape), torch.empty(stats, dtype=torch.float32, device=dev)
-        else:                                                # rows of no sequence are not written by the library
-            out, lse = q.new_zeros(q.shape), torch.full(stats, -float("inf"), dtype=torch.float32, device=dev)
+        out, lse = q.new_empty(q.shape), torch.empty(stats, dtype=torch.float32, device=dev)
         hs = _put_heads(buf, 0, (q, k, v, out))
         _check(load_library().fewbit_attention_fwd(ctypes.addressof(buf), *hs, lse.data_ptr(), _stream_ptr(stream, dev)), "fewbit_attention_fwd")
     return out, lse
@@ -283,15 +280,14 @@ def fewbit_attention_bwd(grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tenso
     if grad_out.shape != q.shape or out.shape != q.shape or lse.shape != stats or not lse.is_contiguous():
         raise ValueError("grad_out, out and lse must have the shapes that the forward pass gives")
     _need(grad_out, "grad_out", dev, q.dtype), _need(out, "out", dev, q.dtype), _need(lse, "lse", dev, torch.float32)
+    lib, base = load_library(), ctypes.addressof(buf)
     with _on(dev, stream, grad_out, q, k, v, out, lse, q_offsets, k_offsets):
-        if q_offsets is None:
-            grads = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
-        else:
-            grads = q.new_zeros(q.shape), k.new_zeros(k.shape), v.new_zeros(v.shape)
-        ws = torch.empty(stats, dtype=torch.float32, device=dev)
+        grads = q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape)
+        ws_bytes = lib.fewbit_attention_workspace_bytes(base)
+        ws = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
         hs = _put_heads(buf, 0, (grad_out, q, k, v, out, *grads))
-        _check(load_library().fewbit_attention_bwd(ctypes.addressof(buf), *hs[:5], lse.data_ptr(), *hs[5:], ws.data_ptr(), 4 * ws.numel(),
-                                                   _stream_ptr(stream, dev)), "fewbit_attention_bwd")
+        _check(lib.fewbit_attention_bwd(base, *hs[:5], lse.data_ptr(), *hs[5:], ws.data_ptr(), ws_bytes, _stream_ptr(stream, dev)),
+               "fewbit_attention_bwd")
     return grads
 
 
