@@ -87,10 +87,10 @@ __device__ __forceinline__ Work find_work(const Params &p, int block, int heads,
         const long long q1 = min(max(static_cast<long long>(p.q_offsets[w.batch + 1]), q0), p.q_rows);
         const long long k0 = min(max(static_cast<long long>(p.k_offsets[w.batch]), 0ll), p.k_rows);
         const long long k1 = min(max(static_cast<long long>(p.k_offsets[w.batch + 1]), k0), p.k_rows);
-        w.q_first = static_cast<int>(q0);
-        w.k_first = static_cast<int>(k0);
-        w.q_len = static_cast<int>(min(q1 - q0, static_cast<long long>(p.q_len)));
-        w.k_len = static_cast<int>(min(k1 - k0, static_cast<long long>(p.k_len)));
+        w.q_first = uniform(static_cast<int>(q0));
+        w.k_first = uniform(static_cast<int>(k0));
+        w.q_len = uniform(static_cast<int>(min(q1 - q0, static_cast<long long>(p.q_len))));
+        w.k_len = uniform(static_cast<int>(min(k1 - k0, static_cast<long long>(p.k_len))));
         w.q_batch = 0;
     }
     return w;
@@ -190,7 +190,7 @@ __device__ __forceinline__ uint32_t start_cta(Sync *sync, int barriers, const ui
     fence_before();
     __syncthreads();
     fence_after();
-    return *reinterpret_cast<volatile uint32_t *>(&sync->tmem);
+    return uniform(*reinterpret_cast<volatile uint32_t *>(&sync->tmem));
 }
 // Every role is through: nothing is in flight any more.
 __device__ __forceinline__ void end_cta(uint32_t tmem) {
@@ -232,7 +232,7 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_address(raw) + 1023u) & ~1023u;
     Sync *sync = reinterpret_cast<Sync *>(raw + (base - smem_address(raw)) + 6 * kBytes);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform(static_cast<int>(threadIdx.x >> 5)), lane = threadIdx.x & 31;
     pdl_wait();
     const Work w = find_work(p, blockIdx.x, p.heads, true);
     if (w.packed && w.batch == p.batch) {
@@ -243,8 +243,8 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
     if (q0 >= w.q_len) return;                                        // packed: a shorter sequence
     const int kv_head = w.head / p.group;
     // key tiles of each row tile (0 also for a row tile past the end)
-    const int n0 = key_tiles(p, w, min(q0 + kTile, w.q_len) - 1);
-    const int n1 = q0 + kTile < w.q_len ? key_tiles(p, w, min(q0 + 2 * kTile, w.q_len) - 1) : 0;
+    const int n0 = uniform(key_tiles(p, w, min(q0 + kTile, w.q_len) - 1));
+    const int n1 = uniform(q0 + kTile < w.q_len ? key_tiles(p, w, min(q0 + 2 * kTile, w.q_len) - 1) : 0);
     const int n = max(n0, n1);
 
     constexpr uint32_t counts[fBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 4, 4, 4, 4, 1, 1, 1};
@@ -295,19 +295,17 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
                 }
             }
         } else if (warp == kMmaWarp) {
+            const uint32_t leader = elect_leader();
             auto scores = [&](int t, int j) {                         // S of row tile t against key tile j
-                if (lane == 0) {
-                    product_rows<T, DIM>(tm_s + t * kTile, sm_q + t * kBytes, sm_k + (j & 1) * kBytes);
-                    commit(bar(fS + t));
-                }
-                __syncwarp();
+                product_rows<T, DIM>(leader, tm_s + t * kTile, sm_q + t * kBytes, sm_k + (j & 1) * kBytes);
+                commit(leader, bar(fS + t));
             };
             bool ok = n == 0 || (wait(fQ, 0) && (n1 == 0 || wait(fQ + 1, 0)) && wait(fKFull, 0));
             if (ok && n > 0) {
                 fence_after();
                 if (n0 > 0) scores(0, 0);
                 if (n1 > 0) scores(1, 0);
-                if (lane == 0) commit(bar(fKEmpty));
+                commit(leader, bar(fKEmpty));
             }
             for (int j = 0; ok && j < n; ++j) {
                 ok = wait(fVFull + (j & 1), (j >> 1) & 1) && (j + 1 >= n || wait(fKFull + ((j + 1) & 1), ((j + 1) >> 1) & 1));
@@ -321,26 +319,18 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
                     ok = wait(fP + t, j & 1);
                     if (!ok) break;
                     fence_after();
-                    if (lane == 0) product_columns<T, DIM, 0, 6>(tm_o + t * kTile, at, at + 32, sm_v + (j & 1) * kBytes, j > 0);
-                    __syncwarp();
+                    product_columns<T, DIM, 0, 6>(leader, tm_o + t * kTile, at, at + 32, sm_v + (j & 1) * kBytes, j > 0);
                     ok = wait(fPEnd + t, j & 1);
                     if (!ok) break;
                     fence_after();
-                    if (lane == 0) {
-                        product_columns<T, DIM, 6, 8>(tm_o + t * kTile, at, at + 32, sm_v + (j & 1) * kBytes, true);
-                        commit(bar(fO + t));
-                    }
-                    __syncwarp();
+                    product_columns<T, DIM, 6, 8>(leader, tm_o + t * kTile, at, at + 32, sm_v + (j & 1) * kBytes, true);
+                    commit(leader, bar(fO + t));
                     if (j + 1 < nt) scores(t, j + 1);
                 }
-                if (lane == 0) {
-                    commit(bar(fVEmpty + (j & 1)));
-                    if (j + 1 < n) commit(bar(fKEmpty + ((j + 1) & 1)));
-                }
-                __syncwarp();
+                commit(leader, bar(fVEmpty + (j & 1)));
+                if (j + 1 < n) commit(leader, bar(fKEmpty + ((j + 1) & 1)));
             }
-            if (lane == 0) commit(bar(fDrain));
-            __syncwarp();
+            commit(leader, bar(fDrain));
             barrier_wait(bar(fDrain), 0, nullptr, p.timeouts);
         }
     } else {
@@ -453,7 +443,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
     const uint32_t base = smem_address(raw);                          // no room to align it here: the host checks
     Sync *sync = reinterpret_cast<Sync *>(raw + 7 * kBytes);
     float *half_delta = reinterpret_cast<float *>(sync + 1);          // [2][128]
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform(static_cast<int>(threadIdx.x >> 5)), lane = threadIdx.x & 31;
     pdl_wait();
     const Work w = find_work(p, blockIdx.x, p.heads, true);
     if (w.packed && w.batch == p.batch) {
@@ -463,7 +453,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
     const int q0 = w.tile * kTile;
     if (q0 >= w.q_len) return;
     const int kv_head = w.head / p.group;
-    const int n = key_tiles(p, w, min(q0 + kTile, w.q_len) - 1);
+    const int n = uniform(key_tiles(p, w, min(q0 + kTile, w.q_len) - 1));
 
     constexpr uint32_t counts[qBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 8, 1};
     const uint32_t tmem = start_cta(sync, qBars, counts);
@@ -509,25 +499,20 @@ attention_dq_kernel(const __grid_constant__ Params p) {
                     if (issued_v > s) barrier_wait(bar(qVFull + s), ((issued_v - 1 - s) >> 1) & 1, nullptr, p.timeouts);
             }
         } else if (warp == kMmaWarp) {
+            const uint32_t leader = elect_leader();
             // K tile j is used by S_j and, transposed, by dQ_j; V tile j by dP_j
             auto scores = [&](int j) {
                 if (!wait(qKFull + j % 3, (j / 3) & 1)) return false;
                 if (w.packed && (j + 1) * kTile > w.k_len) clear_rows<HALVES>(sm_k + (j % 3) * kBytes, w.k_len - j * kTile);
-                if (lane == 0) {
-                    product_rows<T, DIM>(tm_s + (j & 1) * kTile, sm_q, sm_k + (j % 3) * kBytes);
-                    commit(bar(qS + (j & 1)));
-                }
-                __syncwarp();
+                product_rows<T, DIM>(leader, tm_s + (j & 1) * kTile, sm_q, sm_k + (j % 3) * kBytes);
+                commit(leader, bar(qS + (j & 1)));
                 return true;
             };
             auto dprobs = [&](int j) {
                 if (!wait(qVFull + (j & 1), (j >> 1) & 1)) return false;
-                if (lane == 0) {
-                    product_rows<T, DIM>(tm_dp, sm_g, sm_v + (j & 1) * kBytes);
-                    commit(bar(qDp));
-                    commit(bar(qVEmpty + (j & 1)));
-                }
-                __syncwarp();
+                product_rows<T, DIM>(leader, tm_dp, sm_g, sm_v + (j & 1) * kBytes);
+                commit(leader, bar(qDp));
+                commit(leader, bar(qVEmpty + (j & 1)));
                 return true;
             };
             bool ok = n == 0 || (wait(qQ, 0) && scores(0) && dprobs(0) && (n < 2 || scores(1)));
@@ -536,16 +521,12 @@ attention_dq_kernel(const __grid_constant__ Params p) {
                 if (!ok) break;
                 fence_after();
                 if (j + 1 < n && !(ok = dprobs(j + 1))) break;
-                if (lane == 0) {
-                    const uint32_t at = tm_s + (j & 1) * kTile;
-                    product_columns<T, DIM>(tm_dq, at, at + 64, sm_k + (j % 3) * kBytes, j > 0);
-                    commit(bar(qKEmpty + j % 3));
-                }
-                __syncwarp();
+                const uint32_t at = tm_s + (j & 1) * kTile;
+                product_columns<T, DIM>(leader, tm_dq, at, at + 64, sm_k + (j % 3) * kBytes, j > 0);
+                commit(leader, bar(qKEmpty + j % 3));
                 if (j + 2 < n) ok = scores(j + 2);                    // over dS_j, after its product
             }
-            if (lane == 0) commit(bar(qDone));
-            __syncwarp();
+            commit(leader, bar(qDone));
             barrier_wait(bar(qDone), 0, nullptr, p.timeouts);
         }
     } else {
@@ -661,7 +642,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
     const uint32_t base = smem_address(raw);
     float *stat = reinterpret_cast<float *>(raw + 7 * kBytes);        // [stage][-lse * log2 e, -delta][128]
     Sync *sync = reinterpret_cast<Sync *>(raw + 7 * kBytes + 2 * kStatBytes);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform(static_cast<int>(threadIdx.x >> 5)), lane = threadIdx.x & 31;
     pdl_wait();
     const int rank = p.split > 1 ? static_cast<int>(cluster_rank()) : 0;
     const Work w = find_work(p, blockIdx.x / p.split, p.kv_heads, false);
@@ -679,7 +660,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
     const int reach = w.k_len - w.q_len;                              // row i sees keys up to i + reach
     const int first = p.causal ? max(0, k0 - reach) / kTile : 0;
     const int each = max(0, (w.q_len + kTile - 1) / kTile - first);
-    const int n = (each * p.group - rank + p.split - 1) / p.split;
+    const int n = uniform((each * p.group - rank + p.split - 1) / p.split);
 
     constexpr uint32_t counts[kBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 8, 8, 1, 1, 1, 1, 1, 8, 1, 8, 1};
     const uint32_t tmem = start_cta(sync, kBars, counts);
@@ -736,28 +717,23 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                 }
             }
         } else if (warp == kMmaWarp) {
+            const uint32_t leader = elect_leader();
             // Q tile j is used by S_j and, transposed, by dK_j; G tile j by dP_j and, transposed, by dV_j
             auto rows_left = [&](int j) { return w.q_len - (first + (rank + j * p.split) % each) * kTile; };
             auto scores = [&](int j) {
                 const uint32_t tile = sm_q + (j % 3) * kBytes;
                 if (!wait(kQFull + j % 3, (j / 3) & 1)) return false;
                 if (w.packed && rows_left(j) < kTile) clear_rows<HALVES>(tile, rows_left(j));
-                if (lane == 0) {
-                    product_rows<T, DIM>(tm_s, sm_k, tile);
-                    commit(bar(kS));
-                }
-                __syncwarp();
+                product_rows<T, DIM>(leader, tm_s, sm_k, tile);
+                commit(leader, bar(kS));
                 return true;
             };
             auto dprobs = [&](int j) {
                 const uint32_t tile = sm_g + (j & 1) * kBytes;
                 if (!wait(kGFull + (j & 1), (j >> 1) & 1)) return false;
                 if (w.packed && rows_left(j) < kTile) clear_rows<HALVES>(tile, rows_left(j));
-                if (lane == 0) {
-                    product_rows<T, DIM>(tm_dp, sm_v, tile);
-                    commit(bar(kDp));
-                }
-                __syncwarp();
+                product_rows<T, DIM>(leader, tm_dp, sm_v, tile);
+                commit(leader, bar(kDp));
                 return true;
             };
             ok = n == 0 || (wait(kKv, 0) && scores(0) && dprobs(0));
@@ -765,24 +741,17 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                 ok = wait(kP, j & 1);                                 // P_j written over S_j
                 if (!ok) break;
                 fence_after();
-                if (lane == 0) {
-                    product_columns<T, DIM>(tm_dv, tm_s, tm_s + 64, sm_g + (j & 1) * kBytes, j > 0);
-                    commit(bar(kGEmpty + (j & 1)));
-                }
-                __syncwarp();
+                product_columns<T, DIM>(leader, tm_dv, tm_s, tm_s + 64, sm_g + (j & 1) * kBytes, j > 0);
+                commit(leader, bar(kGEmpty + (j & 1)));
                 if (j + 1 < n && !(ok = scores(j + 1))) break;
                 ok = wait(kDs, j & 1);                                // dS_j written over dP_j
                 if (!ok) break;
                 fence_after();
-                if (lane == 0) {
-                    product_columns<T, DIM>(tm_dk, tm_dp, tm_dp + 64, sm_q + (j % 3) * kBytes, j > 0);
-                    commit(bar(kQEmpty + j % 3));
-                }
-                __syncwarp();
+                product_columns<T, DIM>(leader, tm_dk, tm_dp, tm_dp + 64, sm_q + (j % 3) * kBytes, j > 0);
+                commit(leader, bar(kQEmpty + j % 3));
                 if (j + 1 < n) ok = dprobs(j + 1);
             }
-            if (lane == 0) commit(bar(kDone));
-            __syncwarp();
+            commit(leader, bar(kDone));
             barrier_wait(bar(kDone), 0, nullptr, p.timeouts);
         }
     } else {

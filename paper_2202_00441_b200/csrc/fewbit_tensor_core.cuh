@@ -153,37 +153,50 @@ template <typename T>
 __host__ __device__ constexpr uint32_t instruction(uint32_t n, bool b_mn) {
     return 1u << 4 | Format<T>::value << 7 | Format<T>::value << 10 | (b_mn ? 1u << 16 : 0u) | (n >> 3) << 17 | (128u >> 4) << 24;
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(accumulate)) : "memory");
+// The issuing warp runs these with all its lanes and in step: operands then live in uniform registers, where the instruction
+// takes them, and only `leader` (one lane's 1, chosen by elect) issues.  In a branch of one lane every operand is moved there
+// first, and an MMA takes 110 clocks to issue in place of the 64 that it computes.
+__device__ __forceinline__ uint32_t elect_leader() {
+    uint32_t leader;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(leader));
+    return leader;
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
-    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-                 :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(accumulate)) : "memory");
+template <typename V>
+__device__ __forceinline__ V uniform(V x) { return __shfl_sync(0xffffffffu, x, 0); }
+__device__ __forceinline__ void mma_ss(uint32_t leader, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(accumulate)), "r"(leader) : "memory");
 }
-// the barrier's phase ends when every MMA issued so far by this thread has finished
-__device__ __forceinline__ void commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(bar) : "memory");
+__device__ __forceinline__ void mma_ts(uint32_t leader, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 q, %5, 0;\n@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+                 :: "r"(d), "r"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(accumulate)), "r"(leader) : "memory");
+}
+// the barrier's phase ends when every MMA issued so far by the leader has finished
+__device__ __forceinline__ void commit(uint32_t leader, uint32_t bar) {
+    asm volatile("{\n.reg .pred q;\nsetp.ne.b32 q, %1, 0;\n@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}"
+                 :: "r"(bar), "r"(leader) : "memory");
 }
 
 // D (128 x 128) = A B^T over DIM: both tiles K-major
 template <typename T, int DIM>
-__device__ __forceinline__ void product_rows(uint32_t d, uint32_t a, uint32_t b) {
+__device__ __forceinline__ void product_rows(uint32_t leader, uint32_t d, uint32_t a, uint32_t b) {
     constexpr uint32_t idesc = instruction<T>(128, false);
+    const uint64_t da = k_major(a), db = k_major(b);
 #pragma unroll
     for (int k = 0; k < DIM / 16; ++k) {
-        const uint32_t off = (k / 4) * kHalfTile + (k % 4) * 32;
-        mma_ss(d, k_major(a + off), k_major(b + off), idesc, k > 0);
+        const uint64_t off = ((k / 4) * kHalfTile + (k % 4) * 32) >> 4;
+        mma_ss(leader, d, da + off, db + off, idesc, k > 0);
     }
 }
 // D (128 x DIM) (+)= A B over steps [FIRST, LAST) of 16: A (128 x 128, 16 bits) in tensor memory, 16 columns of its
 // contraction in 8 TMEM columns, the second 64 of them at `a2`; B's rows are the contraction
 template <typename T, int DIM, int FIRST = 0, int LAST = 8>
-__device__ __forceinline__ void product_columns(uint32_t d, uint32_t a, uint32_t a2, uint32_t b, bool accumulate) {
+__device__ __forceinline__ void product_columns(uint32_t leader, uint32_t d, uint32_t a, uint32_t a2, uint32_t b, bool accumulate) {
     constexpr uint32_t idesc = instruction<T>(DIM, true);
+    const uint64_t db = mn_major(b);
 #pragma unroll
     for (int k = FIRST; k < LAST; ++k)
-        mma_ts(d, k < 4 ? a + 8 * k : a2 + 8 * (k - 4), mn_major(b + k * 2048), idesc, accumulate || k > FIRST);
+        mma_ts(leader, d, k < 4 ? a + 8 * k : a2 + 8 * (k - 4), db + k * (2048 >> 4), idesc, accumulate || k > FIRST);
 }
 
 template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
