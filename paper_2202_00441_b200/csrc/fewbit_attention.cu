@@ -196,6 +196,7 @@ fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *s, const fewbit
     if (st != FEWBIT_OK) return st;
     p.o = rows_of(out);
     p.go = rows_of(grad_out);
+    p.kin = rows_of(k);
     p.dq = rows_of(grad_q);
     p.dk = rows_of(grad_k);
     p.dv = rows_of(grad_v);

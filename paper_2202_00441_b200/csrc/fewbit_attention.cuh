@@ -4,11 +4,11 @@
 //   S = c Q K^T,  P = exp(S - lse),  O = P V            lse_i = log sum_j exp(S_ij)
 //   delta_i = dO_i . O_i,  dV = P^T dO,  dP = dO V^T,  dS = P (dP - delta),  dQ = c dS K,  dK = c dS^T Q
 //
-// Every kernel has the same roles: warps 0-7 do the element-wise work (a thread owns a row of 128 and half or all
-// of a tile's columns, so row sums never leave the thread), warp 8 issues tcgen05.mma, warp 9 the TMA loads.
+// Every kernel has the same roles: warps 0-15 do the element-wise work (a thread owns a row of 128 and a quarter or
+// half of a tile's columns), warp 16 issues tcgen05.mma, warp 17 the TMA loads.
 // Tiles are 128 x 128; the second operand of a "columns" product is the same shared-memory tile that served the
 // "rows" product, read the other way round, and its first operand (P or dS, rounded to 16 bits) goes through
-// tensor memory, so nothing element-wise ever touches shared memory.
+// tensor memory, so no tile of element-wise results ever touches shared memory.
 //
 //   forward   two row tiles a CTA: one tile's softmax runs while the other's products do
 //   dQ        one row tile against all keys: S, dP, dQ (3 products); writes the rows' -lse and -delta for the next kernel
@@ -33,10 +33,11 @@ namespace attn {
 using namespace tc;
 
 constexpr int kTile = 128;
-constexpr int kThreadsAttn = 384;      // three warpgroups: two element-wise ones, and the MMA and load warps (two idle ones fill it up)
-constexpr int kMmaWarp = 8, kLoadWarp = 9;
-// 168 registers a thread at launch: 2 x 128 x 208 + 128 x 80 = 63488 of 64512
-constexpr int kWorkRegisters = 208, kIssueRegisters = 80;
+constexpr int kThreadsAttn = 640;      // five warpgroups: four element-wise ones, and the MMA and load warps (two idle ones fill it up)
+constexpr int kMmaWarp = 16, kLoadWarp = 17;
+constexpr int kWorkThreads = 512;
+// 96 registers a thread at launch: 512 x 104 + 128 x 64 = 61440 = 640 x 96
+constexpr int kWorkRegisters = 104, kIssueRegisters = 64;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kStatBytes = 2 * kTile * 4;   // a row tile's -lse * log2(e) and -delta
 
@@ -46,7 +47,7 @@ struct Rows {                         // an output tensor
 };
 struct Params {
     CUtensorMap q, k, v, g;           // g: the gradient of the output
-    Rows out, o, go, dq, dk, dv;      // o, go: outputs and their gradients, read row by row for delta
+    Rows out, o, go, kin, dq, dk, dv; // o, go: outputs and their gradients, read row by row for delta; kin: k, read row by row
     float *lse, *stat;                // stat: a block of kStatBytes for each row tile
     const int *q_offsets, *k_offsets;
     unsigned int *timeouts;
@@ -105,7 +106,7 @@ __device__ __forceinline__ int key_tiles(const Params &p, const Work &w, int las
 
 // Shared memory: tiles first (1 KB aligned), then the barriers.
 struct Sync {
-    unsigned long long bar[20];
+    unsigned long long bar[26];
     uint32_t tmem;
     int stop;
 };
@@ -129,11 +130,11 @@ __device__ __forceinline__ void load_halves(uint32_t dst, const CUtensorMap *map
     for (int h = 0; h < HALVES; ++h) load_tile(dst + h * kHalfTile, map, 64 * h, row, head, batch, bar);
 }
 
-// 32 values of one row, scaled and rounded, to columns [col, col + 32) of a tensor of `dim` columns.
-template <typename T>
+// N values of one row, scaled and rounded, to columns [col, col + N) of a tensor of `dim` columns.
+template <typename T, int N>
 __device__ __forceinline__ void store_columns(T *row, int col, int dim, const uint32_t *r, float factor) {
 #pragma unroll
-    for (int c = 0; c < 32; c += 8) {
+    for (int c = 0; c < N; c += 8) {
         if (col + c >= dim) break;                                    // dim is a multiple of 8
         uint4 v;
         v.x = pack2<T>(__uint_as_float(r[c]) * factor, __uint_as_float(r[c + 1]) * factor);
@@ -203,11 +204,20 @@ __device__ __forceinline__ void end_cta(uint32_t tmem) {
 // ---------------------------------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------------------------------
-// Barriers: q (2 row tiles), k full/empty (2 stages), v full/empty, S full (2), first three quarters of P ready (2), all of
-// it (2), O done (2), drained.
+// Barriers: q (2 row tiles), k full/empty (2 stages), v full/empty, S full (2), the first half of each thread's part of P
+// ready (2), all of it (2), O done (2), drained.
 enum { fQ = 0, fKFull = 2, fKEmpty = 4, fVFull = 6, fVEmpty = 8, fS = 10, fP = 12, fPEnd = 14, fO = 16, fDrain = 18, fBars = 19 };
 
-template <int DIM> constexpr int fwd_smem() { return 6 * (DIM / 64) * static_cast<int>(kHalfTile) + 1024 + static_cast<int>(sizeof(Sync)); }
+template <int DIM> constexpr int fwd_smem() { return 6 * (DIM / 64) * static_cast<int>(kHalfTile) + 1024 + static_cast<int>(sizeof(Sync)) + 4 * kTile * 4; }
+
+// Barriers of the 256 threads of one row tile.
+__device__ __forceinline__ void tile_barrier(int id) { asm volatile("bar.sync %0, 256;" :: "r"(id) : "memory"); }
+__device__ __forceinline__ bool tile_any(int id, bool x) {
+    uint32_t any;
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %1, 0;\nbarrier.cta.red.or.pred q, %2, 256, p;\nselp.u32 %0, 1, 0, q;\n}"
+                 : "=r"(any) : "r"(static_cast<uint32_t>(x)), "r"(id) : "memory");
+    return any != 0;
+}
 
 // 32 columns of a row: probabilities, rounded to `s_at`, and their sum.  MIXED: a quarter of them on the FMA pipe.
 template <typename T, bool MIXED>
@@ -232,6 +242,7 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_address(raw) + 1023u) & ~1023u;
     Sync *sync = reinterpret_cast<Sync *>(raw + (base - smem_address(raw)) + 6 * kBytes);
+    float *exchange = reinterpret_cast<float *>(sync + 1);            // [row tile][half][128]
     const int warp = uniform(static_cast<int>(threadIdx.x >> 5)), lane = threadIdx.x & 31;
     pdl_wait();
     const Work w = find_work(p, blockIdx.x, p.heads, true);
@@ -247,12 +258,12 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
     const int n1 = uniform(q0 + kTile < w.q_len ? key_tiles(p, w, min(q0 + 2 * kTile, w.q_len) - 1) : 0);
     const int n = max(n0, n1);
 
-    constexpr uint32_t counts[fBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 4, 4, 4, 4, 1, 1, 1};
+    constexpr uint32_t counts[fBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 8, 8, 8, 8, 1, 1, 1};
     const uint32_t tmem = start_cta(sync, fBars, counts);
     auto bar = [&](int i) { return smem_address(&sync->bar[i]); };
     auto wait = [&](int i, uint32_t parity) { return barrier_wait(bar(i), parity, &sync->stop, p.timeouts); };
     const uint32_t sm_q = base, sm_k = base + 2 * kBytes, sm_v = base + 4 * kBytes;
-    // tensor memory: S (and P in its first half) of both row tiles, then O of both
+    // tensor memory: S of both row tiles (each half of P in the first half of the scores that it came from), then O of both
     const uint32_t tm_s = tmem, tm_o = tmem + 2 * kTile;
 
     if (warp >= kMmaWarp) {
@@ -315,15 +326,15 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
                     const int nt = t ? n1 : n0;
                     if (j >= nt) continue;
                     const uint32_t at = tm_s + t * kTile;
-                    // the product starts on three quarters of P while the last one is computed
+                    // the product starts on one half of P while the other is computed
                     ok = wait(fP + t, j & 1);
                     if (!ok) break;
                     fence_after();
-                    product_columns<T, DIM, 0, 6>(leader, tm_o + t * kTile, at, at + 32, sm_v + (j & 1) * kBytes, j > 0);
+                    product_columns<T, DIM, 4, 64, 0x33>(leader, tm_o + t * kTile, at, sm_v + (j & 1) * kBytes, j > 0);
                     ok = wait(fPEnd + t, j & 1);
                     if (!ok) break;
                     fence_after();
-                    product_columns<T, DIM, 6, 8>(leader, tm_o + t * kTile, at, at + 32, sm_v + (j & 1) * kBytes, true);
+                    product_columns<T, DIM, 4, 64, 0xcc>(leader, tm_o + t * kTile, at, sm_v + (j & 1) * kBytes, true);
                     commit(leader, bar(fO + t));
                     if (j + 1 < nt) scores(t, j + 1);
                 }
@@ -335,49 +346,61 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
         }
     } else {
         take_registers<kWorkRegisters>();
-        const int t = warp >> 2;                                      // row tile
-        const int nt = t ? n1 : n0;
-        const int i = q0 + t * kTile + (threadIdx.x & 127);           // this thread's row
+        const int t = warp >> 3, half = (warp >> 2) & 1;              // row tile; columns [64 half, 64 half + 64) of every key tile
+        const int nt = t ? n1 : n0, r = threadIdx.x & 127;
+        const int i = q0 + t * kTile + r;                             // this thread's row
         const uint32_t my_lane = static_cast<uint32_t>(warp & 3) << 21;
-        const uint32_t s_at = tm_s + t * kTile + my_lane, o_at = tm_o + t * kTile + my_lane;
+        const uint32_t s_at = tm_s + t * kTile + 64 * half + my_lane, o_at = tm_o + t * kTile + half * (DIM / 2) + my_lane;
+        float *mine = exchange + (2 * t + half) * kTile + r, *other = exchange + (2 * t + 1 - half) * kTile + r;
         // the row sees keys [0, seen)
         const int seen = p.causal ? min(w.k_len, i + 1 + w.k_len - w.q_len) : w.k_len;
         const int tile_seen = p.causal ? min(w.k_len, q0 + t * kTile + 1 + w.k_len - w.q_len) : w.k_len;   // by its first row
-        float top = -INFINITY, sum = 0.0f;                            // of the raw products
+        float top = -INFINITY, sum = 0.0f;                            // of the raw products; the sum of this thread's columns
         bool ok = true;
         for (int j = 0; j < nt; ++j) {
-            ok = wait(fS + t, j & 1);
-            if (!ok) break;
+            ok = wait(fS + t, j & 1);                                 // (a wait given up ends the loop below, for all threads of the tile)
             fence_after();
-            uint32_t s[128];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld32(s_at + 32 * c, s + 32 * c);
+            uint32_t s[64];
+            tmem_ld32(s_at, s);
+            tmem_ld32(s_at + 32, s + 32);
             wait_ld();
             const bool edge = (j + 1) * kTile > tile_seen;
             if (edge) {
-                const int limit = seen - j * kTile;
+                const int limit = seen - j * kTile - 64 * half;
 #pragma unroll
-                for (int c = 0; c < 128; ++c) s[c] = c < limit ? s[c] : 0xff800000u;
+                for (int c = 0; c < 64; ++c) s[c] = c < limit ? s[c] : 0xff800000u;
             }
             float best[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int c = 0; c < 128; c += 2)                          // two at a time: a three-operand maximum
+            for (int c = 0; c < 64; c += 2)                           // two at a time: a three-operand maximum
                 best[(c >> 1) & 3] = fmaxf(best[(c >> 1) & 3], fmaxf(__uint_as_float(s[c]), __uint_as_float(s[c + 1])));
             const float high = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3]));
             // The sums' reference moves only when a product passes it by 2^8: until then probabilities up to 2^8
-            // are held, which cost no precision, and O needs no rescaling.
-            const bool move = high > top && (high - top) * p.scale_log2 > 8.0f;
-            if (__any_sync(0xffffffffu, move)) {
-                const float next = move ? high : top;
+            // are held, which cost no precision, and O needs no rescaling.  The row's two threads move it together: whether
+            // any row of the tile's 256 threads moves is one barrier, and only then they exchange their maxima.
+            const bool above = high > top && (high - top) * p.scale_log2 > 8.0f;
+            if (tile_any(1 + t, above || !ok)) {
+                if (tile_any(1 + t, !ok)) {
+                    ok = false;
+                    break;
+                }
+                *mine = high;
+                tile_barrier(1 + t);
+                const float row_high = fmaxf(high, *other);
+                const bool move = row_high > top && (row_high - top) * p.scale_log2 > 8.0f;
+                const float next = move ? row_high : top;
                 const float factor = move ? exp2_fast((top - next) * p.scale_log2) : 1.0f;
                 top = next;
                 sum *= factor;
                 if (j > 0) {
                     ok = wait(fO + t, (j - 1) & 1);
-                    if (!ok) break;
+                    if (tile_any(1 + t, !ok)) {
+                        ok = false;
+                        break;
+                    }
                     fence_after();
 #pragma unroll
-                    for (int c = 0; c < DIM / 32; ++c) {
+                    for (int c = 0; c < DIM / 64; ++c) {
                         uint32_t o[32];
                         tmem_ld32(o_at + 32 * c, o);
                         wait_ld();
@@ -390,36 +413,37 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
             const float shift = top == -INFINITY ? 0.0f : -top * p.scale_log2;
             float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
+            for (int c = 0; c < 2; ++c) {
                 if (edge) fwd_probabilities<T, false>(s + 32 * c, p.scale_log2, shift, part, s_at + 16 * c);
                 else fwd_probabilities<T, true>(s + 32 * c, p.scale_log2, shift, part, s_at + 16 * c);
-                if (c >= 2) {
-                    wait_st();
-                    fence_before();
-                    __syncwarp();
-                    if (lane == 0) barrier_arrive(bar((c == 2 ? fP : fPEnd) + t));
-                }
+                wait_st();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) barrier_arrive(bar((c == 0 ? fP : fPEnd) + t));
             }
             sum += (part[0] + part[1]) + (part[2] + part[3]);
         }
         if (nt > 0 && ok) ok = wait(fO + t, (nt - 1) & 1);
         fence_after();
+        *mine = sum;                                                  // (the last exchange of maxima was read before P was ready)
+        tile_barrier(1 + t);
+        sum += *other;
         if (ok) {
             const bool live = i < w.q_len;
             T *row = static_cast<T *>(p.out.p) + (live ? row_of(w, p.out, w.head, i, w.q_first) : 0);
             if (nt > 0) {
                 const float factor = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
 #pragma unroll
-                for (int c = 0; c < DIM / 32; ++c) {
+                for (int c = 0; c < DIM / 64; ++c) {
                     uint32_t o[32];
                     tmem_ld32(o_at + 32 * c, o);
                     wait_ld();
-                    if (live) store_columns<T>(row, 32 * c, p.dim, o, factor);
+                    if (live) store_columns<T, 32>(row, half * (DIM / 2) + 32 * c, p.dim, o, factor);
                 }
-            } else if (live) {
+            } else if (live && half == 0) {
                 zero_columns<T>(row, p.dim);
             }
-            if (live) p.lse[stat_of(p, w, w.head, i)] = sum == 0.0f ? -INFINITY : top * p.scale + logf(sum);
+            if (live && half == 0) p.lse[stat_of(p, w, w.head, i)] = sum == 0.0f ? -INFINITY : top * p.scale + logf(sum);
         }
     }
     end_cta(tmem);
@@ -432,7 +456,7 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
 // dP full, dS ready, dQ done.
 enum { qQ = 0, qKFull = 1, qKEmpty = 4, qVFull = 7, qVEmpty = 9, qS = 11, qDp = 13, qDs = 14, qDone = 15, qBars = 16 };
 
-template <int DIM> constexpr int dq_smem() { return 7 * (DIM / 64) * static_cast<int>(kHalfTile) + static_cast<int>(sizeof(Sync)) + 2 * kTile * 4; }
+template <int DIM> constexpr int dq_smem() { return 7 * (DIM / 64) * static_cast<int>(kHalfTile) + static_cast<int>(sizeof(Sync)) + 4 * kTile * 4; }
 
 template <typename T, int DIM>
 __global__ void __launch_bounds__(kThreadsAttn, 1)
@@ -442,7 +466,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
     extern __shared__ __align__(1024) uint8_t raw[];
     const uint32_t base = smem_address(raw);                          // no room to align it here: the host checks
     Sync *sync = reinterpret_cast<Sync *>(raw + 7 * kBytes);
-    float *half_delta = reinterpret_cast<float *>(sync + 1);          // [2][128]
+    float *part_delta = reinterpret_cast<float *>(sync + 1);          // [4][128]
     const int warp = uniform(static_cast<int>(threadIdx.x >> 5)), lane = threadIdx.x & 31;
     pdl_wait();
     const Work w = find_work(p, blockIdx.x, p.heads, true);
@@ -455,7 +479,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
     const int kv_head = w.head / p.group;
     const int n = uniform(key_tiles(p, w, min(q0 + kTile, w.q_len) - 1));
 
-    constexpr uint32_t counts[qBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 8, 1};
+    constexpr uint32_t counts[qBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 16, 1};
     const uint32_t tmem = start_cta(sync, qBars, counts);
     auto bar = [&](int i) { return smem_address(&sync->bar[i]); };
     auto wait = [&](int i, uint32_t parity) { return barrier_wait(bar(i), parity, &sync->stop, p.timeouts); };
@@ -522,7 +546,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
                 fence_after();
                 if (j + 1 < n && !(ok = dprobs(j + 1))) break;
                 const uint32_t at = tm_s + (j & 1) * kTile;
-                product_columns<T, DIM>(leader, tm_dq, at, at + 64, sm_k + (j % 3) * kBytes, j > 0);
+                product_columns<T, DIM, 2, 32>(leader, tm_dq, at, sm_k + (j % 3) * kBytes, j > 0);
                 commit(leader, bar(qKEmpty + j % 3));
                 if (j + 2 < n) ok = scores(j + 2);                    // over dS_j, after its product
             }
@@ -531,7 +555,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
         }
     } else {
         take_registers<kWorkRegisters>();
-        const int part = warp >> 2;                                   // columns [64 part, 64 part + 64) of every tile
+        const int part = warp >> 2;                                   // columns [32 part, 32 part + 32) of every tile
         const int r = threadIdx.x & 127, i = q0 + r;
         const bool live = i < w.q_len;
         const uint32_t my_lane = static_cast<uint32_t>(warp & 3) << 21;
@@ -539,7 +563,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
         if (live) {
             const T *o = static_cast<const T *>(p.o.p) + row_of(w, p.o, w.head, i, w.q_first);
             const T *g = static_cast<const T *>(p.go.p) + row_of(w, p.go, w.head, i, w.q_first);
-            for (int c = 8 * part; c < p.dim; c += 16) {
+            for (int c = 8 * part; c < p.dim; c += 32) {
                 float a[8], b[8];
                 load8(o + c, a);
                 load8(g + c, b);
@@ -549,31 +573,30 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             const float l = p.lse[stat_of(p, w, w.head, i)];
             if (l != -INFINITY) minus_lse = -l * kLog2e;
         }
-        half_delta[part * kTile + r] = delta;
-        asm volatile("bar.sync 1, 256;" ::: "memory");                // the element-wise warps only
-        const float minus_delta = -(half_delta[r] + half_delta[kTile + r]);
-        stat_block(p, w, w.head, w.tile)[part * kTile + r] = part == 0 ? minus_lse : minus_delta;
+        part_delta[part * kTile + r] = delta;
+        asm volatile("bar.sync 1, %0;" :: "n"(kWorkThreads) : "memory");   // the element-wise warps only
+        const float minus_delta = -((part_delta[r] + part_delta[kTile + r]) + (part_delta[2 * kTile + r] + part_delta[3 * kTile + r]));
+        if (part < 2) stat_block(p, w, w.head, w.tile)[part * kTile + r] = part == 0 ? minus_lse : minus_delta;
         const int seen = p.causal ? min(w.k_len, i + 1 + w.k_len - w.q_len) : w.k_len;
         const int tile_seen = p.causal ? min(w.k_len, q0 + 1 + w.k_len - w.q_len) : w.k_len;
         bool ok = true;
         for (int j = 0; j < n; ++j) {
-            const uint32_t s_at = tm_s + (j & 1) * kTile + 64 * part + my_lane, dp_at = tm_dp + 64 * part + my_lane;
+            const uint32_t s_at = tm_s + (j & 1) * kTile + 32 * part + my_lane;
             ok = wait(qS + (j & 1), (j >> 1) & 1);
             if (!ok) break;
             fence_after();
-            uint32_t s[64], d[64], out[32];
-            float prob[64];
+            uint32_t s[32], d[32], out[16];
+            float prob[32];
             tmem_ld32(s_at, s);
-            tmem_ld32(s_at + 32, s + 32);
             wait_ld();
             const bool edge = (j + 1) * kTile > tile_seen;
             if (edge) {
 #pragma unroll
-                for (int c = 0; c < 64; c += 2)
+                for (int c = 0; c < 32; c += 2)
                     exp2_scaled<false>(prob[c], prob[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), p.scale_log2, minus_lse, minus_lse);
             } else {
 #pragma unroll
-                for (int c = 0; c < 64; c += 2) {
+                for (int c = 0; c < 32; c += 2) {
                     if (c % 8 == 6) exp2_scaled<true>(prob[c], prob[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), p.scale_log2, minus_lse, minus_lse);
                     else exp2_scaled<false>(prob[c], prob[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), p.scale_log2, minus_lse, minus_lse);
                 }
@@ -581,23 +604,22 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             ok = wait(qDp, j & 1);
             if (!ok) break;
             fence_after();
-            tmem_ld32(dp_at, d);
-            tmem_ld32(dp_at + 32, d + 32);
+            tmem_ld32(tm_dp + 32 * part + my_lane, d);
             wait_ld();
-            float ds[64];
+            float ds[32];
 #pragma unroll
-            for (int c = 0; c < 64; c += 2) {
+            for (int c = 0; c < 32; c += 2) {
                 add2(ds[c], ds[c + 1], __uint_as_float(d[c]), __uint_as_float(d[c + 1]), minus_delta, minus_delta);
                 mul2(ds[c], ds[c + 1], ds[c], ds[c + 1], prob[c], prob[c + 1]);
             }
             if (edge) {                                               // places that the row does not see, whatever they hold
-                const int limit = seen - j * kTile - 64 * part;
+                const int limit = seen - j * kTile - 32 * part;
 #pragma unroll
-                for (int c = 0; c < 64; ++c) ds[c] = c < limit ? ds[c] : 0.0f;
+                for (int c = 0; c < 32; ++c) ds[c] = c < limit ? ds[c] : 0.0f;
             }
 #pragma unroll
-            for (int c = 0; c < 32; ++c) out[c] = pack2<T>(ds[2 * c], ds[2 * c + 1]);
-            tmem_st32(s_at, out);                                     // over the first half of what this thread read
+            for (int c = 0; c < 16; ++c) out[c] = pack2<T>(ds[2 * c], ds[2 * c + 1]);
+            tmem_st16(s_at, out);                                     // over the first half of what this thread read
             wait_st();
             fence_before();
             __syncwarp();
@@ -608,14 +630,11 @@ attention_dq_kernel(const __grid_constant__ Params p) {
         if (ok) {
             T *row = static_cast<T *>(p.dq.p) + (live ? row_of(w, p.dq, w.head, i, w.q_first) : 0);
             if (n > 0) {
-#pragma unroll
-                for (int c = 0; c < DIM / 64; ++c) {
-                    uint32_t o[32];
-                    const int col = part * (DIM / 2) + 32 * c;
-                    tmem_ld32(tm_dq + my_lane + col, o);
-                    wait_ld();
-                    if (live) store_columns<T>(row, col, p.dim, o, p.scale);
-                }
+                uint32_t o[DIM / 4];
+                if constexpr (DIM == 128) tmem_ld32(tm_dq + my_lane + 32 * part, o);
+                else tmem_ld16(tm_dq + my_lane + 16 * part, o);
+                wait_ld();
+                if (live) store_columns<T, DIM / 4>(row, part * (DIM / 4), p.dim, o, p.scale);
             } else if (live && part == 0) {
                 zero_columns<T>(row, p.dim);
             }
@@ -627,9 +646,10 @@ attention_dq_kernel(const __grid_constant__ Params p) {
 // ---------------------------------------------------------------------------------------------------
 // backward, dK and dV
 // ---------------------------------------------------------------------------------------------------
-// Barriers: k and v, q full/empty (3 stages: a tile is used twice, one iteration apart), statistics full/empty (2 stages),
-// g full/empty (2 stages), S full, P ready, dP full, dS ready, done.
-enum { kKv = 0, kQFull = 1, kQEmpty = 4, kTFull = 7, kTEmpty = 9, kGFull = 11, kGEmpty = 13, kS = 15, kP = 16, kDp = 17, kDs = 18, kDone = 19, kBars = 20 };
+// Barriers: v, k in tensor memory, q full/empty (3 stages), g full/empty (3 stages), statistics full/empty (2 stages), S full
+// and read, dP full, P ready (and dP read) and used, dS ready and used, done.
+enum { kV = 0, kK = 1, kQFull = 2, kQEmpty = 5, kGFull = 8, kGEmpty = 11, kTFull = 14, kTEmpty = 16, kS = 18, kSRead = 19, kDp = 20, kP = 21, kPUsed = 22,
+       kDs = 23, kDsUsed = 24, kDone = 25, kBars = 26 };
 
 template <int DIM> constexpr int dkv_smem() { return 7 * (DIM / 64) * static_cast<int>(kHalfTile) + 2 * kStatBytes + static_cast<int>(sizeof(Sync)); }
 
@@ -662,13 +682,14 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
     const int each = max(0, (w.q_len + kTile - 1) / kTile - first);
     const int n = uniform((each * p.group - rank + p.split - 1) / p.split);
 
-    constexpr uint32_t counts[kBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 8, 8, 1, 1, 1, 1, 1, 8, 1, 8, 1};
+    constexpr uint32_t counts[kBars] = {1, 16, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 16, 16, 1, 16, 1, 16, 1, 16, 1, 1};
     const uint32_t tmem = start_cta(sync, kBars, counts);
     auto bar = [&](int i) { return smem_address(&sync->bar[i]); };
     auto wait = [&](int i, uint32_t parity) { return barrier_wait(bar(i), parity, &sync->stop, p.timeouts); };
-    const uint32_t sm_k = base, sm_v = base + kBytes, sm_q = base + 2 * kBytes, sm_g = base + 5 * kBytes;
-    // tensor memory: S (P in its place), dP (dS in its place), dV, dK
-    const uint32_t tm_s = tmem, tm_dp = tmem + kTile, tm_dv = tmem + 2 * kTile, tm_dk = tmem + 3 * kTile;
+    const uint32_t sm_v = base, sm_q = base + kBytes, sm_g = base + 4 * kBytes;
+    // tensor memory: one place for S and dP in turn (each is read into registers at once, which frees it), one for P and dS in
+    // turn, the K tile, dV, dK
+    const uint32_t tm_s = tmem, tm_dp = tmem, tm_p = tmem + kTile, tm_ds = tm_p, tm_k = tm_p + kTile / 2, tm_dv = tmem + 2 * kTile, tm_dk = tmem + 3 * kTile;
 
     bool ok = true;
     if (warp >= kMmaWarp) {
@@ -677,12 +698,10 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             int issued_q = 0, issued_t = 0, issued_g = 0;
             if (n > 0 && lane == 0) {
                 prefetch_map(&p.q);
-                prefetch_map(&p.k);
                 prefetch_map(&p.v);
                 prefetch_map(&p.g);
-                barrier_expect(bar(kKv), 2 * kBytes);
-                load_halves<HALVES>(sm_k, &p.k, w.k_first + k0, w.head, w.q_batch, bar(kKv));
-                load_halves<HALVES>(sm_v, &p.v, w.k_first + k0, w.head, w.q_batch, bar(kKv));
+                barrier_expect(bar(kV), kBytes);
+                load_halves<HALVES>(sm_v, &p.v, w.k_first + k0, w.head, w.q_batch, bar(kV));
             }
             for (int j = 0; j < n; ++j) {
                 const int s = j & 1, s3 = j % 3, at = rank + j * p.split;
@@ -700,21 +719,21 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                     load_bytes(smem_address(stat + s * 2 * kTile), stat_block(p, w, head, tile), kStatBytes, bar(kTFull + s));
                 }
                 issued_t = j + 1;
-                if (!wait(kGEmpty + s, again)) break;
+                if (!wait(kGEmpty + s3, ((j / 3) & 1) ^ 1)) break;
                 if (lane == 0) {
-                    barrier_expect(bar(kGFull + s), kBytes);
-                    load_halves<HALVES>(sm_g + s * kBytes, &p.g, w.q_first + q0, head, w.q_batch, bar(kGFull + s));
+                    barrier_expect(bar(kGFull + s3), kBytes);
+                    load_halves<HALVES>(sm_g + s3 * kBytes, &p.g, w.q_first + q0, head, w.q_batch, bar(kGFull + s3));
                 }
                 issued_g = j + 1;
             }
             if (stopped(sync)) {
-                if (n > 0) barrier_wait(bar(kKv), 0, nullptr, p.timeouts);
-                for (int s = 0; s < 3; ++s)
+                if (n > 0) barrier_wait(bar(kV), 0, nullptr, p.timeouts);
+                for (int s = 0; s < 3; ++s) {
                     if (issued_q > s) barrier_wait(bar(kQFull + s), ((issued_q - 1 - s) / 3) & 1, nullptr, p.timeouts);
-                for (int s = 0; s < 2; ++s) {
-                    if (issued_t > s) barrier_wait(bar(kTFull + s), ((issued_t - 1 - s) >> 1) & 1, nullptr, p.timeouts);
-                    if (issued_g > s) barrier_wait(bar(kGFull + s), ((issued_g - 1 - s) >> 1) & 1, nullptr, p.timeouts);
+                    if (issued_g > s) barrier_wait(bar(kGFull + s), ((issued_g - 1 - s) / 3) & 1, nullptr, p.timeouts);
                 }
+                for (int s = 0; s < 2; ++s)
+                    if (issued_t > s) barrier_wait(bar(kTFull + s), ((issued_t - 1 - s) >> 1) & 1, nullptr, p.timeouts);
             }
         } else if (warp == kMmaWarp) {
             const uint32_t leader = elect_leader();
@@ -724,68 +743,100 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                 const uint32_t tile = sm_q + (j % 3) * kBytes;
                 if (!wait(kQFull + j % 3, (j / 3) & 1)) return false;
                 if (w.packed && rows_left(j) < kTile) clear_rows<HALVES>(tile, rows_left(j));
-                product_rows<T, DIM>(leader, tm_s, sm_k, tile);
+                product_rows_tmem<T, DIM>(leader, tm_s, tm_k, tile);
                 commit(leader, bar(kS));
                 return true;
             };
             auto dprobs = [&](int j) {
-                const uint32_t tile = sm_g + (j & 1) * kBytes;
-                if (!wait(kGFull + (j & 1), (j >> 1) & 1)) return false;
+                const uint32_t tile = sm_g + (j % 3) * kBytes;
+                if (!wait(kGFull + j % 3, (j / 3) & 1)) return false;
                 if (w.packed && rows_left(j) < kTile) clear_rows<HALVES>(tile, rows_left(j));
                 product_rows<T, DIM>(leader, tm_dp, sm_v, tile);
                 commit(leader, bar(kDp));
                 return true;
             };
-            ok = n == 0 || (wait(kKv, 0) && scores(0) && dprobs(0));
+            ok = n == 0 || wait(kK, 0);
+            fence_after();
+            ok = ok && (n == 0 || (scores(0) && wait(kV, 0) && wait(kSRead, 0)));
+            fence_after();
+            if (ok && n > 0) ok = dprobs(0);
             for (int j = 0; ok && j < n; ++j) {
-                ok = wait(kP, j & 1);                                 // P_j written over S_j
+                ok = wait(kP, j & 1);                                 // P_j written, and dP_j in registers: S_j+1 may take its place
                 if (!ok) break;
                 fence_after();
-                product_columns<T, DIM>(leader, tm_dv, tm_s, tm_s + 64, sm_g + (j & 1) * kBytes, j > 0);
-                commit(leader, bar(kGEmpty + (j & 1)));
+                product_columns<T, DIM, 8, 64>(leader, tm_dv, tm_p, sm_g + (j % 3) * kBytes, j > 0);
+                commit(leader, bar(kPUsed));
+                commit(leader, bar(kGEmpty + j % 3));
                 if (j + 1 < n && !(ok = scores(j + 1))) break;
-                ok = wait(kDs, j & 1);                                // dS_j written over dP_j
+                ok = wait(kDs, j & 1);                                // dS_j written over P_j
                 if (!ok) break;
                 fence_after();
-                product_columns<T, DIM>(leader, tm_dk, tm_dp, tm_dp + 64, sm_q + (j % 3) * kBytes, j > 0);
+                product_columns<T, DIM, 8, 64>(leader, tm_dk, tm_ds, sm_q + (j % 3) * kBytes, j > 0);
+                commit(leader, bar(kDsUsed));
                 commit(leader, bar(kQEmpty + j % 3));
-                if (j + 1 < n) ok = dprobs(j + 1);
+                if (j + 1 < n) {
+                    ok = wait(kSRead, (j + 1) & 1);                   // S_j+1 is in registers: dP_j+1 may take its place
+                    if (!ok) break;
+                    fence_after();
+                    ok = dprobs(j + 1);
+                }
             }
             commit(leader, bar(kDone));
             barrier_wait(bar(kDone), 0, nullptr, p.timeouts);
         }
+        if (p.split > 1) {                                            // the element-wise warps' two barriers, below
+            cluster_sync();
+            cluster_sync();
+        }
     } else {
         take_registers<kWorkRegisters>();
-        const int part = warp >> 2;                                   // rows [64 part, 64 part + 64) of every row tile
+        const int part = warp >> 2;                                   // rows [32 part, 32 part + 32) of every row tile
         const int key = k0 + (threadIdx.x & 127);
         const uint32_t my_lane = static_cast<uint32_t>(warp & 3) << 21;
-        const uint32_t s_at = tm_s + 64 * part + my_lane, dp_at = tm_dp + 64 * part + my_lane;
+        if (n > 0) {                                                  // the K tile to tensor memory: a quarter of a row for each thread
+            uint32_t x[DIM / 8];
+            const T *src = static_cast<const T *>(p.kin.p) + (key < w.k_len ? row_of(w, p.kin, w.head, key, w.k_first) : 0);
+#pragma unroll
+            for (int c = 0; c < DIM / 4; c += 8) {
+                const int col = part * (DIM / 4) + c;
+                const uint4 v = key < w.k_len && col < p.dim ? *reinterpret_cast<const uint4 *>(src + col) : make_uint4(0, 0, 0, 0);
+                x[c / 2] = v.x; x[c / 2 + 1] = v.y; x[c / 2 + 2] = v.z; x[c / 2 + 3] = v.w;
+            }
+            if constexpr (DIM == 128) tmem_st16(tm_k + 16 * part + my_lane, x);
+            else tmem_st8(tm_k + 8 * part + my_lane, x);
+            wait_st();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) barrier_arrive(bar(kK));
+        }
         for (int j = 0; j < n; ++j) {
             const int q0 = (first + (rank + j * p.split) % each) * kTile;
             ok = wait(kTFull + (j & 1), (j >> 1) & 1) && wait(kS, j & 1);
             if (!ok) break;
             fence_after();
-            const float4 *l4 = reinterpret_cast<const float4 *>(stat + (j & 1) * 2 * kTile + 64 * part);
+            const float4 *l4 = reinterpret_cast<const float4 *>(stat + (j & 1) * 2 * kTile + 32 * part);
             const float4 *d4 = l4 + kTile / 4;
-            uint32_t s[64], d[64], out[32];
-            float prob[64];
-            tmem_ld32(s_at, s);
-            tmem_ld32(s_at + 32, s + 32);
+            uint32_t s[32], out[16];
+            float prob[32];
+            tmem_ld32(tm_s + 32 * part + my_lane, s);
             wait_ld();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) barrier_arrive(bar(kSRead));
             // rows past the end and rows that see nothing have -lse = -inf: their probabilities are 0
             if (p.causal && k0 + kTile - 1 > q0 + reach) {            // some rows do not see this thread's key
-                const int from = key - reach - q0 - 64 * part;
+                const int from = key - reach - q0 - 32 * part;
 #pragma unroll
-                for (int c = 0; c < 16; ++c) {
+                for (int c = 0; c < 8; ++c) {
                     const float4 l = l4[c];
                     exp2_scaled<false>(prob[4 * c], prob[4 * c + 1], __uint_as_float(s[4 * c]), __uint_as_float(s[4 * c + 1]), p.scale_log2, l.x, l.y);
                     exp2_scaled<false>(prob[4 * c + 2], prob[4 * c + 3], __uint_as_float(s[4 * c + 2]), __uint_as_float(s[4 * c + 3]), p.scale_log2, l.z, l.w);
                 }
 #pragma unroll
-                for (int c = 0; c < 64; ++c) prob[c] = c >= from ? prob[c] : 0.0f;
+                for (int c = 0; c < 32; ++c) prob[c] = c >= from ? prob[c] : 0.0f;
             } else {
 #pragma unroll
-                for (int c = 0; c < 16; ++c) {
+                for (int c = 0; c < 8; ++c) {
                     const float4 l = l4[c];
                     exp2_scaled<false>(prob[4 * c], prob[4 * c + 1], __uint_as_float(s[4 * c]), __uint_as_float(s[4 * c + 1]), p.scale_log2, l.x, l.y);
                     if (c & 1) exp2_scaled<true>(prob[4 * c + 2], prob[4 * c + 3], __uint_as_float(s[4 * c + 2]), __uint_as_float(s[4 * c + 3]), p.scale_log2, l.z, l.w);
@@ -793,30 +844,32 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                 }
             }
 #pragma unroll
-            for (int c = 0; c < 32; ++c) out[c] = pack2<T>(prob[2 * c], prob[2 * c + 1]);
-            tmem_st32(s_at, out);
+            for (int c = 0; c < 16; ++c) out[c] = pack2<T>(prob[2 * c], prob[2 * c + 1]);
+            ok = (j == 0 || wait(kDsUsed, (j - 1) & 1)) && wait(kDp, j & 1);
+            if (!ok) break;
+            fence_after();
+            tmem_st16(tm_p + 16 * part + my_lane, out);
+            tmem_ld32(tm_dp + 32 * part + my_lane, s);
+            wait_ld();
             wait_st();
             fence_before();
             __syncwarp();
             if (lane == 0) barrier_arrive(bar(kP));
-            ok = wait(kDp, j & 1);
-            if (!ok) break;
-            fence_after();
-            tmem_ld32(dp_at, d);
-            tmem_ld32(dp_at + 32, d + 32);
-            wait_ld();
 #pragma unroll
-            for (int c = 0; c < 16; ++c) {
+            for (int c = 0; c < 8; ++c) {
                 const float4 e = d4[c];
                 float v0, v1, v2, v3;
-                add2(v0, v1, __uint_as_float(d[4 * c]), __uint_as_float(d[4 * c + 1]), e.x, e.y);
-                add2(v2, v3, __uint_as_float(d[4 * c + 2]), __uint_as_float(d[4 * c + 3]), e.z, e.w);
+                add2(v0, v1, __uint_as_float(s[4 * c]), __uint_as_float(s[4 * c + 1]), e.x, e.y);
+                add2(v2, v3, __uint_as_float(s[4 * c + 2]), __uint_as_float(s[4 * c + 3]), e.z, e.w);
                 mul2(v0, v1, v0, v1, prob[4 * c], prob[4 * c + 1]);
                 mul2(v2, v3, v2, v3, prob[4 * c + 2], prob[4 * c + 3]);
                 out[2 * c] = pack2<T>(v0, v1);
                 out[2 * c + 1] = pack2<T>(v2, v3);
             }
-            tmem_st32(dp_at, out);
+            ok = wait(kPUsed, j & 1);
+            if (!ok) break;
+            fence_after();
+            tmem_st16(tm_ds + 16 * part + my_lane, out);
             wait_st();
             fence_before();
             __syncwarp();
@@ -827,64 +880,62 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
         }
         if (ok) ok = wait(kDone, 0);
         fence_after();
-    }
-    // dV by the first four warps, dK by the next
-    const int part = (warp >> 2) & 1, r = threadIdx.x & 127, key = k0 + r;
-    const bool works = warp < kMmaWarp, live = works && key < w.k_len;
-    const Rows &to = part == 0 ? p.dv : p.dk;
-    const float factor = part == 0 ? 1.0f : p.scale;
-    const uint32_t from = (part == 0 ? tm_dv : tm_dk) + (static_cast<uint32_t>(warp & 3) << 21);
-    T *row = static_cast<T *>(to.p) + (live ? row_of(w, to, w.head, key, w.k_first) : 0);
-    if (p.split == 1) {
-        if (works && ok) {
-            if (n > 0) {
-#pragma unroll
-                for (int c = 0; c < DIM / 32; ++c) {
-                    uint32_t o[32];
-                    tmem_ld32(from + 32 * c, o);
-                    wait_ld();
-                    if (live) store_columns<T>(row, 32 * c, p.dim, o, factor);
-                }
-            } else if (live) {
-                zero_columns<T>(row, p.dim);
-            }
-        }
-    } else {
-        // Each CTA lays its sums out in its own shared memory, [dV or dK][column][key] (the tiles are no longer needed), and
-        // adds up a share of the columns over the cluster, in the order of the ranks.
-        const uint32_t mine = base + static_cast<uint32_t>(part * DIM) * (kTile * 4) + r * 4;
-        if (works) {
-#pragma unroll
-            for (int c = 0; c < DIM / 32; ++c) {
-                uint32_t o[32];
+        // dV by every other four warps, dK by the rest; the first eight warps take the first half of the columns
+        const int which = part & 1, half = part >> 1, r = threadIdx.x & 127;
+        const bool live = key < w.k_len;
+        const Rows &to = which == 0 ? p.dv : p.dk;
+        const float factor = which == 0 ? 1.0f : p.scale;
+        const uint32_t from = (which == 0 ? tm_dv : tm_dk) + my_lane;
+        T *row = static_cast<T *>(to.p) + (live ? row_of(w, to, w.head, key, w.k_first) : 0);
+        if (p.split == 1) {
+            if (ok) {
                 if (n > 0) {
-                    tmem_ld32(from + 32 * c, o);
-                    wait_ld();
+#pragma unroll
+                    for (int c = 0; c < DIM / 64; ++c) {
+                        uint32_t o[32];
+                        const int col = half * (DIM / 2) + 32 * c;
+                        tmem_ld32(from + col, o);
+                        wait_ld();
+                        if (live) store_columns<T, 32>(row, col, p.dim, o, factor);
+                    }
+                } else if (live && half == 0) {
+                    zero_columns<T>(row, p.dim);
                 }
+            }
+        } else {
+            // Each CTA lays its sums out in its own shared memory, [dV or dK][column][key] (the tiles are no longer needed), and
+            // adds up a share of the columns over the cluster, in the order of the ranks.
+            const uint32_t mine = base + static_cast<uint32_t>(which * DIM) * (kTile * 4) + r * 4;
+#pragma unroll
+            for (int c = 0; c < DIM / 64; ++c) {
+                uint32_t o[32];
+                const int col = half * (DIM / 2) + 32 * c;
+                tmem_ld32(from + col, o);                             // (what it holds does not matter where there was no row tile)
+                wait_ld();
 #pragma unroll
                 for (int e = 0; e < 32; ++e)
-                    asm volatile("st.shared.u32 [%0], %1;" :: "r"(mine + (32 * c + e) * (kTile * 4)), "r"(n > 0 ? o[e] : 0u) : "memory");
+                    asm volatile("st.shared.u32 [%0], %1;" :: "r"(mine + (col + e) * (kTile * 4)), "r"(n > 0 ? o[e] : 0u) : "memory");
             }
-        }
-        cluster_sync();
-        if (live) {
-            const int share = DIM / p.split;                          // a multiple of 16
-            for (int c = rank * share; c < (rank + 1) * share && c < p.dim; c += 8) {
-                float v[8];
+            cluster_sync();
+            if (live) {
+                const int share = DIM / p.split;                          // a multiple of 16
+                for (int c = rank * share + half * (share / 2); c < rank * share + (half + 1) * (share / 2) && c < p.dim; c += 8) {
+                    float v[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = load_peer(mine + (c + e) * (kTile * 4), 0);
-                for (int k = 1; k < p.split; ++k)
+                    for (int e = 0; e < 8; ++e) v[e] = load_peer(mine + (c + e) * (kTile * 4), 0);
+                    for (int k = 1; k < p.split; ++k)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] += load_peer(mine + (c + e) * (kTile * 4), k);
-                uint4 x;
-                x.x = pack2<T>(v[0] * factor, v[1] * factor);
-                x.y = pack2<T>(v[2] * factor, v[3] * factor);
-                x.z = pack2<T>(v[4] * factor, v[5] * factor);
-                x.w = pack2<T>(v[6] * factor, v[7] * factor);
-                *reinterpret_cast<uint4 *>(row + c) = x;
+                        for (int e = 0; e < 8; ++e) v[e] += load_peer(mine + (c + e) * (kTile * 4), k);
+                    uint4 x;
+                    x.x = pack2<T>(v[0] * factor, v[1] * factor);
+                    x.y = pack2<T>(v[2] * factor, v[3] * factor);
+                    x.z = pack2<T>(v[4] * factor, v[5] * factor);
+                    x.w = pack2<T>(v[6] * factor, v[7] * factor);
+                    *reinterpret_cast<uint4 *>(row + c) = x;
+                }
             }
+            cluster_sync();                                               // nobody's shared memory goes before it has been read
         }
-        cluster_sync();                                               // nobody's shared memory goes before it has been read
     }
     end_cta(tmem);
 }

@@ -90,7 +90,8 @@ __device__ __forceinline__ float load_peer(uint32_t address, uint32_t rank) {
     return v;
 }
 
-// ---- registers: a warpgroup hands some to the others (the sums stay within what the CTA was launched with)
+// ---- registers: a warpgroup hands some to the others (the sums stay within what the CTA was launched with).  Code behind
+// the roles' branches runs with the smaller number: it must be next to nothing.
 template <int N> __device__ __forceinline__ void give_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" :: "n"(N)); }
 template <int N> __device__ __forceinline__ void take_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" :: "n"(N)); }
 
@@ -117,6 +118,12 @@ __device__ __forceinline__ void tmem_ld32(uint32_t at, uint32_t *r) {
                    "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
                  : "r"(at) : "memory");
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t at, uint32_t *r) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(at) : "memory");
+}
 __device__ __forceinline__ void tmem_st32(uint32_t at, const uint32_t *r) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
                  "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
@@ -131,6 +138,11 @@ __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t *r) {
                  :: "r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
                     "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
                  : "memory");
+}
+
+__device__ __forceinline__ void tmem_st8(uint32_t at, const uint32_t *r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 :: "r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
 
 // ---- tcgen05.mma ----------------------------------------------------------------------------------
@@ -188,15 +200,25 @@ __device__ __forceinline__ void product_rows(uint32_t leader, uint32_t d, uint32
         mma_ss(leader, d, da + off, db + off, idesc, k > 0);
     }
 }
-// D (128 x DIM) (+)= A B over steps [FIRST, LAST) of 16: A (128 x 128, 16 bits) in tensor memory, 16 columns of its
-// contraction in 8 TMEM columns, the second 64 of them at `a2`; B's rows are the contraction
-template <typename T, int DIM, int FIRST = 0, int LAST = 8>
-__device__ __forceinline__ void product_columns(uint32_t leader, uint32_t d, uint32_t a, uint32_t a2, uint32_t b, bool accumulate) {
+// The same with A (16 bits) in tensor memory: a step of 16 takes 8 TMEM columns.  An MMA from tensor memory reads half the
+// shared memory of one whose operands both lie there, which takes all of the 128 bytes that a clock has.
+template <typename T, int DIM>
+__device__ __forceinline__ void product_rows_tmem(uint32_t leader, uint32_t d, uint32_t a, uint32_t b) {
+    constexpr uint32_t idesc = instruction<T>(128, false);
+    const uint64_t db = k_major(b);
+#pragma unroll
+    for (int k = 0; k < DIM / 16; ++k) mma_ts(leader, d, a + 8 * k, db + (((k / 4) * kHalfTile + (k % 4) * 32) >> 4), idesc, k > 0);
+}
+// D (128 x DIM) (+)= A B: A (128 x 128, 16 bits) in tensor memory, B's rows are the contraction.  Its 8 steps of 16 take 8
+// TMEM columns of A each, GROUP steps side by side and each group PITCH columns after the one before (the element-wise
+// threads write where they have read).  STEPS: a bit for each step to do; the first one of an accumulation is bit 0.
+template <typename T, int DIM, int GROUP, int PITCH, int STEPS = 0xff>
+__device__ __forceinline__ void product_columns(uint32_t leader, uint32_t d, uint32_t a, uint32_t b, bool accumulate) {
     constexpr uint32_t idesc = instruction<T>(DIM, true);
     const uint64_t db = mn_major(b);
 #pragma unroll
-    for (int k = FIRST; k < LAST; ++k)
-        mma_ts(leader, d, k < 4 ? a + 8 * k : a2 + 8 * (k - 4), db + k * (2048 >> 4), idesc, accumulate || k > FIRST);
+    for (int k = 0; k < 8; ++k)
+        if (STEPS >> k & 1) mma_ts(leader, d, a + (k / GROUP) * PITCH + (k % GROUP) * 8, db + k * (2048 >> 4), idesc, accumulate || k > 0);
 }
 
 template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
