@@ -23,6 +23,7 @@
 
 #include <climits>
 #include <cmath>
+#include <type_traits>
 
 #include "fewbit_device.cuh"
 #include "fewbit_tensor_core.cuh"
@@ -210,11 +211,11 @@ enum { fQ = 0, fKFull = 2, fKEmpty = 4, fVFull = 6, fVEmpty = 8, fS = 10, fP = 1
 
 template <int DIM> constexpr int fwd_smem() { return 6 * (DIM / 64) * static_cast<int>(kHalfTile) + 1024 + static_cast<int>(sizeof(Sync)) + 4 * kTile * 4; }
 
-// Barriers of the 256 threads of one row tile.
-__device__ __forceinline__ void tile_barrier(int id) { asm volatile("bar.sync %0, 256;" :: "r"(id) : "memory"); }
-__device__ __forceinline__ bool tile_any(int id, bool x) {
+// Barriers of two warps.
+__device__ __forceinline__ void pair_barrier(int id) { asm volatile("bar.sync %0, 64;" :: "r"(id) : "memory"); }
+__device__ __forceinline__ bool pair_any(int id, bool x) {
     uint32_t any;
-    asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %1, 0;\nbarrier.cta.red.or.pred q, %2, 256, p;\nselp.u32 %0, 1, 0, q;\n}"
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %1, 0;\nbarrier.cta.red.or.pred q, %2, 64, p;\nselp.u32 %0, 1, 0, q;\n}"
                  : "=r"(any) : "r"(static_cast<uint32_t>(x)), "r"(id) : "memory");
     return any != 0;
 }
@@ -263,7 +264,7 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
     auto bar = [&](int i) { return smem_address(&sync->bar[i]); };
     auto wait = [&](int i, uint32_t parity) { return barrier_wait(bar(i), parity, &sync->stop, p.timeouts); };
     const uint32_t sm_q = base, sm_k = base + 2 * kBytes, sm_v = base + 4 * kBytes;
-    // tensor memory: S of both row tiles (each half of P in the first half of the scores that it came from), then O of both
+    // tensor memory: S of both row tiles (each 32 columns of P in the first half of the scores that they came from), then O of both
     const uint32_t tm_s = tmem, tm_o = tmem + 2 * kTile;
 
     if (warp >= kMmaWarp) {
@@ -330,11 +331,11 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
                     ok = wait(fP + t, j & 1);
                     if (!ok) break;
                     fence_after();
-                    product_columns<T, DIM, 4, 64, 0x33>(leader, tm_o + t * kTile, at, sm_v + (j & 1) * kBytes, j > 0);
+                    product_columns<T, DIM, 2, 32, 0xcc>(leader, tm_o + t * kTile, at, sm_v + (j & 1) * kBytes, j > 0);
                     ok = wait(fPEnd + t, j & 1);
                     if (!ok) break;
                     fence_after();
-                    product_columns<T, DIM, 4, 64, 0xcc>(leader, tm_o + t * kTile, at, sm_v + (j & 1) * kBytes, true);
+                    product_columns<T, DIM, 2, 32, 0x33>(leader, tm_o + t * kTile, at, sm_v + (j & 1) * kBytes, true);
                     commit(leader, bar(fO + t));
                     if (j + 1 < nt) scores(t, j + 1);
                 }
@@ -351,6 +352,7 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
         const int i = q0 + t * kTile + r;                             // this thread's row
         const uint32_t my_lane = static_cast<uint32_t>(warp & 3) << 21;
         const uint32_t s_at = tm_s + t * kTile + 64 * half + my_lane, o_at = tm_o + t * kTile + half * (DIM / 2) + my_lane;
+        const int pair = 1 + 4 * t + (warp & 3);                      // barrier of the two warps that share their rows
         float *mine = exchange + (2 * t + half) * kTile + r, *other = exchange + (2 * t + 1 - half) * kTile + r;
         // the row sees keys [0, seen)
         const int seen = p.causal ? min(w.k_len, i + 1 + w.k_len - w.q_len) : w.k_len;
@@ -360,32 +362,41 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
         for (int j = 0; j < nt; ++j) {
             ok = wait(fS + t, j & 1);                                 // (a wait given up ends the loop below, for all threads of the tile)
             fence_after();
-            uint32_t s[64];
-            tmem_ld32(s_at, s);
-            tmem_ld32(s_at + 32, s + 32);
-            wait_ld();
             const bool edge = (j + 1) * kTile > tile_seen;
-            if (edge) {
-                const int limit = seen - j * kTile - 64 * half;
+            const int limit = seen - j * kTile - 64 * half;
+            // Scores are read twice, 32 columns at a time, for the maximum and for the probabilities: reading them costs less
+            // than holding 64 of them in registers.
+            uint32_t s[32];
+            auto read = [&](int c) {
+                tmem_ld32(s_at + 32 * c, s);
+                wait_ld();
+                if (edge) {
 #pragma unroll
-                for (int c = 0; c < 64; ++c) s[c] = c < limit ? s[c] : 0xff800000u;
-            }
+                    for (int e = 0; e < 32; ++e) s[e] = 32 * c + e < limit ? s[e] : 0xff800000u;
+                }
+            };
             float best[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            auto maximum = [&]() {
 #pragma unroll
-            for (int c = 0; c < 64; c += 2)                           // two at a time: a three-operand maximum
-                best[(c >> 1) & 3] = fmaxf(best[(c >> 1) & 3], fmaxf(__uint_as_float(s[c]), __uint_as_float(s[c + 1])));
+                for (int e = 0; e < 32; e += 2)                       // two at a time: a three-operand maximum
+                    best[(e >> 1) & 3] = fmaxf(best[(e >> 1) & 3], fmaxf(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
+            };
+            read(0);
+            maximum();
+            read(1);
+            maximum();
             const float high = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3]));
             // The sums' reference moves only when a product passes it by 2^8: until then probabilities up to 2^8
             // are held, which cost no precision, and O needs no rescaling.  The row's two threads move it together: whether
-            // any row of the tile's 256 threads moves is one barrier, and only then they exchange their maxima.
+            // any row of their two warps moves is one barrier, and only then they exchange their maxima.
             const bool above = high > top && (high - top) * p.scale_log2 > 8.0f;
-            if (tile_any(1 + t, above || !ok)) {
-                if (tile_any(1 + t, !ok)) {
+            if (pair_any(pair, above || !ok)) {
+                if (pair_any(pair, !ok)) {
                     ok = false;
                     break;
                 }
                 *mine = high;
-                tile_barrier(1 + t);
+                pair_barrier(pair);
                 const float row_high = fmaxf(high, *other);
                 const bool move = row_high > top && (row_high - top) * p.scale_log2 > 8.0f;
                 const float next = move ? row_high : top;
@@ -394,7 +405,7 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
                 sum *= factor;
                 if (j > 0) {
                     ok = wait(fO + t, (j - 1) & 1);
-                    if (tile_any(1 + t, !ok)) {
+                    if (pair_any(pair, !ok)) {
                         ok = false;
                         break;
                     }
@@ -413,20 +424,21 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
             const float shift = top == -INFINITY ? 0.0f : -top * p.scale_log2;
             float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                if (edge) fwd_probabilities<T, false>(s + 32 * c, p.scale_log2, shift, part, s_at + 16 * c);
-                else fwd_probabilities<T, true>(s + 32 * c, p.scale_log2, shift, part, s_at + 16 * c);
+            for (int c = 1; c >= 0; --c) {                            // (columns 32 to 63 are still there)
+                if (c == 0) read(0);
+                if (edge) fwd_probabilities<T, false>(s, p.scale_log2, shift, part, s_at + 32 * c);
+                else fwd_probabilities<T, true>(s, p.scale_log2, shift, part, s_at + 32 * c);
                 wait_st();
                 fence_before();
                 __syncwarp();
-                if (lane == 0) barrier_arrive(bar((c == 0 ? fP : fPEnd) + t));
+                if (lane == 0) barrier_arrive(bar((c == 1 ? fP : fPEnd) + t));
             }
             sum += (part[0] + part[1]) + (part[2] + part[3]);
         }
         if (nt > 0 && ok) ok = wait(fO + t, (nt - 1) & 1);
         fence_after();
         *mine = sum;                                                  // (the last exchange of maxima was read before P was ready)
-        tile_barrier(1 + t);
+        pair_barrier(pair);
         sum += *other;
         if (ok) {
             const bool live = i < w.q_len;
@@ -456,7 +468,7 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
 // dP full, dS ready, dQ done.
 enum { qQ = 0, qKFull = 1, qKEmpty = 4, qVFull = 7, qVEmpty = 9, qS = 11, qDp = 13, qDs = 14, qDone = 15, qBars = 16 };
 
-template <int DIM> constexpr int dq_smem() { return 7 * (DIM / 64) * static_cast<int>(kHalfTile) + static_cast<int>(sizeof(Sync)) + 4 * kTile * 4; }
+template <int DIM> constexpr int dq_smem() { return 7 * (DIM / 64) * static_cast<int>(kHalfTile) + static_cast<int>(sizeof(Sync)) + kTile * 4; }
 
 template <typename T, int DIM>
 __global__ void __launch_bounds__(kThreadsAttn, 1)
@@ -466,7 +478,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
     extern __shared__ __align__(1024) uint8_t raw[];
     const uint32_t base = smem_address(raw);                          // no room to align it here: the host checks
     Sync *sync = reinterpret_cast<Sync *>(raw + 7 * kBytes);
-    float *part_delta = reinterpret_cast<float *>(sync + 1);          // [4][128]
+    float *row_delta = reinterpret_cast<float *>(sync + 1);           // [128]
     const int warp = uniform(static_cast<int>(threadIdx.x >> 5)), lane = threadIdx.x & 31;
     pdl_wait();
     const Work w = find_work(p, blockIdx.x, p.heads, true);
@@ -559,23 +571,38 @@ attention_dq_kernel(const __grid_constant__ Params p) {
         const int r = threadIdx.x & 127, i = q0 + r;
         const bool live = i < w.q_len;
         const uint32_t my_lane = static_cast<uint32_t>(warp & 3) << 21;
-        float delta = 0.0f, minus_lse = -INFINITY;                    // a row that sees nothing: every probability is 0
-        if (live) {
-            const T *o = static_cast<const T *>(p.o.p) + row_of(w, p.o, w.head, i, w.q_first);
-            const T *g = static_cast<const T *>(p.go.p) + row_of(w, p.go, w.head, i, w.q_first);
-            for (int c = 8 * part; c < p.dim; c += 32) {
-                float a[8], b[8];
-                load8(o + c, a);
-                load8(g + c, b);
+        // delta: DIM / 8 lanes read a row's outputs and gradients, 8 rows for each warp, all of them in flight at once
+        {
+            constexpr int kLanes = DIM / 8, kRows = 32 / kLanes;
+            float o[8 / kRows][8], g[8 / kRows][8];
+            const int col = lane % kLanes * 8;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) delta = fmaf(a[e], b[e], delta);
+            for (int x = 0; x < 8 / kRows; ++x) {
+                const int row = q0 + 8 * warp + kRows * x + lane / kLanes;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[x][e] = g[x][e] = 0.0f;
+                if (row < w.q_len && col < p.dim) {
+                    load8(static_cast<const T *>(p.o.p) + row_of(w, p.o, w.head, row, w.q_first) + col, o[x]);
+                    load8(static_cast<const T *>(p.go.p) + row_of(w, p.go, w.head, row, w.q_first) + col, g[x]);
+                }
             }
+#pragma unroll
+            for (int x = 0; x < 8 / kRows; ++x) {
+                float sum = 0.0f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum = fmaf(o[x][e], g[x][e], sum);
+#pragma unroll
+                for (int m = kLanes / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+                if (lane % kLanes == 0) row_delta[8 * warp + kRows * x + lane / kLanes] = sum;
+            }
+        }
+        float minus_lse = -INFINITY;                                  // a row that sees nothing: every probability is 0
+        if (live) {
             const float l = p.lse[stat_of(p, w, w.head, i)];
             if (l != -INFINITY) minus_lse = -l * kLog2e;
         }
-        part_delta[part * kTile + r] = delta;
         asm volatile("bar.sync 1, %0;" :: "n"(kWorkThreads) : "memory");   // the element-wise warps only
-        const float minus_delta = -((part_delta[r] + part_delta[kTile + r]) + (part_delta[2 * kTile + r] + part_delta[3 * kTile + r]));
+        const float minus_delta = -row_delta[r];
         if (part < 2) stat_block(p, w, w.head, w.tile)[part * kTile + r] = part == 0 ? minus_lse : minus_delta;
         const int seen = p.causal ? min(w.k_len, i + 1 + w.k_len - w.q_len) : w.k_len;
         const int tile_seen = p.causal ? min(w.k_len, q0 + 1 + w.k_len - w.q_len) : w.k_len;
@@ -791,15 +818,16 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
     } else {
         take_registers<kWorkRegisters>();
         const int part = warp >> 2;                                   // rows [32 part, 32 part + 32) of every row tile
-        const int key = k0 + (threadIdx.x & 127);
+        const int row_key = k0 + (threadIdx.x & 127);                 // this thread's row of K, dV and dK
+        const int key = k0 + 32 * (warp & 3) + lane / 4;              // the first of its 4 keys, 8 apart, in S and dP
         const uint32_t my_lane = static_cast<uint32_t>(warp & 3) << 21;
         if (n > 0) {                                                  // the K tile to tensor memory: a quarter of a row for each thread
             uint32_t x[DIM / 8];
-            const T *src = static_cast<const T *>(p.kin.p) + (key < w.k_len ? row_of(w, p.kin, w.head, key, w.k_first) : 0);
+            const T *src = static_cast<const T *>(p.kin.p) + (row_key < w.k_len ? row_of(w, p.kin, w.head, row_key, w.k_first) : 0);
 #pragma unroll
             for (int c = 0; c < DIM / 4; c += 8) {
                 const int col = part * (DIM / 4) + c;
-                const uint4 v = key < w.k_len && col < p.dim ? *reinterpret_cast<const uint4 *>(src + col) : make_uint4(0, 0, 0, 0);
+                const uint4 v = row_key < w.k_len && col < p.dim ? *reinterpret_cast<const uint4 *>(src + col) : make_uint4(0, 0, 0, 0);
                 x[c / 2] = v.x; x[c / 2 + 1] = v.y; x[c / 2 + 2] = v.z; x[c / 2 + 3] = v.w;
             }
             if constexpr (DIM == 128) tmem_st16(tm_k + 16 * part + my_lane, x);
@@ -814,33 +842,42 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             ok = wait(kTFull + (j & 1), (j >> 1) & 1) && wait(kS, j & 1);
             if (!ok) break;
             fence_after();
-            const float4 *l4 = reinterpret_cast<const float4 *>(stat + (j & 1) * 2 * kTile + 32 * part);
-            const float4 *d4 = l4 + kTile / 4;
+            // A thread holds 8 rows' values for each of 4 keys, not 32 rows' for one: the statistics that it reads are a quarter
+            // (reads of shared memory are what the tensor cores' operands compete with).
+            const float2 *l2 = reinterpret_cast<const float2 *>(stat + (j & 1) * 2 * kTile + 32 * part) + lane % 4;
+            const float2 *d2 = l2 + kTile / 2;
             uint32_t s[32], out[16];
             float prob[32];
-            tmem_ld32(tm_s + 32 * part + my_lane, s);
+            tmem_ld_16x32(tm_s + 32 * part + my_lane, s);
+            tmem_ld_16x32(tm_s + 32 * part + my_lane + (16u << 16), s + 16);
             wait_ld();
             fence_before();
             __syncwarp();
             if (lane == 0) barrier_arrive(bar(kSRead));
             // rows past the end and rows that see nothing have -lse = -inf: their probabilities are 0
-            if (p.causal && k0 + kTile - 1 > q0 + reach) {            // some rows do not see this thread's key
-                const int from = key - reach - q0 - 32 * part;
+            if (p.causal && k0 + kTile - 1 > q0 + reach) {            // some rows do not see some keys
+                const int from = key - reach - q0 - 32 * part - 2 * (lane % 4);   // of the first of the 4 keys, which are 8 apart
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    const float4 l = l4[c];
-                    exp2_scaled<false>(prob[4 * c], prob[4 * c + 1], __uint_as_float(s[4 * c]), __uint_as_float(s[4 * c + 1]), p.scale_log2, l.x, l.y);
-                    exp2_scaled<false>(prob[4 * c + 2], prob[4 * c + 3], __uint_as_float(s[4 * c + 2]), __uint_as_float(s[4 * c + 3]), p.scale_log2, l.z, l.w);
+                for (int c = 0; c < 4; ++c) {
+                    const float2 l = l2[4 * c];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int x = 16 * (k / 2) + 4 * c + 2 * (k % 2);
+                        exp2_scaled<false>(prob[x], prob[x + 1], __uint_as_float(s[x]), __uint_as_float(s[x + 1]), p.scale_log2, l.x, l.y);
+                        prob[x] = 8 * c >= from + 8 * k ? prob[x] : 0.0f;
+                        prob[x + 1] = 8 * c + 1 >= from + 8 * k ? prob[x + 1] : 0.0f;
+                    }
                 }
-#pragma unroll
-                for (int c = 0; c < 32; ++c) prob[c] = c >= from ? prob[c] : 0.0f;
             } else {
 #pragma unroll
-                for (int c = 0; c < 8; ++c) {
-                    const float4 l = l4[c];
-                    exp2_scaled<false>(prob[4 * c], prob[4 * c + 1], __uint_as_float(s[4 * c]), __uint_as_float(s[4 * c + 1]), p.scale_log2, l.x, l.y);
-                    if (c & 1) exp2_scaled<true>(prob[4 * c + 2], prob[4 * c + 3], __uint_as_float(s[4 * c + 2]), __uint_as_float(s[4 * c + 3]), p.scale_log2, l.z, l.w);
-                    else exp2_scaled<false>(prob[4 * c + 2], prob[4 * c + 3], __uint_as_float(s[4 * c + 2]), __uint_as_float(s[4 * c + 3]), p.scale_log2, l.z, l.w);
+                for (int c = 0; c < 4; ++c) {
+                    const float2 l = l2[4 * c];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int x = 16 * (k / 2) + 4 * c + 2 * (k % 2);
+                        if (k == 3) exp2_scaled<true>(prob[x], prob[x + 1], __uint_as_float(s[x]), __uint_as_float(s[x + 1]), p.scale_log2, l.x, l.y);
+                        else exp2_scaled<false>(prob[x], prob[x + 1], __uint_as_float(s[x]), __uint_as_float(s[x + 1]), p.scale_log2, l.x, l.y);
+                    }
                 }
             }
 #pragma unroll
@@ -848,28 +885,32 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             ok = (j == 0 || wait(kDsUsed, (j - 1) & 1)) && wait(kDp, j & 1);
             if (!ok) break;
             fence_after();
-            tmem_st16(tm_p + 16 * part + my_lane, out);
-            tmem_ld32(tm_dp + 32 * part + my_lane, s);
+            tmem_st_16x16(tm_p + 16 * part + my_lane, out);
+            tmem_st_16x16(tm_p + 16 * part + my_lane + (16u << 16), out + 8);
+            tmem_ld_16x32(tm_dp + 32 * part + my_lane, s);
+            tmem_ld_16x32(tm_dp + 32 * part + my_lane + (16u << 16), s + 16);
             wait_ld();
             wait_st();
             fence_before();
             __syncwarp();
             if (lane == 0) barrier_arrive(bar(kP));
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {
-                const float4 e = d4[c];
-                float v0, v1, v2, v3;
-                add2(v0, v1, __uint_as_float(s[4 * c]), __uint_as_float(s[4 * c + 1]), e.x, e.y);
-                add2(v2, v3, __uint_as_float(s[4 * c + 2]), __uint_as_float(s[4 * c + 3]), e.z, e.w);
-                mul2(v0, v1, v0, v1, prob[4 * c], prob[4 * c + 1]);
-                mul2(v2, v3, v2, v3, prob[4 * c + 2], prob[4 * c + 3]);
-                out[2 * c] = pack2<T>(v0, v1);
-                out[2 * c + 1] = pack2<T>(v2, v3);
+            for (int c = 0; c < 4; ++c) {
+                const float2 e = d2[4 * c];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int x = 16 * (k / 2) + 4 * c + 2 * (k % 2);
+                    float v0, v1;
+                    add2(v0, v1, __uint_as_float(s[x]), __uint_as_float(s[x + 1]), e.x, e.y);
+                    mul2(v0, v1, v0, v1, prob[x], prob[x + 1]);
+                    out[x / 2] = pack2<T>(v0, v1);
+                }
             }
             ok = wait(kPUsed, j & 1);
             if (!ok) break;
             fence_after();
-            tmem_st16(tm_ds + 16 * part + my_lane, out);
+            tmem_st_16x16(tm_ds + 16 * part + my_lane, out);
+            tmem_st_16x16(tm_ds + 16 * part + my_lane + (16u << 16), out + 8);
             wait_st();
             fence_before();
             __syncwarp();
@@ -882,11 +923,11 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
         fence_after();
         // dV by every other four warps, dK by the rest; the first eight warps take the first half of the columns
         const int which = part & 1, half = part >> 1, r = threadIdx.x & 127;
-        const bool live = key < w.k_len;
+        const bool live = row_key < w.k_len;
         const Rows &to = which == 0 ? p.dv : p.dk;
         const float factor = which == 0 ? 1.0f : p.scale;
         const uint32_t from = (which == 0 ? tm_dv : tm_dk) + my_lane;
-        T *row = static_cast<T *>(to.p) + (live ? row_of(w, to, w.head, key, w.k_first) : 0);
+        T *row = static_cast<T *>(to.p) + (live ? row_of(w, to, w.head, row_key, w.k_first) : 0);
         if (p.split == 1) {
             if (ok) {
                 if (n > 0) {
@@ -903,13 +944,15 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                 }
             }
         } else {
-            // Each CTA lays its sums out in its own shared memory, [dV or dK][column][key] (the tiles are no longer needed), and
-            // adds up a share of the columns over the cluster, in the order of the ranks.
+            // Each CTA adds up a share of the columns over the cluster, and lays the others of its sums out in its own shared
+            // memory, [dV or dK][column][key] (the tiles are no longer needed), for their CTAs.
             const uint32_t mine = base + static_cast<uint32_t>(which * DIM) * (kTile * 4) + r * 4;
+            const int share = DIM / p.split;
 #pragma unroll
             for (int c = 0; c < DIM / 64; ++c) {
                 uint32_t o[32];
                 const int col = half * (DIM / 2) + 32 * c;
+                if (share >= 32 && col / share == rank) continue;
                 tmem_ld32(from + col, o);                             // (what it holds does not matter where there was no row tile)
                 wait_ld();
 #pragma unroll
@@ -917,24 +960,28 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                     asm volatile("st.shared.u32 [%0], %1;" :: "r"(mine + (col + e) * (kTile * 4)), "r"(n > 0 ? o[e] : 0u) : "memory");
             }
             cluster_sync();
-            if (live) {
-                const int share = DIM / p.split;                          // a multiple of 16
-                for (int c = rank * share + half * (share / 2); c < rank * share + (half + 1) * (share / 2) && c < p.dim; c += 8) {
-                    float v[8];
+            auto add_up = [&](auto columns) {                         // this thread's columns of the share: half of them
+                constexpr int N = decltype(columns)::value;
+                uint32_t o[N];
+                const int col = rank * share + half * N;
+                if constexpr (N == 32) tmem_ld32(from + col, o);
+                else if constexpr (N == 16) tmem_ld16(from + col, o);
+                else tmem_ld8(from + col, o);
+                wait_ld();
+                for (int k = 1; k < p.split; ++k) {
+                    const uint32_t peer = static_cast<uint32_t>((rank + k) % p.split);
+                    float v[N];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = load_peer(mine + (c + e) * (kTile * 4), 0);
-                    for (int k = 1; k < p.split; ++k)
+                    for (int e = 0; e < N; ++e) v[e] = load_peer(mine + (col + e) * (kTile * 4), peer);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] += load_peer(mine + (c + e) * (kTile * 4), k);
-                    uint4 x;
-                    x.x = pack2<T>(v[0] * factor, v[1] * factor);
-                    x.y = pack2<T>(v[2] * factor, v[3] * factor);
-                    x.z = pack2<T>(v[4] * factor, v[5] * factor);
-                    x.w = pack2<T>(v[6] * factor, v[7] * factor);
-                    *reinterpret_cast<uint4 *>(row + c) = x;
+                    for (int e = 0; e < N; ++e) o[e] = __float_as_uint((k == 1 && n == 0 ? 0.0f : __uint_as_float(o[e])) + v[e]);
                 }
-            }
-            cluster_sync();                                               // nobody's shared memory goes before it has been read
+                if (live) store_columns<T, N>(row, col, p.dim, o, factor);
+            };
+            if (share / 2 == 32) add_up(std::integral_constant<int, 32>{});
+            else if (share / 2 == 16) add_up(std::integral_constant<int, 16>{});
+            else add_up(std::integral_constant<int, 8>{});
+            cluster_sync();                                           // nobody's shared memory goes before it has been read
         }
     }
     end_cta(tmem);

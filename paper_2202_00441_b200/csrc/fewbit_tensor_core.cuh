@@ -140,6 +140,24 @@ __device__ __forceinline__ void tmem_st16(uint32_t at, const uint32_t *r) {
                  : "memory");
 }
 
+__device__ __forceinline__ void tmem_ld8(uint32_t at, uint32_t *r) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(at) : "memory");
+}
+// 16 lanes x 32 columns of 32 bits: in group g of 8 columns a thread gets columns 8g + 2 (lane % 4) and the next one of
+// lanes lane / 4 (r[4g], r[4g + 1]) and lane / 4 + 8 (r[4g + 2], r[4g + 3])
+__device__ __forceinline__ void tmem_ld_16x32(uint32_t at, uint32_t *r) {
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                 : "r"(at) : "memory");
+}
+// 16 lanes x 16 columns of 32 bits: in group g of 4 columns a thread gives column 4g + lane % 4 of lanes lane / 4 (r[2g]) and
+// lane / 4 + 8 (r[2g + 1]): where pairs of the values above, rounded to 16 bits, belong
+__device__ __forceinline__ void tmem_st_16x16(uint32_t at, const uint32_t *r) {
+    asm volatile("tcgen05.st.sync.aligned.16x128b.x4.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                 :: "r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
 __device__ __forceinline__ void tmem_st8(uint32_t at, const uint32_t *r) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
                  :: "r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
@@ -211,14 +229,15 @@ __device__ __forceinline__ void product_rows_tmem(uint32_t leader, uint32_t d, u
 }
 // D (128 x DIM) (+)= A B: A (128 x 128, 16 bits) in tensor memory, B's rows are the contraction.  Its 8 steps of 16 take 8
 // TMEM columns of A each, GROUP steps side by side and each group PITCH columns after the one before (the element-wise
-// threads write where they have read).  STEPS: a bit for each step to do; the first one of an accumulation is bit 0.
+// threads write where they have read).  STEPS: a bit for each step to do.
 template <typename T, int DIM, int GROUP, int PITCH, int STEPS = 0xff>
 __device__ __forceinline__ void product_columns(uint32_t leader, uint32_t d, uint32_t a, uint32_t b, bool accumulate) {
     constexpr uint32_t idesc = instruction<T>(DIM, true);
+    constexpr int kFirst = STEPS & 1 ? 0 : STEPS & 2 ? 1 : 2;
     const uint64_t db = mn_major(b);
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-        if (STEPS >> k & 1) mma_ts(leader, d, a + (k / GROUP) * PITCH + (k % GROUP) * 8, db + k * (2048 >> 4), idesc, accumulate || k > 0);
+        if (STEPS >> k & 1) mma_ts(leader, d, a + (k / GROUP) * PITCH + (k % GROUP) * 8, db + k * (2048 >> 4), idesc, accumulate || k > kFirst);
 }
 
 template <typename T> __device__ __forceinline__ uint32_t pack2(float lo, float hi);
