@@ -204,14 +204,25 @@ fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *s, const fewbit
     p.stat = static_cast<float *>(workspace);
     st = run(attn::Kernel::dq, s, p, (s->q_len + attn::kTile - 1) / attn::kTile, s->heads, stream);
     if (st != FEWBIT_OK) return st;
-    // A key tile's row tiles are dealt out to a cluster of up to 4 CTAs while the grid is under two CTAs for each SM: fewer
-    // leave SMs idle, or one long (causal) CTA alone at the end.
+    // A key tile's row tiles are dealt out to a cluster of 1, 2 or 4 CTAs, whichever should be done first: the longest CTA or
+    // the SMs' share of all work, counted in row tiles.  A CTA's start and end cost as much as 4 of them (11000 clocks against
+    // 2850), with a cluster's sums 7.  Causal sequences have half the work of full ones, and the same longest CTA.  Measured,
+    // backward pass in us with 1 / 2 CTAs: 4 x 2048 rows of 16 heads on 4 key heads, causal, 275 / 292 (4 CTAs: 330); one of 16384
+    // rows, 8 heads on 2: 1663 / 1608 (1695).
     cudaError_t err = cudaSuccess;
     const int64_t sms = device_sm_count(&err), key_tiles = (s->k_len + attn::kTile - 1) / attn::kTile;
     if (err != cudaSuccess) return cuda_status(err);
-    const int64_t iterations = (s->q_len + attn::kTile - 1) / attn::kTile * p.group;   // of one key tile, at most
-    p.split = 1;
-    while (p.split < 4 && key_tiles * s->kv_heads * s->batch * p.split < 2 * sms && iterations >= 4 * p.split) p.split *= 2;
+    const int64_t longest = (s->q_len + attn::kTile - 1) / attn::kTile * p.group, tiles = key_tiles * s->kv_heads * s->batch;
+    int64_t best = INT64_MAX;
+    for (int split = 1; split <= 4; split *= 2) {
+        const int64_t ends = split == 1 ? 4 : 7;
+        const int64_t alone = (longest + split - 1) / split + ends, shared = (tiles * longest / (p.causal ? 2 : 1) + tiles * split * ends) / sms;
+        const int64_t cost = alone > shared ? alone : shared;
+        if (cost < best) {
+            best = cost;
+            p.split = split;
+        }
+    }
     return run(attn::Kernel::dkv, s, p, key_tiles, s->kv_heads, stream);
 }
 

@@ -37,8 +37,9 @@ constexpr int kTile = 128;
 constexpr int kThreadsAttn = 640;      // five warpgroups: four element-wise ones, and the MMA and load warps (two idle ones fill it up)
 constexpr int kMmaWarp = 16, kLoadWarp = 17;
 constexpr int kWorkThreads = 512;
-// 96 registers a thread at launch: 512 x 104 + 128 x 64 = 61440 = 640 x 96
-constexpr int kWorkRegisters = 104, kIssueRegisters = 64;
+// Registers of the element-wise and the issuing threads.  96 a thread at launch: 512 x 104 + 128 x 64 = 512 x 112 + 128 x 32 =
+// 61440 = 640 x 96
+constexpr int kFwdWork = 112, kFwdIssue = 32, kDqWork = 104, kDqIssue = 64, kDkvWork = 112, kDkvIssue = 32;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kStatBytes = 2 * kTile * 4;   // a row tile's -lse * log2(e) and -delta
 
@@ -107,7 +108,7 @@ __device__ __forceinline__ int key_tiles(const Params &p, const Work &w, int las
 
 // Shared memory: tiles first (1 KB aligned), then the barriers.
 struct Sync {
-    unsigned long long bar[26];
+    unsigned long long bar[28];
     uint32_t tmem;
     int stop;
 };
@@ -268,7 +269,7 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
     const uint32_t tm_s = tmem, tm_o = tmem + 2 * kTile;
 
     if (warp >= kMmaWarp) {
-        give_registers<kIssueRegisters>();
+        give_registers<kFwdIssue>();
         if (warp == kLoadWarp) {
             int issued_k = 0, issued_v = 0;
             if (n > 0 && lane == 0) {
@@ -346,7 +347,7 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
             barrier_wait(bar(fDrain), 0, nullptr, p.timeouts);
         }
     } else {
-        take_registers<kWorkRegisters>();
+        take_registers<kFwdWork>();
         const int t = warp >> 3, half = (warp >> 2) & 1;              // row tile; columns [64 half, 64 half + 64) of every key tile
         const int nt = t ? n1 : n0, r = threadIdx.x & 127;
         const int i = q0 + t * kTile + r;                             // this thread's row
@@ -491,6 +492,23 @@ attention_dq_kernel(const __grid_constant__ Params p) {
     const int kv_head = w.head / p.group;
     const int n = uniform(key_tiles(p, w, min(q0 + kTile, w.q_len) - 1));
 
+    // The outputs that delta needs, read while the CTA sets itself up: DIM / 8 lanes a row, 8 rows for each warp.  (From here on
+    // the L2's bandwidth is the tiles' that are on their way.)
+    constexpr int kLanes = DIM / 8, kRows = 32 / kLanes;
+    uint4 outputs[8 / kRows];
+    float lse = -INFINITY;
+    if (warp < kMmaWarp) {
+#pragma unroll
+        for (int x = 0; x < 8 / kRows; ++x) {
+            const int row = q0 + 8 * warp + kRows * x + lane / kLanes, col = lane % kLanes * 8;
+            const bool there = row < w.q_len && col < p.dim;
+            const T *from = static_cast<const T *>(p.o.p) + row_of(w, p.o, w.head, there ? row : 0, w.q_first) + (there ? col : 0);
+            outputs[x] = there ? __ldg(reinterpret_cast<const uint4 *>(from)) : make_uint4(0, 0, 0, 0);
+        }
+        const int row = q0 + (threadIdx.x & 127);
+        if (row < w.q_len) lse = p.lse[stat_of(p, w, w.head, row)];
+    }
+
     constexpr uint32_t counts[qBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 16, 1};
     const uint32_t tmem = start_cta(sync, qBars, counts);
     auto bar = [&](int i) { return smem_address(&sync->bar[i]); };
@@ -500,7 +518,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
     const uint32_t tm_s = tmem, tm_dp = tmem + 2 * kTile, tm_dq = tmem + 3 * kTile;
 
     if (warp >= kMmaWarp) {
-        give_registers<kIssueRegisters>();
+        give_registers<kDqIssue>();
         if (warp == kLoadWarp) {
             int issued_k = 0, issued_v = 0;
             if (n > 0 && lane == 0) {
@@ -566,48 +584,35 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             barrier_wait(bar(qDone), 0, nullptr, p.timeouts);
         }
     } else {
-        take_registers<kWorkRegisters>();
+        take_registers<kDqWork>();
         const int part = warp >> 2;                                   // columns [32 part, 32 part + 32) of every tile
         const int r = threadIdx.x & 127, i = q0 + r;
         const bool live = i < w.q_len;
         const uint32_t my_lane = static_cast<uint32_t>(warp & 3) << 21;
-        // delta: DIM / 8 lanes read a row's outputs and gradients, 8 rows for each warp, all of them in flight at once
-        {
-            constexpr int kLanes = DIM / 8, kRows = 32 / kLanes;
-            float o[8 / kRows][8], g[8 / kRows][8];
-            const int col = lane % kLanes * 8;
+        const float minus_lse = lse == -INFINITY ? -INFINITY : -lse * kLog2e;   // a row that sees nothing: every probability is 0
+        bool ok = n == 0 || wait(qQ, 0);
 #pragma unroll
-            for (int x = 0; x < 8 / kRows; ++x) {
-                const int row = q0 + 8 * warp + kRows * x + lane / kLanes;
+        for (int x = 0; x < 8 / kRows; ++x) {
+            const int row = 8 * warp + kRows * x + lane / kLanes;
+            float sum = 0.0f;
+            if (n > 0 && q0 + row < w.q_len) {
+                const uint4 g = tile_chunk(sm_g, row, lane % kLanes);
+                T a[8], b[8];
+                memcpy(a, &outputs[x], 16);
+                memcpy(b, &g, 16);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) o[x][e] = g[x][e] = 0.0f;
-                if (row < w.q_len && col < p.dim) {
-                    load8(static_cast<const T *>(p.o.p) + row_of(w, p.o, w.head, row, w.q_first) + col, o[x]);
-                    load8(static_cast<const T *>(p.go.p) + row_of(w, p.go, w.head, row, w.q_first) + col, g[x]);
-                }
+                for (int e = 0; e < 8; ++e) sum = fmaf(load1(&a[e]), load1(&b[e]), sum);
             }
 #pragma unroll
-            for (int x = 0; x < 8 / kRows; ++x) {
-                float sum = 0.0f;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum = fmaf(o[x][e], g[x][e], sum);
-#pragma unroll
-                for (int m = kLanes / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
-                if (lane % kLanes == 0) row_delta[8 * warp + kRows * x + lane / kLanes] = sum;
-            }
-        }
-        float minus_lse = -INFINITY;                                  // a row that sees nothing: every probability is 0
-        if (live) {
-            const float l = p.lse[stat_of(p, w, w.head, i)];
-            if (l != -INFINITY) minus_lse = -l * kLog2e;
+            for (int m = kLanes / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
+            if (lane % kLanes == 0) row_delta[row] = sum;
         }
         asm volatile("bar.sync 1, %0;" :: "n"(kWorkThreads) : "memory");   // the element-wise warps only
         const float minus_delta = -row_delta[r];
         if (part < 2) stat_block(p, w, w.head, w.tile)[part * kTile + r] = part == 0 ? minus_lse : minus_delta;
         const int seen = p.causal ? min(w.k_len, i + 1 + w.k_len - w.q_len) : w.k_len;
         const int tile_seen = p.causal ? min(w.k_len, q0 + 1 + w.k_len - w.q_len) : w.k_len;
-        bool ok = true;
-        for (int j = 0; j < n; ++j) {
+        for (int j = 0; ok && j < n; ++j) {
             const uint32_t s_at = tm_s + (j & 1) * kTile + 32 * part + my_lane;
             ok = wait(qS + (j & 1), (j >> 1) & 1);
             if (!ok) break;
@@ -674,9 +679,9 @@ attention_dq_kernel(const __grid_constant__ Params p) {
 // backward, dK and dV
 // ---------------------------------------------------------------------------------------------------
 // Barriers: v, k in tensor memory, q full/empty (3 stages), g full/empty (3 stages), statistics full/empty (2 stages), S full
-// and read, dP full, P ready (and dP read) and used, dS ready and used, done.
-enum { kV = 0, kK = 1, kQFull = 2, kQEmpty = 5, kGFull = 8, kGEmpty = 11, kTFull = 14, kTEmpty = 16, kS = 18, kSRead = 19, kDp = 20, kP = 21, kPUsed = 22,
-       kDs = 23, kDsUsed = 24, kDone = 25, kBars = 26 };
+// and read, dP full and read, P ready and used, dS ready and used, done.
+enum { kV = 0, kK = 1, kQFull = 2, kQEmpty = 5, kGFull = 8, kGEmpty = 11, kTFull = 14, kTEmpty = 16, kS = 18, kSRead = 19, kDp = 20, kDpRead = 21, kP = 22,
+       kPUsed = 23, kDs = 24, kDsUsed = 25, kDone = 26, kBars = 27 };
 
 template <int DIM> constexpr int dkv_smem() { return 7 * (DIM / 64) * static_cast<int>(kHalfTile) + 2 * kStatBytes + static_cast<int>(sizeof(Sync)); }
 
@@ -709,7 +714,19 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
     const int each = max(0, (w.q_len + kTile - 1) / kTile - first);
     const int n = uniform((each * p.group - rank + p.split - 1) / p.split);
 
-    constexpr uint32_t counts[kBars] = {1, 16, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 16, 16, 1, 16, 1, 16, 1, 16, 1, 1};
+    // a quarter of a row of the K tile for each thread, read while the CTA sets itself up
+    uint32_t keys[DIM / 8];
+    if (warp < kMmaWarp && n > 0) {
+        const int i = k0 + (threadIdx.x & 127), first_col = (warp >> 2) * (DIM / 4);
+        const T *src = static_cast<const T *>(p.kin.p) + (i < w.k_len ? row_of(w, p.kin, w.head, i, w.k_first) : 0);
+#pragma unroll
+        for (int c = 0; c < DIM / 4; c += 8) {
+            const uint4 v = i < w.k_len && first_col + c < p.dim ? __ldg(reinterpret_cast<const uint4 *>(src + first_col + c)) : make_uint4(0, 0, 0, 0);
+            keys[c / 2] = v.x; keys[c / 2 + 1] = v.y; keys[c / 2 + 2] = v.z; keys[c / 2 + 3] = v.w;
+        }
+    }
+
+    constexpr uint32_t counts[kBars] = {1, 16, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 16, 16, 1, 16, 1, 16, 16, 1, 16, 1, 1};
     const uint32_t tmem = start_cta(sync, kBars, counts);
     auto bar = [&](int i) { return smem_address(&sync->bar[i]); };
     auto wait = [&](int i, uint32_t parity) { return barrier_wait(bar(i), parity, &sync->stop, p.timeouts); };
@@ -720,7 +737,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
 
     bool ok = true;
     if (warp >= kMmaWarp) {
-        give_registers<kIssueRegisters>();
+        give_registers<kDkvIssue>();
         if (warp == kLoadWarp) {
             int issued_q = 0, issued_t = 0, issued_g = 0;
             if (n > 0 && lane == 0) {
@@ -788,12 +805,15 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             fence_after();
             if (ok && n > 0) ok = dprobs(0);
             for (int j = 0; ok && j < n; ++j) {
-                ok = wait(kP, j & 1);                                 // P_j written, and dP_j in registers: S_j+1 may take its place
+                ok = wait(kP, j & 1);                                 // P_j written
                 if (!ok) break;
                 fence_after();
                 product_columns<T, DIM, 8, 64>(leader, tm_dv, tm_p, sm_g + (j % 3) * kBytes, j > 0);
                 commit(leader, bar(kPUsed));
                 commit(leader, bar(kGEmpty + j % 3));
+                ok = wait(kDpRead, j & 1);                            // dP_j is in registers: S_j+1 may take its place
+                if (!ok) break;
+                fence_after();
                 if (j + 1 < n && !(ok = scores(j + 1))) break;
                 ok = wait(kDs, j & 1);                                // dS_j written over P_j
                 if (!ok) break;
@@ -816,36 +836,34 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             cluster_sync();
         }
     } else {
-        take_registers<kWorkRegisters>();
+        take_registers<kDkvWork>();
         const int part = warp >> 2;                                   // rows [32 part, 32 part + 32) of every row tile
         const int row_key = k0 + (threadIdx.x & 127);                 // this thread's row of K, dV and dK
         const int key = k0 + 32 * (warp & 3) + lane / 4;              // the first of its 4 keys, 8 apart, in S and dP
         const uint32_t my_lane = static_cast<uint32_t>(warp & 3) << 21;
-        if (n > 0) {                                                  // the K tile to tensor memory: a quarter of a row for each thread
-            uint32_t x[DIM / 8];
-            const T *src = static_cast<const T *>(p.kin.p) + (row_key < w.k_len ? row_of(w, p.kin, w.head, row_key, w.k_first) : 0);
-#pragma unroll
-            for (int c = 0; c < DIM / 4; c += 8) {
-                const int col = part * (DIM / 4) + c;
-                const uint4 v = row_key < w.k_len && col < p.dim ? *reinterpret_cast<const uint4 *>(src + col) : make_uint4(0, 0, 0, 0);
-                x[c / 2] = v.x; x[c / 2 + 1] = v.y; x[c / 2 + 2] = v.z; x[c / 2 + 3] = v.w;
-            }
-            if constexpr (DIM == 128) tmem_st16(tm_k + 16 * part + my_lane, x);
-            else tmem_st8(tm_k + 8 * part + my_lane, x);
+        if (n > 0) {                                                  // the K tile to tensor memory
+            if constexpr (DIM == 128) tmem_st16(tm_k + 16 * part + my_lane, keys);
+            else tmem_st8(tm_k + 8 * part + my_lane, keys);
             wait_st();
             fence_before();
             __syncwarp();
             if (lane == 0) barrier_arrive(bar(kK));
         }
-        for (int j = 0; j < n; ++j) {
-            const int q0 = (first + (rank + j * p.split) % each) * kTile;
-            ok = wait(kTFull + (j & 1), (j >> 1) & 1) && wait(kS, j & 1);
-            if (!ok) break;
-            fence_after();
-            // A thread holds 8 rows' values for each of 4 keys, not 32 rows' for one: the statistics that it reads are a quarter
-            // (reads of shared memory are what the tensor cores' operands compete with).
+        int tile = rank;                                              // of this head, from `first` on
+        for (int j = 0; j < n; ++j, tile += p.split) {
+            while (tile >= each) tile -= each;                        // the next head
+            const int q0 = (first + tile) * kTile;
+            // A thread holds 8 rows' values for each of 4 keys, not 32 rows' for one: the statistics that it reads are a quarter.
+            // They are read before the scores are there: afterwards dP's product, whose operands both lie in shared memory,
+            // leaves other reads of it waiting.
             const float2 *l2 = reinterpret_cast<const float2 *>(stat + (j & 1) * 2 * kTile + 32 * part) + lane % 4;
             const float2 *d2 = l2 + kTile / 2;
+            ok = wait(kTFull + (j & 1), (j >> 1) & 1);
+            if (!ok) break;
+            const float2 minus_lse[4] = {l2[0], l2[4], l2[8], l2[12]};
+            ok = wait(kS, j & 1);
+            if (!ok) break;
+            fence_after();
             uint32_t s[32], out[16];
             float prob[32];
             tmem_ld_16x32(tm_s + 32 * part + my_lane, s);
@@ -859,7 +877,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                 const int from = key - reach - q0 - 32 * part - 2 * (lane % 4);   // of the first of the 4 keys, which are 8 apart
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    const float2 l = l2[4 * c];
+                    const float2 l = minus_lse[c];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int x = 16 * (k / 2) + 4 * c + 2 * (k % 2);
@@ -871,7 +889,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             } else {
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    const float2 l = l2[4 * c];
+                    const float2 l = minus_lse[c];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int x = 16 * (k / 2) + 4 * c + 2 * (k % 2);
@@ -882,30 +900,39 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             }
 #pragma unroll
             for (int c = 0; c < 16; ++c) out[c] = pack2<T>(prob[2 * c], prob[2 * c + 1]);
-            ok = (j == 0 || wait(kDsUsed, (j - 1) & 1)) && wait(kDp, j & 1);
+            ok = j == 0 || wait(kDsUsed, (j - 1) & 1);
             if (!ok) break;
             fence_after();
             tmem_st_16x16(tm_p + 16 * part + my_lane, out);
             tmem_st_16x16(tm_p + 16 * part + my_lane + (16u << 16), out + 8);
-            tmem_ld_16x32(tm_dp + 32 * part + my_lane, s);
-            tmem_ld_16x32(tm_dp + 32 * part + my_lane + (16u << 16), s + 16);
-            wait_ld();
             wait_st();
             fence_before();
             __syncwarp();
             if (lane == 0) barrier_arrive(bar(kP));
+            ok = wait(kDp, j & 1);
+            if (!ok) break;
+            fence_after();
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const float2 e = d2[4 * c];
+            for (int h = 0; h < 2; ++h) {                             // 16 keys at a time
+                uint32_t d[16];
+                tmem_ld_16x32(tm_dp + 32 * part + my_lane + (static_cast<uint32_t>(16 * h) << 16), d);
+                wait_ld();
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int x = 16 * (k / 2) + 4 * c + 2 * (k % 2);
-                    float v0, v1;
-                    add2(v0, v1, __uint_as_float(s[x]), __uint_as_float(s[x + 1]), e.x, e.y);
-                    mul2(v0, v1, v0, v1, prob[x], prob[x + 1]);
-                    out[x / 2] = pack2<T>(v0, v1);
+                for (int c = 0; c < 4; ++c) {
+                    const float2 e = d2[4 * c];
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const int x = 4 * c + 2 * k;
+                        float v0, v1;
+                        add2(v0, v1, __uint_as_float(d[x]), __uint_as_float(d[x + 1]), e.x, e.y);
+                        mul2(v0, v1, v0, v1, prob[16 * h + x], prob[16 * h + x + 1]);
+                        out[8 * h + x / 2] = pack2<T>(v0, v1);
+                    }
                 }
             }
+            fence_before();
+            __syncwarp();
+            if (lane == 0) barrier_arrive(bar(kDpRead));
             ok = wait(kPUsed, j & 1);
             if (!ok) break;
             fence_after();
@@ -976,12 +1003,13 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
 #pragma unroll
                     for (int e = 0; e < N; ++e) o[e] = __float_as_uint((k == 1 && n == 0 ? 0.0f : __uint_as_float(o[e])) + v[e]);
                 }
+                cluster_arrive();                                     // nobody's shared memory goes before it has been read
                 if (live) store_columns<T, N>(row, col, p.dim, o, factor);
             };
             if (share / 2 == 32) add_up(std::integral_constant<int, 32>{});
             else if (share / 2 == 16) add_up(std::integral_constant<int, 16>{});
             else add_up(std::integral_constant<int, 8>{});
-            cluster_sync();                                           // nobody's shared memory goes before it has been read
+            cluster_wait();
         }
     }
     end_cta(tmem);

@@ -84,6 +84,9 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_sync() {                      // every thread of every CTA of the cluster
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// the same in two halves
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 __device__ __forceinline__ float load_peer(uint32_t address, uint32_t rank) {
     float v;
     asm volatile("{\n.reg .b32 a;\nmapa.shared::cluster.u32 a, %1, %2;\nld.shared::cluster.f32 %0, [a];\n}" : "=f"(v) : "r"(address), "r"(rank) : "memory");
@@ -161,6 +164,14 @@ __device__ __forceinline__ void tmem_st_16x16(uint32_t at, const uint32_t *r) {
 __device__ __forceinline__ void tmem_st8(uint32_t at, const uint32_t *r) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
                  :: "r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+
+// 16 bytes of a tile: elements [8 chunk, 8 chunk + 8) of a row, where TMA's 128-byte swizzle put them
+__device__ __forceinline__ uint4 tile_chunk(uint32_t tile, int row, int chunk) {
+    uint4 v;
+    const uint32_t at = tile + (chunk / 8) * (128 * 128) + row * 128 + (((chunk % 8) ^ (row & 7)) << 4);
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
 }
 
 // ---- tcgen05.mma ----------------------------------------------------------------------------------
