@@ -61,21 +61,32 @@ struct AdamBatch {
     AdamTensor t[CAP];
 };
 
-// 32 random bits for a place: a Weyl step, then two multiply-xorshift rounds (odd constants from the
-// golden ratio and the roots of 2 and 3).
-__device__ __forceinline__ uint32_t random_bits(uint32_t place, uint32_t seed) {
-    uint32_t x = place * 0x9E3779B1u + seed;
+// 32 random bits for a place: a Weyl step (place * kWeyl + seed, which the caller takes), then two multiply-xorshift rounds
+// (odd constants from the golden ratio and the roots of 2 and 3).  The last shift is left to whoever takes the two halves.
+constexpr uint32_t kWeyl = 0x9E3779B1u;
+__device__ __forceinline__ uint32_t random_bits(uint32_t x) {
     x = (x ^ (x >> 15)) * 0x6A09E667u;
-    x = (x ^ (x >> 13)) * 0xBB67AE85u;
-    return x ^ (x >> 16);
+    return (x ^ (x >> 13)) * 0xBB67AE85u;
 }
 
-// Magnitude u in [0, 448 (1 + 2^-22)] to an e4m3 code, rounded up where the 20 bits cut from the mantissa plus
-// `noise` (20 bits) carry.  Below 2^-6 the codes have the fixed step 2^-9: adding 2^-6 lines the mantissa up with it.
+// Magnitude u in [0, 448 (1 + 2^-22)] to an e4m3 code, in the low byte, rounded up where the 20 bits cut from the mantissa
+// plus `noise` (20 bits, the last 4 zero) carry.  From 2^-6 on the codes step as the mantissa does; below it they have the
+// fixed step 2^-9, which u / 2 + 2^-7 turns into the mantissa's, and the larger of the two is the one that counts.
+// ((127 - 7) * 8 = 960; code 8 is 2^-6.)
 __device__ __forceinline__ uint32_t encode(float u, uint32_t noise) {
-    const bool sub = u < 0.015625f;
-    const uint32_t b = __float_as_uint(sub ? __fadd_rn(u, 0.015625f) : u) + noise;
-    return min((b >> 20) - (sub ? 968u : 960u), 126u);   // (127 - 7) * 8 = 960; code 8 is 2^-6
+    const float t = fmaxf(u, fmaf(u, 0.5f, 0.0078125f));
+    return (__float_as_uint(t) + noise - (960u << 20)) >> 20;
+}
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+__device__ __forceinline__ uint32_t high_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
+}
+__device__ __forceinline__ float max_nan(float a, float b) {          // NaN if one of them is
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+    return d;
 }
 
 __device__ __forceinline__ void decode4(uint32_t w, float scale, float *out) {
@@ -160,41 +171,50 @@ adamw_kernel(const __grid_constant__ AdamBatch<CAP> a) {
             load8_some(static_cast<const float *>(t.m) + at, m, valid, wide);
             load8_some(static_cast<const float *>(t.v) + at, v, valid, wide);
         }
-        uint32_t top_m = 0, top_r = 0;
+        if (!wide) {                                         // places past the tensor's end are zeros, whatever the block's scale
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (e >= valid) m[e] = v[e] = 0.0f;
+        }
+        float top_m = 0.0f, top_r = 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
+            // (not the packed forms of these operations: the compiler fuses a packed product with a packed sum)
             const float x = g[e] * gs;
             m[e] = __fadd_rn(__fmul_rn(m[e], a.s.beta1), __fmul_rn(x, a.s.one_minus_beta1));
             v[e] = __fadd_rn(__fmul_rn(v[e], a.s.beta2), __fmul_rn(__fmul_rn(x, x), a.s.one_minus_beta2));
             r[e] = __fsqrt_rn(v[e]);
-            p[e] = p[e] * a.s.keep - a.s.step_size * (m[e] / (r[e] * a.s.inv_root_bc2 + a.s.eps));
+            // (two ulp of the update: far below the parameter's own rounding)
+            p[e] = fmaf(p[e], a.s.keep, -a.s.step_size * __fdividef(m[e], fmaf(r[e], a.s.inv_root_bc2, a.s.eps)));
             if constexpr (EIGHT) {
-                // places past the tensor's end (valid < 8) hold g = m = v = 0 (NaN under a NaN scale or factor): not counted
-                if (e < valid) {
-                    top_m = max(top_m, __float_as_uint(m[e]) & 0x7fffffffu);
-                    top_r = max(top_r, __float_as_uint(r[e]) & 0x7fffffffu);
-                }
+                top_m = max_nan(top_m, fabsf(m[e]));
+                top_r = max_nan(top_r, r[e]);
             }
         }
         if constexpr (MASTER) store8_some(t.master + at, p, valid, wide);
         store8_some(static_cast<T *>(t.param) + at, p, valid, wide);
         if constexpr (EIGHT) {
-            top_m = __reduce_max_sync(0xffffffffu, top_m);
-            top_r = __reduce_max_sync(0xffffffffu, top_r);
             float scale_m, factor_m, scale_r, factor_r;
-            block_scale(top_m, scale_m, factor_m);
-            block_scale(top_r, scale_r, factor_r);
-            uint32_t wm[2] = {0u, 0u}, wr[2] = {0u, 0u};
-            const uint32_t place = (a.s.block0 + b) * kBlock + lane * 8;
+            block_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(top_m)), scale_m, factor_m);
+            block_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(top_r)), scale_r, factor_r);
+            uint32_t cm[8], cr[8], wm[2], wr[2];
+            const uint32_t place = ((a.s.block0 + b) * kBlock + lane * 8) * kWeyl + a.s.seed;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const uint32_t h = random_bits(place + e, a.s.seed);
-                uint32_t cm = encode(__fmul_rn(fabsf(m[e]), factor_m), (h & 0xffffu) << 4) | ((__float_as_uint(m[e]) >> 31) << 7);
-                const float ur = __fmul_rn(r[e], factor_r);
-                uint32_t cr = encode(ur, (h >> 16) << 4);
-                if (cr == 0u && ur > 0.0f) cr = 1u;
-                wm[e >> 2] |= (cm & 0xffu) << (8 * (e & 3));
-                wr[e >> 2] |= (cr & 0xffu) << (8 * (e & 3));
+                const uint32_t h = random_bits(place + e * kWeyl);
+                cm[e] = encode(__fmul_rn(fabsf(m[e]), factor_m), ((h ^ (h >> 16)) << 4) & 0xffff0u);
+                cr[e] = encode(__fmul_rn(r[e], factor_r), (h >> 12) & 0xffff0u);
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                wm[k] = low_bytes(cm[4 * k], cm[4 * k + 1], cm[4 * k + 2], cm[4 * k + 3]);
+                wm[k] |= high_bytes(__float_as_uint(m[4 * k]), __float_as_uint(m[4 * k + 1]), __float_as_uint(m[4 * k + 2]), __float_as_uint(m[4 * k + 3])) & 0x80808080u;
+                wr[k] = low_bytes(cr[4 * k], cr[4 * k + 1], cr[4 * k + 2], cr[4 * k + 3]);
+                if ((wr[k] - 0x01010101u) & ~wr[k] & 0x80808080u) {   // some code is 0 (rare): only that of a zero may be
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (((wr[k] >> (8 * e)) & 0xffu) == 0 && __fmul_rn(r[4 * k + e], factor_r) > 0.0f) wr[k] |= 1u << (8 * e);
+                }
             }
             store_codes(static_cast<uint8_t *>(t.m) + at, make_uint2(wm[0], wm[1]), valid, wide);
             store_codes(static_cast<uint8_t *>(t.v) + at, make_uint2(wr[0], wr[1]), valid, wide);

@@ -1,4 +1,5 @@
-// Packed binary32 arithmetic of sm_100: one instruction for two lanes, each rounded as the scalar operation is.
+// Packed binary32 arithmetic of sm_100: one instruction for two lanes.  (The compiler may fuse a
+// product with a sum, whatever rounding they name: not for arithmetic whose roundings are part of the result's definition.)
 #pragma once
 
 namespace fewbit {
