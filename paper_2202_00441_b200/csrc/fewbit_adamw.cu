@@ -18,6 +18,7 @@
 #include <cmath>
 
 #include "fewbit_device.cuh"
+#include "fewbit_packed.cuh"
 
 namespace fewbit {
 bool pdl_enabled();
@@ -26,7 +27,7 @@ int device_sm_count(cudaError_t *err);
 namespace {
 
 constexpr int kBlock = FEWBIT_ADAMW_BLOCK;
-constexpr int kAdamThreads = 256;
+constexpr int kAdamThreads = 256, kAdamCtas = 4;   // CTAs on an SM
 
 struct AdamTensor {
     void *param;
@@ -83,6 +84,30 @@ __device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c
 __device__ __forceinline__ uint32_t high_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
 }
+// Roots of 8 values, correctly rounded (their codes must not depend on how they were computed).  From 2^-100 on: s = v / sqrt(v)
+// from an approximate inverse root, then one Newton step whose residual v - s^2 a fused multiply-add gives exactly; equal to
+// the rounded root for every one of these binary32 values.  Smaller ones (zero among them), infinities and NaN take the
+// library's root, for the whole lane: a fifth of the instructions of eight of them is what the others need.
+__device__ __forceinline__ void roots(const float (&v)[8], float (&r)[8]) {
+    bool other = false;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        float y0, y1, s0, s1, e0, e1;
+        asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y0) : "f"(v[e]));
+        asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y1) : "f"(v[e + 1]));
+        mul2(s0, s1, v[e], v[e + 1], y0, y1);
+        fma2(e0, e1, s0, s1, s0, s1, -v[e], -v[e + 1]);
+        mul2(y0, y1, y0, y1, -0.5f, -0.5f);
+        fma2(r[e], r[e + 1], e0, e1, y0, y1, s0, s1);
+        other |= __float_as_uint(v[e]) - 0x0d800000u >= 0x72000000u;
+        other |= __float_as_uint(v[e + 1]) - 0x0d800000u >= 0x72000000u;
+    }
+    if (other) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) r[e] = __fsqrt_rn(v[e]);
+    }
+}
+
 __device__ __forceinline__ float max_nan(float a, float b) {          // NaN if one of them is
     float d;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
@@ -93,7 +118,8 @@ __device__ __forceinline__ void decode4(uint32_t w, float scale, float *out) {
     const __half2_raw lo = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w & 0xffffu), __NV_E4M3);
     const __half2_raw hi = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w >> 16), __NV_E4M3);
     const float2 a = __half22float2(__half2(lo)), b = __half22float2(__half2(hi));
-    out[0] = a.x * scale; out[1] = a.y * scale; out[2] = b.x * scale; out[3] = b.y * scale;
+    mul2(out[0], out[1], a.x, a.y, scale, scale);
+    mul2(out[2], out[3], b.x, b.y, scale, scale);
 }
 
 // (scale to store, factor from value to code) of a block whose largest magnitude has the bits `top`.
@@ -135,19 +161,114 @@ __device__ __forceinline__ void store_codes(uint8_t *p, uint2 w, int valid, bool
         if (e < valid) p[e] = static_cast<uint8_t>((e < 4 ? w.x : w.y) >> (8 * (e & 3)));
 }
 
+// One block: what a warp does with 8 elements of each lane, `valid` of them there.  WIDE: all of them, on aligned buffers.
+template <typename T, bool EIGHT, bool MASTER, bool WIDE>
+__device__ __forceinline__ void update_block(const AdamTensor &t, const AdamScalars &s, float gs, uint32_t b, uint32_t block, size_t at, int valid) {
+    constexpr bool wide = WIDE;
+    const int lane = threadIdx.x & 31;
+    float p[8], g[8], m[8], v[8], r[8];
+    load8_some(static_cast<const T *>(t.grad) + at, g, valid, wide);
+    if constexpr (MASTER) load8_some(t.master + at, p, valid, wide);
+    else load8_some(static_cast<const T *>(t.param) + at, p, valid, wide);
+    if constexpr (EIGHT) {
+        const uint2 cm = load_codes(static_cast<const uint8_t *>(t.m) + at, valid, wide);
+        const uint2 cv = load_codes(static_cast<const uint8_t *>(t.v) + at, valid, wide);
+        const float sm = t.m_scale[block], sv = t.v_scale[block];
+        decode4(cm.x, sm, m); decode4(cm.y, sm, m + 4);
+        decode4(cv.x, sv, v); decode4(cv.y, sv, v + 4);
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) mul2(v[e], v[e + 1], v[e], v[e + 1], v[e], v[e + 1]);
+    } else {
+        load8_some(static_cast<const float *>(t.m) + at, m, valid, wide);
+        load8_some(static_cast<const float *>(t.v) + at, v, valid, wide);
+    }
+    if constexpr (!WIDE) {                                         // places past the tensor's end are zeros, whatever the block's scale
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (e >= valid) m[e] = v[e] = 0.0f;
+    }
+    float top_m = 0.0f, top_r = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; e += 2) {
+        // Packed products, but scalar sums: the compiler fuses a packed product with a packed sum.
+        float x0, x1, y0, y1;
+        mul2(g[e], g[e + 1], g[e], g[e + 1], gs, gs);
+        mul2(x0, x1, m[e], m[e + 1], s.beta1, s.beta1);
+        mul2(y0, y1, g[e], g[e + 1], s.one_minus_beta1, s.one_minus_beta1);
+        m[e] = __fadd_rn(x0, y0);
+        m[e + 1] = __fadd_rn(x1, y1);
+        mul2(x0, x1, v[e], v[e + 1], s.beta2, s.beta2);
+        mul2(y0, y1, g[e], g[e + 1], g[e], g[e + 1]);
+        mul2(y0, y1, y0, y1, s.one_minus_beta2, s.one_minus_beta2);
+        v[e] = __fadd_rn(x0, y0);
+        v[e + 1] = __fadd_rn(x1, y1);
+    }
+    roots(v, r);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        // (two ulp of the update: far below the parameter's own rounding)
+        p[e] = fmaf(p[e], s.keep, -s.step_size * __fdividef(m[e], fmaf(r[e], s.inv_root_bc2, s.eps)));
+        if constexpr (EIGHT) {
+            top_m = max_nan(top_m, fabsf(m[e]));
+            top_r = max_nan(top_r, r[e]);
+        }
+    }
+    if constexpr (MASTER) store8_some(t.master + at, p, valid, wide);
+    store8_some(static_cast<T *>(t.param) + at, p, valid, wide);
+    if constexpr (EIGHT) {
+        float scale_m, factor_m, scale_r, factor_r;
+        block_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(top_m)), scale_m, factor_m);
+        block_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(top_r)), scale_r, factor_r);
+        uint32_t cm[8], cr[8], wm[2], wr[2];
+        const uint32_t place = ((s.block0 + b) * kBlock + lane * 8) * kWeyl + s.seed;
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            float um[2], ur[2];
+            mul2(um[0], um[1], fabsf(m[e]), fabsf(m[e + 1]), factor_m, factor_m);
+            mul2(ur[0], ur[1], r[e], r[e + 1], factor_r, factor_r);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const uint32_t h = random_bits(place + (e + x) * kWeyl);
+                cm[e + x] = encode(um[x], ((h << 4) ^ (h >> 12)) & 0xffff0u);
+                cr[e + x] = encode(ur[x], (h >> 12) & 0xffff0u);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            wm[k] = low_bytes(cm[4 * k], cm[4 * k + 1], cm[4 * k + 2], cm[4 * k + 3]);
+            wm[k] |= high_bytes(__float_as_uint(m[4 * k]), __float_as_uint(m[4 * k + 1]), __float_as_uint(m[4 * k + 2]), __float_as_uint(m[4 * k + 3])) & 0x80808080u;
+            wr[k] = low_bytes(cr[4 * k], cr[4 * k + 1], cr[4 * k + 2], cr[4 * k + 3]);
+            if ((wr[k] - 0x01010101u) & ~wr[k] & 0x80808080u) {   // some code is 0 (rare): only that of a zero may be
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (((wr[k] >> (8 * e)) & 0xffu) == 0 && __fmul_rn(r[4 * k + e], factor_r) > 0.0f) wr[k] |= 1u << (8 * e);
+            }
+        }
+        store_codes(static_cast<uint8_t *>(t.m) + at, make_uint2(wm[0], wm[1]), valid, wide);
+        store_codes(static_cast<uint8_t *>(t.v) + at, make_uint2(wr[0], wr[1]), valid, wide);
+        if (lane == 0) { t.m_scale[block] = scale_m; t.v_scale[block] = scale_r; }
+    } else {
+        store8_some(static_cast<float *>(t.m) + at, m, valid, wide);
+        store8_some(static_cast<float *>(t.v) + at, v, valid, wide);
+    }
+}
+
 template <typename T, bool EIGHT, bool MASTER, int CAP>
-__global__ void __launch_bounds__(kAdamThreads)
+__global__ void __launch_bounds__(kAdamThreads, kAdamCtas)
 adamw_kernel(const __grid_constant__ AdamBatch<CAP> a) {
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31;
     const uint32_t warps = gridDim.x * (kAdamThreads / 32);
     pdl_wait();
     const float gs = a.s.grad_scale ? *a.s.grad_scale : 1.0f;
+    uint32_t lo = 0;
     for (uint32_t b = blockIdx.x * (kAdamThreads / 32) + (threadIdx.x >> 5); b < a.blocks; b += warps) {
-        uint32_t lo = 0, hi = a.count;                       // the last tensor that starts at or before block b
-        while (hi - lo > 1) {
-            const uint32_t mid = (lo + hi) >> 1;
-            if (a.first[mid] <= b) lo = mid; else hi = mid;
+        if (lo + 1 < a.count && a.first[lo + 1] <= b) {      // not the last block's tensor: the last one that starts at or before b
+            uint32_t hi = a.count;
+            while (hi - lo > 1) {
+                const uint32_t mid = (lo + hi) >> 1;
+                if (a.first[mid] <= b) lo = mid; else hi = mid;
+            }
         }
         const AdamTensor &t = a.t[lo];
         const unsigned long long n = t.n & ~kWideBit;
@@ -155,74 +276,8 @@ adamw_kernel(const __grid_constant__ AdamBatch<CAP> a) {
         const size_t at = static_cast<size_t>(block) * kBlock + lane * 8;
         const int valid = at >= n ? 0 : (n - at < 8 ? static_cast<int>(n - at) : 8);
         const bool wide = (t.n & kWideBit) && static_cast<size_t>(block + 1) * kBlock <= n;   // the same for the whole warp
-        float p[8], g[8], m[8], v[8], r[8];
-        load8_some(static_cast<const T *>(t.grad) + at, g, valid, wide);
-        if constexpr (MASTER) load8_some(t.master + at, p, valid, wide);
-        else load8_some(static_cast<const T *>(t.param) + at, p, valid, wide);
-        if constexpr (EIGHT) {
-            const uint2 cm = load_codes(static_cast<const uint8_t *>(t.m) + at, valid, wide);
-            const uint2 cv = load_codes(static_cast<const uint8_t *>(t.v) + at, valid, wide);
-            const float sm = t.m_scale[block], sv = t.v_scale[block];
-            decode4(cm.x, sm, m); decode4(cm.y, sm, m + 4);
-            decode4(cv.x, sv, v); decode4(cv.y, sv, v + 4);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= v[e];
-        } else {
-            load8_some(static_cast<const float *>(t.m) + at, m, valid, wide);
-            load8_some(static_cast<const float *>(t.v) + at, v, valid, wide);
-        }
-        if (!wide) {                                         // places past the tensor's end are zeros, whatever the block's scale
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (e >= valid) m[e] = v[e] = 0.0f;
-        }
-        float top_m = 0.0f, top_r = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            // (not the packed forms of these operations: the compiler fuses a packed product with a packed sum)
-            const float x = g[e] * gs;
-            m[e] = __fadd_rn(__fmul_rn(m[e], a.s.beta1), __fmul_rn(x, a.s.one_minus_beta1));
-            v[e] = __fadd_rn(__fmul_rn(v[e], a.s.beta2), __fmul_rn(__fmul_rn(x, x), a.s.one_minus_beta2));
-            r[e] = __fsqrt_rn(v[e]);
-            // (two ulp of the update: far below the parameter's own rounding)
-            p[e] = fmaf(p[e], a.s.keep, -a.s.step_size * __fdividef(m[e], fmaf(r[e], a.s.inv_root_bc2, a.s.eps)));
-            if constexpr (EIGHT) {
-                top_m = max_nan(top_m, fabsf(m[e]));
-                top_r = max_nan(top_r, r[e]);
-            }
-        }
-        if constexpr (MASTER) store8_some(t.master + at, p, valid, wide);
-        store8_some(static_cast<T *>(t.param) + at, p, valid, wide);
-        if constexpr (EIGHT) {
-            float scale_m, factor_m, scale_r, factor_r;
-            block_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(top_m)), scale_m, factor_m);
-            block_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(top_r)), scale_r, factor_r);
-            uint32_t cm[8], cr[8], wm[2], wr[2];
-            const uint32_t place = ((a.s.block0 + b) * kBlock + lane * 8) * kWeyl + a.s.seed;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t h = random_bits(place + e * kWeyl);
-                cm[e] = encode(__fmul_rn(fabsf(m[e]), factor_m), ((h ^ (h >> 16)) << 4) & 0xffff0u);
-                cr[e] = encode(__fmul_rn(r[e], factor_r), (h >> 12) & 0xffff0u);
-            }
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                wm[k] = low_bytes(cm[4 * k], cm[4 * k + 1], cm[4 * k + 2], cm[4 * k + 3]);
-                wm[k] |= high_bytes(__float_as_uint(m[4 * k]), __float_as_uint(m[4 * k + 1]), __float_as_uint(m[4 * k + 2]), __float_as_uint(m[4 * k + 3])) & 0x80808080u;
-                wr[k] = low_bytes(cr[4 * k], cr[4 * k + 1], cr[4 * k + 2], cr[4 * k + 3]);
-                if ((wr[k] - 0x01010101u) & ~wr[k] & 0x80808080u) {   // some code is 0 (rare): only that of a zero may be
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (((wr[k] >> (8 * e)) & 0xffu) == 0 && __fmul_rn(r[4 * k + e], factor_r) > 0.0f) wr[k] |= 1u << (8 * e);
-                }
-            }
-            store_codes(static_cast<uint8_t *>(t.m) + at, make_uint2(wm[0], wm[1]), valid, wide);
-            store_codes(static_cast<uint8_t *>(t.v) + at, make_uint2(wr[0], wr[1]), valid, wide);
-            if (lane == 0) { t.m_scale[block] = scale_m; t.v_scale[block] = scale_r; }
-        } else {
-            store8_some(static_cast<float *>(t.m) + at, m, valid, wide);
-            store8_some(static_cast<float *>(t.v) + at, v, valid, wide);
-        }
+        if (wide) update_block<T, EIGHT, MASTER, true>(t, a.s, gs, b, block, at, valid);
+        else update_block<T, EIGHT, MASTER, false>(t, a.s, gs, b, block, at, valid);
     }
 }
 
@@ -247,7 +302,7 @@ cudaError_t launch_adamw(const fewbit_adamw_tensor *tensors, const void *const *
     }
     a.blocks = at;
     const unsigned want = (at + kAdamThreads / 32 - 1) / (kAdamThreads / 32);
-    const unsigned most = static_cast<unsigned>(sms) * 8;
+    const unsigned most = static_cast<unsigned>(sms) * kAdamCtas;
     return launch_pdl(adamw_kernel<T, EIGHT, MASTER, CAP>, want < most ? want : most, kAdamThreads, 0, st, pdl_enabled(), a);
 }
 
