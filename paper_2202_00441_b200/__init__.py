@@ -17,4 +17,5 @@ from .operators import (  # noqa: F401
     fewbit_attention_timeout_count, fewbit_qk_norm_rope_bwd, fewbit_qk_norm_rope_fwd,
 )
 from . import workloads  # noqa: F401
-from .autograd import FewBitActivation, fewbit_activation  # noqa: F401
+from .autograd import FewBitActivation, fewbit_activation, fewbit_attention, fewbit_qk_norm_rope  # noqa: F401
+from .optim import FewBitAdamW  # noqa: F401

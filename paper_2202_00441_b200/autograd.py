@@ -1,4 +1,5 @@
-"""Drop-in activation modules over the C ABI (Listing 1 as a PyTorch layer).
+"""Drop-in activation modules over the C ABI (Listing 1 as a PyTorch layer), and attention and the head norm with
+rotation as differentiable functions.
 
 ``FewBitActivation("gelu", bits=3)`` replaces ``nn.GELU()``: the forward pass
 returns the exact activation, autograd keeps only ``bits`` bits per element
@@ -12,6 +13,7 @@ import torch
 from torch import nn
 
 from .binding import Table, fewbit_bwd, fewbit_fwd, fewbit_fwd_bias, fewbit_table_create, fewbit_table_create_folded
+from .operators import fewbit_attention_bwd, fewbit_attention_fwd, fewbit_qk_norm_rope_bwd, fewbit_qk_norm_rope_fwd
 
 
 def _flat_aligned(t: torch.Tensor) -> torch.Tensor:
@@ -90,3 +92,72 @@ def fewbit_activation(x: torch.Tensor, table: Table, bias: torch.Tensor | None =
     if bias is not None:
         return _FewBitBiasFunction.apply(x, bias, table)
     return _FewBitFunction.apply(x, table)
+
+
+def _attention_layout(t: torch.Tensor) -> torch.Tensor:
+    """`t` as the library takes it: contiguous heads, strides that are multiples of 8 elements, 16-byte alignment."""
+    st = t.stride()
+    if st[-1] != 1 or t.data_ptr() % 16 or any(s % 8 or s <= 0 for s, n in zip(st[:-1], t.shape[:-1]) if n > 1):
+        return t.clone(memory_format=torch.contiguous_format)
+    return t
+
+
+class _AttentionFunction(torch.autograd.Function):
+    """Keeps q, k, v, the output and one number for each row and head; the probabilities are recomputed."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, kw):
+        q, k, v = _attention_layout(q), _attention_layout(k), _attention_layout(v)
+        out, lse = fewbit_attention_fwd(q, k, v, **kw)
+        ctx.kw = kw
+        ctx.save_for_backward(q, k, v, out, lse)
+        return out
+
+    @staticmethod
+    def backward(ctx, grad_out):
+        q, k, v, out, lse = ctx.saved_tensors
+        return (*fewbit_attention_bwd(_attention_layout(grad_out), q, k, v, out, lse, **ctx.kw), None)
+
+
+def fewbit_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool = False, scale: float | None = None,
+                     q_offsets: torch.Tensor | None = None, k_offsets: torch.Tensor | None = None,
+                     max_q_len: int | None = None, max_k_len: int | None = None) -> torch.Tensor:
+    """softmax(scale q k^T) v with gradients; arguments as in ``fewbit_attention_fwd``.  Tensors whose strides the library
+    does not take (a transposed head, an expanded batch) are copied first."""
+    return _AttentionFunction.apply(q, k, v, {"causal": causal, "scale": scale, "q_offsets": q_offsets, "k_offsets": k_offsets,
+                                              "max_q_len": max_q_len, "max_k_len": max_k_len})
+
+
+def _contiguous_heads(t: torch.Tensor) -> torch.Tensor:
+    return t if t.stride(-1) == 1 or t.shape[-1] == 1 else t.contiguous()
+
+
+class _QkNormRopeFunction(torch.autograd.Function):
+    """Keeps the inputs only: the norm's factor is recomputed."""
+
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, kw):
+        q, k = _contiguous_heads(q), _contiguous_heads(k)
+        wide = [None if w is None else w.detach().float().contiguous() for w in (q_weight, k_weight)]
+        out = fewbit_qk_norm_rope_fwd(q, k, *wide, **kw)
+        ctx.kw, ctx.weight_types = kw, [None if w is None else w.dtype for w in (q_weight, k_weight)]
+        ctx.save_for_backward(q, k, *wide)
+        return out
+
+    @staticmethod
+    def backward(ctx, grad_q, grad_k):
+        q, k, qw, kw_ = ctx.saved_tensors
+        wanted = (ctx.needs_input_grad[2] and qw is not None) or (ctx.needs_input_grad[3] and kw_ is not None)
+        dq, dk, dqw, dkw = fewbit_qk_norm_rope_bwd(_contiguous_heads(grad_q), _contiguous_heads(grad_k), q, k, qw, kw_,
+                                                   weight_grads=wanted, **ctx.kw)
+        dws = [g.to(t) if g is not None and t is not None else None for g, t in zip((dqw, dkw), ctx.weight_types)]
+        return dq, dk, dws[0], dws[1], None
+
+
+def fewbit_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: torch.Tensor | None, k_weight: torch.Tensor | None,
+                        cos: torch.Tensor | None, sin: torch.Tensor | None, *, positions: torch.Tensor | None = None,
+                        eps: float = 1e-6, interleaved: bool = False):
+    """RMS norm of every query and key head and the position rotation, with gradients for q, k and the weights (of any
+    floating type); arguments as in ``fewbit_qk_norm_rope_fwd``."""
+    return _QkNormRopeFunction.apply(q, k, q_weight, k_weight,
+                                     {"cos": cos, "sin": sin, "positions": positions, "eps": eps, "interleaved": interleaved})

@@ -116,6 +116,8 @@ fewbit_status fill(const fewbit_attention_shape *s, const Sizes &z, Params *p) {
     static std::atomic<unsigned int *> cached[64];                    // per device
     int dev = 0;
     cudaError_t err = cudaGetDevice(&dev);
+    // a thread that has not used the runtime yet (autograd's) has no context, which the tensor maps' encoder needs
+    if (err == cudaSuccess) err = cudaSetDevice(dev);
     if (err != cudaSuccess) return cuda_status(err);
     unsigned int *at = dev < 64 ? cached[dev].load(std::memory_order_acquire) : nullptr;
     if (at == nullptr) {

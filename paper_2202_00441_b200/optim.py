@@ -1,0 +1,93 @@
+"""AdamW with moments of 8 (or 32) bits as a PyTorch optimizer over ``fewbit_adamw_step``."""
+from __future__ import annotations
+
+import torch
+
+from .operators import ADAMW_BLOCK, fewbit_adamw_create, fewbit_adamw_step
+
+
+class FewBitAdamW(torch.optim.Optimizer):
+    """Drop-in for ``torch.optim.AdamW`` on CUDA parameters of float32, bfloat16 or float16.
+
+    state_bits: 8 keeps each moment as one float8 code an element and one float32 scale for each 256 elements (rounded
+    stochastically, from ``seed``), 32 keeps float32 moments.  master: 16-bit parameters get a float32 copy that the step
+    updates; the parameter is its rounding.  All parameters of one type and device are updated in one launch (up to 400
+    tensors).  ``step(grad_scale=t)`` multiplies every gradient by the one float32 value ``t`` on the device."""
+
+    def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8, weight_decay: float = 1e-2,
+                 state_bits: int = 8, master: bool = True, seed: int = 0):
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32")
+        self._handles, self.seed = {}, int(seed)
+        super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay, state_bits=state_bits, master=master))
+
+    def add_param_group(self, group):
+        super().add_param_group(group)
+        for p in self.param_groups[-1]["params"]:
+            if not p.is_cuda or not p.is_contiguous() or p.dtype not in (torch.float32, torch.bfloat16, torch.float16):
+                raise ValueError("parameters must be contiguous CUDA tensors of float32, bfloat16 or float16")
+
+    def __getstate__(self):
+        return {**super().__getstate__(), "seed": self.seed}
+
+    def __setstate__(self, state):
+        super().__setstate__(state)
+        self._handles = {}
+
+    def load_state_dict(self, state_dict):
+        super().load_state_dict(state_dict)
+        # the base class converts floating state to the parameter's type; codes, scales and masters keep theirs
+        for saved, group in zip(state_dict["param_groups"], self.param_groups):
+            for key, p in zip(saved["params"], group["params"]):
+                if key in state_dict["state"]:
+                    self.state[p] = {k: v.to(p.device, copy=True) if torch.is_tensor(v) else v for k, v in state_dict["state"][key].items()}
+        self._handles = {}
+
+    def _init_state(self, p, group):
+        state = self.state[p]
+        state["step"] = 0
+        if group["state_bits"] == 8:
+            blocks = -(-p.numel() // ADAMW_BLOCK)
+            for name in ("exp_avg", "exp_avg_sq"):
+                state[name] = torch.zeros(p.shape, dtype=torch.uint8, device=p.device).view(torch.float8_e4m3fn)
+                state[name + "_scale"] = torch.zeros(blocks, dtype=torch.float32, device=p.device)
+        else:
+            for name in ("exp_avg", "exp_avg_sq"):
+                state[name] = torch.zeros(p.shape, dtype=torch.float32, device=p.device)
+        if group["master"] and p.dtype != torch.float32:
+            state["master"] = p.detach().float()
+
+    @torch.no_grad()
+    def step(self, closure=None, grad_scale: torch.Tensor | None = None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        for number, group in enumerate(self.param_groups):
+            buckets = {}
+            for p in group["params"]:
+                if p.grad is None:
+                    continue
+                if p.grad.is_sparse:
+                    raise RuntimeError("FewBitAdamW takes dense gradients")
+                if not self.state[p]:
+                    self._init_state(p, group)
+                buckets.setdefault((p.device, p.dtype, self.state[p]["step"]), []).append(p)
+            for place, ((device, dtype, step), params) in enumerate(buckets.items()):
+                names = ["exp_avg", "exp_avg_sq"]
+                if group["state_bits"] == 8:
+                    names += ["exp_avg_scale", "exp_avg_sq_scale"]
+                lists = [[self.state[p][n] for p in params] for n in names] + [None] * (4 - len(names))
+                masters = [self.state[p]["master"] for p in params] if "master" in self.state[params[0]] else None
+                # the handle holds addresses: it is made anew when a parameter or its state has moved
+                where = [t.data_ptr() for x in [params, *lists, masters] if x is not None for t in x]
+                held = self._handles.get((number, device, dtype))
+                if held is None or held[0] != where:
+                    held = self._handles[(number, device, dtype)] = (where, fewbit_adamw_create(params, *lists, masters))
+                grads = [p.grad.to(dtype).contiguous() for p in params]
+                seed = (self.seed + 0x9E3779B1 * (step + 1) + 0x85EBCA6B * (64 * number + place)) & 0xFFFFFFFF
+                fewbit_adamw_step(held[1], grads, step=step + 1, lr=float(group["lr"]), betas=group["betas"], eps=group["eps"],
+                                  weight_decay=group["weight_decay"], seed=seed, grad_scale=grad_scale)
+                for p in params:
+                    self.state[p]["step"] = step + 1
+        return loss
