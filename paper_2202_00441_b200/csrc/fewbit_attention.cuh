@@ -469,7 +469,7 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
 // dP full, dS ready, dQ done.
 enum { qQ = 0, qKFull = 1, qKEmpty = 4, qVFull = 7, qVEmpty = 9, qS = 11, qDp = 13, qDs = 14, qDone = 15, qBars = 16 };
 
-template <int DIM> constexpr int dq_smem() { return 7 * (DIM / 64) * static_cast<int>(kHalfTile) + static_cast<int>(sizeof(Sync)) + kTile * 4; }
+template <int DIM> constexpr int dq_smem() { return 7 * (DIM / 64) * static_cast<int>(kHalfTile) + static_cast<int>(sizeof(Sync)) + 5 * kTile * 4; }
 
 template <typename T, int DIM>
 __global__ void __launch_bounds__(kThreadsAttn, 1)
@@ -480,6 +480,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
     const uint32_t base = smem_address(raw);                          // no room to align it here: the host checks
     Sync *sync = reinterpret_cast<Sync *>(raw + 7 * kBytes);
     float *row_delta = reinterpret_cast<float *>(sync + 1);           // [128]
+    float *row_sum = row_delta + kTile;                               // [4][128]
     const int warp = uniform(static_cast<int>(threadIdx.x >> 5)), lane = threadIdx.x & 31;
     pdl_wait();
     const Work w = find_work(p, blockIdx.x, p.heads, true);
@@ -499,7 +500,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
     float lse = -INFINITY;
     if (warp < kMmaWarp) {
 #pragma unroll
-        for (int x = 0; x < 8 / kRows; ++x) {
+        for (int x = 0; n > 1 && x < 8 / kRows; ++x) {
             const int row = q0 + 8 * warp + kRows * x + lane / kLanes, col = lane % kLanes * 8;
             const bool there = row < w.q_len && col < p.dim;
             const T *from = static_cast<const T *>(p.o.p) + row_of(w, p.o, w.head, there ? row : 0, w.q_first) + (there ? col : 0);
@@ -590,12 +591,15 @@ attention_dq_kernel(const __grid_constant__ Params p) {
         const bool live = i < w.q_len;
         const uint32_t my_lane = static_cast<uint32_t>(warp & 3) << 21;
         const float minus_lse = lse == -INFINITY ? -INFINITY : -lse * kLog2e;   // a row that sees nothing: every probability is 0
-        bool ok = n == 0 || wait(qQ, 0);
+        // delta from the rounded outputs is off by their rounding.  Rows that see few keys feel that most, and those of one key
+        // tile (n = 1) need no outputs: their delta is the sum of P dP, which is all there before dS is computed.  Longer rows
+        // know at the end how far theirs was off, by the sum of dS, which should be 0: dK gets the corrected value.
+        bool ok = n <= 1 || wait(qQ, 0);
 #pragma unroll
         for (int x = 0; x < 8 / kRows; ++x) {
             const int row = 8 * warp + kRows * x + lane / kLanes;
             float sum = 0.0f;
-            if (n > 0 && q0 + row < w.q_len) {
+            if (n > 1 && q0 + row < w.q_len) {
                 const uint4 g = tile_chunk(sm_g, row, lane % kLanes);
                 T a[8], b[8];
                 memcpy(a, &outputs[x], 16);
@@ -608,14 +612,21 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             if (lane % kLanes == 0) row_delta[row] = sum;
         }
         asm volatile("bar.sync 1, %0;" :: "n"(kWorkThreads) : "memory");   // the element-wise warps only
-        const float minus_delta = -row_delta[r];
-        if (part < 2) stat_block(p, w, w.head, w.tile)[part * kTile + r] = part == 0 ? minus_lse : minus_delta;
+        float minus_delta = -row_delta[r], drift = 0.0f;
+        auto over_parts = [&](float mine) {                           // a row's sum over its four threads
+            row_sum[part * kTile + r] = mine;
+            asm volatile("bar.sync 1, %0;" :: "n"(kWorkThreads) : "memory");
+            return (row_sum[r] + row_sum[kTile + r]) + (row_sum[2 * kTile + r] + row_sum[3 * kTile + r]);
+        };
         const int seen = p.causal ? min(w.k_len, i + 1 + w.k_len - w.q_len) : w.k_len;
         const int tile_seen = p.causal ? min(w.k_len, q0 + 1 + w.k_len - w.q_len) : w.k_len;
         for (int j = 0; ok && j < n; ++j) {
             const uint32_t s_at = tm_s + (j & 1) * kTile + 32 * part + my_lane;
             ok = wait(qS + (j & 1), (j >> 1) & 1);
-            if (!ok) break;
+            if (!ok) {
+                if (n == 1) over_parts(0.0f);                         // the others wait there
+                break;
+            }
             fence_after();
             uint32_t s[32], d[32], out[16];
             float prob[32];
@@ -634,20 +645,39 @@ attention_dq_kernel(const __grid_constant__ Params p) {
                 }
             }
             ok = wait(qDp, j & 1);
-            if (!ok) break;
+            if (!ok) {
+                if (n == 1) over_parts(0.0f);
+                break;
+            }
             fence_after();
             tmem_ld32(tm_dp + 32 * part + my_lane, d);
             wait_ld();
             float ds[32];
+            const int limit = seen - j * kTile - 32 * part;           // places from here on the row does not see, whatever they hold
+            if (n == 1) {
+                float sum = 0.0f;
 #pragma unroll
-            for (int c = 0; c < 32; c += 2) {
-                add2(ds[c], ds[c + 1], __uint_as_float(d[c]), __uint_as_float(d[c + 1]), minus_delta, minus_delta);
-                mul2(ds[c], ds[c + 1], ds[c], ds[c + 1], prob[c], prob[c + 1]);
-            }
-            if (edge) {                                               // places that the row does not see, whatever they hold
-                const int limit = seen - j * kTile - 32 * part;
+                for (int c = 0; c < 32; ++c) {
+                    ds[c] = c < limit ? prob[c] * __uint_as_float(d[c]) : 0.0f;
+                    sum += ds[c];
+                }
+                minus_delta = -over_parts(sum);
 #pragma unroll
-                for (int c = 0; c < 32; ++c) ds[c] = c < limit ? ds[c] : 0.0f;
+                for (int c = 0; c < 32; ++c) ds[c] = c < limit ? fmaf(prob[c], minus_delta, ds[c]) : 0.0f;
+            } else {
+#pragma unroll
+                for (int c = 0; c < 32; c += 2) {
+                    add2(ds[c], ds[c + 1], __uint_as_float(d[c]), __uint_as_float(d[c + 1]), minus_delta, minus_delta);
+                    mul2(ds[c], ds[c + 1], ds[c], ds[c + 1], prob[c], prob[c + 1]);
+                }
+                if (edge) {
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) ds[c] = c < limit ? ds[c] : 0.0f;
+                }
+                float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+                for (int c = 0; c < 32; c += 2) add2(sum[0], sum[1], sum[0], sum[1], ds[c], ds[c + 1]);
+                drift += sum[0] + sum[1];
             }
 #pragma unroll
             for (int c = 0; c < 16; ++c) out[c] = pack2<T>(ds[2 * c], ds[2 * c + 1]);
@@ -657,6 +687,9 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             __syncwarp();
             if (lane == 0) barrier_arrive(bar(qDs));
         }
+        if (n > 1) minus_delta -= over_parts(drift);
+        // (a row past the sequence's end may hold anything: its probabilities are 0, and 0 is what they multiply)
+        if (part < 2) stat_block(p, w, w.head, w.tile)[part * kTile + r] = part == 0 ? minus_lse : live ? minus_delta : 0.0f;
         if (ok) ok = wait(qDone, 0);
         fence_after();
         if (ok) {
