@@ -13,7 +13,7 @@ from .binding import (  # noqa: F401
     fewbit_set_option, fewbit_get_option, fewbit_tail_warp_count,
 )
 from .operators import (  # noqa: F401
-    AdamWTensors, fewbit_adamw_create, fewbit_adamw_step, fewbit_attention_bwd, fewbit_attention_fwd,
+    fewbit_adamw_create, fewbit_adamw_step, fewbit_attention_bwd, fewbit_attention_fwd,
     fewbit_attention_timeout_count, fewbit_qk_norm_rope_bwd, fewbit_qk_norm_rope_fwd,
 )
 from . import workloads  # noqa: F401

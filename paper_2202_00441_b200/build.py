@@ -10,6 +10,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libfewbit.so")
+TORCH_LIB = os.path.join(PKG, "_fewbit_torch.so")
 OBJ_DIR = os.path.join(PKG, "build")
 
 # (source, object stem, extra flags); the forward kernels are instantiated once per activation
@@ -39,6 +40,29 @@ def _stale(target: str, deps) -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def build_torch_module(force: bool = False) -> str:
+    """The extension module that marshals PyTorch tensors (host code only; links libfewbit.so beside it)."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+
+    src, obj = os.path.join(CSRC, "fewbit_torch.cpp"), os.path.join(OBJ_DIR, "fewbit_torch.o")
+    deps = [src, os.path.join(INCLUDE, "fewbit.h")]
+    if force or _stale(obj, deps):
+        includes = [*cpp_extension.include_paths("cuda"), sysconfig.get_paths()["include"], INCLUDE]
+        subprocess.check_call(["g++", "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-DTORCH_EXTENSION_NAME=_fewbit_torch",
+                               "-DTORCH_API_INCLUDE_EXTENSION_H", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                               *[f for i in includes for f in ("-isystem", i)], "-c", src, "-o", obj])
+    if force or _stale(TORCH_LIB, [obj]):
+        tmp = TORCH_LIB + f".{os.getpid()}.tmp"
+        libs = [f for d in cpp_extension.library_paths("cuda") if os.path.isdir(d) for f in ("-L", d)]
+        subprocess.check_call(["g++", "-shared", "-o", tmp, obj, *libs, "-lc10", "-lc10_cuda", "-ltorch", "-ltorch_cpu", "-ltorch_python",
+                               "-L", PKG, "-l:libfewbit.so", "-Wl,-rpath,$ORIGIN"])
+        os.replace(tmp, TORCH_LIB)
+    return TORCH_LIB
+
+
 def build_library(force: bool = False, verbose: bool = False) -> str:
     headers = [os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".h", ".cuh"))]
     headers.append(os.path.join(INCLUDE, "fewbit.h"))
@@ -63,6 +87,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
         tmp = LIB + f".{os.getpid()}.tmp"
         subprocess.check_call([_nvcc(), "-shared", "-o", tmp, *objs])
         os.replace(tmp, LIB)
+    build_torch_module(force)
     return LIB
 
 
