@@ -204,6 +204,7 @@ fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *s, const fewbit
     p.dv = rows_of(grad_v);
     p.lse = const_cast<float *>(lse);
     p.stat = static_cast<float *>(workspace);
+    p.after_dq = s->q_len > 0;
     st = run(attn::Kernel::dq, s, p, (s->q_len + attn::kTile - 1) / attn::kTile, s->heads, stream);
     if (st != FEWBIT_OK) return st;
     // A key tile's row tiles are dealt out to a cluster of 1, 2 or 4 CTAs, whichever should be done first: the longest CTA or

@@ -59,6 +59,7 @@ struct Params {
     int tiles;                        // row or key tiles (of the kernel's size) in q_len or k_len
     int split;                        // CTAs of a cluster that share a key tile (dK, dV)
     bool causal;
+    bool after_dq;                    // dK, dV: launched right behind the dQ kernel, whose start is all that its CTAs have waited for
     float scale, scale_log2;          // scale * log2(e)
 };
 
@@ -483,6 +484,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
     float *row_sum = row_delta + kTile;                               // [4][128]
     const int warp = uniform(static_cast<int>(threadIdx.x >> 5)), lane = threadIdx.x & 31;
     pdl_wait();
+    pdl_launch_dependents();                                          // the dK and dV kernel may set itself up
     const Work w = find_work(p, blockIdx.x, p.heads, true);
     if (w.packed && w.batch == p.batch) {
         fill_outside<T>(p, w, p.q_offsets, p.q_rows, p.dq, nullptr);
@@ -728,7 +730,9 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
     float *stat = reinterpret_cast<float *>(raw + 7 * kBytes);        // [stage][-lse * log2 e, -delta][128]
     Sync *sync = reinterpret_cast<Sync *>(raw + 7 * kBytes + 2 * kStatBytes);
     const int warp = uniform(static_cast<int>(threadIdx.x >> 5)), lane = threadIdx.x & 31;
-    pdl_wait();
+    // Behind the dQ kernel only the statistics are still to come (whatever ran before it has ended, or it would not have
+    // started): they are waited for where they are loaded.  Every CTA waits, so that this grid never ends before that one.
+    if (!p.after_dq) pdl_wait();
     const int rank = p.split > 1 ? static_cast<int>(cluster_rank()) : 0;
     const Work w = find_work(p, blockIdx.x / p.split, p.kv_heads, false);
     if (w.packed && w.batch == p.batch) {                             // (the whole cluster)
@@ -736,10 +740,14 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             fill_outside<T>(p, w, p.k_offsets, p.k_rows, p.dk, nullptr);
             fill_outside<T>(p, w, p.k_offsets, p.k_rows, p.dv, nullptr);
         }
+        pdl_wait();
         return;
     }
     const int k0 = w.tile * kTile;
-    if (k0 >= w.k_len) return;
+    if (k0 >= w.k_len) {
+        pdl_wait();
+        return;
+    }
     // row tiles [first, last) see a key of this tile; all query heads of the group, one after the other, dealt out to the
     // cluster's CTAs in turn
     const int reach = w.k_len - w.q_len;                              // row i sees keys up to i + reach
@@ -780,6 +788,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                 barrier_expect(bar(kV), kBytes);
                 load_halves<HALVES>(sm_v, &p.v, w.k_first + k0, w.head, w.q_batch, bar(kV));
             }
+            if (n == 0) pdl_wait();
             for (int j = 0; j < n; ++j) {
                 const int s = j & 1, s3 = j % 3, at = rank + j * p.split;
                 const int head = w.head * p.group + at / each, tile = first + at % each, q0 = tile * kTile;
@@ -790,6 +799,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                     load_halves<HALVES>(sm_q + s3 * kBytes, &p.q, w.q_first + q0, head, w.q_batch, bar(kQFull + s3));
                 }
                 issued_q = j + 1;
+                if (j == 0) pdl_wait();
                 if (!wait(kTEmpty + s, again)) break;
                 if (lane == 0) {
                     barrier_expect(bar(kTFull + s), kStatBytes);
