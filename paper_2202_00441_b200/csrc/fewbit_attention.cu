@@ -126,7 +126,38 @@ fewbit_status fill(const fewbit_attention_shape *s, const Sizes &z, Params *p) {
         if (dev < 64) cached[dev].store(at, std::memory_order_release);
     }
     p->timeouts = at;
-    return FEWBIT_OK;
+    p->sms = device_sm_count(&err);
+    return cuda_status(err);
+}
+
+// The CTAs of a cluster that share one tile: 1, 2, 4 or 8, whichever should be done first, by the longest CTA or by the SMs'
+// share of all work, counted in tiles of the long axis (`longest` of them for each of `tiles`; causal sequences have half
+// the work, and the same longest CTA).  A CTA's start and end cost as much as ends.alone tiles, with a cluster's sums
+// ends.joined.
+struct Ends { int alone, joined; };
+// dK, dV: 11000 and 20000 clocks against 2850 for a tile; the others have shorter ends and longer tiles by their chain of one
+// tile after another.  Measured, in us.  Backward pass with dK's and dV's clusters of 1 / 2 / 4: 4 x 2048 rows of 16 heads on 4
+// key heads, causal, 275 / 292 / 330; one of 16384 rows, 8 heads on 2, 1663 / 1608 / 1695.  Forward and backward pass with
+// one CTA for a row tile against the clusters chosen here: one row on 8192 keys, 8 heads on 2, 92.7 and 85.7 against 25.7 and
+// 35.4; 64 rows on 9000 keys, 4 heads, 102.9 and 99.0 against 27.3 and 41.2; 1024 rows, causal, 20.7 and 37.5 against 16.3 and
+// 35.1; 4096 rows, causal, 59.9 and 120 against 47.7 and 119; 2 x 2048 rows stay with one: 35.0, with two 36.2.
+constexpr Ends kDkvEnds = {4, 7};
+constexpr Ends kDqEnds = {6, 9};
+constexpr Ends kForwardEnds = {3, 7};
+
+int choose_split(int64_t sms, int64_t tiles, int64_t longest, bool causal, int most, Ends ends) {
+    int64_t best = INT64_MAX;
+    int choice = 1;
+    for (int split = 1; split <= most && (split == 1 || split <= longest); split *= 2) {
+        const int64_t each = split == 1 ? ends.alone : ends.joined;
+        const int64_t alone = (longest + split - 1) / split + each, shared = (tiles * longest / (causal ? 2 : 1) + tiles * split * each) / sms;
+        const int64_t cost = alone > shared ? alone : shared;
+        if (cost < best) {
+            best = cost;
+            choice = split;
+        }
+    }
+    return choice;
 }
 
 fewbit_status run(attn::Kernel which, const fewbit_attention_shape *s, Params &p, int64_t tiles, int heads, void *stream) {
@@ -163,7 +194,9 @@ fewbit_status fewbit_attention_fwd(const fewbit_attention_shape *s, const fewbit
     if (st != FEWBIT_OK) return st;
     p.out = rows_of(out);
     p.lse = lse;
-    return run(attn::Kernel::forward, s, p, (s->q_len + 2 * attn::kTile - 1) / (2 * attn::kTile), s->heads, stream);
+    const int64_t row_tiles = (s->q_len + 2 * attn::kTile - 1) / (2 * attn::kTile), key_tiles = (s->k_len + attn::kTile - 1) / attn::kTile;
+    p.split = choose_split(p.sms, row_tiles * s->heads * s->batch, key_tiles, p.causal, s->head_dim > 64 ? 8 : 4, kForwardEnds);
+    return run(attn::Kernel::forward, s, p, row_tiles, s->heads, stream);
 }
 
 size_t fewbit_attention_workspace_bytes(const fewbit_attention_shape *s) {
@@ -205,27 +238,11 @@ fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *s, const fewbit
     p.lse = const_cast<float *>(lse);
     p.stat = static_cast<float *>(workspace);
     p.after_dq = s->q_len > 0;
-    st = run(attn::Kernel::dq, s, p, (s->q_len + attn::kTile - 1) / attn::kTile, s->heads, stream);
+    const int64_t row_tiles = (s->q_len + attn::kTile - 1) / attn::kTile, key_tiles = (s->k_len + attn::kTile - 1) / attn::kTile;
+    p.split = choose_split(p.sms, row_tiles * s->heads * s->batch, key_tiles, p.causal, s->head_dim > 64 ? 8 : 4, kDqEnds);
+    st = run(attn::Kernel::dq, s, p, row_tiles, s->heads, stream);
     if (st != FEWBIT_OK) return st;
-    // A key tile's row tiles are dealt out to a cluster of 1, 2 or 4 CTAs, whichever should be done first: the longest CTA or
-    // the SMs' share of all work, counted in row tiles.  A CTA's start and end cost as much as 4 of them (11000 clocks against
-    // 2850), with a cluster's sums 7.  Causal sequences have half the work of full ones, and the same longest CTA.  Measured,
-    // backward pass in us with 1 / 2 CTAs: 4 x 2048 rows of 16 heads on 4 key heads, causal, 275 / 292 (4 CTAs: 330); one of 16384
-    // rows, 8 heads on 2: 1663 / 1608 (1695).
-    cudaError_t err = cudaSuccess;
-    const int64_t sms = device_sm_count(&err), key_tiles = (s->k_len + attn::kTile - 1) / attn::kTile;
-    if (err != cudaSuccess) return cuda_status(err);
-    const int64_t longest = (s->q_len + attn::kTile - 1) / attn::kTile * p.group, tiles = key_tiles * s->kv_heads * s->batch;
-    int64_t best = INT64_MAX;
-    for (int split = 1; split <= 4; split *= 2) {
-        const int64_t ends = split == 1 ? 4 : 7;
-        const int64_t alone = (longest + split - 1) / split + ends, shared = (tiles * longest / (p.causal ? 2 : 1) + tiles * split * ends) / sms;
-        const int64_t cost = alone > shared ? alone : shared;
-        if (cost < best) {
-            best = cost;
-            p.split = split;
-        }
-    }
+    p.split = choose_split(p.sms, key_tiles * s->kv_heads * s->batch, row_tiles * p.group, p.causal, 4, kDkvEnds);
     return run(attn::Kernel::dkv, s, p, key_tiles, s->kv_heads, stream);
 }
 

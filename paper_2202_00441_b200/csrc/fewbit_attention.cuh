@@ -12,8 +12,9 @@
 //
 //   forward   two row tiles a CTA: one tile's softmax runs while the other's products do
 //   dQ        one row tile against all keys: S, dP, dQ (3 products); writes the rows' -lse and -delta for the next kernel
-//   dK, dV    one key tile against all rows of all query heads that share it: S^T, dP^T, dV, dK (4 products); a
-//             cluster of 1, 2 or 4 CTAs takes the row tiles in turn and adds up through distributed shared memory
+//   dK, dV    one key tile against all rows of all query heads that share it: S^T, dP^T, dV, dK (4 products)
+// Where there are few tiles, a cluster of CTAs shares each of them: the tiles of the long axis are dealt out in turn, and
+// the sums are joined through distributed shared memory, in a fixed order.
 // S and dP are computed in both backward kernels (7 products where 5 would do): in exchange nothing is added
 // with atomics, so no binary32 copy of dQ is zeroed, summed and converted, and results are the same every time.
 //
@@ -57,7 +58,8 @@ struct Params {
     int batch, heads, kv_heads, group, dim;
     int q_len, k_len;                 // of every sequence, or the most of any
     int tiles;                        // row or key tiles (of the kernel's size) in q_len or k_len
-    int split;                        // CTAs of a cluster that share a key tile (dK, dV)
+    int split;                        // CTAs of a cluster that share a row tile's keys, or a key tile's rows (dK, dV)
+    int sms;                          // (the host's)
     bool causal;
     bool after_dq;                    // dK, dV: launched right behind the dQ kernel, whose start is all that its CTAs have waited for
     float scale, scale_log2;          // scale * log2(e)
@@ -106,6 +108,9 @@ __device__ __forceinline__ int key_tiles(const Params &p, const Work &w, int las
     if (p.causal) keys = min(keys, max(0, last + 1 + w.k_len - w.q_len));
     return (keys + kTile - 1) / kTile;
 }
+
+// How many of n tiles fall to CTA `rank` of `split` that take them in turn.
+__device__ __forceinline__ int share_of(int n, int rank, int split) { return (n - rank + split - 1) / split; }
 
 // Shared memory: tiles first (1 KB aligned), then the barriers.
 struct Sync {
@@ -211,7 +216,7 @@ __device__ __forceinline__ void end_cta(uint32_t tmem) {
 // ready (2), all of it (2), O done (2), drained.
 enum { fQ = 0, fKFull = 2, fKEmpty = 4, fVFull = 6, fVEmpty = 8, fS = 10, fP = 12, fPEnd = 14, fO = 16, fDrain = 18, fBars = 19 };
 
-template <int DIM> constexpr int fwd_smem() { return 6 * (DIM / 64) * static_cast<int>(kHalfTile) + 1024 + static_cast<int>(sizeof(Sync)) + 4 * kTile * 4; }
+template <int DIM> constexpr int fwd_smem() { return 6 * (DIM / 64) * static_cast<int>(kHalfTile) + 1024 + static_cast<int>(sizeof(Sync)) + 8 * kTile * 4; }
 
 // Barriers of two warps.
 __device__ __forceinline__ void pair_barrier(int id) { asm volatile("bar.sync %0, 64;" :: "r"(id) : "memory"); }
@@ -246,19 +251,23 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
     const uint32_t base = (smem_address(raw) + 1023u) & ~1023u;
     Sync *sync = reinterpret_cast<Sync *>(raw + (base - smem_address(raw)) + 6 * kBytes);
     float *exchange = reinterpret_cast<float *>(sync + 1);            // [row tile][half][128]
+    float *joined = exchange + 4 * kTile;                             // [row tile][reference, sum][128], for the cluster
     const int warp = uniform(static_cast<int>(threadIdx.x >> 5)), lane = threadIdx.x & 31;
     pdl_wait();
-    const Work w = find_work(p, blockIdx.x, p.heads, true);
-    if (w.packed && w.batch == p.batch) {
-        fill_outside<T>(p, w, p.q_offsets, p.q_rows, p.out, p.lse);
+    const int rank = p.split > 1 ? static_cast<int>(cluster_rank()) : 0;
+    const Work w = find_work(p, blockIdx.x / p.split, p.heads, true);
+    if (w.packed && w.batch == p.batch) {                             // (the whole cluster)
+        if (rank == 0) fill_outside<T>(p, w, p.q_offsets, p.q_rows, p.out, p.lse);
         return;
     }
     const int q0 = w.tile * 2 * kTile;
     if (q0 >= w.q_len) return;                                        // packed: a shorter sequence
     const int kv_head = w.head / p.group;
     // key tiles of each row tile (0 also for a row tile past the end)
-    const int n0 = uniform(key_tiles(p, w, min(q0 + kTile, w.q_len) - 1));
-    const int n1 = uniform(q0 + kTile < w.q_len ? key_tiles(p, w, min(q0 + 2 * kTile, w.q_len) - 1) : 0);
+    // that fall to this CTA: number rank, rank + split, ...
+    const int n0 = uniform(share_of(key_tiles(p, w, min(q0 + kTile, w.q_len) - 1), rank, p.split));
+    const int n1 = uniform(share_of(q0 + kTile < w.q_len ? key_tiles(p, w, min(q0 + 2 * kTile, w.q_len) - 1) : 0, rank, p.split));
+    auto key_tile = [&](int j) { return rank + j * p.split; };
     const int n = max(n0, n1);
 
     constexpr uint32_t counts[fBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 8, 8, 8, 8, 1, 1, 1};
@@ -290,13 +299,13 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
                 if (!wait(fKEmpty + s, again)) break;
                 if (lane == 0) {
                     barrier_expect(bar(fKFull + s), kBytes);
-                    load_halves<HALVES>(sm_k + s * kBytes, &p.k, w.k_first + j * kTile, kv_head, w.q_batch, bar(fKFull + s));
+                    load_halves<HALVES>(sm_k + s * kBytes, &p.k, w.k_first + key_tile(j) * kTile, kv_head, w.q_batch, bar(fKFull + s));
                 }
                 issued_k = j + 1;
                 if (!wait(fVEmpty + s, again)) break;
                 if (lane == 0) {
                     barrier_expect(bar(fVFull + s), kBytes);
-                    load_halves<HALVES>(sm_v + s * kBytes, &p.v, w.k_first + j * kTile, kv_head, w.q_batch, bar(fVFull + s));
+                    load_halves<HALVES>(sm_v + s * kBytes, &p.v, w.k_first + key_tile(j) * kTile, kv_head, w.q_batch, bar(fVFull + s));
                 }
                 issued_v = j + 1;
             }
@@ -324,7 +333,7 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
             for (int j = 0; ok && j < n; ++j) {
                 ok = wait(fVFull + (j & 1), (j >> 1) & 1) && (j + 1 >= n || wait(fKFull + ((j + 1) & 1), ((j + 1) >> 1) & 1));
                 if (!ok) break;
-                if (w.packed && (j + 1) * kTile > w.k_len) clear_rows<HALVES>(sm_v + (j & 1) * kBytes, w.k_len - j * kTile);
+                if (w.packed && (key_tile(j) + 1) * kTile > w.k_len) clear_rows<HALVES>(sm_v + (j & 1) * kBytes, w.k_len - key_tile(j) * kTile);
                 for (int t = 0; t < 2 && ok; ++t) {
                     const int nt = t ? n1 : n0;
                     if (j >= nt) continue;
@@ -347,6 +356,10 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
             commit(leader, bar(fDrain));
             barrier_wait(bar(fDrain), 0, nullptr, p.timeouts);
         }
+        if (p.split > 1) {                                            // the element-wise warps' two barriers, below
+            cluster_sync();
+            cluster_sync();
+        }
     } else {
         take_registers<kFwdWork>();
         const int t = warp >> 3, half = (warp >> 2) & 1;              // row tile; columns [64 half, 64 half + 64) of every key tile
@@ -364,14 +377,14 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
         for (int j = 0; j < nt; ++j) {
             ok = wait(fS + t, j & 1);                                 // (a wait given up ends the loop below, for all threads of the tile)
             fence_after();
-            const bool edge = (j + 1) * kTile > tile_seen;
-            const int limit = seen - j * kTile - 64 * half;
+            const bool edge = (key_tile(j) + 1) * kTile > tile_seen;
+            const int limit = seen - key_tile(j) * kTile - 64 * half;
             // Scores are read twice, 32 columns at a time, for the maximum and for the probabilities: reading them costs less
             // than holding 64 of them in registers.
             uint32_t s[32];
             auto read = [&](int c) {
                 tmem_ld32(s_at + 32 * c, s);
-                wait_ld();
+                wait_ld(s);
                 if (edge) {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) s[e] = 32 * c + e < limit ? s[e] : 0xff800000u;
@@ -416,7 +429,7 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
                     for (int c = 0; c < DIM / 64; ++c) {
                         uint32_t o[32];
                         tmem_ld32(o_at + 32 * c, o);
-                        wait_ld();
+                        wait_ld(o);
 #pragma unroll
                         for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * factor);
                         tmem_st32(o_at + 32 * c, o);
@@ -442,22 +455,68 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
         *mine = sum;                                                  // (the last exchange of maxima was read before P was ready)
         pair_barrier(pair);
         sum += *other;
-        if (ok) {
-            const bool live = i < w.q_len;
-            T *row = static_cast<T *>(p.out.p) + (live ? row_of(w, p.out, w.head, i, w.q_first) : 0);
-            if (nt > 0) {
-                const float factor = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+        const bool live = i < w.q_len;
+        T *row = static_cast<T *>(p.out.p) + (live ? row_of(w, p.out, w.head, i, w.q_first) : 0);
+        if (p.split == 1) {
+            if (ok) {
+                if (nt > 0) {
+                    const float factor = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
 #pragma unroll
-                for (int c = 0; c < DIM / 64; ++c) {
-                    uint32_t o[32];
-                    tmem_ld32(o_at + 32 * c, o);
-                    wait_ld();
-                    if (live) store_columns<T, 32>(row, half * (DIM / 2) + 32 * c, p.dim, o, factor);
+                    for (int c = 0; c < DIM / 64; ++c) {
+                        uint32_t o[32];
+                        tmem_ld32(o_at + 32 * c, o);
+                        wait_ld(o);
+                        if (live) store_columns<T, 32>(row, half * (DIM / 2) + 32 * c, p.dim, o, factor);
+                    }
+                } else if (live && half == 0) {
+                    zero_columns<T>(row, p.dim);
                 }
-            } else if (live && half == 0) {
-                zero_columns<T>(row, p.dim);
+                if (live && half == 0) p.lse[stat_of(p, w, w.head, i)] = sum == 0.0f ? -INFINITY : top * p.scale + logf(sum);
             }
-            if (live && half == 0) p.lse[stat_of(p, w, w.head, i)] = sum == 0.0f ? -INFINITY : top * p.scale + logf(sum);
+        } else {
+            // Every CTA lays its O, reference and sum of each row out in shared memory, [row tile][column][row]; a share of the
+            // columns is brought to the largest reference, added up and divided by each.
+            // (The tiles that this overwrites are the other row tile's too, which may see more keys: all its products first.)
+            asm volatile("bar.sync 9, %0;" :: "n"(kWorkThreads) : "memory");
+            const uint32_t mine_o = base + static_cast<uint32_t>(t * DIM) * (kTile * 4) + r * 4;
+            const uint32_t mine_stat = smem_address(joined + 2 * t * kTile + r);
+#pragma unroll
+            for (int c = 0; c < DIM / 64; ++c) {
+                uint32_t o[32];
+                tmem_ld32(o_at + 32 * c, o);                          // (what it holds does not matter where there was no key tile)
+                wait_ld(o);
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    asm volatile("st.shared.u32 [%0], %1;" :: "r"(mine_o + (half * (DIM / 2) + 32 * c + e) * (kTile * 4)), "r"(nt > 0 ? o[e] : 0u) : "memory");
+            }
+            if (half == 0) {
+                joined[2 * t * kTile + r] = top;
+                joined[(2 * t + 1) * kTile + r] = sum;
+            }
+            cluster_sync();
+            float high = -INFINITY, total = 0.0f;
+            for (int k = 0; k < p.split; ++k) high = fmaxf(high, load_peer(mine_stat, k));
+            const float reference = high == -INFINITY ? 0.0f : high * p.scale_log2;
+            for (int k = 0; k < p.split; ++k) total += exp2_fast(load_peer(mine_stat, k) * p.scale_log2 - reference) * load_peer(mine_stat + kTile * 4, k);
+            const float factor = total > 0.0f || total != total ? 1.0f / total : 0.0f;
+            const int share = DIM / p.split;                          // a multiple of 16
+            for (int col = rank * share + half * (share / 2); col < rank * share + (half + 1) * (share / 2); col += 8) {
+                float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+                for (int k = 0; k < p.split; ++k) {
+                    const float weight = exp2_fast(load_peer(mine_stat, k) * p.scale_log2 - reference);
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = load_peer(mine_o + (col + e) * (kTile * 4), k);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = fmaf(weight, x[e], v[e]);
+                }
+                uint32_t o[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(v[e]);
+                if (live) store_columns<T, 8>(row, col, p.dim, o, factor);
+            }
+            if (live && half == 0 && rank == 0) p.lse[stat_of(p, w, w.head, i)] = total == 0.0f ? -INFINITY : high * p.scale + logf(total);
+            cluster_sync();                                           // nobody's shared memory goes before it has been read
         }
     }
     end_cta(tmem);
@@ -485,15 +544,19 @@ attention_dq_kernel(const __grid_constant__ Params p) {
     const int warp = uniform(static_cast<int>(threadIdx.x >> 5)), lane = threadIdx.x & 31;
     pdl_wait();
     pdl_launch_dependents();                                          // the dK and dV kernel may set itself up
-    const Work w = find_work(p, blockIdx.x, p.heads, true);
-    if (w.packed && w.batch == p.batch) {
-        fill_outside<T>(p, w, p.q_offsets, p.q_rows, p.dq, nullptr);
+    const int rank = p.split > 1 ? static_cast<int>(cluster_rank()) : 0;
+    const Work w = find_work(p, blockIdx.x / p.split, p.heads, true);
+    if (w.packed && w.batch == p.batch) {                             // (the whole cluster)
+        if (rank == 0) fill_outside<T>(p, w, p.q_offsets, p.q_rows, p.dq, nullptr);
         return;
     }
     const int q0 = w.tile * kTile;
     if (q0 >= w.q_len) return;
     const int kv_head = w.head / p.group;
-    const int n = uniform(key_tiles(p, w, min(q0 + kTile, w.q_len) - 1));
+    // key tiles that the rows see, and how many of them fall to this CTA: number rank, rank + split, ...
+    const int n_all = uniform(key_tiles(p, w, min(q0 + kTile, w.q_len) - 1));
+    const int n = share_of(n_all, rank, p.split);
+    auto key_tile = [&](int j) { return rank + j * p.split; };
 
     // The outputs that delta needs, read while the CTA sets itself up: DIM / 8 lanes a row, 8 rows for each warp.  (From here on
     // the L2's bandwidth is the tiles' that are on their way.)
@@ -502,7 +565,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
     float lse = -INFINITY;
     if (warp < kMmaWarp) {
 #pragma unroll
-        for (int x = 0; n > 1 && x < 8 / kRows; ++x) {
+        for (int x = 0; n > 0 && n_all > 1 && x < 8 / kRows; ++x) {
             const int row = q0 + 8 * warp + kRows * x + lane / kLanes, col = lane % kLanes * 8;
             const bool there = row < w.q_len && col < p.dim;
             const T *from = static_cast<const T *>(p.o.p) + row_of(w, p.o, w.head, there ? row : 0, w.q_first) + (there ? col : 0);
@@ -538,13 +601,13 @@ attention_dq_kernel(const __grid_constant__ Params p) {
                 if (!wait(qKEmpty + s3, ((j / 3) & 1) ^ 1)) break;
                 if (lane == 0) {
                     barrier_expect(bar(qKFull + s3), kBytes);
-                    load_halves<HALVES>(sm_k + s3 * kBytes, &p.k, w.k_first + j * kTile, kv_head, w.q_batch, bar(qKFull + s3));
+                    load_halves<HALVES>(sm_k + s3 * kBytes, &p.k, w.k_first + key_tile(j) * kTile, kv_head, w.q_batch, bar(qKFull + s3));
                 }
                 issued_k = j + 1;
                 if (!wait(qVEmpty + s, ((j >> 1) & 1) ^ 1)) break;
                 if (lane == 0) {
                     barrier_expect(bar(qVFull + s), kBytes);
-                    load_halves<HALVES>(sm_v + s * kBytes, &p.v, w.k_first + j * kTile, kv_head, w.q_batch, bar(qVFull + s));
+                    load_halves<HALVES>(sm_v + s * kBytes, &p.v, w.k_first + key_tile(j) * kTile, kv_head, w.q_batch, bar(qVFull + s));
                 }
                 issued_v = j + 1;
             }
@@ -560,7 +623,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             // K tile j is used by S_j and, transposed, by dQ_j; V tile j by dP_j
             auto scores = [&](int j) {
                 if (!wait(qKFull + j % 3, (j / 3) & 1)) return false;
-                if (w.packed && (j + 1) * kTile > w.k_len) clear_rows<HALVES>(sm_k + (j % 3) * kBytes, w.k_len - j * kTile);
+                if (w.packed && (key_tile(j) + 1) * kTile > w.k_len) clear_rows<HALVES>(sm_k + (j % 3) * kBytes, w.k_len - key_tile(j) * kTile);
                 product_rows<T, DIM>(leader, tm_s + (j & 1) * kTile, sm_q, sm_k + (j % 3) * kBytes);
                 commit(leader, bar(qS + (j & 1)));
                 return true;
@@ -586,6 +649,10 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             commit(leader, bar(qDone));
             barrier_wait(bar(qDone), 0, nullptr, p.timeouts);
         }
+        if (p.split > 1) {                                            // the element-wise warps' two barriers, below
+            cluster_sync();
+            cluster_sync();
+        }
     } else {
         take_registers<kDqWork>();
         const int part = warp >> 2;                                   // columns [32 part, 32 part + 32) of every tile
@@ -594,14 +661,15 @@ attention_dq_kernel(const __grid_constant__ Params p) {
         const uint32_t my_lane = static_cast<uint32_t>(warp & 3) << 21;
         const float minus_lse = lse == -INFINITY ? -INFINITY : -lse * kLog2e;   // a row that sees nothing: every probability is 0
         // delta from the rounded outputs is off by their rounding.  Rows that see few keys feel that most, and those of one key
-        // tile (n = 1) need no outputs: their delta is the sum of P dP, which is all there before dS is computed.  Longer rows
+        // tile (`single`) need no outputs: their delta is the sum of P dP, which is all there before dS is computed.  Longer rows
         // know at the end how far theirs was off, by the sum of dS, which should be 0: dK gets the corrected value.
-        bool ok = n <= 1 || wait(qQ, 0);
+        const bool single = n_all == 1;
+        bool ok = n == 0 || single || wait(qQ, 0);
 #pragma unroll
         for (int x = 0; x < 8 / kRows; ++x) {
             const int row = 8 * warp + kRows * x + lane / kLanes;
             float sum = 0.0f;
-            if (n > 1 && q0 + row < w.q_len) {
+            if (n > 0 && !single && q0 + row < w.q_len) {
                 const uint4 g = tile_chunk(sm_g, row, lane % kLanes);
                 T a[8], b[8];
                 memcpy(a, &outputs[x], 16);
@@ -626,15 +694,15 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             const uint32_t s_at = tm_s + (j & 1) * kTile + 32 * part + my_lane;
             ok = wait(qS + (j & 1), (j >> 1) & 1);
             if (!ok) {
-                if (n == 1) over_parts(0.0f);                         // the others wait there
+                if (single) over_parts(0.0f);                         // the others wait there
                 break;
             }
             fence_after();
             uint32_t s[32], d[32], out[16];
             float prob[32];
             tmem_ld32(s_at, s);
-            wait_ld();
-            const bool edge = (j + 1) * kTile > tile_seen;
+            wait_ld(s);
+            const bool edge = (key_tile(j) + 1) * kTile > tile_seen;
             if (edge) {
 #pragma unroll
                 for (int c = 0; c < 32; c += 2)
@@ -648,15 +716,15 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             }
             ok = wait(qDp, j & 1);
             if (!ok) {
-                if (n == 1) over_parts(0.0f);
+                if (single) over_parts(0.0f);
                 break;
             }
             fence_after();
             tmem_ld32(tm_dp + 32 * part + my_lane, d);
-            wait_ld();
+            wait_ld(d);
             float ds[32];
-            const int limit = seen - j * kTile - 32 * part;           // places from here on the row does not see, whatever they hold
-            if (n == 1) {
+            const int limit = seen - key_tile(j) * kTile - 32 * part;           // places from here on the row does not see, whatever they hold
+            if (single) {
                 float sum = 0.0f;
 #pragma unroll
                 for (int c = 0; c < 32; ++c) {
@@ -689,22 +757,61 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             __syncwarp();
             if (lane == 0) barrier_arrive(bar(qDs));
         }
-        if (n > 1) minus_delta -= over_parts(drift);
-        // (a row past the sequence's end may hold anything: its probabilities are 0, and 0 is what they multiply)
-        if (part < 2) stat_block(p, w, w.head, w.tile)[part * kTile + r] = part == 0 ? minus_lse : live ? minus_delta : 0.0f;
+        const float row_drift = single ? 0.0f : over_parts(drift);
         if (ok) ok = wait(qDone, 0);
         fence_after();
-        if (ok) {
-            T *row = static_cast<T *>(p.dq.p) + (live ? row_of(w, p.dq, w.head, i, w.q_first) : 0);
-            if (n > 0) {
-                uint32_t o[DIM / 4];
-                if constexpr (DIM == 128) tmem_ld32(tm_dq + my_lane + 32 * part, o);
-                else tmem_ld16(tm_dq + my_lane + 16 * part, o);
-                wait_ld();
-                if (live) store_columns<T, DIM / 4>(row, part * (DIM / 4), p.dim, o, p.scale);
-            } else if (live && part == 0) {
-                zero_columns<T>(row, p.dim);
+        T *row = static_cast<T *>(p.dq.p) + (live ? row_of(w, p.dq, w.head, i, w.q_first) : 0);
+        // (a row past the sequence's end may hold anything: its probabilities are 0, and 0 is what they multiply)
+        auto write_stat = [&](float off) {
+            if (part < 2) stat_block(p, w, w.head, w.tile)[part * kTile + r] = part == 0 ? minus_lse : live ? minus_delta - off : 0.0f;
+        };
+        if (p.split == 1) {
+            write_stat(row_drift);
+            if (ok) {
+                if (n > 0) {
+                    uint32_t o[DIM / 4];
+                    if constexpr (DIM == 128) tmem_ld32(tm_dq + my_lane + 32 * part, o);
+                    else tmem_ld16(tm_dq + my_lane + 16 * part, o);
+                    wait_ld(o);
+                    if (live) store_columns<T, DIM / 4>(row, part * (DIM / 4), p.dim, o, p.scale);
+                } else if (live && part == 0) {
+                    zero_columns<T>(row, p.dim);
+                }
             }
+        } else {
+            // Every CTA lays its sums out in shared memory, [column][row] and the rows' drift; a share of the columns is added up
+            // by each.  The first CTA, which has the first key tile, knows the row's delta.
+            const uint32_t mine = base + r * 4, mine_drift = smem_address(row_delta + r);
+            uint32_t o[DIM / 4];
+            if constexpr (DIM == 128) tmem_ld32(tm_dq + my_lane + 32 * part, o);
+            else tmem_ld16(tm_dq + my_lane + 16 * part, o);           // (what it holds does not matter where there was no key tile)
+            wait_ld(o);
+#pragma unroll
+            for (int e = 0; e < DIM / 4; ++e)
+                asm volatile("st.shared.u32 [%0], %1;" :: "r"(mine + (part * (DIM / 4) + e) * (kTile * 4)), "r"(n > 0 ? o[e] : 0u) : "memory");
+            if (part == 0) row_delta[r] = n > 0 ? row_drift : 0.0f;
+            cluster_sync();
+            if (rank == 0) {
+                float off = 0.0f;
+                for (int k = 0; k < p.split; ++k) off += load_peer(mine_drift, k);
+                write_stat(off);
+            }
+            const int share = DIM / p.split, each = share / 4 > 8 ? share / 4 : 8;   // columns of this CTA, and of a thread
+            for (int col = rank * share + part * each; col < rank * share + min((part + 1) * each, share); col += 8) {
+                float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+                for (int k = 0; k < p.split; ++k) {
+                    float x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = load_peer(mine + (col + e) * (kTile * 4), k);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] += x[e];
+                }
+                uint32_t y[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = __float_as_uint(v[e]);
+                if (live) store_columns<T, 8>(row, col, p.dim, y, p.scale);
+            }
+            cluster_sync();                                           // nobody's shared memory goes before it has been read
         }
     }
     end_cta(tmem);
@@ -753,7 +860,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
     const int reach = w.k_len - w.q_len;                              // row i sees keys up to i + reach
     const int first = p.causal ? max(0, k0 - reach) / kTile : 0;
     const int each = max(0, (w.q_len + kTile - 1) / kTile - first);
-    const int n = uniform((each * p.group - rank + p.split - 1) / p.split);
+    const int n = uniform(share_of(each * p.group, rank, p.split));
 
     // a quarter of a row of the K tile for each thread, read while the CTA sets itself up
     uint32_t keys[DIM / 8];
@@ -911,7 +1018,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             float prob[32];
             tmem_ld_16x32(tm_s + 32 * part + my_lane, s);
             tmem_ld_16x32(tm_s + 32 * part + my_lane + (16u << 16), s + 16);
-            wait_ld();
+            wait_ld(s);
             fence_before();
             __syncwarp();
             if (lane == 0) barrier_arrive(bar(kSRead));
@@ -959,7 +1066,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             for (int h = 0; h < 2; ++h) {                             // 16 keys at a time
                 uint32_t d[16];
                 tmem_ld_16x32(tm_dp + 32 * part + my_lane + (static_cast<uint32_t>(16 * h) << 16), d);
-                wait_ld();
+                wait_ld(d);
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     const float2 e = d2[4 * c];
@@ -1006,7 +1113,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                         uint32_t o[32];
                         const int col = half * (DIM / 2) + 32 * c;
                         tmem_ld32(from + col, o);
-                        wait_ld();
+                        wait_ld(o);
                         if (live) store_columns<T, 32>(row, col, p.dim, o, factor);
                     }
                 } else if (live && half == 0) {
@@ -1024,7 +1131,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                 const int col = half * (DIM / 2) + 32 * c;
                 if (share >= 32 && col / share == rank) continue;
                 tmem_ld32(from + col, o);                             // (what it holds does not matter where there was no row tile)
-                wait_ld();
+                wait_ld(o);
 #pragma unroll
                 for (int e = 0; e < 32; ++e)
                     asm volatile("st.shared.u32 [%0], %1;" :: "r"(mine + (col + e) * (kTile * 4)), "r"(n > 0 ? o[e] : 0u) : "memory");
@@ -1037,7 +1144,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                 if constexpr (N == 32) tmem_ld32(from + col, o);
                 else if constexpr (N == 16) tmem_ld16(from + col, o);
                 else tmem_ld8(from + col, o);
-                wait_ld();
+                wait_ld(o);
                 for (int k = 1; k < p.split; ++k) {
                     const uint32_t peer = static_cast<uint32_t>((rank + k) % p.split);
                     float v[N];

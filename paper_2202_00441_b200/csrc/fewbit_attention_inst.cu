@@ -58,9 +58,9 @@ cudaError_t launch_bf16(
     Kernel which, bool wide, const Params &p, unsigned grid, cudaStream_t st) {
     switch (which) {
     case Kernel::forward:
-        return wide ? launch<attention_fwd_kernel<T, 128>, fwd_smem<128>()>(p, grid, 1, st) : launch<attention_fwd_kernel<T, 64>, fwd_smem<64>()>(p, grid, 1, st);
+        return wide ? launch<attention_fwd_kernel<T, 128>, fwd_smem<128>()>(p, grid * p.split, p.split, st) : launch<attention_fwd_kernel<T, 64>, fwd_smem<64>()>(p, grid * p.split, p.split, st);
     case Kernel::dq:
-        return wide ? launch<attention_dq_kernel<T, 128>, dq_smem<128>()>(p, grid, 1, st) : launch<attention_dq_kernel<T, 64>, dq_smem<64>()>(p, grid, 1, st);
+        return wide ? launch<attention_dq_kernel<T, 128>, dq_smem<128>()>(p, grid * p.split, p.split, st) : launch<attention_dq_kernel<T, 64>, dq_smem<64>()>(p, grid * p.split, p.split, st);
     default:
         return wide ? launch<attention_dkv_kernel<T, 128>, dkv_smem<128>()>(p, grid * p.split, p.split, st) : launch<attention_dkv_kernel<T, 64>, dkv_smem<64>()>(p, grid * p.split, p.split, st);
     }

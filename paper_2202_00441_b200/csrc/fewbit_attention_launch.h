@@ -6,7 +6,7 @@ namespace fewbit {
 namespace attn {
 struct Params;
 enum class Kernel { forward, dq, dkv };
-// wide: head_dim above 64; grid: CTAs, or clusters of p.split CTAs for dkv
+// wide: head_dim above 64; grid: clusters of p.split CTAs
 cudaError_t launch_bf16(Kernel which, bool wide, const Params &p, unsigned grid, cudaStream_t st);
 cudaError_t launch_f16(Kernel which, bool wide, const Params &p, unsigned grid, cudaStream_t st);
 }  // namespace attn

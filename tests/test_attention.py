@@ -102,6 +102,11 @@ CASES = [
     (1, 384, 2100, 8, 2, 64, True, torch.bfloat16, "padded"),
     (1, 2100, 256, 2, 1, 80, False, torch.bfloat16, "plain"),
     (5, 64, 64, 2, 1, 120, True, torch.bfloat16, "plain"),
+    (1, 1, 5000, 4, 2, 128, True, torch.bfloat16, "plain"),       # few rows, many keys: CTAs share them
+    (2, 3, 2049, 2, 1, 64, False, torch.float16, "heads_first"),
+    (1, 130, 3333, 1, 1, 96, True, torch.bfloat16, "plain"),
+    (1, 1500, 1500, 2, 1, 128, True, torch.float16, "fused"),
+    (1, 3000, 70, 3, 3, 64, False, torch.bfloat16, "plain"),
 ]
 
 
