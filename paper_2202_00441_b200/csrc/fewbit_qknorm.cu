@@ -11,6 +11,7 @@
 // apart; neighbouring pairs: pieces side by side), so no value ever changes lanes and the sums are a
 // few shuffles.  A CTA works on one chunk of heads (blockIdx.y) for a stride of tokens: a group reads a
 // token's cosines and sines once for the chunk, and kHeads heads are in flight at a time.
+#include <atomic>
 #include <cmath>
 
 #include "fewbit_device.cuh"
@@ -324,6 +325,81 @@ qk_fwd_kernel(const __grid_constant__ QkParams q) {
     }
 }
 
+template <int V, int CU, bool FULL>
+__device__ __forceinline__ void write_partial(const QkParams &q, const Units<V, CU, FULL> &u, float (&da)[CU][V], float (&db)[CU][V]) {
+    if (q.partial == nullptr) return;
+    __shared__ float sums[kQkThreads / 32][kQkMaxDim];
+    // the CTA's sum of every element of the weight, in a fixed order: over a warp's groups, then over its warps
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int c = 0; c < CU; ++c)
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            for (int o = q.group; o < 32; o <<= 1) {
+                da[c][e] += __shfl_xor_sync(0xffffffffu, da[c][e], o);
+                db[c][e] += __shfl_xor_sync(0xffffffffu, db[c][e], o);
+            }
+            if (lane < q.group) {
+                if (u.has_a(c)) sums[warp][u.a[c] + e] = da[c][e];
+                if (u.has_b(c)) sums[warp][u.b[c] + e] = db[c][e];
+            }
+        }
+    __syncthreads();
+    if (static_cast<int>(threadIdx.x) < q.dim) {
+        float total = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kQkThreads / 32; ++w) total += sums[w][threadIdx.x];
+        q.partial[(static_cast<size_t>(blockIdx.y) * gridDim.x + blockIdx.x) * q.dim + threadIdx.x] = total;
+    }
+}
+
+// One head of the backward pass; `live`: it exists (all lanes take part in the sums).
+template <typename T, int V, int CU, bool INTER, bool FULL>
+__device__ __forceinline__ void bwd_head(const QkParams &q, const Units<V, CU, FULL> &u, const Turn<V, CU, INTER, FULL> &turn, const Chunk<T, V> (&x)[CU][2],
+                                         const Chunk<T, V> (&g)[CU][2], const float (&wa)[CU][V], const float (&wb)[CU][V],
+                                         float (&da)[CU][V], float (&db)[CU][V], bool live, T *dst) {
+    float va[CU][V], vb[CU][V], ga[CU][V], gb[CU][V], squares[2] = {0.0f, 0.0f}, dots[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int c = 0; c < CU; ++c) {
+        x[c][0].widen(va[c]);
+        x[c][1].widen(vb[c]);
+        g[c][0].widen(ga[c]);
+        g[c][1].widen(gb[c]);
+        vdot<V>(squares, va[c], va[c]);
+        vdot<V>(squares, vb[c], vb[c]);
+    }
+    turn.template apply<true>(ga, gb);
+    // t = g' x: the weight's gradient without r, and, times the weight, the terms of the dot product
+    float ta[CU][V], tb[CU][V];
+#pragma unroll
+    for (int c = 0; c < CU; ++c) {
+        vmul<V>(ta[c], ga[c], va[c]);
+        vmul<V>(tb[c], gb[c], vb[c]);
+        vdot<V>(dots, ta[c], wa[c]);
+        vdot<V>(dots, tb[c], wb[c]);
+    }
+    float sum = squares[0] + squares[1], dot = dots[0] + dots[1];
+    for (int o = q.group >> 1; o > 0; o >>= 1) {          // both sums in one go
+        sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        dot += __shfl_xor_sync(0xffffffffu, dot, o);
+    }
+    const float r = rsqrtf(sum * q.inv_dim + q.eps);
+    const float shift = -dot * q.inv_dim * r * r * r;
+    if (!live) return;
+#pragma unroll
+    for (int c = 0; c < CU; ++c) {
+        vaxpy<V>(da[c], ta[c], r, da[c]);
+        vaxpy<V>(db[c], tb[c], r, db[c]);
+        vscale<V>(ga[c], ga[c], r);                       // dx = (r g') w - (r^3 mean) x
+        vscale<V>(gb[c], gb[c], r);
+        vscale<V>(va[c], va[c], shift);
+        vscale<V>(vb[c], vb[c], shift);
+        vfma<V>(va[c], ga[c], wa[c], va[c]);
+        vfma<V>(vb[c], gb[c], wb[c], vb[c]);
+    }
+    store_head<T, V, CU, FULL>(dst, u, va, vb);
+}
+
 template <typename T, int V, int CU, bool INTER, bool FULL>
 __global__ void __launch_bounds__(kQkThreads, kBwdCtasPerSm)
 qk_bwd_kernel(const __grid_constant__ QkParams q) {
@@ -333,7 +409,6 @@ qk_bwd_kernel(const __grid_constant__ QkParams q) {
     const QkTensor &in = q.in[hc.which], &gin = q.g[hc.which], &out = q.out[hc.which];
     Units<V, CU, FULL> u;
     u.place(q, threadIdx.x & (q.group - 1), INTER);
-    __shared__ float sums[kQkThreads / 32][kQkMaxDim];
     pdl_wait();
     float wa[CU][V], wb[CU][V], da[CU][V], db[CU][V];
     load_weight<V, CU, FULL>(q.weight[hc.which], u, wa, wb);
@@ -359,72 +434,141 @@ qk_bwd_kernel(const __grid_constant__ QkParams q) {
             }
 #pragma unroll
             for (int j = 0; j < kBwdHeads; ++j) {
-                float va[CU][V], vb[CU][V], ga[CU][V], gb[CU][V], squares[2] = {0.0f, 0.0f}, dots[2] = {0.0f, 0.0f};
-#pragma unroll
-                for (int c = 0; c < CU; ++c) {
-                    x[j][c][0].widen(va[c]);
-                    x[j][c][1].widen(vb[c]);
-                    g[j][c][0].widen(ga[c]);
-                    g[j][c][1].widen(gb[c]);
-                    vdot<V>(squares, va[c], va[c]);
-                    vdot<V>(squares, vb[c], vb[c]);
-                }
-                turn.template apply<true>(ga, gb);
-                // t = g' x: the weight's gradient without r, and, times the weight, the terms of the dot product
-                float ta[CU][V], tb[CU][V];
-#pragma unroll
-                for (int c = 0; c < CU; ++c) {
-                    vmul<V>(ta[c], ga[c], va[c]);
-                    vmul<V>(tb[c], gb[c], vb[c]);
-                    vdot<V>(dots, ta[c], wa[c]);
-                    vdot<V>(dots, tb[c], wb[c]);
-                }
-                float sum = squares[0] + squares[1], dot = dots[0] + dots[1];
-                for (int o = q.group >> 1; o > 0; o >>= 1) {          // both sums in one go
-                    sum += __shfl_xor_sync(0xffffffffu, sum, o);
-                    dot += __shfl_xor_sync(0xffffffffu, dot, o);
-                }
-                const float r = rsqrtf(sum * q.inv_dim + q.eps);
-                const float shift = -dot * q.inv_dim * r * r * r;
-                if (!live || head + j >= hc.end) continue;
-#pragma unroll
-                for (int c = 0; c < CU; ++c) {
-                    vaxpy<V>(da[c], ta[c], r, da[c]);
-                    vaxpy<V>(db[c], tb[c], r, db[c]);
-                    vscale<V>(ga[c], ga[c], r);                       // dx = (r g') w - (r^3 mean) x
-                    vscale<V>(gb[c], gb[c], r);
-                    vscale<V>(va[c], va[c], shift);
-                    vscale<V>(vb[c], vb[c], shift);
-                    vfma<V>(va[c], ga[c], wa[c], va[c]);
-                    vfma<V>(vb[c], gb[c], wb[c], vb[c]);
-                }
-                store_head<T, V, CU, FULL>(dst + j * out.h, u, va, vb);
+                bwd_head<T, V, CU, INTER, FULL>(q, u, turn, x[j], g[j], wa, wb, da, db, live && head + j < hc.end, dst + j * out.h);
             }
         }
     }
-    if (q.partial == nullptr) return;
-    // the CTA's sum of every element of the weight, in a fixed order: over a warp's groups, then over its warps
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    write_partial<V, CU, FULL>(q, u, da, db);
+}
+
+// Full lanes: what a thread will read is copied to shared memory ahead of its use, kAhead heads in advance and over the ends of
+// tokens, so that loads are in flight all the time and take no registers.  No thread reads what another one copied.
+__device__ __forceinline__ void copy16(uint32_t to, const void *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
+}
+template <typename T, int V, bool INTER, int N>
+struct Ahead {
+    static constexpr int kAhead = N == 2 ? 3 : 5, kSlots = kAhead + 1;
+    static constexpr int kItem = 2 * N, kTurn = V / 2;                // 16-byte pieces of a head (of N tensors); of a token's cos and sin
+    static constexpr uint32_t kPiece = kQkThreads * 16;
+    static constexpr int kBytes = (kSlots * kItem + 2 * kTurn) * static_cast<int>(kPiece);
+    uint32_t at;                                                      // this thread's place in a piece
+    uint32_t base;                                                    // the next head to be copied: its token, ...
+    int head = 0, heads, ahead;
+    uint32_t slot = 0, parity = 0, used = 0, turned = 0;
+    bool live = false;
+    const T *from[N];
+
+    __device__ __forceinline__ void start(const QkParams &q, const QkTensor *const (&t)[N], const HeadChunk &hc, const Units<V, 1, true> &u, uint32_t shared) {
+        at = shared + threadIdx.x * 16;
+        base = blockIdx.x * (kQkThreads / q.group);
+        heads = hc.end - hc.first;
+        ahead = 2 * heads > kAhead ? kAhead : 1;                      // a token's cosines are read before those of the next but one come
+        for (int k = 0; k < ahead; ++k) next(q, t, hc, u);
+    }
+    __device__ __forceinline__ void next(const QkParams &q, const QkTensor *const (&t)[N], const HeadChunk &hc, const Units<V, 1, true> &u) {
+        if (base < q.tokens) {
+            if (head == 0) {
+                const uint32_t token = base + threadIdx.x / q.group;
+                live = token < q.tokens;
+                if (live) {
+                    const uint32_t bi = token / q.length, i = token % q.length;
 #pragma unroll
-    for (int c = 0; c < CU; ++c)
+                    for (int n = 0; n < N; ++n) from[n] = static_cast<const T *>(t[n]->p) + bi * t[n]->b + i * t[n]->i + hc.first * t[n]->h;
+                    const long long pos = position_of(q, token, i);
+                    const uint32_t to = at + (kSlots * kItem + parity * kTurn) * kPiece;
+                    const long long col = pos * q.half + (INTER ? u.a[0] / 2 : u.a[0]);
+                    if (pos >= 0 && pos < q.table_rows) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) {
-            for (int o = q.group; o < 32; o <<= 1) {
-                da[c][e] += __shfl_xor_sync(0xffffffffu, da[c][e], o);
-                db[c][e] += __shfl_xor_sync(0xffffffffu, db[c][e], o);
+                        for (int e = 0; e < V / 4; ++e) {
+                            copy16(to + e * kPiece, q.cos + col + 4 * e);
+                            copy16(to + (V / 4 + e) * kPiece, q.sin + col + 4 * e);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < kTurn; ++e)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" :: "r"(to + e * kPiece), "r"(0x7fc00000u) : "memory");
+                    }
+                }
+                parity ^= 1;
             }
-            if (lane < q.group) {
-                if (u.has_a(c)) sums[warp][u.a[c] + e] = da[c][e];
-                if (u.has_b(c)) sums[warp][u.b[c] + e] = db[c][e];
+            if (live) {
+#pragma unroll
+                for (int n = 0; n < N; ++n) {
+                    copy16(at + (slot * kItem + 2 * n) * kPiece, from[n] + u.a[0]);
+                    copy16(at + (slot * kItem + 2 * n + 1) * kPiece, from[n] + u.b[0]);
+                    from[n] += t[n]->h;
+                }
+            }
+            slot = slot == kSlots - 1 ? 0 : slot + 1;
+            if (++head == heads) {
+                head = 0;
+                base += gridDim.x * (kQkThreads / q.group);
             }
         }
-    __syncthreads();
-    if (static_cast<int>(threadIdx.x) < q.dim) {
-        float total = 0.0f;
-#pragma unroll
-        for (int w = 0; w < kQkThreads / 32; ++w) total += sums[w][threadIdx.x];
-        q.partial[(static_cast<size_t>(blockIdx.y) * gridDim.x + blockIdx.x) * q.dim + threadIdx.x] = total;
+        asm volatile("cp.async.commit_group;" ::: "memory");
     }
+    static __device__ __forceinline__ uint4 piece(uint32_t from) {
+        uint4 r;
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(from) : "memory");
+        return r;
+    }
+    // The oldest head, and with `first` its token's cosines; what comes next takes its place
+    __device__ __forceinline__ void take(Chunk<T, V> (&x)[N][1][2], Turn<V, 1, INTER, true> &turn, bool first) {
+        if (ahead == kAhead) asm volatile("cp.async.wait_group %0;" :: "n"(kAhead - 1) : "memory");
+        else asm volatile("cp.async.wait_group 0;" ::: "memory");
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            x[n][0][0].raw = piece(at + (used * kItem + 2 * n) * kPiece);
+            x[n][0][1].raw = piece(at + (used * kItem + 2 * n + 1) * kPiece);
+        }
+        used = used == kSlots - 1 ? 0 : used + 1;
+        if (first) {
+            const uint32_t row = at + (kSlots * kItem + turned * kTurn) * kPiece;
+#pragma unroll
+            for (int e = 0; e < V / 4; ++e) {
+                const uint4 c = piece(row + e * kPiece), s = piece(row + (V / 4 + e) * kPiece);
+                turn.c[0][4 * e] = __uint_as_float(c.x); turn.c[0][4 * e + 1] = __uint_as_float(c.y);
+                turn.c[0][4 * e + 2] = __uint_as_float(c.z); turn.c[0][4 * e + 3] = __uint_as_float(c.w);
+                turn.s[0][4 * e] = __uint_as_float(s.x); turn.s[0][4 * e + 1] = __uint_as_float(s.y);
+                turn.s[0][4 * e + 2] = __uint_as_float(s.z); turn.s[0][4 * e + 3] = __uint_as_float(s.w);
+            }
+            turned ^= 1;
+        }
+    }
+};
+
+template <typename T, int V, bool INTER>
+__global__ void __launch_bounds__(kQkThreads, kBwdCtasPerSm)
+qk_bwd_ahead_kernel(const __grid_constant__ QkParams q) {
+    extern __shared__ __align__(16) uint8_t shared[];
+    pdl_launch_dependents();
+    const HeadChunk hc(q);
+    const QkTensor &out = q.out[hc.which];
+    const QkTensor *const from[2] = {&q.in[hc.which], &q.g[hc.which]};
+    Units<V, 1, true> u;
+    u.place(q, threadIdx.x & (q.group - 1), INTER);
+    pdl_wait();
+    Ahead<T, V, INTER, 2> in;
+    in.start(q, from, hc, u, static_cast<uint32_t>(__cvta_generic_to_shared(shared)));
+    float wa[1][V], wb[1][V], da[1][V], db[1][V];
+    load_weight<V, 1, true>(q.weight[hc.which], u, wa, wb);
+#pragma unroll
+    for (int e = 0; e < V; ++e) da[0][e] = db[0][e] = 0.0f;
+    for (uint32_t base = blockIdx.x * (kQkThreads / q.group); base < q.tokens; base += gridDim.x * (kQkThreads / q.group)) {
+        const uint32_t token = base + threadIdx.x / q.group;
+        const bool live = token < q.tokens;
+        T *dst = static_cast<T *>(out.p);
+        if (live) dst += token / q.length * out.b + token % q.length * out.i + hc.first * out.h;
+        Turn<V, 1, INTER, true> turn;
+        for (int head = hc.first; head < hc.end; ++head, dst += out.h) {
+            Chunk<T, V> x[2][1][2];
+            in.take(x, turn, head == hc.first);
+            in.next(q, from, hc, u);
+            bwd_head<T, V, 1, INTER, true>(q, u, turn, x[0], x[1], wa, wb, da, db, live, dst);
+        }
+    }
+    write_partial<V, 1, true>(q, u, da, db);
 }
 
 // Adds up the CTAs' partial sums, `q_ctas` rows of the queries' weight and then `k_ctas` of the keys': 32 columns and
@@ -451,9 +595,22 @@ qk_weight_kernel(const float *partial, int q_ctas, int k_ctas, int dim, float *d
 }
 
 using QkLaunch = cudaError_t (*)(const QkParams &, unsigned, unsigned, cudaStream_t);
-template <typename K>
-cudaError_t launch_qk(K kernel, const QkParams &q, unsigned x, unsigned y, cudaStream_t st) {
+template <auto kernel, int smem>
+cudaError_t launch_qk(const QkParams &q, unsigned x, unsigned y, cudaStream_t st) {
+    if (smem > 0) {
+        static std::atomic<unsigned long long> ready{0};              // devices (up to 64) whose limit has been raised
+        int dev = 0;
+        cudaError_t err = cudaGetDevice(&dev);
+        if (err != cudaSuccess) return err;
+        const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+        if ((ready.load(std::memory_order_relaxed) & bit) == 0) {
+            err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+            if (err != cudaSuccess) return err;
+            ready.fetch_or(bit, std::memory_order_relaxed);
+        }
+    }
     cudaLaunchConfig_t cfg = {};
+    cfg.dynamicSmemBytes = smem;
     cfg.gridDim = dim3(x, y);
     cfg.blockDim = dim3(kQkThreads);
     cfg.stream = st;
@@ -466,11 +623,12 @@ cudaError_t launch_qk(K kernel, const QkParams &q, unsigned x, unsigned y, cudaS
 }
 template <typename T, int V, int CU, bool INTER, bool FULL>
 cudaError_t launch_fwd(const QkParams &q, unsigned x, unsigned y, cudaStream_t st) {
-    return launch_qk(qk_fwd_kernel<T, V, CU, INTER, FULL>, q, x, y, st);
+    return launch_qk<qk_fwd_kernel<T, V, CU, INTER, FULL>, 0>(q, x, y, st);
 }
 template <typename T, int V, int CU, bool INTER, bool FULL>
 cudaError_t launch_bwd_qk(const QkParams &q, unsigned x, unsigned y, cudaStream_t st) {
-    return launch_qk(qk_bwd_kernel<T, V, CU, INTER, FULL>, q, x, y, st);
+    if constexpr (FULL) return launch_qk<qk_bwd_ahead_kernel<T, V, INTER>, Ahead<T, V, INTER, 2>::kBytes>(q, x, y, st);
+    else return launch_qk<qk_bwd_kernel<T, V, CU, INTER, FULL>, 0>(q, x, y, st);
 }
 // [dtype][interleaved][variant]: 16-byte pieces with full lanes, 16-byte pieces, 8-byte pieces of the 16-bit types, single
 // elements; a lane holds CU units so that 32 lanes cover the largest head
