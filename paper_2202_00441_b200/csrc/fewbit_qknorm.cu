@@ -26,8 +26,10 @@ namespace {
 constexpr int kQkThreads = 256;
 constexpr int kQkMaxDim = 256;
 // Heads in flight and CTAs on an SM, chosen together: bytes in flight against registers.  Measured on 4 x 8192 tokens,
-// 32 + 8 heads of 128, bfloat16, forward / backward in us: (4, 2 CTAs) 116 / -, (4, 3) 129 / -, (2, 3) 137 / -, (2, 4) 143 / -;
-// (2, 2) - / 210, (1, 2) - / 213, (1, 3) - / 306, (2, 3) - / 361 (spilled registers).
+// 32 + 8 heads of 128, bfloat16, forward / backward in us: (4, 2 CTAs) 112 / -, (4, 3) 129 / -, (2, 3) 137 / -, (2, 4) 143 / -;
+// (2, 2) - / 210, (1, 2) - / 213, (1, 3) - / 306, (2, 3) - / 361 (spilled registers).  Full lanes, backward: 178 with copies
+// ahead (Ahead, below), at 5.7 TB/s = 87 % of the copy bandwidth; the forward pass, at 6.05 TB/s = 92 %, loses by them (3, 5 or
+// 7 heads ahead: 130, 133, 134; bursts of 4 or 8 heads: 132, 126): its bursts of loads between stores suit the memory better.
 constexpr int kFwdHeads = 4, kBwdHeads = 2;
 constexpr int kChunkHeads = 8;
 constexpr int kFwdCtasPerSm = 2, kBwdCtasPerSm = 2;
@@ -448,7 +450,7 @@ __device__ __forceinline__ void copy16(uint32_t to, const void *from) {
 }
 template <typename T, int V, bool INTER, int N>
 struct Ahead {
-    static constexpr int kAhead = N == 2 ? 3 : 5, kSlots = kAhead + 1;
+    static constexpr int kAhead = 3, kSlots = kAhead + 1;
     static constexpr int kItem = 2 * N, kTurn = V / 2;                // 16-byte pieces of a head (of N tensors); of a token's cos and sin
     static constexpr uint32_t kPiece = kQkThreads * 16;
     static constexpr int kBytes = (kSlots * kItem + 2 * kTurn) * static_cast<int>(kPiece);
