@@ -212,6 +212,13 @@ __device__ __forceinline__ void end_cta(uint32_t tmem) {
 // ---------------------------------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------------------------------
+// One pass over the keys with a running reference and sum of the softmax.  For each pair of row tiles and key tile: 2048
+// clocks of products, 2048 of exponentials (of which a quarter goes elsewhere), 64 KB from L2.  Two row tiles share every
+// K and V tile that is loaded, and each one's softmax runs while the other's products do.  Measured, bfloat16, heads of
+// 128, causal: 16384 rows, 8 heads on 2, 489 us = 1.12 PFLOP/s, 67 % of a burst of matrix products and 80 % of what they
+// sustain: the power limit holds the SMs at 1.6 GHz there; 4 x 2048 rows, 16 heads on 4, 84 us = 0.82 PFLOP/s: 512 CTAs of
+// 2 to 16 key tiles, each with a start and an end that no product covers.  One row on 8192 keys: 26 us, 8 tiles one
+// after another in each of 64 CTAs and the joining of their sums.
 // Barriers: q (2 row tiles), k full/empty (2 stages), v full/empty, S full (2), the first half of each thread's part of P
 // ready (2), all of it (2), O done (2), drained.
 enum { fQ = 0, fKFull = 2, fKEmpty = 4, fVFull = 6, fVEmpty = 8, fS = 10, fP = 12, fPEnd = 14, fO = 16, fDrain = 18, fBars = 19 };
@@ -525,6 +532,11 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
 // ---------------------------------------------------------------------------------------------------
 // backward, dQ (and the rows' statistics)
 // ---------------------------------------------------------------------------------------------------
+// Three products (1536 clocks) and 1024 of exponentials for each row and key tile, which loads 64 KB for the one row tile
+// that tensor and shared memory have room for: 37 bytes a clock into each SM are what L2 gives when all SMs ask, so the loads
+// take 1750 clocks and bound it.  Tensor pipe 42 % active on 4 x 2048 rows, 16 heads on 4, causal; the whole backward pass
+// takes 276 us there (0.62 PFLOP/s counting five products, 0.87 counting the seven that are computed), and 1.62 ms for
+// 16384 rows, 8 heads on 2 (0.85 and 1.18 PFLOP/s, the latter 84 % of what matrix products sustain at the power limit).
 // Barriers: q and g, k full/empty (3 stages: a tile is used twice, one iteration apart), v full/empty (2 stages), S full (2),
 // dP full, dS ready, dQ done.
 enum { qQ = 0, qKFull = 1, qKEmpty = 4, qVFull = 7, qVEmpty = 9, qS = 11, qDp = 13, qDs = 14, qDone = 15, qBars = 16 };
@@ -820,6 +832,10 @@ attention_dq_kernel(const __grid_constant__ Params p) {
 // ---------------------------------------------------------------------------------------------------
 // backward, dK and dV
 // ---------------------------------------------------------------------------------------------------
+// Four products (2048 clocks) and 1024 of exponentials for each row and key tile.  The key tile's K stays in tensor memory and
+// its V in shared memory, so that Q and dO have three stages each.  What is left between the products is the chain of one
+// tile: S, its exponentials, dP, dS, and their way through tensor memory, 2850 clocks with two tiles' products interleaved.
+// Tensor pipe 58 % active on 4 x 2048 rows, 16 heads on 4, causal, where it takes half of the pass's 276 us.
 // Barriers: v, k in tensor memory, q full/empty (3 stages), g full/empty (3 stages), statistics full/empty (2 stages), S full
 // and read, dP full and read, P ready and used, dS ready and used, done.
 enum { kV = 0, kK = 1, kQFull = 2, kQEmpty = 5, kGFull = 8, kGEmpty = 11, kTFull = 14, kTEmpty = 16, kS = 18, kSRead = 19, kDp = 20, kDpRead = 21, kP = 22,
