@@ -85,6 +85,10 @@ CASES = [
     (1, 6, 0, 3, 66, 0, torch.float16, False, "fused", None, True),
     (1, 0, 2, 2, 64, 64, torch.float32, False, "fused", None, True),
     (1, 9000, 6, 2, 32, 32, torch.bfloat16, False, "fused", None, True),
+    # several rounds of tokens for each CTA, chunks of 1, 2, 3 and 8 heads
+    (1, 20011, 1, 2, 64, 64, torch.bfloat16, False, "fused", None, True),
+    (3, 5003, 9, 3, 128, 128, torch.float16, True, "fused", torch.int32, True),
+    (1, 12007, 3, 1, 128, 128, torch.float32, False, "heads_first", torch.int64, True),
 ]
 
 
@@ -154,6 +158,19 @@ def test_positions_outside_the_tables_make_nan_and_read_nothing():
     qo, ko = fb.fewbit_qk_norm_rope_fwd(q, k, *w, c, s, positions=p)
     assert qo[0, [1, 2]].isnan().all() and ko[0, [1, 2]].isnan().all()
     assert qo[0, [0, 3]].isfinite().all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,r", [(64, 64), (64, 32)])
+def test_gradients_of_positions_outside_the_tables_are_nan(d, r):
+    q, k, w, c, s, _ = inputs(1, 4, 2, 1, d, r, torch.bfloat16, "fused", None, True)
+    p = torch.tensor([[0, -1, c.shape[0], c.shape[0] - 1]], device="cuda")
+    gq, gk = torch.ones_like(q), torch.ones_like(k)
+    dq, dk, dqw, dkw = fb.fewbit_qk_norm_rope_bwd(gq, gk, q, k, *w, c, s, positions=p)
+    good = fb.fewbit_qk_norm_rope_bwd(gq[:, ::3], gk[:, ::3], q[:, ::3], k[:, ::3], *w, c, s, positions=p[:, ::3].contiguous())
+    assert dq[0, [1, 2], :, :r].isnan().all() and dk[0, [1, 2], :, :r].isnan().all()
+    assert torch.equal(dq[:, ::3], good[0]) and torch.equal(dk[:, ::3], good[1])
+    assert dqw[:r].isnan().all() and dkw[:r].isnan().all()
 
 
 @pytest.mark.gpu
