@@ -27,9 +27,10 @@ constexpr int kQkThreads = 256;
 constexpr int kQkMaxDim = 256;
 // Heads in flight and CTAs on an SM, chosen together: bytes in flight against registers.  Measured on 4 x 8192 tokens,
 // 32 + 8 heads of 128, bfloat16, forward / backward in us: (4, 2 CTAs) 112 / -, (4, 3) 129 / -, (2, 3) 137 / -, (2, 4) 143 / -;
-// (2, 2) - / 210, (1, 2) - / 213, (1, 3) - / 306, (2, 3) - / 361 (spilled registers).  Full lanes, backward: 178 with copies
-// ahead (Ahead, below), at 5.7 TB/s = 87 % of the copy bandwidth; the forward pass, at 6.05 TB/s = 92 %, loses by them (3, 5 or
-// 7 heads ahead: 130, 133, 134; bursts of 4 or 8 heads: 132, 126): its bursts of loads between stores suit the memory better.
+// (2, 2) - / 210, (1, 2) - / 213, (1, 3) - / 306, (2, 3) - / 361 (spilled registers).  With copies ahead (Ahead, below) the
+// backward pass takes 178, 5.7 TB/s = 87 % of the copy bandwidth; of heads half of which are rotated 245 -> 222, of 96 elements
+// 233 -> 162, neighbouring pairs 284 -> 222.  The forward pass, at 6.05 TB/s = 92 %, loses by them (3, 5 or 7 heads ahead: 130,
+// 133, 134; bursts of 4 or 8 heads: 132, 126): its bursts of loads between stores suit the memory better.
 constexpr int kFwdHeads = 4, kBwdHeads = 2;
 constexpr int kChunkHeads = 8;
 constexpr int kFwdCtasPerSm = 2, kBwdCtasPerSm = 2;
@@ -443,64 +444,84 @@ qk_bwd_kernel(const __grid_constant__ QkParams q) {
     write_partial<V, CU, FULL>(q, u, da, db);
 }
 
-// Full lanes: what a thread will read is copied to shared memory ahead of its use, kAhead heads in advance and over the ends of
-// tokens, so that loads are in flight all the time and take no registers.  No thread reads what another one copied.
-__device__ __forceinline__ void copy16(uint32_t to, const void *from) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
+// What a thread will read of its heads (and with full lanes of the tables) is copied to shared memory ahead of its use, kAhead heads
+// in advance and over the ends of tokens, so that loads are in flight all the time and take no registers.  No thread reads what
+// another one copied.
+// BYTES side by side in memory for all lanes go past the L1; halves of what a lane reads go through it, which merges them.
+template <int BYTES, bool HALVES>
+__device__ __forceinline__ void copy_ahead(uint32_t to, const void *from) {
+    if constexpr (BYTES == 16 && !HALVES) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" :: "r"(to), "l"(from), "n"(BYTES) : "memory");
 }
-template <typename T, int V, bool INTER, int N>
+template <typename T, int V, bool INTER, bool FULL>
 struct Ahead {
     static constexpr int kAhead = 3, kSlots = kAhead + 1;
-    static constexpr int kItem = 2 * N, kTurn = V / 2;                // 16-byte pieces of a head (of N tensors); of a token's cos and sin
-    static constexpr uint32_t kPiece = kQkThreads * 16;
-    static constexpr int kBytes = (kSlots * kItem + 2 * kTurn) * static_cast<int>(kPiece);
-    uint32_t at;                                                      // this thread's place in a piece
+    static constexpr int kItem = 4, kBytes = V * sizeof(T);           // pieces of a head (values, gradients); bytes of each
+    static constexpr int kTurn = FULL ? V / 2 : 0;                    // 16-byte pieces of a token's cos and sin
+    static constexpr uint32_t kPiece = kQkThreads * kBytes, kTurnPiece = kQkThreads * 16, kHeads = kSlots * kItem * kPiece;
+    static constexpr int kShared = static_cast<int>(kHeads + 2 * kTurn * kTurnPiece);
+    uint32_t at, turn_at;                                             // this thread's place in a piece
     uint32_t base;                                                    // the next head to be copied: its token, ...
     int head = 0, heads, ahead;
     uint32_t slot = 0, parity = 0, used = 0, turned = 0;
     bool live = false;
-    const T *from[N];
+    const T *x, *g;
 
-    __device__ __forceinline__ void start(const QkParams &q, const QkTensor *const (&t)[N], const HeadChunk &hc, const Units<V, 1, true> &u, uint32_t shared) {
-        at = shared + threadIdx.x * 16;
+    __device__ __forceinline__ uint32_t place(uint32_t slot, int k) const { return at + (slot * kItem + k) * kPiece; }
+    __device__ __forceinline__ void start(const QkParams &q, const HeadChunk &hc, const Units<V, 1, FULL> &u, uint32_t shared) {
+        at = shared + threadIdx.x * kBytes;
+        turn_at = shared + kHeads + threadIdx.x * 16;
         base = blockIdx.x * (kQkThreads / q.group);
         heads = hc.end - hc.first;
         ahead = 2 * heads > kAhead ? kAhead : 1;                      // a token's cosines are read before those of the next but one come
-        for (int k = 0; k < ahead; ++k) next(q, t, hc, u);
+        if constexpr (!FULL) {                                        // pieces that a lane does not have are zeros
+            Chunk<T, V> none;
+            none.zero();
+#pragma unroll
+            for (int k = 0; k < kSlots * kItem; ++k)
+                if (!(k & 1 ? u.has_b(0) : u.has_a(0))) put(at + k * kPiece, none.raw);
+        }
+        for (int k = 0; k < ahead; ++k) next(q, hc, u);
     }
-    __device__ __forceinline__ void next(const QkParams &q, const QkTensor *const (&t)[N], const HeadChunk &hc, const Units<V, 1, true> &u) {
+    __device__ __forceinline__ void next(const QkParams &q, const HeadChunk &hc, const Units<V, 1, FULL> &u) {
+        const QkTensor &xt = q.in[hc.which], &gt = q.g[hc.which];
         if (base < q.tokens) {
             if (head == 0) {
                 const uint32_t token = base + threadIdx.x / q.group;
                 live = token < q.tokens;
                 if (live) {
                     const uint32_t bi = token / q.length, i = token % q.length;
+                    x = static_cast<const T *>(xt.p) + bi * xt.b + i * xt.i + hc.first * xt.h;
+                    g = static_cast<const T *>(gt.p) + bi * gt.b + i * gt.i + hc.first * gt.h;
+                    if constexpr (FULL) {
+                        const long long pos = position_of(q, token, i);
+                        const uint32_t to = turn_at + parity * kTurn * kTurnPiece;
+                        const long long col = pos * q.half + (INTER ? u.a[0] / 2 : u.a[0]);
+                        if (pos >= 0 && pos < q.table_rows) {
 #pragma unroll
-                    for (int n = 0; n < N; ++n) from[n] = static_cast<const T *>(t[n]->p) + bi * t[n]->b + i * t[n]->i + hc.first * t[n]->h;
-                    const long long pos = position_of(q, token, i);
-                    const uint32_t to = at + (kSlots * kItem + parity * kTurn) * kPiece;
-                    const long long col = pos * q.half + (INTER ? u.a[0] / 2 : u.a[0]);
-                    if (pos >= 0 && pos < q.table_rows) {
+                            for (int e = 0; e < V / 4; ++e) {
+                                copy_ahead<16, (V > 4)>(to + e * kTurnPiece, q.cos + col + 4 * e);
+                                copy_ahead<16, (V > 4)>(to + (V / 4 + e) * kTurnPiece, q.sin + col + 4 * e);
+                            }
+                        } else {
 #pragma unroll
-                        for (int e = 0; e < V / 4; ++e) {
-                            copy16(to + e * kPiece, q.cos + col + 4 * e);
-                            copy16(to + (V / 4 + e) * kPiece, q.sin + col + 4 * e);
+                            for (int e = 0; e < kTurn; ++e) put(to + e * kTurnPiece, make_uint4(0x7fc00000u, 0x7fc00000u, 0x7fc00000u, 0x7fc00000u));
                         }
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < kTurn; ++e)
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" :: "r"(to + e * kPiece), "r"(0x7fc00000u) : "memory");
                     }
                 }
                 parity ^= 1;
             }
             if (live) {
-#pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    copy16(at + (slot * kItem + 2 * n) * kPiece, from[n] + u.a[0]);
-                    copy16(at + (slot * kItem + 2 * n + 1) * kPiece, from[n] + u.b[0]);
-                    from[n] += t[n]->h;
+                if (u.has_a(0)) {
+                    copy_ahead<kBytes, INTER>(place(slot, 0), x + u.a[0]);
+                    copy_ahead<kBytes, INTER>(place(slot, 2), g + u.a[0]);
                 }
+                if (u.has_b(0)) {
+                    copy_ahead<kBytes, INTER>(place(slot, 1), x + u.b[0]);
+                    copy_ahead<kBytes, INTER>(place(slot, 3), g + u.b[0]);
+                }
+                x += xt.h;
+                g += gt.h;
             }
             slot = slot == kSlots - 1 ? 0 : slot + 1;
             if (++head == heads) {
@@ -510,67 +531,79 @@ struct Ahead {
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    static __device__ __forceinline__ uint4 piece(uint32_t from) {
-        uint4 r;
-        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(from) : "memory");
-        return r;
+    static __device__ __forceinline__ void put(uint32_t to, uint4 r) {
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" :: "r"(to), "r"(r.x), "r"(r.y), "r"(r.z), "r"(r.w) : "memory");
     }
-    // The oldest head, and with `first` its token's cosines; what comes next takes its place
-    __device__ __forceinline__ void take(Chunk<T, V> (&x)[N][1][2], Turn<V, 1, INTER, true> &turn, bool first) {
+    static __device__ __forceinline__ void put(uint32_t to, uint2 r) {
+        asm volatile("st.shared.v2.b32 [%0], {%1, %2};" :: "r"(to), "r"(r.x), "r"(r.y) : "memory");
+    }
+    static __device__ __forceinline__ void get(uint32_t from, uint4 &r) {
+        asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(from) : "memory");
+    }
+    static __device__ __forceinline__ void get(uint32_t from, uint2 &r) {
+        asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(from) : "memory");
+    }
+    // The oldest head: values, gradients
+    __device__ __forceinline__ void take(Chunk<T, V> (&xs)[1][2], Chunk<T, V> (&gs)[1][2]) {
         if (ahead == kAhead) asm volatile("cp.async.wait_group %0;" :: "n"(kAhead - 1) : "memory");
         else asm volatile("cp.async.wait_group 0;" ::: "memory");
-#pragma unroll
-        for (int n = 0; n < N; ++n) {
-            x[n][0][0].raw = piece(at + (used * kItem + 2 * n) * kPiece);
-            x[n][0][1].raw = piece(at + (used * kItem + 2 * n + 1) * kPiece);
-        }
+        get(place(used, 0), xs[0][0].raw);
+        get(place(used, 1), xs[0][1].raw);
+        get(place(used, 2), gs[0][0].raw);
+        get(place(used, 3), gs[0][1].raw);
         used = used == kSlots - 1 ? 0 : used + 1;
-        if (first) {
-            const uint32_t row = at + (kSlots * kItem + turned * kTurn) * kPiece;
+    }
+    // The cosines of its token, which it is the first head of
+    __device__ __forceinline__ void take(Turn<V, 1, INTER, FULL> &turn) {
+        const uint32_t row = turn_at + turned * kTurn * kTurnPiece;
 #pragma unroll
-            for (int e = 0; e < V / 4; ++e) {
-                const uint4 c = piece(row + e * kPiece), s = piece(row + (V / 4 + e) * kPiece);
-                turn.c[0][4 * e] = __uint_as_float(c.x); turn.c[0][4 * e + 1] = __uint_as_float(c.y);
-                turn.c[0][4 * e + 2] = __uint_as_float(c.z); turn.c[0][4 * e + 3] = __uint_as_float(c.w);
-                turn.s[0][4 * e] = __uint_as_float(s.x); turn.s[0][4 * e + 1] = __uint_as_float(s.y);
-                turn.s[0][4 * e + 2] = __uint_as_float(s.z); turn.s[0][4 * e + 3] = __uint_as_float(s.w);
-            }
-            turned ^= 1;
+        for (int e = 0; e < V / 4; ++e) {
+            uint4 c, s;
+            get(row + e * kTurnPiece, c);
+            get(row + (V / 4 + e) * kTurnPiece, s);
+            turn.c[0][4 * e] = __uint_as_float(c.x); turn.c[0][4 * e + 1] = __uint_as_float(c.y);
+            turn.c[0][4 * e + 2] = __uint_as_float(c.z); turn.c[0][4 * e + 3] = __uint_as_float(c.w);
+            turn.s[0][4 * e] = __uint_as_float(s.x); turn.s[0][4 * e + 1] = __uint_as_float(s.y);
+            turn.s[0][4 * e + 2] = __uint_as_float(s.z); turn.s[0][4 * e + 3] = __uint_as_float(s.w);
         }
+        turned ^= 1;
     }
 };
 
-template <typename T, int V, bool INTER>
+template <typename T, int V, bool INTER, bool FULL>
 __global__ void __launch_bounds__(kQkThreads, kBwdCtasPerSm)
 qk_bwd_ahead_kernel(const __grid_constant__ QkParams q) {
     extern __shared__ __align__(16) uint8_t shared[];
     pdl_launch_dependents();
     const HeadChunk hc(q);
     const QkTensor &out = q.out[hc.which];
-    const QkTensor *const from[2] = {&q.in[hc.which], &q.g[hc.which]};
-    Units<V, 1, true> u;
+    Units<V, 1, FULL> u;
     u.place(q, threadIdx.x & (q.group - 1), INTER);
     pdl_wait();
-    Ahead<T, V, INTER, 2> in;
-    in.start(q, from, hc, u, static_cast<uint32_t>(__cvta_generic_to_shared(shared)));
+    Ahead<T, V, INTER, FULL> in;
+    in.start(q, hc, u, static_cast<uint32_t>(__cvta_generic_to_shared(shared)));
     float wa[1][V], wb[1][V], da[1][V], db[1][V];
-    load_weight<V, 1, true>(q.weight[hc.which], u, wa, wb);
+    load_weight<V, 1, FULL>(q.weight[hc.which], u, wa, wb);
 #pragma unroll
     for (int e = 0; e < V; ++e) da[0][e] = db[0][e] = 0.0f;
     for (uint32_t base = blockIdx.x * (kQkThreads / q.group); base < q.tokens; base += gridDim.x * (kQkThreads / q.group)) {
         const uint32_t token = base + threadIdx.x / q.group;
         const bool live = token < q.tokens;
-        T *dst = static_cast<T *>(out.p);
-        if (live) dst += token / q.length * out.b + token % q.length * out.i + hc.first * out.h;
-        Turn<V, 1, INTER, true> turn;
+        const uint32_t bi = live ? token / q.length : 0, i = live ? token % q.length : 0;
+        T *dst = static_cast<T *>(out.p) + bi * out.b + i * out.i + hc.first * out.h;
+        Turn<V, 1, INTER, FULL> turn;
+        if constexpr (!FULL) turn.load(q, u, position_of(q, live ? token : 0, i));
         for (int head = hc.first; head < hc.end; ++head, dst += out.h) {
-            Chunk<T, V> x[2][1][2];
-            in.take(x, turn, head == hc.first);
-            in.next(q, from, hc, u);
-            bwd_head<T, V, 1, INTER, true>(q, u, turn, x[0], x[1], wa, wb, da, db, live, dst);
+            Chunk<T, V> x[1][2], g[1][2];
+            in.take(x, g);
+            if constexpr (FULL) {
+                if (head == hc.first) in.take(turn);
+            }
+            in.next(q, hc, u);
+            bwd_head<T, V, 1, INTER, FULL>(q, u, turn, x, g, wa, wb, da, db, live, dst);
         }
     }
-    write_partial<V, 1, true>(q, u, da, db);
+    write_partial<V, 1, FULL>(q, u, da, db);
 }
 
 // Adds up the CTAs' partial sums, `q_ctas` rows of the queries' weight and then `k_ctas` of the keys': 32 columns and
@@ -629,7 +662,7 @@ cudaError_t launch_fwd(const QkParams &q, unsigned x, unsigned y, cudaStream_t s
 }
 template <typename T, int V, int CU, bool INTER, bool FULL>
 cudaError_t launch_bwd_qk(const QkParams &q, unsigned x, unsigned y, cudaStream_t st) {
-    if constexpr (FULL) return launch_qk<qk_bwd_ahead_kernel<T, V, INTER>, Ahead<T, V, INTER, 2>::kBytes>(q, x, y, st);
+    if constexpr (V > 1) return launch_qk<qk_bwd_ahead_kernel<T, V, INTER, FULL>, Ahead<T, V, INTER, FULL>::kShared>(q, x, y, st);
     else return launch_qk<qk_bwd_kernel<T, V, CU, INTER, FULL>, 0>(q, x, y, st);
 }
 // [dtype][interleaved][variant]: 16-byte pieces with full lanes, 16-byte pieces, 8-byte pieces of the 16-bit types, single
