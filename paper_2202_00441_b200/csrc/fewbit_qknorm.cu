@@ -28,9 +28,10 @@ constexpr int kQkMaxDim = 256;
 // Heads in flight and CTAs on an SM, chosen together: bytes in flight against registers.  Measured on 4 x 8192 tokens,
 // 32 + 8 heads of 128, bfloat16, forward / backward in us: (4, 2 CTAs) 112 / -, (4, 3) 129 / -, (2, 3) 137 / -, (2, 4) 143 / -;
 // (2, 2) - / 210, (1, 2) - / 213, (1, 3) - / 306, (2, 3) - / 361 (spilled registers).  With copies ahead (Ahead, below) the
-// backward pass takes 178, 5.7 TB/s = 87 % of the copy bandwidth; of heads half of which are rotated 245 -> 222, of 96 elements
-// 233 -> 162, neighbouring pairs 284 -> 222.  The forward pass, at 6.05 TB/s = 92 %, loses by them (3, 5 or 7 heads ahead: 130,
-// 133, 134; bursts of 4 or 8 heads: 132, 126): its bursts of loads between stores suit the memory better.
+// backward pass takes 178 to 197 on different GPUs, 5.7 to 5.1 TB/s = 87 to 78 % of the copy bandwidth; neighbouring pairs 284 ->
+// 214, heads half of which are rotated 245 -> 224, of 96 elements 233 -> 151, of 80 227 -> 150.  The forward pass, at 6.05 TB/s
+// = 92 %, loses by them (3, 5 or 7 heads ahead: 130, 133, 134; bursts of 4 or 8 heads: 132, 126): its bursts of loads
+// between stores suit the memory better.
 constexpr int kFwdHeads = 4, kBwdHeads = 2;
 constexpr int kChunkHeads = 8;
 constexpr int kFwdCtasPerSm = 2, kBwdCtasPerSm = 2;
@@ -52,7 +53,7 @@ struct QkParams {
     int dim, rot, half;                 // half = rot / 2
     int units, rot_units;               // units of a head; those that are rotated half against half
     int group;                          // G
-    bool positions64;
+    bool positions64, vector_tables;    // vector_tables: 16-byte reads of four columns of cos and sin are aligned
     float eps, inv_dim;
 };
 
@@ -183,20 +184,39 @@ struct Turn {
                 }
         } else {
 #pragma unroll
-        for (int k = 0; k < CU; ++k)
+            for (int k = 0; k < CU; ++k) {
+                if constexpr (V % 4 == 0) {                   // a unit that is rotated as a whole, or not at all
+                    const int first = INTER ? u.a[k] / 2 : u.a[k];
+                    const bool none = u.a[k] < 0 || first >= q.half, whole = first + V <= q.half && (!INTER || u.b[k] >= 0);
+                    if (q.vector_tables && (none || whole)) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                int j = -1;                                   // the pair's column of the tables
-                if (u.a[k] >= 0) {
-                    if (!INTER) j = u.a[k] + V <= q.half ? u.a[k] + e : -1;
-                    else if (V == 1) j = u.a[k] < q.rot ? u.a[k] / 2 : -1;
-                    else {
-                        const int first = e < V / 2 ? u.a[k] + 2 * e : u.b[k] + 2 * (e - V / 2);
-                        j = (e < V / 2 || u.b[k] >= 0) && first < q.rot ? first / 2 : -1;
+                        for (int e = 0; e < V; e += 4) {
+                            float4 x = none && known ? make_float4(1.0f, 1.0f, 1.0f, 1.0f) : make_float4(bad, bad, bad, bad);
+                            float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                            if (!none && known) {
+                                x = __ldg(reinterpret_cast<const float4 *>(q.cos + row + first + e));
+                                y = __ldg(reinterpret_cast<const float4 *>(q.sin + row + first + e));
+                            }
+                            c[k][e] = x.x; c[k][e + 1] = x.y; c[k][e + 2] = x.z; c[k][e + 3] = x.w;
+                            s[k][e] = y.x; s[k][e + 1] = y.y; s[k][e + 2] = y.z; s[k][e + 3] = y.w;
+                        }
+                        continue;
                     }
                 }
-                c[k][e] = !known ? bad : (j >= 0 ? __ldg(q.cos + row + j) : 1.0f);
-                s[k][e] = known && j >= 0 ? __ldg(q.sin + row + j) : 0.0f;
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    int j = -1;                               // the pair's column of the tables
+                    if (u.a[k] >= 0) {
+                        if (!INTER) j = u.a[k] + V <= q.half ? u.a[k] + e : -1;
+                        else if (V == 1) j = u.a[k] < q.rot ? u.a[k] / 2 : -1;
+                        else {
+                            const int first = e < V / 2 ? u.a[k] + 2 * e : u.b[k] + 2 * (e - V / 2);
+                            j = (e < V / 2 || u.b[k] >= 0) && first < q.rot ? first / 2 : -1;
+                        }
+                    }
+                    c[k][e] = !known ? bad : (j >= 0 ? __ldg(q.cos + row + j) : 1.0f);
+                    s[k][e] = known && j >= 0 ? __ldg(q.sin + row + j) : 0.0f;
+                }
             }
         }
     }
@@ -447,8 +467,9 @@ qk_bwd_kernel(const __grid_constant__ QkParams q) {
 // What a thread will read of its heads (and with full lanes of the tables) is copied to shared memory ahead of its use, kAhead heads
 // in advance and over the ends of tokens, so that loads are in flight all the time and take no registers.  No thread reads what
 // another one copied.
-// BYTES side by side in memory for all lanes go past the L1; halves of what a lane reads go through it, which merges them.
-template <int BYTES, bool HALVES>
+// Neighbouring lanes' pieces go past the L1.  HALVES: a lane's two pieces are neighbours, and the L1 merges what two copies ask
+// of the same sectors (neighbouring pairs, 128 elements: 214 us against 285 past the L1).
+template <int BYTES, bool HALVES = false>
 __device__ __forceinline__ void copy_ahead(uint32_t to, const void *from) {
     if constexpr (BYTES == 16 && !HALVES) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
     else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" :: "r"(to), "l"(from), "n"(BYTES) : "memory");
@@ -500,8 +521,8 @@ struct Ahead {
                         if (pos >= 0 && pos < q.table_rows) {
 #pragma unroll
                             for (int e = 0; e < V / 4; ++e) {
-                                copy_ahead<16, (V > 4)>(to + e * kTurnPiece, q.cos + col + 4 * e);
-                                copy_ahead<16, (V > 4)>(to + (V / 4 + e) * kTurnPiece, q.sin + col + 4 * e);
+                                copy_ahead<16>(to + e * kTurnPiece, q.cos + col + 4 * e);
+                                copy_ahead<16>(to + (V / 4 + e) * kTurnPiece, q.sin + col + 4 * e);
                             }
                         } else {
 #pragma unroll
@@ -512,14 +533,10 @@ struct Ahead {
                 parity ^= 1;
             }
             if (live) {
-                if (u.has_a(0)) {
-                    copy_ahead<kBytes, INTER>(place(slot, 0), x + u.a[0]);
-                    copy_ahead<kBytes, INTER>(place(slot, 2), g + u.a[0]);
-                }
-                if (u.has_b(0)) {
-                    copy_ahead<kBytes, INTER>(place(slot, 1), x + u.b[0]);
-                    copy_ahead<kBytes, INTER>(place(slot, 3), g + u.b[0]);
-                }
+                if (u.has_a(0)) copy_ahead<kBytes, INTER>(place(slot, 0), x + u.a[0]);
+                if (u.has_b(0)) copy_ahead<kBytes, INTER>(place(slot, 1), x + u.b[0]);
+                if (u.has_a(0)) copy_ahead<kBytes, INTER>(place(slot, 2), g + u.a[0]);
+                if (u.has_b(0)) copy_ahead<kBytes, INTER>(place(slot, 3), g + u.b[0]);
                 x += xt.h;
                 g += gt.h;
             }
@@ -752,6 +769,7 @@ int fill(const fewbit_qk_shape *s, const fewbit_heads *const *all, int n, int he
         if (ctas >= sms || q->chunk <= heads_in_flight) break;
     }
     q->positions64 = s->positions_are_64bit != 0;
+    q->vector_tables = table % 16 == 0 && q->half % 4 == 0;
     q->eps = s->eps;
     q->inv_dim = 1.0f / static_cast<float>(s->head_dim);
     return variant;
