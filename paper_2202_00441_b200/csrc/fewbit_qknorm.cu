@@ -7,10 +7,10 @@
 // Memory bound: 2 (forward) or 3 (backward) elements moved for each element, some 10 to 30 operations.
 //
 // Decomposition: a head belongs to G lanes (a power of two).  A lane holds a "unit": two pieces of V
-// elements that the rotation pairs with one another ((j, j + rotary_dim/2) pairs: pieces rotary_dim/2
-// apart; neighbouring pairs: pieces side by side), so no value ever changes lanes and the sums are a
-// few shuffles.  A CTA works on one chunk of heads (blockIdx.y) for a stride of tokens: a group reads a
-// token's cosines and sines once for the chunk, and kHeads heads are in flight at a time.
+// elements, where those of the one are rotated with those of the other (pairs (j, j + rotary_dim/2)) or each holds whole
+// pairs (neighbouring ones), so no value ever changes lanes and the sums are a few shuffles; neighbouring lanes'
+// pieces are neighbours.  A CTA works on one chunk of heads (blockIdx.y) for a stride of tokens: a group reads a
+// token's cosines and sines once for the chunk, and some heads are in flight at a time.
 #include <atomic>
 #include <cmath>
 
@@ -28,10 +28,10 @@ constexpr int kQkMaxDim = 256;
 // Heads in flight and CTAs on an SM, chosen together: bytes in flight against registers.  Measured on 4 x 8192 tokens,
 // 32 + 8 heads of 128, bfloat16, forward / backward in us: (4, 2 CTAs) 112 / -, (4, 3) 129 / -, (2, 3) 137 / -, (2, 4) 143 / -;
 // (2, 2) - / 210, (1, 2) - / 213, (1, 3) - / 306, (2, 3) - / 361 (spilled registers).  With copies ahead (Ahead, below) the
-// backward pass takes 178 to 197 on different GPUs, 5.7 to 5.1 TB/s = 87 to 78 % of the copy bandwidth; neighbouring pairs 284 ->
-// 214, heads half of which are rotated 245 -> 224, of 96 elements 233 -> 151, of 80 227 -> 150.  The forward pass, at 6.05 TB/s
-// = 92 %, loses by them (3, 5 or 7 heads ahead: 130, 133, 134; bursts of 4 or 8 heads: 132, 126): its bursts of loads
-// between stores suit the memory better.
+// backward pass takes 176 to 197, by where the tensors lie, 5.75 to 5.1 TB/s = 88 to 78 % of the copy bandwidth; heads half of
+// which are rotated 245 -> 170, of 96 elements 233 -> 150, of 80 227 -> 149.  The forward pass, at 6.05 TB/s = 92 %, loses by
+// them (3, 5 or 7 heads ahead: 130, 133, 134; bursts of 4 or 8 heads: 132, 126): its bursts of loads between stores suit the
+// memory better.
 constexpr int kFwdHeads = 4, kBwdHeads = 2;
 constexpr int kChunkHeads = 8;
 constexpr int kFwdCtasPerSm = 2, kBwdCtasPerSm = 2;
@@ -139,8 +139,8 @@ struct Units {
         for (int c = 0; c < CU; ++c) {
             const int u = sub + c * q.group;
             if (FULL) {
-                a[c] = interleaved ? 2 * u * V : u * V;
-                b[c] = interleaved ? a[c] + V : q.half + a[c];
+                a[c] = u * V;
+                b[c] = q.half + a[c];
                 continue;
             }
             a[c] = b[c] = -1;
@@ -149,8 +149,11 @@ struct Units {
                 a[c] = u * V;
                 b[c] = q.half + u * V;
             } else {
-                a[c] = 2 * q.rot_units * V + 2 * (u - q.rot_units) * V;
-                b[c] = a[c] + V < q.dim ? a[c] + V : -1;
+                const bool pairs = V == 1 && interleaved;             // single elements: a pair
+                const int first = 2 * q.rot_units * V + (u - q.rot_units) * V;
+                a[c] = pairs ? 2 * u : first;
+                b[c] = pairs ? a[c] + 1 : first + (q.units - q.rot_units) * V;
+                if (b[c] >= q.dim) b[c] = -1;
             }
         }
     }
@@ -167,42 +170,36 @@ struct Turn {
         const bool known = pos >= 0 && pos < q.table_rows;
         const float bad = __uint_as_float(0x7fc00000u);
         const long long row = known ? pos * q.half : 0;
-        if constexpr (FULL) {                                 // whole vectors (16-byte aligned by the host's check)
-            static_assert(V % 4 == 0, "");
 #pragma unroll
-            for (int k = 0; k < CU; ++k)
+        for (int k = 0; k < CU; ++k) {
+            if constexpr (V % 4 == 0) {
+                // Columns in one run, or (neighbouring pairs) one for each piece; each rotated as a whole, or not at all.
+                constexpr int RUNS = INTER ? 2 : 1, W = V / RUNS;
+                bool none[RUNS], vectors = FULL || q.vector_tables;
 #pragma unroll
-                for (int e = 0; e < V; e += 4) {
-                    const int j = (INTER ? u.a[k] / 2 : u.a[k]) + e;
-                    float4 x = make_float4(bad, bad, bad, bad), y = x;
-                    if (known) {
-                        x = __ldg(reinterpret_cast<const float4 *>(q.cos + row + j));
-                        y = __ldg(reinterpret_cast<const float4 *>(q.sin + row + j));
-                    }
-                    c[k][e] = x.x; c[k][e + 1] = x.y; c[k][e + 2] = x.z; c[k][e + 3] = x.w;
-                    s[k][e] = y.x; s[k][e + 1] = y.y; s[k][e + 2] = y.z; s[k][e + 3] = y.w;
+                for (int h = 0; h < RUNS; ++h) {
+                    const int at = h ? u.b[k] : u.a[k], end = INTER ? 2 * q.half : q.half;
+                    none[h] = !FULL && (at < 0 || at >= end);
+                    vectors = vectors && (FULL || none[h] || at + V <= end);
                 }
-        } else {
+                if (vectors) {
 #pragma unroll
-            for (int k = 0; k < CU; ++k) {
-                if constexpr (V % 4 == 0) {                   // a unit that is rotated as a whole, or not at all
-                    const int first = INTER ? u.a[k] / 2 : u.a[k];
-                    const bool none = u.a[k] < 0 || first >= q.half, whole = first + V <= q.half && (!INTER || u.b[k] >= 0);
-                    if (q.vector_tables && (none || whole)) {
+                    for (int h = 0; h < RUNS; ++h) {
+                        const long long from = row + (INTER ? (h ? u.b[k] : u.a[k]) / 2 : u.a[k]);
 #pragma unroll
-                        for (int e = 0; e < V; e += 4) {
-                            float4 x = none && known ? make_float4(1.0f, 1.0f, 1.0f, 1.0f) : make_float4(bad, bad, bad, bad);
-                            float4 y = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                            if (!none && known) {
-                                x = __ldg(reinterpret_cast<const float4 *>(q.cos + row + first + e));
-                                y = __ldg(reinterpret_cast<const float4 *>(q.sin + row + first + e));
-                            }
-                            c[k][e] = x.x; c[k][e + 1] = x.y; c[k][e + 2] = x.z; c[k][e + 3] = x.w;
-                            s[k][e] = y.x; s[k][e + 1] = y.y; s[k][e + 2] = y.z; s[k][e + 3] = y.w;
+                        for (int e = 0; e < W; ++e) {
+                            c[k][h * W + e] = none[h] && known ? 1.0f : bad;
+                            s[k][h * W + e] = 0.0f;
                         }
-                        continue;
+                        if (known && !none[h]) {
+                            read<W>(&c[k][h * W], q.cos + from);
+                            read<W>(&s[k][h * W], q.sin + from);
+                        }
                     }
+                    continue;
                 }
+            }
+            if constexpr (!FULL) {
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
                     int j = -1;                               // the pair's column of the tables
@@ -217,6 +214,19 @@ struct Turn {
                     c[k][e] = !known ? bad : (j >= 0 ? __ldg(q.cos + row + j) : 1.0f);
                     s[k][e] = known && j >= 0 ? __ldg(q.sin + row + j) : 0.0f;
                 }
+            }
+        }
+    }
+    template <int W>
+    static __device__ __forceinline__ void read(float *to, const float *from) {
+        if constexpr (W == 2) {
+            const float2 x = __ldg(reinterpret_cast<const float2 *>(from));
+            to[0] = x.x; to[1] = x.y;
+        } else {
+#pragma unroll
+            for (int e = 0; e < W; e += 4) {
+                const float4 x = __ldg(reinterpret_cast<const float4 *>(from + e));
+                to[e] = x.x; to[e + 1] = x.y; to[e + 2] = x.z; to[e + 3] = x.w;
             }
         }
     }
@@ -467,12 +477,10 @@ qk_bwd_kernel(const __grid_constant__ QkParams q) {
 // What a thread will read of its heads (and with full lanes of the tables) is copied to shared memory ahead of its use, kAhead heads
 // in advance and over the ends of tokens, so that loads are in flight all the time and take no registers.  No thread reads what
 // another one copied.
-// Neighbouring lanes' pieces go past the L1.  HALVES: a lane's two pieces are neighbours, and the L1 merges what two copies ask
-// of the same sectors (neighbouring pairs, 128 elements: 214 us against 285 past the L1).
-template <int BYTES, bool HALVES = false>
+template <int BYTES>
 __device__ __forceinline__ void copy_ahead(uint32_t to, const void *from) {
-    if constexpr (BYTES == 16 && !HALVES) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" :: "r"(to), "l"(from), "n"(BYTES) : "memory");
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" :: "r"(to), "l"(from) : "memory");
 }
 template <typename T, int V, bool INTER, bool FULL>
 struct Ahead {
@@ -517,12 +525,21 @@ struct Ahead {
                     if constexpr (FULL) {
                         const long long pos = position_of(q, token, i);
                         const uint32_t to = turn_at + parity * kTurn * kTurnPiece;
-                        const long long col = pos * q.half + (INTER ? u.a[0] / 2 : u.a[0]);
                         if (pos >= 0 && pos < q.table_rows) {
+                            const long long row = pos * q.half, a = row + (INTER ? u.a[0] / 2 : u.a[0]), b = row + u.b[0] / 2;
 #pragma unroll
                             for (int e = 0; e < V / 4; ++e) {
-                                copy_ahead<16>(to + e * kTurnPiece, q.cos + col + 4 * e);
-                                copy_ahead<16>(to + (V / 4 + e) * kTurnPiece, q.sin + col + 4 * e);
+                                const uint32_t cos = to + e * kTurnPiece, sin = to + (V / 4 + e) * kTurnPiece;
+                                if constexpr (INTER && V == 4) {      // two columns of each piece
+                                    copy_ahead<8>(cos, q.cos + a);
+                                    copy_ahead<8>(cos + 8, q.cos + b);
+                                    copy_ahead<8>(sin, q.sin + a);
+                                    copy_ahead<8>(sin + 8, q.sin + b);
+                                } else {
+                                    const long long from = !INTER ? a + 4 * e : e == 0 ? a : b;
+                                    copy_ahead<16>(cos, q.cos + from);
+                                    copy_ahead<16>(sin, q.sin + from);
+                                }
                             }
                         } else {
 #pragma unroll
@@ -533,10 +550,10 @@ struct Ahead {
                 parity ^= 1;
             }
             if (live) {
-                if (u.has_a(0)) copy_ahead<kBytes, INTER>(place(slot, 0), x + u.a[0]);
-                if (u.has_b(0)) copy_ahead<kBytes, INTER>(place(slot, 1), x + u.b[0]);
-                if (u.has_a(0)) copy_ahead<kBytes, INTER>(place(slot, 2), g + u.a[0]);
-                if (u.has_b(0)) copy_ahead<kBytes, INTER>(place(slot, 3), g + u.b[0]);
+                if (u.has_a(0)) copy_ahead<kBytes>(place(slot, 0), x + u.a[0]);
+                if (u.has_b(0)) copy_ahead<kBytes>(place(slot, 1), x + u.b[0]);
+                if (u.has_a(0)) copy_ahead<kBytes>(place(slot, 2), g + u.a[0]);
+                if (u.has_b(0)) copy_ahead<kBytes>(place(slot, 3), g + u.b[0]);
                 x += xt.h;
                 g += gt.h;
             }
