@@ -28,10 +28,10 @@ constexpr int kQkMaxDim = 256;
 // Heads in flight and CTAs on an SM, chosen together: bytes in flight against registers.  Measured on 4 x 8192 tokens,
 // 32 + 8 heads of 128, bfloat16, forward / backward in us: (4, 2 CTAs) 112 / -, (4, 3) 129 / -, (2, 3) 137 / -, (2, 4) 143 / -;
 // (2, 2) - / 210, (1, 2) - / 213, (1, 3) - / 306, (2, 3) - / 361 (spilled registers).  With copies ahead (Ahead, below) the
-// backward pass takes 176 to 197, by where the tensors lie, 5.75 to 5.1 TB/s = 88 to 78 % of the copy bandwidth; heads half of
-// which are rotated 245 -> 170, of 96 elements 233 -> 150, of 80 227 -> 149.  The forward pass, at 6.05 TB/s = 92 %, loses by
-// them (3, 5 or 7 heads ahead: 130, 133, 134; bursts of 4 or 8 heads: 132, 126): its bursts of loads between stores suit the
-// memory better.
+// backward pass takes 164 to 178, by where the tensors lie, 6.15 to 5.7 TB/s = 94 to 87 % of the copy bandwidth; heads half of
+// which are rotated 245 -> 165, neighbouring pairs 284 -> 172, heads of 96 elements 233 -> 148, of 80 227 -> 147.  The forward
+// pass, at 6.05 TB/s = 92 %, loses by them (3, 5 or 7 heads ahead: 130, 133, 134; bursts of 4 or 8 heads: 132, 126): its
+// bursts of loads between stores suit the memory better.
 constexpr int kFwdHeads = 4, kBwdHeads = 2;
 constexpr int kChunkHeads = 8;
 constexpr int kFwdCtasPerSm = 2, kBwdCtasPerSm = 2;
@@ -474,9 +474,10 @@ qk_bwd_kernel(const __grid_constant__ QkParams q) {
     write_partial<V, CU, FULL>(q, u, da, db);
 }
 
-// What a thread will read of its heads (and with full lanes of the tables) is copied to shared memory ahead of its use, kAhead heads
-// in advance and over the ends of tokens, so that loads are in flight all the time and take no registers.  No thread reads what
-// another one copied.
+// What a thread will read of its heads is copied to shared memory ahead of its use, kAhead heads in advance and over the ends
+// of tokens, so that loads are in flight all the time and take no registers.  No thread reads what another one copied.
+// (More heads ahead suit the memory worse: 2, 3, 4, 5 heads 164, 188, 190, 191 us on the shape above, with tensors in one place,
+// 178, 179, 179, 180 in another.)
 template <int BYTES>
 __device__ __forceinline__ void copy_ahead(uint32_t to, const void *from) {
     if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
@@ -484,25 +485,22 @@ __device__ __forceinline__ void copy_ahead(uint32_t to, const void *from) {
 }
 template <typename T, int V, bool INTER, bool FULL>
 struct Ahead {
-    static constexpr int kAhead = 3, kSlots = kAhead + 1;
+    static constexpr int kAhead = 2, kSlots = kAhead + 1;
     static constexpr int kItem = 4, kBytes = V * sizeof(T);           // pieces of a head (values, gradients); bytes of each
-    static constexpr int kTurn = FULL ? V / 2 : 0;                    // 16-byte pieces of a token's cos and sin
-    static constexpr uint32_t kPiece = kQkThreads * kBytes, kTurnPiece = kQkThreads * 16, kHeads = kSlots * kItem * kPiece;
-    static constexpr int kShared = static_cast<int>(kHeads + 2 * kTurn * kTurnPiece);
-    uint32_t at, turn_at;                                             // this thread's place in a piece
+    static constexpr uint32_t kPiece = kQkThreads * kBytes;
+    static constexpr int kShared = kSlots * kItem * static_cast<int>(kPiece);
+    uint32_t at;                                                      // this thread's place in a piece
     uint32_t base;                                                    // the next head to be copied: its token, ...
-    int head = 0, heads, ahead;
-    uint32_t slot = 0, parity = 0, used = 0, turned = 0;
+    int head = 0, heads;
+    uint32_t slot = 0, used = 0;
     bool live = false;
     const T *x, *g;
 
     __device__ __forceinline__ uint32_t place(uint32_t slot, int k) const { return at + (slot * kItem + k) * kPiece; }
     __device__ __forceinline__ void start(const QkParams &q, const HeadChunk &hc, const Units<V, 1, FULL> &u, uint32_t shared) {
         at = shared + threadIdx.x * kBytes;
-        turn_at = shared + kHeads + threadIdx.x * 16;
         base = blockIdx.x * (kQkThreads / q.group);
         heads = hc.end - hc.first;
-        ahead = 2 * heads > kAhead ? kAhead : 1;                      // a token's cosines are read before those of the next but one come
         if constexpr (!FULL) {                                        // pieces that a lane does not have are zeros
             Chunk<T, V> none;
             none.zero();
@@ -510,7 +508,7 @@ struct Ahead {
             for (int k = 0; k < kSlots * kItem; ++k)
                 if (!(k & 1 ? u.has_b(0) : u.has_a(0))) put(at + k * kPiece, none.raw);
         }
-        for (int k = 0; k < ahead; ++k) next(q, hc, u);
+        for (int k = 0; k < kAhead; ++k) next(q, hc, u);
     }
     __device__ __forceinline__ void next(const QkParams &q, const HeadChunk &hc, const Units<V, 1, FULL> &u) {
         const QkTensor &xt = q.in[hc.which], &gt = q.g[hc.which];
@@ -522,32 +520,7 @@ struct Ahead {
                     const uint32_t bi = token / q.length, i = token % q.length;
                     x = static_cast<const T *>(xt.p) + bi * xt.b + i * xt.i + hc.first * xt.h;
                     g = static_cast<const T *>(gt.p) + bi * gt.b + i * gt.i + hc.first * gt.h;
-                    if constexpr (FULL) {
-                        const long long pos = position_of(q, token, i);
-                        const uint32_t to = turn_at + parity * kTurn * kTurnPiece;
-                        if (pos >= 0 && pos < q.table_rows) {
-                            const long long row = pos * q.half, a = row + (INTER ? u.a[0] / 2 : u.a[0]), b = row + u.b[0] / 2;
-#pragma unroll
-                            for (int e = 0; e < V / 4; ++e) {
-                                const uint32_t cos = to + e * kTurnPiece, sin = to + (V / 4 + e) * kTurnPiece;
-                                if constexpr (INTER && V == 4) {      // two columns of each piece
-                                    copy_ahead<8>(cos, q.cos + a);
-                                    copy_ahead<8>(cos + 8, q.cos + b);
-                                    copy_ahead<8>(sin, q.sin + a);
-                                    copy_ahead<8>(sin + 8, q.sin + b);
-                                } else {
-                                    const long long from = !INTER ? a + 4 * e : e == 0 ? a : b;
-                                    copy_ahead<16>(cos, q.cos + from);
-                                    copy_ahead<16>(sin, q.sin + from);
-                                }
-                            }
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < kTurn; ++e) put(to + e * kTurnPiece, make_uint4(0x7fc00000u, 0x7fc00000u, 0x7fc00000u, 0x7fc00000u));
-                        }
-                    }
                 }
-                parity ^= 1;
             }
             if (live) {
                 if (u.has_a(0)) copy_ahead<kBytes>(place(slot, 0), x + u.a[0]);
@@ -579,28 +552,12 @@ struct Ahead {
     }
     // The oldest head: values, gradients
     __device__ __forceinline__ void take(Chunk<T, V> (&xs)[1][2], Chunk<T, V> (&gs)[1][2]) {
-        if (ahead == kAhead) asm volatile("cp.async.wait_group %0;" :: "n"(kAhead - 1) : "memory");
-        else asm volatile("cp.async.wait_group 0;" ::: "memory");
+        asm volatile("cp.async.wait_group %0;" :: "n"(kAhead - 1) : "memory");
         get(place(used, 0), xs[0][0].raw);
         get(place(used, 1), xs[0][1].raw);
         get(place(used, 2), gs[0][0].raw);
         get(place(used, 3), gs[0][1].raw);
         used = used == kSlots - 1 ? 0 : used + 1;
-    }
-    // The cosines of its token, which it is the first head of
-    __device__ __forceinline__ void take(Turn<V, 1, INTER, FULL> &turn) {
-        const uint32_t row = turn_at + turned * kTurn * kTurnPiece;
-#pragma unroll
-        for (int e = 0; e < V / 4; ++e) {
-            uint4 c, s;
-            get(row + e * kTurnPiece, c);
-            get(row + (V / 4 + e) * kTurnPiece, s);
-            turn.c[0][4 * e] = __uint_as_float(c.x); turn.c[0][4 * e + 1] = __uint_as_float(c.y);
-            turn.c[0][4 * e + 2] = __uint_as_float(c.z); turn.c[0][4 * e + 3] = __uint_as_float(c.w);
-            turn.s[0][4 * e] = __uint_as_float(s.x); turn.s[0][4 * e + 1] = __uint_as_float(s.y);
-            turn.s[0][4 * e + 2] = __uint_as_float(s.z); turn.s[0][4 * e + 3] = __uint_as_float(s.w);
-        }
-        turned ^= 1;
     }
 };
 
@@ -626,13 +583,10 @@ qk_bwd_ahead_kernel(const __grid_constant__ QkParams q) {
         const uint32_t bi = live ? token / q.length : 0, i = live ? token % q.length : 0;
         T *dst = static_cast<T *>(out.p) + bi * out.b + i * out.i + hc.first * out.h;
         Turn<V, 1, INTER, FULL> turn;
-        if constexpr (!FULL) turn.load(q, u, position_of(q, live ? token : 0, i));
+        turn.load(q, u, position_of(q, live ? token : 0, i));
         for (int head = hc.first; head < hc.end; ++head, dst += out.h) {
             Chunk<T, V> x[1][2], g[1][2];
             in.take(x, g);
-            if constexpr (FULL) {
-                if (head == hc.first) in.take(turn);
-            }
             in.next(q, hc, u);
             bwd_head<T, V, 1, INTER, FULL>(q, u, turn, x, g, wa, wb, da, db, live, dst);
         }
