@@ -30,8 +30,9 @@ constexpr int kQkMaxDim = 256;
 // (2, 2) - / 210, (1, 2) - / 213, (1, 3) - / 306, (2, 3) - / 361 (spilled registers).  With copies ahead (Ahead, below) the
 // backward pass takes 164 to 178, by where the tensors lie, 6.15 to 5.7 TB/s = 94 to 87 % of the copy bandwidth; heads half of
 // which are rotated 245 -> 165, neighbouring pairs 284 -> 172, heads of 96 elements 233 -> 148, of 80 227 -> 147.  The forward
-// pass, at 6.05 TB/s = 92 %, loses by them (3, 5 or 7 heads ahead: 130, 133, 134; bursts of 4 or 8 heads: 132, 126): its
-// bursts of loads between stores suit the memory better.
+// pass, at 6.05 TB/s = 92 %, loses by them with full lanes (1, 2, 3, 5 heads ahead: 147, 121, 131, 133; bursts of 4 or 8 heads:
+// 132, 126): its bursts of loads between stores suit the memory better.  Other forms gain (2 / 3 heads ahead): heads half of
+// which are rotated 135 -> 113 / 119, of 96 elements 128 -> 103 / 96, of 80 121 -> 97 / 93.
 constexpr int kFwdHeads = 4, kBwdHeads = 2;
 constexpr int kChunkHeads = 8;
 constexpr int kFwdCtasPerSm = 2, kBwdCtasPerSm = 2;
@@ -307,6 +308,31 @@ struct HeadChunk {
     }
 };
 
+// One head of the forward pass; `live`: it exists (all lanes take part in the sum).
+template <typename T, int V, int CU, bool INTER, bool FULL>
+__device__ __forceinline__ void fwd_head(const QkParams &q, const Units<V, CU, FULL> &u, const Turn<V, CU, INTER, FULL> &turn, const Chunk<T, V> (&x)[CU][2],
+                                         const float (&wa)[CU][V], const float (&wb)[CU][V], bool live, T *dst) {
+    float va[CU][V], vb[CU][V], sum[2] = {0.0f, 0.0f};
+#pragma unroll
+    for (int c = 0; c < CU; ++c) {
+        x[c][0].widen(va[c]);
+        x[c][1].widen(vb[c]);
+        vdot<V>(sum, va[c], va[c]);
+        vdot<V>(sum, vb[c], vb[c]);
+    }
+    const float r = rsqrtf(group_sum(sum[0] + sum[1], q.group) * q.inv_dim + q.eps);
+    if (!live) return;
+#pragma unroll
+    for (int c = 0; c < CU; ++c) {
+        vscale<V>(va[c], va[c], r);
+        vscale<V>(vb[c], vb[c], r);
+        vmul<V>(va[c], va[c], wa[c]);
+        vmul<V>(vb[c], vb[c], wb[c]);
+    }
+    turn.template apply<false>(va, vb);
+    store_head<T, V, CU, FULL>(dst, u, va, vb);
+}
+
 template <typename T, int V, int CU, bool INTER, bool FULL>
 __global__ void __launch_bounds__(kQkThreads, kFwdCtasPerSm)
 qk_fwd_kernel(const __grid_constant__ QkParams q) {
@@ -334,25 +360,7 @@ qk_fwd_kernel(const __grid_constant__ QkParams q) {
             for (int j = 0; j < kFwdHeads; ++j) load_head<T, V, CU, FULL>(src + j * in.h, live && head + j < hc.end, u, x[j]);
 #pragma unroll
             for (int j = 0; j < kFwdHeads; ++j) {
-                float va[CU][V], vb[CU][V], sum[2] = {0.0f, 0.0f};
-#pragma unroll
-                for (int c = 0; c < CU; ++c) {
-                    x[j][c][0].widen(va[c]);
-                    x[j][c][1].widen(vb[c]);
-                    vdot<V>(sum, va[c], va[c]);
-                    vdot<V>(sum, vb[c], vb[c]);
-                }
-                const float r = rsqrtf(group_sum(sum[0] + sum[1], q.group) * q.inv_dim + q.eps);
-                if (!live || head + j >= hc.end) continue;
-#pragma unroll
-                for (int c = 0; c < CU; ++c) {
-                    vscale<V>(va[c], va[c], r);
-                    vscale<V>(vb[c], vb[c], r);
-                    vmul<V>(va[c], va[c], wa[c]);
-                    vmul<V>(vb[c], vb[c], wb[c]);
-                }
-                turn.template apply<false>(va, vb);
-                store_head<T, V, CU, FULL>(dst + j * out.h, u, va, vb);
+                fwd_head<T, V, CU, INTER, FULL>(q, u, turn, x[j], wa, wb, live && head + j < hc.end, dst + j * out.h);
             }
         }
     }
@@ -476,17 +484,17 @@ qk_bwd_kernel(const __grid_constant__ QkParams q) {
 
 // What a thread will read of its heads is copied to shared memory ahead of its use, kAhead heads in advance and over the ends
 // of tokens, so that loads are in flight all the time and take no registers.  No thread reads what another one copied.
-// (More heads ahead suit the memory worse: 2, 3, 4, 5 heads 164, 188, 190, 191 us on the shape above, with tensors in one place,
+// (Backward, more heads ahead suit the memory worse: 2, 3, 4, 5 heads 164, 188, 190, 191 us on the shape above, with tensors in one place,
 // 178, 179, 179, 180 in another.)
 template <int BYTES>
 __device__ __forceinline__ void copy_ahead(uint32_t to, const void *from) {
     if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" :: "r"(to), "l"(from) : "memory");
     else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" :: "r"(to), "l"(from) : "memory");
 }
-template <typename T, int V, bool INTER, bool FULL>
+template <typename T, int V, bool INTER, bool FULL, bool BACK>
 struct Ahead {
-    static constexpr int kAhead = 2, kSlots = kAhead + 1;
-    static constexpr int kItem = 4, kBytes = V * sizeof(T);           // pieces of a head (values, gradients); bytes of each
+    static constexpr int kAhead = BACK ? 2 : 3, kSlots = kAhead + 1;
+    static constexpr int kItem = BACK ? 4 : 2, kBytes = V * sizeof(T);   // pieces of a head (values, gradients); bytes of each
     static constexpr uint32_t kPiece = kQkThreads * kBytes;
     static constexpr int kShared = kSlots * kItem * static_cast<int>(kPiece);
     uint32_t at;                                                      // this thread's place in a piece
@@ -519,16 +527,18 @@ struct Ahead {
                 if (live) {
                     const uint32_t bi = token / q.length, i = token % q.length;
                     x = static_cast<const T *>(xt.p) + bi * xt.b + i * xt.i + hc.first * xt.h;
-                    g = static_cast<const T *>(gt.p) + bi * gt.b + i * gt.i + hc.first * gt.h;
+                    if constexpr (BACK) g = static_cast<const T *>(gt.p) + bi * gt.b + i * gt.i + hc.first * gt.h;
                 }
             }
             if (live) {
                 if (u.has_a(0)) copy_ahead<kBytes>(place(slot, 0), x + u.a[0]);
                 if (u.has_b(0)) copy_ahead<kBytes>(place(slot, 1), x + u.b[0]);
-                if (u.has_a(0)) copy_ahead<kBytes>(place(slot, 2), g + u.a[0]);
-                if (u.has_b(0)) copy_ahead<kBytes>(place(slot, 3), g + u.b[0]);
                 x += xt.h;
-                g += gt.h;
+                if constexpr (BACK) {
+                    if (u.has_a(0)) copy_ahead<kBytes>(place(slot, 2), g + u.a[0]);
+                    if (u.has_b(0)) copy_ahead<kBytes>(place(slot, 3), g + u.b[0]);
+                    g += gt.h;
+                }
             }
             slot = slot == kSlots - 1 ? 0 : slot + 1;
             if (++head == heads) {
@@ -551,15 +561,47 @@ struct Ahead {
         asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "r"(from) : "memory");
     }
     // The oldest head: values, gradients
-    __device__ __forceinline__ void take(Chunk<T, V> (&xs)[1][2], Chunk<T, V> (&gs)[1][2]) {
+    __device__ __forceinline__ void take(Chunk<T, V> (&xs)[1][2], Chunk<T, V> (*gs)[2]) {
         asm volatile("cp.async.wait_group %0;" :: "n"(kAhead - 1) : "memory");
         get(place(used, 0), xs[0][0].raw);
         get(place(used, 1), xs[0][1].raw);
-        get(place(used, 2), gs[0][0].raw);
-        get(place(used, 3), gs[0][1].raw);
+        if constexpr (BACK) {
+            get(place(used, 2), gs[0][0].raw);
+            get(place(used, 3), gs[0][1].raw);
+        }
         used = used == kSlots - 1 ? 0 : used + 1;
     }
 };
+
+template <typename T, int V, bool INTER, bool FULL>
+__global__ void __launch_bounds__(kQkThreads, kFwdCtasPerSm)
+qk_fwd_ahead_kernel(const __grid_constant__ QkParams q) {
+    extern __shared__ __align__(16) uint8_t shared[];
+    pdl_launch_dependents();
+    const HeadChunk hc(q);
+    const QkTensor &out = q.out[hc.which];
+    Units<V, 1, FULL> u;
+    u.place(q, threadIdx.x & (q.group - 1), INTER);
+    pdl_wait();
+    Ahead<T, V, INTER, FULL, false> in;
+    in.start(q, hc, u, static_cast<uint32_t>(__cvta_generic_to_shared(shared)));
+    float wa[1][V], wb[1][V];
+    load_weight<V, 1, FULL>(q.weight[hc.which], u, wa, wb);
+    for (uint32_t base = blockIdx.x * (kQkThreads / q.group); base < q.tokens; base += gridDim.x * (kQkThreads / q.group)) {
+        const uint32_t token = base + threadIdx.x / q.group;
+        const bool live = token < q.tokens;
+        const uint32_t bi = live ? token / q.length : 0, i = live ? token % q.length : 0;
+        T *dst = static_cast<T *>(out.p) + bi * out.b + i * out.i + hc.first * out.h;
+        Turn<V, 1, INTER, FULL> turn;
+        turn.load(q, u, position_of(q, live ? token : 0, i));
+        for (int head = hc.first; head < hc.end; ++head, dst += out.h) {
+            Chunk<T, V> x[1][2];
+            in.take(x, nullptr);
+            in.next(q, hc, u);
+            fwd_head<T, V, 1, INTER, FULL>(q, u, turn, x, wa, wb, live, dst);
+        }
+    }
+}
 
 template <typename T, int V, bool INTER, bool FULL>
 __global__ void __launch_bounds__(kQkThreads, kBwdCtasPerSm)
@@ -571,7 +613,7 @@ qk_bwd_ahead_kernel(const __grid_constant__ QkParams q) {
     Units<V, 1, FULL> u;
     u.place(q, threadIdx.x & (q.group - 1), INTER);
     pdl_wait();
-    Ahead<T, V, INTER, FULL> in;
+    Ahead<T, V, INTER, FULL, true> in;
     in.start(q, hc, u, static_cast<uint32_t>(__cvta_generic_to_shared(shared)));
     float wa[1][V], wb[1][V], da[1][V], db[1][V];
     load_weight<V, 1, FULL>(q.weight[hc.which], u, wa, wb);
@@ -646,11 +688,12 @@ cudaError_t launch_qk(const QkParams &q, unsigned x, unsigned y, cudaStream_t st
 }
 template <typename T, int V, int CU, bool INTER, bool FULL>
 cudaError_t launch_fwd(const QkParams &q, unsigned x, unsigned y, cudaStream_t st) {
-    return launch_qk<qk_fwd_kernel<T, V, CU, INTER, FULL>, 0>(q, x, y, st);
+    if constexpr (V > 1 && !FULL) return launch_qk<qk_fwd_ahead_kernel<T, V, INTER, FULL>, Ahead<T, V, INTER, FULL, false>::kShared>(q, x, y, st);
+    else return launch_qk<qk_fwd_kernel<T, V, CU, INTER, FULL>, 0>(q, x, y, st);
 }
 template <typename T, int V, int CU, bool INTER, bool FULL>
 cudaError_t launch_bwd_qk(const QkParams &q, unsigned x, unsigned y, cudaStream_t st) {
-    if constexpr (V > 1) return launch_qk<qk_bwd_ahead_kernel<T, V, INTER, FULL>, Ahead<T, V, INTER, FULL>::kShared>(q, x, y, st);
+    if constexpr (V > 1) return launch_qk<qk_bwd_ahead_kernel<T, V, INTER, FULL>, Ahead<T, V, INTER, FULL, true>::kShared>(q, x, y, st);
     else return launch_qk<qk_bwd_kernel<T, V, CU, INTER, FULL>, 0>(q, x, y, st);
 }
 // [dtype][interleaved][variant]: 16-byte pieces with full lanes, 16-byte pieces, 8-byte pieces of the 16-bit types, single
