@@ -30,9 +30,10 @@ constexpr int kQkMaxDim = 256;
 // (2, 2) - / 210, (1, 2) - / 213, (1, 3) - / 306, (2, 3) - / 361 (spilled registers).  With copies ahead (Ahead, below) the
 // backward pass takes 164 to 178, by where the tensors lie, 6.15 to 5.7 TB/s = 94 to 87 % of the copy bandwidth; heads half of
 // which are rotated 245 -> 165, neighbouring pairs 284 -> 172, heads of 96 elements 233 -> 148, of 80 227 -> 147.  The forward
-// pass, at 6.05 TB/s = 92 %, loses by them with full lanes (1, 2, 3, 5 heads ahead: 147, 121, 131, 133; bursts of 4 or 8 heads:
-// 132, 126): its bursts of loads between stores suit the memory better.  Other forms gain (2 / 3 heads ahead): heads half of
-// which are rotated 135 -> 113 / 119, of 96 elements 128 -> 103 / 96, of 80 121 -> 97 / 93.
+// pass of 16-bit types, at 6.05 TB/s = 92 %, loses by them with full lanes (1, 2, 3, 5 heads ahead: 147, 121, 131, 133; bursts of
+// 4 or 8 heads: 132, 126): its bursts of loads between stores suit the memory better.  Binary32 gains with 2 heads ahead,
+// 235 -> 215 = 95 % (3: 236), and so do the forms without full lanes (2 / 3 heads ahead): heads half of which are rotated
+// 135 -> 113 / 119, of 96 elements 128 -> 103 / 96, of 80 121 -> 97 / 93.
 constexpr int kFwdHeads = 4, kBwdHeads = 2;
 constexpr int kChunkHeads = 8;
 constexpr int kFwdCtasPerSm = 2, kBwdCtasPerSm = 2;
@@ -493,7 +494,7 @@ __device__ __forceinline__ void copy_ahead(uint32_t to, const void *from) {
 }
 template <typename T, int V, bool INTER, bool FULL, bool BACK>
 struct Ahead {
-    static constexpr int kAhead = BACK ? 2 : 3, kSlots = kAhead + 1;
+    static constexpr int kAhead = BACK || FULL ? 2 : 3, kSlots = kAhead + 1;
     static constexpr int kItem = BACK ? 4 : 2, kBytes = V * sizeof(T);   // pieces of a head (values, gradients); bytes of each
     static constexpr uint32_t kPiece = kQkThreads * kBytes;
     static constexpr int kShared = kSlots * kItem * static_cast<int>(kPiece);
@@ -688,7 +689,7 @@ cudaError_t launch_qk(const QkParams &q, unsigned x, unsigned y, cudaStream_t st
 }
 template <typename T, int V, int CU, bool INTER, bool FULL>
 cudaError_t launch_fwd(const QkParams &q, unsigned x, unsigned y, cudaStream_t st) {
-    if constexpr (V > 1 && !FULL) return launch_qk<qk_fwd_ahead_kernel<T, V, INTER, FULL>, Ahead<T, V, INTER, FULL, false>::kShared>(q, x, y, st);
+    if constexpr (V > 1 && (!FULL || sizeof(T) == 4)) return launch_qk<qk_fwd_ahead_kernel<T, V, INTER, FULL>, Ahead<T, V, INTER, FULL, false>::kShared>(q, x, y, st);
     else return launch_qk<qk_fwd_kernel<T, V, CU, INTER, FULL>, 0>(q, x, y, st);
 }
 template <typename T, int V, int CU, bool INTER, bool FULL>
