@@ -770,6 +770,9 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             if (lane == 0) barrier_arrive(bar(qDs));
         }
         const float row_drift = single ? 0.0f : over_parts(drift);
+        // A row of one key has P = 1 and dS = 0 whatever its score: what the recomputed P leaves of dS is rounding and nothing
+        // else.  (Times 0: a NaN stays one.)
+        const float factor = seen == 1 ? 0.0f : p.scale;
         if (ok) ok = wait(qDone, 0);
         fence_after();
         T *row = static_cast<T *>(p.dq.p) + (live ? row_of(w, p.dq, w.head, i, w.q_first) : 0);
@@ -785,7 +788,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
                     if constexpr (DIM == 128) tmem_ld32(tm_dq + my_lane + 32 * part, o);
                     else tmem_ld16(tm_dq + my_lane + 16 * part, o);
                     wait_ld(o);
-                    if (live) store_columns<T, DIM / 4>(row, part * (DIM / 4), p.dim, o, p.scale);
+                    if (live) store_columns<T, DIM / 4>(row, part * (DIM / 4), p.dim, o, factor);
                 } else if (live && part == 0) {
                     zero_columns<T>(row, p.dim);
                 }
@@ -821,7 +824,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
                 uint32_t y[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[e] = __float_as_uint(v[e]);
-                if (live) store_columns<T, 8>(row, col, p.dim, y, p.scale);
+                if (live) store_columns<T, 8>(row, col, p.dim, y, factor);
             }
             cluster_sync();                                           // nobody's shared memory goes before it has been read
         }
@@ -1066,6 +1069,13 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             }
 #pragma unroll
             for (int c = 0; c < 16; ++c) out[c] = pack2<T>(prob[2 * c], prob[2 * c + 1]);
+            if (p.causal && k0 == 0 && reach <= 0 && -reach - q0 >= 0 && -reach - q0 < kTile) {
+                // the one row that sees key 0 alone: its P is 1 and its dS 0, as in the dQ kernel
+                const int lone = -reach - q0 - 32 * part - 2 * (lane % 4);
+#pragma unroll
+                for (int x = 0; x < 32; ++x)
+                    if (8 * (x / 4 % 4) + x % 2 == lone) prob[x] = 0.0f;
+            }
             ok = j == 0 || wait(kDsUsed, (j - 1) & 1);
             if (!ok) break;
             fence_after();
@@ -1118,7 +1128,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
         const int which = part & 1, half = part >> 1, r = threadIdx.x & 127;
         const bool live = row_key < w.k_len;
         const Rows &to = which == 0 ? p.dv : p.dk;
-        const float factor = which == 0 ? 1.0f : p.scale;
+        const float factor = which == 0 ? 1.0f : w.k_len == 1 ? 0.0f : p.scale;   // (rows of one key have no dS)
         const uint32_t from = (which == 0 ? tm_dv : tm_dk) + my_lane;
         T *row = static_cast<T *>(to.p) + (live ? row_of(w, to, w.head, row_key, w.k_first) : 0);
         if (p.split == 1) {

@@ -1,0 +1,72 @@
+"""Attention where it meets an edge: rows of one key, memory that belongs to no sequence, gradients of scores far apart, values
+that are not a number, no heads."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import paper_2202_00441_b200 as fb
+import test_attention as ta
+from paper_2202_00441_b200 import operators as ops
+
+pytestmark = pytest.mark.gpu
+NAN = float("nan")
+
+
+# ---- rows that see one key: P = 1 whatever the score, so dS, dQ and their share of dK are exactly zero ---------------------
+ONE_KEY = [
+    # b, n, m, h, hk, d, causal, dtype
+    (1, 1, 1, 1, 1, 64, True, torch.bfloat16),
+    (3, 1, 1, 8, 2, 128, False, torch.float16),
+    (3, 2035, 1, 6, 2, 64, True, torch.bfloat16),                 # only the last row sees the key
+    (2, 322, 1, 4, 1, 96, False, torch.bfloat16),
+    (2, 257, 257, 4, 2, 128, True, torch.bfloat16),               # row 0 of a causal sequence
+    (1, 300, 40, 2, 1, 64, True, torch.float16),                  # row 260
+    (1, 2100, 2100, 2, 1, 128, True, torch.bfloat16),             # tiles shared by clusters
+    (1, 1500, 1500, 6, 1, 72, True, torch.float16),
+]
+
+
+@pytest.mark.parametrize("case", ONE_KEY, ids=lambda c: "x".join(map(str, c[:6])) + f"_{'causal' if c[6] else 'full'}_{str(c[7])[6:]}")
+def test_rows_of_one_key_have_no_score_gradient(case):
+    b, n, m, h, hk, d, causal, dtype = case
+    q, k, v, g = ta.make(b, n, m, h, hk, d, dtype, seed=11)
+    q = q * 8                                                     # scores of tens: the recomputed P is off by the most
+    alone = torch.full((n,), m == 1, device="cuda")
+    if causal:
+        alone = (torch.arange(n, device="cuda") + m - n + 1).clamp(max=m) == 1
+    assert alone.any()
+    out, lse = fb.fewbit_attention_fwd(q, k, v, causal=causal)
+    dq, dk, dv = fb.fewbit_attention_bwd(g, q, k, v, out, lse, causal=causal)
+    assert (dq[:, alone] == 0).all()
+    if m == 1:
+        assert (dk == 0).all()
+    g = g * alone[:, None, None]                                  # only those rows: nothing reaches dK, and key 0 has dV
+    dq, dk, dv = fb.fewbit_attention_bwd(g, q, k, v, out, lse, causal=causal)
+    assert (dq == 0).all() and (dk == 0).all()
+    want = g.double().sum(1).view(b, hk, h // hk, d).sum(2)
+    size = g.double().abs().sum(1).view(b, hk, h // hk, d).sum(2)
+    assert ((dv[:, 0].double() - want).abs() <= 1.05 * ta.E[dtype] * (want.abs() + 2.0 ** -7 * size) + ta.TINY[dtype]).all()
+    assert (dv[:, 1:] == 0).all()
+
+
+def test_packed_sequences_of_one_token_have_no_score_gradient():
+    n = 70
+    q, k, v, g = (x[0] for x in ta.make(1, n, n, 4, 2, 64, torch.bfloat16, seed=12))
+    off = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    kw = dict(q_offsets=off, k_offsets=off, max_q_len=1, max_k_len=1)
+    for causal in (False, True):
+        out, lse = fb.fewbit_attention_fwd(q, k, v, causal=causal, **kw)
+        dq, dk, dv = fb.fewbit_attention_bwd(g, q, k, v, out, lse, causal=causal, **kw)
+        assert (dq == 0).all() and (dk == 0).all()
+        assert torch.equal(out, v.repeat_interleave(2, 1))
+
+
+def test_a_gradient_that_is_not_finite_shows_in_rows_of_one_key():
+    q, k, v, g = ta.make(1, 4, 1, 2, 2, 64, torch.bfloat16, seed=13)
+    g[0, 2, 1, 5] = NAN
+    out, lse = fb.fewbit_attention_fwd(q, k, v)
+    dq, dk, dv = fb.fewbit_attention_bwd(g, q, k, v, out, lse)
+    assert dq[0, 2, 1].isnan().all() and dk[0, 0, 1].isnan().all() and dv[0, 0, 1, 5].isnan()
+    assert (dq[0, :, 0] == 0).all() and (dk[0, 0, 0] == 0).all()
