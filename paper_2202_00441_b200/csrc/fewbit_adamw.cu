@@ -29,9 +29,9 @@ namespace {
 constexpr int kBlock = FEWBIT_ADAMW_BLOCK;
 // CTAs on an SM.  Measured: binary32 with 32-bit moments, 8 layers of width 640 and 1999 words (1.14 GB moved), 189 us = 6.0
 // TB/s, 92 % of the copy bandwidth, where memory bounds it (3 and 5 CTAs: 195 and 202); bfloat16 with a master copy and 8-bit
-// moments, 24 layers of width 1280 and 32003 words (8.24 GB), 1590 us = 5.2 TB/s, 79 %: 650 instructions for a warp's
-// block keep 69 % of the issue slots busy, most of them for the codes and their noise.  Copying a warp's next block to shared
-// memory meanwhile costs more instructions than the waits it saves: 1740 (with 3 CTAs 1630).
+// moments, 24 layers of width 1280 and 32003 words (8.24 GB), 1750 us = 4.7 TB/s, 72 %: 650 instructions for a warp's
+// block keep 68 % of the issue slots busy, most of them for the codes, their noise and the roots.  Copying a warp's next block to
+// shared memory meanwhile costs more instructions than the waits it saves (8 to 9 %, with 3 CTAs 2 to 3 %).
 constexpr int kAdamThreads = 256, kAdamCtas = 4;
 
 struct AdamTensor {
@@ -89,30 +89,6 @@ __device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c
 __device__ __forceinline__ uint32_t high_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
 }
-// Roots of 8 values, correctly rounded (their codes must not depend on how they were computed).  From 2^-100 on: s = v / sqrt(v)
-// from an approximate inverse root, then one Newton step whose residual v - s^2 a fused multiply-add gives exactly; equal to
-// the rounded root for every one of these binary32 values.  Smaller ones (zero among them), infinities and NaN take the
-// library's root, for the whole lane: a fifth of the instructions of eight of them is what the others need.
-__device__ __forceinline__ void roots(const float (&v)[8], float (&r)[8]) {
-    bool other = false;
-#pragma unroll
-    for (int e = 0; e < 8; e += 2) {
-        float y0, y1, s0, s1, e0, e1;
-        asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y0) : "f"(v[e]));
-        asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y1) : "f"(v[e + 1]));
-        mul2(s0, s1, v[e], v[e + 1], y0, y1);
-        fma2(e0, e1, s0, s1, s0, s1, -v[e], -v[e + 1]);
-        mul2(y0, y1, y0, y1, -0.5f, -0.5f);
-        fma2(r[e], r[e + 1], e0, e1, y0, y1, s0, s1);
-        other |= __float_as_uint(v[e]) - 0x0d800000u >= 0x72000000u;
-        other |= __float_as_uint(v[e + 1]) - 0x0d800000u >= 0x72000000u;
-    }
-    if (other) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) r[e] = __fsqrt_rn(v[e]);
-    }
-}
-
 __device__ __forceinline__ float max_nan(float a, float b) {          // NaN if one of them is
     float d;
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
@@ -208,9 +184,9 @@ __device__ __forceinline__ void update_block(const AdamTensor &t, const AdamScal
         v[e] = __fadd_rn(x0, y0);
         v[e + 1] = __fadd_rn(x1, y1);
     }
-    roots(v, r);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
+        r[e] = __fsqrt_rn(v[e]);                                  // (correctly rounded: codes must not depend on how it is computed)
         // (two ulp of the update: far below the parameter's own rounding)
         p[e] = fmaf(p[e], s.keep, -s.step_size * __fdividef(m[e], fmaf(r[e], s.inv_root_bc2, s.eps)));
         if constexpr (EIGHT) {
