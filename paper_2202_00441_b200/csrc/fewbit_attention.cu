@@ -161,8 +161,8 @@ int choose_split(int64_t sms, int64_t tiles, int64_t longest, bool causal, int m
 }
 
 fewbit_status run(attn::Kernel which, const fewbit_attention_shape *s, Params &p, int64_t tiles, int heads, void *stream) {
-    p.tiles = static_cast<int>(tiles);
-    const unsigned grid = static_cast<unsigned>(tiles * heads * (s->batch + (p.q_offsets != nullptr)));   // one more for rows of no sequence
+    p.tiles = static_cast<int>(p.q_offsets != nullptr && tiles == 0 ? 1 : tiles);   // packed rows of no sequence are there without any tile
+    const unsigned grid = static_cast<unsigned>(static_cast<int64_t>(p.tiles) * heads * (s->batch + (p.q_offsets != nullptr)));   // one more for rows of no sequence
     if (grid == 0) return FEWBIT_OK;
     const cudaError_t err = (s->dtype == FEWBIT_F16 ? attn::launch_f16 : attn::launch_bf16)(which, s->head_dim > 64, p, grid, static_cast<cudaStream_t>(stream));
     if (err == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
@@ -179,7 +179,7 @@ fewbit_status fewbit_attention_fwd(const fewbit_attention_shape *s, const fewbit
     using namespace fewbit;
     Sizes z;
     if (const fewbit_status st = check_shape(s, &z); st != FEWBIT_OK) return st;
-    if (s->batch == 0 || s->heads == 0 || z.q_rows == 0 || s->q_len == 0) return FEWBIT_OK;
+    if (z.batch == 0 || s->heads == 0 || z.q_rows == 0) return FEWBIT_OK;
     for (const fewbit_heads *t : {q, out})
         if (const fewbit_status st = check_tensor(t, z.q_rows, s->heads, z.batch); st != FEWBIT_OK) return st;
     for (const fewbit_heads *t : {k, v})
@@ -213,7 +213,7 @@ fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *s, const fewbit
     using namespace fewbit;
     Sizes z;
     if (const fewbit_status st = check_shape(s, &z); st != FEWBIT_OK) return st;
-    if (s->batch == 0 || s->heads == 0 || (z.q_rows == 0 && z.k_rows == 0)) return FEWBIT_OK;
+    if (z.batch == 0 || s->heads == 0 || (z.q_rows == 0 && z.k_rows == 0)) return FEWBIT_OK;
     for (const fewbit_heads *t : {grad_out, q, out, grad_q})
         if (const fewbit_status st = check_tensor(t, z.q_rows, s->heads, z.batch); st != FEWBIT_OK) return st;
     for (const fewbit_heads *t : {k, v, grad_k, grad_v})
@@ -237,11 +237,11 @@ fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *s, const fewbit
     p.dv = rows_of(grad_v);
     p.lse = const_cast<float *>(lse);
     p.stat = static_cast<float *>(workspace);
-    p.after_dq = s->q_len > 0;
+    p.after_dq = some;
     const int64_t row_tiles = (s->q_len + attn::kTile - 1) / attn::kTile, key_tiles = (s->k_len + attn::kTile - 1) / attn::kTile;
     p.split = choose_split(p.sms, row_tiles * s->heads * s->batch, key_tiles, p.causal, s->head_dim > 64 ? 8 : 4, kDqEnds);
-    st = run(attn::Kernel::dq, s, p, row_tiles, s->heads, stream);
-    if (st != FEWBIT_OK) return st;
+    if (some) st = run(attn::Kernel::dq, s, p, row_tiles, s->heads, stream);
+    if (st != FEWBIT_OK || z.k_rows == 0) return st;
     p.split = choose_split(p.sms, key_tiles * s->kv_heads * s->batch, row_tiles * p.group, p.causal, 4, kDkvEnds);
     return run(attn::Kernel::dkv, s, p, key_tiles, s->kv_heads, stream);
 }

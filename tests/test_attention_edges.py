@@ -70,3 +70,48 @@ def test_a_gradient_that_is_not_finite_shows_in_rows_of_one_key():
     dq, dk, dv = fb.fewbit_attention_bwd(g, q, k, v, out, lse)
     assert dq[0, 2, 1].isnan().all() and dk[0, 0, 1].isnan().all() and dv[0, 0, 1, 5].isnan()
     assert (dq[0, :, 0] == 0).all() and (dk[0, 0, 0] == 0).all()
+
+
+# ---- every row of a packed tensor is written --------------------------------------------------------------------------------
+def _h(t):
+    return ctypes.byref(ops._Heads(t.data_ptr(), 0, t.stride(0), t.stride(1)))
+
+
+def packed_call(q_offsets, k_offsets, max_q, max_k, rows=150, keys=90, h=4, hk=2, d=64, causal=False):
+    """Forward and backward pass through the C ABI into buffers full of NaN."""
+    lib = fb.load_library()
+    q, k, v, g = ta.make(1, rows, keys, h, hk, d, torch.bfloat16, seed=14)
+    q, k, v, g = q[0], k[0], v[0], g[0]
+    qo, ko = (torch.tensor(o, dtype=torch.int32, device="cuda") for o in (q_offsets, k_offsets))
+    out, dq, dk, dv = (torch.full_like(t, NAN) for t in (q, q, k, v))
+    lse = torch.full((h, rows), NAN, device="cuda")
+    s = ops._AttentionShape(batch=len(q_offsets) - 1, heads=h, kv_heads=hk, head_dim=d, q_len=max_q, k_len=max_k, q_rows=rows, k_rows=keys,
+                            q_offsets=qo.data_ptr(), k_offsets=ko.data_ptr(), causal=causal, scale=d ** -0.5, dtype=1)
+    stream = torch.cuda.current_stream().cuda_stream
+    assert lib.fewbit_attention_fwd(ctypes.byref(s), _h(q), _h(k), _h(v), _h(out), lse.data_ptr(), stream) == 0
+    bytes_ = lib.fewbit_attention_workspace_bytes(ctypes.byref(s))
+    ws = torch.full((bytes_ // 4 + 4,), NAN, device="cuda")
+    assert lib.fewbit_attention_bwd(ctypes.byref(s), _h(g), _h(q), _h(k), _h(v), _h(out), lse.data_ptr(), _h(dq), _h(dk), _h(dv), ws.data_ptr(),
+                                    bytes_, stream) == 0
+    torch.cuda.synchronize()
+    return (q, k, v, g), dict(out=out, lse=lse, dq=dq, dk=dk, dv=dv)
+
+
+@pytest.mark.parametrize("offsets", [([0], [0]), ([40], [17]), ([5, 5, 5], [0, 0, 0]), ([0, 0], [90, 90])], ids=str)
+@pytest.mark.parametrize("lens", [(0, 0), (150, 90), (0, 90), (150, 0)], ids=str)
+def test_tensors_without_a_sequence_are_zeroed(offsets, lens):
+    _, r = packed_call(*offsets, *lens)
+    assert (r["lse"] == -math.inf).all()
+    for name in ("out", "dq", "dk", "dv"):
+        assert (r[name] == 0).all(), name
+
+
+@pytest.mark.parametrize("lens", [(0, 90), (150, 0), (0, 0)], ids=str)
+def test_a_bound_of_zero_on_one_side_leaves_nothing_unwritten(lens):
+    """Sequences on the other side only: rows that see no key, keys that no row sees."""
+    q_offsets = [0, 0, 0] if lens[0] == 0 else [10, 100, 150]
+    k_offsets = [0, 0, 0] if lens[1] == 0 else [3, 50, 90]
+    _, r = packed_call(q_offsets, k_offsets, *lens)
+    assert (r["lse"] == -math.inf).all()
+    for name in ("out", "dq", "dk", "dv"):
+        assert (r[name] == 0).all(), name
