@@ -351,10 +351,11 @@ FEWBIT_API fewbit_status fewbit_qk_norm_rope_bwd(const fewbit_qk_shape *shape, c
  *                   of q and keys [k_offsets[b], k_offsets[b+1]) of k and v,
  *                   in tensors of q_rows and k_rows rows (batch_stride is not
  *                   used); q_len and k_len are then upper bounds of the
- *                   sequences' lengths.  Rows in front of the first and behind
- *                   the last sequence get zeros (lse: -inf).
- *                   Offsets are clamped to [0, q_rows] / [0, k_rows], lengths to
- *                   [0, q_len] / [0, k_len].
+ *                   sequences' lengths.  Offsets are clamped to [0, q_rows] /
+ *                   [0, k_rows], lengths to [0, q_len] / [0, k_len].  Rows in
+ *                   front of the first and behind the last sequence, and those
+ *                   of a sequence past its clamped length, belong to none: they
+ *                   get zeros (lse: -inf).
  *   scale           finite, > 0
  * lse: (batch, heads, q_len), or (heads, q_rows) for packed sequences.
  * A row that sees no key has out = 0, lse = -inf and zero gradients.

@@ -167,17 +167,21 @@ __device__ __forceinline__ float *stat_block(const Params &p, const Work &w, int
                                   : (static_cast<long long>(w.batch) * p.heads + head) * ((p.q_len + kTile - 1) / kTile) + tile;
     return p.stat + at * (kStatBytes / 4);
 }
-// Packed sequences: rows in front of the first and behind the last one are zero in every output, their lse -inf.
-// The CTAs of the extra sequence share them.
+// Packed sequences: rows in front of the first and behind the last one, and those of a sequence past the bound of its
+// length, are zero in every output, their lse -inf.  The CTAs of the extra sequence share them.
 template <typename T>
-__device__ __forceinline__ void fill_outside(const Params &p, const Work &w, const int *offsets, long long rows, const Rows &t, float *lse) {
-    const long long first = min(max(static_cast<long long>(offsets[0]), 0ll), rows);
-    const long long last = min(max(static_cast<long long>(offsets[p.batch]), first), rows);
-    for (long long i = static_cast<long long>(w.tile) * kThreadsAttn + threadIdx.x; i < first + rows - last;
-         i += static_cast<long long>(p.tiles) * kThreadsAttn) {
-        const long long row = i < first ? i : last + (i - first);
+__device__ __forceinline__ void fill_outside(const Params &p, const Work &w, const int *offsets, long long rows, int longest, const Rows &t, float *lse) {
+    auto clear = [&](long long row) {
         zero_columns<T>(static_cast<T *>(t.p) + row * t.i + w.head * t.h, p.dim);
         if (lse != nullptr) lse[static_cast<long long>(w.head) * rows + row] = -INFINITY;
+    };
+    const long long start = static_cast<long long>(w.tile) * kThreadsAttn + threadIdx.x, step = static_cast<long long>(p.tiles) * kThreadsAttn;
+    const long long first = min(max(static_cast<long long>(offsets[0]), 0ll), rows);
+    const long long last = min(max(static_cast<long long>(offsets[p.batch]), first), rows);
+    for (long long i = start; i < first + rows - last; i += step) clear(i < first ? i : last + (i - first));
+    for (long long b = start; b < p.batch; b += step) {               // a thread for each sequence: longer ones than announced are rare
+        const long long from = min(max(static_cast<long long>(offsets[b]), 0ll), rows), end = min(static_cast<long long>(offsets[b + 1]), rows);
+        for (long long i = from + longest; i < end; ++i) clear(i);
     }
 }
 
@@ -264,7 +268,7 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
     const int rank = p.split > 1 ? static_cast<int>(cluster_rank()) : 0;
     const Work w = find_work(p, blockIdx.x / p.split, p.heads, true);
     if (w.packed && w.batch == p.batch) {                             // (the whole cluster)
-        if (rank == 0) fill_outside<T>(p, w, p.q_offsets, p.q_rows, p.out, p.lse);
+        if (rank == 0) fill_outside<T>(p, w, p.q_offsets, p.q_rows, p.q_len, p.out, p.lse);
         return;
     }
     const int q0 = w.tile * 2 * kTile;
@@ -559,7 +563,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
     const int rank = p.split > 1 ? static_cast<int>(cluster_rank()) : 0;
     const Work w = find_work(p, blockIdx.x / p.split, p.heads, true);
     if (w.packed && w.batch == p.batch) {                             // (the whole cluster)
-        if (rank == 0) fill_outside<T>(p, w, p.q_offsets, p.q_rows, p.dq, nullptr);
+        if (rank == 0) fill_outside<T>(p, w, p.q_offsets, p.q_rows, p.q_len, p.dq, nullptr);
         return;
     }
     const int q0 = w.tile * kTile;
@@ -863,8 +867,8 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
     const Work w = find_work(p, blockIdx.x / p.split, p.kv_heads, false);
     if (w.packed && w.batch == p.batch) {                             // (the whole cluster)
         if (rank == 0) {
-            fill_outside<T>(p, w, p.k_offsets, p.k_rows, p.dk, nullptr);
-            fill_outside<T>(p, w, p.k_offsets, p.k_rows, p.dv, nullptr);
+            fill_outside<T>(p, w, p.k_offsets, p.k_rows, p.k_len, p.dk, nullptr);
+            fill_outside<T>(p, w, p.k_offsets, p.k_rows, p.k_len, p.dv, nullptr);
         }
         pdl_wait();
         return;

@@ -115,3 +115,20 @@ def test_a_bound_of_zero_on_one_side_leaves_nothing_unwritten(lens):
     assert (r["lse"] == -math.inf).all()
     for name in ("out", "dq", "dk", "dv"):
         assert (r[name] == 0).all(), name
+
+
+@pytest.mark.parametrize("causal", [False, True])
+def test_rows_past_the_length_bounds_are_zeroed(causal):
+    """Sequences longer than max_q_len or max_k_len end there; what lies behind belongs to no sequence."""
+    qo, ko, most_q, most_k = [2, 202, 262, 400], [1, 141, 146, 390], 128, 100
+    x, r = packed_call(qo, ko, most_q, most_k, rows=420, keys=400, causal=causal)
+    q, k, v, g = x
+    inside_q, inside_k = torch.zeros(420, dtype=torch.bool, device="cuda"), torch.zeros(400, dtype=torch.bool, device="cuda")
+    for i in range(3):
+        a = slice(qo[i], min(qo[i + 1], qo[i] + most_q))
+        c = slice(ko[i], min(ko[i + 1], ko[i] + most_k))
+        inside_q[a], inside_k[c] = True, True
+        ta.compare(q[a], k[c], v[c], g[a], {"out": r["out"][a], "lse": r["lse"][:, a], "dq": r["dq"][a], "dk": r["dk"][c], "dv": r["dv"][c]}, causal, 0.125)
+    assert (r["lse"][:, ~inside_q] == -math.inf).all()
+    for name, inside in (("out", inside_q), ("dq", inside_q), ("dk", inside_k), ("dv", inside_k)):
+        assert (r[name][~inside] == 0).all(), name
