@@ -341,7 +341,8 @@ FEWBIT_API fewbit_status fewbit_qk_norm_rope_bwd(const fewbit_qk_shape *shape, c
  *   dtype           FEWBIT_BF16 or FEWBIT_F16 (products with binary32 sums on
  *                   the tensor cores; the probabilities and their gradients
  *                   are rounded to `dtype` as operands of the second products)
- *   heads, kv_heads query head h reads key head h / (heads / kv_heads)
+ *   heads, kv_heads query head h reads key head h / (heads / kv_heads); without query heads
+ *                   a call reads and writes nothing
  *   head_dim        a multiple of 8, 8 .. 128
  *   causal          row i of a sequence sees keys j <= i + k_len - q_len (the
  *                   last row sees every key)

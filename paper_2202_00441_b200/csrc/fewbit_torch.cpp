@@ -192,7 +192,11 @@ std::tuple<Tensor, Tensor, Tensor> attention_bwd(const Tensor &g, const Tensor &
     if (lse.sizes() != at::IntArrayRef(a.stats) || lse.scalar_type() != at::kFloat || lse.device() != q.device() || !lse.is_contiguous())
         refuse("lse must be what the forward pass gave");
     const c10::cuda::OptionalCUDAGuard guard(q.device());
-    Tensor dq = at::empty(q.sizes(), q.options()), dk = at::empty(k.sizes(), k.options()), dv = at::empty(v.sizes(), v.options());
+    // without query heads the library has nothing to do, and the sums over them are zero
+    const bool none = a.s.heads == 0;
+    Tensor dq = at::empty(q.sizes(), q.options());
+    Tensor dk = none ? at::zeros(k.sizes(), k.options()) : at::empty(k.sizes(), k.options());
+    Tensor dv = none ? at::zeros(v.sizes(), v.options()) : at::empty(v.sizes(), v.options());
     const size_t bytes = fewbit_attention_workspace_bytes(&a.s);
     Tensor ws = at::empty({static_cast<int64_t>(bytes)}, q.options().dtype(at::kByte));
     const fewbit_heads h[8] = {heads_of(g), heads_of(q), heads_of(k), heads_of(v), heads_of(out), heads_of(dq), heads_of(dk), heads_of(dv)};

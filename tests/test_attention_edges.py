@@ -132,3 +132,13 @@ def test_rows_past_the_length_bounds_are_zeroed(causal):
     assert (r["lse"][:, ~inside_q] == -math.inf).all()
     for name, inside in (("out", inside_q), ("dq", inside_q), ("dk", inside_k), ("dv", inside_k)):
         assert (r[name][~inside] == 0).all(), name
+
+
+def test_without_query_heads_the_key_gradients_are_zero():
+    kv = torch.randn(2, 300, 2, 64, device="cuda").bfloat16()
+    q = kv.new_empty(2, 300, 0, 64)
+    out, lse = fb.fewbit_attention_fwd(q, kv, kv)
+    full = [torch.full_like(kv, NAN) for _ in range(4)]           # what an allocation of that size finds
+    del full
+    dq, dk, dv = fb.fewbit_attention_bwd(q, q, kv, kv, out, lse)
+    assert dq.shape == q.shape and (dk == 0).all() and (dv == 0).all()
