@@ -420,8 +420,10 @@ FEWBIT_API fewbit_status fewbit_attention_timeout_count(uint64_t *count);
  * Each product and sum of the moments is rounded to binary32 by itself, so the
  * codes follow from the inputs and the seed alone.
  * The 16 + 16 random bits of an element are a hash of `seed` and of its place
- * in the call (tensors in order, each taking a whole number of blocks); give
- * every step its own seed.  A positive second moment never becomes zero.  A
+ * in the call (tensors in order, each taking a whole number of blocks):
+ * place * 0x9E3779B1 + seed is what is hashed, so seeds that differ by a small
+ * multiple of that constant give the same bits a few places apart.  Give every
+ * step a seed of its own that is no count but a hash of one.  A positive second moment never becomes zero.  A
  * block with a non-finite value gets a NaN scale: it reads back as NaN.  A
  * block whose largest magnitude is below 2^-126 reads back as zero.
  * Moments of 32 bits: exp_avg = m, exp_avg_sq = v, binary32; no scales.

@@ -187,7 +187,7 @@ def fewbit_adamw_step(tensors, grads: Sequence[torch.Tensor], *, step: int, lr: 
                       stream: Optional[torch.cuda.Stream] = None) -> None:
     """One AdamW step on all parameters of ``tensors``, in place.  ``grads``: contiguous tensors of the parameters' dtype.
     ``grad_scale``: one float32 value on the device that multiplies every gradient.  ``seed``: 32 bits for the
-    stochastic rounding of 8-bit moments, a new value each step."""
+    stochastic rounding of 8-bit moments, a new value each step (unrelated to the last one's, as a hash gives it)."""
     if stream is not None:
         with _On(stream, grad_scale, *grads, *tensors.tensors()):
             tensors.step(grads, step, lr, betas[0], betas[1], eps, weight_decay, seed & 0xFFFFFFFF, grad_scale)

@@ -6,6 +6,24 @@ import torch
 from .operators import ADAMW_BLOCK, fewbit_adamw_create, fewbit_adamw_step
 
 
+def _mix(x: int) -> int:
+    """The 64-bit finaliser of SplitMix64 (Steele, Lea and Flood, Fast splittable pseudorandom number generators, 2014)."""
+    x = (x + 0x9E3779B97F4A7C15) & 0xFFFFFFFFFFFFFFFF
+    x = ((x ^ (x >> 30)) * 0xBF58476D1CE4E5B9) & 0xFFFFFFFFFFFFFFFF
+    x = ((x ^ (x >> 27)) * 0x94D049BB133111EB) & 0xFFFFFFFFFFFFFFFF
+    return x ^ (x >> 31)
+
+
+def _noise_seed(*parts: int) -> int:
+    """32 bits for one call's stochastic rounding.  The library's noise for a place is a hash of place * odd constant + seed: all
+    seeds' noise is one sequence of 2^32 values that starts at different places.  A seed that grew by a fixed amount each step
+    would start next to the last one's; mixed ones start anywhere."""
+    x = 0
+    for part in parts:
+        x = _mix(x ^ (part & 0xFFFFFFFFFFFFFFFF))
+    return x >> 32
+
+
 class FewBitAdamW(torch.optim.Optimizer):
     """Drop-in for ``torch.optim.AdamW`` on CUDA parameters of float32, bfloat16 or float16.
 
@@ -85,9 +103,9 @@ class FewBitAdamW(torch.optim.Optimizer):
                 if held is None or held[0] != where:
                     held = self._handles[(number, device, dtype)] = (where, fewbit_adamw_create(params, *lists, masters))
                 grads = [p.grad.to(dtype).contiguous() for p in params]
-                seed = (self.seed + 0x9E3779B1 * (step + 1) + 0x85EBCA6B * (64 * number + place)) & 0xFFFFFFFF
                 fewbit_adamw_step(held[1], grads, step=step + 1, lr=float(group["lr"]), betas=group["betas"], eps=group["eps"],
-                                  weight_decay=group["weight_decay"], seed=seed, grad_scale=grad_scale)
+                                  weight_decay=group["weight_decay"], seed=_noise_seed(self.seed, step + 1, number, place),
+                                  grad_scale=grad_scale)
                 for p in params:
                     self.state[p]["step"] = step + 1
         return loss

@@ -1,0 +1,103 @@
+"""AdamW at its edges: blocks of the smallest magnitudes, the noise of stochastic rounding over places, launches and steps, and
+the handles that an optimizer keeps."""
+import math
+
+import pytest
+import torch
+
+import paper_2202_00441_b200 as fb
+import test_adamw as tw
+from paper_2202_00441_b200 import optim
+
+WEYL = 0x9E3779B1                                                 # the noise of a place is a hash of place * WEYL + seed
+
+
+# ---- noise ------------------------------------------------------------------------------------------------------------------
+@pytest.mark.gpu
+def test_noise_goes_on_over_the_ends_of_launches():
+    """901 tensors in three launches give the same codes as one tensor with the same values at the same places."""
+    sizes = [((37 * i) % 700,) for i in range(901)]
+    s = tw.make(sizes, torch.float32, 8, False, seed=31)
+    blocks = [-(-n // 256) for (n,) in sizes]
+    total = sum(blocks) * 256
+    flat = {k: torch.zeros(total, device="cuda") for k in ("p", "g")}
+    flat |= {k: torch.zeros(total, device="cuda").to(torch.float8_e4m3fn) for k in ("m", "v")}
+    flat |= {k: torch.cat(s[k]) for k in ("ms", "vs")}
+    at = [256 * sum(blocks[:i]) for i in range(len(sizes))]
+    for k in ("p", "g", "m", "v"):
+        for a, (n,), x in zip(at, sizes, s[k]):
+            flat[k].view(torch.uint8 if k in "mv" else torch.float32)[a:a + n] = x.view(torch.uint8 if k in "mv" else torch.float32)
+    fb.fewbit_adamw_step(tw.handle(s, 8, False), s["g"], seed=99, **tw.KW)
+    one = fb.fewbit_adamw_create([flat["p"]], [flat["m"]], [flat["v"]], [flat["ms"]], [flat["vs"]])
+    fb.fewbit_adamw_step(one, [flat["g"]], seed=99, **tw.KW)
+    for k in ("m", "v"):
+        whole = flat[k].view(torch.uint8)
+        assert all(torch.equal(whole[a:a + n], x.view(torch.uint8)) for a, (n,), x in zip(at, sizes, s[k]))
+    assert torch.equal(flat["ms"], torch.cat(s["ms"])) and torch.equal(flat["vs"], torch.cat(s["vs"]))
+
+
+@pytest.mark.gpu
+def test_rounding_is_unbiased_over_unrelated_seeds():
+    """The mean over 512 seeds that are no multiples of one another: with a step d between its neighbours the mean's standard
+    deviation is at most d / 2 / sqrt(512); the bound is six of them plus the 2^-16 step of the random numbers."""
+    n, seeds = 4096, 512
+    base = tw.make([(n,)], torch.float32, 8, False, seed=22)
+    drawn = torch.randint(0, 2 ** 32, (seeds,), generator=torch.Generator().manual_seed(5)).tolist()
+    mean = {"m": 0, "v": 0}
+    for seed in drawn:
+        s = {k: [x.clone() for x in v] for k, v in base.items()}
+        fb.fewbit_adamw_step(tw.handle(s, 8, False), s["g"], seed=seed, **tw.KW)
+        for k in mean:
+            mean[k] = mean[k] + tw.wide(s[k][0], s[k + "s"][0], n) / seeds
+    m0, v0 = tw.wide(base["m"][0], base["ms"][0], n), tw.wide(base["v"][0], base["vs"][0], n) ** 2
+    _, m, v, _ = tw.reference(base["p"][0].double(), base["g"][0].double(), m0, v0, tw.KW)
+    for k, val in (("m", m), ("v", v.sqrt())):
+        each = s[k + "s"][0].double().repeat_interleave(256)[:n]
+        step = torch.maximum(2.0 ** -9 * each, 2.0 ** torch.floor(torch.log2(val.abs() / each)) * each / 8)
+        assert ((mean[k] - val).abs() <= step * (3 / math.sqrt(seeds) + 2.0 ** -15)).all()
+
+
+class _Recorder:
+    """Stands for fewbit_adamw_create and fewbit_adamw_step: what an optimizer asks of them."""
+
+    def __init__(self, monkeypatch):
+        self.created, self.seeds = 0, []
+        monkeypatch.setattr(optim, "fewbit_adamw_create", self.create)
+        monkeypatch.setattr(optim, "fewbit_adamw_step", lambda h, grads, *, seed, **kw: self.seeds.append(seed))
+
+    def create(self, *lists):
+        self.created += 1
+        return object()
+
+
+class _CpuAdamW(fb.FewBitAdamW):
+    def add_param_group(self, group):                            # without the check for CUDA tensors
+        torch.optim.Optimizer.add_param_group(self, group)
+
+
+def _steps(opt, params, count, missing=()):
+    for step in range(count):
+        for i, p in enumerate(params):
+            p.grad = None if (step, i) in missing else torch.ones_like(p)
+        opt.step()
+
+
+def test_steps_of_the_optimizer_do_not_share_their_noise(monkeypatch):
+    """Two seeds s and t give the same noise field, moved by (t - s) / WEYL mod 2^32 places.  Steps that follow one another, and
+    groups and types within a step, have to lie far apart: 4096 places, which chance leaves in 2 of 10^6 pairs."""
+    rec = _Recorder(monkeypatch)
+    params = [torch.nn.Parameter(torch.zeros(8, dtype=t)) for t in (torch.float32, torch.bfloat16, torch.float32)]
+    opt = _CpuAdamW([{"params": params[:2]}, {"params": params[2:]}], seed=5)
+    _steps(opt, params, 300)
+    assert len(rec.seeds) == 900 and all(0 <= s < 2 ** 32 for s in rec.seeds)
+    back = pow(WEYL, -1, 2 ** 32)
+    for near in range(1, 7):                                     # the same and the next two steps
+        for s, t in zip(rec.seeds, rec.seeds[near:]):
+            shift = (t - s) * back % 2 ** 32
+            assert min(shift, 2 ** 32 - shift) > 4096
+    again = _Recorder(monkeypatch)
+    _steps(_CpuAdamW([{"params": params[:2]}, {"params": params[2:]}], seed=5), params, 10)
+    assert again.seeds == rec.seeds[:30]
+    other = _Recorder(monkeypatch)
+    _steps(_CpuAdamW([{"params": params[:2]}, {"params": params[2:]}], seed=6), params, 10)
+    assert not set(other.seeds) & set(again.seeds)
