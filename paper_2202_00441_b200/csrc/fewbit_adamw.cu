@@ -103,12 +103,12 @@ __device__ __forceinline__ void decode4(uint32_t w, float scale, float *out) {
     mul2(out[2], out[3], b.x, b.y, scale, scale);
 }
 
-// (scale to store, factor from value to code) of a block whose largest magnitude has the bits `top`.
-__device__ __forceinline__ void block_scale(uint32_t top, float &scale, float &factor) {
+// (scale to store, factor from value times `lift` to code) of a block whose largest magnitude has the bits `top`.
+__device__ __forceinline__ void block_scale(uint32_t top, float lift, float &scale, float &factor) {
     const float t = __uint_as_float(top);
     if (top >= 0x7f800000u) { scale = __uint_as_float(0x7fc00000u); factor = 0.0f; }   // inf or NaN in the block
-    else if (top < 0x00800000u) { scale = 0.0f; factor = 0.0f; }                        // 1 / t could overflow
-    else { scale = t * (1.0f / 448.0f); factor = __fmul_rn(__frcp_rn(t), 448.0f); }
+    else if (top < 0x00800000u) { scale = 0.0f; factor = 0.0f; }                        // the scale would have few bits or none
+    else { scale = t * (1.0f / 448.0f); factor = __fmul_rn(__frcp_rn(__fmul_rn(t, lift)), 448.0f); }
 }
 
 template <typename T>
@@ -198,8 +198,16 @@ __device__ __forceinline__ void update_block(const AdamTensor &t, const AdamScal
     store8_some(static_cast<T *>(t.param) + at, p, valid, wide);
     if constexpr (EIGHT) {
         float scale_m, factor_m, scale_r, factor_r;
-        block_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(top_m)), scale_m, factor_m);
-        block_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(top_r)), scale_r, factor_r);
+        // 448 / t overflows for t up to 448 / 2^128 = 1.3e-36: first moments of that size are lifted before they are scaled (from here on
+        // only their codes and signs count).  Roots are 2^-74.5 at least, or zero.
+        const uint32_t most_m = __reduce_max_sync(0xffffffffu, __float_as_uint(top_m));
+        const bool low = most_m < 0x0d800000u;                    // 2^-100
+        if (low) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) m[e] = __fmul_rn(m[e], 0x1p64f);
+        }
+        block_scale(most_m, low ? 0x1p64f : 1.0f, scale_m, factor_m);
+        block_scale(__reduce_max_sync(0xffffffffu, __float_as_uint(top_r)), 1.0f, scale_r, factor_r);
         uint32_t cm[8], cr[8], wm[2], wr[2];
         const uint32_t place = ((s.block0 + b) * kBlock + lane * 8) * kWeyl + s.seed;
 #pragma unroll

@@ -12,6 +12,43 @@ from paper_2202_00441_b200 import optim
 WEYL = 0x9E3779B1                                                 # the noise of a place is a hash of place * WEYL + seed
 
 
+# ---- blocks of tiny values ----------------------------------------------------------------------------------------------------
+@pytest.mark.gpu
+@pytest.mark.parametrize("top", [2.0 ** -118, 2.0 ** -119.5, 2.0 ** -122, 1e-37, 2.0 ** -126])
+def test_blocks_of_tiny_moments_keep_their_values(top):
+    """Moments with zero gradients decay through these sizes.  The scale of a block is top / 448, a subnormal here: its step of
+    2^-149 is at most 2^-14.1 of it (2^-126 / 448 = 2^-134.8), so a value is off by one float8 step or by that."""
+    n = 512
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    m = torch.randn(n, generator=gen, device="cuda").clamp(-3, 3) / 3 * 0.9 * top
+    m[0], m[1::5] = top, 0.0
+    m[256] = -top
+    p = torch.zeros(n, device="cuda")                             # moments from a gradient alone
+    codes = [torch.zeros(n, device="cuda").to(torch.float8_e4m3fn) for _ in range(2)]
+    scales = [torch.zeros(2, device="cuda") for _ in range(2)]
+    g = (m.double() / 0.5).float()
+    h = fb.fewbit_adamw_create([p], codes[:1], codes[1:], scales[:1], scales[1:])
+    fb.fewbit_adamw_step(h, [g], step=1, lr=0.0, betas=(0.5, 0.5), eps=1e-8, seed=77)
+    want = 0.5 * g.double()
+    back = tw.wide(codes[0], scales[0], n)
+    each = scales[0].double().repeat_interleave(256)
+    assert ((scales[0].double() * 448 - top).abs() <= 2.0 ** -13 * top).all()
+    step = torch.maximum(2.0 ** -9 * each, want.abs() / 8)
+    assert ((back - want).abs() <= step * (1 + 2.0 ** -12) + 2.0 ** -13 * want.abs()).all()
+    assert (back[want == 0] == 0).all()
+    assert ((back[[0, 256]] - want[[0, 256]]).abs() <= 2.0 ** -13 * top).all()
+
+
+@pytest.mark.gpu
+def test_blocks_below_the_normal_numbers_read_back_as_zero():
+    g = torch.full((256,), 2.0 ** -127, device="cuda")
+    codes = [torch.zeros(256, device="cuda").to(torch.float8_e4m3fn) for _ in range(2)]
+    scales = [torch.zeros(1, device="cuda") for _ in range(2)]
+    h = fb.fewbit_adamw_create([torch.zeros(256, device="cuda")], codes[:1], codes[1:], scales[:1], scales[1:])
+    fb.fewbit_adamw_step(h, [g], step=1, lr=0.0, betas=(0.5, 0.5), eps=1e-8, seed=1)
+    assert float(scales[0]) == 0 and (tw.wide(codes[0], scales[0], 256) == 0).all()
+
+
 # ---- noise ------------------------------------------------------------------------------------------------------------------
 @pytest.mark.gpu
 def test_noise_goes_on_over_the_ends_of_launches():
