@@ -106,26 +106,27 @@ class _AttentionFunction(torch.autograd.Function):
     """Keeps q, k, v, the output and one number for each row and head; the probabilities are recomputed."""
 
     @staticmethod
-    def forward(ctx, q, k, v, kw):
+    def forward(ctx, q, k, v, q_offsets, k_offsets, kw):
         q, k, v = _attention_layout(q), _attention_layout(k), _attention_layout(v)
-        out, lse = fewbit_attention_fwd(q, k, v, **kw)
+        out, lse = fewbit_attention_fwd(q, k, v, q_offsets=q_offsets, k_offsets=k_offsets, **kw)
         ctx.kw = kw
-        ctx.save_for_backward(q, k, v, out, lse)
+        ctx.save_for_backward(q, k, v, out, lse, q_offsets, k_offsets)   # (autograd refuses a backward pass when one has been changed)
         return out
 
     @staticmethod
     def backward(ctx, grad_out):
-        q, k, v, out, lse = ctx.saved_tensors
-        return (*fewbit_attention_bwd(_attention_layout(grad_out), q, k, v, out, lse, **ctx.kw), None)
+        q, k, v, out, lse, q_offsets, k_offsets = ctx.saved_tensors
+        return (*fewbit_attention_bwd(_attention_layout(grad_out), q, k, v, out, lse, q_offsets=q_offsets, k_offsets=k_offsets, **ctx.kw),
+                None, None, None)
 
 
 def fewbit_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool = False, scale: float | None = None,
                      q_offsets: torch.Tensor | None = None, k_offsets: torch.Tensor | None = None,
                      max_q_len: int | None = None, max_k_len: int | None = None) -> torch.Tensor:
     """softmax(scale q k^T) v with gradients; arguments as in ``fewbit_attention_fwd``.  Tensors whose strides the library
-    does not take (a transposed head, an expanded batch) are copied first."""
-    return _AttentionFunction.apply(q, k, v, {"causal": causal, "scale": scale, "q_offsets": q_offsets, "k_offsets": k_offsets,
-                                              "max_q_len": max_q_len, "max_k_len": max_k_len})
+    does not take (a transposed head, an expanded batch) are copied first.  The offsets are kept for the backward pass as they
+    are: a program that reuses their buffer before it gets autograd's error."""
+    return _AttentionFunction.apply(q, k, v, q_offsets, k_offsets, {"causal": causal, "scale": scale, "max_q_len": max_q_len, "max_k_len": max_k_len})
 
 
 def _contiguous_heads(t: torch.Tensor) -> torch.Tensor:
@@ -136,28 +137,28 @@ class _QkNormRopeFunction(torch.autograd.Function):
     """Keeps the inputs only: the norm's factor is recomputed."""
 
     @staticmethod
-    def forward(ctx, q, k, q_weight, k_weight, kw):
+    def forward(ctx, q, k, q_weight, k_weight, cos, sin, positions, kw):
         q, k = _contiguous_heads(q), _contiguous_heads(k)
         wide = [None if w is None else w.detach().float().contiguous() for w in (q_weight, k_weight)]
-        out = fewbit_qk_norm_rope_fwd(q, k, *wide, **kw)
+        out = fewbit_qk_norm_rope_fwd(q, k, *wide, cos, sin, positions=positions, **kw)
         ctx.kw, ctx.weight_types = kw, [None if w is None else w.dtype for w in (q_weight, k_weight)]
-        ctx.save_for_backward(q, k, *wide)
+        ctx.save_for_backward(q, k, *wide, cos, sin, positions)
         return out
 
     @staticmethod
     def backward(ctx, grad_q, grad_k):
-        q, k, qw, kw_ = ctx.saved_tensors
+        q, k, qw, kw_, cos, sin, positions = ctx.saved_tensors
         wanted = (ctx.needs_input_grad[2] and qw is not None) or (ctx.needs_input_grad[3] and kw_ is not None)
-        dq, dk, dqw, dkw = fewbit_qk_norm_rope_bwd(_contiguous_heads(grad_q), _contiguous_heads(grad_k), q, k, qw, kw_,
-                                                   weight_grads=wanted, **ctx.kw)
+        dq, dk, dqw, dkw = fewbit_qk_norm_rope_bwd(_contiguous_heads(grad_q), _contiguous_heads(grad_k), q, k, qw, kw_, cos, sin,
+                                                   positions=positions, weight_grads=wanted, **ctx.kw)
         dws = [g.to(t) if g is not None and t is not None else None for g, t in zip((dqw, dkw), ctx.weight_types)]
-        return dq, dk, dws[0], dws[1], None
+        return dq, dk, dws[0], dws[1], None, None, None, None
 
 
 def fewbit_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: torch.Tensor | None, k_weight: torch.Tensor | None,
                         cos: torch.Tensor | None, sin: torch.Tensor | None, *, positions: torch.Tensor | None = None,
                         eps: float = 1e-6, interleaved: bool = False):
     """RMS norm of every query and key head and the position rotation, with gradients for q, k and the weights (of any
-    floating type); arguments as in ``fewbit_qk_norm_rope_fwd``."""
-    return _QkNormRopeFunction.apply(q, k, q_weight, k_weight,
-                                     {"cos": cos, "sin": sin, "positions": positions, "eps": eps, "interleaved": interleaved})
+    floating type); arguments as in ``fewbit_qk_norm_rope_fwd``.  Tables and positions are kept for the backward pass as they
+    are: a program that changes them before it gets autograd's error."""
+    return _QkNormRopeFunction.apply(q, k, q_weight, k_weight, cos, sin, positions, {"eps": eps, "interleaved": interleaved})
