@@ -159,6 +159,8 @@ def fewbit_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: torch.Tensor
                         cos: torch.Tensor | None, sin: torch.Tensor | None, *, positions: torch.Tensor | None = None,
                         eps: float = 1e-6, interleaved: bool = False):
     """RMS norm of every query and key head and the position rotation, with gradients for q, k and the weights (of any
-    floating type); arguments as in ``fewbit_qk_norm_rope_fwd``.  Tables and positions are kept for the backward pass as they
-    are: a program that changes them before it gets autograd's error."""
+    floating type), but none for the tables; arguments as in ``fewbit_qk_norm_rope_fwd``.  Tables and positions are kept for the
+    backward pass as they are: a program that changes them before it gets autograd's error."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (cos, sin)):
+        raise ValueError("cos and sin have no gradient here: pass tables that do not require one (detach them)")
     return _QkNormRopeFunction.apply(q, k, q_weight, k_weight, cos, sin, positions, {"eps": eps, "interleaved": interleaved})

@@ -32,3 +32,13 @@ def test_tables_and_positions_changed_before_the_backward_pass_are_an_error(whic
     {"cos": c, "sin": s, "positions": p}[which].zero_()
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         (a.sum() + b.sum()).backward()
+
+
+@pytest.mark.gpu
+def test_tables_that_want_a_gradient_are_refused():
+    q, k, w, c, s, _ = tq.inputs(1, 9, 2, 1, 64, 64, torch.float32, "fused", None, True)
+    for cos, sin in ((c.clone().requires_grad_(), s), (c, s.clone().requires_grad_())):
+        with pytest.raises(ValueError, match="cos and sin"):
+            fb.fewbit_qk_norm_rope(q, k, *w, cos, sin)
+        with torch.no_grad():
+            fb.fewbit_qk_norm_rope(q, k, *w, cos, sin)
