@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import torch
 from torch import nn
+from torch.autograd.function import once_differentiable
 
 from .binding import Table, fewbit_bwd, fewbit_fwd, fewbit_fwd_bias, fewbit_table_create, fewbit_table_create_folded
 from .operators import fewbit_attention_bwd, fewbit_attention_fwd, fewbit_qk_norm_rope_bwd, fewbit_qk_norm_rope_fwd
@@ -114,6 +115,7 @@ class _AttentionFunction(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_out):
         q, k, v, out, lse, q_offsets, k_offsets = ctx.saved_tensors
         return (*fewbit_attention_bwd(_attention_layout(grad_out), q, k, v, out, lse, q_offsets=q_offsets, k_offsets=k_offsets, **ctx.kw),
@@ -146,6 +148,7 @@ class _QkNormRopeFunction(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, grad_q, grad_k):
         q, k, qw, kw_, cos, sin, positions = ctx.saved_tensors
         wanted = (ctx.needs_input_grad[2] and qw is not None) or (ctx.needs_input_grad[3] and kw_ is not None)

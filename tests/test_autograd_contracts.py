@@ -42,3 +42,18 @@ def test_tables_that_want_a_gradient_are_refused():
             fb.fewbit_qk_norm_rope(q, k, *w, cos, sin)
         with torch.no_grad():
             fb.fewbit_qk_norm_rope(q, k, *w, cos, sin)
+
+
+@pytest.mark.gpu
+def test_second_derivatives_are_refused():
+    q, k, v, *offsets = _packed()
+    out = fb.fewbit_attention(q, k, v, q_offsets=offsets[0], k_offsets=offsets[1], max_q_len=40, max_k_len=40)
+    (dq,) = torch.autograd.grad(out.float().square().sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        dq.float().sum().backward()
+    q, k, w, c, s, _ = tq.inputs(1, 9, 2, 1, 64, 64, torch.float32, "fused", None, True)
+    q = q.clone().requires_grad_()
+    a, b = fb.fewbit_qk_norm_rope(q, k, *w, c, s)
+    (dq,) = torch.autograd.grad(a.square().sum() + b.sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        dq.sum().backward()
