@@ -396,8 +396,8 @@ FEWBIT_API fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *shap
 
 /*
  * Diagnostic: *count (HOST) receives how often a wait inside the attention kernels gave up on the current
- * device since the library was loaded (each wait is limited to two seconds; the results of such a launch are
- * not valid).  Always 0 unless the device or the program is broken.  Synchronises the device.
+ * device since the library was loaded (each wait is limited to two seconds; the results that such a launch could
+ * not finish are NaN).  Always 0 unless the device or the program is broken.  Synchronises the device.
  */
 FEWBIT_API fewbit_status fewbit_attention_timeout_count(uint64_t *count);
 

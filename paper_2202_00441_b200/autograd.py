@@ -127,7 +127,8 @@ def fewbit_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causa
                      max_q_len: int | None = None, max_k_len: int | None = None) -> torch.Tensor:
     """softmax(scale q k^T) v with gradients; arguments as in ``fewbit_attention_fwd``.  Tensors whose strides the library
     does not take (a transposed head, an expanded batch) are copied first.  The offsets are kept for the backward pass as they
-    are: a program that reuses their buffer before it gets autograd's error."""
+    are: a program that reuses their buffer before it gets autograd's error.  Should a wait inside a kernel give up (a broken device:
+    two seconds), the results that it leaves unfinished are NaN, and ``fewbit_attention_timeout_count`` tells."""
     return _AttentionFunction.apply(q, k, v, q_offsets, k_offsets, {"causal": causal, "scale": scale, "max_q_len": max_q_len, "max_k_len": max_k_len})
 
 

@@ -42,6 +42,7 @@ constexpr int kWorkThreads = 512;
 // 61440 = 640 x 96
 constexpr int kFwdWork = 112, kFwdIssue = 32, kDqWork = 104, kDqIssue = 64, kDkvWork = 112, kDkvIssue = 32;
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr uint32_t kNan = 0x7fc00000u;
 constexpr int kStatBytes = 2 * kTile * 4;   // a row tile's -lse * log2(e) and -delta
 
 struct Rows {                         // an output tensor
@@ -463,27 +464,26 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
         }
         if (nt > 0 && ok) ok = wait(fO + t, (nt - 1) & 1);
         fence_after();
+        if (!ok) sum = NAN;                                           // given up: out and lse say so
         *mine = sum;                                                  // (the last exchange of maxima was read before P was ready)
         pair_barrier(pair);
         sum += *other;
         const bool live = i < w.q_len;
         T *row = static_cast<T *>(p.out.p) + (live ? row_of(w, p.out, w.head, i, w.q_first) : 0);
         if (p.split == 1) {
-            if (ok) {
-                if (nt > 0) {
-                    const float factor = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+            if (nt > 0) {
+                const float factor = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
 #pragma unroll
-                    for (int c = 0; c < DIM / 64; ++c) {
-                        uint32_t o[32];
-                        tmem_ld32(o_at + 32 * c, o);
-                        wait_ld(o);
-                        if (live) store_columns<T, 32>(row, half * (DIM / 2) + 32 * c, p.dim, o, factor);
-                    }
-                } else if (live && half == 0) {
-                    zero_columns<T>(row, p.dim);
+                for (int c = 0; c < DIM / 64; ++c) {
+                    uint32_t o[32];
+                    tmem_ld32(o_at + 32 * c, o);
+                    wait_ld(o);
+                    if (live) store_columns<T, 32>(row, half * (DIM / 2) + 32 * c, p.dim, o, factor);
                 }
-                if (live && half == 0) p.lse[stat_of(p, w, w.head, i)] = sum == 0.0f ? -INFINITY : top * p.scale + logf(sum);
+            } else if (live && half == 0) {
+                zero_columns<T>(row, p.dim);
             }
+            if (live && half == 0) p.lse[stat_of(p, w, w.head, i)] = sum == 0.0f ? -INFINITY : top * p.scale + logf(sum);
         } else {
             // Every CTA lays its O, reference and sum of each row out in shared memory, [row tile][column][row]; a share of the
             // columns is brought to the largest reference, added up and divided by each.
@@ -776,8 +776,10 @@ attention_dq_kernel(const __grid_constant__ Params p) {
         const float row_drift = single ? 0.0f : over_parts(drift);
         // A row of one key has P = 1 and dS = 0 whatever its score: what the recomputed P leaves of dS is rounding and nothing
         // else.  (Times 0: a NaN stays one.)
-        const float factor = seen == 1 ? 0.0f : p.scale;
+        float factor = seen == 1 ? 0.0f : p.scale;
         if (ok) ok = wait(qDone, 0);
+        if (stopped(sync)) ok = false;                                // (qDone comes in any case)
+        if (!ok) factor = NAN;                                        // given up: dQ and, through delta, dK say so
         fence_after();
         T *row = static_cast<T *>(p.dq.p) + (live ? row_of(w, p.dq, w.head, i, w.q_first) : 0);
         // (a row past the sequence's end may hold anything: its probabilities are 0, and 0 is what they multiply)
@@ -785,17 +787,15 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             if (part < 2) stat_block(p, w, w.head, w.tile)[part * kTile + r] = part == 0 ? minus_lse : live ? minus_delta - off : 0.0f;
         };
         if (p.split == 1) {
-            write_stat(row_drift);
-            if (ok) {
-                if (n > 0) {
-                    uint32_t o[DIM / 4];
-                    if constexpr (DIM == 128) tmem_ld32(tm_dq + my_lane + 32 * part, o);
-                    else tmem_ld16(tm_dq + my_lane + 16 * part, o);
-                    wait_ld(o);
-                    if (live) store_columns<T, DIM / 4>(row, part * (DIM / 4), p.dim, o, factor);
-                } else if (live && part == 0) {
-                    zero_columns<T>(row, p.dim);
-                }
+            write_stat(ok ? row_drift : NAN);
+            if (n > 0) {
+                uint32_t o[DIM / 4];
+                if constexpr (DIM == 128) tmem_ld32(tm_dq + my_lane + 32 * part, o);
+                else tmem_ld16(tm_dq + my_lane + 16 * part, o);
+                wait_ld(o);
+                if (live) store_columns<T, DIM / 4>(row, part * (DIM / 4), p.dim, o, factor);
+            } else if (live && part == 0) {
+                zero_columns<T>(row, p.dim);
             }
         } else {
             // Every CTA lays its sums out in shared memory, [column][row] and the rows' drift; a share of the columns is added up
@@ -807,8 +807,8 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             wait_ld(o);
 #pragma unroll
             for (int e = 0; e < DIM / 4; ++e)
-                asm volatile("st.shared.u32 [%0], %1;" :: "r"(mine + (part * (DIM / 4) + e) * (kTile * 4)), "r"(n > 0 ? o[e] : 0u) : "memory");
-            if (part == 0) row_delta[r] = n > 0 ? row_drift : 0.0f;
+                asm volatile("st.shared.u32 [%0], %1;" :: "r"(mine + (part * (DIM / 4) + e) * (kTile * 4)), "r"(!ok ? kNan : n > 0 ? o[e] : 0u) : "memory");
+            if (part == 0) row_delta[r] = !ok ? NAN : n > 0 ? row_drift : 0.0f;
             cluster_sync();
             if (rank == 0) {
                 float off = 0.0f;
@@ -1127,28 +1127,28 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             }
         }
         if (ok) ok = wait(kDone, 0);
+        if (stopped(sync)) ok = false;                                // (kDone comes in any case)
         fence_after();
         // dV by every other four warps, dK by the rest; the first eight warps take the first half of the columns
         const int which = part & 1, half = part >> 1, r = threadIdx.x & 127;
         const bool live = row_key < w.k_len;
         const Rows &to = which == 0 ? p.dv : p.dk;
-        const float factor = which == 0 ? 1.0f : w.k_len == 1 ? 0.0f : p.scale;   // (rows of one key have no dS)
+        // (rows of one key have no dS; NaN: a wait was given up)
+        const float factor = !ok ? NAN : which == 0 ? 1.0f : w.k_len == 1 ? 0.0f : p.scale;
         const uint32_t from = (which == 0 ? tm_dv : tm_dk) + my_lane;
         T *row = static_cast<T *>(to.p) + (live ? row_of(w, to, w.head, row_key, w.k_first) : 0);
         if (p.split == 1) {
-            if (ok) {
-                if (n > 0) {
+            if (n > 0) {
 #pragma unroll
-                    for (int c = 0; c < DIM / 64; ++c) {
-                        uint32_t o[32];
-                        const int col = half * (DIM / 2) + 32 * c;
-                        tmem_ld32(from + col, o);
-                        wait_ld(o);
-                        if (live) store_columns<T, 32>(row, col, p.dim, o, factor);
-                    }
-                } else if (live && half == 0) {
-                    zero_columns<T>(row, p.dim);
+                for (int c = 0; c < DIM / 64; ++c) {
+                    uint32_t o[32];
+                    const int col = half * (DIM / 2) + 32 * c;
+                    tmem_ld32(from + col, o);
+                    wait_ld(o);
+                    if (live) store_columns<T, 32>(row, col, p.dim, o, factor);
                 }
+            } else if (live && half == 0) {
+                zero_columns<T>(row, p.dim);
             }
         } else {
             // Each CTA adds up a share of the columns over the cluster, and lays the others of its sums out in its own shared
@@ -1164,7 +1164,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                 wait_ld(o);
 #pragma unroll
                 for (int e = 0; e < 32; ++e)
-                    asm volatile("st.shared.u32 [%0], %1;" :: "r"(mine + (col + e) * (kTile * 4)), "r"(n > 0 ? o[e] : 0u) : "memory");
+                    asm volatile("st.shared.u32 [%0], %1;" :: "r"(mine + (col + e) * (kTile * 4)), "r"(!ok ? kNan : n > 0 ? o[e] : 0u) : "memory");
             }
             cluster_sync();
             auto add_up = [&](auto columns) {                         // this thread's columns of the share: half of them

@@ -31,23 +31,27 @@ __device__ __forceinline__ bool barrier_try(uint32_t bar, uint32_t parity) {
                  : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
-__device__ __forceinline__ uint64_t now_ns() {
+__device__ __forceinline__ uint32_t now_ticks() {                     // of 2^17 ns
     uint64_t t;
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-    return t;
+    return static_cast<uint32_t>(t >> 17);
 }
 
-// No wait is endless: after this long a wait gives up, the CTA's other waits follow, and the kernel winds up.
-constexpr uint64_t kWaitLimitNs = 2000000000ull;
+// No wait is endless: after two seconds a wait gives up, the CTA's other waits follow, and the kernel winds up.  The timer runs
+// on while the program is not on the device: a round of tries counts for a tenth of a second at most.
+constexpr uint32_t kWaitLimit = 15259, kRoundLimit = 763;
 
 // Waits of a whole warp (every lane gets the same answer).  false: given up; `stop` (shared memory) is set.
 __device__ __forceinline__ bool barrier_wait_slow(uint32_t bar, uint32_t parity, volatile int *stop, unsigned int *timeouts) {
-    const uint64_t t0 = now_ns();
+    uint32_t last = now_ticks(), spent = 0;
     for (;;) {
         for (int i = 0; i < 64; ++i)
             if (barrier_try(bar, parity)) return true;
         if (stop != nullptr && *stop != 0) return false;
-        if (now_ns() - t0 > kWaitLimitNs) {
+        const uint32_t now = now_ticks();
+        spent += min(now - last, kRoundLimit);
+        last = now;
+        if (spent > kWaitLimit) {
             if (stop != nullptr) *stop = 1;
             atomicAdd(timeouts, 1u);
             return false;
