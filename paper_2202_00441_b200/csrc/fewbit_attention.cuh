@@ -406,17 +406,19 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
             auto maximum = [&]() {
 #pragma unroll
                 for (int e = 0; e < 32; e += 2)                       // two at a time: a three-operand maximum
-                    best[(e >> 1) & 3] = fmaxf(best[(e >> 1) & 3], fmaxf(__uint_as_float(s[e]), __uint_as_float(s[e + 1])));
+                    best[(e >> 1) & 3] = max3_nan(best[(e >> 1) & 3], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
             };
             read(0);
             maximum();
             read(1);
             maximum();
-            const float high = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3]));
+            const float high = max3_nan(max3_nan(best[0], best[1], best[2]), best[3], best[3]);
             // The sums' reference moves only when a product passes it by 2^8: until then probabilities up to 2^8
             // are held, which cost no precision, and O needs no rescaling.  The row's two threads move it together: whether
-            // any row of their two warps moves is one barrier, and only then they exchange their maxima.
-            const bool above = high > top && (high - top) * p.scale_log2 > 8.0f;
+            // any row of their two warps moves is one barrier, and only then they exchange their maxima.  A score that is NaN
+            // becomes the reference, and with it the whole row.
+            auto moves = [&](float to) { return to != top && !((to - top) * p.scale_log2 <= 8.0f); };
+            const bool above = moves(high);
             if (pair_any(pair, above || !ok)) {
                 if (pair_any(pair, !ok)) {
                     ok = false;
@@ -424,8 +426,8 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
                 }
                 *mine = high;
                 pair_barrier(pair);
-                const float row_high = fmaxf(high, *other);
-                const bool move = row_high > top && (row_high - top) * p.scale_log2 > 8.0f;
+                const float row_high = max3_nan(high, *other, high);
+                const bool move = moves(row_high);
                 const float next = move ? row_high : top;
                 const float factor = move ? exp2_fast((top - next) * p.scale_log2) : 1.0f;
                 top = next;

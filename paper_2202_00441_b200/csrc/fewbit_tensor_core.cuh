@@ -272,6 +272,11 @@ template <> __device__ __forceinline__ uint32_t pack2<__half>(float lo, float hi
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
     return d;
 }
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {   // NaN if one of them is
+    float d;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
 __device__ __forceinline__ float exp2_fast(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -281,7 +286,8 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // 2^x for two values on the FMA pipe, which has room where the exponential unit (16 results a clock) is the limit:
 // x = n + f with n the nearest integer, f in [-1/2, 1/2]; 2^f by the degree-4 polynomial of least relative error (2.6e-6,
 // found by iteratively reweighted least squares), n added to the exponent.  Values below 2^-126 come out as 2^-126; a NaN or
-// an infinity comes out as a value that is not finite in 16 bits.
+// an infinity comes out as a value that is not finite in 16 bits but may be in 32: where such a value may be the only one of a
+// sum, the caller has to see to it.
 __device__ __forceinline__ void exp2_polynomial(float &d0, float &d1, float x0, float x1) {
     constexpr float kMagic = 12582912.0f;                             // 1.5 * 2^23: the sum's low bits are the integer
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(x0) : "f"(x0), "f"(-126.0f));

@@ -142,3 +142,26 @@ def test_without_query_heads_the_key_gradients_are_zero():
     del full
     dq, dk, dv = fb.fewbit_attention_bwd(q, q, kv, kv, out, lse)
     assert dq.shape == q.shape and (dk == 0).all() and (dv == 0).all()
+
+
+# ---- values -----------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("d", [64, 128])
+def test_one_key_that_is_not_a_number_makes_the_rows_that_see_it_nan(d):
+    """A softmax with one NaN is NaN throughout, its sum's logarithm too; rows that do not see the key keep their values.  Key i
+    of head i is NaN, in two of three key tiles."""
+    h, n = 128, 384
+    q, k, v, _ = ta.make(1, n, n, h, h, d, torch.bfloat16, seed=15)
+    clean = fb.fewbit_attention_fwd(q, k, v, causal=True)
+    for first in (0, 128):
+        bad = k.clone()
+        at = torch.arange(h, device="cuda")
+        bad[0, first + at, at] = NAN
+        seen = torch.arange(n, device="cuda")[None] >= first + at[:, None]           # (head, row)
+        for causal in (True, False):
+            out, lse = fb.fewbit_attention_fwd(q, bad, v, causal=causal)
+            sees = seen if causal else torch.ones_like(seen)
+            assert lse[0][sees].isnan().all()
+            assert out[0].transpose(0, 1)[sees].isnan().all()
+            if causal:
+                assert torch.equal(lse[0][~seen], clean[1][0][~seen])
+                assert torch.equal(out[0].transpose(0, 1)[~seen], clean[0][0].transpose(0, 1)[~seen])
