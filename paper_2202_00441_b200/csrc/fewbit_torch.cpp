@@ -205,11 +205,12 @@ std::tuple<Tensor, Tensor, Tensor> attention_bwd(const Tensor &g, const Tensor &
     return {dq, dk, dv};
 }
 
-// What a program keeps for its steps.
+// What a program keeps for its steps: the tensors, not where they lie (`p.data = ...` puts other memory under a parameter).
 class AdamW {
 public:
-    AdamW(std::vector<Tensor> params, std::vector<Tensor> m, std::vector<Tensor> v, std::optional<std::vector<Tensor>> ms, std::optional<std::vector<Tensor>> vs,
-          std::optional<std::vector<Tensor>> masters) {
+    AdamW(std::vector<Tensor> params_, std::vector<Tensor> m_, std::vector<Tensor> v_, std::optional<std::vector<Tensor>> ms_, std::optional<std::vector<Tensor>> vs_,
+          std::optional<std::vector<Tensor>> masters_)
+        : params(std::move(params_)), m(std::move(m_)), v(std::move(v_)), ms(std::move(ms_)), vs(std::move(vs_)), masters(std::move(masters_)) {
         const size_t n = params.size();
         if (n == 0 || m.size() != n || v.size() != n || (ms && ms->size() != n) || (vs && vs->size() != n) || (masters && masters->size() != n))
             refuse("every list must have one tensor for each parameter, and there must be one");
@@ -219,27 +220,12 @@ public:
         type = params[0].scalar_type();
         device = params[0].device();
         if (masters && dtype == FEWBIT_F32) refuse("float32 parameters need no master copy");
-        auto pointer = [&](const Tensor &t, at::ScalarType want, int64_t numel) {
-            if (t.device() != device || !t.is_cuda() || t.scalar_type() != want || t.numel() != numel || !t.is_contiguous())
-                refuse("parameters, moments (float32, or float8_e4m3fn with a float32 scale for each 256 elements) and masters (float32) must be contiguous CUDA "
-                       "tensors of one device and matching sizes");
-            return t.data_ptr();
-        };
-        const auto state = bits == 8 ? at::kFloat8_e4m3fn : at::kFloat;
-        for (size_t i = 0; i < n; ++i) {
-            const int64_t numel = params[i].numel(), blocks = (numel + FEWBIT_ADAMW_BLOCK - 1) / FEWBIT_ADAMW_BLOCK;
-            descs.push_back({pointer(params[i], type, numel), pointer(m[i], state, numel), pointer(v[i], state, numel),
-                             ms ? static_cast<float *>(pointer((*ms)[i], at::kFloat, blocks)) : nullptr,
-                             vs ? static_cast<float *>(pointer((*vs)[i], at::kFloat, blocks)) : nullptr,
-                             masters ? static_cast<float *>(pointer((*masters)[i], at::kFloat, numel)) : nullptr, static_cast<uint64_t>(numel)});
-        }
-        for (auto *x : {&params, &m, &v}) keep.insert(keep.end(), x->begin(), x->end());
-        for (auto *x : {&ms, &vs, &masters})
-            if (*x) keep.insert(keep.end(), (*x)->begin(), (*x)->end());
+        descriptions();
     }
     void step(const std::vector<Tensor> &grads, int64_t step, double lr, double beta1, double beta2, double eps, double weight_decay, int64_t seed,
               const Optional &grad_scale) const {
-        if (grads.size() != descs.size()) refuse("one gradient for each parameter is needed");
+        if (grads.size() != params.size()) refuse("one gradient for each parameter is needed");
+        const std::vector<fewbit_adamw_tensor> descs = descriptions();
         std::vector<const void *> pointers(grads.size());
         for (size_t i = 0; i < grads.size(); ++i) {
             const Tensor &g = grads[i];
@@ -255,16 +241,40 @@ public:
         check(fewbit_adamw_step(descs.data(), pointers.data(), static_cast<int>(descs.size()), &o, c10::cuda::getCurrentCUDAStream(device.index()).stream()),
               "fewbit_adamw_step");
     }
-    size_t size() const { return descs.size(); }
-    std::vector<Tensor> tensors() const { return keep; }
+    size_t size() const { return params.size(); }
+    std::vector<Tensor> tensors() const {
+        std::vector<Tensor> all;
+        for (auto *x : {&params, &m, &v}) all.insert(all.end(), x->begin(), x->end());
+        for (auto *x : {&ms, &vs, &masters})
+            if (*x) all.insert(all.end(), (*x)->begin(), (*x)->end());
+        return all;
+    }
     int bits;
     at::Device device = at::kCPU;
 
 private:
+    std::vector<fewbit_adamw_tensor> descriptions() const {
+        auto pointer = [&](const Tensor &t, at::ScalarType want, int64_t numel) {
+            if (t.device() != device || !t.is_cuda() || t.scalar_type() != want || t.numel() != numel || !t.is_contiguous())
+                refuse("parameters, moments (float32, or float8_e4m3fn with a float32 scale for each 256 elements) and masters (float32) must be contiguous CUDA "
+                       "tensors of one device and matching sizes");
+            return t.data_ptr();
+        };
+        const auto state = bits == 8 ? at::kFloat8_e4m3fn : at::kFloat;
+        std::vector<fewbit_adamw_tensor> descs(params.size());
+        for (size_t i = 0; i < descs.size(); ++i) {
+            const int64_t numel = params[i].numel(), blocks = (numel + FEWBIT_ADAMW_BLOCK - 1) / FEWBIT_ADAMW_BLOCK;
+            descs[i] = {pointer(params[i], type, numel), pointer(m[i], state, numel), pointer(v[i], state, numel),
+                        ms ? static_cast<float *>(pointer((*ms)[i], at::kFloat, blocks)) : nullptr,
+                        vs ? static_cast<float *>(pointer((*vs)[i], at::kFloat, blocks)) : nullptr,
+                        masters ? static_cast<float *>(pointer((*masters)[i], at::kFloat, numel)) : nullptr, static_cast<uint64_t>(numel)};
+        }
+        return descs;
+    }
     fewbit_dtype dtype;
     at::ScalarType type;
-    std::vector<fewbit_adamw_tensor> descs;
-    std::vector<Tensor> keep;
+    std::vector<Tensor> params, m, v;
+    std::optional<std::vector<Tensor>> ms, vs, masters;
 };
 
 }  // namespace

@@ -138,3 +138,29 @@ def test_steps_of_the_optimizer_do_not_share_their_noise(monkeypatch):
     other = _Recorder(monkeypatch)
     _steps(_CpuAdamW([{"params": params[:2]}, {"params": params[2:]}], seed=6), params, 10)
     assert not set(other.seeds) & set(again.seeds)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_handle_follows_its_tensors(bits):
+    """Other memory put under a parameter and its state: the next step works there, and nothing is written where they lay."""
+    s, t = (tw.make([(700,), (300,)], torch.bfloat16, bits, True, seed=41) for _ in range(2))
+    h, other = tw.handle(s, bits, True), tw.handle(t, bits, True)
+    names = [k for k in s if k != "g" and s[k]]
+    left = {k: [x.detach() for x in s[k]] for k in names}        # keeps the old memory
+    for k in names:
+        for x in s[k]:
+            x.data = x.data.clone()
+    before = {k: [x.clone() for x in left[k]] for k in names}
+    fb.fewbit_adamw_step(h, s["g"], seed=7, **tw.KW)
+    fb.fewbit_adamw_step(other, t["g"], seed=7, **tw.KW)
+
+    def same(a, b):
+        return torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+    for k in names:
+        assert all(same(a, b) for a, b in zip(s[k], t[k])), k
+        assert all(same(a, b) for a, b in zip(left[k], before[k])), k
+    s["p"][0].data = s["p"][0].data[:100].clone()
+    with pytest.raises(ValueError):
+        fb.fewbit_adamw_step(h, s["g"], seed=8, **tw.KW)
