@@ -83,25 +83,30 @@ class FewBitAdamW(torch.optim.Optimizer):
                 loss = closure()
         for number, group in enumerate(self.param_groups):
             buckets = {}
-            for p in group["params"]:
+            for index, p in enumerate(group["params"]):
                 if p.grad is None:
                     continue
                 if p.grad.is_sparse:
                     raise RuntimeError("FewBitAdamW takes dense gradients")
                 if not self.state[p]:
                     self._init_state(p, group)
-                buckets.setdefault((p.device, p.dtype, self.state[p]["step"]), []).append(p)
-            for place, ((device, dtype, step), params) in enumerate(buckets.items()):
+                buckets.setdefault((p.device, p.dtype, self.state[p]["step"]), []).append((index, p))
+            for place, ((device, dtype, step), members) in enumerate(buckets.items()):
+                params = [p for _, p in members]
                 names = ["exp_avg", "exp_avg_sq"]
                 if group["state_bits"] == 8:
                     names += ["exp_avg_scale", "exp_avg_sq_scale"]
                 lists = [[self.state[p][n] for p in params] for n in names] + [None] * (4 - len(names))
                 masters = [self.state[p]["master"] for p in params] if "master" in self.state[params[0]] else None
-                # the handle holds addresses: it is made anew when a parameter or its state has moved
-                where = [t.data_ptr() for x in [params, *lists, masters] if x is not None for t in x]
-                held = self._handles.get((number, device, dtype))
-                if held is None or held[0] != where:
-                    held = self._handles[(number, device, dtype)] = (where, fewbit_adamw_create(params, *lists, masters))
+                # a handle for each set of parameters that step together; made anew when one of them or of their state is another tensor
+                key = (number, tuple(i for i, _ in members))
+                tensors = [t for x in [params, *lists, masters] if x is not None for t in x]
+                held = self._handles.pop(key, None)
+                if held is None or len(held[0]) != len(tensors) or any(a is not b for a, b in zip(held[0], tensors)):
+                    held = (tensors, fewbit_adamw_create(params, *lists, masters))
+                self._handles[key] = held
+                if len(self._handles) > 64:                      # the one that has not been used for longest
+                    del self._handles[next(iter(self._handles))]
                 grads = [p.grad.to(dtype).contiguous() for p in params]
                 fewbit_adamw_step(held[1], grads, step=step + 1, lr=float(group["lr"]), betas=group["betas"], eps=group["eps"],
                                   weight_decay=group["weight_decay"], seed=_noise_seed(self.seed, step + 1, number, place),

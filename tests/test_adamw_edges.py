@@ -140,6 +140,17 @@ def test_steps_of_the_optimizer_do_not_share_their_noise(monkeypatch):
     assert not set(other.seeds) & set(again.seeds)
 
 
+# ---- handles ------------------------------------------------------------------------------------------------------------------
+def test_parameters_a_step_apart_keep_their_handles(monkeypatch):
+    rec = _Recorder(monkeypatch)
+    params = [torch.nn.Parameter(torch.zeros(8)) for _ in range(3)]
+    opt = _CpuAdamW(params)
+    _steps(opt, params, 3, missing={(1, 2)})                     # the last parameter falls a step behind
+    made = rec.created
+    _steps(opt, params, 20)
+    assert rec.created <= made + 1                               # (two handles for the two of them, from then on)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("bits", [8, 32])
 def test_a_handle_follows_its_tensors(bits):
