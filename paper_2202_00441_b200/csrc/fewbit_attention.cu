@@ -250,7 +250,8 @@ fewbit_status fewbit_attention_timeout_count(uint64_t *count) {
     using namespace fewbit;
     if (count == nullptr) return FEWBIT_ERR_INVALID_ARG;
     unsigned int n = 0;
-    const cudaError_t err = cudaMemcpyFromSymbol(&n, g_attention_timeouts, sizeof(n));
+    cudaError_t err = cudaDeviceSynchronize();                        // (a copy alone does not wait for non-blocking streams)
+    if (err == cudaSuccess) err = cudaMemcpyFromSymbol(&n, g_attention_timeouts, sizeof(n));
     *count = n;
     return cuda_status(err);
 }

@@ -165,3 +165,17 @@ def test_one_key_that_is_not_a_number_makes_the_rows_that_see_it_nan(d):
             if causal:
                 assert torch.equal(lse[0][~seen], clean[1][0][~seen])
                 assert torch.equal(out[0].transpose(0, 1)[~seen], clean[0][0].transpose(0, 1)[~seen])
+
+
+# ---- the count of waits that gave up ----------------------------------------------------------------------------------------
+def test_the_timeout_count_waits_for_every_stream():
+    x = torch.randn(8192, 8192, device="cuda").bfloat16()
+    y = torch.empty_like(x)
+    torch.mm(x, x, out=y)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        for _ in range(200):                                      # some 140 ms
+            torch.mm(x, x, out=y)
+    assert fb.fewbit_attention_timeout_count() == 0
+    assert side.query()
