@@ -68,9 +68,11 @@ class _On:
     handed out again before the call has read it."""
 
     def __init__(self, stream, *tensors):
+        tensors = [t for t in tensors if t is not None]
+        if any(t.device != stream.device for t in tensors):
+            raise ValueError("the stream is of another device than the tensors")   # (the call would go to the current stream of theirs)
         for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+            t.record_stream(stream)
         self.inner = torch.cuda.stream(stream)
 
     def __enter__(self):
