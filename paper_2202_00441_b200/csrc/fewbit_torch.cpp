@@ -2,6 +2,7 @@
 // The same as operators.py would do through ctypes, in a few microseconds: a small tensor's kernel takes no longer.
 #include <torch/extension.h>
 
+#include <ATen/MemoryOverlap.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
@@ -94,12 +95,29 @@ Tensor output(const Optional &given, const Tensor &model) {
     like(*given, model, "out does not match q and k");
     return *given;
 }
+// Tensors that a call writes, `a` for the queries and `b` for the keys, against all that it reads: an output may be its own side's input,
+// element for element, and share no other memory (as far as ATen tells: not for views with gaps).
+void no_overlap(const Tensor &a, const Tensor &b, std::initializer_list<std::reference_wrapper<const Tensor>> of_a, std::initializer_list<std::reference_wrapper<const Tensor>> of_b) {
+    const char *what = "an output overlaps itself, the other output or an input in part";
+    for (const Tensor *t : {&a, &b})
+        if (at::has_internal_overlap(*t) == at::MemOverlap::Yes) refuse(what);
+    auto shares = [&](const Tensor &x, const Tensor &y, bool own_side) {
+        const auto s = at::get_overlap_status(x, y);
+        return s == at::MemOverlapStatus::Partial || (s == at::MemOverlapStatus::Full && !own_side);
+    };
+    if (shares(a, b, false)) refuse(what);
+    for (const Tensor &t : of_a)
+        if (shares(a, t, true) || shares(b, t, false)) refuse(what);
+    for (const Tensor &t : of_b)
+        if (shares(b, t, true) || shares(a, t, false)) refuse(what);
+}
 
 std::tuple<Tensor, Tensor> qk_norm_rope_fwd(const Tensor &q, const Tensor &k, const Optional &qw, const Optional &kw, const Optional &cos, const Optional &sin,
                                             const Optional &positions, double eps, bool interleaved, const Optional &q_out, const Optional &k_out) {
     const fewbit_qk_shape s = qk_shape(q, k, qw, kw, cos, sin, positions, eps, interleaved);
     const c10::cuda::OptionalCUDAGuard guard(q.device());
     Tensor a = output(q_out, q), b = output(k_out, k);
+    if (q_out || k_out) no_overlap(a, b, {q}, {k});
     const fewbit_heads h[4] = {heads_of(q), heads_of(k), heads_of(a), heads_of(b)};
     check(fewbit_qk_norm_rope_fwd(&s, &h[0], &h[1], &h[2], &h[3], stream_of(q)), "fewbit_qk_norm_rope_fwd");
     return {a, b};
@@ -113,6 +131,7 @@ std::tuple<Tensor, Tensor, Optional, Optional> qk_norm_rope_bwd(const Tensor &gq
     like(gk, k, "the gradients do not match q and k");
     const c10::cuda::OptionalCUDAGuard guard(q.device());
     Tensor a = output(q_out, q), b = output(k_out, k), ws;
+    if (q_out || k_out) no_overlap(a, b, {q, gq}, {k, gk});
     Optional dqw, dkw;
     size_t bytes = 0;
     if (weight_grads) {

@@ -96,7 +96,8 @@ def fewbit_qk_norm_rope_fwd(q: torch.Tensor, k: torch.Tensor, q_weight: Optional
     q_weight, k_weight: (head_dim,) float32 or None.  cos, sin: (rows, rotary_dim / 2) float32 tables, or None for no
     rotation; ``positions`` (batch, length) picks their rows (a position past the tables makes its heads NaN), without it
     token i has position i.  ``interleaved``: neighbouring elements are rotated with each other instead of the two
-    halves.  ``out``: a pair of tensors to write to (q and k themselves are allowed)."""
+    halves.  ``out``: a pair of tensors to write to (q and k themselves are allowed, but
+    no other overlap)."""
     q_out, k_out = (None, None) if out is None else out
     if stream is not None:
         with _On(stream, q, k, q_weight, k_weight, cos, sin, positions, q_out, k_out):

@@ -21,3 +21,26 @@ def test_a_stream_of_another_device_is_refused():
         with pytest.raises(ValueError, match="device"):
             ops._On(stream, *tensors)
     assert recorded == []
+
+
+@pytest.mark.gpu
+def test_outputs_that_overlap_are_refused():
+    """Elements that share memory with one another, or with other elements of an input, would be written in any order."""
+    flat = torch.randn(2, 3 * 5 * 4 * 64 + 64, device="cuda")
+    n = 3 * 5 * 4 * 64
+    q, k = (x[:n].view(3, 5, 4, 64) for x in flat)
+    moved_q, moved_k = (x[64:64 + n].view(3, 5, 4, 64) for x in flat)
+    same = torch.empty(1, 1, 1, 64, device="cuda").expand(3, 5, 4, 64)
+    c, s = tq.tables(5, 64)
+    new = torch.empty_like(q)
+    g = torch.randn_like(q)
+    for out in ((same, new), (new, same), (moved_q, new), (new, moved_k), (k, new), (new, q), (new, new)):
+        with pytest.raises(ValueError, match="overlap"):
+            fb.fewbit_qk_norm_rope_fwd(q, k, None, None, c, s, out=out)
+        with pytest.raises(ValueError, match="overlap"):
+            fb.fewbit_qk_norm_rope_bwd(g, g.clone(), q, k, None, None, c, s, out=out, weight_grads=False)
+    with pytest.raises(ValueError, match="overlap"):
+        fb.fewbit_qk_norm_rope_bwd(moved_q.contiguous(), moved_k, q, k.clone(), None, None, c, s, out=(new, k), weight_grads=False)
+    want = fb.fewbit_qk_norm_rope_fwd(q, k, None, None, c, s)
+    fb.fewbit_qk_norm_rope_fwd(q, k, None, None, c, s, out=(q, k))
+    assert torch.equal(q, want[0]) and torch.equal(k, want[1])
