@@ -36,6 +36,11 @@ fewbit_dtype dtype_of(const Tensor &t) {
 }
 void *stream_of(const Tensor &t) { return c10::cuda::getCurrentCUDAStream(t.get_device()).stream(); }
 
+// A size that the C structs hold in 31 bits; more than that (a view expanded to it) would come out as another size.
+int size_of(int64_t n) {
+    if (n > INT32_MAX) refuse("the tensors are too large: batch, heads and head_dim are counted in 31 bits");
+    return static_cast<int>(n);
+}
 // (batch, length, heads, head_dim) or (rows, heads, head_dim)
 fewbit_heads heads_of(const Tensor &t) {
     const auto st = t.strides();
@@ -60,11 +65,11 @@ fewbit_qk_shape qk_shape(const Tensor &q, const Tensor &k, const Optional &qw, c
         refuse("q and k must have one type and device, and the same batch, length and head_dim");
     fewbit_qk_shape s = {};
     s.dtype = dtype_of(q);
-    s.batch = q.size(0);
+    s.batch = size_of(q.size(0));
     s.length = q.size(1);
-    s.heads = static_cast<int>(q.size(2));
-    s.kv_heads = static_cast<int>(k.size(2));
-    s.head_dim = static_cast<int>(std::min<int64_t>(q.size(3), INT32_MAX));
+    s.heads = size_of(q.size(2));
+    s.kv_heads = size_of(k.size(2));
+    s.head_dim = size_of(q.size(3));
     s.interleaved = interleaved;
     s.eps = static_cast<float>(eps);
     s.q_weight = vector_of(qw, q, q.size(3));
@@ -166,13 +171,13 @@ Attention attention_shape(const Tensor &q, const Tensor &k, const Tensor &v, boo
     Attention a;
     fewbit_attention_shape &s = a.s;
     s.dtype = dtype_of(q);
-    s.heads = static_cast<int>(q.size(n - 2));
-    s.kv_heads = static_cast<int>(k.size(n - 2));
-    s.head_dim = static_cast<int>(std::min<int64_t>(q.size(n - 1), INT32_MAX));
+    s.heads = size_of(q.size(n - 2));
+    s.kv_heads = size_of(k.size(n - 2));
+    s.head_dim = size_of(q.size(n - 1));
     s.causal = causal;
     s.scale = static_cast<float>(scale ? *scale : 1.0 / std::sqrt(static_cast<double>(q.size(n - 1))));
     if (!packed) {
-        s.batch = static_cast<int>(q.size(0));
+        s.batch = size_of(q.size(0));
         s.q_len = q.size(1);
         s.k_len = k.size(1);
         a.stats = {q.size(0), q.size(2), q.size(1)};
@@ -181,7 +186,7 @@ Attention attention_shape(const Tensor &q, const Tensor &k, const Tensor &v, boo
     for (const Tensor *o : {&*q_offsets, &*k_offsets})
         if (o->scalar_type() != at::kInt || o->device() != q.device() || o->dim() != 1 || o->numel() < 1 || o->numel() != q_offsets->numel() || !o->is_contiguous())
             refuse("q_offsets and k_offsets must be contiguous vectors of batch + 1 int32 values on the device of q");
-    s.batch = static_cast<int>(q_offsets->numel() - 1);
+    s.batch = size_of(q_offsets->numel() - 1);
     s.q_rows = q.size(0);
     s.k_rows = k.size(0);
     s.q_len = std::min(*max_q, s.q_rows);

@@ -44,3 +44,15 @@ def test_outputs_that_overlap_are_refused():
     want = fb.fewbit_qk_norm_rope_fwd(q, k, None, None, c, s)
     fb.fewbit_qk_norm_rope_fwd(q, k, None, None, c, s, out=(q, k))
     assert torch.equal(q, want[0]) and torch.equal(k, want[1])
+
+
+@pytest.mark.gpu
+def test_sizes_past_31_bits_are_refused():
+    x = torch.zeros(1, 1, 1, 8, device="cuda", dtype=torch.bfloat16)
+    many = 2 ** 32 + 1
+    for shape in ((many, 1, 1, 8), (1, 1, many, 8)):
+        big = x.expand(shape)
+        with pytest.raises(ValueError, match="too large"):
+            fb.fewbit_attention_fwd(big, big, big)
+        with pytest.raises(ValueError, match="too large"):
+            fb.fewbit_qk_norm_rope_fwd(big, big, None, None, None, None)
