@@ -43,6 +43,7 @@ class FewBitAdamW(torch.optim.Optimizer):
         super().add_param_group(group)
         for p in self.param_groups[-1]["params"]:
             if not p.is_cuda or not p.is_contiguous() or p.dtype not in (torch.float32, torch.bfloat16, torch.float16):
+                del self.param_groups[-1]
                 raise ValueError("parameters must be contiguous CUDA tensors of float32, bfloat16 or float16")
 
     def __getstate__(self):

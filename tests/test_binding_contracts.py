@@ -56,3 +56,14 @@ def test_sizes_past_31_bits_are_refused():
             fb.fewbit_attention_fwd(big, big, big)
         with pytest.raises(ValueError, match="too large"):
             fb.fewbit_qk_norm_rope_fwd(big, big, None, None, None, None)
+
+
+@pytest.mark.gpu
+def test_a_refused_parameter_group_is_not_kept():
+    p = torch.nn.Parameter(torch.zeros(8, device="cuda"))
+    opt = fb.FewBitAdamW([p])
+    with pytest.raises(ValueError):
+        opt.add_param_group({"params": [torch.nn.Parameter(torch.zeros(4))]})
+    assert len(opt.param_groups) == 1
+    p.grad = torch.ones_like(p)
+    opt.step()
