@@ -167,6 +167,16 @@ def test_one_key_that_is_not_a_number_makes_the_rows_that_see_it_nan(d):
                 assert torch.equal(out[0].transpose(0, 1)[~seen], clean[0][0].transpose(0, 1)[~seen])
 
 
+def test_gradients_of_scores_that_are_far_apart():
+    """Scores of up to a hundred: P is nearly 0 or 1, and dS a difference of near values.  The bound of `compare` has delta's error
+    (from the rounded output) in it; the scores' own rounding, 144 x 2^-24 in the exponent, is 2^-17 of P and below its 5 %."""
+    q, k, v, g = ta.make(1, 200, 1500, 2, 1, 64, torch.bfloat16, seed=3)
+    k = k * torch.linspace(0.05, 6, 1500, device="cuda")[None, :, None, None].bfloat16()
+    out, lse = fb.fewbit_attention_fwd(q, k, v, scale=0.5)
+    dq, dk, dv = fb.fewbit_attention_bwd(g, q, k, v, out, lse, scale=0.5)
+    ta.compare(q[0], k[0], v[0], g[0], {"out": out[0], "lse": lse[0], "dq": dq[0], "dk": dk[0], "dv": dv[0]}, False, 0.5)
+
+
 # ---- the count of waits that gave up ----------------------------------------------------------------------------------------
 def test_the_timeout_count_waits_for_every_stream():
     x = torch.randn(8192, 8192, device="cuda").bfloat16()
