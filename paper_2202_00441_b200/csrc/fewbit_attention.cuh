@@ -1024,6 +1024,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             __syncwarp();
             if (lane == 0) barrier_arrive(bar(kK));
         }
+        const int alone = p.causal && k0 == 0 && reach <= 0 ? -reach : INT_MIN;   // the one row that sees key 0 and no other
         int tile = rank;                                              // of this head, from `first` on
         for (int j = 0; j < n; ++j, tile += p.split) {
             while (tile >= each) tile -= each;                        // the next head
@@ -1075,13 +1076,6 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             }
 #pragma unroll
             for (int c = 0; c < 16; ++c) out[c] = pack2<T>(prob[2 * c], prob[2 * c + 1]);
-            if (p.causal && k0 == 0 && reach <= 0 && -reach - q0 >= 0 && -reach - q0 < kTile) {
-                // the one row that sees key 0 alone: its P is 1 and its dS 0, as in the dQ kernel
-                const int lone = -reach - q0 - 32 * part - 2 * (lane % 4);
-#pragma unroll
-                for (int x = 0; x < 32; ++x)
-                    if (8 * (x / 4 % 4) + x % 2 == lone) prob[x] = 0.0f;
-            }
             ok = j == 0 || wait(kDsUsed, (j - 1) & 1);
             if (!ok) break;
             fence_after();
@@ -1091,6 +1085,12 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             fence_before();
             __syncwarp();
             if (lane == 0) barrier_arrive(bar(kP));
+            if (static_cast<uint32_t>(alone - q0) < kTile) {          // its P is 1 and its dS 0, as in the dQ kernel
+                const int place = alone - q0 - 32 * part - 2 * (lane % 4);
+#pragma unroll
+                for (int x = 0; x < 32; ++x)
+                    if (8 * (x / 4 % 4) + x % 2 == place) prob[x] = 0.0f;
+            }
             ok = wait(kDp, j & 1);
             if (!ok) break;
             fence_after();
