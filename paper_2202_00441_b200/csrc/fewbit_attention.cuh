@@ -217,12 +217,14 @@ __device__ __forceinline__ void end_cta(uint32_t tmem) {
 // ---------------------------------------------------------------------------------------------------
 // forward
 // ---------------------------------------------------------------------------------------------------
-// One pass over the keys with a running reference and sum of the softmax.  For each pair of row tiles and key tile: 2048
+// One pass over the keys with a running reference and sum of the softmax (Milakov and Gimelshein, Online normalizer calculation
+// for softmax, 2018; that the reference may stay while it does no harm, and that a share of the exponentials may be computed by a
+// polynomial, is known from later published work on attention).  For each pair of row tiles and key tile: 2048
 // clocks of products, 2048 of exponentials (of which a quarter goes elsewhere), 64 KB from L2.  Two row tiles share every
 // K and V tile that is loaded, and each one's softmax runs while the other's products do.  Measured, bfloat16, heads of
-// 128, causal: 16384 rows, 8 heads on 2, 489 us = 1.12 PFLOP/s, 67 % of a burst of matrix products and 80 % of what they
-// sustain: the power limit holds the SMs at 1.6 GHz there; 4 x 2048 rows, 16 heads on 4, 84 us = 0.82 PFLOP/s: 512 CTAs of
-// 2 to 16 key tiles, each with a start and an end that no product covers.  One row on 8192 keys: 26 us, 8 tiles one
+// 128, causal: 16384 rows, 8 heads on 2, 484 us = 1.14 PFLOP/s, 68 % of a burst of matrix products and 81 % of what they
+// sustain: the power limit holds the SMs at 1.6 GHz there; 4 x 2048 rows, 16 heads on 4, 89 us = 0.77 PFLOP/s: 512 CTAs of
+// 2 to 16 key tiles, each with a start and an end that no product covers.  One row on 8192 keys: 25 us, 8 tiles one
 // after another in each of 64 CTAs and the joining of their sums.
 // Barriers: q (2 row tiles), k full/empty (2 stages), v full/empty, S full (2), the first half of each thread's part of P
 // ready (2), all of it (2), O done (2), drained.
@@ -541,7 +543,7 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
 // Three products (1536 clocks) and 1024 of exponentials for each row and key tile, which loads 64 KB for the one row tile
 // that tensor and shared memory have room for: 37 bytes a clock into each SM are what L2 gives when all SMs ask, so the loads
 // take 1750 clocks and bound it.  Tensor pipe 42 % active on 4 x 2048 rows, 16 heads on 4, causal; the whole backward pass
-// takes 276 us there (0.62 PFLOP/s counting five products, 0.87 counting the seven that are computed), and 1.62 ms for
+// takes 275 us there (0.62 PFLOP/s counting five products, 0.87 counting the seven that are computed), and 1.61 ms for
 // 16384 rows, 8 heads on 2 (0.85 and 1.18 PFLOP/s, the latter 84 % of what matrix products sustain at the power limit).
 // Barriers: q and g, k full/empty (3 stages: a tile is used twice, one iteration apart), v full/empty (2 stages), S full (2),
 // dP full, dS ready, dQ done.
@@ -555,7 +557,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
     constexpr int HALVES = DIM / 64;
     constexpr uint32_t kBytes = HALVES * kHalfTile;
     extern __shared__ __align__(1024) uint8_t raw[];
-    const uint32_t base = smem_address(raw);                          // no room to align it here: the host checks
+    const uint32_t base = smem_address(raw);                          // (its declaration aligns it: there is no room to do it here)
     Sync *sync = reinterpret_cast<Sync *>(raw + 7 * kBytes);
     float *row_delta = reinterpret_cast<float *>(sync + 1);           // [128]
     float *row_sum = row_delta + kTile;                               // [4][128]
@@ -844,7 +846,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
 // Four products (2048 clocks) and 1024 of exponentials for each row and key tile.  The key tile's K stays in tensor memory and
 // its V in shared memory, so that Q and dO have three stages each.  What is left between the products is the chain of one
 // tile: S, its exponentials, dP, dS, and their way through tensor memory, 2850 clocks with two tiles' products interleaved.
-// Tensor pipe 58 % active on 4 x 2048 rows, 16 heads on 4, causal, where it takes half of the pass's 276 us.
+// Tensor pipe 60 % active on 4 x 2048 rows, 16 heads on 4, causal, where it takes half of the pass's 275 us.
 // Barriers: v, k in tensor memory, q full/empty (3 stages), g full/empty (3 stages), statistics full/empty (2 stages), S full
 // and read, dP full and read, P ready and used, dS ready and used, done.
 enum { kV = 0, kK = 1, kQFull = 2, kQEmpty = 5, kGFull = 8, kGEmpty = 11, kTFull = 14, kTEmpty = 16, kS = 18, kSRead = 19, kDp = 20, kDpRead = 21, kP = 22,

@@ -26,13 +26,13 @@ namespace {
 constexpr int kQkThreads = 256;
 constexpr int kQkMaxDim = 256;
 // Heads in flight and CTAs on an SM, chosen together: bytes in flight against registers.  Measured on 4 x 8192 tokens,
-// 32 + 8 heads of 128, bfloat16, forward / backward in us: (4, 2 CTAs) 112 / -, (4, 3) 129 / -, (2, 3) 137 / -, (2, 4) 143 / -;
+// 32 + 8 heads of 128, bfloat16, forward / backward in us, back to back on the same tensors: (4, 2 CTAs) 111 / -, (4, 3) 129 / -, (2, 3) 137 / -, (2, 4) 143 / -;
 // (2, 2) - / 210, (1, 2) - / 213, (1, 3) - / 306, (2, 3) - / 361 (spilled registers).  With copies ahead (Ahead, below) the
-// backward pass takes 164 to 178, by where the tensors lie, 6.15 to 5.7 TB/s = 94 to 87 % of the copy bandwidth; heads half of
-// which are rotated 245 -> 165, neighbouring pairs 284 -> 172, heads of 96 elements 233 -> 148, of 80 227 -> 147.  The forward
-// pass of 16-bit types, at 6.05 TB/s = 92 %, loses by them with full lanes (1, 2, 3, 5 heads ahead: 147, 121, 131, 133; bursts of
+// backward pass takes 162 to 168, and 176 = 88 % of the copy bandwidth where every pass has other tensors than the last (back to
+// back, part of what the last pass wrote is still in L2); heads half of which are rotated 245 -> 165, neighbouring pairs 284 -> 172, heads of 96 elements 233 -> 148, of 80 227 -> 147.  The forward
+// pass of 16-bit types, 116 = 89 % with other tensors each time, loses by them with full lanes (1, 2, 3, 5 heads ahead: 147, 121, 131, 133; bursts of
 // 4 or 8 heads: 132, 126): its bursts of loads between stores suit the memory better.  Binary32 gains with 2 heads ahead,
-// 235 -> 215 = 95 % (3: 236), and so do the forms without full lanes (2 / 3 heads ahead): heads half of which are rotated
+// 235 -> 215 (3: 236; 222 = 92 % with other tensors each time), and so do the forms without full lanes (2 / 3 heads ahead): heads half of which are rotated
 // 135 -> 113 / 119, of 96 elements 128 -> 103 / 96, of 80 121 -> 97 / 93.
 constexpr int kFwdHeads = 4, kBwdHeads = 2;
 constexpr int kChunkHeads = 8;

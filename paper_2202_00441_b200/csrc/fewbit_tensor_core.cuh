@@ -284,7 +284,8 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 
 // 2^x for two values on the FMA pipe, which has room where the exponential unit (16 results a clock) is the limit:
-// x = n + f with n the nearest integer, f in [-1/2, 1/2]; 2^f by the degree-4 polynomial of least relative error (2.6e-6,
+// x = n + f with n the nearest integer, f in [-1/2, 1/2] (as in Cody and Waite, Software Manual for the Elementary Functions,
+// 1980); 2^f by the degree-4 polynomial of least relative error (2.6e-6,
 // found by iteratively reweighted least squares), n added to the exponent.  Values below 2^-126 come out as 2^-126; a NaN or
 // an infinity comes out as a value that is not finite in 16 bits but may be in 32: where such a value may be the only one of a
 // sum, the caller has to see to it.
