@@ -463,6 +463,87 @@ typedef struct fewbit_adamw_options {
 FEWBIT_API fewbit_status fewbit_adamw_step(const fewbit_adamw_tensor *tensors, const void *const *grads, int count,
                                            const fewbit_adamw_options *options, void *stream);
 
+/*
+ * Dropout whose mask is drawn from a counter wherever it is needed and never
+ * stored.  Element e (counted over the whole tensor) takes word e % 4 of the
+ * Philox4x32-10 block (Salmon et al., 2011) of the counter
+ * (e / 4 mod 2^32, e / 2^34, place, 0) under the key (seed mod 2^32, seed / 2^32);
+ * it is kept where that word is at least round(p * 2^32), and multiplied by
+ * 1 / (1 - p).
+ *   p            0 <= p < 1; 0: nothing is drawn
+ *   seed         of the step;  seed_device  DEVICE (8-byte aligned) or NULL: one
+ *                value that is added to it, so that a captured graph draws anew
+ *                each time.  The backward pass needs the forward pass's values.
+ *   place        tells one use of a seed from another (a layer's number)
+ */
+typedef struct fewbit_dropout_options {
+    double p;
+    uint64_t seed;
+    const int64_t *seed_device;
+    uint32_t place;
+} fewbit_dropout_options;
+
+/*
+ * y = residual + dropout(x), in binary32, rounded once.  x, residual (NULL:
+ * none), y: DEVICE, n elements of `dtype`, aligned to the element type (16-byte
+ * aligned ones move in wider pieces); y may alias x or residual exactly.
+ * Errors: INVALID_ARG, TOO_LARGE, ALIGNMENT, CUDA.
+ */
+FEWBIT_API fewbit_status fewbit_dropout_fwd(const void *x, const void *residual, void *y, size_t n, fewbit_dtype dtype,
+                                            const fewbit_dropout_options *options, void *stream);
+
+/* grad_in = grad_out where x was kept, times 1 / (1 - p); else 0.  (The residual's gradient is grad_out.) */
+FEWBIT_API fewbit_status fewbit_dropout_bwd(const void *grad_out, void *grad_in, size_t n, fewbit_dtype dtype,
+                                            const fewbit_dropout_options *options, void *stream);
+
+/*
+ * A branch's addition to the residual stream and the RMS norm of the sum:
+ *     h = residual + dropout(x),   y = h / sqrt(mean(h^2) + eps) * weight
+ * for each row of `width` elements, in binary32; h is rounded when it is stored,
+ * the norm takes it as it was.
+ *   rows, width   of contiguous tensors; width up to 16384
+ *   weight        DEVICE, width binary32 values, or NULL for ones
+ *   dropout       of x; an element's number is row * width + column
+ * The struct is HOST memory, read during the call only.
+ */
+typedef struct fewbit_norm_shape {
+    int64_t rows, width;
+    const float *weight;
+    float eps;
+    fewbit_dtype dtype;
+    fewbit_dropout_options dropout;
+} fewbit_norm_shape;
+
+/*
+ * residual: NULL for none.  h: NULL if it is not wanted.  y_bits 0: y has `dtype`
+ * and y_scale is NULL.  y_bits 8: y holds e4m3 codes (one byte each), y_scale
+ * one binary32 value a row: y = code * scale, scale = (largest magnitude of the
+ * row) / 448, codes rounded to nearest; a row with a non-finite value gets a NaN
+ * scale, one whose largest magnitude is below 2^-117 reads back as zero.
+ * An output may alias an input of the same type exactly.  One launch.
+ * Errors: INVALID_ARG (NULL, sizes, eps < 0 or NaN, p), UNSUPPORTED (width),
+ * TOO_LARGE (rows above 2^31 - 1), ALIGNMENT, CUDA.
+ */
+FEWBIT_API fewbit_status fewbit_add_rms_norm_fwd(const fewbit_norm_shape *shape, const void *x, const void *residual, void *h, void *y,
+                                                 float *y_scale, int y_bits, void *stream);
+
+/* Bytes of `workspace` for the backward pass with a weight gradient; 0 without a device or for a bad shape. */
+FEWBIT_API size_t fewbit_add_rms_norm_workspace_bytes(const fewbit_norm_shape *shape);
+
+/*
+ * Gradients of fewbit_add_rms_norm_fwd from grad_y, the gradient grad_h that
+ * reaches h from elsewhere (NULL: none) and h as it was stored:
+ * grad_residual (the sum's) and grad_x (the same through the dropout), either
+ * may be NULL; grad_weight: width binary32 values, or NULL.  With it:
+ * `workspace` (DEVICE, 16-byte aligned), and a second launch that adds up the
+ * partial sums in a fixed order.  (The rounding of 8-bit results has no gradient
+ * of its own: grad_y passes it as it is.)  An output may alias an input exactly.
+ * Errors as above, ALLOC (workspace too small).
+ */
+FEWBIT_API fewbit_status fewbit_add_rms_norm_bwd(const fewbit_norm_shape *shape, const void *grad_y, const void *grad_h, const void *h,
+                                                 void *grad_x, void *grad_residual, float *grad_weight, void *workspace,
+                                                 size_t workspace_bytes, void *stream);
+
 /* ------------------------------------------------------------------------- */
 /* Hot path on HOST buffers                                                   */
 /* ------------------------------------------------------------------------- */

@@ -13,9 +13,11 @@ from .binding import (  # noqa: F401
     fewbit_set_option, fewbit_get_option, fewbit_tail_warp_count,
 )
 from .operators import (  # noqa: F401
-    fewbit_adamw_create, fewbit_adamw_step, fewbit_attention_bwd, fewbit_attention_fwd,
-    fewbit_attention_timeout_count, fewbit_qk_norm_rope_bwd, fewbit_qk_norm_rope_fwd,
+    fewbit_adamw_create, fewbit_adamw_step, fewbit_add_rms_norm_bwd, fewbit_add_rms_norm_fwd, fewbit_attention_bwd, fewbit_attention_fwd,
+    fewbit_attention_timeout_count, fewbit_dropout_bwd, fewbit_dropout_fwd, fewbit_qk_norm_rope_bwd, fewbit_qk_norm_rope_fwd,
 )
 from . import workloads  # noqa: F401
-from .autograd import FewBitActivation, fewbit_activation, fewbit_attention, fewbit_qk_norm_rope  # noqa: F401
+from .autograd import (  # noqa: F401
+    FewBitActivation, fewbit_activation, fewbit_add_rms_norm, fewbit_attention, fewbit_dropout, fewbit_qk_norm_rope,
+)
 from .optim import FewBitAdamW  # noqa: F401

@@ -14,7 +14,10 @@ from torch import nn
 from torch.autograd.function import once_differentiable
 
 from .binding import Table, fewbit_bwd, fewbit_fwd, fewbit_fwd_bias, fewbit_table_create, fewbit_table_create_folded
-from .operators import fewbit_attention_bwd, fewbit_attention_fwd, fewbit_qk_norm_rope_bwd, fewbit_qk_norm_rope_fwd
+from .operators import (
+    fewbit_add_rms_norm_bwd, fewbit_add_rms_norm_fwd, fewbit_attention_bwd, fewbit_attention_fwd, fewbit_dropout_bwd, fewbit_dropout_fwd,
+    fewbit_qk_norm_rope_bwd, fewbit_qk_norm_rope_fwd,
+)
 
 
 def _flat_aligned(t: torch.Tensor) -> torch.Tensor:
@@ -168,3 +171,67 @@ def fewbit_qk_norm_rope(q: torch.Tensor, k: torch.Tensor, q_weight: torch.Tensor
     if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (cos, sin)):
         raise ValueError("cos and sin have no gradient here: pass tables that do not require one (detach them)")
     return _QkNormRopeFunction.apply(q, k, q_weight, k_weight, cos, sin, positions, {"eps": eps, "interleaved": interleaved})
+
+
+def _kept_seed(ctx, seed, *tensors):
+    """Keeps the call's tensors and a seed on the device (autograd then refuses a backward pass when one has been changed)."""
+    ctx.seed = None if isinstance(seed, torch.Tensor) else seed
+    ctx.save_for_backward(*tensors, seed if isinstance(seed, torch.Tensor) else None)
+
+
+class _DropoutFunction(torch.autograd.Function):
+    """Keeps nothing but the seed."""
+
+    @staticmethod
+    def forward(ctx, x, residual, seed, p, place):
+        ctx.p, ctx.place = p, place
+        _kept_seed(ctx, seed)
+        return fewbit_dropout_fwd(x.contiguous(), p, seed=seed, place=place, residual=None if residual is None else residual.contiguous())
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad):
+        (seed,) = ctx.saved_tensors
+        dx = fewbit_dropout_bwd(grad.contiguous(), ctx.p, seed=ctx.seed if seed is None else seed, place=ctx.place) if ctx.needs_input_grad[0] else None
+        return dx, grad if ctx.needs_input_grad[1] else None, None, None, None
+
+
+def fewbit_dropout(x: torch.Tensor, p: float, *, seed, place: int = 0, residual: torch.Tensor | None = None) -> torch.Tensor:
+    """``residual`` + dropout of ``x`` (without it: the dropout alone) with gradients for both; arguments as in
+    ``fewbit_dropout_fwd``.  Nothing is kept for the backward pass: the mask is drawn again from ``seed`` and ``place``.  A seed
+    on the device that is changed before the backward pass is autograd's error.  Evaluation: p = 0."""
+    return _DropoutFunction.apply(x, residual, seed, float(p), place)
+
+
+class _AddRmsNormFunction(torch.autograd.Function):
+    """Keeps h, which the residual stream carries on, and the weight: mask and norm's factor are computed again."""
+
+    @staticmethod
+    def forward(ctx, x, residual, weight, seed, eps, p, place):
+        wide = None if weight is None else weight.detach().float().contiguous()
+        y, h = fewbit_add_rms_norm_fwd(x.contiguous(), None if residual is None else residual.contiguous(), wide, eps=eps, p=p, seed=seed, place=place)
+        if h.data_ptr() == x.data_ptr():
+            h = h.view_as(h)                  # an input that is returned: as a tensor of its own
+        ctx.kw, ctx.weight_type = {"eps": eps, "p": p, "place": place}, None if weight is None else weight.dtype
+        ctx.set_materialize_grads(False)
+        _kept_seed(ctx, seed, h, wide)
+        return y, h
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad_y, grad_h):
+        h, wide, seed = ctx.saved_tensors
+        want_x, want_residual, want_weight = ctx.needs_input_grad[:3]
+        if grad_y is None:
+            grad_y = torch.zeros_like(h)
+        dx, dr, dw = fewbit_add_rms_norm_bwd(grad_y.contiguous(), None if grad_h is None else grad_h.contiguous(), h, wide,
+                                             seed=ctx.seed if seed is None else seed, x_grad=want_x, residual_grad=want_residual,
+                                             weight_grad=want_weight, **ctx.kw)
+        return dx, dr, None if dw is None else dw.to(ctx.weight_type), None, None, None, None
+
+
+def fewbit_add_rms_norm(x: torch.Tensor, residual: torch.Tensor | None, weight: torch.Tensor | None, *, eps: float = 1e-6,
+                        p: float = 0.0, seed=0, place: int = 0):
+    """h = residual + dropout(x) and its RMS norm times ``weight`` (of any floating type), with gradients for all three; returns
+    (y, h), where h goes on as the next residual.  Arguments as in ``fewbit_add_rms_norm_fwd``; the backward pass keeps h alone."""
+    return _AddRmsNormFunction.apply(x, residual, weight, seed, float(eps), float(p), place)

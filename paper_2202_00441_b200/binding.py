@@ -103,6 +103,14 @@ def load_library():
     lib.fewbit_attention_workspace_bytes.argtypes = [vp]
     lib.fewbit_attention_timeout_count.argtypes = [ctypes.POINTER(ctypes.c_uint64)]
     lib.fewbit_adamw_step.argtypes = [vp, vp, ci, vp, vp]
+    for name in ("fewbit_dropout_fwd", "fewbit_dropout_bwd", "fewbit_add_rms_norm_fwd", "fewbit_add_rms_norm_bwd"):
+        getattr(lib, name).restype = ci
+    lib.fewbit_dropout_fwd.argtypes = [vp, vp, vp, sz, ci, vp, vp]
+    lib.fewbit_dropout_bwd.argtypes = [vp, vp, sz, ci, vp, vp]
+    lib.fewbit_add_rms_norm_fwd.argtypes = [vp] * 6 + [ci, vp]
+    lib.fewbit_add_rms_norm_bwd.argtypes = [vp] * 8 + [sz, vp]
+    lib.fewbit_add_rms_norm_workspace_bytes.restype = sz
+    lib.fewbit_add_rms_norm_workspace_bytes.argtypes = [vp]
     lib.fewbit_f32_activation_scan.restype = ci
     lib.fewbit_f32_activation_scan.argtypes = [ci, ctypes.c_uint64, ctypes.c_uint64, vp, vp]
     _lib = lib

@@ -7,6 +7,7 @@
 #include <c10/cuda/CUDAStream.h>
 
 #include <optional>
+#include <variant>
 #include <vector>
 
 #include "fewbit.h"
@@ -229,6 +230,128 @@ std::tuple<Tensor, Tensor, Tensor> attention_bwd(const Tensor &g, const Tensor &
     return {dq, dk, dv};
 }
 
+// Dropout's numbers: `seed` is an integer or one int64 value on the device of the tensors.
+using Seed = std::variant<uint64_t, Tensor>;
+fewbit_dropout_options drop_of(double p, const Seed &seed, int64_t place, const Tensor &x) {
+    if (!(p >= 0.0 && p < 1.0)) refuse("p must be at least 0 and below 1");
+    if (place < 0 || place > UINT32_MAX) refuse("place must be a whole number of 32 bits");
+    fewbit_dropout_options o = {p, 0, nullptr, static_cast<uint32_t>(place)};
+    if (const Tensor *t = std::get_if<Tensor>(&seed)) {
+        if (t->scalar_type() != at::kLong || t->numel() != 1 || t->device() != x.device()) refuse("seed must be an integer or one int64 value on the device of the tensors");
+        o.seed_device = t->data_ptr<int64_t>();
+    } else {
+        o.seed = std::get<uint64_t>(seed);
+    }
+    return o;
+}
+// An output against the inputs of its call: one of them element for element, or no shared memory at all.
+void whole_or_none(const Tensor &out, std::initializer_list<const Tensor *> inputs) {
+    for (const Tensor *t : inputs)
+        if (t != nullptr && at::get_overlap_status(out, *t) == at::MemOverlapStatus::Partial) refuse("out overlaps an input in part");
+}
+void dense(const Tensor &t, const char *what) {
+    if (!t.is_cuda() || !t.is_contiguous()) refuse(what);
+}
+
+Tensor dropout_fwd(const Tensor &x, double p, const Seed &seed, int64_t place, const Optional &residual, const Optional &out) {
+    dense(x, "x must be a contiguous CUDA tensor");
+    const fewbit_dtype dtype = dtype_of(x);
+    const fewbit_dropout_options o = drop_of(p, seed, place, x);
+    if (residual) {
+        like(*residual, x, "residual must have the shape, type and device of x");
+        dense(*residual, "residual must be contiguous");
+    }
+    const c10::cuda::OptionalCUDAGuard guard(x.device());
+    Tensor y = out ? *out : at::empty(x.sizes(), x.options());
+    if (out) {
+        like(y, x, "out must have the shape, type and device of x");
+        dense(y, "out must be contiguous");
+        whole_or_none(y, {&x, residual ? &*residual : nullptr});
+    }
+    check(fewbit_dropout_fwd(x.data_ptr(), residual ? residual->data_ptr() : nullptr, y.data_ptr(), x.numel(), dtype, &o, stream_of(x)), "fewbit_dropout_fwd");
+    return y;
+}
+Tensor dropout_bwd(const Tensor &g, double p, const Seed &seed, int64_t place, const Optional &out) {
+    dense(g, "grad_out must be a contiguous CUDA tensor");
+    const fewbit_dtype dtype = dtype_of(g);
+    const fewbit_dropout_options o = drop_of(p, seed, place, g);
+    const c10::cuda::OptionalCUDAGuard guard(g.device());
+    Tensor y = out ? *out : at::empty(g.sizes(), g.options());
+    if (out) {
+        like(y, g, "out must have the shape, type and device of grad_out");
+        dense(y, "out must be contiguous");
+        whole_or_none(y, {&g});
+    }
+    check(fewbit_dropout_bwd(g.data_ptr(), y.data_ptr(), g.numel(), dtype, &o, stream_of(g)), "fewbit_dropout_bwd");
+    return y;
+}
+
+fewbit_norm_shape norm_shape(const Tensor &x, const Optional &weight, double eps, double p, const Seed &seed, int64_t place) {
+    dense(x, "the tensors must be contiguous and on a CUDA device");
+    if (x.dim() < 1) refuse("the tensors must have a last dimension");
+    fewbit_norm_shape s = {};
+    s.dtype = dtype_of(x);
+    s.width = x.size(x.dim() - 1);
+    s.rows = 1;
+    for (int64_t i = 0; i + 1 < x.dim(); ++i) s.rows *= x.size(i);
+    s.eps = static_cast<float>(eps);
+    s.dropout = drop_of(p, seed, place, x);
+    if (weight) {
+        if (weight->scalar_type() != at::kFloat || weight->device() != x.device() || weight->dim() != 1 || weight->numel() != s.width || !weight->is_contiguous())
+            refuse("weight must be a contiguous float32 vector with a value for each element of the last dimension, on the device of the tensors");
+        s.weight = weight->data_ptr<float>();
+    }
+    return s;
+}
+std::vector<Tensor> add_rms_norm_fwd(const Tensor &x, const Optional &residual, const Optional &weight, double eps, double p, const Seed &seed, int64_t place,
+                                     std::optional<int64_t> bits) {
+    const fewbit_norm_shape s = norm_shape(x, weight, eps, p, seed, place);
+    if (bits && *bits != 8) refuse("bits must be 8 or None");
+    if (residual) {
+        like(*residual, x, "residual must have the shape, type and device of x");
+        dense(*residual, "residual must be contiguous");
+    }
+    const c10::cuda::OptionalCUDAGuard guard(x.device());
+    const bool sum = residual || p > 0.0;                             // else h is x
+    Tensor h = sum ? at::empty(x.sizes(), x.options()) : x;
+    Tensor y = at::empty(x.sizes(), bits ? x.options().dtype(at::kFloat8_e4m3fn) : x.options()), scale;
+    if (bits) scale = at::empty(x.sizes().slice(0, x.dim() - 1), x.options().dtype(at::kFloat));
+    check(fewbit_add_rms_norm_fwd(&s, x.data_ptr(), residual ? residual->data_ptr() : nullptr, sum ? h.data_ptr() : nullptr, y.data_ptr(),
+                                  bits ? scale.data_ptr<float>() : nullptr, bits ? 8 : 0, stream_of(x)),
+          "fewbit_add_rms_norm_fwd");
+    if (bits) return {y, scale, h};
+    return {y, h};
+}
+std::tuple<Optional, Optional, Optional> add_rms_norm_bwd(const Tensor &grad_y, const Optional &grad_h, const Tensor &h, const Optional &weight, double eps, double p,
+                                                          const Seed &seed, int64_t place, bool x_grad, bool residual_grad, bool weight_grad) {
+    const fewbit_norm_shape s = norm_shape(h, weight, eps, p, seed, place);
+    like(grad_y, h, "grad_y must have the shape, type and device of h");
+    dense(grad_y, "grad_y must be contiguous");
+    if (grad_h) {
+        like(*grad_h, h, "grad_h must have the shape, type and device of h");
+        dense(*grad_h, "grad_h must be contiguous");
+    }
+    const c10::cuda::OptionalCUDAGuard guard(h.device());
+    // without dropout the two gradients are one
+    const bool dropped = p > 0.0;
+    Optional gx, gr, gw;
+    if (residual_grad || (x_grad && !dropped)) gr = at::empty(h.sizes(), h.options());
+    if (x_grad && dropped) gx = at::empty(h.sizes(), h.options());
+    Tensor ws;
+    size_t bytes = 0;
+    if (weight_grad) {
+        gw = at::empty({s.width}, h.options().dtype(at::kFloat));
+        bytes = fewbit_add_rms_norm_workspace_bytes(&s);
+        ws = at::empty({static_cast<int64_t>(bytes)}, h.options().dtype(at::kByte));
+    }
+    check(fewbit_add_rms_norm_bwd(&s, grad_y.data_ptr(), grad_h ? grad_h->data_ptr() : nullptr, h.data_ptr(), gx ? gx->data_ptr() : nullptr,
+                                  gr ? gr->data_ptr() : nullptr, gw ? gw->data_ptr<float>() : nullptr, bytes ? ws.data_ptr() : nullptr, bytes, stream_of(h)),
+          "fewbit_add_rms_norm_bwd");
+    if (x_grad && !dropped) gx = gr;
+    if (!residual_grad) gr.reset();
+    return {gx, gr, gw};
+}
+
 // What a program keeps for its steps: the tensors, not where they lie (`p.data = ...` puts other memory under a parameter).
 class AdamW {
 public:
@@ -317,6 +440,10 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
     m.def("qk_norm_rope_bwd", &qk_norm_rope_bwd);
     m.def("attention_fwd", &attention_fwd);
     m.def("attention_bwd", &attention_bwd);
+    m.def("dropout_fwd", &dropout_fwd);
+    m.def("dropout_bwd", &dropout_bwd);
+    m.def("add_rms_norm_fwd", &add_rms_norm_fwd);
+    m.def("add_rms_norm_bwd", &add_rms_norm_bwd);
     py::class_<AdamW>(m, "AdamWTensors", "The parameters and moments of fewbit_adamw_step, made once and updated in place by every step; keeps them alive.")
         .def(py::init<std::vector<Tensor>, std::vector<Tensor>, std::vector<Tensor>, std::optional<std::vector<Tensor>>, std::optional<std::vector<Tensor>>,
                       std::optional<std::vector<Tensor>>>())

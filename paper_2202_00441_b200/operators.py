@@ -46,6 +46,15 @@ class _AdamWOptions(ctypes.Structure):
                 ("seed", ctypes.c_uint32), ("state_bits", ctypes.c_int), ("dtype", ctypes.c_int)]
 
 
+class _DropoutOptions(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("seed_device", ctypes.c_void_p), ("place", ctypes.c_uint32)]
+
+
+class _NormShape(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("weight", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("dtype", ctypes.c_int), ("dropout", _DropoutOptions)]
+
+
 _TORCH_LIB = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_fewbit_torch.so")
 _module = None
 
@@ -164,6 +173,72 @@ def fewbit_attention_timeout_count(device=None) -> int:
     with torch.cuda.device(device):
         _check(load_library().fewbit_attention_timeout_count(ctypes.byref(out)), "fewbit_attention_timeout_count")
     return int(out.value)
+
+
+# ---------------------------------------------------------------------------------------------------------------
+# dropout, and the norm of the residual stream
+# ---------------------------------------------------------------------------------------------------------------
+
+def _seed(seed):
+    return seed if isinstance(seed, torch.Tensor) else int(seed) & 0xFFFFFFFFFFFFFFFF
+
+
+def _tensor_seed(seed):
+    return seed if isinstance(seed, torch.Tensor) else None
+
+
+def fewbit_dropout_fwd(x: torch.Tensor, p: float, *, seed, place: int = 0, residual: Optional[torch.Tensor] = None,
+                       out: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """``residual`` + dropout of ``x`` (without ``residual``: the dropout alone), in one pass; the mask is not stored.
+
+    x: contiguous, float32, bfloat16 or float16.  An element is dropped with probability ``p`` (0 <= p < 1) and else multiplied
+    by 1 / (1 - p).  ``seed``: 64 bits for the step, or one int64 value on the device (so that a captured graph draws anew with
+    every value written there); ``place``: 32 bits that tell the uses of one seed apart.  The same seed, place and shape give the
+    same mask.  ``out``: x or residual itself, or a tensor that shares no memory with them."""
+    args = (x, p, _seed(seed), place, residual, out)
+    if stream is not None:
+        with _On(stream, x, residual, out, _tensor_seed(seed)):
+            return _torch_module().dropout_fwd(*args)
+    return _torch_module().dropout_fwd(*args)
+
+
+def fewbit_dropout_bwd(grad_out: torch.Tensor, p: float, *, seed, place: int = 0, out: Optional[torch.Tensor] = None,
+                       stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Gradient of ``fewbit_dropout_fwd`` for x: ``grad_out`` through the same mask, drawn again.  (For residual it is grad_out.)"""
+    args = (grad_out, p, _seed(seed), place, out)
+    if stream is not None:
+        with _On(stream, grad_out, out, _tensor_seed(seed)):
+            return _torch_module().dropout_bwd(*args)
+    return _torch_module().dropout_bwd(*args)
+
+
+def fewbit_add_rms_norm_fwd(x: torch.Tensor, residual: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None, *,
+                            eps: float = 1e-6, p: float = 0.0, seed=0, place: int = 0, bits: Optional[int] = None,
+                            stream: Optional[torch.cuda.Stream] = None):
+    """h = residual + dropout(x) and y = h / sqrt(mean(h^2) + eps) * weight over the last dimension, in one pass; returns (y, h).
+
+    x, residual: contiguous, of one shape and type (float32, bfloat16 or float16); the last dimension has up to 16384 elements.
+    weight: float32 or None.  ``p``, ``seed``, ``place``: as in ``fewbit_dropout_fwd``.  Without residual and dropout h is x itself.
+    ``bits=8``: returns (codes, scale, h): float8_e4m3fn codes and one float32 scale for each row, y = code * scale (what a
+    product in 8 bits with scales by rows takes)."""
+    args = (x, residual, weight, eps, p, _seed(seed), place, bits)
+    if stream is not None:
+        with _On(stream, x, residual, weight, _tensor_seed(seed)):
+            return tuple(_torch_module().add_rms_norm_fwd(*args))
+    return tuple(_torch_module().add_rms_norm_fwd(*args))
+
+
+def fewbit_add_rms_norm_bwd(grad_y: torch.Tensor, grad_h: Optional[torch.Tensor], h: torch.Tensor, weight: Optional[torch.Tensor] = None, *,
+                            eps: float = 1e-6, p: float = 0.0, seed=0, place: int = 0, x_grad: bool = True, residual_grad: bool = True,
+                            weight_grad: bool = True, stream: Optional[torch.cuda.Stream] = None):
+    """Gradients (grad_x, grad_residual, grad_weight) of ``fewbit_add_rms_norm_fwd`` from the gradient of y, that which reaches h
+    from elsewhere (or None) and h as the forward pass returned it; grad_weight is float32.  Those that are not wanted are None.
+    Without dropout grad_x and grad_residual are one tensor.  The same inputs give the same bits."""
+    args = (grad_y, grad_h, h, weight, eps, p, _seed(seed), place, x_grad, residual_grad, weight_grad)
+    if stream is not None:
+        with _On(stream, grad_y, grad_h, h, weight, _tensor_seed(seed)):
+            return _torch_module().add_rms_norm_bwd(*args)
+    return _torch_module().add_rms_norm_bwd(*args)
 
 
 # ---------------------------------------------------------------------------------------------------------------
