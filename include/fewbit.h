@@ -395,6 +395,79 @@ FEWBIT_API fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *shap
                                               void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * What comes between attention's products and its softmax.  With the distance
+ *     d = j - i - (k_len - q_len)
+ * of key j from row i (both counted within their sequence; the last row and
+ * the last key are level), the score of a visible key is
+ *     z = scale q.k;   cap > 0: z = cap tanh(z / cap);
+ *     z -= slopes[h] |d|;   z += distance_bias[h][clamp(d, -R, R) + R]
+ * (each where given), and row i of a sequence sees key j if
+ *     not causal, or d <= 0, or j < prefix_lens[b];   and
+ *     q_documents[i] == k_documents[j]     (where given)
+ *
+ *   cap             finite, >= 0; 0: none
+ *   slopes          DEVICE, a binary32 value for each query head, or NULL
+ *   distance_bias   DEVICE, heads x (2 R + 1) binary32 values, R = max_distance,
+ *                   1 .. FEWBIT_MAX_DISTANCE, or NULL.  -inf hides the key; so does a
+ *                   finite value below -2.3e38 (the scores are held in units of ln 2).
+ *   prefix_lens     DEVICE, int32 for each sequence, or NULL; causal attention only
+ *   q_documents, k_documents  DEVICE int32 (batch, q_len) and (batch, k_len),
+ *                   contiguous, or (q_rows) and (k_rows) for packed sequences;
+ *                   both or neither.  Any numbers; where they do not fall along a
+ *                   sequence, tiles that no document of theirs shares are skipped.
+ * Buffers are 4-byte aligned.  What is said about rows that see nothing and about
+ * non-finite values in fewbit_attention_shape holds for every key that a mask hides.
+ */
+#define FEWBIT_MAX_DISTANCE 4096
+typedef struct fewbit_attention_scores {
+    float cap;
+    const float *slopes;
+    const float *distance_bias;
+    int max_distance;
+    const int32_t *prefix_lens;
+    const int32_t *q_documents, *k_documents;
+} fewbit_attention_scores;
+
+/* fewbit_attention_fwd with these scores (NULL: the plain ones).  Errors as there. */
+FEWBIT_API fewbit_status fewbit_attention_scores_fwd(const fewbit_attention_shape *shape, const fewbit_attention_scores *scores, const fewbit_heads *q,
+                                                     const fewbit_heads *k, const fewbit_heads *v, const fewbit_heads *out, float *lse, void *stream);
+
+/*
+ * Bytes of `workspace` for the backward pass; 0 for a bad shape.  bias_gradient: with the gradient of distance_bias, which
+ * takes 4 KB for each pair of a row tile and a key tile (128 x 128) within max_distance of each other, and each head.
+ */
+FEWBIT_API size_t fewbit_attention_scores_workspace_bytes(const fewbit_attention_shape *shape, const fewbit_attention_scores *scores, int bias_gradient);
+
+/*
+ * fewbit_attention_bwd with these scores.  grad_distance_bias: heads x (2 R + 1) binary32 values, or NULL: the gradients of the
+ * scores, summed over the batch, the rows and the keys of each distance in a fixed order (one launch more).
+ */
+FEWBIT_API fewbit_status fewbit_attention_scores_bwd(const fewbit_attention_shape *shape, const fewbit_attention_scores *scores, const fewbit_heads *grad_out,
+                                                     const fewbit_heads *q, const fewbit_heads *k, const fewbit_heads *v, const fewbit_heads *out,
+                                                     const float *lse, const fewbit_heads *grad_q, const fewbit_heads *grad_k,
+                                                     const fewbit_heads *grad_v, float *grad_distance_bias, void *workspace,
+                                                     size_t workspace_bytes, void *stream);
+
+/*
+ * A learned bias of relative positions by buckets (Raffel et al., Exploring the limits of transfer learning, 2020), spread
+ * over the distances d = -R .. R for fewbit_attention_scores: distance_bias[h][d + R] = table[bucket(d)][h].  With
+ * B = buckets (half of them if bidirectional), n = |d| if bidirectional, else max(-d, 0), and m = B / 2 rounded down:
+ *     n < m:  bucket = n
+ *     else    bucket = min(B - 1, m + floor(log(n / m) / log(R / m) * (B - m)))     with the floor of the exact value
+ * and B is added for d > 0 if bidirectional.
+ *   table           DEVICE, buckets x heads elements of `dtype`, contiguous
+ *   buckets         2 .. 1024, bidirectional: even, from 4
+ *   max_distance    R: larger than m, up to FEWBIT_MAX_DISTANCE
+ * Errors: INVALID_ARG, TOO_LARGE (heads above 2^16), ALIGNMENT, CUDA.
+ */
+FEWBIT_API fewbit_status fewbit_relative_bias_fwd(const void *table, int buckets, int heads, int max_distance, int bidirectional,
+                                                  fewbit_dtype dtype, float *distance_bias, void *stream);
+
+/* grad_table[b][h] (of `dtype`) = the sum of grad_distance_bias[h] over the distances of bucket b, in a fixed order. */
+FEWBIT_API fewbit_status fewbit_relative_bias_bwd(const float *grad_distance_bias, int buckets, int heads, int max_distance, int bidirectional,
+                                                  fewbit_dtype dtype, void *grad_table, void *stream);
+
+/*
  * Diagnostic: *count (HOST) receives how often a wait inside the attention kernels gave up on the current
  * device since the library was loaded (each wait is limited to two seconds; the results that such a launch could
  * not finish are NaN).  Always 0 unless the device or the program is broken.  Synchronises the device.

@@ -15,9 +15,11 @@ from .binding import (  # noqa: F401
 from .operators import (  # noqa: F401
     fewbit_adamw_create, fewbit_adamw_step, fewbit_add_rms_norm_bwd, fewbit_add_rms_norm_fwd, fewbit_attention_bwd, fewbit_attention_fwd,
     fewbit_attention_timeout_count, fewbit_dropout_bwd, fewbit_dropout_fwd, fewbit_qk_norm_rope_bwd, fewbit_qk_norm_rope_fwd,
+    fewbit_relative_bias_bwd, fewbit_relative_bias_fwd,
 )
 from . import workloads  # noqa: F401
 from .autograd import (  # noqa: F401
     FewBitActivation, fewbit_activation, fewbit_add_rms_norm, fewbit_attention, fewbit_dropout, fewbit_qk_norm_rope,
+    fewbit_relative_bias,
 )
 from .optim import FewBitAdamW  # noqa: F401

@@ -15,6 +15,7 @@ from torch.autograd.function import once_differentiable
 
 from .binding import Table, fewbit_bwd, fewbit_fwd, fewbit_fwd_bias, fewbit_table_create, fewbit_table_create_folded
 from .operators import (
+    fewbit_relative_bias_bwd, fewbit_relative_bias_fwd,
     fewbit_add_rms_norm_bwd, fewbit_add_rms_norm_fwd, fewbit_attention_bwd, fewbit_attention_fwd, fewbit_dropout_bwd, fewbit_dropout_fwd,
     fewbit_qk_norm_rope_bwd, fewbit_qk_norm_rope_fwd,
 )
@@ -110,29 +111,60 @@ class _AttentionFunction(torch.autograd.Function):
     """Keeps q, k, v, the output and one number for each row and head; the probabilities are recomputed."""
 
     @staticmethod
-    def forward(ctx, q, k, v, q_offsets, k_offsets, kw):
+    def forward(ctx, q, k, v, q_offsets, k_offsets, slopes, distance_bias, prefix_lens, q_documents, k_documents, kw):
         q, k, v = _attention_layout(q), _attention_layout(k), _attention_layout(v)
-        out, lse = fewbit_attention_fwd(q, k, v, q_offsets=q_offsets, k_offsets=k_offsets, **kw)
-        ctx.kw = kw
-        ctx.save_for_backward(q, k, v, out, lse, q_offsets, k_offsets)   # (autograd refuses a backward pass when one has been changed)
+        if distance_bias is not None:
+            distance_bias = distance_bias.detach().contiguous()
+        given = {"q_offsets": q_offsets, "k_offsets": k_offsets, "slopes": slopes, "distance_bias": distance_bias, "prefix_lens": prefix_lens,
+                 "q_documents": q_documents, "k_documents": k_documents}
+        out, lse = fewbit_attention_fwd(q, k, v, **given, **kw)
+        ctx.kw, ctx.names = kw, tuple(given)
+        ctx.save_for_backward(q, k, v, out, lse, *given.values())        # (autograd refuses a backward pass when one has been changed)
         return out
 
     @staticmethod
     @once_differentiable
     def backward(ctx, grad_out):
-        q, k, v, out, lse, q_offsets, k_offsets = ctx.saved_tensors
-        return (*fewbit_attention_bwd(_attention_layout(grad_out), q, k, v, out, lse, q_offsets=q_offsets, k_offsets=k_offsets, **ctx.kw),
-                None, None, None)
+        q, k, v, out, lse, *given = ctx.saved_tensors
+        want_bias = ctx.needs_input_grad[6]
+        grads = fewbit_attention_bwd(_attention_layout(grad_out), q, k, v, out, lse, bias_grad=want_bias, **dict(zip(ctx.names, given)), **ctx.kw)
+        return (*grads[:3], None, None, None, grads[3] if want_bias else None, None, None, None, None)
 
 
 def fewbit_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool = False, scale: float | None = None,
                      q_offsets: torch.Tensor | None = None, k_offsets: torch.Tensor | None = None,
-                     max_q_len: int | None = None, max_k_len: int | None = None) -> torch.Tensor:
-    """softmax(scale q k^T) v with gradients; arguments as in ``fewbit_attention_fwd``.  Tensors whose strides the library
-    does not take (a transposed head, an expanded batch) are copied first.  The offsets are kept for the backward pass as they
-    are: a program that reuses their buffer before it gets autograd's error.  Should a wait inside a kernel give up (a broken device:
-    two seconds), the results that it leaves unfinished are NaN, and ``fewbit_attention_timeout_count`` tells."""
-    return _AttentionFunction.apply(q, k, v, q_offsets, k_offsets, {"causal": causal, "scale": scale, "max_q_len": max_q_len, "max_k_len": max_k_len})
+                     max_q_len: int | None = None, max_k_len: int | None = None, cap: float | None = None,
+                     slopes: torch.Tensor | None = None, distance_bias: torch.Tensor | None = None, prefix_lens: torch.Tensor | None = None,
+                     q_documents: torch.Tensor | None = None, k_documents: torch.Tensor | None = None) -> torch.Tensor:
+    """softmax(scale q k^T) v with gradients for q, k, v and ``distance_bias``; arguments as in ``fewbit_attention_fwd``.  Tensors
+    whose strides the library does not take (a transposed head, an expanded batch) are copied first.  Offsets, slopes, prefixes and
+    documents are kept for the backward pass as they are: a program that reuses their buffers before it gets autograd's error.  Should
+    a wait inside a kernel give up (a broken device: two seconds), the results that it leaves unfinished are NaN, and
+    ``fewbit_attention_timeout_count`` tells."""
+    if slopes is not None and slopes.requires_grad and torch.is_grad_enabled():
+        raise ValueError("slopes have no gradient here: pass ones that do not require one (detach them), or a distance_bias")
+    return _AttentionFunction.apply(q, k, v, q_offsets, k_offsets, slopes, distance_bias, prefix_lens, q_documents, k_documents,
+                                    {"causal": causal, "scale": scale, "max_q_len": max_q_len, "max_k_len": max_k_len, "cap": cap})
+
+
+class _RelativeBiasFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, table, max_distance, bidirectional):
+        ctx.bidirectional = bidirectional
+        ctx.like = table.new_empty(()), table.shape                     # type and shape alone are kept
+        return fewbit_relative_bias_fwd(table.contiguous(), max_distance, bidirectional=bidirectional)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, grad):
+        like, shape = ctx.like
+        return fewbit_relative_bias_bwd(grad.contiguous(), like.expand(shape), bidirectional=ctx.bidirectional), None, None
+
+
+def fewbit_relative_bias(table: torch.Tensor, max_distance: int, *, bidirectional: bool = False) -> torch.Tensor:
+    """A learned bias of relative positions, (buckets, heads), as the ``distance_bias`` of ``fewbit_attention``, with the table's
+    gradient; arguments as in ``fewbit_relative_bias_fwd``.  One result can serve all layers that share the table."""
+    return _RelativeBiasFunction.apply(table, max_distance, bidirectional)
 
 
 def _contiguous_heads(t: torch.Tensor) -> torch.Tensor:

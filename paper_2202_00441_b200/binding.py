@@ -103,6 +103,14 @@ def load_library():
     lib.fewbit_attention_workspace_bytes.argtypes = [vp]
     lib.fewbit_attention_timeout_count.argtypes = [ctypes.POINTER(ctypes.c_uint64)]
     lib.fewbit_adamw_step.argtypes = [vp, vp, ci, vp, vp]
+    for name in ("fewbit_attention_scores_fwd", "fewbit_attention_scores_bwd", "fewbit_relative_bias_fwd", "fewbit_relative_bias_bwd"):
+        getattr(lib, name).restype = ci
+    lib.fewbit_attention_scores_fwd.argtypes = [vp] * 8
+    lib.fewbit_attention_scores_bwd.argtypes = [vp] * 13 + [sz, vp]
+    lib.fewbit_attention_scores_workspace_bytes.restype = sz
+    lib.fewbit_attention_scores_workspace_bytes.argtypes = [vp, vp, ci]
+    lib.fewbit_relative_bias_fwd.argtypes = [vp, ci, ci, ci, ci, ci, vp, vp]
+    lib.fewbit_relative_bias_bwd.argtypes = [vp, ci, ci, ci, ci, ci, vp, vp]
     for name in ("fewbit_dropout_fwd", "fewbit_dropout_bwd", "fewbit_add_rms_norm_fwd", "fewbit_add_rms_norm_bwd"):
         getattr(lib, name).restype = ci
     lib.fewbit_dropout_fwd.argtypes = [vp, vp, vp, sz, ci, vp, vp]

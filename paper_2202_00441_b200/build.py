@@ -20,7 +20,10 @@ SOURCES = [("fewbit_kernels.cu", "fewbit_kernels", []), ("fewbit_host.cu", "fewb
            ("fewbit_qknorm.cu", "fewbit_qknorm", []), ("fewbit_attention.cu", "fewbit_attention", []),
            ("fewbit_residual.cu", "fewbit_residual", []),
            ("fewbit_attention_inst.cu", "fewbit_attention_bf16", ["-DFEWBIT_ATTN_F16=0"]),
-           ("fewbit_attention_inst.cu", "fewbit_attention_f16", ["-DFEWBIT_ATTN_F16=1"])]
+           ("fewbit_attention_inst.cu", "fewbit_attention_f16", ["-DFEWBIT_ATTN_F16=1"]),
+           ("fewbit_attention_inst.cu", "fewbit_attention_scores_bf16", ["-DFEWBIT_ATTN_F16=0", "-DFEWBIT_ATTN_SCORES=1"]),
+           ("fewbit_attention_inst.cu", "fewbit_attention_scores_f16", ["-DFEWBIT_ATTN_F16=1", "-DFEWBIT_ATTN_SCORES=1"]),
+           ("fewbit_bias.cu", "fewbit_bias", [])]
 SOURCES += [("fewbit_fwd_inst.cu", f"fewbit_fwd_act{a}", [f"-DFEWBIT_ACT_ID={a}"]) for a in range(9)]
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",

@@ -160,25 +160,72 @@ int choose_split(int64_t sms, int64_t tiles, int64_t longest, bool causal, int m
     return choice;
 }
 
-fewbit_status run(attn::Kernel which, const fewbit_attention_shape *s, Params &p, int64_t tiles, int heads, void *stream) {
+bool shaped(const fewbit_attention_scores *c) { return c != nullptr && (c->cap > 0 || c->slopes || c->distance_bias || c->prefix_lens || c->q_documents); }
+
+fewbit_status check_scores(const fewbit_attention_shape *s, const fewbit_attention_scores *c, const Sizes &z) {
+    if (c == nullptr) return FEWBIT_OK;
+    // (the kernels hold scale / cap and cap * log2(e))
+    if (!(c->cap >= 0) || (c->cap > 0 && !(std::isfinite(s->scale / c->cap) && s->scale / c->cap > 0 && std::isfinite(c->cap * attn::kLog2e)))) return FEWBIT_ERR_INVALID_ARG;
+    if (c->distance_bias != nullptr && (c->max_distance < 1 || c->max_distance > FEWBIT_MAX_DISTANCE)) return FEWBIT_ERR_INVALID_ARG;
+    if ((c->prefix_lens != nullptr && !s->causal) || (c->q_documents == nullptr) != (c->k_documents == nullptr)) return FEWBIT_ERR_INVALID_ARG;
+    uintptr_t all = 0;
+    for (const void *p : {static_cast<const void *>(c->slopes), static_cast<const void *>(c->distance_bias), static_cast<const void *>(c->prefix_lens),
+                          static_cast<const void *>(c->q_documents), static_cast<const void *>(c->k_documents)})
+        all |= reinterpret_cast<uintptr_t>(p);
+    if (all & 3) return FEWBIT_ERR_ALIGNMENT;
+    if (shaped(c) && (z.q_rows > 1 << 30 || z.k_rows > 1 << 30)) return FEWBIT_ERR_TOO_LARGE;   // distances are counted in 31 bits
+    if (c->distance_bias != nullptr && s->heads > 65535) return FEWBIT_ERR_TOO_LARGE;
+    return FEWBIT_OK;
+}
+
+void fill_scores(const fewbit_attention_shape *s, const fewbit_attention_scores *c, Params *p) {
+    if (!shaped(c)) return;
+    attn::Scores &to = p->scores;
+    to.capped = c->cap > 0;
+    to.cap_in = to.capped ? s->scale / c->cap : 0.0f;
+    to.cap_out = c->cap * attn::kLog2e;
+    to.slopes = c->slopes;
+    to.bias = c->distance_bias;
+    to.reach = c->distance_bias != nullptr ? c->max_distance : 0;
+    to.prefix = c->prefix_lens;
+    to.q_docs = c->q_documents;
+    to.k_docs = c->k_documents;
+}
+
+// What the bias's gradient takes of the workspace, behind the rows' statistics.
+struct BiasSpace {
+    size_t near, far, written;        // bytes
+    int64_t tiles;                    // key tiles of a sequence
+    int near_tiles;
+};
+BiasSpace bias_space(const fewbit_attention_shape *s, int max_distance) {
+    BiasSpace b;
+    const int64_t row_tiles = (s->q_len + attn::kTile - 1) / attn::kTile, most = (2 * static_cast<int64_t>(max_distance) + 254 + 127) / 128;
+    b.tiles = (s->k_len + attn::kTile - 1) / attn::kTile;
+    if (b.tiles == 0) b.tiles = 1;
+    b.near_tiles = static_cast<int>(row_tiles < most ? row_tiles : most);
+    const size_t places = static_cast<size_t>(s->batch) * s->heads * b.tiles;
+    b.near = places * b.near_tiles * attn::kNearFloats * 4;
+    b.far = places * attn::kFarFloats * 4;
+    b.written = places * sizeof(int4);
+    return b;
+}
+
+fewbit_status run(attn::Kernel which, const fewbit_attention_shape *s, bool scores, Params &p, int64_t tiles, int heads, void *stream) {
     p.tiles = static_cast<int>(p.q_offsets != nullptr && tiles == 0 ? 1 : tiles);   // packed rows of no sequence are there without any tile
     const unsigned grid = static_cast<unsigned>(static_cast<int64_t>(p.tiles) * heads * (s->batch + (p.q_offsets != nullptr)));   // one more for rows of no sequence
     if (grid == 0) return FEWBIT_OK;
-    const cudaError_t err = (s->dtype == FEWBIT_F16 ? attn::launch_f16 : attn::launch_bf16)(which, s->head_dim > 64, p, grid, static_cast<cudaStream_t>(stream));
+    const auto launch = scores ? (s->dtype == FEWBIT_F16 ? attn::launch_scores_f16 : attn::launch_scores_bf16) : s->dtype == FEWBIT_F16 ? attn::launch_f16 : attn::launch_bf16;
+    const cudaError_t err = launch(which, s->head_dim > 64, p, grid, static_cast<cudaStream_t>(stream));
     if (err == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
     return cuda_status(err);
 }
 
-}  // namespace
-}  // namespace fewbit
-
-extern "C" {
-
-fewbit_status fewbit_attention_fwd(const fewbit_attention_shape *s, const fewbit_heads *q, const fewbit_heads *k, const fewbit_heads *v,
-                                   const fewbit_heads *out, float *lse, void *stream) {
-    using namespace fewbit;
+fewbit_status forward(const fewbit_attention_shape *s, const fewbit_attention_scores *scores, const fewbit_heads *q, const fewbit_heads *k, const fewbit_heads *v,
+                      const fewbit_heads *out, float *lse, void *stream) {
     Sizes z;
     if (const fewbit_status st = check_shape(s, &z); st != FEWBIT_OK) return st;
+    if (const fewbit_status st = check_scores(s, scores, z); st != FEWBIT_OK) return st;
     if (z.batch == 0 || s->heads == 0 || z.q_rows == 0) return FEWBIT_OK;
     for (const fewbit_heads *t : {q, out})
         if (const fewbit_status st = check_tensor(t, z.q_rows, s->heads, z.batch); st != FEWBIT_OK) return st;
@@ -194,34 +241,42 @@ fewbit_status fewbit_attention_fwd(const fewbit_attention_shape *s, const fewbit
     if (st != FEWBIT_OK) return st;
     p.out = rows_of(out);
     p.lse = lse;
+    fill_scores(s, scores, &p);
     const int64_t row_tiles = (s->q_len + 2 * attn::kTile - 1) / (2 * attn::kTile), key_tiles = (s->k_len + attn::kTile - 1) / attn::kTile;
     p.split = choose_split(p.sms, row_tiles * s->heads * s->batch, key_tiles, p.causal, s->head_dim > 64 ? 8 : 4, kForwardEnds);
-    return run(attn::Kernel::forward, s, p, row_tiles, s->heads, stream);
+    return run(attn::Kernel::forward, s, shaped(scores), p, row_tiles, s->heads, stream);
 }
 
-size_t fewbit_attention_workspace_bytes(const fewbit_attention_shape *s) {
-    using namespace fewbit;
-    Sizes z;
-    if (check_shape(s, &z) != FEWBIT_OK) return 0;
+size_t stat_bytes(const fewbit_attention_shape *s, const Sizes &z) {
     const size_t tiles = z.packed ? static_cast<size_t>(z.q_rows / attn::kTile + s->batch + 1) : static_cast<size_t>((s->q_len + attn::kTile - 1) / attn::kTile) * s->batch;
     return tiles * s->heads * attn::kStatBytes;
 }
 
-fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *s, const fewbit_heads *grad_out, const fewbit_heads *q, const fewbit_heads *k,
-                                   const fewbit_heads *v, const fewbit_heads *out, const float *lse, const fewbit_heads *grad_q,
-                                   const fewbit_heads *grad_k, const fewbit_heads *grad_v, void *workspace, size_t workspace_bytes, void *stream) {
-    using namespace fewbit;
+fewbit_status backward(const fewbit_attention_shape *s, const fewbit_attention_scores *scores, const fewbit_heads *grad_out, const fewbit_heads *q,
+                       const fewbit_heads *k, const fewbit_heads *v, const fewbit_heads *out, const float *lse, const fewbit_heads *grad_q,
+                       const fewbit_heads *grad_k, const fewbit_heads *grad_v, float *grad_bias, void *workspace, size_t workspace_bytes, void *stream) {
     Sizes z;
     if (const fewbit_status st = check_shape(s, &z); st != FEWBIT_OK) return st;
+    if (const fewbit_status st = check_scores(s, scores, z); st != FEWBIT_OK) return st;
+    if (grad_bias != nullptr && (scores == nullptr || scores->distance_bias == nullptr)) return FEWBIT_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(grad_bias) & 3) return FEWBIT_ERR_ALIGNMENT;
+    if (grad_bias != nullptr && (z.batch == 0 || s->batch == 0 || s->heads == 0 || z.k_rows == 0)) {   // the sums of nothing
+        const cudaError_t err = cudaMemsetAsync(grad_bias, 0, sizeof(float) * s->heads * (2 * scores->max_distance + 1), static_cast<cudaStream_t>(stream));
+        if (err != cudaSuccess) return cuda_status(err);
+        grad_bias = nullptr;
+    }
     if (z.batch == 0 || s->heads == 0 || (z.q_rows == 0 && z.k_rows == 0)) return FEWBIT_OK;
     for (const fewbit_heads *t : {grad_out, q, out, grad_q})
         if (const fewbit_status st = check_tensor(t, z.q_rows, s->heads, z.batch); st != FEWBIT_OK) return st;
     for (const fewbit_heads *t : {k, v, grad_k, grad_v})
         if (const fewbit_status st = check_tensor(t, z.k_rows, s->kv_heads, z.batch); st != FEWBIT_OK) return st;
     const bool some = z.q_rows > 0;
-    if (some && (lse == nullptr || workspace == nullptr)) return FEWBIT_ERR_INVALID_ARG;
+    if ((some && lse == nullptr) || ((some || grad_bias != nullptr) && workspace == nullptr)) return FEWBIT_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(lse) & 3) || (reinterpret_cast<uintptr_t>(workspace) & 15)) return FEWBIT_ERR_ALIGNMENT;
-    if (workspace_bytes < fewbit_attention_workspace_bytes(s)) return FEWBIT_ERR_ALLOC;
+    const size_t stats = stat_bytes(s, z);
+    BiasSpace b = {};
+    if (grad_bias != nullptr) b = bias_space(s, scores->max_distance);
+    if (workspace_bytes < stats + b.near + b.far + b.written) return FEWBIT_ERR_ALLOC;
     Params p = {};
     fewbit_status st = fill(s, z, &p);
     if (st == FEWBIT_OK && some) st = encode(&p.q, q, s, z.q_rows, s->heads, z.batch);
@@ -238,12 +293,62 @@ fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *s, const fewbit
     p.lse = const_cast<float *>(lse);
     p.stat = static_cast<float *>(workspace);
     p.after_dq = some;
+    fill_scores(s, scores, &p);
+    if (grad_bias != nullptr) {
+        uint8_t *at = static_cast<uint8_t *>(workspace) + stats;
+        p.scores.written = reinterpret_cast<int4 *>(at);
+        p.scores.near = reinterpret_cast<float *>(at + b.written);
+        p.scores.far = reinterpret_cast<float *>(at + b.written + b.near);
+        p.scores.near_tiles = b.near_tiles;
+    }
     const int64_t row_tiles = (s->q_len + attn::kTile - 1) / attn::kTile, key_tiles = (s->k_len + attn::kTile - 1) / attn::kTile;
     p.split = choose_split(p.sms, row_tiles * s->heads * s->batch, key_tiles, p.causal, s->head_dim > 64 ? 8 : 4, kDqEnds);
-    if (some) st = run(attn::Kernel::dq, s, p, row_tiles, s->heads, stream);
+    if (some) st = run(attn::Kernel::dq, s, shaped(scores), p, row_tiles, s->heads, stream);
     if (st != FEWBIT_OK || z.k_rows == 0) return st;
     p.split = choose_split(p.sms, key_tiles * s->kv_heads * s->batch, row_tiles * p.group, p.causal, 4, kDkvEnds);
-    return run(attn::Kernel::dkv, s, p, key_tiles, s->kv_heads, stream);
+    st = run(grad_bias != nullptr ? attn::Kernel::dkv_bias : attn::Kernel::dkv, s, shaped(scores), p, key_tiles, s->kv_heads, stream);
+    if (st != FEWBIT_OK || grad_bias == nullptr) return st;
+    const cudaError_t err = attn::launch_bias_gradient(p, grad_bias, static_cast<cudaStream_t>(stream));
+    if (err == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
+    return cuda_status(err);
+}
+
+}  // namespace
+}  // namespace fewbit
+
+extern "C" {
+
+fewbit_status fewbit_attention_fwd(const fewbit_attention_shape *s, const fewbit_heads *q, const fewbit_heads *k, const fewbit_heads *v,
+                                   const fewbit_heads *out, float *lse, void *stream) {
+    return fewbit::forward(s, nullptr, q, k, v, out, lse, stream);
+}
+
+fewbit_status fewbit_attention_scores_fwd(const fewbit_attention_shape *s, const fewbit_attention_scores *scores, const fewbit_heads *q, const fewbit_heads *k,
+                                          const fewbit_heads *v, const fewbit_heads *out, float *lse, void *stream) {
+    return fewbit::forward(s, scores, q, k, v, out, lse, stream);
+}
+
+size_t fewbit_attention_workspace_bytes(const fewbit_attention_shape *s) { return fewbit_attention_scores_workspace_bytes(s, nullptr, 0); }
+
+size_t fewbit_attention_scores_workspace_bytes(const fewbit_attention_shape *s, const fewbit_attention_scores *scores, int bias_gradient) {
+    using namespace fewbit;
+    Sizes z;
+    if (check_shape(s, &z) != FEWBIT_OK || check_scores(s, scores, z) != FEWBIT_OK) return 0;
+    BiasSpace b = {};
+    if (bias_gradient && scores != nullptr && scores->distance_bias != nullptr) b = bias_space(s, scores->max_distance);
+    return stat_bytes(s, z) + b.near + b.far + b.written;
+}
+
+fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *s, const fewbit_heads *grad_out, const fewbit_heads *q, const fewbit_heads *k,
+                                   const fewbit_heads *v, const fewbit_heads *out, const float *lse, const fewbit_heads *grad_q,
+                                   const fewbit_heads *grad_k, const fewbit_heads *grad_v, void *workspace, size_t workspace_bytes, void *stream) {
+    return fewbit::backward(s, nullptr, grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, nullptr, workspace, workspace_bytes, stream);
+}
+
+fewbit_status fewbit_attention_scores_bwd(const fewbit_attention_shape *s, const fewbit_attention_scores *scores, const fewbit_heads *grad_out, const fewbit_heads *q,
+                                          const fewbit_heads *k, const fewbit_heads *v, const fewbit_heads *out, const float *lse, const fewbit_heads *grad_q,
+                                          const fewbit_heads *grad_k, const fewbit_heads *grad_v, float *grad_bias, void *workspace, size_t workspace_bytes, void *stream) {
+    return fewbit::backward(s, scores, grad_out, q, k, v, out, lse, grad_q, grad_k, grad_v, grad_bias, workspace, workspace_bytes, stream);
 }
 
 fewbit_status fewbit_attention_timeout_count(uint64_t *count) {

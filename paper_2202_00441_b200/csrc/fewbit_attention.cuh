@@ -27,6 +27,7 @@
 #include <type_traits>
 
 #include "fewbit_device.cuh"
+#include "fewbit_scores.cuh"
 #include "fewbit_tensor_core.cuh"
 
 namespace fewbit {
@@ -41,7 +42,7 @@ constexpr int kWorkThreads = 512;
 // Registers of the element-wise and the issuing threads.  96 a thread at launch: 512 x 104 + 128 x 64 = 512 x 112 + 128 x 32 =
 // 61440 = 640 x 96
 constexpr int kFwdWork = 112, kFwdIssue = 32, kDqWork = 104, kDqIssue = 64, kDkvWork = 112, kDkvIssue = 32;
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr uint32_t kNan = 0x7fc00000u;
 constexpr int kStatBytes = 2 * kTile * 4;   // a row tile's -lse * log2(e) and -delta
 
@@ -64,7 +65,9 @@ struct Params {
     bool causal;
     bool after_dq;                    // dK, dV: launched right behind the dQ kernel, whose start is all that its CTAs have waited for
     float scale, scale_log2;          // scale * log2(e)
+    Scores scores;                    // (kernels of MODE 1 and 2)
 };
+// MODE of the kernels: 0 plain scores, 1 with caps, biases and masks (fewbit_scores.cuh), 2 (dK and dV) with the bias's gradient too
 
 // What one CTA works on.
 struct Work {
@@ -104,10 +107,31 @@ __device__ __forceinline__ Work find_work(const Params &p, int block, int heads,
 }
 
 // Key tiles that rows [first, last] of a sequence see any key of.
-__device__ __forceinline__ int key_tiles(const Params &p, const Work &w, int last) {
+__device__ __forceinline__ int key_tiles(const Params &p, const Work &w, int last, int prefix = 0) {
     int keys = w.k_len;
-    if (p.causal) keys = min(keys, max(0, last + 1 + w.k_len - w.q_len));
+    if (p.causal) keys = min(keys, max(prefix, last + 1 + w.k_len - w.q_len));
     return (keys + kTile - 1) / kTile;
+}
+// The row sees keys [0, seen), but for its document's.
+__device__ __forceinline__ int seen_by(const Params &p, const Work &w, int row, int prefix = 0) {
+    return p.causal ? min(w.k_len, max(prefix, row + 1 + w.k_len - w.q_len)) : w.k_len;
+}
+
+// The plain scores' Mods do nothing.
+template <int MODE>
+__device__ __forceinline__ Mods find_mods(const Params &p, const Work &w, int head) {
+    Mods m = {};
+    if constexpr (MODE > 0) {
+        const Scores &sc = p.scores;
+        if (sc.prefix != nullptr) m.prefix = uniform(min(max(sc.prefix[w.batch], 0), w.k_len));
+        if (sc.q_docs != nullptr) {
+            m.q_docs = sc.q_docs + (w.packed ? w.q_first : static_cast<long long>(w.batch) * p.q_len);
+            m.k_docs = sc.k_docs + (w.packed ? w.k_first : static_cast<long long>(w.batch) * p.k_len);
+        }
+        if (sc.bias != nullptr) m.bias = sc.bias + static_cast<long long>(head) * (2 * sc.reach + 1) + sc.reach;
+        if (sc.slopes != nullptr) m.slope = -uniform(sc.slopes[head]) * kLog2e;
+    }
+    return m;
 }
 
 // How many of n tiles fall to CTA `rank` of `split` that take them in turn.
@@ -119,6 +143,7 @@ struct Sync {
     uint32_t tmem;
     int stop;
 };
+constexpr int kDocPlace = 16;          // bytes behind everything else, for shared_tiles
 
 // A tile of `rows` valid rows: the rest may hold another sequence's values, which a zero probability does not
 // silence when they are not finite.  One warp clears them.
@@ -230,7 +255,7 @@ __device__ __forceinline__ void end_cta(uint32_t tmem) {
 // ready (2), all of it (2), O done (2), drained.
 enum { fQ = 0, fKFull = 2, fKEmpty = 4, fVFull = 6, fVEmpty = 8, fS = 10, fP = 12, fPEnd = 14, fO = 16, fDrain = 18, fBars = 19 };
 
-template <int DIM> constexpr int fwd_smem() { return 6 * (DIM / 64) * static_cast<int>(kHalfTile) + 1024 + static_cast<int>(sizeof(Sync)) + 8 * kTile * 4; }
+template <int DIM> constexpr int fwd_smem() { return 6 * (DIM / 64) * static_cast<int>(kHalfTile) + 1024 + static_cast<int>(sizeof(Sync)) + 8 * kTile * 4 + kDocPlace; }
 
 // Barriers of two warps.
 __device__ __forceinline__ void pair_barrier(int id) { asm volatile("bar.sync %0, 64;" :: "r"(id) : "memory"); }
@@ -256,7 +281,7 @@ __device__ __forceinline__ void fwd_probabilities(const uint32_t *s, float scale
     tmem_st16(at, r);
 }
 
-template <typename T, int DIM>
+template <typename T, int DIM, int MODE>
 __global__ void __launch_bounds__(kThreadsAttn, 1)
 attention_fwd_kernel(const __grid_constant__ Params p) {
     constexpr int HALVES = DIM / 64;
@@ -279,9 +304,21 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
     const int kv_head = w.head / p.group;
     // key tiles of each row tile (0 also for a row tile past the end)
     // that fall to this CTA: number rank, rank + split, ...
-    const int n0 = uniform(share_of(key_tiles(p, w, min(q0 + kTile, w.q_len) - 1), rank, p.split));
-    const int n1 = uniform(share_of(q0 + kTile < w.q_len ? key_tiles(p, w, min(q0 + 2 * kTile, w.q_len) - 1) : 0, rank, p.split));
-    auto key_tile = [&](int j) { return rank + j * p.split; };
+    const Mods mods = find_mods<MODE>(p, w, w.head);
+    int all0 = key_tiles(p, w, min(q0 + kTile, w.q_len) - 1, mods.prefix);
+    int all1 = q0 + kTile < w.q_len ? key_tiles(p, w, min(q0 + 2 * kTile, w.q_len) - 1, mods.prefix) : 0;
+    int skipped = 0;                                                  // key tiles in front, which neither row tile sees
+    if constexpr (MODE > 0) {
+        if (mods.q_docs != nullptr) {
+            const int2 tiles = shared_tiles(mods.q_docs, q0, min(q0 + 2 * kTile, w.q_len), mods.k_docs, w.k_len, max(all0, all1), reinterpret_cast<int *>(joined + 4 * kTile));
+            skipped = tiles.x;
+            all0 = max(0, min(all0, tiles.y) - skipped);
+            all1 = max(0, min(all1, tiles.y) - skipped);
+        }
+    }
+    const int n0 = uniform(share_of(all0, rank, p.split));
+    const int n1 = uniform(share_of(all1, rank, p.split));
+    auto key_tile = [&](int j) { return skipped + rank + j * p.split; };
     const int n = max(n0, n1);
 
     constexpr uint32_t counts[fBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 8, 8, 8, 8, 1, 1, 1};
@@ -383,25 +420,55 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
         const uint32_t s_at = tm_s + t * kTile + 64 * half + my_lane, o_at = tm_o + t * kTile + half * (DIM / 2) + my_lane;
         const int pair = 1 + 4 * t + (warp & 3);                      // barrier of the two warps that share their rows
         float *mine = exchange + (2 * t + half) * kTile + r, *other = exchange + (2 * t + 1 - half) * kTile + r;
-        // the row sees keys [0, seen)
-        const int seen = p.causal ? min(w.k_len, i + 1 + w.k_len - w.q_len) : w.k_len;
-        const int tile_seen = p.causal ? min(w.k_len, q0 + t * kTile + 1 + w.k_len - w.q_len) : w.k_len;   // by its first row
+        const int seen = seen_by(p, w, i, mods.prefix), tile_seen = seen_by(p, w, q0 + t * kTile, mods.prefix);   // by its first row
+        const float unit = MODE > 0 ? 1.0f : p.scale_log2, natural = MODE > 0 ? kLn2 : p.scale;   // of the scores, in units of ln 2 and by themselves
+        int document = 0;
+        if constexpr (MODE > 0) {
+            if (mods.q_docs != nullptr && i < w.q_len) document = __ldg(mods.q_docs + i);
+        }
         float top = -INFINITY, sum = 0.0f;                            // of the raw products; the sum of this thread's columns
         bool ok = true;
         for (int j = 0; j < nt; ++j) {
+            int key_document[2] = {0, 0};                             // of this lane's key of each 32
+            if constexpr (MODE > 0) {
+                if (mods.k_docs != nullptr) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) key_document[c] = __ldg(mods.k_docs + min(key_tile(j) * kTile + 64 * half + 32 * c + lane, w.k_len - 1));
+                }
+            }
             ok = wait(fS + t, j & 1);                                 // (a wait given up ends the loop below, for all threads of the tile)
             fence_after();
-            const bool edge = (key_tile(j) + 1) * kTile > tile_seen;
+            bool edge = (key_tile(j) + 1) * kTile > tile_seen;
             const int limit = seen - key_tile(j) * kTile - 64 * half;
             // Scores are read twice, 32 columns at a time, for the maximum and for the probabilities: reading them costs less
             // than holding 64 of them in registers.
             uint32_t s[32];
+            bool exact = MODE == 0 && edge;                           // some may be -inf, which the polynomial does not make 0
             auto read = [&](int c) {
                 tmem_ld32(s_at + 32 * c, s);
                 wait_ld(s);
-                if (edge) {
+                if (MODE == 0 && edge) {
 #pragma unroll
                     for (int e = 0; e < 32; ++e) s[e] = 32 * c + e < limit ? s[e] : 0xff800000u;
+                }
+            };
+            // MODE 1: the scores take the products' place, with what is hidden already out, so that they are shaped once
+            auto shape = [&](int c) {
+                if constexpr (MODE > 0) {
+                    uint32_t none[16];
+                    const bool finite = shape_scores<false>(p.scores, mods, p.scale_log2, key_tile(j) * kTile + 64 * half + 32 * c - i - (w.k_len - w.q_len), s, none);
+                    uint32_t word = edge ? low_bits(limit - 32 * c) : 0xffffffffu;
+                    if (mods.k_docs != nullptr) word &= same_document(document, key_document[c]);
+                    const bool hides = __any_sync(0xffffffffu, word != 0xffffffffu);
+                    if (hides) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) s[e] = word >> e & 1 ? s[e] : 0xff800000u;
+                    }
+                    exact = exact || hides || !finite;
+                    if (c == 0) {
+                        tmem_st32(s_at, s);
+                        wait_st();
+                    }
                 }
             };
             float best[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
@@ -411,15 +478,17 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
                     best[(e >> 1) & 3] = max3_nan(best[(e >> 1) & 3], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
             };
             read(0);
+            shape(0);
             maximum();
             read(1);
+            shape(1);
             maximum();
             const float high = max3_nan(max3_nan(best[0], best[1], best[2]), best[3], best[3]);
             // The sums' reference moves only when a product passes it by 2^8: until then probabilities up to 2^8
             // are held, which cost no precision, and O needs no rescaling.  The row's two threads move it together: whether
             // any row of their two warps moves is one barrier, and only then they exchange their maxima.  A score that is NaN
             // becomes the reference, and with it the whole row.
-            auto moves = [&](float to) { return to != top && !((to - top) * p.scale_log2 <= 8.0f); };
+            auto moves = [&](float to) { return to != top && !((to - top) * unit <= 8.0f); };
             const bool above = moves(high);
             if (pair_any(pair, above || !ok)) {
                 if (pair_any(pair, !ok)) {
@@ -431,7 +500,7 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
                 const float row_high = max3_nan(high, *other, high);
                 const bool move = moves(row_high);
                 const float next = move ? row_high : top;
-                const float factor = move ? exp2_fast((top - next) * p.scale_log2) : 1.0f;
+                const float factor = move ? exp2_fast((top - next) * unit) : 1.0f;
                 top = next;
                 sum *= factor;
                 if (j > 0) {
@@ -452,13 +521,13 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
                     }
                 }
             }
-            const float shift = top == -INFINITY ? 0.0f : -top * p.scale_log2;
+            const float shift = top == -INFINITY ? 0.0f : -top * unit;
             float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int c = 1; c >= 0; --c) {                            // (columns 32 to 63 are still there)
                 if (c == 0) read(0);
-                if (edge) fwd_probabilities<T, false>(s, p.scale_log2, shift, part, s_at + 32 * c);
-                else fwd_probabilities<T, true>(s, p.scale_log2, shift, part, s_at + 32 * c);
+                if (exact) fwd_probabilities<T, false>(s, unit, shift, part, s_at + 32 * c);
+                else fwd_probabilities<T, true>(s, unit, shift, part, s_at + 32 * c);
                 wait_st();
                 fence_before();
                 __syncwarp();
@@ -487,7 +556,7 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
             } else if (live && half == 0) {
                 zero_columns<T>(row, p.dim);
             }
-            if (live && half == 0) p.lse[stat_of(p, w, w.head, i)] = sum == 0.0f ? -INFINITY : top * p.scale + logf(sum);
+            if (live && half == 0) p.lse[stat_of(p, w, w.head, i)] = sum == 0.0f ? -INFINITY : top * natural + logf(sum);
         } else {
             // Every CTA lays its O, reference and sum of each row out in shared memory, [row tile][column][row]; a share of the
             // columns is brought to the largest reference, added up and divided by each.
@@ -511,14 +580,14 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
             cluster_sync();
             float high = -INFINITY, total = 0.0f;
             for (int k = 0; k < p.split; ++k) high = fmaxf(high, load_peer(mine_stat, k));
-            const float reference = high == -INFINITY ? 0.0f : high * p.scale_log2;
-            for (int k = 0; k < p.split; ++k) total += exp2_fast(load_peer(mine_stat, k) * p.scale_log2 - reference) * load_peer(mine_stat + kTile * 4, k);
+            const float reference = high == -INFINITY ? 0.0f : high * unit;
+            for (int k = 0; k < p.split; ++k) total += exp2_fast(load_peer(mine_stat, k) * unit - reference) * load_peer(mine_stat + kTile * 4, k);
             const float factor = total > 0.0f || total != total ? 1.0f / total : 0.0f;
             const int share = DIM / p.split;                          // a multiple of 16
             for (int col = rank * share + half * (share / 2); col < rank * share + (half + 1) * (share / 2); col += 8) {
                 float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
                 for (int k = 0; k < p.split; ++k) {
-                    const float weight = exp2_fast(load_peer(mine_stat, k) * p.scale_log2 - reference);
+                    const float weight = exp2_fast(load_peer(mine_stat, k) * unit - reference);
                     float x[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) x[e] = load_peer(mine_o + (col + e) * (kTile * 4), k);
@@ -530,7 +599,7 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
                 for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(v[e]);
                 if (live) store_columns<T, 8>(row, col, p.dim, o, factor);
             }
-            if (live && half == 0 && rank == 0) p.lse[stat_of(p, w, w.head, i)] = total == 0.0f ? -INFINITY : high * p.scale + logf(total);
+            if (live && half == 0 && rank == 0) p.lse[stat_of(p, w, w.head, i)] = total == 0.0f ? -INFINITY : high * natural + logf(total);
             cluster_sync();                                           // nobody's shared memory goes before it has been read
         }
     }
@@ -549,9 +618,9 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
 // dP full, dS ready, dQ done.
 enum { qQ = 0, qKFull = 1, qKEmpty = 4, qVFull = 7, qVEmpty = 9, qS = 11, qDp = 13, qDs = 14, qDone = 15, qBars = 16 };
 
-template <int DIM> constexpr int dq_smem() { return 7 * (DIM / 64) * static_cast<int>(kHalfTile) + static_cast<int>(sizeof(Sync)) + 5 * kTile * 4; }
+template <int DIM> constexpr int dq_smem() { return 7 * (DIM / 64) * static_cast<int>(kHalfTile) + static_cast<int>(sizeof(Sync)) + 5 * kTile * 4 + kDocPlace; }
 
-template <typename T, int DIM>
+template <typename T, int DIM, int MODE>
 __global__ void __launch_bounds__(kThreadsAttn, 1)
 attention_dq_kernel(const __grid_constant__ Params p) {
     constexpr int HALVES = DIM / 64;
@@ -574,9 +643,18 @@ attention_dq_kernel(const __grid_constant__ Params p) {
     if (q0 >= w.q_len) return;
     const int kv_head = w.head / p.group;
     // key tiles that the rows see, and how many of them fall to this CTA: number rank, rank + split, ...
-    const int n_all = uniform(key_tiles(p, w, min(q0 + kTile, w.q_len) - 1));
+    const Mods mods = find_mods<MODE>(p, w, w.head);
+    int all = key_tiles(p, w, min(q0 + kTile, w.q_len) - 1, mods.prefix), skipped = 0;
+    if constexpr (MODE > 0) {
+        if (mods.q_docs != nullptr) {
+            const int2 tiles = shared_tiles(mods.q_docs, q0, min(q0 + kTile, w.q_len), mods.k_docs, w.k_len, all, reinterpret_cast<int *>(row_sum + 4 * kTile));
+            skipped = tiles.x;
+            all = max(0, tiles.y - skipped);
+        }
+    }
+    const int n_all = uniform(all);
     const int n = share_of(n_all, rank, p.split);
-    auto key_tile = [&](int j) { return rank + j * p.split; };
+    auto key_tile = [&](int j) { return skipped + rank + j * p.split; };
 
     // The outputs that delta needs, read while the CTA sets itself up: DIM / 8 lanes a row, 8 rows for each warp.  (From here on
     // the L2's bandwidth is the tiles' that are on their way.)
@@ -708,10 +786,18 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             asm volatile("bar.sync 1, %0;" :: "n"(kWorkThreads) : "memory");
             return (row_sum[r] + row_sum[kTile + r]) + (row_sum[2 * kTile + r] + row_sum[3 * kTile + r]);
         };
-        const int seen = p.causal ? min(w.k_len, i + 1 + w.k_len - w.q_len) : w.k_len;
-        const int tile_seen = p.causal ? min(w.k_len, q0 + 1 + w.k_len - w.q_len) : w.k_len;
+        const int seen = seen_by(p, w, i, mods.prefix), tile_seen = seen_by(p, w, q0, mods.prefix);
+        const float unit = MODE > 0 ? 1.0f : p.scale_log2;            // of the scores, in units of ln 2
+        int document = 0, visible = 0;                                // with documents: how many keys the row sees here
+        if constexpr (MODE > 0) {
+            if (mods.q_docs != nullptr && live) document = __ldg(mods.q_docs + i);
+        }
         for (int j = 0; ok && j < n; ++j) {
             const uint32_t s_at = tm_s + (j & 1) * kTile + 32 * part + my_lane;
+            int key_document = 0;
+            if constexpr (MODE > 0) {
+                if (mods.k_docs != nullptr) key_document = __ldg(mods.k_docs + min(key_tile(j) * kTile + 32 * part + lane, w.k_len - 1));
+            }
             ok = wait(qS + (j & 1), (j >> 1) & 1);
             if (!ok) {
                 if (single) over_parts(0.0f);                         // the others wait there
@@ -719,19 +805,37 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             }
             fence_after();
             uint32_t s[32], d[32], out[16];
+            uint32_t bent[16];                                        // MODE 1, capped: 1 - t^2
             float prob[32];
             tmem_ld32(s_at, s);
             wait_ld(s);
-            const bool edge = (key_tile(j) + 1) * kTile > tile_seen;
-            if (edge) {
+            bool edge = (key_tile(j) + 1) * kTile > tile_seen;
+            const int limit = seen - key_tile(j) * kTile - 32 * part;           // places from here on the row does not see, whatever they hold
+            uint32_t word = 0xffffffffu;
+            bool finite = true;
+            auto sees = [&](int c) { return MODE > 0 ? (word >> c & 1) != 0 : c < limit; };
+            if constexpr (MODE > 0) {
+                finite = shape_scores<true>(p.scores, mods, p.scale_log2, key_tile(j) * kTile + 32 * part - i - (w.k_len - w.q_len), s, bent);
+                if (edge) word = low_bits(limit);
+                if (mods.k_docs != nullptr) {
+                    word &= same_document(document, key_document);
+                    visible += __popc(word);
+                }
+                edge = __any_sync(0xffffffffu, word != 0xffffffffu);
+            }
+            if (edge || !finite) {
 #pragma unroll
                 for (int c = 0; c < 32; c += 2)
-                    exp2_scaled<false>(prob[c], prob[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), p.scale_log2, minus_lse, minus_lse);
+                    exp2_scaled<false>(prob[c], prob[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), unit, minus_lse, minus_lse);
+                if constexpr (MODE > 0) {                             // (what a document hides may be larger than the row's sum)
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) prob[c] = sees(c) ? prob[c] : 0.0f;
+                }
             } else {
 #pragma unroll
                 for (int c = 0; c < 32; c += 2) {
-                    if (c % 8 == 6) exp2_scaled<true>(prob[c], prob[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), p.scale_log2, minus_lse, minus_lse);
-                    else exp2_scaled<false>(prob[c], prob[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), p.scale_log2, minus_lse, minus_lse);
+                    if (c % 8 == 6) exp2_scaled<true>(prob[c], prob[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), unit, minus_lse, minus_lse);
+                    else exp2_scaled<false>(prob[c], prob[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), unit, minus_lse, minus_lse);
                 }
             }
             ok = wait(qDp, j & 1);
@@ -743,17 +847,16 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             tmem_ld32(tm_dp + 32 * part + my_lane, d);
             wait_ld(d);
             float ds[32];
-            const int limit = seen - key_tile(j) * kTile - 32 * part;           // places from here on the row does not see, whatever they hold
             if (single) {
                 float sum = 0.0f;
 #pragma unroll
                 for (int c = 0; c < 32; ++c) {
-                    ds[c] = c < limit ? prob[c] * __uint_as_float(d[c]) : 0.0f;
+                    ds[c] = sees(c) ? prob[c] * __uint_as_float(d[c]) : 0.0f;
                     sum += ds[c];
                 }
                 minus_delta = -over_parts(sum);
 #pragma unroll
-                for (int c = 0; c < 32; ++c) ds[c] = c < limit ? fmaf(prob[c], minus_delta, ds[c]) : 0.0f;
+                for (int c = 0; c < 32; ++c) ds[c] = sees(c) ? fmaf(prob[c], minus_delta, ds[c]) : 0.0f;
             } else {
 #pragma unroll
                 for (int c = 0; c < 32; c += 2) {
@@ -762,12 +865,21 @@ attention_dq_kernel(const __grid_constant__ Params p) {
                 }
                 if (edge) {
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) ds[c] = c < limit ? ds[c] : 0.0f;
+                    for (int c = 0; c < 32; ++c) ds[c] = sees(c) ? ds[c] : 0.0f;
                 }
                 float sum[2] = {0.0f, 0.0f};
 #pragma unroll
                 for (int c = 0; c < 32; c += 2) add2(sum[0], sum[1], sum[0], sum[1], ds[c], ds[c + 1]);
                 drift += sum[0] + sum[1];
+            }
+            if constexpr (MODE > 0) {
+                if (p.scores.capped) {
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) {
+                        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&bent[c]));
+                        mul2(ds[2 * c], ds[2 * c + 1], ds[2 * c], ds[2 * c + 1], f.x, f.y);
+                    }
+                }
             }
 #pragma unroll
             for (int c = 0; c < 16; ++c) out[c] = pack2<T>(ds[2 * c], ds[2 * c + 1]);
@@ -780,7 +892,19 @@ attention_dq_kernel(const __grid_constant__ Params p) {
         const float row_drift = single ? 0.0f : over_parts(drift);
         // A row of one key has P = 1 and dS = 0 whatever its score: what the recomputed P leaves of dS is rounding and nothing
         // else.  (Times 0: a NaN stays one.)
-        float factor = seen == 1 ? 0.0f : p.scale;
+        bool one = seen == 1;
+        const bool documents = MODE > 0 && mods.q_docs != nullptr;
+        if (documents) {                                              // as many as its four threads found, in all CTAs of the cluster
+            asm volatile("bar.sync 1, %0;" :: "n"(kWorkThreads) : "memory");   // (the sums above have been read)
+            const float found = over_parts(static_cast<float>(visible));
+            if (p.split == 1) {
+                one = found == 1.0f;
+            } else {
+                asm volatile("bar.sync 1, %0;" :: "n"(kWorkThreads) : "memory");
+                if (part == 0) row_sum[r] = found;
+            }
+        }
+        float factor = one ? 0.0f : p.scale;
         if (ok) ok = wait(qDone, 0);
         if (stopped(sync)) ok = false;                                // (qDone comes in any case)
         if (!ok) factor = NAN;                                        // given up: dQ and, through delta, dK say so
@@ -819,6 +943,11 @@ attention_dq_kernel(const __grid_constant__ Params p) {
                 for (int k = 0; k < p.split; ++k) off += load_peer(mine_drift, k);
                 write_stat(off);
             }
+            if (documents && ok) {
+                float found = 0.0f;
+                for (int k = 0; k < p.split; ++k) found += load_peer(smem_address(row_sum + r), k);
+                factor = found == 1.0f ? 0.0f : p.scale;
+            }
             const int share = DIM / p.split, each = share / 4 > 8 ? share / 4 : 8;   // columns of this CTA, and of a thread
             for (int col = rank * share + part * each; col < rank * share + min((part + 1) * each, share); col += 8) {
                 float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
@@ -852,9 +981,9 @@ attention_dq_kernel(const __grid_constant__ Params p) {
 enum { kV = 0, kK = 1, kQFull = 2, kQEmpty = 5, kGFull = 8, kGEmpty = 11, kTFull = 14, kTEmpty = 16, kS = 18, kSRead = 19, kDp = 20, kDpRead = 21, kP = 22,
        kPUsed = 23, kDs = 24, kDsUsed = 25, kDone = 26, kBars = 27 };
 
-template <int DIM> constexpr int dkv_smem() { return 7 * (DIM / 64) * static_cast<int>(kHalfTile) + 2 * kStatBytes + static_cast<int>(sizeof(Sync)); }
+template <int DIM> constexpr int dkv_smem() { return 7 * (DIM / 64) * static_cast<int>(kHalfTile) + 2 * kStatBytes + static_cast<int>(sizeof(Sync)) + kDocPlace; }
 
-template <typename T, int DIM>
+template <typename T, int DIM, int MODE>
 __global__ void __launch_bounds__(kThreadsAttn, 1)
 attention_dkv_kernel(const __grid_constant__ Params p) {
     constexpr int HALVES = DIM / 64;
@@ -878,16 +1007,34 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
         return;
     }
     const int k0 = w.tile * kTile;
+    // MODE 2: places of this key tile for the sums by distance, one for each query head of the group
+    auto place_of = [&](int head) { return (static_cast<long long>(w.batch) * p.heads + head) * p.tiles + w.tile; };
+    auto far_of = [&](int head) { return p.scores.far + place_of(head) * kFarFloats + rank * 32 + warp * 2; };
+    if (MODE == 2 && warp < kMmaWarp && lane < 2)
+        for (int h = 0; h < p.group; ++h) far_of(w.head * p.group + h)[lane] = 0.0f;
     if (k0 >= w.k_len) {
+        if (MODE == 2 && rank == 0)
+            for (int h = threadIdx.x; h < p.group; h += kThreadsAttn) p.scores.written[place_of(w.head * p.group + h)] = make_int4(0, 0, 0, 0);
         pdl_wait();
         return;
     }
     // row tiles [first, last) see a key of this tile; all query heads of the group, one after the other, dealt out to the
     // cluster's CTAs in turn
     const int reach = w.k_len - w.q_len;                              // row i sees keys up to i + reach
-    const int first = p.causal ? max(0, k0 - reach) / kTile : 0;
-    const int each = max(0, (w.q_len + kTile - 1) / kTile - first);
+    Mods mods = find_mods<MODE>(p, w, w.head * p.group);
+    int first_tile = p.causal && k0 >= mods.prefix ? max(0, k0 - reach) / kTile : 0, last_tile = (w.q_len + kTile - 1) / kTile;
+    if constexpr (MODE > 0) {
+        if (mods.q_docs != nullptr) {
+            const int2 tiles = shared_tiles(mods.k_docs, k0, min(k0 + kTile, w.k_len), mods.q_docs, w.q_len, last_tile, reinterpret_cast<int *>(sync + 1));
+            first_tile = max(first_tile, tiles.x);
+            last_tile = tiles.y;
+        }
+    }
+    const int first = first_tile;
+    const int each = max(0, last_tile - first);
     const int n = uniform(share_of(each * p.group, rank, p.split));
+    if (MODE == 2 && rank == 0)
+        for (int h = threadIdx.x; h < p.group; h += kThreadsAttn) p.scores.written[place_of(w.head * p.group + h)] = make_int4(first, first + each, reach, 0);
 
     // a quarter of a row of the K tile for each thread, read while the CTA sets itself up
     uint32_t keys[DIM / 8];
@@ -1026,11 +1173,46 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             __syncwarp();
             if (lane == 0) barrier_arrive(bar(kK));
         }
-        const int alone = p.causal && k0 == 0 && reach <= 0 ? -reach : INT_MIN;   // the one row that sees key 0 and no other
+        const int alone = p.causal && k0 == 0 && reach <= 0 && mods.prefix <= 1 ? -reach : INT_MIN;   // the one row that sees key 0 and no other
         int tile = rank;                                              // of this head, from `first` on
+        [[maybe_unused]] int head = w.head * p.group;
+        // MODE > 0: the documents of this thread's keys, and whether the warp's keys are all of one
+        [[maybe_unused]] int key_documents[4] = {0, 0, 0, 0};
+        [[maybe_unused]] bool one_document = true;
+        if constexpr (MODE > 0) {
+            if (mods.k_docs != nullptr) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) key_documents[k] = __ldg(mods.k_docs + min(key + 8 * k, w.k_len - 1));
+                const int d = __ldg(mods.k_docs + min(k0 + 32 * (warp & 3) + lane, w.k_len - 1));
+                one_document = __all_sync(0xffffffffu, d == uniform(d));
+            }
+        }
+        // MODE 2: this thread's sums of the scores' gradients further behind and further ahead than the table reaches
+        [[maybe_unused]] float behind = 0.0f, ahead = 0.0f;
+        [[maybe_unused]] auto write_far = [&]() {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                behind += __shfl_xor_sync(0xffffffffu, behind, o);
+                ahead += __shfl_xor_sync(0xffffffffu, ahead, o);
+            }
+            if (lane < 2) far_of(head)[lane] = lane == 0 ? behind : ahead;
+            behind = ahead = 0.0f;
+        };
         for (int j = 0; j < n; ++j, tile += p.split) {
-            while (tile >= each) tile -= each;                        // the next head
+            while (tile >= each) {                                    // the next head
+                tile -= each;
+                if constexpr (MODE == 2) write_far();
+                if constexpr (MODE > 0) {
+                    ++head;
+                    if (p.scores.bias != nullptr) mods.bias += 2 * p.scores.reach + 1;
+                    if (p.scores.slopes != nullptr) mods.slope = -uniform(__ldg(p.scores.slopes + head)) * kLog2e;
+                }
+            }
             const int q0 = (first + tile) * kTile;
+            [[maybe_unused]] int row_document = 0;                    // of this lane's row of the warp's 32
+            if constexpr (MODE > 0) {
+                if (mods.q_docs != nullptr) row_document = __ldg(mods.q_docs + min(q0 + 32 * part + lane, w.q_len - 1));
+            }
             // A thread holds 8 rows' values for each of 4 keys, not 32 rows' for one: the statistics that it reads are a quarter.
             // They are read before the scores are there: afterwards dP's product, whose operands both lie in shared memory,
             // leaves other reads of it waiting.
@@ -1051,17 +1233,64 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             __syncwarp();
             if (lane == 0) barrier_arrive(bar(kSRead));
             // rows past the end and rows that see nothing have -lse = -inf: their probabilities are 0
-            if (p.causal && k0 + kTile - 1 > q0 + reach) {            // some rows do not see some keys
-                const int from = key - reach - q0 - 32 * part - 2 * (lane % 4);   // of the first of the 4 keys, which are 8 apart
+            [[maybe_unused]] uint32_t bent[16];                       // MODE > 0, capped: 1 - t^2
+            [[maybe_unused]] const int away = key - q0 - 32 * part - 2 * (lane % 4) - reach;   // distance of the first key and row
+            [[maybe_unused]] const int least = k0 + 32 * (warp & 3) - q0 - 32 * part - reach - 31;   // of the warp's last row and first key
+            float unit = p.scale_log2;
+            bool plain = true;
+            if constexpr (MODE > 0) {
+                plain = shape_transposed(p.scores, mods, p.scale_log2, away, least, s, bent);
+                unit = 1.0f;
+                uint32_t word = 0xffffffffu;                          // a bit for each value, in their order
+                if (p.causal && k0 + kTile - 1 > q0 + reach && k0 + kTile > mods.prefix) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int past = key + 8 * k < mods.prefix ? INT_MIN : away + 8 * k;   // a key is seen by the rows from here on
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const int x = 16 * (k / 2) + 4 * c + 2 * (k % 2);
+                            if (8 * c < past) word &= ~(1u << x);
+                            if (8 * c + 1 < past) word &= ~(2u << x);
+                        }
+                    }
+                }
+                if (k0 + kTile > w.k_len) {                           // places past the last key have no part in the sums by distance
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        if (key + 8 * k >= w.k_len) word &= ~((k % 2 ? 0xccccu : 0x3333u) << 16 * (k / 2));
+                }
+                if (mods.k_docs != nullptr && !(one_document && __all_sync(0xffffffffu, row_document == key_documents[0]))) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        const int d0 = __shfl_sync(0xffffffffu, row_document, 8 * c + 2 * (lane % 4)), d1 = __shfl_sync(0xffffffffu, row_document, 8 * c + 2 * (lane % 4) + 1);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) {
+                            const int x = 16 * (k / 2) + 4 * c + 2 * (k % 2);
+                            if (d0 != key_documents[k]) word &= ~(1u << x);
+                            if (d1 != key_documents[k]) word &= ~(2u << x);
+                        }
+                    }
+                }
+                if (__any_sync(0xffffffffu, word != 0xffffffffu)) {
+                    plain = false;
+#pragma unroll
+                    for (int x = 0; x < 32; ++x) s[x] = word >> x & 1 ? s[x] : 0xff800000u;
+                }
+            }
+            const bool diagonal = MODE == 0 && p.causal && k0 + kTile - 1 > q0 + reach;   // some rows do not see some keys
+            if (diagonal || !plain) {
+                [[maybe_unused]] const int from = key - reach - q0 - 32 * part - 2 * (lane % 4);   // of the first of the 4 keys, which are 8 apart
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     const float2 l = minus_lse[c];
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int x = 16 * (k / 2) + 4 * c + 2 * (k % 2);
-                        exp2_scaled<false>(prob[x], prob[x + 1], __uint_as_float(s[x]), __uint_as_float(s[x + 1]), p.scale_log2, l.x, l.y);
-                        prob[x] = 8 * c >= from + 8 * k ? prob[x] : 0.0f;
-                        prob[x + 1] = 8 * c + 1 >= from + 8 * k ? prob[x + 1] : 0.0f;
+                        exp2_scaled<false>(prob[x], prob[x + 1], __uint_as_float(s[x]), __uint_as_float(s[x + 1]), unit, l.x, l.y);
+                        if constexpr (MODE == 0) {
+                            prob[x] = 8 * c >= from + 8 * k ? prob[x] : 0.0f;
+                            prob[x + 1] = 8 * c + 1 >= from + 8 * k ? prob[x + 1] : 0.0f;
+                        }
                     }
                 }
             } else {
@@ -1071,13 +1300,22 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         const int x = 16 * (k / 2) + 4 * c + 2 * (k % 2);
-                        if (k == 3) exp2_scaled<true>(prob[x], prob[x + 1], __uint_as_float(s[x]), __uint_as_float(s[x + 1]), p.scale_log2, l.x, l.y);
-                        else exp2_scaled<false>(prob[x], prob[x + 1], __uint_as_float(s[x]), __uint_as_float(s[x + 1]), p.scale_log2, l.x, l.y);
+                        if (k == 3) exp2_scaled<true>(prob[x], prob[x + 1], __uint_as_float(s[x]), __uint_as_float(s[x + 1]), unit, l.x, l.y);
+                        else exp2_scaled<false>(prob[x], prob[x + 1], __uint_as_float(s[x]), __uint_as_float(s[x + 1]), unit, l.x, l.y);
                     }
                 }
             }
 #pragma unroll
             for (int c = 0; c < 16; ++c) out[c] = pack2<T>(prob[2 * c], prob[2 * c + 1]);
+            if constexpr (MODE == 1) {                                // from here on only dS of the products is wanted
+                if (p.scores.capped) {
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) {
+                        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&bent[c]));
+                        mul2(prob[2 * c], prob[2 * c + 1], prob[2 * c], prob[2 * c + 1], f.x, f.y);
+                    }
+                }
+            }
             ok = j == 0 || wait(kDsUsed, (j - 1) & 1);
             if (!ok) break;
             fence_after();
@@ -1096,6 +1334,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             ok = wait(kDp, j & 1);
             if (!ok) break;
             fence_after();
+            [[maybe_unused]] float diagonals[7][2] = {};              // MODE 2: sums of dS by (key - row) / 8 and the row's parity
 #pragma unroll
             for (int h = 0; h < 2; ++h) {                             // 16 keys at a time
                 uint32_t d[16];
@@ -1110,6 +1349,17 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                         float v0, v1;
                         add2(v0, v1, __uint_as_float(d[x]), __uint_as_float(d[x + 1]), e.x, e.y);
                         mul2(v0, v1, v0, v1, prob[16 * h + x], prob[16 * h + x + 1]);
+                        if constexpr (MODE == 2) {
+                            // (a hidden key's gradient is 0 whatever its values hold)
+                            v0 = prob[16 * h + x] == 0.0f ? 0.0f : v0;
+                            v1 = prob[16 * h + x + 1] == 0.0f ? 0.0f : v1;
+                            diagonals[2 * h + k - c + 3][0] += v0;
+                            diagonals[2 * h + k - c + 3][1] += v1;
+                            if (p.scores.capped) {
+                                const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&bent[8 * h + x / 2]));
+                                mul2(v0, v1, v0, v1, f.x, f.y);
+                            }
+                        }
                         out[8 * h + x / 2] = pack2<T>(v0, v1);
                     }
                 }
@@ -1117,6 +1367,29 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             fence_before();
             __syncwarp();
             if (lane == 0) barrier_arrive(bar(kDpRead));
+            if constexpr (MODE == 2) {
+                const int far = beyond(least, p.scores.reach), nearest = max(0, first_near(k0, reach, p.scores.reach)), at = first + tile - nearest;
+                if (far != 0) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int m = 0; m < 7; ++m) sum += diagonals[m][0] + diagonals[m][1];
+                    (far < 0 ? behind : ahead) += sum;
+                }
+                if (at >= 0 && at < p.scores.near_tiles && (first + tile) * kTile < k0 + 127 - reach + p.scores.reach) {
+                    float *to = p.scores.near + (place_of(head) * p.scores.near_tiles + at) * kNearFloats + warp * 64 + 16 * (lane % 4) + lane / 4;
+                    float a[2] = {0.0f, 0.0f};
+                    if (far == 0) sum_diagonals(diagonals, a);
+                    // the warp's 64 sums are of distances from least - 1 on; two of them this lane's
+                    const int d = least - 1 + 16 * (lane % 4) + lane / 4;
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        if (d + 8 * x <= -p.scores.reach) { behind += a[x]; a[x] = 0.0f; }
+                        else if (d + 8 * x >= p.scores.reach) { ahead += a[x]; a[x] = 0.0f; }
+                    }
+                    to[0] = a[0];
+                    to[8] = a[1];
+                }
+            }
             ok = wait(kPUsed, j & 1);
             if (!ok) break;
             fence_after();
@@ -1132,6 +1405,12 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
         }
         if (ok) ok = wait(kDone, 0);
         if (stopped(sync)) ok = false;                                // (kDone comes in any case)
+        if constexpr (MODE == 2) {
+            if (n > 0) {
+                if (!ok) behind = ahead = NAN;                        // given up: the bias's gradient says so
+                write_far();
+            }
+        }
         fence_after();
         // dV by every other four warps, dK by the rest; the first eight warps take the first half of the columns
         const int which = part & 1, half = part >> 1, r = threadIdx.x & 127;

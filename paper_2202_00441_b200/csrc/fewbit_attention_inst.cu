@@ -1,4 +1,5 @@
-// The attention kernels for one 16-bit type (FEWBIT_ATTN_F16: binary16, else bfloat16).
+// The attention kernels for one 16-bit type (FEWBIT_ATTN_F16: binary16, else bfloat16), with plain scores or with caps, biases
+// and masks (FEWBIT_ATTN_SCORES).
 #include <atomic>
 
 #include "fewbit_attention.cuh"
@@ -50,19 +51,37 @@ cudaError_t launch(const Params &p, unsigned grid, unsigned cluster, cudaStream_
 
 }  // namespace
 
+#if FEWBIT_ATTN_SCORES
+constexpr int kMode = 1;
+#if FEWBIT_ATTN_F16
+cudaError_t launch_scores_f16(
+#else
+cudaError_t launch_scores_bf16(
+#endif
+#else
+constexpr int kMode = 0;
 #if FEWBIT_ATTN_F16
 cudaError_t launch_f16(
 #else
 cudaError_t launch_bf16(
 #endif
+#endif
     Kernel which, bool wide, const Params &p, unsigned grid, cudaStream_t st) {
     switch (which) {
     case Kernel::forward:
-        return wide ? launch<attention_fwd_kernel<T, 128>, fwd_smem<128>()>(p, grid * p.split, p.split, st) : launch<attention_fwd_kernel<T, 64>, fwd_smem<64>()>(p, grid * p.split, p.split, st);
+        return wide ? launch<attention_fwd_kernel<T, 128, kMode>, fwd_smem<128>()>(p, grid * p.split, p.split, st)
+                    : launch<attention_fwd_kernel<T, 64, kMode>, fwd_smem<64>()>(p, grid * p.split, p.split, st);
     case Kernel::dq:
-        return wide ? launch<attention_dq_kernel<T, 128>, dq_smem<128>()>(p, grid * p.split, p.split, st) : launch<attention_dq_kernel<T, 64>, dq_smem<64>()>(p, grid * p.split, p.split, st);
+        return wide ? launch<attention_dq_kernel<T, 128, kMode>, dq_smem<128>()>(p, grid * p.split, p.split, st)
+                    : launch<attention_dq_kernel<T, 64, kMode>, dq_smem<64>()>(p, grid * p.split, p.split, st);
+#if FEWBIT_ATTN_SCORES
+    case Kernel::dkv_bias:
+        return wide ? launch<attention_dkv_kernel<T, 128, 2>, dkv_smem<128>()>(p, grid * p.split, p.split, st)
+                    : launch<attention_dkv_kernel<T, 64, 2>, dkv_smem<64>()>(p, grid * p.split, p.split, st);
+#endif
     default:
-        return wide ? launch<attention_dkv_kernel<T, 128>, dkv_smem<128>()>(p, grid * p.split, p.split, st) : launch<attention_dkv_kernel<T, 64>, dkv_smem<64>()>(p, grid * p.split, p.split, st);
+        return wide ? launch<attention_dkv_kernel<T, 128, kMode>, dkv_smem<128>()>(p, grid * p.split, p.split, st)
+                    : launch<attention_dkv_kernel<T, 64, kMode>, dkv_smem<64>()>(p, grid * p.split, p.split, st);
     }
 }
 

@@ -52,6 +52,9 @@ fewbit_heads heads_of(const Tensor &t) {
 void like(const Tensor &t, const Tensor &model, const char *what) {
     if (t.sizes() != model.sizes() || t.scalar_type() != model.scalar_type() || t.device() != model.device()) refuse(what);
 }
+void dense(const Tensor &t, const char *what) {
+    if (!t.is_cuda() || !t.is_contiguous()) refuse(what);
+}
 const float *vector_of(const Optional &w, const Tensor &q, int64_t n) {
     if (!w) return nullptr;
     if (w->scalar_type() != at::kFloat || w->device() != q.device() || w->dim() != 1 || w->numel() != n || !w->is_contiguous())
@@ -198,20 +201,61 @@ Attention attention_shape(const Tensor &q, const Tensor &k, const Tensor &v, boo
     return a;
 }
 
+fewbit_attention_scores scores_of(const Attention &a, const Tensor &q, const Tensor &k, std::optional<double> cap, const Optional &slopes, const Optional &distance_bias,
+                                  const Optional &prefix_lens, const Optional &q_documents, const Optional &k_documents) {
+    fewbit_attention_scores c = {};
+    auto is = [&](const Tensor &t, at::ScalarType type) { return t.scalar_type() == type && t.device() == q.device() && t.is_contiguous(); };
+    if (cap) {
+        if (!(*cap >= 0)) refuse("cap must not be negative");
+        c.cap = static_cast<float>(*cap);
+    }
+    if (slopes) {
+        if (!is(*slopes, at::kFloat) || slopes->dim() != 1 || slopes->size(0) != a.s.heads) refuse("slopes must be a contiguous float32 vector with a value for each head of q, on its device");
+        c.slopes = slopes->data_ptr<float>();
+    }
+    if (distance_bias) {
+        const Tensor &t = *distance_bias;
+        if (!is(t, at::kFloat) || t.dim() != 2 || t.size(0) != a.s.heads || t.size(1) % 2 != 1 || t.size(1) < 3 || t.size(1) > 2 * FEWBIT_MAX_DISTANCE + 1)
+            refuse("distance_bias must be a contiguous float32 (heads, 2 R + 1) tensor on the device of q, R from 1 to 4096");
+        c.distance_bias = t.data_ptr<float>();
+        c.max_distance = static_cast<int>(t.size(1) / 2);
+    }
+    if (prefix_lens) {
+        if (!a.s.causal) refuse("prefix_lens are for causal attention");
+        if (!is(*prefix_lens, at::kInt) || prefix_lens->dim() != 1 || prefix_lens->size(0) != a.s.batch) refuse("prefix_lens must be a contiguous int32 vector with a value for each sequence, on the device of q");
+        c.prefix_lens = prefix_lens->data_ptr<int32_t>();
+    }
+    if (q_documents.has_value() != k_documents.has_value()) refuse("q_documents and k_documents come together");
+    if (q_documents) {
+        const int64_t lead = q.dim() - 2;                             // (batch, length) or (rows)
+        if (!is(*q_documents, at::kInt) || !is(*k_documents, at::kInt) || q_documents->sizes() != q.sizes().slice(0, lead) || k_documents->sizes() != k.sizes().slice(0, lead))
+            refuse("q_documents and k_documents must be contiguous int32 tensors with a value for each row of q and of k, on their device");
+        c.q_documents = q_documents->data_ptr<int32_t>();
+        c.k_documents = k_documents->data_ptr<int32_t>();
+    }
+    return c;
+}
+
 std::tuple<Tensor, Tensor> attention_fwd(const Tensor &q, const Tensor &k, const Tensor &v, bool causal, std::optional<double> scale, const Optional &q_offsets,
-                                         const Optional &k_offsets, std::optional<int64_t> max_q, std::optional<int64_t> max_k) {
+                                         const Optional &k_offsets, std::optional<int64_t> max_q, std::optional<int64_t> max_k, std::optional<double> cap,
+                                         const Optional &slopes, const Optional &distance_bias, const Optional &prefix_lens, const Optional &q_documents,
+                                         const Optional &k_documents) {
     const Attention a = attention_shape(q, k, v, causal, scale, q_offsets, k_offsets, max_q, max_k);
+    const fewbit_attention_scores c = scores_of(a, q, k, cap, slopes, distance_bias, prefix_lens, q_documents, k_documents);
     const c10::cuda::OptionalCUDAGuard guard(q.device());
     Tensor out = at::empty(q.sizes(), q.options()), lse = at::empty(a.stats, q.options().dtype(at::kFloat));
     const fewbit_heads h[4] = {heads_of(q), heads_of(k), heads_of(v), heads_of(out)};
-    check(fewbit_attention_fwd(&a.s, &h[0], &h[1], &h[2], &h[3], lse.data_ptr<float>(), stream_of(q)), "fewbit_attention_fwd");
+    check(fewbit_attention_scores_fwd(&a.s, &c, &h[0], &h[1], &h[2], &h[3], lse.data_ptr<float>(), stream_of(q)), "fewbit_attention_fwd");
     return {out, lse};
 }
 
-std::tuple<Tensor, Tensor, Tensor> attention_bwd(const Tensor &g, const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &out, const Tensor &lse,
-                                                 bool causal, std::optional<double> scale, const Optional &q_offsets, const Optional &k_offsets,
-                                                 std::optional<int64_t> max_q, std::optional<int64_t> max_k) {
+std::vector<Tensor> attention_bwd(const Tensor &g, const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &out, const Tensor &lse,
+                                  bool causal, std::optional<double> scale, const Optional &q_offsets, const Optional &k_offsets,
+                                  std::optional<int64_t> max_q, std::optional<int64_t> max_k, std::optional<double> cap, const Optional &slopes,
+                                  const Optional &distance_bias, const Optional &prefix_lens, const Optional &q_documents, const Optional &k_documents,
+                                  bool bias_grad) {
     const Attention a = attention_shape(q, k, v, causal, scale, q_offsets, k_offsets, max_q, max_k);
+    const fewbit_attention_scores c = scores_of(a, q, k, cap, slopes, distance_bias, prefix_lens, q_documents, k_documents);
     like(g, q, "grad_out must have the shape and type of the output");
     like(out, q, "out must be what the forward pass gave");
     if (lse.sizes() != at::IntArrayRef(a.stats) || lse.scalar_type() != at::kFloat || lse.device() != q.device() || !lse.is_contiguous())
@@ -222,12 +266,43 @@ std::tuple<Tensor, Tensor, Tensor> attention_bwd(const Tensor &g, const Tensor &
     Tensor dq = at::empty(q.sizes(), q.options());
     Tensor dk = none ? at::zeros(k.sizes(), k.options()) : at::empty(k.sizes(), k.options());
     Tensor dv = none ? at::zeros(v.sizes(), v.options()) : at::empty(v.sizes(), v.options());
-    const size_t bytes = fewbit_attention_workspace_bytes(&a.s);
+    bias_grad = bias_grad && distance_bias;
+    Tensor db;
+    if (bias_grad) db = none ? at::zeros(distance_bias->sizes(), distance_bias->options()) : at::empty(distance_bias->sizes(), distance_bias->options());
+    const size_t bytes = fewbit_attention_scores_workspace_bytes(&a.s, &c, bias_grad);
     Tensor ws = at::empty({static_cast<int64_t>(bytes)}, q.options().dtype(at::kByte));
     const fewbit_heads h[8] = {heads_of(g), heads_of(q), heads_of(k), heads_of(v), heads_of(out), heads_of(dq), heads_of(dk), heads_of(dv)};
-    check(fewbit_attention_bwd(&a.s, &h[0], &h[1], &h[2], &h[3], &h[4], lse.data_ptr<float>(), &h[5], &h[6], &h[7], ws.data_ptr(), bytes, stream_of(q)),
+    check(fewbit_attention_scores_bwd(&a.s, &c, &h[0], &h[1], &h[2], &h[3], &h[4], lse.data_ptr<float>(), &h[5], &h[6], &h[7],
+                                      bias_grad && !none ? db.data_ptr<float>() : nullptr, ws.data_ptr(), bytes, stream_of(q)),
           "fewbit_attention_bwd");
+    if (bias_grad) return {dq, dk, dv, db};
     return {dq, dk, dv};
+}
+
+Tensor relative_bias_fwd(const Tensor &table, int64_t max_distance, bool bidirectional) {
+    dense(table, "table must be a contiguous CUDA tensor");
+    if (table.dim() != 2) refuse("table must be (buckets, heads)");
+    const fewbit_dtype dtype = dtype_of(table);
+    const int buckets = size_of(table.size(0)), heads = size_of(table.size(1));
+    if (max_distance < 1 || max_distance > FEWBIT_MAX_DISTANCE) refuse("max_distance must be from 1 to 4096");
+    const c10::cuda::OptionalCUDAGuard guard(table.device());
+    Tensor bias = at::empty({heads, 2 * max_distance + 1}, table.options().dtype(at::kFloat));
+    check(fewbit_relative_bias_fwd(table.data_ptr(), buckets, heads, static_cast<int>(max_distance), bidirectional, dtype, bias.data_ptr<float>(), stream_of(table)),
+          "fewbit_relative_bias_fwd");
+    return bias;
+}
+Tensor relative_bias_bwd(const Tensor &grad, const Tensor &table, bool bidirectional) {
+    dense(grad, "grad_distance_bias must be a contiguous CUDA tensor");
+    if (table.dim() != 2 || grad.dim() != 2 || grad.scalar_type() != at::kFloat || grad.device() != table.device() || grad.size(0) != table.size(1) || grad.size(1) % 2 != 1 ||
+        grad.size(1) < 3 || grad.size(1) > 2 * FEWBIT_MAX_DISTANCE + 1)
+        refuse("grad_distance_bias must be float32 (heads, 2 R + 1) for a table (buckets, heads) on the same device");
+    const fewbit_dtype dtype = dtype_of(table);
+    const int buckets = size_of(table.size(0)), heads = size_of(table.size(1));
+    const c10::cuda::OptionalCUDAGuard guard(grad.device());
+    Tensor out = at::empty(table.sizes(), grad.options().dtype(table.scalar_type()));
+    check(fewbit_relative_bias_bwd(grad.data_ptr<float>(), buckets, heads, static_cast<int>(grad.size(1) / 2), bidirectional, dtype, out.data_ptr(), stream_of(grad)),
+          "fewbit_relative_bias_bwd");
+    return out;
 }
 
 // Dropout's numbers: `seed` is an integer or one int64 value on the device of the tensors.
@@ -248,9 +323,6 @@ fewbit_dropout_options drop_of(double p, const Seed &seed, int64_t place, const 
 void whole_or_none(const Tensor &out, std::initializer_list<const Tensor *> inputs) {
     for (const Tensor *t : inputs)
         if (t != nullptr && at::get_overlap_status(out, *t) == at::MemOverlapStatus::Partial) refuse("out overlaps an input in part");
-}
-void dense(const Tensor &t, const char *what) {
-    if (!t.is_cuda() || !t.is_contiguous()) refuse(what);
 }
 
 Tensor dropout_fwd(const Tensor &x, double p, const Seed &seed, int64_t place, const Optional &residual, const Optional &out) {
@@ -440,6 +512,8 @@ PYBIND11_MODULE(TORCH_EXTENSION_NAME, m) {
     m.def("qk_norm_rope_bwd", &qk_norm_rope_bwd);
     m.def("attention_fwd", &attention_fwd);
     m.def("attention_bwd", &attention_bwd);
+    m.def("relative_bias_fwd", &relative_bias_fwd);
+    m.def("relative_bias_bwd", &relative_bias_bwd);
     m.def("dropout_fwd", &dropout_fwd);
     m.def("dropout_bwd", &dropout_bwd);
     m.def("add_rms_norm_fwd", &add_rms_norm_fwd);

@@ -34,6 +34,11 @@ class _AttentionShape(ctypes.Structure):
                 ("scale", ctypes.c_float), ("dtype", ctypes.c_int)]
 
 
+class _AttentionScores(ctypes.Structure):
+    _fields_ = [("cap", ctypes.c_float), ("slopes", ctypes.c_void_p), ("distance_bias", ctypes.c_void_p), ("max_distance", ctypes.c_int),
+                ("prefix_lens", ctypes.c_void_p), ("q_documents", ctypes.c_void_p), ("k_documents", ctypes.c_void_p)]
+
+
 class _AdamWTensor(ctypes.Structure):
     _fields_ = [("param", ctypes.c_void_p), ("exp_avg", ctypes.c_void_p), ("exp_avg_sq", ctypes.c_void_p),
                 ("exp_avg_scale", ctypes.c_void_p), ("exp_avg_sq_scale", ctypes.c_void_p), ("master", ctypes.c_void_p),
@@ -135,8 +140,10 @@ def fewbit_qk_norm_rope_bwd(grad_q_out: torch.Tensor, grad_k_out: torch.Tensor, 
 
 def fewbit_attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool = False, scale: Optional[float] = None,
                          q_offsets: Optional[torch.Tensor] = None, k_offsets: Optional[torch.Tensor] = None,
-                         max_q_len: Optional[int] = None, max_k_len: Optional[int] = None,
-                         stream: Optional[torch.cuda.Stream] = None):
+                         max_q_len: Optional[int] = None, max_k_len: Optional[int] = None, cap: Optional[float] = None,
+                         slopes: Optional[torch.Tensor] = None, distance_bias: Optional[torch.Tensor] = None,
+                         prefix_lens: Optional[torch.Tensor] = None, q_documents: Optional[torch.Tensor] = None,
+                         k_documents: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
     """softmax(scale q k^T) v for every head; returns (out, lse).
 
     q: (batch, q_len, heads, head_dim), k and v: (batch, k_len, kv_heads, head_dim), bfloat16 or float16, head_dim a multiple
@@ -145,25 +152,61 @@ def fewbit_attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, c
     Packed sequences: q (rows, heads, head_dim), k and v (key rows, ...), with int32 ``q_offsets`` and ``k_offsets`` on the
     device (batch + 1 values each) and the longest sequence's lengths ``max_q_len`` and ``max_k_len``.
     lse: float32 (batch, heads, q_len), or (heads, rows) when packed: the logarithm of each row's sum of exponentials,
-    -inf for a row that sees no key (whose out is 0)."""
+    -inf for a row that sees no key (whose out is 0).
+
+    The scores z = scale q k^T can be changed and masked further, with d = j - i - (k_len - q_len) for row i and key j:
+    ``cap``: z becomes cap tanh(z / cap).  ``slopes`` (heads,) float32: minus slope |d|.  ``distance_bias`` (heads, 2 R + 1)
+    float32, R up to 4096: plus the bias of d, cut to [-R, R] (see ``fewbit_relative_bias_fwd``; -inf hides the key).
+    ``prefix_lens`` (batch,) int32, with ``causal``: the first keys of a sequence that every row sees.  ``q_documents`` and
+    ``k_documents``, int32 (batch, q_len) and (batch, k_len), or (rows,) and (key rows,) when packed: a row sees the keys of its
+    own document only (numbers that grow along the sequence let whole tiles be skipped)."""
+    args = (q, k, v, causal, scale, q_offsets, k_offsets, max_q_len, max_k_len, cap, slopes, distance_bias, prefix_lens, q_documents, k_documents)
     if stream is not None:
-        with _On(stream, q, k, v, q_offsets, k_offsets):
-            return _torch_module().attention_fwd(q, k, v, causal, scale, q_offsets, k_offsets, max_q_len, max_k_len)
-    return _torch_module().attention_fwd(q, k, v, causal, scale, q_offsets, k_offsets, max_q_len, max_k_len)
+        with _On(stream, q, k, v, q_offsets, k_offsets, slopes, distance_bias, prefix_lens, q_documents, k_documents):
+            return _torch_module().attention_fwd(*args)
+    return _torch_module().attention_fwd(*args)
 
 
 def fewbit_attention_bwd(grad_out: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
                          lse: torch.Tensor, *, causal: bool = False, scale: Optional[float] = None,
                          q_offsets: Optional[torch.Tensor] = None, k_offsets: Optional[torch.Tensor] = None,
-                         max_q_len: Optional[int] = None, max_k_len: Optional[int] = None,
+                         max_q_len: Optional[int] = None, max_k_len: Optional[int] = None, cap: Optional[float] = None,
+                         slopes: Optional[torch.Tensor] = None, distance_bias: Optional[torch.Tensor] = None,
+                         prefix_lens: Optional[torch.Tensor] = None, q_documents: Optional[torch.Tensor] = None,
+                         k_documents: Optional[torch.Tensor] = None, bias_grad: bool = True,
                          stream: Optional[torch.cuda.Stream] = None):
     """Gradients (grad_q, grad_k, grad_v) of ``fewbit_attention_fwd`` from its inputs and outputs and ``grad_out``; the
-    probabilities are recomputed.  The same inputs give the same bits."""
-    args = (grad_out, q, k, v, out, lse, causal, scale, q_offsets, k_offsets, max_q_len, max_k_len)
+    probabilities are recomputed.  With ``distance_bias`` a fourth one, its gradient (unless ``bias_grad`` is False).  The same
+    inputs give the same bits."""
+    args = (grad_out, q, k, v, out, lse, causal, scale, q_offsets, k_offsets, max_q_len, max_k_len, cap, slopes, distance_bias, prefix_lens,
+            q_documents, k_documents, bias_grad)
     if stream is not None:
-        with _On(stream, grad_out, q, k, v, out, lse, q_offsets, k_offsets):
-            return _torch_module().attention_bwd(*args)
-    return _torch_module().attention_bwd(*args)
+        with _On(stream, grad_out, q, k, v, out, lse, q_offsets, k_offsets, slopes, distance_bias, prefix_lens, q_documents, k_documents):
+            return tuple(_torch_module().attention_bwd(*args))
+    return tuple(_torch_module().attention_bwd(*args))
+
+
+def fewbit_relative_bias_fwd(table: torch.Tensor, max_distance: int, *, bidirectional: bool = False,
+                             stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """The learned bias of relative positions by buckets, ``table`` (buckets, heads), spread over the distances from
+    -max_distance to max_distance: float32 (heads, 2 max_distance + 1), the ``distance_bias`` of ``fewbit_attention_fwd``.
+
+    Half of a direction's buckets hold one distance each, the others logarithmically wider ones up to ``max_distance``, and the
+    last what lies further.  ``bidirectional``: half the buckets for the keys behind their row (and level with it), half for those
+    ahead; else all for those behind, and a key ahead counts as level."""
+    if stream is not None:
+        with _On(stream, table):
+            return _torch_module().relative_bias_fwd(table, max_distance, bidirectional)
+    return _torch_module().relative_bias_fwd(table, max_distance, bidirectional)
+
+
+def fewbit_relative_bias_bwd(grad_distance_bias: torch.Tensor, table: torch.Tensor, *, bidirectional: bool = False,
+                             stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """Gradient of ``fewbit_relative_bias_fwd`` for its table (of which only shape and type are used)."""
+    if stream is not None:
+        with _On(stream, grad_distance_bias):
+            return _torch_module().relative_bias_bwd(grad_distance_bias, table, bidirectional)
+    return _torch_module().relative_bias_bwd(grad_distance_bias, table, bidirectional)
 
 
 def fewbit_attention_timeout_count(device=None) -> int:
