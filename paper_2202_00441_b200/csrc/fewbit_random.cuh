@@ -11,7 +11,7 @@ struct RandomKeys {              // of the ten rounds
     uint32_t a[10], b[10];
 };
 
-__device__ __forceinline__ RandomKeys random_keys(uint64_t seed) {
+__host__ __device__ __forceinline__ RandomKeys random_keys(uint64_t seed) {
     RandomKeys k;
 #pragma unroll
     for (int i = 0; i < 10; ++i) {
@@ -21,9 +21,10 @@ __device__ __forceinline__ RandomKeys random_keys(uint64_t seed) {
     return k;
 }
 
-// The words of elements [4 group, 4 group + 4).
-__device__ __forceinline__ uint4 random_words(const RandomKeys &k, uint64_t group, uint32_t place) {
-    uint32_t c0 = static_cast<uint32_t>(group), c1 = static_cast<uint32_t>(group >> 32), c2 = place, c3 = 0;
+// The words of elements [4 group, 4 group + 4), group = high 2^32 + low.  Where `high` is the same for several groups, half of
+// the first two rounds' products are too, and the compiler takes them once.
+__device__ __forceinline__ uint4 random_words(const RandomKeys &k, uint32_t low, uint32_t high, uint32_t place) {
+    uint32_t c0 = low, c1 = high, c2 = place, c3 = 0;
 #pragma unroll
     for (int i = 0; i < 10; ++i) {
         const uint64_t m0 = static_cast<uint64_t>(c0) * 0xD2511F53u, m1 = static_cast<uint64_t>(c2) * 0xCD9E8D57u;
@@ -37,27 +38,28 @@ __device__ __forceinline__ uint4 random_words(const RandomKeys &k, uint64_t grou
 
 // What dropout needs to know: an element is kept where its word is at least `limit`.
 struct Drop {
+    RandomKeys keys;             // of a seed that the host knows: operands straight from the kernel's parameters
     uint64_t seed;
-    const int64_t *seed_device;  // added to it, if any
+    const int64_t *seed_device;  // added to it, if any: its keys are added up where they are used
     uint32_t place, limit;
     float scale;                 // 1 / (1 - p)
     bool on;
 };
-__device__ __forceinline__ RandomKeys random_keys(const Drop &d) {
+__device__ __forceinline__ RandomKeys device_keys(const Drop &d) {
     return random_keys(d.seed + (d.seed_device != nullptr ? static_cast<uint64_t>(__ldg(d.seed_device)) : 0));
 }
 
-// v[e] of the N elements from `first` on (a multiple of N, N 1, 4 or 8): scaled where kept, else 0.
+// v[e] of N elements (1, 4 or 8) from the group (low, high) on: scaled where kept, else 0.  N 1: the one at place `i` of the group.
 template <int N>
-__device__ __forceinline__ void drop(const Drop &d, const RandomKeys &k, uint64_t first, float *v) {
+__device__ __forceinline__ void drop(const Drop &d, const RandomKeys &k, uint32_t low, uint32_t high, uint32_t i, float *v) {
     if constexpr (N == 1) {
-        const uint4 w = random_words(k, first >> 2, d.place);
-        const uint32_t i = static_cast<uint32_t>(first) & 3, word = i < 2 ? (i == 0 ? w.x : w.y) : (i == 2 ? w.z : w.w);
+        const uint4 w = random_words(k, low, high, d.place);
+        const uint32_t word = i < 2 ? (i == 0 ? w.x : w.y) : (i == 2 ? w.z : w.w);
         v[0] = word >= d.limit ? v[0] * d.scale : 0.0f;
     } else {
 #pragma unroll
         for (int e = 0; e < N; e += 4) {
-            const uint4 w = random_words(k, (first + e) >> 2, d.place);
+            const uint4 w = random_words(k, low + e / 4, high, d.place);   // (8 elements from a multiple of 8 on share `high`)
             v[e] = w.x >= d.limit ? v[e] * d.scale : 0.0f;
             v[e + 1] = w.y >= d.limit ? v[e + 1] * d.scale : 0.0f;
             v[e + 2] = w.z >= d.limit ? v[e + 2] * d.scale : 0.0f;

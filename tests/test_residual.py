@@ -169,7 +169,8 @@ CASES = [
     (9, 31, 1, 0.1, True, True), (17, 64, 0, 0.0, True, True), (33, 333, 0, 0.2, True, True), (4, 512, 0, 0.1, False, False), (5, 640, 0, 0.0, True, True),
     (300, 1000, 4, 0.1, True, True), (2, 1288, 8, 0.0, True, True), (3, 2052, 0, 0.1, True, True), (700, 4096, 0, 0.1, True, True), (2, 8191, 3, 0.1, True, True),
     (2, 8192, 0, 0.0, True, True), (3, 8200, 0, 0.1, True, True), (2, 16383, 0, 0.1, True, True), (1, 16384, 0, 0.1, True, True), (1300, 16384, 0, 0.0, True, True),
-    (40000, 48, 0, 0.1, True, True),
+    (40000, 48, 0, 0.1, True, True), (5000, 5, 0, 0.2, True, True), (3000, 256, 0, 0.1, True, True), (1000, 509, 0, 0.1, True, True), (20000, 1026, 0, 0.0, True, True),
+    (700, 4099, 0, 0.1, True, True), (500, 8197, 0, 0.0, True, True), (9, 16377, 0, 0.1, True, True), (3, 2049, 8, 0.1, True, False),
 ]
 
 
@@ -267,6 +268,23 @@ def test_norm_past_32_bits_of_elements():
     g[-4:] = new((4, width), torch.bfloat16, 2)
     gx, _, _ = fb.fewbit_add_rms_norm_bwd(g, None, h, p=0.25, seed=3, place=1, residual_grad=False, weight_grad=False)
     assert ((gx[-4:] != 0) <= mask).all() and (gx[-4:] != 0).double().mean() > 0.7
+
+
+@pytest.mark.gpu
+def test_the_counters_upper_half():
+    """From element 2^34 on the generator's second counter counts; one row has elements on both sides."""
+    width = 16376
+    first_row = (1 << 34) // width
+    rows = first_row + 3
+    x = torch.ones(rows, width, dtype=torch.bfloat16, device="cuda")
+    assert (1 << 34) % width and x.numel() > 1 << 34
+    gx, _, _ = fb.fewbit_add_rms_norm_bwd(x, x, x, eps=0.0, p=0.25, seed=77, place=2, residual_grad=False, weight_grad=False)
+    at = first_row * width // 4 * 4
+    want = kept((3 * width,), 0.25, 77, 2, at).cuda()
+    assert torch.equal(gx.view(-1)[at:at + 3 * width] != 0, want)
+    del gx
+    y = fb.fewbit_dropout_fwd(x, 0.25, seed=77, place=2, out=x)
+    assert torch.equal(y.view(-1)[at:at + 3 * width] != 0, want)
 
 
 @pytest.mark.gpu
