@@ -184,6 +184,21 @@ void fill_scores(const fewbit_attention_shape *s, const fewbit_attention_scores 
     to.capped = c->cap > 0;
     to.cap_in = to.capped ? s->scale / c->cap : 0.0f;
     to.cap_out = c->cap * attn::kLog2e;
+    // tanh(a) / a by powers of a^2, for magnitudes up to 0.3 and 1, with a = cap_in s and the result's factor folded in: where the
+    // folded coefficients are normal numbers, else the exponential form serves all.
+    to.near_limit = to.odd_limit = -1.0f;
+    if (to.capped && to.cap_in > 0x1p-12f && to.cap_in < 0x1p12f && to.cap_out > 0x1p-12f && to.cap_out < 0x1p24f) {
+        const double near_odd[3] = {0.9999988675117493, -0.33310022950172424, 0.12633946537971497};
+        const double odd[6] = {0.9999994039535522, -0.3332904279232025, 0.13281433284282684, -0.051605671644210815, 0.016743114218115807, -0.0030670601408928633};
+        double power = static_cast<double>(to.cap_in) * to.cap_out;
+        for (int k = 0; k < 6; ++k, power *= static_cast<double>(to.cap_in) * to.cap_in) {
+            if (k < 3) to.near_odd[k] = static_cast<float>(near_odd[k] * power);
+            to.odd[k] = static_cast<float>(odd[k] * power);
+        }
+        to.near_limit = 0.3f / to.cap_in;
+        to.odd_limit = 1.0f / to.cap_in;
+    }
+    to.cap_out_2 = to.capped ? 1.0f / to.cap_out / to.cap_out : 0.0f;
     to.slopes = c->slopes;
     to.bias = c->distance_bias;
     to.reach = c->distance_bias != nullptr ? c->max_distance : 0;

@@ -65,9 +65,10 @@ struct Params {
     bool causal;
     bool after_dq;                    // dK, dV: launched right behind the dQ kernel, whose start is all that its CTAs have waited for
     float scale, scale_log2;          // scale * log2(e)
-    Scores scores;                    // (kernels of MODE 1 and 2)
+    Scores scores;                    // (kernels of MODE 1 to 3)
 };
-// MODE of the kernels: 0 plain scores, 1 with caps, biases and masks (fewbit_scores.cuh), 2 (dK and dV) with the bias's gradient too
+// MODE of the kernels (fewbit_scores.cuh): 0 plain scores; 1 cap and masks; 2 biases too; 3 (dK and dV) the gradient of a bias by
+// distance, too.  (One kernel for 1 and 2 spills and runs 10 to 20 % longer in either case.)
 
 // What one CTA works on.
 struct Work {
@@ -143,7 +144,7 @@ struct Sync {
     uint32_t tmem;
     int stop;
 };
-constexpr int kDocPlace = 16;          // bytes behind everything else, for shared_tiles
+constexpr int kDocPlace = kScanWarps * 8;   // bytes behind everything else, for scan_tiles
 
 // A tile of `rows` valid rows: the rest may hold another sequence's values, which a zero probability does not
 // silence when they are not finite.  One warp clears them.
@@ -266,14 +267,19 @@ __device__ __forceinline__ bool pair_any(int id, bool x) {
     return any != 0;
 }
 
-// 32 columns of a row: probabilities, rounded to `s_at`, and their sum.  MIXED: a quarter of them on the FMA pipe.
-template <typename T, bool MIXED>
+// 32 columns of a row: probabilities, rounded to `s_at`, and their sum.  MIXED: a quarter of them on the FMA pipe.  READY: s holds the
+// exponents themselves.
+template <typename T, bool MIXED, bool READY = false>
 __device__ __forceinline__ void fwd_probabilities(const uint32_t *s, float scale, float shift, float (&part)[4], uint32_t at) {
     uint32_t r[16];
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
         float a, b;
-        if (MIXED && e % 4 == 3) exp2_scaled<true>(a, b, __uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]), scale, shift, shift);
+        if (READY && MIXED && e % 4 == 3) exp2_polynomial(a, b, __uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
+        else if (READY) {
+            a = exp2_fast(__uint_as_float(s[2 * e]));
+            b = exp2_fast(__uint_as_float(s[2 * e + 1]));
+        } else if (MIXED && e % 4 == 3) exp2_scaled<true>(a, b, __uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]), scale, shift, shift);
         else exp2_scaled<false>(a, b, __uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]), scale, shift, shift);
         add2(part[2 * (e & 1)], part[2 * (e & 1) + 1], part[2 * (e & 1)], part[2 * (e & 1) + 1], a, b);
         r[e] = pack2<T>(a, b);
@@ -308,21 +314,21 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
     int all0 = key_tiles(p, w, min(q0 + kTile, w.q_len) - 1, mods.prefix);
     int all1 = q0 + kTile < w.q_len ? key_tiles(p, w, min(q0 + 2 * kTile, w.q_len) - 1, mods.prefix) : 0;
     int skipped = 0;                                                  // key tiles in front, which neither row tile sees
-    if constexpr (MODE > 0) {
-        if (mods.q_docs != nullptr) {
-            const int2 tiles = shared_tiles(mods.q_docs, q0, min(q0 + 2 * kTile, w.q_len), mods.k_docs, w.k_len, max(all0, all1), reinterpret_cast<int *>(joined + 4 * kTile));
-            skipped = tiles.x;
-            all0 = max(0, min(all0, tiles.y) - skipped);
-            all1 = max(0, min(all1, tiles.y) - skipped);
-        }
+    int2 *const scanned = reinterpret_cast<int2 *>(joined + 4 * kTile);
+    if (MODE > 0 && mods.q_docs != nullptr) scan_tiles<8>(mods.q_docs, q0, min(q0 + 2 * kTile, w.q_len), mods.k_docs, w.k_len, max(all0, all1), scanned);
+    constexpr uint32_t counts[fBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 8, 8, 8, 8, 1, 1, 1};
+    const uint32_t tmem = start_cta(sync, fBars, counts);
+    if (MODE > 0 && mods.q_docs != nullptr) {
+        const int2 tiles = scanned_tiles(scanned);
+        skipped = tiles.x;
+        all0 = max(0, min(all0, tiles.y) - skipped);
+        all1 = max(0, min(all1, tiles.y) - skipped);
     }
     const int n0 = uniform(share_of(all0, rank, p.split));
     const int n1 = uniform(share_of(all1, rank, p.split));
     auto key_tile = [&](int j) { return skipped + rank + j * p.split; };
     const int n = max(n0, n1);
 
-    constexpr uint32_t counts[fBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 8, 8, 8, 8, 1, 1, 1};
-    const uint32_t tmem = start_cta(sync, fBars, counts);
     auto bar = [&](int i) { return smem_address(&sync->bar[i]); };
     auto wait = [&](int i, uint32_t parity) { return barrier_wait(bar(i), parity, &sync->stop, p.timeouts); };
     const uint32_t sm_q = base, sm_k = base + 2 * kBytes, sm_v = base + 4 * kBytes;
@@ -421,29 +427,46 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
         const int pair = 1 + 4 * t + (warp & 3);                      // barrier of the two warps that share their rows
         float *mine = exchange + (2 * t + half) * kTile + r, *other = exchange + (2 * t + 1 - half) * kTile + r;
         const int seen = seen_by(p, w, i, mods.prefix), tile_seen = seen_by(p, w, q0 + t * kTile, mods.prefix);   // by its first row
-        const float unit = MODE > 0 ? 1.0f : p.scale_log2, natural = MODE > 0 ? kLn2 : p.scale;   // of the scores, in units of ln 2 and by themselves
+        // Scores that are biased are shaped in front of the maximum and kept in the products' place, in units of ln 2; a cap alone,
+        // which keeps the products' order, is taken on the way to the exponentials (`late`).
+        constexpr bool early = MODE > 1;
+        const bool late = MODE == 1 && p.scores.capped;
+        const float unit = early ? 1.0f : p.scale_log2, natural = early ? kLn2 : p.scale;   // of what the maximum is of
         int document = 0;
+        [[maybe_unused]] bool one_document = true;                    // of the warp's rows
         if constexpr (MODE > 0) {
-            if (mods.q_docs != nullptr && i < w.q_len) document = __ldg(mods.q_docs + i);
+            if (mods.q_docs != nullptr) {
+                document = __ldg(mods.q_docs + min(i, w.q_len - 1));
+                one_document = __all_sync(0xffffffffu, document == uniform(document));
+            }
         }
+        // the reference of the exponents, in units of ln 2
+        auto reference_of = [&](float high) { return MODE == 1 && late ? bend_one(p.scores, high) : high * unit; };
         float top = -INFINITY, sum = 0.0f;                            // of the raw products; the sum of this thread's columns
+        float shift = 0.0f;
         bool ok = true;
-        for (int j = 0; j < nt; ++j) {
-            int key_document[2] = {0, 0};                             // of this lane's key of each 32
+        // the documents of this lane's key of each 32 in the next tile, which wait for memory while this one is worked on
+        [[maybe_unused]] int next_document[2] = {0, 0};
+        auto load_documents = [&](int j) {
             if constexpr (MODE > 0) {
                 if (mods.k_docs != nullptr) {
 #pragma unroll
-                    for (int c = 0; c < 2; ++c) key_document[c] = __ldg(mods.k_docs + min(key_tile(j) * kTile + 64 * half + 32 * c + lane, w.k_len - 1));
+                    for (int c = 0; c < 2; ++c) next_document[c] = __ldg(mods.k_docs + min(key_tile(j) * kTile + 64 * half + 32 * c + lane, w.k_len - 1));
                 }
             }
+        };
+        if (nt > 0) load_documents(0);
+        for (int j = 0; j < nt; ++j) {
             ok = wait(fS + t, j & 1);                                 // (a wait given up ends the loop below, for all threads of the tile)
             fence_after();
+            [[maybe_unused]] const int key_document[2] = {next_document[0], next_document[1]};
+            if (j + 1 < nt) load_documents(j + 1);
             bool edge = (key_tile(j) + 1) * kTile > tile_seen;
             const int limit = seen - key_tile(j) * kTile - 64 * half;
             // Scores are read twice, 32 columns at a time, for the maximum and for the probabilities: reading them costs less
             // than holding 64 of them in registers.
             uint32_t s[32];
-            bool exact = MODE == 0 && edge;                           // some may be -inf, which the polynomial does not make 0
+            [[maybe_unused]] bool exact = edge;                       // some may be -inf, which the polynomial does not make 0
             auto read = [&](int c) {
                 tmem_ld32(s_at + 32 * c, s);
                 wait_ld(s);
@@ -452,37 +475,58 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
                     for (int e = 0; e < 32; ++e) s[e] = 32 * c + e < limit ? s[e] : 0xff800000u;
                 }
             };
-            // MODE 1: the scores take the products' place, with what is hidden already out, so that they are shaped once
-            auto shape = [&](int c) {
-                if constexpr (MODE > 0) {
-                    uint32_t none[16];
-                    const bool finite = shape_scores<false>(p.scores, mods, p.scale_log2, key_tile(j) * kTile + 64 * half + 32 * c - i - (w.k_len - w.q_len), s, none);
-                    uint32_t word = edge ? low_bits(limit - 32 * c) : 0xffffffffu;
-                    if (mods.k_docs != nullptr) word &= same_document(document, key_document[c]);
-                    const bool hides = __any_sync(0xffffffffu, word != 0xffffffffu);
-                    if (hides) {
+            // MODE > 0: whether the whole warp sees all 64 keys, else what each thread's row sees, a word for each 32
+            [[maybe_unused]] bool open = !edge;
+            [[maybe_unused]] uint32_t words[2] = {0xffffffffu, 0xffffffffu};
+            if constexpr (MODE > 0) {
+                if (mods.k_docs != nullptr) open = __all_sync(0xffffffffu, open && one_document && key_document[0] == document && key_document[1] == document);
+                if (!open) {
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) s[e] = word >> e & 1 ? s[e] : 0xff800000u;
+                    for (int c = 0; c < 2; ++c) {
+                        if (edge) words[c] = low_bits(limit - 32 * c);
+                        if (mods.k_docs != nullptr) words[c] &= same_document(document, key_document[c]);
                     }
-                    exact = exact || hides || !finite;
+                }
+                exact = !open;
+            }
+            [[maybe_unused]] float largest_of[2] = {0.0f, 0.0f};      // products
+            auto hide = [&](int c) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) s[e] = words[c] >> e & 1 ? s[e] : 0xff800000u;
+            };
+            auto prepare = [&](int c) {
+                if constexpr (early) {
+                    uint32_t none[16];
+                    const bool finite = shape_scores<MODE, false>(p.scores, mods, p.scale_log2, key_tile(j) * kTile + 64 * half + 32 * c - i - (w.k_len - w.q_len), s, none);
+                    exact = exact || !finite;
+                    if (!open) hide(c);
                     if (c == 0) {
                         tmem_st32(s_at, s);
                         wait_st();
                     }
+                } else if (late) {
+                    largest_of[c] = largest(s);
                 }
             };
             float best[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-            auto maximum = [&]() {
+            auto maximum = [&](int c) {
+                if (MODE == 1 && !open) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2)
+                        best[(e >> 1) & 3] = max3_nan(best[(e >> 1) & 3], words[c] >> e & 1 ? __uint_as_float(s[e]) : -INFINITY,
+                                                      words[c] >> (e + 1) & 1 ? __uint_as_float(s[e + 1]) : -INFINITY);
+                    return;
+                }
 #pragma unroll
                 for (int e = 0; e < 32; e += 2)                       // two at a time: a three-operand maximum
                     best[(e >> 1) & 3] = max3_nan(best[(e >> 1) & 3], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
             };
             read(0);
-            shape(0);
-            maximum();
+            prepare(0);
+            maximum(0);
             read(1);
-            shape(1);
-            maximum();
+            prepare(1);
+            maximum(1);
             const float high = max3_nan(max3_nan(best[0], best[1], best[2]), best[3], best[3]);
             // The sums' reference moves only when a product passes it by 2^8: until then probabilities up to 2^8
             // are held, which cost no precision, and O needs no rescaling.  The row's two threads move it together: whether
@@ -500,8 +544,9 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
                 const float row_high = max3_nan(high, *other, high);
                 const bool move = moves(row_high);
                 const float next = move ? row_high : top;
-                const float factor = move ? exp2_fast((top - next) * unit) : 1.0f;
+                const float factor = !move ? 1.0f : MODE == 1 && late ? exp2_fast(reference_of(top) - reference_of(next)) : exp2_fast((top - next) * unit);
                 top = next;
+                if (MODE == 1) shift = top == -INFINITY ? 0.0f : -reference_of(top);
                 sum *= factor;
                 if (j > 0) {
                     ok = wait(fO + t, (j - 1) & 1);
@@ -521,13 +566,34 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
                     }
                 }
             }
-            const float shift = top == -INFINITY ? 0.0f : -top * unit;
+            if (MODE != 1) shift = top == -INFINITY ? 0.0f : -top * unit;
             float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
             for (int c = 1; c >= 0; --c) {                            // (columns 32 to 63 are still there)
                 if (c == 0) read(0);
-                if (exact) fwd_probabilities<T, false>(s, unit, shift, part, s_at + 32 * c);
-                else fwd_probabilities<T, true>(s, unit, shift, part, s_at + 32 * c);
+                if (MODE == 1 && (late || !open)) {                   // exponents first, so that what is hidden is hidden in them
+                    if (late) {
+                        bend<1, true>(p.scores, largest_of[c], s, shift);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 32; e += 2) {
+                            float a, b;
+                            fma2(a, b, __uint_as_float(s[e]), __uint_as_float(s[e + 1]), unit, unit, shift, shift);
+                            s[e] = __float_as_uint(a);
+                            s[e + 1] = __float_as_uint(b);
+                        }
+                    }
+                    if (open) {
+                        fwd_probabilities<T, true, true>(s, unit, shift, part, s_at + 32 * c);
+                    } else {
+                        hide(c);
+                        fwd_probabilities<T, false, true>(s, unit, shift, part, s_at + 32 * c);
+                    }
+                } else if (exact) {
+                    fwd_probabilities<T, false>(s, unit, shift, part, s_at + 32 * c);
+                } else {
+                    fwd_probabilities<T, true>(s, unit, shift, part, s_at + 32 * c);
+                }
                 wait_st();
                 fence_before();
                 __syncwarp();
@@ -556,7 +622,7 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
             } else if (live && half == 0) {
                 zero_columns<T>(row, p.dim);
             }
-            if (live && half == 0) p.lse[stat_of(p, w, w.head, i)] = sum == 0.0f ? -INFINITY : top * natural + logf(sum);
+            if (live && half == 0) p.lse[stat_of(p, w, w.head, i)] = sum == 0.0f ? -INFINITY : (MODE == 1 && late ? reference_of(top) * kLn2 : top * natural) + logf(sum);
         } else {
             // Every CTA lays its O, reference and sum of each row out in shared memory, [row tile][column][row]; a share of the
             // columns is brought to the largest reference, added up and divided by each.
@@ -574,20 +640,21 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
                     asm volatile("st.shared.u32 [%0], %1;" :: "r"(mine_o + (half * (DIM / 2) + 32 * c + e) * (kTile * 4)), "r"(nt > 0 ? o[e] : 0u) : "memory");
             }
             if (half == 0) {
-                joined[2 * t * kTile + r] = top;
+                joined[2 * t * kTile + r] = MODE == 1 && late && top > -INFINITY ? reference_of(top) : top;
                 joined[(2 * t + 1) * kTile + r] = sum;
             }
             cluster_sync();
             float high = -INFINITY, total = 0.0f;
+            const float joined_unit = MODE == 1 && late ? 1.0f : unit;
             for (int k = 0; k < p.split; ++k) high = fmaxf(high, load_peer(mine_stat, k));
-            const float reference = high == -INFINITY ? 0.0f : high * unit;
-            for (int k = 0; k < p.split; ++k) total += exp2_fast(load_peer(mine_stat, k) * unit - reference) * load_peer(mine_stat + kTile * 4, k);
+            const float reference = high == -INFINITY ? 0.0f : high * joined_unit;
+            for (int k = 0; k < p.split; ++k) total += exp2_fast(load_peer(mine_stat, k) * joined_unit - reference) * load_peer(mine_stat + kTile * 4, k);
             const float factor = total > 0.0f || total != total ? 1.0f / total : 0.0f;
             const int share = DIM / p.split;                          // a multiple of 16
             for (int col = rank * share + half * (share / 2); col < rank * share + (half + 1) * (share / 2); col += 8) {
                 float v[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
                 for (int k = 0; k < p.split; ++k) {
-                    const float weight = exp2_fast(load_peer(mine_stat, k) * unit - reference);
+                    const float weight = exp2_fast(load_peer(mine_stat, k) * joined_unit - reference);
                     float x[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) x[e] = load_peer(mine_o + (col + e) * (kTile * 4), k);
@@ -599,7 +666,7 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
                 for (int e = 0; e < 8; ++e) o[e] = __float_as_uint(v[e]);
                 if (live) store_columns<T, 8>(row, col, p.dim, o, factor);
             }
-            if (live && half == 0 && rank == 0) p.lse[stat_of(p, w, w.head, i)] = total == 0.0f ? -INFINITY : high * natural + logf(total);
+            if (live && half == 0 && rank == 0) p.lse[stat_of(p, w, w.head, i)] = total == 0.0f ? -INFINITY : high * (MODE == 1 && late ? kLn2 : natural) + logf(total);
             cluster_sync();                                           // nobody's shared memory goes before it has been read
         }
     }
@@ -644,17 +711,12 @@ attention_dq_kernel(const __grid_constant__ Params p) {
     const int kv_head = w.head / p.group;
     // key tiles that the rows see, and how many of them fall to this CTA: number rank, rank + split, ...
     const Mods mods = find_mods<MODE>(p, w, w.head);
-    int all = key_tiles(p, w, min(q0 + kTile, w.q_len) - 1, mods.prefix), skipped = 0;
-    if constexpr (MODE > 0) {
-        if (mods.q_docs != nullptr) {
-            const int2 tiles = shared_tiles(mods.q_docs, q0, min(q0 + kTile, w.q_len), mods.k_docs, w.k_len, all, reinterpret_cast<int *>(row_sum + 4 * kTile));
-            skipped = tiles.x;
-            all = max(0, tiles.y - skipped);
-        }
-    }
-    const int n_all = uniform(all);
-    const int n = share_of(n_all, rank, p.split);
+    const bool documents = MODE > 0 && mods.q_docs != nullptr;
+    int n_all = uniform(key_tiles(p, w, min(q0 + kTile, w.q_len) - 1, mods.prefix)), skipped = 0;
+    int n = share_of(n_all, rank, p.split);
     auto key_tile = [&](int j) { return skipped + rank + j * p.split; };
+    int2 *const scanned = reinterpret_cast<int2 *>(row_sum + 4 * kTile);
+    if (documents) scan_tiles<4>(mods.q_docs, q0, min(q0 + kTile, w.q_len), mods.k_docs, w.k_len, n_all, scanned);
 
     // The outputs that delta needs, read while the CTA sets itself up: DIM / 8 lanes a row, 8 rows for each warp.  (From here on
     // the L2's bandwidth is the tiles' that are on their way.)
@@ -663,7 +725,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
     float lse = -INFINITY;
     if (warp < kMmaWarp) {
 #pragma unroll
-        for (int x = 0; n > 0 && n_all > 1 && x < 8 / kRows; ++x) {
+        for (int x = 0; n > 0 && n_all > 1 && x < 8 / kRows; ++x) {   // (with documents there may be fewer)
             const int row = q0 + 8 * warp + kRows * x + lane / kLanes, col = lane % kLanes * 8;
             const bool there = row < w.q_len && col < p.dim;
             const T *from = static_cast<const T *>(p.o.p) + row_of(w, p.o, w.head, there ? row : 0, w.q_first) + (there ? col : 0);
@@ -675,6 +737,12 @@ attention_dq_kernel(const __grid_constant__ Params p) {
 
     constexpr uint32_t counts[qBars] = {1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 16, 1};
     const uint32_t tmem = start_cta(sync, qBars, counts);
+    if (documents) {
+        const int2 tiles = scanned_tiles(scanned);
+        skipped = tiles.x;
+        n_all = uniform(tiles.y - skipped);
+        n = share_of(n_all, rank, p.split);
+    }
     auto bar = [&](int i) { return smem_address(&sync->bar[i]); };
     auto wait = [&](int i, uint32_t parity) { return barrier_wait(bar(i), parity, &sync->stop, p.timeouts); };
     const uint32_t sm_q = base, sm_g = base + kBytes, sm_k = base + 2 * kBytes, sm_v = base + 5 * kBytes;
@@ -682,7 +750,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
     const uint32_t tm_s = tmem, tm_dp = tmem + 2 * kTile, tm_dq = tmem + 3 * kTile;
 
     if (warp >= kMmaWarp) {
-        give_registers<kDqIssue>();
+        give_registers<MODE == 0 ? kDqIssue : kFwdIssue>();
         if (warp == kLoadWarp) {
             int issued_k = 0, issued_v = 0;
             if (n > 0 && lane == 0) {
@@ -752,7 +820,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             cluster_sync();
         }
     } else {
-        take_registers<kDqWork>();
+        take_registers<MODE == 0 ? kDqWork : kFwdWork>();
         const int part = warp >> 2;                                   // columns [32 part, 32 part + 32) of every tile
         const int r = threadIdx.x & 127, i = q0 + r;
         const bool live = i < w.q_len;
@@ -787,23 +855,29 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             return (row_sum[r] + row_sum[kTile + r]) + (row_sum[2 * kTile + r] + row_sum[3 * kTile + r]);
         };
         const int seen = seen_by(p, w, i, mods.prefix), tile_seen = seen_by(p, w, q0, mods.prefix);
-        const float unit = MODE > 0 ? 1.0f : p.scale_log2;            // of the scores, in units of ln 2
+        const bool shaped = MODE > 1 || (MODE == 1 && p.scores.capped);
+        const float unit = shaped ? 1.0f : p.scale_log2;              // of the scores, in units of ln 2
         int document = 0, visible = 0;                                // with documents: how many keys the row sees here
+        [[maybe_unused]] bool one_document = true;                    // of the warp's rows
         if constexpr (MODE > 0) {
-            if (mods.q_docs != nullptr && live) document = __ldg(mods.q_docs + i);
+            if (mods.q_docs != nullptr) {
+                document = __ldg(mods.q_docs + min(i, w.q_len - 1));
+                one_document = __all_sync(0xffffffffu, document == uniform(document));
+            }
         }
+        // of this lane's key in the next tile, which waits for memory while this one is worked on
+        auto document_of = [&](int j) { return MODE > 0 && mods.k_docs != nullptr ? __ldg(mods.k_docs + min(key_tile(j) * kTile + 32 * part + lane, w.k_len - 1)) : 0; };
+        [[maybe_unused]] int next_document = n > 0 ? document_of(0) : 0;
         for (int j = 0; ok && j < n; ++j) {
             const uint32_t s_at = tm_s + (j & 1) * kTile + 32 * part + my_lane;
-            int key_document = 0;
-            if constexpr (MODE > 0) {
-                if (mods.k_docs != nullptr) key_document = __ldg(mods.k_docs + min(key_tile(j) * kTile + 32 * part + lane, w.k_len - 1));
-            }
             ok = wait(qS + (j & 1), (j >> 1) & 1);
             if (!ok) {
                 if (single) over_parts(0.0f);                         // the others wait there
                 break;
             }
             fence_after();
+            [[maybe_unused]] const int key_document = next_document;
+            if (j + 1 < n) next_document = document_of(j + 1);
             uint32_t s[32], d[32], out[16];
             uint32_t bent[16];                                        // MODE 1, capped: 1 - t^2
             float prob[32];
@@ -812,22 +886,21 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             bool edge = (key_tile(j) + 1) * kTile > tile_seen;
             const int limit = seen - key_tile(j) * kTile - 32 * part;           // places from here on the row does not see, whatever they hold
             uint32_t word = 0xffffffffu;
-            bool finite = true;
             auto sees = [&](int c) { return MODE > 0 ? (word >> c & 1) != 0 : c < limit; };
             if constexpr (MODE > 0) {
-                finite = shape_scores<true>(p.scores, mods, p.scale_log2, key_tile(j) * kTile + 32 * part - i - (w.k_len - w.q_len), s, bent);
+                if (shaped) shape_scores<MODE, true>(p.scores, mods, p.scale_log2, key_tile(j) * kTile + 32 * part - i - (w.k_len - w.q_len), s, bent);
                 if (edge) word = low_bits(limit);
                 if (mods.k_docs != nullptr) {
-                    word &= same_document(document, key_document);
+                    if (!(one_document && __all_sync(0xffffffffu, key_document == document))) word &= same_document(document, key_document);
                     visible += __popc(word);
                 }
                 edge = __any_sync(0xffffffffu, word != 0xffffffffu);
             }
-            if (edge || !finite) {
+            if (MODE > 0 || edge) {
 #pragma unroll
                 for (int c = 0; c < 32; c += 2)
                     exp2_scaled<false>(prob[c], prob[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), unit, minus_lse, minus_lse);
-                if constexpr (MODE > 0) {                             // (what a document hides may be larger than the row's sum)
+                if (MODE > 0 && edge) {                               // (what a document hides may be larger than the row's sum)
 #pragma unroll
                     for (int c = 0; c < 32; ++c) prob[c] = sees(c) ? prob[c] : 0.0f;
                 }
@@ -893,7 +966,6 @@ attention_dq_kernel(const __grid_constant__ Params p) {
         // A row of one key has P = 1 and dS = 0 whatever its score: what the recomputed P leaves of dS is rounding and nothing
         // else.  (Times 0: a NaN stays one.)
         bool one = seen == 1;
-        const bool documents = MODE > 0 && mods.q_docs != nullptr;
         if (documents) {                                              // as many as its four threads found, in all CTAs of the cluster
             asm volatile("bar.sync 1, %0;" :: "n"(kWorkThreads) : "memory");   // (the sums above have been read)
             const float found = over_parts(static_cast<float>(visible));
@@ -1007,13 +1079,13 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
         return;
     }
     const int k0 = w.tile * kTile;
-    // MODE 2: places of this key tile for the sums by distance, one for each query head of the group
+    // MODE 3: places of this key tile for the sums by distance, one for each query head of the group
     auto place_of = [&](int head) { return (static_cast<long long>(w.batch) * p.heads + head) * p.tiles + w.tile; };
     auto far_of = [&](int head) { return p.scores.far + place_of(head) * kFarFloats + rank * 32 + warp * 2; };
-    if (MODE == 2 && warp < kMmaWarp && lane < 2)
+    if (MODE == 3 && warp < kMmaWarp && lane < 2)
         for (int h = 0; h < p.group; ++h) far_of(w.head * p.group + h)[lane] = 0.0f;
     if (k0 >= w.k_len) {
-        if (MODE == 2 && rank == 0)
+        if (MODE == 3 && rank == 0)
             for (int h = threadIdx.x; h < p.group; h += kThreadsAttn) p.scores.written[place_of(w.head * p.group + h)] = make_int4(0, 0, 0, 0);
         pdl_wait();
         return;
@@ -1023,18 +1095,11 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
     const int reach = w.k_len - w.q_len;                              // row i sees keys up to i + reach
     Mods mods = find_mods<MODE>(p, w, w.head * p.group);
     int first_tile = p.causal && k0 >= mods.prefix ? max(0, k0 - reach) / kTile : 0, last_tile = (w.q_len + kTile - 1) / kTile;
-    if constexpr (MODE > 0) {
-        if (mods.q_docs != nullptr) {
-            const int2 tiles = shared_tiles(mods.k_docs, k0, min(k0 + kTile, w.k_len), mods.q_docs, w.q_len, last_tile, reinterpret_cast<int *>(sync + 1));
-            first_tile = max(first_tile, tiles.x);
-            last_tile = tiles.y;
-        }
-    }
-    const int first = first_tile;
-    const int each = max(0, last_tile - first);
-    const int n = uniform(share_of(each * p.group, rank, p.split));
-    if (MODE == 2 && rank == 0)
-        for (int h = threadIdx.x; h < p.group; h += kThreadsAttn) p.scores.written[place_of(w.head * p.group + h)] = make_int4(first, first + each, reach, 0);
+    const bool documents = MODE > 0 && mods.q_docs != nullptr;
+    int2 *const scanned = reinterpret_cast<int2 *>(sync + 1);
+    if (documents) scan_tiles<4>(mods.k_docs, k0, min(k0 + kTile, w.k_len), mods.q_docs, w.q_len, last_tile, scanned);
+    int first = first_tile, each = max(0, last_tile - first);
+    int n = uniform(share_of(each * p.group, rank, p.split));
 
     // a quarter of a row of the K tile for each thread, read while the CTA sets itself up
     uint32_t keys[DIM / 8];
@@ -1050,6 +1115,14 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
 
     constexpr uint32_t counts[kBars] = {1, 16, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 1, 16, 16, 1, 16, 1, 16, 16, 1, 16, 1, 1};
     const uint32_t tmem = start_cta(sync, kBars, counts);
+    if (documents) {
+        const int2 tiles = scanned_tiles(scanned);
+        first = max(first_tile, tiles.x);
+        each = max(0, tiles.y - first);
+        n = uniform(share_of(each * p.group, rank, p.split));
+    }
+    if (MODE == 3 && rank == 0)
+        for (int h = threadIdx.x; h < p.group; h += kThreadsAttn) p.scores.written[place_of(w.head * p.group + h)] = make_int4(first, first + each, reach, 0);
     auto bar = [&](int i) { return smem_address(&sync->bar[i]); };
     auto wait = [&](int i, uint32_t parity) { return barrier_wait(bar(i), parity, &sync->stop, p.timeouts); };
     const uint32_t sm_v = base, sm_q = base + kBytes, sm_g = base + 4 * kBytes;
@@ -1187,7 +1260,13 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                 one_document = __all_sync(0xffffffffu, d == uniform(d));
             }
         }
-        // MODE 2: this thread's sums of the scores' gradients further behind and further ahead than the table reaches
+        // of this lane's row of the warp's 32 in the next tile, which waits for memory while this one is worked on
+        auto document_of = [&](int of) { return documents ? __ldg(mods.q_docs + min((first + of) * kTile + 32 * part + lane, w.q_len - 1)) : 0; };
+        [[maybe_unused]] int next_document = 0;
+        if constexpr (MODE > 0) {
+            if (n > 0) next_document = document_of(rank % each);
+        }
+        // MODE 3: this thread's sums of the scores' gradients further behind and further ahead than the table reaches
         [[maybe_unused]] float behind = 0.0f, ahead = 0.0f;
         [[maybe_unused]] auto write_far = [&]() {
 #pragma unroll
@@ -1201,17 +1280,21 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
         for (int j = 0; j < n; ++j, tile += p.split) {
             while (tile >= each) {                                    // the next head
                 tile -= each;
-                if constexpr (MODE == 2) write_far();
-                if constexpr (MODE > 0) {
+                if constexpr (MODE == 3) write_far();
+                if constexpr (MODE > 1) {
                     ++head;
                     if (p.scores.bias != nullptr) mods.bias += 2 * p.scores.reach + 1;
                     if (p.scores.slopes != nullptr) mods.slope = -uniform(__ldg(p.scores.slopes + head)) * kLog2e;
                 }
             }
             const int q0 = (first + tile) * kTile;
-            [[maybe_unused]] int row_document = 0;                    // of this lane's row of the warp's 32
+            [[maybe_unused]] const int row_document = next_document;
             if constexpr (MODE > 0) {
-                if (mods.q_docs != nullptr) row_document = __ldg(mods.q_docs + min(q0 + 32 * part + lane, w.q_len - 1));
+                if (documents && j + 1 < n) {
+                    int next = tile + p.split;
+                    while (next >= each) next -= each;
+                    next_document = document_of(next);
+                }
             }
             // A thread holds 8 rows' values for each of 4 keys, not 32 rows' for one: the statistics that it reads are a quarter.
             // They are read before the scores are there: afterwards dP's product, whose operands both lie in shared memory,
@@ -1237,10 +1320,12 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             [[maybe_unused]] const int away = key - q0 - 32 * part - 2 * (lane % 4) - reach;   // distance of the first key and row
             [[maybe_unused]] const int least = k0 + 32 * (warp & 3) - q0 - 32 * part - reach - 31;   // of the warp's last row and first key
             float unit = p.scale_log2;
-            bool plain = true;
+            [[maybe_unused]] bool open = true, finite = true;         // the whole warp sees all its keys; tables may hold -inf
             if constexpr (MODE > 0) {
-                plain = shape_transposed(p.scores, mods, p.scale_log2, away, least, s, bent);
-                unit = 1.0f;
+                if (MODE > 1 || p.scores.capped) {
+                    finite = shape_transposed<MODE>(p.scores, mods, p.scale_log2, away, least, s, bent);
+                    unit = 1.0f;
+                }
                 uint32_t word = 0xffffffffu;                          // a bit for each value, in their order
                 if (p.causal && k0 + kTile - 1 > q0 + reach && k0 + kTile > mods.prefix) {
 #pragma unroll
@@ -1271,14 +1356,14 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                         }
                     }
                 }
-                if (__any_sync(0xffffffffu, word != 0xffffffffu)) {
-                    plain = false;
+                open = __all_sync(0xffffffffu, word == 0xffffffffu);
+                if (!open) {
 #pragma unroll
                     for (int x = 0; x < 32; ++x) s[x] = word >> x & 1 ? s[x] : 0xff800000u;
                 }
             }
             const bool diagonal = MODE == 0 && p.causal && k0 + kTile - 1 > q0 + reach;   // some rows do not see some keys
-            if (diagonal || !plain) {
+            if (diagonal || !open || !finite) {
                 [[maybe_unused]] const int from = key - reach - q0 - 32 * part - 2 * (lane % 4);   // of the first of the 4 keys, which are 8 apart
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
@@ -1307,7 +1392,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             }
 #pragma unroll
             for (int c = 0; c < 16; ++c) out[c] = pack2<T>(prob[2 * c], prob[2 * c + 1]);
-            if constexpr (MODE == 1) {                                // from here on only dS of the products is wanted
+            if constexpr (MODE == 1 || MODE == 2) {                    // from here on only dS of the products is wanted
                 if (p.scores.capped) {
 #pragma unroll
                     for (int c = 0; c < 16; ++c) {
@@ -1334,7 +1419,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             ok = wait(kDp, j & 1);
             if (!ok) break;
             fence_after();
-            [[maybe_unused]] float diagonals[7][2] = {};              // MODE 2: sums of dS by (key - row) / 8 and the row's parity
+            [[maybe_unused]] float diagonals[7][2] = {};              // MODE 3: sums of dS by (key - row) / 8 and the row's parity
 #pragma unroll
             for (int h = 0; h < 2; ++h) {                             // 16 keys at a time
                 uint32_t d[16];
@@ -1349,12 +1434,13 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                         float v0, v1;
                         add2(v0, v1, __uint_as_float(d[x]), __uint_as_float(d[x + 1]), e.x, e.y);
                         mul2(v0, v1, v0, v1, prob[16 * h + x], prob[16 * h + x + 1]);
-                        if constexpr (MODE == 2) {
-                            // (a hidden key's gradient is 0 whatever its values hold)
-                            v0 = prob[16 * h + x] == 0.0f ? 0.0f : v0;
-                            v1 = prob[16 * h + x + 1] == 0.0f ? 0.0f : v1;
-                            diagonals[2 * h + k - c + 3][0] += v0;
-                            diagonals[2 * h + k - c + 3][1] += v1;
+                        if constexpr (MODE == 3) {
+                            if (!open) {                              // a hidden key's gradient is 0 whatever its values hold
+                                v0 = prob[16 * h + x] == 0.0f ? 0.0f : v0;
+                                v1 = prob[16 * h + x + 1] == 0.0f ? 0.0f : v1;
+                            }
+                            float(&sum)[2] = diagonals[2 * h + k - c + 3];
+                            add2(sum[0], sum[1], sum[0], sum[1], v0, v1);
                             if (p.scores.capped) {
                                 const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&bent[8 * h + x / 2]));
                                 mul2(v0, v1, v0, v1, f.x, f.y);
@@ -1367,7 +1453,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             fence_before();
             __syncwarp();
             if (lane == 0) barrier_arrive(bar(kDpRead));
-            if constexpr (MODE == 2) {
+            if constexpr (MODE == 3) {
                 const int far = beyond(least, p.scores.reach), nearest = max(0, first_near(k0, reach, p.scores.reach)), at = first + tile - nearest;
                 if (far != 0) {
                     float sum = 0.0f;
@@ -1405,7 +1491,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
         }
         if (ok) ok = wait(kDone, 0);
         if (stopped(sync)) ok = false;                                // (kDone comes in any case)
-        if constexpr (MODE == 2) {
+        if constexpr (MODE == 3) {
             if (n > 0) {
                 if (!ok) behind = ahead = NAN;                        // given up: the bias's gradient says so
                 write_far();

@@ -49,41 +49,42 @@ cudaError_t launch(const Params &p, unsigned grid, unsigned cluster, cudaStream_
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
+template <int DIM, int MODE>
+cudaError_t launch_one(Kernel which, const Params &p, unsigned grid, cudaStream_t st) {
+    switch (which) {
+    case Kernel::forward: return launch<attention_fwd_kernel<T, DIM, MODE>, fwd_smem<DIM>()>(p, grid * p.split, p.split, st);
+    case Kernel::dq: return launch<attention_dq_kernel<T, DIM, MODE>, dq_smem<DIM>()>(p, grid * p.split, p.split, st);
+    default:
+        if constexpr (MODE == 2) {
+            if (which == Kernel::dkv_bias) return launch<attention_dkv_kernel<T, DIM, 3>, dkv_smem<DIM>()>(p, grid * p.split, p.split, st);
+        }
+        return launch<attention_dkv_kernel<T, DIM, MODE>, dkv_smem<DIM>()>(p, grid * p.split, p.split, st);
+    }
+}
+
 }  // namespace
 
 #if FEWBIT_ATTN_SCORES
-constexpr int kMode = 1;
 #if FEWBIT_ATTN_F16
 cudaError_t launch_scores_f16(
 #else
 cudaError_t launch_scores_bf16(
 #endif
+    Kernel which, bool wide, const Params &p, unsigned grid, cudaStream_t st) {
+    const bool biased = p.scores.slopes != nullptr || p.scores.bias != nullptr;
+    if (biased) return wide ? launch_one<128, 2>(which, p, grid, st) : launch_one<64, 2>(which, p, grid, st);
+    return wide ? launch_one<128, 1>(which, p, grid, st) : launch_one<64, 1>(which, p, grid, st);
+}
 #else
-constexpr int kMode = 0;
 #if FEWBIT_ATTN_F16
 cudaError_t launch_f16(
 #else
 cudaError_t launch_bf16(
 #endif
-#endif
     Kernel which, bool wide, const Params &p, unsigned grid, cudaStream_t st) {
-    switch (which) {
-    case Kernel::forward:
-        return wide ? launch<attention_fwd_kernel<T, 128, kMode>, fwd_smem<128>()>(p, grid * p.split, p.split, st)
-                    : launch<attention_fwd_kernel<T, 64, kMode>, fwd_smem<64>()>(p, grid * p.split, p.split, st);
-    case Kernel::dq:
-        return wide ? launch<attention_dq_kernel<T, 128, kMode>, dq_smem<128>()>(p, grid * p.split, p.split, st)
-                    : launch<attention_dq_kernel<T, 64, kMode>, dq_smem<64>()>(p, grid * p.split, p.split, st);
-#if FEWBIT_ATTN_SCORES
-    case Kernel::dkv_bias:
-        return wide ? launch<attention_dkv_kernel<T, 128, 2>, dkv_smem<128>()>(p, grid * p.split, p.split, st)
-                    : launch<attention_dkv_kernel<T, 64, 2>, dkv_smem<64>()>(p, grid * p.split, p.split, st);
-#endif
-    default:
-        return wide ? launch<attention_dkv_kernel<T, 128, kMode>, dkv_smem<128>()>(p, grid * p.split, p.split, st)
-                    : launch<attention_dkv_kernel<T, 64, kMode>, dkv_smem<64>()>(p, grid * p.split, p.split, st);
-    }
+    return wide ? launch_one<128, 0>(which, p, grid, st) : launch_one<64, 0>(which, p, grid, st);
 }
+#endif
 
 }  // namespace attn
 }  // namespace fewbit

@@ -12,10 +12,10 @@ namespace {
 // ---------------------------------------------------------------------------------------------------
 // the attention's gradient by distance
 // ---------------------------------------------------------------------------------------------------
-// A CTA takes 32 distances of one head, a lane each; its warps share the key tiles.  Each pair of tiles holds a warp's sums
+// A CTA takes 32 distances of one head, a lane each; its warps share the pairs of tiles.  Each pair of tiles holds a warp's sums
 // over 32 x 32 pieces, 64 distances apiece; up to 8 of the 16 pieces have a given one.  The last CTA of a head adds up what
 // lies at and beyond the table's ends.  No atomics: the order is fixed.
-constexpr int kGradThreads = 512, kGradWarps = kGradThreads / 32;
+constexpr int kGradThreads = 1024, kGradWarps = kGradThreads / 32, kGradTogether = 4;
 
 __global__ void __launch_bounds__(kGradThreads)
 bias_gradient_kernel(Scores sc, int batch, int heads, int tiles, int split, int groups, float *grad) {
@@ -45,19 +45,29 @@ bias_gradient_kernel(Scores sc, int batch, int heads, int tiles, int split, int 
     }
     const int first = -sc.reach + 1 + 32 * static_cast<int>(blockIdx.x), d = first + lane;
     float sum = 0.0f;
-    for (int item = warp; item < items; item += kGradWarps) {
-        const long long place = place_of(item);
-        const int4 written = sc.written[place];
-        const int k0 = item % tiles * kTile, reach = written.z, nearest = max(0, first_near(k0, reach, sc.reach));
-        // row tiles with a pair at one of these distances
-        const int least = max(max(written.x, nearest), first_near(k0, reach, first + 32));
-        for (int t = least; t < min(written.y, nearest + sc.near_tiles) && t * kTile <= k0 - reach + 127 - first; ++t) {
-            const float *from = sc.near + (place * sc.near_tiles + t - nearest) * kNearFloats;
-            const int at = d - (k0 - t * kTile - reach) + 32;         // in a piece on the diagonal
+    // up to 3 row tiles of a key tile have a pair at one of these distances; four such pairs of tiles wait for memory together
+    for (long long at0 = warp; at0 < 3ll * items; at0 += kGradTogether * kGradWarps) {
+        int4 written[kGradTogether];
+        long long place[kGradTogether];
+        int item[kGradTogether];
+#pragma unroll
+        for (int i = 0; i < kGradTogether; ++i) {
+            item[i] = static_cast<int>(min((at0 + i * kGradWarps) / 3, items - 1ll));
+            place[i] = place_of(item[i]);
+            written[i] = sc.written[place[i]];
+        }
+#pragma unroll
+        for (int i = 0; i < kGradTogether; ++i) {
+            const long long at = at0 + i * kGradWarps;
+            const int k0 = item[i] % tiles * kTile, reach = written[i].z, nearest = max(0, first_near(k0, reach, sc.reach));
+            const int t = max(max(written[i].x, nearest), first_near(k0, reach, first + 32)) + static_cast<int>(at % 3);
+            const bool there = at < 3ll * items && t < min(written[i].y, nearest + sc.near_tiles) && t * kTile <= k0 - reach + 127 - first;
+            const float *from = sc.near + (place[i] * sc.near_tiles + (there ? t - nearest : 0)) * kNearFloats;
+            const int u0 = d - (k0 - t * kTile - reach) + 32;         // in a piece on the diagonal
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
-                const int u = at - 32 * (k & 3) + 32 * (k >> 2);
-                if (u >= 0 && u < 64) sum += from[k * 64 + u];
+                const int u = u0 - 32 * (k & 3) + 32 * (k >> 2);
+                sum += there && u >= 0 && u < 64 ? from[k * 64 + u] : 0.0f;
             }
         }
     }

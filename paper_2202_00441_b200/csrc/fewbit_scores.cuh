@@ -5,14 +5,18 @@
 //   z = c s log2 e,  or  cap tanh(c s / cap) log2 e;   z -= slope |d| log2 e;   z += B[clamp(d)] log2 e
 // and backward, with t the tanh: dS = dZ (1 - t^2), dB[e] = sum of dZ over all pairs at distance e.
 //
-// tanh: where no product of a warp's piece passes the cap itself, an odd polynomial of degree 11 (relative error 6e-7 on [-1, 1],
-// found by Lawson's reweighted least squares) on the FMA pipe, which has room; two results of the exponential unit otherwise.
-// (tanh.approx.f32 has 11 bits: with a cap of 50 a score would be off by 0.02.)
+// tanh: an odd polynomial of the product, scale and cap folded into its coefficients: of degree 5 where no product of a warp's 32 x 32
+// piece passes 0.3 caps (relative error 1.1e-6), of degree 11 up to the cap itself (6e-7), both found by Lawson's reweighted least
+// squares; two results of the exponential unit otherwise.  FMA and exponential pipe are what bounds the capped kernels: the
+// polynomials take 4 and 7 multiplications an element.  (tanh.approx.f32 has 11 bits: with a cap of 50 a score would be off by 0.02.)
 // Bias: a warp works on 32 rows x 32 keys; where all of them lie further apart than the table reaches, the bias is one number,
 // else each element's is read, 32 neighbouring ones at a time.
 // Documents: a lane holds the document of one key, and each document among a warp's 32 keys (mostly one or two) becomes one
 // word of votes.  Tiles in front of the first and behind the last that shares a document with the CTA's own are skipped.
 #pragma once
+
+#include <climits>
+#include <type_traits>
 
 #include "fewbit_tensor_core.cuh"
 
@@ -23,6 +27,9 @@ using namespace tc;
 
 struct Scores {
     float cap_in, cap_out;            // scale / cap, cap * log2(e)
+    float cap_out_2;                  // cap_out^-2
+    float near_odd[3], odd[6];        // capped scores of products up to near_limit and odd_limit: s Q(s^2), in units of ln 2
+    float near_limit, odd_limit;
     const float *slopes, *bias;
     int reach;                        // the table's largest distance
     const int *prefix, *q_docs, *k_docs;
@@ -54,138 +61,137 @@ __device__ __forceinline__ float tanh_wide(float a) {                 // absolut
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + exp2_fast(2.885390081777927f * a)));
     return fmaf(-2.0f, r, 1.0f);
 }
-// (t0, t1) = tanh(a0, a1) for magnitudes up to 1
-__device__ __forceinline__ void tanh_small(float &t0, float &t1, float a0, float a1) {
-    float y0, y1, p0, p1;
-    mul2(y0, y1, a0, a1, a0, a1);
-    fma2(p0, p1, y0, y1, -0.0030670601408928633f, -0.0030670601408928633f, 0.016743114218115807f, 0.016743114218115807f);
-    fma2(p0, p1, p0, p1, y0, y1, -0.051605671644210815f, -0.051605671644210815f);
-    fma2(p0, p1, p0, p1, y0, y1, 0.13281433284282684f, 0.13281433284282684f);
-    fma2(p0, p1, p0, p1, y0, y1, -0.3332904279232025f, -0.3332904279232025f);
-    fma2(p0, p1, p0, p1, y0, y1, 0.9999994039535522f, 0.9999994039535522f);
-    mul2(t0, t1, p0, p1, a0, a1);
-}
+// One product's capped score.
+__device__ __forceinline__ float bend_one(const Scores &sc, float s) { return tanh_wide(s * sc.cap_in) * sc.cap_out; }
 __device__ __forceinline__ float abs_max3(float a, float b, float c) {
     float d;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(fabsf(b)), "f"(fabsf(c)));
     return d;
 }
-
-// 32 products, in registers, to tanh(c s / cap), two neighbouring ones at a time.
-__device__ __forceinline__ void bend(float cap_in, uint32_t (&s)[32]) {
-    float high = 0.0f;
+__device__ __forceinline__ float largest(const uint32_t (&s)[32]) {   // magnitude
+    float high[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int e = 0; e < 32; e += 2) {
-        float a, b;
-        mul2(a, b, __uint_as_float(s[e]), __uint_as_float(s[e + 1]), cap_in, cap_in);
-        high = abs_max3(high, a, b);
-        s[e] = __float_as_uint(a);
-        s[e + 1] = __float_as_uint(b);
-    }
-    if (__any_sync(0xffffffffu, high > 1.0f)) {
-#pragma unroll
-        for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(tanh_wide(__uint_as_float(s[e])));
-    } else {
+    for (int e = 0; e < 32; e += 2) high[e / 2 % 2] = abs_max3(high[e / 2 % 2], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
+    return fmaxf(high[0], high[1]);
+}
+// 32 products to capped scores plus `add`, with the shortest form that the warp's largest product (`high`) allows.
+template <int MODE, bool ADD>
+__device__ __forceinline__ void bend(const Scores &sc, float high, uint32_t (&s)[32], float add) {
+    auto odd = [&](auto degree, const float *c) {                     // s Q(s^2)
+        constexpr int N = decltype(degree)::value;
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
-            float a, b;
-            tanh_small(a, b, __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
-            s[e] = __float_as_uint(a);
-            s[e + 1] = __float_as_uint(b);
+            const float a = __uint_as_float(s[e]), b = __uint_as_float(s[e + 1]);
+            float y0, y1, q0, q1;
+            mul2(y0, y1, a, b, a, b);
+            fma2(q0, q1, y0, y1, c[N], c[N], c[N - 1], c[N - 1]);
+#pragma unroll
+            for (int k = N - 2; k >= 0; --k) fma2(q0, q1, q0, q1, y0, y1, c[k], c[k]);
+            if (ADD) fma2(q0, q1, q0, q1, a, b, add, add);
+            else mul2(q0, q1, q0, q1, a, b);
+            s[e] = __float_as_uint(q0);
+            s[e + 1] = __float_as_uint(q1);
+        }
+    };
+    if (MODE == 1 && !__any_sync(0xffffffffu, high > sc.near_limit)) {   // (with biases, a rare pair, the code's size counts for more)
+        odd(std::integral_constant<int, 2>{}, sc.near_odd);
+    } else if (!__any_sync(0xffffffffu, high > sc.odd_limit)) {
+        odd(std::integral_constant<int, 5>{}, sc.odd);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 32; ++e) {
+            const float t = tanh_wide(__uint_as_float(s[e]) * sc.cap_in);
+            s[e] = __float_as_uint(ADD ? fmaf(t, sc.cap_out, add) : t * sc.cap_out);
         }
     }
 }
-// 1 - t^2 of two, as binary16: 2^-12 of it, less than dS's own rounding, for half the registers
-__device__ __forceinline__ uint32_t bent_slope(float t0, float t1) {
+// 1 - t^2 of two capped scores, as binary16: 2^-12 of it, less than dS's own rounding, for half the registers
+__device__ __forceinline__ uint32_t bent_slope(float cap_out_2, uint32_t z0, uint32_t z1) {
     float a, b;
-    mul2(a, b, t0, t1, t0, t1);
-    return pack2<__half>(1.0f - a, 1.0f - b);
+    mul2(a, b, __uint_as_float(z0), __uint_as_float(z1), __uint_as_float(z0), __uint_as_float(z1));
+    fma2(a, b, a, b, -cap_out_2, -cap_out_2, 1.0f, 1.0f);
+    return pack2<__half>(a, b);
 }
 
 // Whether rows and keys of a warp's 32 x 32 piece (`least`: the distance of its last row and first key; the others are up to 62
 // more) are all further apart than the table reaches: -1 the keys lie behind, 1 ahead, 0 not all.
 __device__ __forceinline__ int beyond(int least, int reach) { return least + 62 <= -reach ? -1 : least >= reach ? 1 : 0; }
 
-// A thread's row and 32 neighbouring keys from `away` on (the distance of the first; lane's rows are neighbours: away falls by
-// one with each lane).  s: products in, scores in units of ln 2 out.  GRADIENT: bent gets 1 - t^2 of each pair.  Returns
-// whether every score is finite where the products are (bias tables may hold -inf).  For a whole warp.
-template <bool GRADIENT>
-__device__ __forceinline__ bool shape_scores(const Scores &sc, const Mods &m, float scale_log2, int away, uint32_t (&s)[32], uint32_t (&bent)[16]) {
-    float factor = scale_log2;
-    if (sc.capped) {
-        bend(sc.cap_in, s);
-        factor = sc.cap_out;
-        if constexpr (GRADIENT) {
+// The bias of 32 products or capped scores (factor: what brings them to units of ln 2), value x at distance away + at(x) of a
+// warp's 32 x 32 piece whose smallest distance is `least`.  Returns whether every result is finite where the scores are (tables
+// may hold -inf).  look(x): the table's value for it in units of ln 2, for pieces within the table's reach.
+template <typename At, typename Look>
+__device__ __forceinline__ bool add_bias(const Scores &sc, const Mods &m, float factor, int away, int least, uint32_t (&s)[32], At at, Look look) {
+    if (sc.slopes != nullptr) {
+        const float first = static_cast<float>(away);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) bent[e] = bent_slope(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
+        for (int x = 0; x < 32; x += 2) {                             // (one pass for both takes 5 % longer)
+            float v0, v1;
+            mul2(v0, v1, __uint_as_float(s[x]), __uint_as_float(s[x + 1]), factor, factor);
+            s[x] = __float_as_uint(v0);
+            s[x + 1] = __float_as_uint(v1);
         }
-    }
+        if (m.slope != 0.0f) {
 #pragma unroll
-    for (int e = 0; e < 32; e += 2) {
-        float a, b;
-        mul2(a, b, __uint_as_float(s[e]), __uint_as_float(s[e + 1]), factor, factor);
-        s[e] = __float_as_uint(a);
-        s[e + 1] = __float_as_uint(b);
-    }
-    if (m.slope != 0.0f) {
-        const float first = static_cast<float>(away);
-#pragma unroll
-        for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(fmaf(m.slope, fabsf(first + static_cast<float>(e)), __uint_as_float(s[e])));
-    }
-    if (m.bias == nullptr) return true;
-    const int far = beyond(uniform(away) - 31, sc.reach);
-    if (far != 0) {
-        const float b = __ldg(m.bias + (far < 0 ? -sc.reach : sc.reach)) * 1.4426950408889634f;
-#pragma unroll
-        for (int e = 0; e < 32; ++e) s[e] = __float_as_uint(__uint_as_float(s[e]) + b);
-        return b > -INFINITY;
-    }
-#pragma unroll
-    for (int e = 0; e < 32; ++e) {
-        const float b = __ldg(m.bias + max(-sc.reach, min(sc.reach, away + e)));
-        s[e] = __float_as_uint(fmaf(b, 1.4426950408889634f, __uint_as_float(s[e])));
-    }
-    return false;
-}
-
-// The same for the transposed scores of the dK and dV kernel: s[16 (k / 2) + 4 c + 2 (k % 2) + e] is of key 8 k and row 8 c + e
-// from this thread's first ones on, which are `away` apart.
-__device__ __forceinline__ bool shape_transposed(const Scores &sc, const Mods &m, float scale_log2, int away, int least, uint32_t (&s)[32], uint32_t (&bent)[16]) {
-    float factor = scale_log2;
-    if (sc.capped) {
-        bend(sc.cap_in, s);
-        factor = sc.cap_out;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) bent[e] = bent_slope(__uint_as_float(s[2 * e]), __uint_as_float(s[2 * e + 1]));
-    }
-#pragma unroll
-    for (int e = 0; e < 32; e += 2) {
-        float a, b;
-        mul2(a, b, __uint_as_float(s[e]), __uint_as_float(s[e + 1]), factor, factor);
-        s[e] = __float_as_uint(a);
-        s[e + 1] = __float_as_uint(b);
-    }
-    auto distance = [](int x) { return 8 * (2 * (x / 16) + x / 2 % 2) - 8 * (x / 4 % 4) - x % 2; };   // from the first one's
-    if (m.slope != 0.0f) {
-        const float first = static_cast<float>(away);
-#pragma unroll
-        for (int x = 0; x < 32; ++x) s[x] = __float_as_uint(fmaf(m.slope, fabsf(first + static_cast<float>(distance(x))), __uint_as_float(s[x])));
+            for (int x = 0; x < 32; ++x) s[x] = __float_as_uint(fmaf(m.slope, fabsf(first + static_cast<float>(at(x))), __uint_as_float(s[x])));
+        }
+        factor = 1.0f;
     }
     if (m.bias == nullptr) return true;
     const int far = beyond(least, sc.reach);
     if (far != 0) {
         const float b = __ldg(m.bias + (far < 0 ? -sc.reach : sc.reach)) * 1.4426950408889634f;
 #pragma unroll
-        for (int x = 0; x < 32; ++x) s[x] = __float_as_uint(__uint_as_float(s[x]) + b);
+        for (int x = 0; x < 32; x += 2) {
+            float v0, v1;
+            fma2(v0, v1, __uint_as_float(s[x]), __uint_as_float(s[x + 1]), factor, factor, b, b);
+            s[x] = __float_as_uint(v0);
+            s[x + 1] = __float_as_uint(v1);
+        }
         return b > -INFINITY;
     }
+#pragma unroll
+    for (int x = 0; x < 32; ++x) s[x] = __float_as_uint(fmaf(__uint_as_float(s[x]), factor, look(x)));
+    return false;
+}
+
+// A thread's row and 32 neighbouring keys from `away` on (the distance of the first; lanes' rows are neighbours: away falls by
+// one with each lane).  s: products in, scores in units of ln 2 out (MODE 1: only with a cap).  GRADIENT: bent gets 1 - t^2 of each pair.
+template <int MODE, bool GRADIENT>
+__device__ __forceinline__ bool shape_scores(const Scores &sc, const Mods &m, float scale_log2, int away, uint32_t (&s)[32], uint32_t (&bent)[16]) {
+    float factor = scale_log2;
+    if (sc.capped) {
+        bend<MODE, false>(sc, largest(s), s, 0.0f);
+        factor = 1.0f;
+        if constexpr (GRADIENT) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) bent[e] = bent_slope(sc.cap_out_2, s[2 * e], s[2 * e + 1]);
+        }
+    }
+    if constexpr (MODE == 1) return true;
+    return add_bias(sc, m, factor, away, uniform(away) - 31, s, [](int x) { return x; },
+                    [&](int x) { return __ldg(m.bias + max(-sc.reach, min(sc.reach, away + x))) * 1.4426950408889634f; });
+}
+// The same for the transposed scores of the dK and dV kernel: s[16 (k / 2) + 4 c + 2 (k % 2) + e] is of key 8 k and row 8 c + e
+// from this thread's first ones on, which are `away` apart.
+template <int MODE>
+__device__ __forceinline__ bool shape_transposed(const Scores &sc, const Mods &m, float scale_log2, int away, int least, uint32_t (&s)[32], uint32_t (&bent)[16]) {
+    float factor = scale_log2;
+    if (sc.capped) {
+        bend<MODE, false>(sc, largest(s), s, 0.0f);
+        factor = 1.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) bent[e] = bent_slope(sc.cap_out_2, s[2 * e], s[2 * e + 1]);
+    }
+    if constexpr (MODE == 1) return true;
     // key minus row takes 14 values: 8 (k - c) - e
     float b[14];
+    if (m.bias != nullptr && beyond(least, sc.reach) == 0) {
 #pragma unroll
-    for (int y = 0; y < 14; ++y) b[y] = __ldg(m.bias + max(-sc.reach, min(sc.reach, away + 8 * (y / 2 - 3) - y % 2)));
-#pragma unroll
-    for (int x = 0; x < 32; ++x) s[x] = __float_as_uint(fmaf(b[2 * (2 * (x / 16) + x / 2 % 2 - x / 4 % 4 + 3) + x % 2], 1.4426950408889634f, __uint_as_float(s[x])));
-    return false;
+        for (int y = 0; y < 14; ++y) b[y] = __ldg(m.bias + max(-sc.reach, min(sc.reach, away + 8 * (y / 2 - 3) - y % 2))) * 1.4426950408889634f;
+    }
+    return add_bias(sc, m, factor, away, least, s, [](int x) { return 8 * (2 * (x / 16) + x / 2 % 2) - 8 * (x / 4 % 4) - x % 2; },
+                    [&](int x) { return b[2 * (2 * (x / 16) + x / 2 % 2 - x / 4 % 4 + 3) + x % 2]; });
 }
 
 // Sums over the diagonals of a warp's 32 keys x 32 rows.  v[m][e]: this thread's sum over its values with (key - row) / 8 = m - 3
@@ -241,46 +247,54 @@ __device__ __forceinline__ uint32_t same_document(int mine, int theirs) {
     return word;
 }
 
-// Tiles [lo, hi) of `n` tiles (documents `theirs`, `their_len` of them) in which a document of `mine` [mine_first, mine_end)
-// may be: their smallest and largest documents overlap.  `place`: 4 words of shared memory, free.  For the whole CTA, with
-// three barriers; the result is the same for all.
-__device__ __forceinline__ int2 shared_tiles(const int *mine, int mine_first, int mine_end, const int *theirs, int their_len, int n, int *place) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-    if (threadIdx.x == 0) {
-        place[0] = INT_MAX; place[1] = INT_MIN;                       // smallest and largest of mine
-        place[2] = INT_MAX; place[3] = 0;                             // lo, hi
-    }
-    __syncthreads();
-    for (int at = mine_first + warp * 32; at < mine_end; at += warps * 32) {
-        const int d = __ldg(mine + min(at + lane, mine_end - 1));
-        const int low = __reduce_min_sync(0xffffffffu, d), high = __reduce_max_sync(0xffffffffu, d);
-        if (lane == 0) {
-            atomicMin(place, low);
-            atomicMax(place + 1, high);
+// Tiles [lo, hi) of `n` tiles (documents `theirs`, `their_len` of them) in which a document of `mine` [mine_first, mine_end), at
+// most 32 * ROWS of them, may be: their smallest and largest documents overlap.  In two parts, with a barrier of the whole CTA
+// between them: scan_tiles lets every warp look at every 20th tile, eight of them waiting for memory together, and leaves what it
+// found in its place of shared memory; scanned_tiles puts that together.
+constexpr int kScanWarps = 20;
+template <int ROWS>
+__device__ __forceinline__ void scan_tiles(const int *mine, int mine_first, int mine_end, const int *theirs, int their_len, int n, int2 *place) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    constexpr int kTogether = 8;
+    int smallest = INT_MAX, greatest = INT_MIN, lo = INT_MAX, hi = 0;
+    if (n > warp) {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            const int d = __ldg(mine + min(mine_first + 32 * i + lane, mine_end - 1));
+            smallest = min(smallest, d);
+            greatest = max(greatest, d);
         }
     }
-    __syncthreads();
-    const int low = place[0], high = place[1];
-    for (int t = warp; t < n; t += warps) {
-        int a = INT_MAX, b = INT_MIN;
+    for (int t0 = warp; t0 < n; t0 += kTogether * kScanWarps) {
+        int low[kTogether], high[kTogether];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int at = t * 128 + 32 * k + lane;
-            if (at < their_len) {
-                const int d = __ldg(theirs + at);
-                a = min(a, d);
-                b = max(b, d);
+        for (int i = 0; i < kTogether; ++i) {
+            int d[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) d[k] = __ldg(theirs + min((t0 + i * kScanWarps) * 128 + 32 * k + lane, their_len - 1));   // (the last one again past the end)
+            low[i] = min(min(d[0], d[1]), min(d[2], d[3]));
+            high[i] = max(max(d[0], d[1]), max(d[2], d[3]));
+        }
+        if (t0 == warp) {
+            smallest = __reduce_min_sync(0xffffffffu, smallest);
+            greatest = __reduce_max_sync(0xffffffffu, greatest);
+        }
+#pragma unroll
+        for (int i = 0; i < kTogether; ++i) {
+            const int t = t0 + i * kScanWarps, a = __reduce_min_sync(0xffffffffu, low[i]), b = __reduce_max_sync(0xffffffffu, high[i]);
+            if (t < n && a <= greatest && b >= smallest) {
+                lo = min(lo, t);
+                hi = t + 1;
             }
         }
-        a = __reduce_min_sync(0xffffffffu, a);
-        b = __reduce_max_sync(0xffffffffu, b);
-        if (lane == 0 && a <= high && b >= low) {
-            atomicMin(place + 2, t);
-            atomicMax(place + 3, t + 1);
-        }
     }
-    __syncthreads();
-    return uniform(place[3]) == 0 ? make_int2(0, 0) : make_int2(uniform(place[2]), uniform(place[3]));
+    if (lane == 0) place[warp] = make_int2(lo, hi);
+}
+__device__ __forceinline__ int2 scanned_tiles(const int2 *place) {
+    const int lane = threadIdx.x & 31;
+    const int2 found = lane < kScanWarps ? place[lane] : make_int2(INT_MAX, 0);
+    const int lo = __reduce_min_sync(0xffffffffu, found.x), hi = __reduce_max_sync(0xffffffffu, found.y);
+    return hi == 0 ? make_int2(0, 0) : make_int2(lo, hi);
 }
 
 }  // namespace attn

@@ -237,6 +237,25 @@ def test_large_products_reach_the_cap(cap):
     check_all(1, 200, 200, 2, 1, 64, False, HALF, "plain", {"cap": cap}, scale=4.0)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("slopes", [False, True])
+@pytest.mark.parametrize("size", [-1.4, 0.4, 1.4])
+def test_one_large_product_at_every_place(size, slopes):
+    """Sequence b has one product of `size` caps, at key b of row 5 + b, and zeros else: whichever form of the tanh it needs, the form
+    that its neighbours would do with is not taken.  lse within 2^-18 (of sums of 130 terms: 2^-24 of 5, and the capped score's 2^-21)."""
+    b, d, cap = 128, 128, 3.0
+    q = torch.zeros(b, 140, 1, d, device="cuda", dtype=BF)
+    k = torch.zeros(b, 130, 1, d, device="cuda", dtype=BF)
+    at = torch.arange(b, device="cuda")
+    k[:, :b, 0, :] = torch.eye(b, device="cuda", dtype=BF)
+    q[at, 5 + at, 0, at] = size * cap
+    mods = {"cap": cap, "scale": 1.0, **({"slopes": torch.zeros(1, device="cuda")} if slopes else {})}
+    _, lse = fb.fewbit_attention_fwd(q, k, k, **mods)
+    z = torch.zeros(b, 140, 130, dtype=torch.float64, device="cuda")
+    z[at, 5 + at, at] = cap * (q[at, 5 + at, 0, at].double() / cap).tanh()
+    assert ((lse[:, 0].double() - torch.logsumexp(z, 2)).abs() <= 2.0 ** -18).all()
+
+
 PACKED = [
     ([0, 40, 40, 300, 301], [0, 40, 50, 310, 310], 4, 2, 64, True, BF, {"cap": 20.0}),
     ([0, 129, 400, 400, 1000], [0, 129, 400, 400, 1000], 2, 1, 128, True, BF, {"docs": "sorted", "cap": 10.0}),
