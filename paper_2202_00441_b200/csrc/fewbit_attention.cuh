@@ -1320,10 +1320,10 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             [[maybe_unused]] const int away = key - q0 - 32 * part - 2 * (lane % 4) - reach;   // distance of the first key and row
             [[maybe_unused]] const int least = k0 + 32 * (warp & 3) - q0 - 32 * part - reach - 31;   // of the warp's last row and first key
             float unit = p.scale_log2;
-            [[maybe_unused]] bool open = true, finite = true;         // the whole warp sees all its keys; tables may hold -inf
+            [[maybe_unused]] bool open = true;                        // the whole warp sees all its keys
             if constexpr (MODE > 0) {
                 if (MODE > 1 || p.scores.capped) {
-                    finite = shape_transposed<MODE>(p.scores, mods, p.scale_log2, away, least, s, bent);
+                    shape_transposed<MODE>(p.scores, mods, p.scale_log2, away, least, s, bent);
                     unit = 1.0f;
                 }
                 uint32_t word = 0xffffffffu;                          // a bit for each value, in their order
@@ -1363,7 +1363,8 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                 }
             }
             const bool diagonal = MODE == 0 && p.causal && k0 + kTile - 1 > q0 + reach;   // some rows do not see some keys
-            if (diagonal || !open || !finite) {
+            // (MODE > 1: tables may hold -inf, which the polynomial does not make 0, and its 2.6e-6 would show in a sum by distance)
+            if (MODE > 1 || diagonal || !open) {
                 [[maybe_unused]] const int from = key - reach - q0 - 32 * part - 2 * (lane % 4);   // of the first of the 4 keys, which are 8 apart
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
@@ -1493,7 +1494,13 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
         if (stopped(sync)) ok = false;                                // (kDone comes in any case)
         if constexpr (MODE == 3) {
             if (n > 0) {
-                if (!ok) behind = ahead = NAN;                        // given up: the bias's gradient says so
+                if (!ok) {                                            // given up: the bias's gradient says so
+                    behind = ahead = NAN;
+                    for (int h = 0; h < p.group; ++h) {
+                        float *to = p.scores.near + place_of(w.head * p.group + h) * p.scores.near_tiles * kNearFloats + warp * 64 + lane;
+                        for (int at = 0; at < p.scores.near_tiles; ++at) to[at * kNearFloats] = to[at * kNearFloats + 32] = NAN;
+                    }
+                }
                 write_far();
             }
         }

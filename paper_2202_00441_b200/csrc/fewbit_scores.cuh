@@ -175,7 +175,7 @@ __device__ __forceinline__ bool shape_scores(const Scores &sc, const Mods &m, fl
 // The same for the transposed scores of the dK and dV kernel: s[16 (k / 2) + 4 c + 2 (k % 2) + e] is of key 8 k and row 8 c + e
 // from this thread's first ones on, which are `away` apart.
 template <int MODE>
-__device__ __forceinline__ bool shape_transposed(const Scores &sc, const Mods &m, float scale_log2, int away, int least, uint32_t (&s)[32], uint32_t (&bent)[16]) {
+__device__ __forceinline__ void shape_transposed(const Scores &sc, const Mods &m, float scale_log2, int away, int least, uint32_t (&s)[32], uint32_t (&bent)[16]) {
     float factor = scale_log2;
     if (sc.capped) {
         bend<MODE, false>(sc, largest(s), s, 0.0f);
@@ -183,14 +183,14 @@ __device__ __forceinline__ bool shape_transposed(const Scores &sc, const Mods &m
 #pragma unroll
         for (int e = 0; e < 16; ++e) bent[e] = bent_slope(sc.cap_out_2, s[2 * e], s[2 * e + 1]);
     }
-    if constexpr (MODE == 1) return true;
+    if constexpr (MODE == 1) return;
     // key minus row takes 14 values: 8 (k - c) - e
     float b[14];
     if (m.bias != nullptr && beyond(least, sc.reach) == 0) {
 #pragma unroll
         for (int y = 0; y < 14; ++y) b[y] = __ldg(m.bias + max(-sc.reach, min(sc.reach, away + 8 * (y / 2 - 3) - y % 2))) * 1.4426950408889634f;
     }
-    return add_bias(sc, m, factor, away, least, s, [](int x) { return 8 * (2 * (x / 16) + x / 2 % 2) - 8 * (x / 4 % 4) - x % 2; },
+    add_bias(sc, m, factor, away, least, s, [](int x) { return 8 * (2 * (x / 16) + x / 2 % 2) - 8 * (x / 4 % 4) - x % 2; },
                     [&](int x) { return b[2 * (2 * (x / 16) + x / 2 % 2 - x / 4 % 4 + 3) + x % 2]; });
 }
 
