@@ -644,7 +644,12 @@ NormPlan norm_plan(int64_t width, uintptr_t pointers, int elem) {
 }
 // CTAs of the backward pass: as many as fit at once.  With kLead, groups of threads that take several rows take every 8th one, or
 // a multiple of 8: then the same elements of each.
-// Rows come ahead through shared memory for 16-bit types (and pieces of 8); ...
+// Rows that a CTA of 512 threads holds, but none of 256: its sums are the weight's gradient without a second launch (5 rows of 640
+// elements: 9.0 us with two CTAs, 7.7 so).  Rows that it would have to take in turn come sooner from several CTAs (4 rows of 4096: 10.3
+// us, 12.2 from one).
+void widen_plan(int64_t rows, NormPlan *q) {
+    if (q->n == 16 && q->group <= 128 && rows > 256 / q->group && rows <= 512 / q->group) q->threads = 512 / q->group * q->group;
+}
 constexpr bool norm_ahead(int kind, int elem, int n) { return kind != kSingle && elem * n < 128; }
 constexpr int norm_ctas_on_sm(bool ahead, int n, int threads) { return threads > 256 ? 1 : ahead && n == 16 ? 2 : 3; }
 int64_t norm_ctas(int64_t rows, const NormPlan &q, int elem, int sms) {
@@ -665,7 +670,7 @@ cudaError_t launch_bwd(NormParams &p, unsigned grid, unsigned threads, cudaStrea
     constexpr int kStage = 3 * N * static_cast<int>(sizeof(T)) * THREADS, kCtas = norm_ctas_on_sm(kAhead, N, THREADS), kRoom = 225 * 1024 / kCtas;
     constexpr int kDepth = !kAhead ? 1 : 3 * kStage <= kRoom ? 3 : 2;
     static_assert(!kAhead || kDepth * kStage <= kRoom);
-    constexpr int kSums = THREADS == 256 ? 4 * N * THREADS : 0, kShared = kDepth > 1 && kDepth * kStage > kSums ? kDepth * kStage : kSums;
+    constexpr int kSums = 4 * N * THREADS, kShared = kDepth > 1 && kDepth * kStage > kSums ? kDepth * kStage : kSums;
     constexpr auto kernel = add_norm_bwd_kernel<T, V, LEAD, N, THREADS, kCtas, (kDepth > 1)>;
     p.depth = kDepth;
     if constexpr (kShared > 32 * 1024) {
@@ -766,7 +771,8 @@ size_t fewbit_add_rms_norm_workspace_bytes(const fewbit_norm_shape *s) {
     const int sms = device_sm_count(&err);
     size_t most = 0;
     for (uintptr_t pointers : {0, 1}) {                      // (buffers of any alignment)
-        const NormPlan q = norm_plan(s->width, pointers, s->dtype == FEWBIT_F32 ? 4 : 2);
+        NormPlan q = norm_plan(s->width, pointers, s->dtype == FEWBIT_F32 ? 4 : 2);
+        widen_plan(s->rows, &q);
         const size_t bytes = static_cast<size_t>(norm_ctas(s->rows, q, s->dtype == FEWBIT_F32 ? 4 : 2, sms)) * s->width * sizeof(float);
         if (bytes > most) most = bytes;
     }
@@ -789,7 +795,8 @@ fewbit_status fewbit_add_rms_norm_bwd(const fewbit_norm_shape *s, const void *gr
     cudaError_t err = cudaSuccess;
     const int sms = device_sm_count(&err);
     if (err != cudaSuccess) return cuda_status(err);
-    const NormPlan q = norm_plan(s->width, all, elem);
+    NormPlan q = norm_plan(s->width, all, elem);
+    widen_plan(s->rows, &q);
     const int64_t ctas = norm_ctas(s->rows, q, elem, sms);
     if (grad_weight != nullptr && workspace_bytes < static_cast<size_t>(ctas) * s->width * sizeof(float)) return FEWBIT_ERR_ALLOC;
     NormParams p = norm_params(s, d, q);
@@ -798,11 +805,11 @@ fewbit_status fewbit_add_rms_norm_bwd(const fewbit_norm_shape *s, const void *gr
     p.h_in = h;
     p.grad_x = grad_x;
     p.grad_residual = grad_residual;
-    p.partial = grad_weight != nullptr ? static_cast<float *>(workspace) : nullptr;
+    p.partial = grad_weight != nullptr && ctas > 1 ? static_cast<float *>(workspace) : grad_weight;
     err = kNormBwd[s->dtype][q.kind][q.threads <= 256 ? size_index(q) : 1 + size_index(q)](p, static_cast<unsigned>(ctas), q.threads, stm);
     if (err != cudaSuccess) return cuda_status(err);
     g_launches.fetch_add(1, std::memory_order_relaxed);
-    if (grad_weight == nullptr) return FEWBIT_OK;
+    if (grad_weight == nullptr || ctas == 1) return FEWBIT_OK;
     err = launch_pdl(norm_weight_kernel, static_cast<unsigned>((s->width + 31) / 32), 1024, 0, stm, pdl_enabled(), static_cast<const float *>(p.partial),
                      static_cast<int>(ctas), p.width, grad_weight);
     if (err == cudaSuccess) g_launches.fetch_add(1, std::memory_order_relaxed);
