@@ -49,23 +49,26 @@ __device__ __forceinline__ RandomKeys device_keys(const Drop &d) {
     return random_keys(d.seed + (d.seed_device != nullptr ? static_cast<uint64_t>(__ldg(d.seed_device)) : 0));
 }
 
-// v[e] of N elements (1, 4 or 8) from the group (low, high) on: scaled where kept, else 0.  N 1: the one at place `i` of the group.
+// The words of N elements (1, 4 or 8) from the group (low, high) on; N 1: of the one at place `i` of the group.  Drawn before the
+// elements are waited for, they fill the time that memory takes.
 template <int N>
-__device__ __forceinline__ void drop(const Drop &d, const RandomKeys &k, uint32_t low, uint32_t high, uint32_t i, float *v) {
+__device__ __forceinline__ void draw(const Drop &d, const RandomKeys &k, uint32_t low, uint32_t high, uint32_t i, uint32_t *words) {
     if constexpr (N == 1) {
         const uint4 w = random_words(k, low, high, d.place);
-        const uint32_t word = i < 2 ? (i == 0 ? w.x : w.y) : (i == 2 ? w.z : w.w);
-        v[0] = word >= d.limit ? v[0] * d.scale : 0.0f;
+        words[0] = i < 2 ? (i == 0 ? w.x : w.y) : (i == 2 ? w.z : w.w);
     } else {
 #pragma unroll
         for (int e = 0; e < N; e += 4) {
             const uint4 w = random_words(k, low + e / 4, high, d.place);   // (8 elements from a multiple of 8 on share `high`)
-            v[e] = w.x >= d.limit ? v[e] * d.scale : 0.0f;
-            v[e + 1] = w.y >= d.limit ? v[e + 1] * d.scale : 0.0f;
-            v[e + 2] = w.z >= d.limit ? v[e + 2] * d.scale : 0.0f;
-            v[e + 3] = w.w >= d.limit ? v[e + 3] * d.scale : 0.0f;
+            words[e] = w.x; words[e + 1] = w.y; words[e + 2] = w.z; words[e + 3] = w.w;
         }
     }
+}
+// v[e]: scaled where kept, else 0.
+template <int N>
+__device__ __forceinline__ void drop(const Drop &d, const uint32_t *words, float *v) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = words[e] >= d.limit ? v[e] * d.scale : 0.0f;
 }
 
 }  // namespace fewbit
