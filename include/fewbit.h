@@ -405,7 +405,7 @@ FEWBIT_API fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *shap
  *     not causal, or d <= 0, or j < prefix_lens[b];   and
  *     q_documents[i] == k_documents[j]     (where given)
  *
- *   cap             finite, >= 0; 0: none
+ *   cap             0: none; else 2^-60 .. 2^60
  *   slopes          DEVICE, a binary32 value for each query head, or NULL
  *   distance_bias   DEVICE, heads x (2 R + 1) binary32 values, R = max_distance,
  *                   1 .. FEWBIT_MAX_DISTANCE, or NULL.  -inf hides the key; so does a
@@ -434,7 +434,8 @@ FEWBIT_API fewbit_status fewbit_attention_scores_fwd(const fewbit_attention_shap
 
 /*
  * Bytes of `workspace` for the backward pass; 0 for a bad shape.  bias_gradient: with the gradient of distance_bias, which
- * takes 4 KB for each pair of a row tile and a key tile (128 x 128) within max_distance of each other, and each head.
+ * takes 4 KB for each pair of a row tile and a key tile (128 x 128) within max_distance of each other, and each head
+ * (4 or so such pairs for a key tile with a max_distance of 128).
  */
 FEWBIT_API size_t fewbit_attention_scores_workspace_bytes(const fewbit_attention_shape *shape, const fewbit_attention_scores *scores, int bias_gradient);
 

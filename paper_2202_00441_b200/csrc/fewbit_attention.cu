@@ -164,8 +164,8 @@ bool shaped(const fewbit_attention_scores *c) { return c != nullptr && (c->cap >
 
 fewbit_status check_scores(const fewbit_attention_shape *s, const fewbit_attention_scores *c, const Sizes &z) {
     if (c == nullptr) return FEWBIT_OK;
-    // (the kernels hold scale / cap and cap * log2(e))
-    if (!(c->cap >= 0) || (c->cap > 0 && !(std::isfinite(s->scale / c->cap) && s->scale / c->cap > 0 && std::isfinite(c->cap * attn::kLog2e)))) return FEWBIT_ERR_INVALID_ARG;
+    // (the kernels hold scale / cap and the squares of capped scores)
+    if (!(c->cap >= 0) || (c->cap > 0 && !(c->cap >= 0x1p-60f && c->cap <= 0x1p60f && std::isfinite(s->scale / c->cap) && s->scale / c->cap > 0))) return FEWBIT_ERR_INVALID_ARG;
     if (c->distance_bias != nullptr && (c->max_distance < 1 || c->max_distance > FEWBIT_MAX_DISTANCE)) return FEWBIT_ERR_INVALID_ARG;
     if ((c->prefix_lens != nullptr && !s->causal) || (c->q_documents == nullptr) != (c->k_documents == nullptr)) return FEWBIT_ERR_INVALID_ARG;
     uintptr_t all = 0;
@@ -185,9 +185,9 @@ void fill_scores(const fewbit_attention_shape *s, const fewbit_attention_scores 
     to.cap_in = to.capped ? s->scale / c->cap : 0.0f;
     to.cap_out = c->cap * attn::kLog2e;
     // tanh(a) / a by powers of a^2, for magnitudes up to 0.3 and 1, with a = cap_in s and the result's factor folded in: where the
-    // folded coefficients are normal numbers, else the exponential form serves all.
+    // folded coefficients are normal numbers, else the form for any argument serves all.
     to.near_limit = to.odd_limit = -1.0f;
-    if (to.capped && to.cap_in > 0x1p-12f && to.cap_in < 0x1p12f && to.cap_out > 0x1p-12f && to.cap_out < 0x1p24f) {
+    if (to.capped && to.cap_in > 0x1p-11f && to.cap_in < 0x1p11f && s->scale > 0x1p-6f && s->scale < 0x1p6f) {
         const double near_odd[3] = {0.9999988675117493, -0.33310022950172424, 0.12633946537971497};
         const double odd[6] = {0.9999994039535522, -0.3332904279232025, 0.13281433284282684, -0.051605671644210815, 0.016743114218115807, -0.0030670601408928633};
         double power = static_cast<double>(to.cap_in) * to.cap_out;
@@ -210,16 +210,15 @@ void fill_scores(const fewbit_attention_shape *s, const fewbit_attention_scores 
 // What the bias's gradient takes of the workspace, behind the rows' statistics.
 struct BiasSpace {
     size_t near, far, written;        // bytes
-    int64_t tiles;                    // key tiles of a sequence
+    int64_t places;                   // key tiles of a sequence, or of all packed ones
     int near_tiles;
 };
-BiasSpace bias_space(const fewbit_attention_shape *s, int max_distance) {
+BiasSpace bias_space(const fewbit_attention_shape *s, const Sizes &z, int max_distance) {
     BiasSpace b;
     const int64_t row_tiles = (s->q_len + attn::kTile - 1) / attn::kTile, most = (2 * static_cast<int64_t>(max_distance) + 254 + 127) / 128;
-    b.tiles = (s->k_len + attn::kTile - 1) / attn::kTile;
-    if (b.tiles == 0) b.tiles = 1;
+    b.places = z.packed ? z.k_rows / attn::kTile + s->batch + 1 : (s->k_len + attn::kTile - 1) / attn::kTile;
     b.near_tiles = static_cast<int>(row_tiles < most ? row_tiles : most);
-    const size_t places = static_cast<size_t>(s->batch) * s->heads * b.tiles;
+    const size_t places = (z.packed ? 1 : static_cast<size_t>(s->batch)) * s->heads * b.places;
     b.near = places * b.near_tiles * attn::kNearFloats * 4;
     b.far = places * attn::kFarFloats * 4;
     b.written = places * sizeof(int4);
@@ -290,7 +289,7 @@ fewbit_status backward(const fewbit_attention_shape *s, const fewbit_attention_s
     if ((reinterpret_cast<uintptr_t>(lse) & 3) || (reinterpret_cast<uintptr_t>(workspace) & 15)) return FEWBIT_ERR_ALIGNMENT;
     const size_t stats = stat_bytes(s, z);
     BiasSpace b = {};
-    if (grad_bias != nullptr) b = bias_space(s, scores->max_distance);
+    if (grad_bias != nullptr) b = bias_space(s, z, scores->max_distance);
     if (workspace_bytes < stats + b.near + b.far + b.written) return FEWBIT_ERR_ALLOC;
     Params p = {};
     fewbit_status st = fill(s, z, &p);
@@ -314,7 +313,11 @@ fewbit_status backward(const fewbit_attention_shape *s, const fewbit_attention_s
         p.scores.written = reinterpret_cast<int4 *>(at);
         p.scores.near = reinterpret_cast<float *>(at + b.written);
         p.scores.far = reinterpret_cast<float *>(at + b.written + b.near);
+        p.scores.places = static_cast<int>(b.places);
         p.scores.near_tiles = b.near_tiles;
+        // packed sequences leave some places out
+        if (z.packed) st = cuda_status(cudaMemsetAsync(p.scores.written, 0, b.written, static_cast<cudaStream_t>(stream)));
+        if (st != FEWBIT_OK) return st;
     }
     const int64_t row_tiles = (s->q_len + attn::kTile - 1) / attn::kTile, key_tiles = (s->k_len + attn::kTile - 1) / attn::kTile;
     p.split = choose_split(p.sms, row_tiles * s->heads * s->batch, key_tiles, p.causal, s->head_dim > 64 ? 8 : 4, kDqEnds);
@@ -350,7 +353,7 @@ size_t fewbit_attention_scores_workspace_bytes(const fewbit_attention_shape *s, 
     Sizes z;
     if (check_shape(s, &z) != FEWBIT_OK || check_scores(s, scores, z) != FEWBIT_OK) return 0;
     BiasSpace b = {};
-    if (bias_gradient && scores != nullptr && scores->distance_bias != nullptr) b = bias_space(s, scores->max_distance);
+    if (bias_gradient && scores != nullptr && scores->distance_bias != nullptr) b = bias_space(s, z, scores->max_distance);
     return stat_bytes(s, z) + b.near + b.far + b.written;
 }
 

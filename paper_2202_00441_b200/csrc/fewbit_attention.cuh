@@ -1079,17 +1079,18 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
         return;
     }
     const int k0 = w.tile * kTile;
-    // MODE 3: places of this key tile for the sums by distance, one for each query head of the group
-    auto place_of = [&](int head) { return (static_cast<long long>(w.batch) * p.heads + head) * p.tiles + w.tile; };
-    auto far_of = [&](int head) { return p.scores.far + place_of(head) * kFarFloats + rank * 32 + warp * 2; };
-    if (MODE == 3 && warp < kMmaWarp && lane < 2)
-        for (int h = 0; h < p.group; ++h) far_of(w.head * p.group + h)[lane] = 0.0f;
     if (k0 >= w.k_len) {
-        if (MODE == 3 && rank == 0)
-            for (int h = threadIdx.x; h < p.group; h += kThreadsAttn) p.scores.written[place_of(w.head * p.group + h)] = make_int4(0, 0, 0, 0);
         pdl_wait();
         return;
     }
+    // MODE 3: places of this key tile for the sums by distance, one for each query head of the group: (batch, heads, tiles), or
+    // (heads, keys / 128 + sequences + 1) for packed sequences, as the rows' statistics
+    auto place_of = [&](int head) {
+        return w.packed ? static_cast<long long>(head) * p.scores.places + w.k_first / kTile + w.batch + w.tile : (static_cast<long long>(w.batch) * p.heads + head) * p.scores.places + w.tile;
+    };
+    auto far_of = [&](int head) { return p.scores.far + place_of(head) * kFarFloats + rank * 32 + warp * 2; };
+    if (MODE == 3 && warp < kMmaWarp && lane < 2)
+        for (int h = 0; h < p.group; ++h) far_of(w.head * p.group + h)[lane] = 0.0f;
     // row tiles [first, last) see a key of this tile; all query heads of the group, one after the other, dealt out to the
     // cluster's CTAs in turn
     const int reach = w.k_len - w.q_len;                              // row i sees keys up to i + reach
@@ -1122,7 +1123,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
         n = uniform(share_of(each * p.group, rank, p.split));
     }
     if (MODE == 3 && rank == 0)
-        for (int h = threadIdx.x; h < p.group; h += kThreadsAttn) p.scores.written[place_of(w.head * p.group + h)] = make_int4(first, first + each, reach, 0);
+        for (int h = threadIdx.x; h < p.group; h += kThreadsAttn) p.scores.written[place_of(w.head * p.group + h)] = make_int4(first, first + each, reach, w.tile + 1);
     auto bar = [&](int i) { return smem_address(&sync->bar[i]); };
     auto wait = [&](int i, uint32_t parity) { return barrier_wait(bar(i), parity, &sync->stop, p.timeouts); };
     const uint32_t sm_v = base, sm_q = base + kBytes, sm_g = base + 4 * kBytes;

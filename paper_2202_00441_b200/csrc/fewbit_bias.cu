@@ -18,17 +18,19 @@ namespace {
 constexpr int kGradThreads = 1024, kGradWarps = kGradThreads / 32, kGradTogether = 4;
 
 __global__ void __launch_bounds__(kGradThreads)
-bias_gradient_kernel(Scores sc, int batch, int heads, int tiles, int split, int groups, float *grad) {
+bias_gradient_kernel(Scores sc, int batch, int heads, int split, int groups, float *grad) {
     pdl_launch_dependents();
     __shared__ float part[2][kGradWarps][33];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, head = blockIdx.y, items = batch * tiles;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, head = blockIdx.y, tiles = sc.places, items = batch * tiles;
     pdl_wait();
     float *to = grad + static_cast<long long>(head) * (2 * sc.reach + 1) + sc.reach;   // of distance 0
     auto place_of = [&](int item) { return (static_cast<long long>(item / tiles) * heads + head) * tiles + item % tiles; };
     if (static_cast<int>(blockIdx.x) == groups) {
         float behind = 0.0f, ahead = 0.0f;
         for (long long i = threadIdx.x; i < static_cast<long long>(items) * split * 16; i += kGradThreads) {
-            const float2 v = reinterpret_cast<const float2 *>(sc.far + place_of(static_cast<int>(i / (split * 16))) * kFarFloats)[i % (split * 16)];
+            const long long place = place_of(static_cast<int>(i / (split * 16)));
+            if (sc.written[place].w == 0) continue;
+            const float2 v = reinterpret_cast<const float2 *>(sc.far + place * kFarFloats)[i % (split * 16)];
             behind += v.x;
             ahead += v.y;
         }
@@ -59,9 +61,9 @@ bias_gradient_kernel(Scores sc, int batch, int heads, int tiles, int split, int 
 #pragma unroll
         for (int i = 0; i < kGradTogether; ++i) {
             const long long at = at0 + i * kGradWarps;
-            const int k0 = item[i] % tiles * kTile, reach = written[i].z, nearest = max(0, first_near(k0, reach, sc.reach));
+            const int k0 = (written[i].w - 1) * kTile, reach = written[i].z, nearest = max(0, first_near(k0, reach, sc.reach));
             const int t = max(max(written[i].x, nearest), first_near(k0, reach, first + 32)) + static_cast<int>(at % 3);
-            const bool there = at < 3ll * items && t < min(written[i].y, nearest + sc.near_tiles) && t * kTile <= k0 - reach + 127 - first;
+            const bool there = at < 3ll * items && written[i].w > 0 && t < min(written[i].y, nearest + sc.near_tiles) && t * kTile <= k0 - reach + 127 - first;
             const float *from = sc.near + (place[i] * sc.near_tiles + (there ? t - nearest : 0)) * kNearFloats;
             const int u0 = d - (k0 - t * kTile - reach) + 32;         // in a piece on the diagonal
 #pragma unroll
@@ -93,7 +95,7 @@ cudaError_t launch_bias_gradient(const Params &p, float *grad, cudaStream_t st) 
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = pdl_enabled() ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, bias_gradient_kernel, p.scores, p.batch, p.heads, p.tiles, p.split, groups, grad);
+    return cudaLaunchKernelEx(&cfg, bias_gradient_kernel, p.scores, p.q_offsets != nullptr ? 1 : p.batch, p.heads, p.split, groups, grad);
 }
 
 }  // namespace attn

@@ -83,6 +83,9 @@ struct Piece {
 // ---------------------------------------------------------------------------------------------------
 // dropout
 // ---------------------------------------------------------------------------------------------------
+// One pass: bound by memory with a residual (bfloat16, 16384 x 4096: 72 us = 5.6 TB/s, 86 % of a copy's rate), by the words without one
+// (59 us, 69 %): four words take 18 products of 32 x 32 bits, which the multipliers do at a quarter of their rate, and 20 logic
+// operations of half the issue rate.  A thread's loads are issued together: waiting for each as it is widened took twice as long.
 constexpr int kDropThreads = 256, kDropVectors = 4;          // pieces of 8 elements for each thread
 constexpr int kDropElems = kDropThreads * kDropVectors * 8;
 
@@ -213,7 +216,7 @@ struct NormParams {
 };
 
 // N elements of a row for each thread, in pieces of V: piece i at column (i * group + thread) * V - lead, of which elements
-// [lo, hi) are the row's.  LEAD: a row whose first element is not the first of a piece of 8 aligned ones starts `lead` elements into
+// [lo, hi) are the row's.  LEAD: a row whose first element is not the first of an aligned piece of 16 bytes starts `lead` elements into
 // one, so that rows of any width move in whole pieces but for their ends; what the ends' pieces hold of the rows beside it is
 // replaced by zeros.  V 1: buffers of any alignment.
 template <int V, bool LEAD>
@@ -352,6 +355,9 @@ __device__ __forceinline__ void over_group(float (&v)[K], int group, float (*par
     }
 }
 
+// Forward: a row for each group of threads, held in registers from its load to its results; one CTA's rows wait for memory while
+// another's sums go round.  Bound by memory: bfloat16, 16384 x 4096, 90 us without dropout (91 % of a copy's rate), 99 with it (83 %: the words
+// keep two thirds of the issue slots busy), 119 with 8-bit results; binary32 164 us (100 %).
 // Places that are not the row's hold 0 from the load on, so that only loads and stores ask.
 template <typename T, int V, bool LEAD, int N, bool CODES>
 __global__ void __launch_bounds__(kNormThreads)
@@ -444,8 +450,12 @@ add_norm_fwd_kernel(const NormParams p) {
     }
 }
 
+// Backward: CTAs stay and take rows in turn, so that the weight's gradient is summed in registers.  bfloat16, 16384 x 4096: 97 us without
+// dropout (84 % of a copy's rate), 149 with it (69 %: instruction issue and the multipliers, as the words come on top of 30 other
+// instructions an element); binary32 177 us (92 %).  Two CTAs of 256 threads that hold the weights beat three that read them again for
+// every row (95 and 134 us), and words drawn in front of the sums (149 and 159).
 // AHEAD: each thread copies its pieces of the next rows to places of its own in shared memory, `depth` - 1 rows ahead of their use
-// (pieces of 4 bytes or more), so that a few CTAs keep memory busy while their rows' sums go round.
+// (pieces of 16 bytes), so that a few CTAs keep memory busy while their rows' sums go round.
 template <typename T, int V, bool LEAD, int N, int THREADS, int CTAS, bool AHEAD>
 __global__ void __launch_bounds__(THREADS, CTAS)
 add_norm_bwd_kernel(const NormParams p) {
@@ -631,7 +641,7 @@ norm_weight_kernel(const float *partial, int rows, int width, float *to) {
 
 constexpr int kNormMaxWidth = 16384;
 
-enum { kWhole, kLead, kSingle };                             // pieces of 16 bytes that are whole, or not at the rows' ends; single elements
+enum { kWhole, kLead, kSingle };                             // pieces of 16 bytes that are whole, or not at the rows' ends (rows of 4099: 1.5 to 2 times as long); single elements (4 to 8 times)
 struct NormPlan {
     int kind, n, group, threads;
 };

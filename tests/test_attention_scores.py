@@ -230,6 +230,32 @@ def test_matches_the_formulas(case):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("cap", [2.0 ** -60, 2.0 ** -30, 2.0 ** 25, 2.0 ** 60])
+def test_the_smallest_and_largest_caps(cap):
+    """Every score next to 0, and scores as if there were no cap: nothing that is not finite comes out of squares and reciprocals."""
+    q, k, v, g = ta.make(1, 150, 150, 2, 1, 64, BF)
+    out, lse = fb.fewbit_attention_fwd(q, k, v, cap=cap)
+    grads = fb.fewbit_attention_bwd(g, q, k, v, out, lse, cap=cap)
+    assert all(torch.isfinite(x).all() for x in (out, lse, *grads))
+    if cap < 1:
+        assert ((lse.double() - math.log(150)).abs() <= 2.0 ** -18).all()
+    else:
+        plain = fb.fewbit_attention_fwd(q, k, v)
+        assert ((lse - plain[1]).abs() <= 2.0 ** -16 * (1 + plain[1].abs())).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("cap,scale", [(200.0, 0.125), (300.0, 0.125), (5000.0, 1.0), (1e6, 0.01), (30.0, 0.001), (2e-4, 0.125)])
+def test_caps_far_from_the_scale(cap, scale):
+    """On both sides of where scale and cap fold into the polynomials' coefficients: the scores' relative error stays below 2^-19, so
+    that lse is within 2^-18 (1 + largest score)."""
+    q, k, _, _ = ta.make(1, 200, 200, 1, 1, 64, BF, size=2.0)
+    _, lse = fb.fewbit_attention_fwd(q, k, k, cap=cap, scale=scale)
+    z = cap * (scale * q[0, :, 0].double() @ k[0, :, 0].double().T / cap).tanh()
+    assert ((lse[0, 0].double() - torch.logsumexp(z, 1)).abs() <= 2.0 ** -18 * (1 + z.abs().amax())).all()
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("cap", [0.25, 2.0, 50.0])
 def test_large_products_reach_the_cap(cap):
     """Products of a size of 100: both forms of the tanh, and slopes 1 - t^2 down to 0."""
@@ -262,6 +288,8 @@ PACKED = [
     ([0, 129, 400, 777], [0, 300, 310, 900], 2, 2, 64, False, HALF, {"reach": 60}),
     ([0, 200, 200, 500], [0, 90, 95, 400], 4, 1, 96, True, BF, {"reach": 128, "slopes": 0.02, "prefix": 80, "docs": "scattered"}),
     ([5, 140, 300], [3, 140, 300], 2, 1, 64, True, BF, {"prefix": 300, "reach": 9}),   # rows in front of the first sequence
+    ([0, 3, 5, 130, 258, 258, 600, 601], [0, 3, 4, 131, 259, 300, 640, 640], 4, 2, 64, False, BF, {"reach": 300}),   # tiles' places next to each other
+    ([0, 512, 640, 650], [0, 384, 512, 1000], 2, 2, 128, False, HALF, {"reach": 40}),
 ]
 
 
@@ -454,7 +482,7 @@ def test_refusals_of_the_library():
 
     at = 1 << 20
     assert fwd(shape(), cap=1.0) == 1                        # (only lse is missing)
-    for cap in (-1.0, float("nan"), float("inf"), 3e38, 1e-42):
+    for cap in (-1.0, float("nan"), float("inf"), 3e38, 1e-42, 2.0 ** -61, 2.0 ** 61):
         assert fwd(shape(), cap=cap) == 1
     assert fwd(shape(), distance_bias=at, max_distance=0) == 1 and fwd(shape(), distance_bias=at, max_distance=4097) == 1
     assert fwd(shape(causal=0), prefix_lens=at) == 1

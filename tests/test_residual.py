@@ -372,6 +372,18 @@ def test_gradients_through_autograd():
             assert (xs.grad == 1).all()
     y0 = fb.fewbit_dropout(x, 0.0, seed=0)
     assert torch.equal(y0, x)
+    # without residual and dropout h is x itself: both ways back to it, and an in-place change of it before the backward pass is seen
+    xs = new((5, 40), torch.float32, 6).requires_grad_()
+    y, h = fb.fewbit_add_rms_norm(xs, None, None)
+    (y.sum() + 3 * h.sum()).backward()
+    wide = xs.detach().double().requires_grad_()
+    (norm_reference(wide, None, None, 1e-6, 0.0, torch.ones(5, 40, dtype=torch.bool, device="cuda"))[1].sum() + 3 * wide.sum()).backward()
+    assert ((xs.grad.double() - wide.grad).abs() <= 2.0 ** -14).all()
+    y, _ = fb.fewbit_add_rms_norm(xs, None, None)
+    with torch.no_grad():
+        xs.add_(1)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.sum().backward()
 
 
 @pytest.mark.gpu
