@@ -4,6 +4,7 @@
 
 #include <cudaTypedefs.h>
 
+#include <algorithm>
 #include <atomic>
 
 namespace fewbit {
@@ -159,6 +160,24 @@ int choose_split(int64_t sms, int64_t tiles, int64_t longest, bool causal, int m
     }
     return choice;
 }
+// The forward pass of scores that are shaped: a tile takes longer, beside which a CTA's ends weigh less (heads up to 64: 2 tiles, 3 with a
+// cluster's sums; wider: 3 and 5), and CTAs that do not all run at once take two rounds at least.  Measured, in us, with the rule above and with this one, a bias table: 2 x
+// 1000 rows, 6 heads of 64, 33.6 and 24.6; 4 x 300 rows on 600 keys, 4 heads, 25.8 and 21.4; 2 x 333 on 517, 8 heads, 23.4 and 20.4; one of 4096
+// rows, 4 heads, 47.1, and of 2048, 8 heads of 128, 36.9 with both; capped the same.  (The backward kernels gain 2 us or nothing.)
+int choose_scores_split(int64_t sms, int64_t tiles, int64_t longest, bool causal, bool wide, int most) {
+    double best = 0.0;
+    int choice = 0;
+    for (int split = 1; split <= most && (split == 1 || split <= longest); split *= 2) {
+        const double ctas = static_cast<double>(tiles * split), ends = split == 1 ? (wide ? 3.0 : 2.0) : wide ? 5.0 : 3.0;
+        const double rounds = ctas <= sms ? 1.0 : std::max(2.0, ctas / sms), mean = static_cast<double>(longest) / split / (causal ? 2 : 1);
+        const double cost = std::max(static_cast<double>((longest + split - 1) / split) + ends, rounds * (mean + ends));
+        if (choice == 0 || cost < best) {
+            best = cost;
+            choice = split;
+        }
+    }
+    return choice;
+}
 
 bool shaped(const fewbit_attention_scores *c) { return c != nullptr && (c->cap > 0 || c->slopes || c->distance_bias || c->prefix_lens || c->q_documents); }
 
@@ -257,7 +276,9 @@ fewbit_status forward(const fewbit_attention_shape *s, const fewbit_attention_sc
     p.lse = lse;
     fill_scores(s, scores, &p);
     const int64_t row_tiles = (s->q_len + 2 * attn::kTile - 1) / (2 * attn::kTile), key_tiles = (s->k_len + attn::kTile - 1) / attn::kTile;
-    p.split = choose_split(p.sms, row_tiles * s->heads * s->batch, key_tiles, p.causal, s->head_dim > 64 ? 8 : 4, kForwardEnds);
+    const int64_t tiles = row_tiles * s->heads * s->batch;
+    const int most = s->head_dim > 64 ? 8 : 4;
+    p.split = shaped(scores) ? choose_scores_split(p.sms, tiles, key_tiles, p.causal, s->head_dim > 64, most) : choose_split(p.sms, tiles, key_tiles, p.causal, most, kForwardEnds);
     return run(attn::Kernel::forward, s, shaped(scores), p, row_tiles, s->heads, stream);
 }
 
