@@ -415,7 +415,7 @@ FEWBIT_API fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *shap
  *                   contiguous, or (q_rows) and (k_rows) for packed sequences;
  *                   both or neither.  Any numbers; where they do not fall along a
  *                   sequence, tiles that no document of theirs shares are skipped.
- * Buffers are 4-byte aligned.  What is said about rows that see nothing and about
+ * The struct is HOST memory, read during the call only; buffers are 4-byte aligned.  What is said about rows that see nothing and about
  * non-finite values in fewbit_attention_shape holds for every key that a mask hides.
  */
 #define FEWBIT_MAX_DISTANCE 4096
