@@ -497,7 +497,8 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
             auto prepare = [&](int c) {
                 if constexpr (early) {
                     uint32_t none[16];
-                    const bool finite = shape_scores<MODE, false>(p.scores, mods, p.scale_log2, key_tile(j) * kTile + 64 * half + 32 * c - i - (w.k_len - w.q_len), s, none);
+                    bool steep;
+                    const bool finite = shape_scores<MODE, false, false>(p.scores, mods, p.scale_log2, key_tile(j) * kTile + 64 * half + 32 * c - i - (w.k_len - w.q_len), s, none, steep);
                     exact = exact || !finite;
                     if (!open) hide(c);
                     if (c == 0) {
@@ -879,7 +880,9 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             [[maybe_unused]] const int key_document = next_document;
             if (j + 1 < n) next_document = document_of(j + 1);
             uint32_t s[32], d[32], out[16];
-            uint32_t bent[16];                                        // MODE 1, capped: 1 - t^2
+            uint32_t bent[16];                                        // capped: 1 - t^2
+            constexpr bool kFine = std::is_same_v<T, __half>;
+            [[maybe_unused]] bool steep = false;
             float prob[32];
             tmem_ld32(s_at, s);
             wait_ld(s);
@@ -888,7 +891,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             uint32_t word = 0xffffffffu;
             auto sees = [&](int c) { return MODE > 0 ? (word >> c & 1) != 0 : c < limit; };
             if constexpr (MODE > 0) {
-                if (shaped) shape_scores<MODE, true>(p.scores, mods, p.scale_log2, key_tile(j) * kTile + 32 * part - i - (w.k_len - w.q_len), s, bent);
+                if (shaped) shape_scores<MODE, true, kFine>(p.scores, mods, p.scale_log2, key_tile(j) * kTile + 32 * part - i - (w.k_len - w.q_len), s, bent, steep);
                 if (edge) word = low_bits(limit);
                 if (mods.k_docs != nullptr) {
                     if (!(one_document && __all_sync(0xffffffffu, key_document == document))) word &= same_document(document, key_document);
@@ -946,13 +949,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
                 drift += sum[0] + sum[1];
             }
             if constexpr (MODE > 0) {
-                if (p.scores.capped) {
-#pragma unroll
-                    for (int c = 0; c < 16; ++c) {
-                        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&bent[c]));
-                        mul2(ds[2 * c], ds[2 * c + 1], ds[2 * c], ds[2 * c + 1], f.x, f.y);
-                    }
-                }
+                if (p.scores.capped) times_bent<kFine>(bent, steep, ds);
             }
 #pragma unroll
             for (int c = 0; c < 16; ++c) out[c] = pack2<T>(ds[2 * c], ds[2 * c + 1]);
@@ -1318,13 +1315,15 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             if (lane == 0) barrier_arrive(bar(kSRead));
             // rows past the end and rows that see nothing have -lse = -inf: their probabilities are 0
             [[maybe_unused]] uint32_t bent[16];                       // MODE > 0, capped: 1 - t^2
+            [[maybe_unused]] constexpr bool kFine = std::is_same_v<T, __half> && MODE < 3;   // (MODE 3 takes them pair by pair)
+            [[maybe_unused]] bool steep = false;
             [[maybe_unused]] const int away = key - q0 - 32 * part - 2 * (lane % 4) - reach;   // distance of the first key and row
             [[maybe_unused]] const int least = k0 + 32 * (warp & 3) - q0 - 32 * part - reach - 31;   // of the warp's last row and first key
             float unit = p.scale_log2;
             [[maybe_unused]] bool open = true;                        // the whole warp sees all its keys
             if constexpr (MODE > 0) {
                 if (MODE > 1 || p.scores.capped) {
-                    shape_transposed<MODE>(p.scores, mods, p.scale_log2, away, least, s, bent);
+                    shape_transposed<MODE, kFine>(p.scores, mods, p.scale_log2, away, least, s, bent, steep);
                     unit = 1.0f;
                 }
                 uint32_t word = 0xffffffffu;                          // a bit for each value, in their order
@@ -1395,13 +1394,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
 #pragma unroll
             for (int c = 0; c < 16; ++c) out[c] = pack2<T>(prob[2 * c], prob[2 * c + 1]);
             if constexpr (MODE == 1 || MODE == 2) {                    // from here on only dS of the products is wanted
-                if (p.scores.capped) {
-#pragma unroll
-                    for (int c = 0; c < 16; ++c) {
-                        const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&bent[c]));
-                        mul2(prob[2 * c], prob[2 * c + 1], prob[2 * c], prob[2 * c + 1], f.x, f.y);
-                    }
-                }
+                if (p.scores.capped) times_bent<kFine>(bent, steep, prob);
             }
             ok = j == 0 || wait(kDsUsed, (j - 1) & 1);
             if (!ok) break;

@@ -81,9 +81,10 @@ __device__ __forceinline__ float largest(const uint32_t (&s)[32]) {   // magnitu
     for (int e = 0; e < 32; e += 2) high[e / 2 % 2] = abs_max3(high[e / 2 % 2], __uint_as_float(s[e]), __uint_as_float(s[e + 1]));
     return fmaxf(high[0], high[1]);
 }
-// 32 products to capped scores plus `add`, with the shortest form that the warp's largest product (`high`) allows.
+// 32 products to capped scores plus `add`, with the shortest form that the warp's largest product (`high`) allows.  Returns whether
+// one of the warp's may lie past the cap.
 template <int MODE, bool ADD>
-__device__ __forceinline__ void bend(const Scores &sc, float high, uint32_t (&s)[32], float add) {
+__device__ __forceinline__ bool bend(const Scores &sc, float high, uint32_t (&s)[32], float add) {
     auto odd = [&](auto degree, const float *c) {                     // s Q(s^2)
         constexpr int N = decltype(degree)::value;
 #pragma unroll
@@ -102,22 +103,72 @@ __device__ __forceinline__ void bend(const Scores &sc, float high, uint32_t (&s)
     };
     if (MODE == 1 && !__any_sync(0xffffffffu, high > sc.near_limit)) {   // (with biases, a rare pair, the code's size counts for more)
         odd(std::integral_constant<int, 2>{}, sc.near_odd);
+        return false;
     } else if (!__any_sync(0xffffffffu, high > sc.odd_limit)) {
         odd(std::integral_constant<int, 5>{}, sc.odd);
+        return false;
     } else {
 #pragma unroll
         for (int e = 0; e < 32; ++e) {
             const float t = tanh_any(__uint_as_float(s[e]) * sc.cap_in);
             s[e] = __float_as_uint(ADD ? fmaf(t, sc.cap_out, add) : t * sc.cap_out);
         }
+        return true;
     }
 }
-// 1 - t^2 of two capped scores, as binary16: 2^-12 of it, less than dS's own rounding, for half the registers
-__device__ __forceinline__ uint32_t bent_slope(float cap_out_2, uint32_t z0, uint32_t z1) {
-    float a, b;
-    mul2(a, b, __uint_as_float(z0), __uint_as_float(z1), __uint_as_float(z0), __uint_as_float(z1));
-    fma2(a, b, a, b, -cap_out_2, -cap_out_2, 1.0f, 1.0f);
-    return pack2<__half>(a, b);
+// 1 - t^2 of 32 capped scores in 16 bits each, for half the registers.  As binary16 it is off by up to 2^-11, an eighth of what dS
+// loses when it is rounded to bfloat16, but as much as dS loses as binary16.  There (FINE) it is kept, up to the cap, where 1 - t^2 is
+// above 0.4, in steps of 2^-15, off by 2^-16; past the cap (`steep`) with 3 bits for the exponent and 13 for the mantissa, off by
+// 2^-14 of it or 2^-20, less than t itself is.  Errors of dQ and dK against that of rounding the results alone, 1000 rows and keys:
+// 1.6 and 1.4 (a cap of 20), as without a cap, instead of 1.8 and 1.6; 1.4 and 1.4 (5) instead of 1.7 and 1.7.
+template <bool FINE>
+__device__ __forceinline__ void bent_slopes(float cap_out_2, bool steep, const uint32_t (&z)[32], uint32_t (&bent)[16]) {
+    auto slopes = [&](float one, auto pack) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            float a, b;
+            mul2(a, b, __uint_as_float(z[2 * e]), __uint_as_float(z[2 * e + 1]), __uint_as_float(z[2 * e]), __uint_as_float(z[2 * e + 1]));
+            fma2(a, b, a, b, -cap_out_2, -cap_out_2, one, one);
+            bent[e] = pack(a, b);
+        }
+    };
+    if (!FINE) {
+        slopes(1.0f, [](float a, float b) { return pack2<__half>(a, b); });
+    } else if (!steep) {                                              // (above 256 a number's last 16 bits count 2^-15)
+        slopes(257.0f, [](float a, float b) { return __byte_perm(__float_as_uint(a), __float_as_uint(b), 0x5410); });
+    } else {                                                          // (1 is 7 << 23 after the product)
+        slopes(1.0f, [](float a, float b) {
+            mul2(a, b, a, b, 0x1p-120f, 0x1p-120f);
+            return __byte_perm((__float_as_uint(a) + 0x200u) >> 10, (__float_as_uint(b) + 0x200u) >> 10, 0x5410);
+        });
+    }
+}
+// 32 values times them
+template <bool FINE>
+__device__ __forceinline__ void times_bent(const uint32_t (&bent)[16], bool steep, float (&x)[32]) {
+    auto times = [&](auto unpack) {
+#pragma unroll
+        for (int c = 0; c < 16; ++c) {
+            float a, b;
+            unpack(bent[c], a, b);
+            mul2(x[2 * c], x[2 * c + 1], x[2 * c], x[2 * c + 1], a, b);
+        }
+    };
+    if (!FINE) {
+        times([](uint32_t w, float &a, float &b) {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&w));
+            a = f.x;
+            b = f.y;
+        });
+    } else if (!steep) {
+        times([](uint32_t w, float &a, float &b) {
+            add2(a, b, __uint_as_float(__byte_perm(w, 0x43800000u, 0x7610)), __uint_as_float(__byte_perm(w, 0x43800000u, 0x7632)), -256.0f, -256.0f);
+        });
+    } else {
+        times([](uint32_t w, float &a, float &b) {
+            mul2(a, b, __uint_as_float((w & 0xffffu) << 10), __uint_as_float(w >> 16 << 10), 0x1p120f, 0x1p120f);
+        });
+    }
 }
 
 // Whether rows and keys of a warp's 32 x 32 piece (`least`: the distance of its last row and first key; the others are up to 62
@@ -163,17 +214,15 @@ __device__ __forceinline__ bool add_bias(const Scores &sc, const Mods &m, float 
 }
 
 // A thread's row and 32 neighbouring keys from `away` on (the distance of the first; lanes' rows are neighbours: away falls by
-// one with each lane).  s: products in, scores in units of ln 2 out (MODE 1: only with a cap).  GRADIENT: bent gets 1 - t^2 of each pair.
-template <int MODE, bool GRADIENT>
-__device__ __forceinline__ bool shape_scores(const Scores &sc, const Mods &m, float scale_log2, int away, uint32_t (&s)[32], uint32_t (&bent)[16]) {
+// one with each lane).  s: products in, scores in units of ln 2 out (MODE 1: only with a cap).  GRADIENT: bent gets 1 - t^2 of each pair
+// (steep: in which form, see bent_slopes).
+template <int MODE, bool GRADIENT, bool FINE>
+__device__ __forceinline__ bool shape_scores(const Scores &sc, const Mods &m, float scale_log2, int away, uint32_t (&s)[32], uint32_t (&bent)[16], bool &steep) {
     float factor = scale_log2;
     if (sc.capped) {
-        bend<MODE, false>(sc, largest(s), s, 0.0f);
+        steep = bend<MODE, false>(sc, largest(s), s, 0.0f);
         factor = 1.0f;
-        if constexpr (GRADIENT) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) bent[e] = bent_slope(sc.cap_out_2, s[2 * e], s[2 * e + 1]);
-        }
+        if constexpr (GRADIENT) bent_slopes<FINE>(sc.cap_out_2, steep, s, bent);
     }
     if constexpr (MODE == 1) return true;
     return add_bias(sc, m, factor, away, uniform(away) - 31, s, [](int x) { return x; },
@@ -181,14 +230,14 @@ __device__ __forceinline__ bool shape_scores(const Scores &sc, const Mods &m, fl
 }
 // The same for the transposed scores of the dK and dV kernel: s[16 (k / 2) + 4 c + 2 (k % 2) + e] is of key 8 k and row 8 c + e
 // from this thread's first ones on, which are `away` apart.
-template <int MODE>
-__device__ __forceinline__ void shape_transposed(const Scores &sc, const Mods &m, float scale_log2, int away, int least, uint32_t (&s)[32], uint32_t (&bent)[16]) {
+template <int MODE, bool FINE>
+__device__ __forceinline__ void shape_transposed(const Scores &sc, const Mods &m, float scale_log2, int away, int least, uint32_t (&s)[32], uint32_t (&bent)[16],
+                                                 bool &steep) {
     float factor = scale_log2;
     if (sc.capped) {
-        bend<MODE, false>(sc, largest(s), s, 0.0f);
+        steep = bend<MODE, false>(sc, largest(s), s, 0.0f);
         factor = 1.0f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) bent[e] = bent_slope(sc.cap_out_2, s[2 * e], s[2 * e + 1]);
+        bent_slopes<FINE>(sc.cap_out_2, steep, s, bent);
     }
     if constexpr (MODE == 1) return;
     // key minus row takes 14 values: 8 (k - c) - e

@@ -264,6 +264,24 @@ def test_large_products_reach_the_cap(cap):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("size", [1.0, 2.0])
+def test_a_cap_costs_no_further_rounding_in_binary16(size):
+    """dK has two roundings to 16 bits, dS's and its own, whose errors do not depend on one another: sqrt(2) times as far off, in the
+    root mean square, as its own alone.  1 - t^2 in steps of 2^-15 (rms 2^-16 / sqrt(3) of at least 0.4) or with 13 bits (rms below
+    2^-14 / sqrt(3)) brings that to at most 1.43, as binary16 (11 bits, near 1 an rms of 2^-12 / sqrt(3)) to 1.57 or more.  size 2:
+    scores past the cap."""
+    q, k, v, g = ta.make(2, 512, 512, 4, 4, 64, HALF, size=size)
+    out, lse = fb.fewbit_attention_fwd(q, k, v, cap=5.0)
+    _, dk, _ = fb.fewbit_attention_bwd(g, q, k, v, out, lse, cap=5.0)
+    error = alone = 0.0
+    for b in range(2):
+        exact = reference(*(x[b].double() for x in (q, k, v, g)), False, 0.125, cap=5.0)[0]["dk"].transpose(0, 1)
+        error += float((dk[b].double() - exact).square().sum())
+        alone += float((exact.to(HALF).double() - exact).square().sum())
+    assert error <= 1.5 ** 2 * alone, math.sqrt(error / alone)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("slopes", [False, True])
 @pytest.mark.parametrize("size", [-1.4, 0.4, 1.4])
 def test_one_large_product_at_every_place(size, slopes):
