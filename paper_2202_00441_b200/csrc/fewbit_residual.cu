@@ -554,7 +554,7 @@ add_norm_bwd_kernel(const NormParams p) {
             sums[1] = gh[0] + gh[1];
         }
         over_group<false>(sums, p.group, part[round & 1]);
-        const float s = rsqrtf(fmaf(sums[0], p.inv_width, p.eps));
+        const float s = live ? rsqrtf(fmaf(sums[0], p.inv_width, p.eps)) : 0.0f;   // (no row, and eps 0: infinite, and 0 times it the weights' sums)
         const float back = -sums[1] * p.inv_width * s * s;
         if constexpr (!AHEAD) load_weights<V, N, LEAD>(p, t, lead, wide, w);
 #pragma unroll
