@@ -6,6 +6,7 @@
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
+#include <limits>
 #include <optional>
 #include <variant>
 #include <vector>
@@ -208,6 +209,7 @@ fewbit_attention_scores scores_of(const Attention &a, const Tensor &q, const Ten
     if (cap) {
         if (!(*cap >= 0)) refuse("cap must not be negative");
         c.cap = static_cast<float>(*cap);
+        if (*cap > 0 && c.cap == 0) c.cap = std::numeric_limits<float>::min();   // (0 is no cap: the library refuses this one, as every cap below its range)
     }
     if (slopes) {
         if (!is(*slopes, at::kFloat) || slopes->dim() != 1 || slopes->size(0) != a.s.heads) refuse("slopes must be a contiguous float32 vector with a value for each head of q, on its device");
