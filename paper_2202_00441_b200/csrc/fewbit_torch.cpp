@@ -232,8 +232,10 @@ fewbit_attention_scores scores_of(const Attention &a, const Tensor &q, const Ten
         const int64_t lead = q.dim() - 2;                             // (batch, length) or (rows)
         if (!is(*q_documents, at::kInt) || !is(*k_documents, at::kInt) || q_documents->sizes() != q.sizes().slice(0, lead) || k_documents->sizes() != k.sizes().slice(0, lead))
             refuse("q_documents and k_documents must be contiguous int32 tensors with a value for each row of q and of k, on their device");
-        c.q_documents = q_documents->data_ptr<int32_t>();
-        c.k_documents = k_documents->data_ptr<int32_t>();
+        if (q_documents->numel() > 0 && k_documents->numel() > 0) {   // (an empty tensor's pointer is NULL; without rows or keys there is nothing to tell apart)
+            c.q_documents = q_documents->data_ptr<int32_t>();
+            c.k_documents = k_documents->data_ptr<int32_t>();
+        }
     }
     return c;
 }

@@ -21,3 +21,22 @@ def test_caps_outside_the_range_are_refused(cap):
         fb.fewbit_attention_fwd(q, k, v, cap=cap)
     with pytest.raises((fb.FewbitError, ValueError)):
         fb.fewbit_attention_bwd(g, q, k, v, q, torch.zeros(1, 1, 20, device="cuda"), cap=cap)
+
+
+@pytest.mark.parametrize("b,n,m", [(2, 5, 0), (2, 0, 5), (2, 0, 0), (0, 5, 5)])
+def test_documents_of_empty_sequences(b, n, m):
+    i32 = {"dtype": torch.int32, "device": "cuda"}
+    for mods in ({}, {"cap": 3.0, "distance_bias": torch.zeros(2, 7, device="cuda")}):
+        q, k, v, g = ta.make(b, n, m, 2, 1, 64, BF)
+        kw = {"q_documents": torch.zeros(b, n, **i32), "k_documents": torch.zeros(b, m, **i32), **mods}
+        out, lse = fb.fewbit_attention_fwd(q, k, v, **kw)
+        grads = fb.fewbit_attention_bwd(g, q, k, v, out, lse, **kw)
+        assert (out == 0).all() and (lse == -math.inf).all() and all((x == 0).all() for x in grads)
+    q, k, v, g = (x[0] for x in ta.make(1, n, m, 2, 1, 64, BF))
+    kw = {"q_documents": torch.zeros(n, **i32), "k_documents": torch.zeros(m, **i32), "q_offsets": torch.tensor([0, n], **i32),
+          "k_offsets": torch.tensor([0, m], **i32), "max_q_len": n, "max_k_len": m}
+    if n and m:
+        return
+    out, lse = fb.fewbit_attention_fwd(q, k, v, **kw)
+    grads = fb.fewbit_attention_bwd(g, q, k, v, out, lse, **kw)
+    assert (out == 0).all() and (lse == -math.inf).all() and all((x == 0).all() for x in grads)
