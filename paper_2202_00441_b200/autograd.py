@@ -254,8 +254,12 @@ class _AddRmsNormFunction(torch.autograd.Function):
     def backward(ctx, grad_y, grad_h):
         h, wide, seed = ctx.saved_tensors
         want_x, want_residual, want_weight = ctx.needs_input_grad[:3]
-        if grad_y is None:
-            grad_y = torch.zeros_like(h)
+        if grad_y is None:                    # the normed result is not used: what reaches h goes on, whatever its rows hold
+            grad_h = grad_h.contiguous()
+            dx = grad_h
+            if want_x and ctx.kw["p"] > 0.0:
+                dx = fewbit_dropout_bwd(grad_h, ctx.kw["p"], seed=ctx.seed if seed is None else seed, place=ctx.kw["place"])
+            return dx if want_x else None, grad_h if want_residual else None, None, None, None, None, None
         dx, dr, dw = fewbit_add_rms_norm_bwd(grad_y.contiguous(), None if grad_h is None else grad_h.contiguous(), h, wide,
                                              seed=ctx.seed if seed is None else seed, x_grad=want_x, residual_grad=want_residual,
                                              weight_grad=want_weight, **ctx.kw)

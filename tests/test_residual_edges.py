@@ -22,3 +22,25 @@ def test_weight_gradients_without_eps(rows, width, offset, dtype):
     want = s * (g - u * (g * u).mean(-1, keepdim=True))
     bound = tr.E[dtype] * want.abs() + tr.TINY[dtype] + 2.0 ** -17 * (s * g.abs() + s * u.abs() * (g * u).abs().mean(-1, keepdim=True))
     assert ((gx.double() - want).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("p", [0.0, 0.3])
+def test_a_gradient_that_reaches_the_stream_alone(p):
+    """Where the normed result is not used, the norm has no part in the gradient: rows whose norm is not finite do not touch it, and the
+    weight has none."""
+    x, r, g = (tr.new((6, 96), torch.float32, i) for i in range(3))
+    r[1] = float("inf")
+    r[2] = float("nan")
+    x[3] = r[3] = 0
+    x, r = x.requires_grad_(), r.requires_grad_()
+    w = torch.ones(96, device="cuda").requires_grad_()
+    before = fb.fewbit_launch_count()
+    _, h = fb.fewbit_add_rms_norm(x, r, w, eps=0.0, p=p, seed=8, place=3)
+    h.backward(g)
+    assert fb.fewbit_launch_count() - before == (2 if p else 1)
+    assert torch.equal(r.grad, g) and w.grad is None
+    assert torch.equal(x.grad, fb.fewbit_dropout_bwd(g, p, seed=8, place=3) if p else g)
+    seed = torch.tensor(8, device="cuda")
+    _, h = fb.fewbit_add_rms_norm(x, None, w, eps=0.0, p=p, seed=seed, place=3)
+    (gx,) = torch.autograd.grad(h, x, g)
+    assert torch.equal(gx, x.grad)
