@@ -40,3 +40,16 @@ def test_documents_of_empty_sequences(b, n, m):
     out, lse = fb.fewbit_attention_fwd(q, k, v, **kw)
     grads = fb.fewbit_attention_bwd(g, q, k, v, out, lse, **kw)
     assert (out == 0).all() and (lse == -math.inf).all() and all((x == 0).all() for x in grads)
+
+
+@pytest.mark.parametrize("both", [False, True])
+@pytest.mark.parametrize("buckets,most", [(625, 3394), (624, 3394), (1024, 4095), (7, 8), (64, 2048), (512, 4096)])
+def test_borders_of_buckets_that_almost_meet_a_distance(buckets, most, both):
+    """625 buckets to 3394: (1524 / 312)^313 falls short of (3394 / 312)^208 by 2e-13 of it, so 1524 belongs below the border."""
+    if both and buckets % 2:
+        buckets *= 2
+    if buckets > 1024:
+        return
+    table = torch.arange(buckets, device="cuda", dtype=torch.float32)[:, None]
+    bias = fb.fewbit_relative_bias_fwd(table, most, bidirectional=both)
+    assert torch.equal(bias[0].long(), ts.exact_buckets(buckets, most, both))
