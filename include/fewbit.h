@@ -410,6 +410,9 @@ FEWBIT_API fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *shap
  *   distance_bias   DEVICE, heads x (2 R + 1) binary32 values, R = max_distance,
  *                   1 .. FEWBIT_MAX_DISTANCE, or NULL.  -inf hides the key; so does a
  *                   finite value below -2.3e38 (the scores are held in units of ln 2).
+ *                   Scores are rounded to 32 bits: with a bias of -1e9 nothing else is left of
+ *                   one.  Rows whose lse is beyond +-710, by biases or slopes, take the
+ *                   backward pass much longer (some 15 times).
  *   prefix_lens     DEVICE, int32 for each sequence, or NULL; causal attention only
  *   q_documents, k_documents  DEVICE int32 (batch, q_len) and (batch, k_len),
  *                   contiguous, or (q_rows) and (k_rows) for packed sequences;

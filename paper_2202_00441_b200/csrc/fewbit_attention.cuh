@@ -218,6 +218,40 @@ __device__ __forceinline__ long long stat_of(const Params &p, const Work &w, int
                     : (static_cast<long long>(w.batch) * p.heads + head) * p.q_len + i;
 }
 
+// Biases can make a row's scores, and lse with them, so large that 32 bits of lse hold nothing of the sum's logarithm (all keys at
+// -1e9, say), or that its rounding would show in the probabilities: from 2^10 on, where three roundings of 2^-14 are.  Such a row is
+// `far`.  The backward kernels of MODE 2 and 3 take its exponents in two steps, first from a reference next to its largest score,
+// which is exact, then by the logarithm of the sum to that reference.  The dQ kernel finds both anew, key by key, and hands them on in the row's
+// statistics, [-reference, -logarithm] in place of [-lse, -delta]; the dK and dV kernel, which tells them by the size of the first, takes delta from
+// the outputs.  4 x 2048 rows, 16 heads on 4 of 128, causal, all of them far: 6.0 ms in place of 395 us (0.7 us a key and row tile; what would take a
+// wait's two seconds is 3 million keys).  What all others pay for the question: 0.6 to 4 % of the backward pass.
+constexpr float kFarLse = 1024.0f;
+__device__ __forceinline__ bool far_row(float minus_lse) { return minus_lse > kFarLse || (minus_lse < -kFarLse && minus_lse > -INFINITY); }   // (-inf: sees nothing)
+// An exponent of a far row: not above 0, whatever one step of the score's rounding is there.  (A NaN stays one.)
+__device__ __forceinline__ float far_exponent(float z, float minus_reference, float minus_log) {
+    const float x = (z + minus_reference) + minus_log;
+    return x > 0.0f ? 0.0f : x;
+}
+// Adds the products of eight elements of two heads.
+template <typename T>
+__device__ __forceinline__ float dot8(uint4 a, uint4 b, float sum) {
+    T x[8], y[8];
+    memcpy(x, &a, 16);
+    memcpy(y, &b, 16);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum = fmaf(load1(&x[e]), load1(&y[e]), sum);
+    return sum;
+}
+// A row's delta from the outputs alone.
+template <typename T>
+__device__ __forceinline__ float delta_of(const Params &p, const Work &w, int head, int i) {
+    const T *o = static_cast<const T *>(p.o.p) + row_of(w, p.o, head, i, w.q_first), *g = static_cast<const T *>(p.go.p) + row_of(w, p.go, head, i, w.q_first);
+    float sum = 0.0f;
+#pragma unroll 1
+    for (int c = 0; c < p.dim; c += 8) sum = dot8<T>(__ldg(reinterpret_cast<const uint4 *>(o + c)), __ldg(reinterpret_cast<const uint4 *>(g + c)), sum);
+    return sum;
+}
+
 __device__ __forceinline__ bool stopped(const Sync *sync) { return *reinterpret_cast<const volatile int *>(&sync->stop) != 0; }
 
 __device__ __forceinline__ uint32_t start_cta(Sync *sync, int barriers, const uint32_t *counts) {
@@ -688,6 +722,15 @@ enum { qQ = 0, qKFull = 1, qKEmpty = 4, qVFull = 7, qVEmpty = 9, qS = 11, qDp = 
 
 template <int DIM> constexpr int dq_smem() { return 7 * (DIM / 64) * static_cast<int>(kHalfTile) + static_cast<int>(sizeof(Sync)) + 5 * kTile * 4 + kDocPlace; }
 
+// A barrier of the element-wise warps, and whether x is true in any of their threads.
+__device__ __forceinline__ void work_barrier() { asm volatile("bar.sync 1, %0;" :: "n"(kWorkThreads) : "memory"); }
+__device__ __forceinline__ bool work_any(bool x) {
+    uint32_t any;
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %1, 0;\nbarrier.cta.red.or.pred q, 1, %2, p;\nselp.u32 %0, 1, 0, q;\n}"
+                 : "=r"(any) : "r"(static_cast<uint32_t>(x)), "n"(kWorkThreads) : "memory");
+    return any != 0;
+}
+
 template <typename T, int DIM, int MODE>
 __global__ void __launch_bounds__(kThreadsAttn, 1)
 attention_dq_kernel(const __grid_constant__ Params p) {
@@ -837,22 +880,19 @@ attention_dq_kernel(const __grid_constant__ Params p) {
             const int row = 8 * warp + kRows * x + lane / kLanes;
             float sum = 0.0f;
             if (n > 0 && !single && q0 + row < w.q_len) {
-                const uint4 g = tile_chunk(sm_g, row, lane % kLanes);
-                T a[8], b[8];
-                memcpy(a, &outputs[x], 16);
-                memcpy(b, &g, 16);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum = fmaf(load1(&a[e]), load1(&b[e]), sum);
+                sum = dot8<T>(outputs[x], tile_chunk(sm_g, row, lane % kLanes), sum);
             }
 #pragma unroll
             for (int m = kLanes / 2; m > 0; m >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, m);
             if (lane % kLanes == 0) row_delta[row] = sum;
         }
-        asm volatile("bar.sync 1, %0;" :: "n"(kWorkThreads) : "memory");   // the element-wise warps only
+        [[maybe_unused]] bool far = false;                            // MODE 2: one of the tile's rows is far
+        if constexpr (MODE > 1) far = work_any(far_row(minus_lse));
+        else work_barrier();
         float minus_delta = -row_delta[r], drift = 0.0f;
         auto over_parts = [&](float mine) {                           // a row's sum over its four threads
             row_sum[part * kTile + r] = mine;
-            asm volatile("bar.sync 1, %0;" :: "n"(kWorkThreads) : "memory");
+            work_barrier();
             return (row_sum[r] + row_sum[kTile + r]) + (row_sum[2 * kTile + r] + row_sum[3 * kTile + r]);
         };
         const int seen = seen_by(p, w, i, mods.prefix), tile_seen = seen_by(p, w, q0, mods.prefix);
@@ -866,110 +906,161 @@ attention_dq_kernel(const __grid_constant__ Params p) {
                 one_document = __all_sync(0xffffffffu, document == uniform(document));
             }
         }
+        if constexpr (MODE > 1) {
+            if (far) {                                                // what they need waits in the tile's statistics: registers are short
+                const bool mine = far_row(minus_lse);
+                float top = -INFINITY, sum = 0.0f, minus_reference = mine ? minus_lse : 0.0f, minus_log = mine ? 0.0f : minus_lse;
+                if (n > 0) ok = wait(qQ, 0) && ok;
+                const int end = mine && ok && n > 0 ? min(seen, (skipped + n_all) * kTile) : 0;
+                const T *keys = static_cast<const T *>(p.kin.p) + row_of(w, p.kin, kv_head, 0, w.k_first);
+#pragma unroll 1
+                for (int k = skipped * kTile + part; k < end; k += 4) {   // (in every CTA of a cluster)
+                    if (documents && __ldg(mods.k_docs + k) != document) continue;
+                    float s = 0.0f;
+#pragma unroll 4
+                    for (int c = 0; c < p.dim; c += 8) s = dot8<T>(tile_chunk(sm_q, r, c / 8), __ldg(reinterpret_cast<const uint4 *>(keys + k * p.kin.i + c)), s);
+                    const float z = shape_one(p.scores, mods, p.scale_log2, k - i - (w.k_len - w.q_len), s);
+                    if (z > top) {
+                        sum = fmaf(sum, exp2_fast(top - z), 1.0f);
+                        top = z;
+                    } else if (z > -INFINITY) {
+                        sum += exp2_fast(z - top);
+                    }
+                }
+                __syncwarp();
+                row_sum[part * kTile + r] = top;
+                work_barrier();
+                const float high = fmaxf(fmaxf(row_sum[r], row_sum[kTile + r]), fmaxf(row_sum[2 * kTile + r], row_sum[3 * kTile + r]));
+                work_barrier();
+                const float total = over_parts(top > -INFINITY ? sum * exp2_fast(top - high) : 0.0f);
+                if (total > 0.0f) {
+                    // (a reference is as large as its row is far, or the next kernel would not know it)
+                    minus_reference = fabsf(high) > kFarLse ? -high : copysignf(kFarLse * 1.001f, minus_lse);
+                    minus_log = -(log2f(total) + (high + minus_reference));
+                }
+                work_barrier();                                       // (the sums have been read)
+                float *const place = stat_block(p, w, w.head, w.tile) + r;   // (a row's threads, in all CTAs of a cluster, write the same)
+                if (n > 0) {
+                    place[0] = minus_reference;
+                    place[kTile] = minus_log;
+                }
+            }
+        }
         // of this lane's key in the next tile, which waits for memory while this one is worked on
         auto document_of = [&](int j) { return MODE > 0 && mods.k_docs != nullptr ? __ldg(mods.k_docs + min(key_tile(j) * kTile + 32 * part + lane, w.k_len - 1)) : 0; };
         [[maybe_unused]] int next_document = n > 0 ? document_of(0) : 0;
-        for (int j = 0; ok && j < n; ++j) {
-            const uint32_t s_at = tm_s + (j & 1) * kTile + 32 * part + my_lane;
-            ok = wait(qS + (j & 1), (j >> 1) & 1);
-            if (!ok) {
-                if (single) over_parts(0.0f);                         // the others wait there
-                break;
-            }
-            fence_after();
-            [[maybe_unused]] const int key_document = next_document;
-            if (j + 1 < n) next_document = document_of(j + 1);
-            uint32_t s[32], d[32], out[16];
-            uint32_t bent[16];                                        // capped: 1 - t^2
-            constexpr bool kFine = std::is_same_v<T, __half>;
-            [[maybe_unused]] bool steep = false;
-            float prob[32];
-            tmem_ld32(s_at, s);
-            wait_ld(s);
-            bool edge = (key_tile(j) + 1) * kTile > tile_seen;
-            const int limit = seen - key_tile(j) * kTile - 32 * part;           // places from here on the row does not see, whatever they hold
-            uint32_t word = 0xffffffffu;
-            auto sees = [&](int c) { return MODE > 0 ? (word >> c & 1) != 0 : c < limit; };
-            if constexpr (MODE > 0) {
-                if (shaped) shape_scores<MODE, true, kFine>(p.scores, mods, p.scale_log2, key_tile(j) * kTile + 32 * part - i - (w.k_len - w.q_len), s, bent, steep);
-                if (edge) word = low_bits(limit);
-                if (mods.k_docs != nullptr) {
-                    if (!(one_document && __all_sync(0xffffffffu, key_document == document))) word &= same_document(document, key_document);
-                    visible += __popc(word);
+        auto all_tiles = [&](auto far_tile) {                         // (far row tiles apart: a branch inside takes 2 % of the others' time)
+            for (int j = 0; ok && j < n; ++j) {
+                const uint32_t s_at = tm_s + (j & 1) * kTile + 32 * part + my_lane;
+                ok = wait(qS + (j & 1), (j >> 1) & 1);
+                if (!ok) {
+                    if (single) over_parts(0.0f);                         // the others wait there
+                    break;
                 }
-                edge = __any_sync(0xffffffffu, word != 0xffffffffu);
-            }
-            if (MODE > 0 || edge) {
-#pragma unroll
-                for (int c = 0; c < 32; c += 2)
-                    exp2_scaled<false>(prob[c], prob[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), unit, minus_lse, minus_lse);
-                if (MODE > 0 && edge) {                               // (what a document hides may be larger than the row's sum)
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) prob[c] = sees(c) ? prob[c] : 0.0f;
+                fence_after();
+                [[maybe_unused]] const int key_document = next_document;
+                if (j + 1 < n) next_document = document_of(j + 1);
+                uint32_t s[32], d[32], out[16];
+                uint32_t bent[16];                                        // capped: 1 - t^2
+                constexpr bool kFine = std::is_same_v<T, __half>;
+                [[maybe_unused]] bool steep = false;
+                float prob[32];
+                tmem_ld32(s_at, s);
+                wait_ld(s);
+                bool edge = (key_tile(j) + 1) * kTile > tile_seen;
+                const int limit = seen - key_tile(j) * kTile - 32 * part;           // places from here on the row does not see, whatever they hold
+                uint32_t word = 0xffffffffu;
+                auto sees = [&](int c) { return MODE > 0 ? (word >> c & 1) != 0 : c < limit; };
+                if constexpr (MODE > 0) {
+                    if (shaped) shape_scores<MODE, true, kFine>(p.scores, mods, p.scale_log2, key_tile(j) * kTile + 32 * part - i - (w.k_len - w.q_len), s, bent, steep);
+                    if (edge) word = low_bits(limit);
+                    if (mods.k_docs != nullptr) {
+                        if (!(one_document && __all_sync(0xffffffffu, key_document == document))) word &= same_document(document, key_document);
+                        visible += __popc(word);
+                    }
+                    edge = __any_sync(0xffffffffu, word != 0xffffffffu);
                 }
-            } else {
+                if (MODE > 0 || edge) {
+                    if constexpr (decltype(far_tile)::value) {
+                        const float *const place = stat_block(p, w, w.head, w.tile) + r;
+                        const float minus_reference = place[0], minus_log = place[kTile];
 #pragma unroll
-                for (int c = 0; c < 32; c += 2) {
-                    if (c % 8 == 6) exp2_scaled<true>(prob[c], prob[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), unit, minus_lse, minus_lse);
-                    else exp2_scaled<false>(prob[c], prob[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), unit, minus_lse, minus_lse);
+                        for (int c = 0; c < 32; ++c) prob[c] = exp2_fast(far_exponent(__uint_as_float(s[c]), minus_reference, minus_log));
+                    } else {
+#pragma unroll
+                        for (int c = 0; c < 32; c += 2)
+                            exp2_scaled<false>(prob[c], prob[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), unit, minus_lse, minus_lse);
+                    }
+                    if (MODE > 0 && edge) {                               // (what a document hides may be larger than the row's sum)
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) prob[c] = sees(c) ? prob[c] : 0.0f;
+                    }
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 32; c += 2) {
+                        if (c % 8 == 6) exp2_scaled<true>(prob[c], prob[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), unit, minus_lse, minus_lse);
+                        else exp2_scaled<false>(prob[c], prob[c + 1], __uint_as_float(s[c]), __uint_as_float(s[c + 1]), unit, minus_lse, minus_lse);
+                    }
                 }
-            }
-            ok = wait(qDp, j & 1);
-            if (!ok) {
-                if (single) over_parts(0.0f);
-                break;
-            }
-            fence_after();
-            tmem_ld32(tm_dp + 32 * part + my_lane, d);
-            wait_ld(d);
-            float ds[32];
-            if (single) {
-                float sum = 0.0f;
-#pragma unroll
-                for (int c = 0; c < 32; ++c) {
-                    ds[c] = sees(c) ? prob[c] * __uint_as_float(d[c]) : 0.0f;
-                    sum += ds[c];
+                ok = wait(qDp, j & 1);
+                if (!ok) {
+                    if (single) over_parts(0.0f);
+                    break;
                 }
-                minus_delta = -over_parts(sum);
+                fence_after();
+                tmem_ld32(tm_dp + 32 * part + my_lane, d);
+                wait_ld(d);
+                float ds[32];
+                if (single) {
+                    float sum = 0.0f;
 #pragma unroll
-                for (int c = 0; c < 32; ++c) ds[c] = sees(c) ? fmaf(prob[c], minus_delta, ds[c]) : 0.0f;
-            } else {
+                    for (int c = 0; c < 32; ++c) {
+                        ds[c] = sees(c) ? prob[c] * __uint_as_float(d[c]) : 0.0f;
+                        sum += ds[c];
+                    }
+                    minus_delta = -over_parts(sum);
 #pragma unroll
-                for (int c = 0; c < 32; c += 2) {
-                    add2(ds[c], ds[c + 1], __uint_as_float(d[c]), __uint_as_float(d[c + 1]), minus_delta, minus_delta);
-                    mul2(ds[c], ds[c + 1], ds[c], ds[c + 1], prob[c], prob[c + 1]);
+                    for (int c = 0; c < 32; ++c) ds[c] = sees(c) ? fmaf(prob[c], minus_delta, ds[c]) : 0.0f;
+                } else {
+#pragma unroll
+                    for (int c = 0; c < 32; c += 2) {
+                        add2(ds[c], ds[c + 1], __uint_as_float(d[c]), __uint_as_float(d[c + 1]), minus_delta, minus_delta);
+                        mul2(ds[c], ds[c + 1], ds[c], ds[c + 1], prob[c], prob[c + 1]);
+                    }
+                    if (edge) {
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) ds[c] = sees(c) ? ds[c] : 0.0f;
+                    }
+                    float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+                    for (int c = 0; c < 32; c += 2) add2(sum[0], sum[1], sum[0], sum[1], ds[c], ds[c + 1]);
+                    drift += sum[0] + sum[1];
                 }
-                if (edge) {
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) ds[c] = sees(c) ? ds[c] : 0.0f;
+                if constexpr (MODE > 0) {
+                    if (p.scores.capped) times_bent<kFine>(bent, steep, ds);
                 }
-                float sum[2] = {0.0f, 0.0f};
 #pragma unroll
-                for (int c = 0; c < 32; c += 2) add2(sum[0], sum[1], sum[0], sum[1], ds[c], ds[c + 1]);
-                drift += sum[0] + sum[1];
+                for (int c = 0; c < 16; ++c) out[c] = pack2<T>(ds[2 * c], ds[2 * c + 1]);
+                tmem_st16(s_at, out);                                     // over the first half of what this thread read
+                wait_st();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) barrier_arrive(bar(qDs));
             }
-            if constexpr (MODE > 0) {
-                if (p.scores.capped) times_bent<kFine>(bent, steep, ds);
-            }
-#pragma unroll
-            for (int c = 0; c < 16; ++c) out[c] = pack2<T>(ds[2 * c], ds[2 * c + 1]);
-            tmem_st16(s_at, out);                                     // over the first half of what this thread read
-            wait_st();
-            fence_before();
-            __syncwarp();
-            if (lane == 0) barrier_arrive(bar(qDs));
-        }
+        };
+        if (MODE > 1 && far) all_tiles(std::bool_constant<(MODE > 1)>{});
+        else all_tiles(std::false_type{});
         const float row_drift = single ? 0.0f : over_parts(drift);
         // A row of one key has P = 1 and dS = 0 whatever its score: what the recomputed P leaves of dS is rounding and nothing
         // else.  (Times 0: a NaN stays one.)
         bool one = seen == 1;
         if (documents) {                                              // as many as its four threads found, in all CTAs of the cluster
-            asm volatile("bar.sync 1, %0;" :: "n"(kWorkThreads) : "memory");   // (the sums above have been read)
+            work_barrier();                                           // (the sums above have been read)
             const float found = over_parts(static_cast<float>(visible));
             if (p.split == 1) {
                 one = found == 1.0f;
             } else {
-                asm volatile("bar.sync 1, %0;" :: "n"(kWorkThreads) : "memory");
+                work_barrier();
                 if (part == 0) row_sum[r] = found;
             }
         }
@@ -981,7 +1072,8 @@ attention_dq_kernel(const __grid_constant__ Params p) {
         T *row = static_cast<T *>(p.dq.p) + (live ? row_of(w, p.dq, w.head, i, w.q_first) : 0);
         // (a row past the sequence's end may hold anything: its probabilities are 0, and 0 is what they multiply)
         auto write_stat = [&](float off) {
-            if (part < 2) stat_block(p, w, w.head, w.tile)[part * kTile + r] = part == 0 ? minus_lse : live ? minus_delta - off : 0.0f;
+            if (part >= 2 || (MODE > 1 && far && n > 0 && far_row(minus_lse) && off == off)) return;   // (far rows' are there)
+            stat_block(p, w, w.head, w.tile)[part * kTile + r] = part == 0 ? minus_lse : live ? minus_delta - off : 0.0f;
         };
         if (p.split == 1) {
             write_stat(ok ? row_drift : NAN);
@@ -1301,7 +1393,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             const float2 *d2 = l2 + kTile / 2;
             ok = wait(kTFull + (j & 1), (j >> 1) & 1);
             if (!ok) break;
-            const float2 minus_lse[4] = {l2[0], l2[4], l2[8], l2[12]};
+            float2 minus_lse[4] = {l2[0], l2[4], l2[8], l2[12]};
             ok = wait(kS, j & 1);
             if (!ok) break;
             fence_after();
@@ -1319,8 +1411,9 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             [[maybe_unused]] bool steep = false;
             [[maybe_unused]] const int away = key - q0 - 32 * part - 2 * (lane % 4) - reach;   // distance of the first key and row
             [[maybe_unused]] const int least = k0 + 32 * (warp & 3) - q0 - 32 * part - reach - 31;   // of the warp's last row and first key
+            [[maybe_unused]] const bool far_lane = MODE > 1 && far_row(stat[(j & 1) * 2 * kTile + 32 * part + lane]);   // this lane's row of the warp's 32
             float unit = p.scale_log2;
-            [[maybe_unused]] bool open = true;                        // the whole warp sees all its keys
+            [[maybe_unused]] bool open = true;                        // the whole warp sees all its keys, and no row is far
             if constexpr (MODE > 0) {
                 if (MODE > 1 || p.scores.capped) {
                     shape_transposed<MODE, kFine>(p.scores, mods, p.scale_log2, away, least, s, bent, steep);
@@ -1356,10 +1449,24 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                         }
                     }
                 }
-                open = __all_sync(0xffffffffu, word == 0xffffffffu);
+                open = __all_sync(0xffffffffu, word == 0xffffffffu && !far_lane);
                 if (!open) {
 #pragma unroll
                     for (int x = 0; x < 32; ++x) s[x] = word >> x & 1 ? s[x] : 0xff800000u;
+                    if (MODE > 1 && __builtin_expect(__any_sync(0xffffffffu, far_lane), 0)) {
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const float2 l = minus_lse[c], log = d2[4 * c];
+                            const float log0 = far_row(l.x) ? log.x : 0.0f, log1 = far_row(l.y) ? log.y : 0.0f;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) {
+                                const int x = 16 * (k / 2) + 4 * c + 2 * (k % 2);
+                                s[x] = __float_as_uint(far_exponent(__uint_as_float(s[x]), l.x, log0));
+                                s[x + 1] = __float_as_uint(far_exponent(__uint_as_float(s[x + 1]), l.y, log1));
+                            }
+                            minus_lse[c] = make_float2(0.0f, 0.0f);
+                        }
+                    }
                 }
             }
             const bool diagonal = MODE == 0 && p.causal && k0 + kTile - 1 > q0 + reach;   // some rows do not see some keys
@@ -1414,6 +1521,14 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
             ok = wait(kDp, j & 1);
             if (!ok) break;
             fence_after();
+            if (MODE > 1 && __builtin_expect(!open && __any_sync(0xffffffffu, far_lane), 0)) {
+                // delta in the logarithm's place, once all warps have read that: their P has been used.  (The warps of a row write the same.)
+                ok = wait(kPUsed, j & 1);
+                if (!ok) break;
+                if (far_lane) stat[(j & 1) * 2 * kTile + kTile + 32 * part + lane] = -delta_of<T>(p, w, head, q0 + 32 * part + lane);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+            }
             [[maybe_unused]] float diagonals[7][2] = {};              // MODE 3: sums of dS by (key - row) / 8 and the row's parity
 #pragma unroll
             for (int h = 0; h < 2; ++h) {                             // 16 keys at a time

@@ -213,6 +213,20 @@ __device__ __forceinline__ bool add_bias(const Scores &sc, const Mods &m, float 
     return false;
 }
 
+// The score of one product at distance `away`, with the roundings of the forms above.
+__device__ __forceinline__ float shape_one(const Scores &sc, const Mods &m, float scale_log2, int away, float s) {
+    if (sc.capped) {
+        s = bend_one(sc, s);
+        scale_log2 = 1.0f;
+    }
+    if (sc.slopes != nullptr) {
+        s *= scale_log2;
+        if (m.slope != 0.0f) s = fmaf(m.slope, fabsf(static_cast<float>(away)), s);
+        scale_log2 = 1.0f;
+    }
+    return m.bias == nullptr ? s : fmaf(s, scale_log2, __ldg(m.bias + max(-sc.reach, min(sc.reach, away))) * 1.4426950408889634f);
+}
+
 // A thread's row and 32 neighbouring keys from `away` on (the distance of the first; lanes' rows are neighbours: away falls by
 // one with each lane).  s: products in, scores in units of ln 2 out (MODE 1: only with a cap).  GRADIENT: bent gets 1 - t^2 of each pair
 // (steep: in which form, see bent_slopes).

@@ -53,3 +53,81 @@ def test_borders_of_buckets_that_almost_meet_a_distance(buckets, most, both):
     table = torch.arange(buckets, device="cuda", dtype=torch.float32)[:, None]
     bias = fb.fewbit_relative_bias_fwd(table, most, bidirectional=both)
     assert torch.equal(bias[0].long(), ts.exact_buckets(buckets, most, both))
+
+
+LARGE = [-1e3, -1e4, -1e6, -1e9, -1e30, -2e38, 1e6, 1e30]
+
+
+@pytest.mark.parametrize("low", LARGE)
+@pytest.mark.parametrize("case", [(1, 150, 150, 2, 2, 64, False, BF, {}), (2, 300, 280, 4, 2, 128, True, HALF, {}), (1, 130, 1500, 2, 1, 128, False, BF, {}),
+                                  (1, 3, 2000, 4, 2, 64, True, HALF, {"prefix": 700}), (2, 200, 333, 2, 1, 96, False, HALF, {"docs": "sorted"}),
+                                  (1, 3000, 70, 2, 1, 64, False, BF, {}), (1, 700, 700, 2, 1, 128, True, BF, {"docs": "scattered", "cap": 5.0}), (1, 1, 1, 1, 1, 8, True, BF, {})],
+                         ids=lambda c: "x".join(map(str, c[:6])))
+def test_rows_whose_biases_are_all_large(case, low):
+    """Every key of the rows has the same large finite bias, and products are 0 (queries and keys in halves of the head that do not
+    meet), so that the scores are equal whatever 32 bits leave of them: the results are those of a bias of 0.  (lse: one rounding to 32 bits
+    of its own, and two of what it is computed from.)"""
+    b, n, m, h, hk, d, causal, dtype, spec = case
+    q, k, v, g = ta.make(b, n, m, h, hk, d, dtype)
+    q[..., : d // 2] = 0
+    k[..., d // 2:] = 0
+    mods = ts.make_mods(b, n, m, h, spec)
+    kw = {"causal": causal, **mods, "distance_bias": torch.full((h, 7), low, device="cuda")}
+    out, lse = fb.fewbit_attention_fwd(q, k, v, **kw)
+    grads = fb.fewbit_attention_bwd(g, q, k, v, out, lse, **kw)
+    assert fb.fewbit_attention_timeout_count() == 0
+    total = bound = 0
+    for i in range(b):
+        zero = {**ts.one(mods, i), "bias": torch.zeros(h, 7, device="cuda")}
+        r, tol = ts.reference(*(x[i].double() for x in (q, k, v, g)), causal, d ** -0.5, **zero)
+        fin = r["lse"] > -math.inf
+        assert torch.equal(lse[i] > -math.inf, fin)
+        want = r["lse"][fin] + low
+        assert ((lse[i].double()[fin] - want).abs() <= 2.0 ** -22 * want.abs() + r["lse_tol"]).all()
+        got = {"out": out[i], "dq": grads[0][i], "dk": grads[1][i], "dv": grads[2][i]}
+        for name, x in got.items():
+            limit = 1.05 * tol[name](ta.E[dtype], ta.TINY[dtype]).transpose(0, 1) + 1e-30
+            err = (x.double() - r[name].transpose(0, 1)).abs()
+            assert (err <= limit).all(), (name, float((err / limit).max()))
+        total, bound = total + r["db"], bound + r["db_tol"]
+    assert ((grads[3].double() - total).abs() <= bound + 1e-30).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, HALF], ids=str)
+@pytest.mark.parametrize("docs", [None, "sorted"])
+def test_rows_that_see_masked_keys_alone_beside_ordinary_ones(docs, dtype):
+    """-1e9 beyond a distance of 40: the first rows, which lie further than that from every key, have nothing else, the others as if it were
+    -inf.  A score of the first rows is what 32 bits leave of it, the bias alone: each of their keys has the same weight."""
+    n, m, reach = 500, 250, 40
+    q, k, v, g = ta.make(1, n, m, 2, 1, 64, dtype)
+    kw = {} if docs is None else dict(zip(("q_documents", "k_documents"), ts.documents(docs, 1, n, m, 5)))
+    bias = torch.randn(2, 2 * reach + 1, device="cuda")
+    bias[:, 0] = bias[:, -1] = -1e9
+    out, lse = fb.fewbit_attention_fwd(q, k, v, distance_bias=bias, **kw)
+    grads = fb.fewbit_attention_bwd(g, q, k, v, out, lse, distance_bias=bias, **kw)
+    # the same in two parts: rows with an ordinary key, by a table with -inf; the others, by products of 0
+    away = torch.arange(m, device="cuda")[None] - torch.arange(n, device="cuda")[:, None] - (m - n)
+    seen = torch.ones(n, m, dtype=torch.bool, device="cuda") if docs is None else kw["q_documents"][0][:, None] == kw["k_documents"][0][None]
+    near = ((away.abs() < reach) & seen).any(1)
+    assert near.any() and not near.all()
+    hidden = bias.clone()
+    hidden[:, 0] = hidden[:, -1] = -math.inf
+    mods = {} if docs is None else {"qd": kw["q_documents"][0], "kd": kw["k_documents"][0]}
+    args = [x[0].double() for x in (q, k, v, g)]
+    ra, ta_ = ts.reference(*args, False, 0.125, bias=hidden, **mods)
+    rb, tb_ = ts.reference(torch.zeros_like(args[0]), *args[1:], False, 0.125, bias=torch.zeros_like(bias), **mods)
+    e, t = ta.E[dtype], ta.TINY[dtype]
+    for name in ("out", "dq"):
+        got = (out if name == "out" else grads[0])[0].double().transpose(0, 1)
+        for r, tol, rows in ((ra, ta_, near), (rb, tb_, ~near)):
+            assert ((got - r[name]).abs()[:, rows] <= (1.05 * tol[name](e, t) + 1e-30)[:, rows]).all(), name
+    # dV, of which the second part's rows have P = 1 / n
+    zero = args[3].clone()
+    zero[~near] = 0
+    parts = [ts.reference(args[0], args[1], args[2], zero, False, 0.125, bias=hidden, **mods)]
+    zero = args[3].clone()
+    zero[near] = 0
+    parts.append(ts.reference(torch.zeros_like(args[0]), args[1], args[2], zero, False, 0.125, bias=torch.zeros_like(bias), **mods))
+    want = sum(r["dv"] for r, _ in parts)
+    limit = sum(tol["dv"](e, t) for _, tol in parts)
+    assert ((grads[2][0].double().transpose(0, 1) - want).abs() <= 1.05 * limit + 1e-30).all()
