@@ -406,7 +406,8 @@ FEWBIT_API fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *shap
  *     q_documents[i] == k_documents[j]     (where given)
  *
  *   cap             0: none; else 2^-60 .. 2^60
- *   slopes          DEVICE, a binary32 value for each query head, or NULL
+ *   slopes          DEVICE, a binary32 value for each query head, or NULL.  A score that
+ *                   they bring below -2.3e38 is held as that, or hides its key.
  *   distance_bias   DEVICE, heads x (2 R + 1) binary32 values, R = max_distance,
  *                   1 .. FEWBIT_MAX_DISTANCE, or NULL.  -inf hides the key; so does a
  *                   finite value below -2.3e38 (the scores are held in units of ln 2).

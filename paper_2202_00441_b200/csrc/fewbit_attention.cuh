@@ -130,7 +130,7 @@ __device__ __forceinline__ Mods find_mods(const Params &p, const Work &w, int he
             m.k_docs = sc.k_docs + (w.packed ? w.k_first : static_cast<long long>(w.batch) * p.k_len);
         }
         if (sc.bias != nullptr) m.bias = sc.bias + static_cast<long long>(head) * (2 * sc.reach + 1) + sc.reach;
-        if (sc.slopes != nullptr) m.slope = -uniform(sc.slopes[head]) * kLog2e;
+        if (sc.slopes != nullptr) m.slope = slope_of(uniform(sc.slopes[head]));
     }
     return m;
 }
@@ -1374,7 +1374,7 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                 if constexpr (MODE > 1) {
                     ++head;
                     if (p.scores.bias != nullptr) mods.bias += 2 * p.scores.reach + 1;
-                    if (p.scores.slopes != nullptr) mods.slope = -uniform(__ldg(p.scores.slopes + head)) * kLog2e;
+                    if (p.scores.slopes != nullptr) mods.slope = slope_of(uniform(__ldg(p.scores.slopes + head)));
                 }
             }
             const int q0 = (first + tile) * kTile;

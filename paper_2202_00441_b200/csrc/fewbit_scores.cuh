@@ -18,6 +18,7 @@
 // word of votes.  Tiles in front of the first and behind the last that shares a document with the CTA's own are skipped.
 #pragma once
 
+#include <cfloat>
 #include <climits>
 #include <type_traits>
 
@@ -59,6 +60,12 @@ struct Mods {
     const float *bias;                // the head's, at distance 0
     float slope;                      // -slope * log2(e)
 };
+
+// -slope * log2(e), finite (a level key's distance of 0 is multiplied by it).
+__device__ __forceinline__ float slope_of(float slope) {
+    const float m = -slope * 1.4426950408889634f;
+    return m < -FLT_MAX ? -FLT_MAX : m;
+}
 
 // Any a, relative error below 2^-19: 1 - 2 / (1 + e^2a) is off by 2^-21 at most, which small values do not bear (a cap far above
 // the scores multiplies it).
@@ -195,7 +202,8 @@ __device__ __forceinline__ bool add_bias(const Scores &sc, const Mods &m, float 
         }
         factor = 1.0f;
     }
-    if (m.bias == nullptr) return true;
+    const bool finite = m.slope > -1e29f;                             // (distances are below 2^31: no product with such a slope overflows)
+    if (m.bias == nullptr) return finite;
     const int far = beyond(least, sc.reach);
     if (far != 0) {
         const float b = __ldg(m.bias + (far < 0 ? -sc.reach : sc.reach)) * 1.4426950408889634f;
@@ -206,7 +214,7 @@ __device__ __forceinline__ bool add_bias(const Scores &sc, const Mods &m, float 
             s[x] = __float_as_uint(v0);
             s[x + 1] = __float_as_uint(v1);
         }
-        return b > -INFINITY;
+        return finite && b > -INFINITY;
     }
 #pragma unroll
     for (int x = 0; x < 32; ++x) s[x] = __float_as_uint(fmaf(__uint_as_float(s[x]), factor, look(x)));

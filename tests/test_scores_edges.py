@@ -131,3 +131,26 @@ def test_rows_that_see_masked_keys_alone_beside_ordinary_ones(docs, dtype):
     want = sum(r["dv"] for r, _ in parts)
     limit = sum(tol["dv"](e, t) for _, tol in parts)
     assert ((grads[2][0].double().transpose(0, 1) - want).abs() <= 1.05 * limit + 1e-30).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, HALF], ids=str)
+@pytest.mark.parametrize("table", [False, True])
+@pytest.mark.parametrize("slope,first", [(1e38, 3), (3e38, 2)])
+def test_slopes_whose_biases_overflow(slope, first, table, dtype):
+    """Scores below what 32 bits hold, from distance `first` on, hide their keys: rows that lie further from every key see nothing, the
+    others their nearest key alone (the next one's score is 1e38 lower), whose weight is 1 and whose score has no gradient."""
+    n, m = 400, 128
+    q, k, v, g = ta.make(1, n, m, 2, 1, 64, dtype)
+    mods = {"slopes": torch.tensor([0.5, slope], device="cuda")}
+    if table:
+        mods["distance_bias"] = torch.zeros(2, 7, device="cuda")
+    out, lse = fb.fewbit_attention_fwd(q, k, v, **mods)
+    grads = fb.fewbit_attention_bwd(g, q, k, v, out, lse, **mods)
+    assert all(torch.isfinite(x).all() for x in (out, *grads)) and torch.isfinite(lse[:, 0]).all()
+    none = n - m - first + 1                                 # row i is n - m - i away from the first key
+    assert (out[:, :none, 1] == 0).all() and (lse[:, 1, :none] == -math.inf).all() and (grads[0][:, :none, 1] == 0).all()
+    nearest = torch.arange(none, n, device="cuda") - (n - m)
+    assert torch.equal(out[:, none:, 1], v[:, nearest.clamp_min(0), 0]) and torch.isfinite(lse[:, 1, none:]).all()
+    # dS is P (dP - delta), with delta off by the rounding of out at most
+    size = (g[0, :, 1].double().abs() * out[0, :, 1].double().abs()).sum(-1, keepdim=True)
+    assert (grads[0][0, :, 1].double().abs()[none:] <= 1.05 * 0.125 * (ta.E[dtype] * size[none:]) * k[0, nearest.clamp_min(0), 0].double().abs() + ta.TINY[dtype]).all()
