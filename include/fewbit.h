@@ -409,7 +409,7 @@ FEWBIT_API fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *shap
  *   slopes          DEVICE, a binary32 value for each query head, or NULL.  A score that
  *                   they bring below -2.3e38 is held as that, or hides its key.
  *   distance_bias   DEVICE, heads x (2 R + 1) binary32 values, R = max_distance,
- *                   1 .. FEWBIT_MAX_DISTANCE, or NULL.  -inf hides the key; so does a
+ *                   1 .. FEWBIT_MAX_DISTANCE, or NULL; up to 65535 heads.  -inf hides the key; so does a
  *                   finite value below -2.3e38 (the scores are held in units of ln 2).
  *                   Scores are rounded to 32 bits: with a bias of -1e9 nothing else is left of
  *                   one.  Rows whose lse is beyond +-710, by biases or slopes, take the
@@ -463,7 +463,7 @@ FEWBIT_API fewbit_status fewbit_attention_scores_bwd(const fewbit_attention_shap
  *   table           DEVICE, buckets x heads elements of `dtype`, contiguous
  *   buckets         2 .. 1024, bidirectional: even, from 4
  *   max_distance    R: larger than m, up to FEWBIT_MAX_DISTANCE
- * Errors: INVALID_ARG, TOO_LARGE (heads above 2^16), ALIGNMENT, CUDA.
+ * Errors: INVALID_ARG, TOO_LARGE (heads above 65535), ALIGNMENT, CUDA.
  */
 FEWBIT_API fewbit_status fewbit_relative_bias_fwd(const void *table, int buckets, int heads, int max_distance, int bidirectional,
                                                   fewbit_dtype dtype, float *distance_bias, void *stream);
