@@ -161,7 +161,7 @@ fewbit_status check_drop(const fewbit_dropout_options *o, Drop *d) {
     d->keys = random_keys(o->seed);
     d->place = o->place;
     d->limit = limit < 4294967295.0 ? static_cast<uint32_t>(limit) : 4294967295u;
-    d->scale = static_cast<float>(1.0 / (1.0 - o->p));
+    d->scale = limit > 4294967295.0 ? 0.0f : static_cast<float>(1.0 / (1.0 - o->p));   // (no word is that large: the largest one passes, and counts 0)
     d->on = o->p > 0.0;
     return FEWBIT_OK;
 }

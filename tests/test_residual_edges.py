@@ -44,3 +44,11 @@ def test_a_gradient_that_reaches_the_stream_alone(p):
     _, h = fb.fewbit_add_rms_norm(x, None, w, eps=0.0, p=p, seed=seed, place=3)
     (gx,) = torch.autograd.grad(h, x, g)
     assert torch.equal(gx, x.grad)
+
+
+def test_probabilities_next_to_one():
+    """From 1 - 2^-33 on round(p 2^32) is above every word: nothing is kept, not even the largest, which element 1 has with this seed."""
+    seed, x = 454088803, torch.ones(64, device="cuda")
+    for p, kept in ((1 - 2.0 ** -32, 2.0 ** 32), (1 - 2.0 ** -40, 0.0), (1 - 2.0 ** -53, 0.0)):
+        for y in (fb.fewbit_dropout_fwd(x, p, seed=seed), fb.fewbit_dropout_bwd(x, p, seed=seed), fb.fewbit_add_rms_norm_fwd(x[None], p=p, seed=seed)[1][0]):
+            assert y[1] == kept and (y[:1] == 0).all() and (y[2:] == 0).all()
