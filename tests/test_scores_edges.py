@@ -154,3 +154,36 @@ def test_slopes_whose_biases_overflow(slope, first, table, dtype):
     # dS is P (dP - delta), with delta off by the rounding of out at most
     size = (g[0, :, 1].double().abs() * out[0, :, 1].double().abs()).sum(-1, keepdim=True)
     assert (grads[0][0, :, 1].double().abs()[none:] <= 1.05 * 0.125 * (ta.E[dtype] * size[none:]) * k[0, nearest.clamp_min(0), 0].double().abs() + ta.TINY[dtype]).all()
+
+
+@pytest.mark.parametrize("low", [-1e6, -1e9, 1e30])
+@pytest.mark.parametrize("case", [([0, 40, 40, 300, 301], [0, 40, 50, 310, 310], 4, 2, 64, True, BF), ([5, 140, 300], [3, 140, 900], 4, 1, 128, False, HALF),
+                                  ([0, 3, 5, 130, 258, 600], [0, 3, 4, 131, 259, 640], 2, 1, 96, True, HALF)], ids=lambda c: f"{len(c[0]) - 1}x{c[0][-1]}x{c[4]}")
+def test_packed_rows_whose_biases_are_all_large_in_every_other_head(case, low):
+    """As above; heads of one group take turns, and no row of another sequence is touched."""
+    qo, ko, h, hk, d, causal, dtype = case
+    b, extra = len(qo) - 1, 9
+    q, k, v, g = (x[0] for x in ta.make(1, qo[-1] + extra, ko[-1] + extra, h, hk, d, dtype))
+    q[..., : d // 2] = 0
+    k[..., d // 2:] = 0
+    bias = torch.zeros(h, 9, device="cuda")
+    bias[1::2] = low
+    offsets = [torch.tensor(o, dtype=torch.int32, device="cuda") for o in (qo, ko)]
+    kw = {"causal": causal, "q_offsets": offsets[0], "k_offsets": offsets[1], "max_q_len": max(y - x for x, y in zip(qo, qo[1:])),
+          "max_k_len": max(y - x for x, y in zip(ko, ko[1:])), "distance_bias": bias}
+    out, lse = fb.fewbit_attention_fwd(q, k, v, **kw)
+    grads = fb.fewbit_attention_bwd(g, q, k, v, out, lse, **kw)
+    total = bound = 0
+    for i in range(b):
+        rows, keys = slice(qo[i], qo[i + 1]), slice(ko[i], ko[i + 1])
+        r, tol = ts.reference(*(x.double() for x in (q[rows], k[keys], v[keys], g[rows])), causal, d ** -0.5, bias=torch.zeros_like(bias))
+        for name, x in (("out", out[rows]), ("dq", grads[0][rows]), ("dk", grads[1][keys]), ("dv", grads[2][keys])):
+            if x.numel():
+                limit = 1.05 * tol[name](ta.E[dtype], ta.TINY[dtype]).transpose(0, 1) + 1e-30
+                assert ((x.double() - r[name].transpose(0, 1)).abs() <= limit).all(), name
+        total, bound = total + r["db"], bound + r["db_tol"]
+    assert ((grads[3].double() - total).abs() <= bound + 1e-30).all()
+    for x, at in ((out, qo), (grads[0], qo), (grads[1], ko), (grads[2], ko)):
+        assert (x[:at[0]] == 0).all() and (x[at[-1]:] == 0).all()
+    again = fb.fewbit_attention_bwd(g, q, k, v, out, lse, **kw)
+    assert all(torch.equal(x, y) for x, y in zip(grads, again))
