@@ -364,6 +364,8 @@ FEWBIT_API fewbit_status fewbit_qk_norm_rope_bwd(const fewbit_qk_shape *shape, c
  * dimensions longer than 1).  Keys past the end of a sequence are not part of
  * any sum, whatever the memory there holds.  A non-finite value inside a
  * sequence's k or v can spread to rows that the causal mask hides it from.
+ * The backward pass recomputes a row's probabilities from its lse, whose rounding to
+ * 32 bits they feel: by about |lse| 2^-23 of themselves.  (Biased scores: see there.)
  */
 typedef struct fewbit_attention_shape {
     int batch, heads, kv_heads, head_dim;

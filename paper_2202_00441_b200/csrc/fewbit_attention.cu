@@ -138,7 +138,7 @@ fewbit_status fill(const fewbit_attention_shape *s, const Sizes &z, Params *p) {
 struct Ends { int alone, joined; };
 // dK, dV: 11000 and 20000 clocks against 2850 for a tile; the others have shorter ends and longer tiles by their chain of one
 // tile after another.  Measured, in us.  Backward pass with dK's and dV's clusters of 1 / 2 / 4: 4 x 2048 rows of 16 heads on 4
-// key heads, causal, 275 / 292 / 330; one of 16384 rows, 8 heads on 2, 1663 / 1608 / 1695.  Forward and backward pass with
+// key heads, causal, 254 / 277 / 335; one of 16384 rows, 8 heads on 2, 1519 / 1414 / 1586 (single passes).  Forward and backward pass with
 // one CTA for a row tile against the clusters chosen here: one row on 8192 keys, 8 heads on 2, 92.7 and 85.7 against 25.7 and
 // 35.4; 64 rows on 9000 keys, 4 heads, 102.9 and 99.0 against 27.3 and 41.2; 1024 rows, causal, 20.7 and 37.5 against 16.3 and
 // 35.1; 4096 rows, causal, 59.9 and 120 against 47.7 and 119; 2 x 2048 rows stay with one: 35.0, with two 36.2.

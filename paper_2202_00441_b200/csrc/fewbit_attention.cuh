@@ -714,7 +714,8 @@ attention_fwd_kernel(const __grid_constant__ Params p) {
 // Three products (1536 clocks) and 1024 of exponentials for each row and key tile, which loads 64 KB for the one row tile
 // that tensor and shared memory have room for: 37 bytes a clock into each SM are what L2 gives when all SMs ask, so the loads
 // take 1750 clocks and bound it.  Tensor pipe 42 % active on 4 x 2048 rows, 16 heads on 4, causal; the whole backward pass
-// takes 275 us there (0.62 PFLOP/s counting five products, 0.87 counting the seven that are computed), and 1.61 ms for
+// takes 275 us there back to back (0.62 PFLOP/s counting five products, 0.87 counting the seven that are computed; 254 us for single passes, which the power
+// limit does not slow down), and 1.61 ms (1.42) for
 // 16384 rows, 8 heads on 2 (0.85 and 1.18 PFLOP/s, the latter 84 % of what matrix products sustain at the power limit).
 // Barriers: q and g, k full/empty (3 stages: a tile is used twice, one iteration apart), v full/empty (2 stages), S full (2),
 // dP full, dS ready, dQ done.
@@ -1136,7 +1137,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
 // Four products (2048 clocks) and 1024 of exponentials for each row and key tile.  The key tile's K stays in tensor memory and
 // its V in shared memory, so that Q and dO have three stages each.  What is left between the products is the chain of one
 // tile: S, its exponentials, dP, dS, and their way through tensor memory, 2850 clocks with two tiles' products interleaved.
-// Tensor pipe 60 % active on 4 x 2048 rows, 16 heads on 4, causal, where it takes half of the pass's 275 us.
+// Tensor pipe 60 % active on 4 x 2048 rows, 16 heads on 4, causal, where it takes half of the pass.
 // Barriers: v, k in tensor memory, q full/empty (3 stages), g full/empty (3 stages), statistics full/empty (2 stages), S full
 // and read, dP full and read, P ready and used, dS ready and used, done.
 enum { kV = 0, kK = 1, kQFull = 2, kQEmpty = 5, kGFull = 8, kGEmpty = 11, kTFull = 14, kTEmpty = 16, kS = 18, kSRead = 19, kDp = 20, kDpRead = 21, kP = 22,

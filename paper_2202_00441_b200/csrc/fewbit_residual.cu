@@ -356,8 +356,8 @@ __device__ __forceinline__ void over_group(float (&v)[K], int group, float (*par
 }
 
 // Forward: a row for each group of threads, held in registers from its load to its results; one CTA's rows wait for memory while
-// another's sums go round.  Bound by memory: bfloat16, 16384 x 4096, 90 us without dropout (91 % of a copy's rate), 99 with it (83 %: the words
-// keep two thirds of the issue slots busy), 119 with 8-bit results; binary32 164 us (100 %).
+// another's sums go round.  Bound by memory: bfloat16, 16384 x 4096, single passes, 88 us without dropout (93 % of a copy's rate), 100 with it (81 %:
+// the words keep two thirds of the issue slots busy), 119 with 8-bit results; binary32 164 us (100 %).  Back to back the one with dropout takes 101 to 107 us.
 // Places that are not the row's hold 0 from the load on, so that only loads and stores ask.
 template <typename T, int V, bool LEAD, int N, bool CODES>
 __global__ void __launch_bounds__(kNormThreads)
@@ -451,8 +451,8 @@ add_norm_fwd_kernel(const NormParams p) {
 }
 
 // Backward: CTAs stay and take rows in turn, so that the weight's gradient is summed in registers.  bfloat16, 16384 x 4096: 97 us without
-// dropout (84 % of a copy's rate), 149 with it (69 %: instruction issue and the multipliers, as the words come on top of 30 other
-// instructions an element); binary32 177 us (92 %).  Two CTAs of 256 threads that hold the weights beat three that read them again for
+// dropout (84 % of a copy's rate), 149 with it (69 %: no unit is at its limit, issue 60 %, memory two thirds; the words come when a row's
+// loads have been used, and 16 warps an SM leave their chain uncovered); binary32 177 us (92 %).  Two CTAs of 256 threads that hold the weights beat three that read them again for
 // every row (95 and 134 us), and words drawn in front of the sums (149 and 159).
 // AHEAD: each thread copies its pieces of the next rows to places of its own in shared memory, `depth` - 1 rows ahead of their use
 // (pieces of 16 bytes), so that a few CTAs keep memory busy while their rows' sums go round.

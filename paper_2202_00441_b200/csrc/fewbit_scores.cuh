@@ -6,13 +6,13 @@
 // and backward, with t the tanh: dS = dZ (1 - t^2), dB[e] = sum of dZ over all pairs at distance e.
 //
 // tanh: an odd polynomial of the product, scale and cap folded into its coefficients: of degree 5 where no product of a warp's 32 x 32
-// piece passes 0.3 caps (relative error 1.1e-6), of degree 11 up to the cap itself (6e-7), both found by Lawson's reweighted least
+// piece passes 0.3 caps (relative error 1.2e-6), of degree 11 up to the cap itself (6.1e-7), both found by Lawson's reweighted least
 // squares; two results of the exponential unit otherwise.  FMA and exponential pipe are what bounds the capped kernels: the
 // polynomials take 4 and 7 multiplications an element.  (tanh.approx.f32 has 11 bits: with a cap of 50 a score would be off by 0.02.)
 // Bias: a warp works on 32 rows x 32 keys; where all of them lie further apart than the table reaches, the bias is one number,
 // else each element's is read, 32 neighbouring ones at a time.
-// Measured, bfloat16, 4 x 2048 rows, 16 heads on 4 of 128, causal, forward and backward: plain scores 90 and 254 us, cap 50 119 and 350, slopes
-// 129 and 335, a table of 128 distances 126 and 355 (395 with its gradient).  What a tile costs more is the chain of one warp's
+// Measured, bfloat16, 4 x 2048 rows, 16 heads on 4 of 128, causal, forward and backward, single passes: plain scores 90 and 254 us, cap 50 121 and
+// 355, slopes 127 and 342, a table of 128 distances 123 and 347 (396 with its gradient).  What a tile costs more is the chain of one warp's
 // instructions: the tensor cores wait for it half of the time.
 // Documents: a lane holds the document of one key, and each document among a warp's 32 keys (mostly one or two) becomes one
 // word of votes.  Tiles in front of the first and behind the last that shares a document with the CTA's own are skipped.
