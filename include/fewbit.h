@@ -414,7 +414,7 @@ FEWBIT_API fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *shap
  *                   1 .. FEWBIT_MAX_DISTANCE, or NULL; up to 65535 heads.  -inf hides the key; so does a
  *                   finite value below -2.3e38 (the scores are held in units of ln 2).
  *                   Scores are rounded to 32 bits: with a bias of -1e9 nothing else is left of
- *                   one.  Rows whose lse is beyond +-710, by biases or slopes, take the
+ *                   one.  Rows whose lse is beyond +-2839, by biases or slopes, take the
  *                   backward pass much longer (some 15 times).
  *   prefix_lens     DEVICE, int32 for each sequence, or NULL; causal attention only
  *   q_documents, k_documents  DEVICE int32 (batch, q_len) and (batch, k_len),
@@ -441,7 +441,7 @@ FEWBIT_API fewbit_status fewbit_attention_scores_fwd(const fewbit_attention_shap
 /*
  * Bytes of `workspace` for the backward pass; 0 for a bad shape.  bias_gradient: with the gradient of distance_bias, which
  * takes 4 KB for each pair of a row tile and a key tile (128 x 128) within max_distance of each other, and each head
- * (4 or so such pairs for a key tile with a max_distance of 128).
+ * (4 or so such pairs for a key tile with a max_distance of 128), and 512 bytes for each row tile and head.
  */
 FEWBIT_API size_t fewbit_attention_scores_workspace_bytes(const fewbit_attention_shape *shape, const fewbit_attention_scores *scores, int bias_gradient);
 

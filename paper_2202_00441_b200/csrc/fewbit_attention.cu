@@ -226,9 +226,14 @@ void fill_scores(const fewbit_attention_shape *s, const fewbit_attention_scores 
     to.k_docs = c->k_documents;
 }
 
+size_t stat_bytes(const fewbit_attention_shape *s, const Sizes &z) {
+    const size_t tiles = z.packed ? static_cast<size_t>(z.q_rows / attn::kTile + s->batch + 1) : static_cast<size_t>((s->q_len + attn::kTile - 1) / attn::kTile) * s->batch;
+    return tiles * s->heads * attn::kStatBytes;
+}
+
 // What the bias's gradient takes of the workspace, behind the rows' statistics.
 struct BiasSpace {
-    size_t near, far, written;        // bytes
+    size_t near, far, written, delta; // bytes
     int64_t places;                   // key tiles of a sequence, or of all packed ones
     int near_tiles;
 };
@@ -241,6 +246,7 @@ BiasSpace bias_space(const fewbit_attention_shape *s, const Sizes &z, int max_di
     b.near = places * b.near_tiles * attn::kNearFloats * 4;
     b.far = places * attn::kFarFloats * 4;
     b.written = places * sizeof(int4);
+    b.delta = stat_bytes(s, z) / 2;
     return b;
 }
 
@@ -282,11 +288,6 @@ fewbit_status forward(const fewbit_attention_shape *s, const fewbit_attention_sc
     return run(attn::Kernel::forward, s, shaped(scores), p, row_tiles, s->heads, stream);
 }
 
-size_t stat_bytes(const fewbit_attention_shape *s, const Sizes &z) {
-    const size_t tiles = z.packed ? static_cast<size_t>(z.q_rows / attn::kTile + s->batch + 1) : static_cast<size_t>((s->q_len + attn::kTile - 1) / attn::kTile) * s->batch;
-    return tiles * s->heads * attn::kStatBytes;
-}
-
 fewbit_status backward(const fewbit_attention_shape *s, const fewbit_attention_scores *scores, const fewbit_heads *grad_out, const fewbit_heads *q,
                        const fewbit_heads *k, const fewbit_heads *v, const fewbit_heads *out, const float *lse, const fewbit_heads *grad_q,
                        const fewbit_heads *grad_k, const fewbit_heads *grad_v, float *grad_bias, void *workspace, size_t workspace_bytes, void *stream) {
@@ -311,7 +312,7 @@ fewbit_status backward(const fewbit_attention_shape *s, const fewbit_attention_s
     const size_t stats = stat_bytes(s, z);
     BiasSpace b = {};
     if (grad_bias != nullptr) b = bias_space(s, z, scores->max_distance);
-    if (workspace_bytes < stats + b.near + b.far + b.written) return FEWBIT_ERR_ALLOC;
+    if (workspace_bytes < stats + b.near + b.far + b.written + b.delta) return FEWBIT_ERR_ALLOC;
     Params p = {};
     fewbit_status st = fill(s, z, &p);
     if (st == FEWBIT_OK && some) st = encode(&p.q, q, s, z.q_rows, s->heads, z.batch);
@@ -334,6 +335,7 @@ fewbit_status backward(const fewbit_attention_shape *s, const fewbit_attention_s
         p.scores.written = reinterpret_cast<int4 *>(at);
         p.scores.near = reinterpret_cast<float *>(at + b.written);
         p.scores.far = reinterpret_cast<float *>(at + b.written + b.near);
+        p.scores.far_delta = reinterpret_cast<float *>(at + b.written + b.near + b.far);
         p.scores.places = static_cast<int>(b.places);
         p.scores.near_tiles = b.near_tiles;
         // packed sequences leave some places out
@@ -375,7 +377,7 @@ size_t fewbit_attention_scores_workspace_bytes(const fewbit_attention_shape *s, 
     if (check_shape(s, &z) != FEWBIT_OK || check_scores(s, scores, z) != FEWBIT_OK) return 0;
     BiasSpace b = {};
     if (bias_gradient && scores != nullptr && scores->distance_bias != nullptr) b = bias_space(s, z, scores->max_distance);
-    return stat_bytes(s, z) + b.near + b.far + b.written;
+    return stat_bytes(s, z) + b.near + b.far + b.written + b.delta;
 }
 
 fewbit_status fewbit_attention_bwd(const fewbit_attention_shape *s, const fewbit_heads *grad_out, const fewbit_heads *q, const fewbit_heads *k,

@@ -219,14 +219,15 @@ __device__ __forceinline__ long long stat_of(const Params &p, const Work &w, int
 }
 
 // Biases can make a row's scores, and lse with them, so large that 32 bits of lse hold nothing of the sum's logarithm (all keys at
-// -1e9, say), or that its rounding would show in the probabilities: from 2^10 on, where three roundings of 2^-14 are.  Such a row is
-// `far`.  The backward kernels of MODE 2 and 3 take its exponents in two steps, first from a reference next to its largest score,
-// which is exact, then by the logarithm of the sum to that reference.  The dQ kernel finds both anew, key by key, and hands them on in the row's
-// statistics, [-reference, -logarithm] in place of [-lse, -delta]; the dK and dV kernel, which tells them by the size of the first, takes delta from
-// the outputs.  4 x 2048 rows, 16 heads on 4 of 128, causal, all of them far: 6.0 ms in place of 395 us (0.7 us a key and row tile; what would take a
-// wait's two seconds is 3 million keys).  What all others pay for the question: 0.6 to 4 % of the backward pass.
-constexpr float kFarLse = 1024.0f;
-__device__ __forceinline__ bool far_row(float minus_lse) { return minus_lse > kFarLse || (minus_lse < -kFarLse && minus_lse > -INFINITY); }   // (-inf: sees nothing)
+// -1e9, say), or that its rounding shows in the probabilities: from 2^12 on, where three roundings of 2^-13 are.  The backward kernels of MODE 2 and 3
+// take such a `far` row's exponents in two steps, first from a reference next to its largest score, which is exact, then by the logarithm of the sum to
+// that reference.  The dQ kernel finds both anew, key by key, and hands them on in the row's statistics, [-reference, -logarithm] in place of
+// [-lse, -delta]; the dK and dV kernel tells them by the size of the first.  Its delta is the dQ kernel's where the workspace has room for it, with a
+// bias's gradient; else it is taken from the outputs, without the correction by the row's own sum (binary16: dK's error is then twice that of
+// its own rounding).  4 x 2048 rows, 16 heads on 4 of 128, causal, all of them far: 6.0 ms in place of 395 us (0.7 us a key and row tile; what would take
+// a wait's two seconds is 3 million keys).  What all others pay for the question: 0.6 to 4 % of the backward pass.
+constexpr float kFar = 4096.0f;
+__device__ __forceinline__ bool far_row(float minus_lse) { return minus_lse > kFar || (minus_lse < -kFar && minus_lse > -INFINITY); }   // (-inf: sees nothing)
 // An exponent of a far row: not above 0, whatever one step of the score's rounding is there.  (A NaN stays one.)
 __device__ __forceinline__ float far_exponent(float z, float minus_reference, float minus_log) {
     const float x = (z + minus_reference) + minus_log;
@@ -936,7 +937,7 @@ attention_dq_kernel(const __grid_constant__ Params p) {
                 const float total = over_parts(top > -INFINITY ? sum * exp2_fast(top - high) : 0.0f);
                 if (total > 0.0f) {
                     // (a reference is as large as its row is far, or the next kernel would not know it)
-                    minus_reference = fabsf(high) > kFarLse ? -high : copysignf(kFarLse * 1.001f, minus_lse);
+                    minus_reference = fabsf(high) > kFar ? -high : copysignf(kFar * 1.001f, minus_lse);
                     minus_log = -(log2f(total) + (high + minus_reference));
                 }
                 work_barrier();                                       // (the sums have been read)
@@ -1073,8 +1074,13 @@ attention_dq_kernel(const __grid_constant__ Params p) {
         T *row = static_cast<T *>(p.dq.p) + (live ? row_of(w, p.dq, w.head, i, w.q_first) : 0);
         // (a row past the sequence's end may hold anything: its probabilities are 0, and 0 is what they multiply)
         auto write_stat = [&](float off) {
-            if (part >= 2 || (MODE > 1 && far && n > 0 && far_row(minus_lse) && off == off)) return;   // (far rows' are there)
-            stat_block(p, w, w.head, w.tile)[part * kTile + r] = part == 0 ? minus_lse : live ? minus_delta - off : 0.0f;
+            if (part >= 2) return;
+            float *const block = stat_block(p, w, w.head, w.tile);
+            if (MODE > 1 && far && n > 0 && far_row(minus_lse) && off == off) {   // (far rows' are there)
+                if (part == 1 && p.scores.far_delta != nullptr) p.scores.far_delta[(block - p.stat) / 2 + r] = minus_delta - off;
+                return;
+            }
+            block[part * kTile + r] = part == 0 ? minus_lse : live ? minus_delta - off : 0.0f;
         };
         if (p.split == 1) {
             write_stat(ok ? row_drift : NAN);
@@ -1526,7 +1532,11 @@ attention_dkv_kernel(const __grid_constant__ Params p) {
                 // delta in the logarithm's place, once all warps have read that: their P has been used.  (The warps of a row write the same.)
                 ok = wait(kPUsed, j & 1);
                 if (!ok) break;
-                if (far_lane) stat[(j & 1) * 2 * kTile + kTile + 32 * part + lane] = -delta_of<T>(p, w, head, q0 + 32 * part + lane);
+                if (far_lane) {
+                    const int row = 32 * part + lane;
+                    stat[(j & 1) * 2 * kTile + kTile + row] =
+                        MODE == 3 ? __ldcg(p.scores.far_delta + (stat_block(p, w, head, first + tile) - p.stat) / 2 + row) : -delta_of<T>(p, w, head, q0 + row);
+                }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
             }

@@ -39,6 +39,7 @@ struct Scores {
     const int *prefix, *q_docs, *k_docs;
     // the bias's gradient: sums by distance of each key tile's near row tiles, sums of the far ones, what was written
     float *near, *far;
+    float *far_delta;                 // -delta of each row (128 for a row tile) whose place in the statistics something else takes
     int4 *written;                    // row tiles [x, y), k_len - q_len, number of the key tile + 1 (0: none has this place)
     int places;                       // for key tiles, of a sequence and head, or of all packed sequences for a head
     int near_tiles;                   // places for near row tiles of one key tile

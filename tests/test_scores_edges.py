@@ -187,3 +187,48 @@ def test_packed_rows_whose_biases_are_all_large_in_every_other_head(case, low):
         assert (x[:at[0]] == 0).all() and (x[at[-1]:] == 0).all()
     again = fb.fewbit_attention_bwd(g, q, k, v, out, lse, **kw)
     assert all(torch.equal(x, y) for x, y in zip(grads, again))
+
+
+@pytest.mark.parametrize("low", [-1e4, -1e9, 1e30])
+@pytest.mark.parametrize("case", [(1, 150, 150, 2, 2, 64, False, BF, {}), (2, 300, 280, 4, 2, 128, True, HALF, {}), (1, 3000, 70, 2, 1, 64, False, HALF, {}),
+                                  (2, 200, 333, 2, 1, 96, False, HALF, {"docs": "sorted", "slopes": 0.0}), (1, 9, 900, 4, 1, 128, True, BF, {"cap": 5.0})],
+                         ids=lambda c: "x".join(map(str, c[:6])))
+def test_rows_whose_biases_are_all_large_without_the_biases_gradient(case, low):
+    """The same, and dQ and dV bit for bit, where the workspace has no room for the rows' delta."""
+    b, n, m, h, hk, d, causal, dtype, spec = case
+    q, k, v, g = ta.make(b, n, m, h, hk, d, dtype)
+    q[..., : d // 2] = 0
+    k[..., d // 2:] = 0
+    mods = ts.make_mods(b, n, m, h, spec)
+    kw = {"causal": causal, **mods, "distance_bias": torch.full((h, 7), low, device="cuda")}
+    out, lse = fb.fewbit_attention_fwd(q, k, v, **kw)
+    dq, dk, dv = fb.fewbit_attention_bwd(g, q, k, v, out, lse, bias_grad=False, **kw)
+    with_bias = fb.fewbit_attention_bwd(g, q, k, v, out, lse, **kw)
+    assert torch.equal(dq, with_bias[0]) and torch.equal(dv, with_bias[2])
+    for i in range(b):
+        r, tol = ts.reference(*(x[i].double() for x in (q, k, v, g)), causal, d ** -0.5, **{**ts.one(mods, i), "bias": torch.zeros(h, 7, device="cuda")})
+        limit = 1.05 * tol["dk"](ta.E[dtype], ta.TINY[dtype]).transpose(0, 1) + 1e-30
+        assert ((dk[i].double() - r["dk"].transpose(0, 1)).abs() <= limit).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, HALF], ids=str)
+@pytest.mark.parametrize("case", [(2, 1455, 3, 4, 1, 64, True, {"slopes": 3.0, "reach": 2000, "prefix": 2}), (1, 1700, 34, 4, 2, 8, False, {"slopes": 3.0, "reach": 1000, "cap": 3.0}),
+                                  (1, 2200, 300, 2, 1, 128, False, {"slopes": 2.5, "reach": 60})], ids=lambda c: "x".join(map(str, c[:6])))
+def test_gradients_of_biases_of_rows_far_from_every_key(case, dtype):
+    """Slopes that bring lse past -2839, from where on a row's probabilities are found anew, and the rows' sums of dS with it in the bias's gradient: within the bound that z's own rounding leaves
+    (2^-24 of its size, in units of ln 2), not delta's from rounded outputs."""
+    b, n, m, h, hk, d, causal, spec = case
+    q, k, v, g = ta.make(b, n, m, h, hk, d, dtype)
+    mods = ts.make_mods(b, n, m, h, spec)
+    kw = {"causal": causal, **mods}
+    out, lse = fb.fewbit_attention_fwd(q, k, v, **kw)
+    db = fb.fewbit_attention_bwd(g, q, k, v, out, lse, **kw)[3]
+    total = bound = 0
+    for i in range(b):
+        r, _ = ts.reference(*(x[i].double() for x in (q, k, v, g)), causal, d ** -0.5, **ts.one(mods, i))
+        size = float(r["lse"][r["lse"] > -math.inf].abs().max())
+        # (db_tol's x, with a cap, leaves the size out; without one it is 2^5 of what this takes)
+        x = 2.0 ** -18 * (1 + spec.get("cap", 0)) if "cap" in spec else 2.0 ** -19 * (1 + size)
+        total, bound = total + r["db"], bound + r["db_tol"] * (2.0 ** -15 + 2.0 ** -18 * 4 + 2.0 ** -23 * size) / (2.0 ** -15 + x)
+    assert float(lse[lse > -math.inf].min()) < -2839
+    assert ((db.double() - total).abs() <= bound + 1e-30).all()
